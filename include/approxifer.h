@@ -319,6 +319,141 @@ int approxifer_encode_host_static(const approxifer_params* params, int64_t G, in
                                   const float* hX, float* hXt, void* cuda_stream);
 
 /*
+ * ---- Operators of hosted models ----------------------------------------------------------------------------------
+ *
+ * A worker runs the hosted model f on its coded query (Section 3: Yt_i = f(Xt_i)).  Where f is a decoder over
+ * sequences, a coded query is a sequence of embeddings, and the worker's time goes into three operators: the
+ * projections, the norm and position rotation of queries and keys on their way into a paged cache, and the attention
+ * that reads that cache.  (The paper leaves f open; these operators have no counterpart in it.)  The rules at the top
+ * of this file hold: device pointers, strides in ELEMENTS, innermost dimension contiguous, work enqueued on
+ * `cuda_stream`, nothing allocated, no state kept, argument errors found on the host.  Each takes one HOST struct, read
+ * during the call.  bfloat16 elements are uint16_t bit patterns; sums, norms and softmax statistics are fp32.
+ */
+
+/* element types */
+#define APPROXIFER_TYPE_BF16 0
+#define APPROXIFER_TYPE_F32 1
+
+/* activations */
+#define APPROXIFER_ACT_NONE 0
+#define APPROXIFER_ACT_RELU 1
+#define APPROXIFER_ACT_GELU 2      /* x Phi(x), by erf */
+#define APPROXIFER_ACT_GELU_TANH 3 /* 0.5 x (1 + tanh(sqrt(2/pi) (x + 0.044715 x^3))) */
+#define APPROXIFER_ACT_SILU 4      /* x / (1 + e^-x) */
+
+/* status[t] of approxifer_qk_norm_rope */
+#define APPROXIFER_ST_POSITION 32u /* positions[t] lies outside the table: the token is neither turned nor cached, q_out[t] = 0 */
+#define APPROXIFER_ST_SLOT 64u     /* slots[t] lies beyond the cache: the token's key and value were not written */
+
+/*
+ * Matrix product with bias, activation and residual:
+ *     Y[m][n] = act( sum_k X[m][k] Wt[n][k] + bias[n] ) + R[m][n],
+ * rounded once, to out_type.  X, Wt and bias are bfloat16; R and Y are of out_type.  bias and R may be NULL; R may be Y
+ * itself (same stride).  Y must not overlap X, Wt or bias.  M = 0 is a valid no-op; 1 <= N, K <= 2^31 - 1.
+ * X and Wt with 16-byte aligned bases and row strides of whole 16 bytes run on the tensor cores; others run an
+ * element-wise kernel.
+ */
+typedef struct approxifer_linear_args {
+  int64_t M, N, K;
+  const uint16_t* X;    /* [M][K] */
+  int64_t x_rstride;
+  const uint16_t* Wt;   /* [N][K] */
+  int64_t w_rstride;
+  const uint16_t* bias; /* [N] or NULL */
+  const void* R;        /* [M][N] or NULL */
+  int64_t r_rstride;
+  void* Y;              /* [M][N] */
+  int64_t y_rstride;
+  int32_t activation;   /* APPROXIFER_ACT_* */
+  int32_t out_type;     /* APPROXIFER_TYPE_* of R and Y */
+} approxifer_linear_args;
+int approxifer_linear(const approxifer_linear_args* args, void* cuda_stream);
+
+/*
+ * Per-head norm of queries and keys with the position rotation, and the new tokens' keys and values written to the
+ * paged cache, in one pass.  For every token t and every head of q and k
+ *     x <- x / sqrt(mean_d x_d^2 + eps) * w_d                  (w = q_weight or k_weight; NULL: x stays as it is)
+ * and then, with c, s the cosine and sine of the token's position,
+ *     (x_a, x_b) <- (x_a c_i - x_b s_i,  x_b c_i + x_a s_i),   i = 0 .. rot/2 - 1,
+ * a = i, b = i + rot/2, or a = 2i, b = 2i+1 with `interleaved`; elements from rot on are not turned.  Each result is
+ * rounded once.  Values are copied.
+ *   cos_sin    [positions_max][rot] fp32: rot/2 cosines, then rot/2 sines, of every position
+ *   positions  [T], 0 <= positions[t] < positions_max (else ST_POSITION)
+ *   slots      [T] int64: where the token goes in the cache, page slots[t] / page_size, row slots[t] % page_size; a
+ *              negative slot is not written (padding), one beyond the cache is not written either (ST_SLOT).  No two
+ *              tokens of a call may have the same slot.
+ *   k_cache, v_cache  [num_pages][Hkv][page_size][D] by strides
+ *   status     [T] of APPROXIFER_ST_* bits, or NULL
+ * `type` is the type of q, k, v, the weights, q_out and the caches.  v with v_cache, or k with k_cache, may be NULL:
+ * that part is left out.  q_out may be q itself.  1 <= D <= 256, rot even, 0 <= rot <= D.
+ */
+typedef struct approxifer_norm_rope_args {
+  int64_t T;
+  int32_t Hq, Hkv, D, rot, interleaved, type;
+  const void* q;     /* [T][Hq][D] */
+  int64_t q_tstride, q_hstride;
+  const void* k;     /* [T][Hkv][D] or NULL */
+  int64_t k_tstride, k_hstride;
+  const void* v;     /* [T][Hkv][D] or NULL */
+  int64_t v_tstride, v_hstride;
+  const void* q_weight; /* [D] or NULL */
+  const void* k_weight; /* [D] or NULL */
+  const float* cos_sin;
+  int64_t positions_max;
+  const int32_t* positions;
+  void* q_out;       /* [T][Hq][D] */
+  int64_t qo_tstride, qo_hstride;
+  void* k_cache;
+  int64_t kc_pstride, kc_hstride, kc_rstride; /* between pages, heads, rows of a page */
+  void* v_cache;
+  int64_t vc_pstride, vc_hstride, vc_rstride;
+  int64_t num_pages;
+  const int64_t* slots;
+  int32_t page_size;
+  float eps;
+  uint32_t* status;  /* [T] or NULL */
+} approxifer_norm_rope_args;
+int approxifer_qk_norm_rope(const approxifer_norm_rope_args* args, void* cuda_stream);
+
+/*
+ * Attention over a paged cache with a sliding window and a few first tokens that stay visible.  The new tokens of
+ * `batch` sequences are packed: sequence b has the queries q_start[b] .. q_start[b+1]-1, which stand at the last
+ * positions of its kv_len[b] cached tokens.  For a query at position p and every head h (kv head h / (Hq / Hkv))
+ *     out = sum_j softmax_j(scale q.k_j) v_j   over the positions j <= p with  j > p - window  or  j < sinks
+ * (window = 0: every j <= p).  Position j lies in page block_table[b][j / page_size], row j % page_size; an entry
+ * outside 0 .. num_pages-1, or beyond the table, is a page that holds nothing (freed): its positions are not visible.
+ * A row without a visible position (also: kv_len[b] shorter than the queries) is zero.  What lies in positions that
+ * a query does not see, NaN included, never influences it.
+ *   q_start  [batch+1] int32, ascending, q_start[0] = 0, q_start[batch] = T
+ *   kv_len   [batch] int32        max_q  an upper bound on every sequence's number of queries (HOST)
+ *   k_cache, v_cache  [num_pages][Hkv][page_size][D] by strides; bfloat16, as q and out
+ * The softmax runs in one pass in fp32; the weights are rounded to bfloat16 for the product with V.
+ * Hq a multiple of Hkv, 1 <= D <= 256, 1 <= page_size.  D a multiple of 8 up to 128, a page size that is a power of two
+ * of at least 8 (single tokens: any), 16-byte aligned bases and strides of whole 16 bytes run on the tensor cores; others
+ * run an element-wise kernel.
+ */
+typedef struct approxifer_attention_args {
+  int64_t T;
+  int32_t batch, max_q, Hq, Hkv, D, page_size, window, sinks;
+  float scale;
+  int32_t reserved;  /* 0 */
+  const uint16_t* q; /* [T][Hq][D] */
+  int64_t q_tstride, q_hstride;
+  const uint16_t* k_cache;
+  int64_t kc_pstride, kc_hstride, kc_rstride;
+  const uint16_t* v_cache;
+  int64_t vc_pstride, vc_hstride, vc_rstride;
+  int64_t num_pages;
+  const int32_t* block_table; /* [batch][table_pages] */
+  int64_t table_stride, table_pages;
+  const int32_t* q_start;
+  const int32_t* kv_len;
+  uint16_t* out;     /* [T][Hq][D] */
+  int64_t o_tstride, o_hstride;
+} approxifer_attention_args;
+int approxifer_attention(const approxifer_attention_args* args, void* cuda_stream);
+
+/*
  * Test hook (not on the hot path): the weights the kernels use, computed on
  * the device by the same code.
  *   which = 0: encoder, w[W][K] = l_j(beta_i);            idx, n untouched

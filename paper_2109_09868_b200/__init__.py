@@ -37,3 +37,8 @@ from .binding import (  # noqa: F401
     strerror,
     version,
 )
+from .hosted import (  # noqa: F401
+    approxifer_attention,
+    approxifer_linear,
+    approxifer_qk_norm_rope,
+)

@@ -50,6 +50,9 @@ EXPORTS = (
     "approxifer_locate_gather",
     "approxifer_encode_bf16",
     "approxifer_decode_bf16",
+    "approxifer_linear",
+    "approxifer_qk_norm_rope",
+    "approxifer_attention",
 )
 
 
@@ -148,6 +151,9 @@ def load() -> ctypes.CDLL:
     lib.approxifer_locate_host.restype = c_int
     lib.approxifer_encode_host_static.argtypes = [pp, c_int64, c_int64, c_void_p, c_void_p, c_void_p]
     lib.approxifer_encode_host_static.restype = c_int
+    for name in ("approxifer_linear", "approxifer_qk_norm_rope", "approxifer_attention"):  # (packed struct, stream)
+        getattr(lib, name).argtypes = [c_char_p, c_void_p]
+        getattr(lib, name).restype = c_int
     del pf, pu, pi
     _lib = lib
     return lib

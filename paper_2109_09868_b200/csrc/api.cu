@@ -326,8 +326,8 @@ const char* approxifer_strerror(int code) {
   switch (code) {
     case APPROXIFER_OK: return "ok";
     case APPROXIFER_E_NULL: return "a required pointer is NULL";
-    case APPROXIFER_E_RANGE: return "argument out of range (K in 1..32, W in 2..32, E >= 0, G >= 0, 1 <= D <= 2^31, row stride >= row length)";
-    case APPROXIFER_E_PARAM: return "inconsistent parameters (locate needs E >= 1 and 2(K+E) <= W; unknown flag bits)";
+    case APPROXIFER_E_RANGE: return "argument out of range (K in 1..32, W in 2..32, E >= 0, G >= 0, 1 <= D <= 2^31, row stride >= row length; hosted-model operators: an extent or stride below its minimum or above its maximum)";
+    case APPROXIFER_E_PARAM: return "inconsistent parameters (locate needs E >= 1 and 2(K+E) <= W; unknown flag bits; hosted-model operators: unknown type or activation, odd rotation, query heads not a multiple of the key heads, misaligned elements)";
     case APPROXIFER_E_CUDA: return "the CUDA runtime reported an error at kernel launch";
     case APPROXIFER_E_WORKSPACE: return "the device workspace is too small to stage a single group";
     case APPROXIFER_E_TOO_LARGE: return "the batch is larger than the built-in staging area (APPROXIFER_STATIC_WORKSPACE_BYTES); split it or use approxifer_encode_host";

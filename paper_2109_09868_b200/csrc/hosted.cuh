@@ -1,0 +1,66 @@
+// Shared declarations of the hosted-model operators (linear, per-head norm with rotary positions, attention over a
+// paged cache).  The C structs of include/approxifer.h are what the launchers take: they hold device pointers and
+// strides, already checked by hosted_api.cu.
+#pragma once
+#include <cuda_bf16.h>
+#include <math_constants.h>
+
+#include "../../include/approxifer.h"
+#include "common.cuh"
+
+namespace approxifer {
+
+using bf16 = __nv_bfloat16;
+
+cudaError_t launch_linear(const approxifer_linear_args& a, cudaStream_t stream);
+cudaError_t launch_norm_rope(const approxifer_norm_rope_args& a, cudaStream_t stream);
+cudaError_t launch_attention(const approxifer_attention_args& a, cudaStream_t stream);
+
+#ifdef __CUDACC__
+__device__ __forceinline__ float widen(float v) { return v; }
+__device__ __forceinline__ float widen(bf16 v) { return __bfloat162float(v); }
+template <typename T>
+__device__ __forceinline__ T narrow(float v);
+template <>
+__device__ __forceinline__ float narrow<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ bf16 narrow<bf16>(float v) { return __float2bfloat16_rn(v); }
+
+// The activations of approxifer_linear, in fp32.
+template <int ACT>
+__device__ __forceinline__ float activate(float x) {
+  if constexpr (ACT == APPROXIFER_ACT_RELU) return x > 0.f ? x : (x == x ? 0.f : x);  // (a NaN stays one)
+  if constexpr (ACT == APPROXIFER_ACT_GELU) return 0.5f * x * (1.f + erff(x * 0.70710678f));
+  if constexpr (ACT == APPROXIFER_ACT_GELU_TANH) return 0.5f * x * (1.f + tanhf(0.79788456f * (x + 0.044715f * x * x * x)));
+  if constexpr (ACT == APPROXIFER_ACT_SILU) return x / (1.f + __expf(-x));
+  return x;
+}
+__device__ __forceinline__ float activate(int act, float x) {
+  switch (act) {
+    case APPROXIFER_ACT_RELU: return activate<APPROXIFER_ACT_RELU>(x);
+    case APPROXIFER_ACT_GELU: return activate<APPROXIFER_ACT_GELU>(x);
+    case APPROXIFER_ACT_GELU_TANH: return activate<APPROXIFER_ACT_GELU_TANH>(x);
+    case APPROXIFER_ACT_SILU: return activate<APPROXIFER_ACT_SILU>(x);
+    default: return x;
+  }
+}
+
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+  return v;
+}
+
+// The sequence a packed token belongs to: the last b with q_start[b] <= t (q_start ascending, q_start[0] = 0).
+__device__ __forceinline__ int sequence_of(const int32_t* q_start, int batch, int64_t t) {
+  int lo = 0, hi = batch - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (__ldg(q_start + mid) <= t) lo = mid;
+    else hi = mid - 1;
+  }
+  return lo;
+}
+#endif
+
+}  // namespace approxifer

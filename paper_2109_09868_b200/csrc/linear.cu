@@ -1,0 +1,67 @@
+// Matrix product with bias, activation and residual: choice of kernel, and the element-wise kernel for operands that
+// the tensor-core kernels cannot take (bases or row strides that are not whole 16 bytes).
+#include "hosted.cuh"
+
+namespace approxifer {
+namespace {
+
+constexpr int kTile = 64, kDepth = 16, kThreads = 256;
+
+// One CTA = a 64 x 64 tile of Y, a thread 4 x 4 of it; both operands go through shared memory 16 columns at a time as
+// fp32.  Bound by the fp32 pipe (a path for odd layouts, not for speed).
+template <typename Out>
+__global__ void __launch_bounds__(kThreads) linear_element_kernel(const __grid_constant__ approxifer_linear_args a, int64_t tiles_n) {
+  __shared__ float xs[kDepth][kTile + 4], ws[kDepth][kTile + 4];
+  const int64_t m0 = (blockIdx.x / tiles_n) * kTile, n0 = (blockIdx.x % tiles_n) * kTile;
+  const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
+  const bf16* X = reinterpret_cast<const bf16*>(a.X);
+  const bf16* Wt = reinterpret_cast<const bf16*>(a.Wt);
+  float acc[4][4] = {};
+  for (int64_t k0 = 0; k0 < a.K; k0 += kDepth) {
+    for (int e = threadIdx.x; e < kTile * kDepth; e += kThreads) {
+      const int row = e / kDepth, col = e % kDepth;
+      const bool in_k = k0 + col < a.K;
+      xs[col][row] = (in_k && m0 + row < a.M) ? widen(X[(m0 + row) * a.x_rstride + k0 + col]) : 0.f;
+      ws[col][row] = (in_k && n0 + row < a.N) ? widen(Wt[(n0 + row) * a.w_rstride + k0 + col]) : 0.f;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kDepth; ++k) {
+      float x[4], w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = xs[k][ty * 4 + i], w[i] = ws[k][tx * 4 + i];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(x[i], w[j], acc[i][j]);
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int64_t m = m0 + ty * 4 + i, n = n0 + tx * 4 + j;
+      if (m >= a.M || n >= a.N) continue;
+      float y = acc[i][j];
+      if (a.bias) y += widen(reinterpret_cast<const bf16*>(a.bias)[n]);
+      y = activate(a.activation, y);
+      if (a.R) y += widen(static_cast<const Out*>(a.R)[m * a.r_rstride + n]);
+      static_cast<Out*>(a.Y)[m * a.y_rstride + n] = narrow<Out>(y);
+    }
+}
+
+}  // namespace
+
+cudaError_t launch_linear(const approxifer_linear_args& a, cudaStream_t stream) {
+  const int64_t tiles_n = (a.N + kTile - 1) / kTile, tiles = tiles_n * ((a.M + kTile - 1) / kTile);
+  if (tiles > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
+  if (a.out_type == APPROXIFER_TYPE_F32)
+    linear_element_kernel<float><<<(unsigned)tiles, kThreads, 0, stream>>>(a, tiles_n);
+  else
+    linear_element_kernel<bf16><<<(unsigned)tiles, kThreads, 0, stream>>>(a, tiles_n);
+  count_launch();
+  return cudaGetLastError();
+}
+
+}  // namespace approxifer

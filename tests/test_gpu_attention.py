@@ -1,0 +1,178 @@
+"""approxifer_attention against its 64-bit plain form: one token and chunks of prompts, windows, sinks, lengths of zero and one,
+pages that end inside a tile, freed pages, NaN wherever nothing may be read, strides."""
+import pytest
+import torch
+
+import hosted_reference as ref
+import paper_2109_09868_b200 as ap
+
+pytestmark = pytest.mark.gpu
+
+
+def inputs(qs, kvs, Hq, Hkv, D, page, seed=0, dirty=True):
+    """Packed queries and a cache whose pages are shuffled; slots that hold no token are NaN."""
+    g = torch.Generator().manual_seed(seed)
+    per = [(n + page - 1) // page for n in kvs]
+    pages = sum(per) + 2
+    order = torch.randperm(pages, generator=g).to(torch.int32)
+    table = torch.full((len(kvs), max(max(per), 1)), -1, dtype=torch.int32)
+    used, at = torch.zeros((pages, page), dtype=torch.bool), 0
+    for b, (n, m) in enumerate(zip(kvs, per)):
+        table[b, :m] = order[at: at + m]
+        for j in range(n):
+            used[table[b, j // page].long(), j % page] = True
+        at += m
+    starts = torch.tensor([sum(qs[:i]) for i in range(len(qs) + 1)], dtype=torch.int32)
+    rnd = lambda *s: torch.randn(s, generator=g).to(torch.bfloat16)  # noqa: E731
+    q, k, v = rnd(sum(qs), Hq, D), rnd(pages, Hkv, page, D), rnd(pages, Hkv, page, D)
+    if dirty:
+        for c in (k, v):
+            c.transpose(1, 2)[~used] = float("nan")
+    return q, k, v, table, starts, torch.tensor(kvs, dtype=torch.int32)
+
+
+def run(x, max_q, window, sinks, scale):
+    return ap.approxifer_attention(*[t.cuda() for t in x], max_q, window=window, sinks=sinks, scale=scale)
+
+
+def check(got, want, bound):
+    got = got.double().cpu()
+    assert torch.isfinite(got).all()
+    over = ((got - want).abs() - bound).max()
+    assert over <= 0, float(over)
+
+
+CASES = [  # queries, cached tokens, Hq, Hkv, D, page, window, sinks
+    # one token for each sequence
+    ([1], [1], 1, 1, 64, 16, 0, 0),
+    ([1, 1, 1], [1, 17, 300], 8, 2, 128, 16, 0, 0),
+    ([1, 1, 1, 1], [5, 128, 129, 1000], 8, 8, 64, 16, 64, 4),
+    ([1, 1], [700, 3], 16, 1, 128, 32, 100, 1),
+    ([1, 1], [1500, 2100], 4, 1, 128, 16, 0, 0),
+    ([1, 1, 1], [90, 91, 92], 6, 2, 80, 8, 17, 3),
+    ([1, 1], [333, 64], 9, 3, 96, 64, 0, 0),
+    ([1], [500], 40, 2, 64, 16, 200, 16),      # 20 query heads share a key head
+    ([1, 1], [77, 400], 4, 2, 72, 24, 50, 2),  # a page size that is no power of two
+    ([1, 1], [0, 40], 4, 2, 64, 16, 8, 2),     # a sequence with nothing cached: its row is zero
+    ([1, 1], [130, 260], 2, 2, 40, 16, 1, 0),  # a window of the token itself
+    ([1], [260], 2, 1, 64, 16, 100, 300),      # more sinks than tokens before the window
+    # prompts and chunks
+    ([5], [5], 1, 1, 64, 16, 0, 0),
+    ([130], [130], 4, 2, 128, 16, 0, 0),
+    ([300, 1, 129], [300, 200, 129], 4, 1, 64, 16, 0, 0),
+    ([257], [257], 2, 2, 128, 64, 100, 4),
+    ([200, 64], [513, 700], 8, 2, 64, 32, 130, 5),
+    ([150, 3], [400, 3], 6, 2, 80, 16, 64, 1),
+    ([90], [600], 3, 1, 96, 8, 0, 0),
+    ([70], [70], 16, 1, 128, 128, 20, 2),
+    ([2, 2], [300, 2], 4, 4, 128, 16, 0, 0),
+    ([33, 7], [20, 7], 4, 2, 64, 16, 0, 0),    # fewer cached tokens than queries: the first rows see nothing
+    ([20], [200], 10, 2, 64, 16, 16, 0),       # 5 query heads share a key head
+    ([40], [120], 4, 2, 72, 24, 50, 2),
+    ([140], [140], 2, 1, 256, 16, 0, 0),
+    ([6], [50], 2, 1, 33, 16, 10, 1),
+    ([400], [400], 2, 1, 128, 16, 5, 40),      # sinks that reach past the window's start
+]
+
+
+@pytest.mark.parametrize("qs,kvs,Hq,Hkv,D,page,window,sinks", CASES)
+def test_attention_matches_the_plain_form(qs, kvs, Hq, Hkv, D, page, window, sinks):
+    x = inputs(qs, kvs, Hq, Hkv, D, page, seed=sum(kvs) + D)
+    scale = D ** -0.5
+    want, bound = ref.attention(*x, window, sinks, scale)
+    check(run(x, max(qs), window, sinks, scale), want, bound)
+
+
+def test_attention_scale_sign_and_large_scores():
+    x = inputs([1, 140], [300, 140], 4, 2, 64, 16, seed=9)
+    for scale in (-0.3, 0.0, 4.0):
+        want, bound = ref.attention(*x, 0, 0, scale)
+        check(run(x, 140, 0, 0, scale), want, bound)
+        one = (x[0][:1], x[1], x[2], x[3][:1], x[4][:2], x[5][:1])
+        check(run(one, 1, 0, 0, scale), want[:1], bound[:1])
+
+
+@pytest.mark.parametrize("D,Hq,Hkv", [(64, 4, 2), (128, 8, 1)])
+def test_attention_freed_pages_and_foreign_tokens_are_not_seen(D, Hq, Hkv):
+    """Pages that left the window are freed and given to others: their entries are -1, out of range, or their content is NaN."""
+    window, sinks, page, n = 100, 4, 16, 700
+    for nq in (1, 90):
+        x = list(inputs([nq], [n], Hq, Hkv, D, page, seed=5))
+        want, bound = ref.attention(*x, window, sinks, D ** -0.5)
+        first = n - nq + 1 - window  # the first position any query's window holds
+        gone = [p for p in range(1, n // page) if (p + 1) * page <= first]
+        for c in (1, 2):
+            x[c] = x[c].clone()
+            x[c][x[3][0, gone].long()] = float("nan")
+            head = x[c].transpose(1, 2)[x[3][0, 0].long()]  # the sinks' page, beyond the sinks
+            head[sinks:] = float("nan")
+        check(run(x, nq, window, sinks, D ** -0.5), want, bound)
+        x[3] = x[3].clone()
+        x[3][0, gone] = torch.tensor([(-1, 10 ** 6, -7)[i % 3] for i in range(len(gone))], dtype=torch.int32)
+        check(run(x, nq, window, sinks, D ** -0.5), want, bound)
+        # a page inside the window that is gone too: its positions are left out
+        x[3][0, n // page - 2] = -1
+        want, bound = ref.attention(*x, window, sinks, D ** -0.5)
+        check(run(x, nq, window, sinks, D ** -0.5), want, bound)
+        x[3][:] = -1
+        assert not run(x, nq, window, sinks, D ** -0.5).any()
+
+
+def test_attention_later_and_earlier_tokens_cannot_reach_a_row():
+    """Infinities and NaN in a key or a value change exactly the rows that see them."""
+    for D, page in ((64, 16), (128, 32)):
+        n, window, sinks = 300, 90, 2
+        x = list(inputs([n], [n], 4, 2, D, page, seed=3))
+        want, bound = ref.attention(*x, window, sinks, D ** -0.5)
+        for at, bad in ((40, float("nan")), (140, float("inf")), (299, float("-inf")), (1, float("nan"))):
+            for which in (1, 2):
+                y = list(x)
+                y[which] = x[which].clone()
+                y[which][x[3][0, at // page].long(), 1, at % page, 3] = bad
+                got = run(y, n, window, sinks, D ** -0.5).double().cpu()
+                sees = torch.tensor([at <= p and (at > p - window or at < sinks) for p in range(n)])
+                check(got[~sees], want[~sees], bound[~sees])
+                check(got[:, :2], want[:, :2], bound[:, :2])  # the other key head
+                if which == 2:  # a value: that element of the rows that see it, no other
+                    assert not torch.isfinite(got[sees][:, 2:, 3]).any()
+                    rest = [d for d in range(D) if d != 3]
+                    check(got[sees][:, 2:][..., rest], want[sees][:, 2:][..., rest], bound[sees][:, 2:][..., rest])
+                elif bad != bad:
+                    assert torch.isnan(got[sees][:, 2:]).all()
+
+
+def test_attention_strides_guards_streams_and_repeatability():
+    for qs, kvs in (([1, 1], [100, 333]), ([77, 130], [100, 333])):
+        q, k, v, table, start, lens = inputs(qs, kvs, 4, 2, 128, 16, seed=11)
+        want, bound = ref.attention(q, k, v, table, start, lens, 60, 4, 0.1)
+        T = q.shape[0]
+        wide = torch.zeros((T, 9, 136), dtype=torch.bfloat16, device="cuda")
+        wide[:, 2:6, 8:] = q.cuda()
+        token_major = [c.cuda().transpose(1, 2).contiguous().transpose(1, 2) for c in (k, v)]  # rows of a page before its heads
+        out = torch.full((T + 2, 4, 136), 7.0, dtype=torch.bfloat16, device="cuda")
+        rest = [t.cuda() for t in (table, start, lens)]
+        args = dict(window=60, sinks=4, scale=0.1)
+        got = ap.approxifer_attention(wide[:, 2:6, 8:], *token_major, *rest, max(qs), out=out[1:-1, :, :128], **args)
+        check(got, want, bound)
+        first = got.clone()
+        got.fill_(7.0)
+        assert bool((out == 7.0).all())
+        for _ in range(3):
+            assert torch.equal(ap.approxifer_attention(q.cuda(), *token_major, *rest, max(qs), **args), first)
+        s = torch.cuda.Stream()
+        qd = q.cuda()
+        s.wait_stream(torch.cuda.current_stream())
+        y = ap.approxifer_attention(qd, *token_major, *rest, max(qs) + 5, stream=s, **args)
+        s.synchronize()
+        assert torch.equal(y, first)
+        # bases and rows that are not whole 16 bytes
+        odd = torch.zeros((T, 4, 131), dtype=torch.bfloat16, device="cuda")
+        odd[:, :, 1:129] = q.cuda()
+        yo = torch.zeros((T, 4, 129), dtype=torch.bfloat16, device="cuda")
+        check(ap.approxifer_attention(odd[:, :, 1:129], *token_major, *rest, max(qs), out=yo[:, :, 1:], **args), want, bound)
+
+
+def test_attention_of_no_tokens():
+    x = inputs([1], [8], 2, 1, 64, 16)
+    none = (x[0][:0], x[1], x[2], x[3], torch.zeros(2, dtype=torch.int32), x[5])
+    assert run(none, 1, 0, 0, 0.1).shape == (0, 2, 64)

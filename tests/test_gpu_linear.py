@@ -1,0 +1,113 @@
+"""approxifer_linear against its 64-bit plain form: shapes from one row to several tiles, odd sizes, strides, unaligned
+bases, every activation, bias and residual present or not, both output types."""
+import pytest
+import torch
+
+import hosted_reference as ref
+import paper_2109_09868_b200 as ap
+
+pytestmark = pytest.mark.gpu
+
+
+def normal(shape, seed, dtype=torch.bfloat16, std=1.0):
+    return (torch.randn(shape, generator=torch.Generator().manual_seed(seed)) * std).to(dtype)
+
+
+def check(got, want, bound):
+    got = got.double().cpu()
+    assert torch.isfinite(got).all()
+    over = ((got - want).abs() - bound).max()
+    assert over <= 0, float(over)
+
+
+CASES = [  # M, N, K, bias, activation, residual, out
+    (1, 1, 1, True, "none", True, torch.bfloat16),
+    (1, 10, 8, False, "none", False, torch.float32),
+    (1, 4096, 512, False, "none", True, torch.bfloat16),
+    (2, 1000, 784, True, "gelu", False, torch.bfloat16),
+    (7, 129, 72, True, "relu", True, torch.float32),
+    (16, 256, 1024, True, "silu", False, torch.bfloat16),
+    (17, 520, 2048, False, "gelu_tanh", True, torch.bfloat16),
+    (33, 128, 64, True, "none", True, torch.bfloat16),
+    (65, 300, 200, True, "silu", True, torch.float32),
+    (100, 1000, 96, False, "gelu", False, torch.bfloat16),
+    (128, 256, 64, False, "none", False, torch.bfloat16),
+    (129, 257, 136, True, "gelu_tanh", True, torch.bfloat16),
+    (320, 10, 784, True, "none", False, torch.float32),
+    (513, 384, 1000, True, "relu", True, torch.bfloat16),
+    (1000, 1000, 160, False, "none", True, torch.float32),
+    (2300, 1100, 320, True, "gelu", True, torch.bfloat16),
+    (3000, 24, 64, False, "silu", False, torch.bfloat16),
+    (40, 33, 77, True, "gelu", True, torch.bfloat16),      # odd K: rows are not whole 16 bytes
+    (300, 65, 13, False, "relu", False, torch.float32),
+]
+
+
+@pytest.mark.parametrize("M,N,K,bias,act,residual,out", CASES)
+def test_linear_matches_the_plain_form(M, N, K, bias, act, residual, out):
+    x, w = normal((M, K), 1), normal((N, K), 2, std=K ** -0.5)
+    b = normal((N,), 3) if bias else None
+    r = normal((M, N), 4, out) if residual else None
+    want, bound = ref.linear(x, w, b, act, r, out)
+    dev = [None if t is None else t.cuda() for t in (x, w, b, r)]
+    got = ap.approxifer_linear(dev[0], dev[1], bias=dev[2], activation=act, residual=dev[3], out_dtype=out)
+    assert got.dtype == out and got.shape == (M, N)
+    check(got, want, bound)
+
+
+@pytest.mark.parametrize("M,N,K", [(3, 200, 256), (150, 328, 200), (700, 512, 512)])
+def test_linear_strides_guards_and_the_residual_in_place(M, N, K):
+    x, w, r = normal((M, K), 1), normal((N, K), 2, std=K ** -0.5), normal((M, N), 3)
+    want, bound = ref.linear(x, w, None, "none", r, torch.bfloat16)
+    xp = torch.full((M, K + 24), float("nan"), dtype=torch.bfloat16, device="cuda")
+    wp = torch.full((N, K + 8), float("nan"), dtype=torch.bfloat16, device="cuda")
+    y = torch.full((M + 2, N + 16), 7.0, dtype=torch.bfloat16, device="cuda")
+    xp[:, 16:16 + K], wp[:, :K] = x.cuda(), w.cuda()
+    y[1:-1, 8:8 + N] = r.cuda()
+    view = y[1:-1, 8:8 + N]
+    got = ap.approxifer_linear(xp[:, 16:16 + K], wp[:, :K], residual=view, Y=view)
+    check(got, want, bound)
+    view.fill_(7.0)
+    assert bool((y == 7.0).all())
+    # the same numbers from bases that are not whole 16 bytes
+    odd = torch.full((M, K + 3), float("nan"), dtype=torch.bfloat16, device="cuda")
+    odd[:, 3:] = x.cuda()
+    yo = torch.empty((M, N + 1), dtype=torch.bfloat16, device="cuda")
+    check(ap.approxifer_linear(odd[:, 3:], wp[:, :K], residual=r.cuda(), Y=yo[:, 1:]), want, bound)
+    # an aligned product into an output whose rows are not whole 16 bytes
+    check(ap.approxifer_linear(xp[:, 16:16 + K], wp[:, :K], residual=r.cuda(), Y=yo[:, 1:]), want, bound)
+
+
+def test_linear_infinities_and_nan_stay_in_their_rows():
+    for M, N, K in ((5, 140, 128), (300, 200, 128)):
+        x, w = normal((M, K), 1), normal((N, K), 2, std=K ** -0.5)
+        want, bound = ref.linear(x, w, None, "relu", None, torch.bfloat16)
+        x[2, 5], x[4, 7] = float("nan"), float("inf")
+        got = ap.approxifer_linear(x.cuda(), w.cuda(), activation="relu").double().cpu()
+        assert torch.isnan(got[2]).all() and torch.equal(torch.isinf(got[4]), w[:, 7].double() > 0)
+        keep = [i for i in range(M) if i not in (2, 4)]
+        check(got[keep], want[keep], bound[keep])
+
+
+def test_linear_is_repeatable_and_runs_on_a_stream_and_in_a_graph():
+    x, w, b = normal((24, 2048), 1).cuda(), normal((1024, 2048), 2, std=0.02).cuda(), normal((1024,), 3).cuda()
+    first = ap.approxifer_linear(x, w, bias=b, activation="gelu")
+    for _ in range(5):
+        assert torch.equal(ap.approxifer_linear(x, w, bias=b, activation="gelu"), first)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    y = ap.approxifer_linear(x, w, bias=b, activation="gelu", stream=s)
+    s.synchronize()
+    assert torch.equal(y, first)
+    out = torch.zeros_like(first)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ap.approxifer_linear(x, w, bias=b, activation="gelu", Y=out)
+    out.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, first)
+
+
+def test_linear_of_no_rows():
+    assert ap.approxifer_linear(torch.empty((0, 64), dtype=torch.bfloat16, device="cuda"), torch.empty((5, 64), dtype=torch.bfloat16, device="cuda")).shape == (0, 5)

@@ -1,0 +1,78 @@
+"""What the hosted-model operators refuse, found on the host before anything is launched."""
+import ctypes
+
+import pytest
+import torch
+
+import paper_2109_09868_b200 as ap
+from paper_2109_09868_b200 import binding, hosted
+
+
+def linear_rc(M=4, N=8, K=16, X=16, xs=16, W=16, ws=16, bias=0, R=0, rs=0, Y=16, ys=8, act=0, kind=0):
+    return ap.load().approxifer_linear(hosted._LINEAR.pack(M, N, K, X, xs, W, ws, bias, R, rs, Y, ys, act, kind), None)
+
+
+def test_linear_refusals():
+    assert linear_rc(M=0, X=0, W=0, Y=0) == binding.OK
+    for bad in (dict(M=-1), dict(N=0), dict(K=0), dict(M=2 ** 31), dict(N=2 ** 31), dict(K=2 ** 31), dict(xs=15), dict(ws=8), dict(ys=7), dict(R=16, rs=7)):
+        assert linear_rc(**bad) == binding.E_RANGE, bad
+    for bad in (dict(X=0), dict(W=0), dict(Y=0)):
+        assert linear_rc(**bad) == binding.E_NULL, bad
+    for bad in (dict(act=5), dict(act=-1), dict(kind=2), dict(X=17), dict(W=1), dict(bias=3), dict(Y=18, kind=1), dict(R=18, rs=8, kind=1)):
+        assert linear_rc(**bad) == binding.E_PARAM, bad
+    assert ap.load().approxifer_linear(None, None) == binding.E_NULL
+
+
+def norm_rope_rc(T=3, Hq=4, Hkv=2, D=8, rot=8, inter=0, kind=0, q=16, qs=(32, 8), k=16, ks=(16, 8), v=16, vs=(16, 8), qw=0, kw=0, cs=16, npos=9,
+                 pos=16, qo=16, qos=(32, 8), kc=16, kcs=(128, 64, 8), vc=16, vcs=(128, 64, 8), pages=5, slots=16, page=8, eps=1e-6, status=0):
+    return ap.load().approxifer_qk_norm_rope(hosted._NORM_ROPE.pack(
+        T, Hq, Hkv, D, rot, inter, kind, q, *qs, k, *ks, v, *vs, qw, kw, cs, npos, pos, qo, *qos, kc, *kcs, vc, *vcs, pages, slots, page, eps, status), None)
+
+
+def test_norm_rope_refusals():
+    assert norm_rope_rc(T=0, q=0, qo=0, cs=0, pos=0, slots=0) == binding.OK
+    for bad in (dict(T=-1), dict(Hq=0), dict(Hkv=0), dict(D=0), dict(D=257, rot=0), dict(rot=10), dict(rot=-2), dict(page=0), dict(pages=-1), dict(qs=(32, 7)),
+                dict(qos=(-1, 8)), dict(ks=(16, 4)), dict(vcs=(128, 64, 7)), dict(kcs=(7, 64, 8))):
+        assert norm_rope_rc(**bad) == binding.E_RANGE, bad
+    for bad in (dict(rot=7), dict(kind=2), dict(eps=-1.0), dict(eps=float("nan")), dict(q=17), dict(kc=17), dict(kind=1, q=18), dict(cs=18)):
+        assert norm_rope_rc(**bad) == binding.E_PARAM, bad
+    for bad in (dict(q=0), dict(qo=0), dict(cs=0), dict(pos=0), dict(slots=0), dict(k=0), dict(vc=0)):
+        assert norm_rope_rc(**bad) == binding.E_NULL, bad
+    assert ap.load().approxifer_qk_norm_rope(None, None) == binding.E_NULL
+
+
+def attention_rc(T=3, batch=1, max_q=3, Hq=4, Hkv=2, D=8, page=8, window=0, sinks=0, scale=1.0, reserved=0, q=16, qs=(32, 8), kc=16, kcs=(128, 64, 8), vc=16,
+                 vcs=(128, 64, 8), pages=5, table=16, ts=4, tp=4, start=16, lens=16, out=16, os=(32, 8)):
+    return ap.load().approxifer_attention(hosted._ATTENTION.pack(
+        T, batch, max_q, Hq, Hkv, D, page, window, sinks, scale, reserved, q, *qs, kc, *kcs, vc, *vcs, pages, table, ts, tp, start, lens, out, *os), None)
+
+
+def test_attention_refusals():
+    assert attention_rc(T=0, batch=0, q=0, kc=0, vc=0, out=0) == binding.OK
+    for bad in (dict(T=-1), dict(batch=0), dict(max_q=0), dict(Hq=0), dict(Hkv=0), dict(D=0), dict(D=257), dict(page=0), dict(window=-1), dict(sinks=-1),
+                dict(pages=-1), dict(tp=-1), dict(qs=(32, 7)), dict(os=(-32, 8)), dict(kcs=(128, 64, 7)), dict(vcs=(128, 7, 8)), dict(ts=-4)):
+        assert attention_rc(**bad) == binding.E_RANGE, bad
+    for bad in (dict(Hq=5), dict(scale=float("nan")), dict(scale=float("inf")), dict(reserved=1), dict(q=17), dict(vc=17)):
+        assert attention_rc(**bad) == binding.E_PARAM, bad
+    for bad in (dict(q=0), dict(kc=0), dict(vc=0), dict(table=0), dict(start=0), dict(lens=0), dict(out=0)):
+        assert attention_rc(**bad) == binding.E_NULL, bad
+    assert ap.load().approxifer_attention(None, None) == binding.E_NULL
+
+
+def test_packed_structs_are_as_long_as_the_header_says():
+    # eight bytes a pointer or 64-bit integer, four the others
+    assert hosted._LINEAR.size == 12 * 8 + 2 * 4
+    assert hosted._NORM_ROPE.size == 29 * 8 + 8 * 4
+    assert hosted._ATTENTION.size == 21 * 8 + 10 * 4
+    assert ctypes.sizeof(ctypes.c_void_p) == 8
+
+
+def test_binding_refuses_what_the_library_cannot_take():
+    x = torch.zeros(2, 8, dtype=torch.bfloat16)
+    with pytest.raises(ValueError):
+        ap.approxifer_linear(x, x)
+    with pytest.raises(ValueError):
+        ap.approxifer_qk_norm_rope(x.view(2, 1, 8), None, None, None, None, torch.zeros(4, 8), torch.zeros(2, dtype=torch.int32), None, None, None)
+    with pytest.raises(ValueError):
+        ap.approxifer_attention(x.view(2, 1, 8), x.view(1, 1, 2, 8), x.view(1, 1, 2, 8), torch.zeros(1, 1, dtype=torch.int32),
+                                torch.zeros(2, dtype=torch.int32), torch.zeros(1, dtype=torch.int32), 2)
