@@ -313,13 +313,13 @@ int approxifer_debug_fma_peak(int iters, int blocks, float* sink, void* cuda_str
 }
 
 int approxifer_reset_device_wait_timeouts(void) {
-  return (reset_decode_wait_timeouts() == cudaSuccess && reset_pack_wait_timeouts() == cudaSuccess) ? APPROXIFER_OK : APPROXIFER_E_CUDA;
+  return (reset_decode_wait_timeouts() == cudaSuccess && reset_pack_wait_timeouts() == cudaSuccess && reset_hosted_wait_timeouts() == cudaSuccess) ? APPROXIFER_OK : APPROXIFER_E_CUDA;
 }
 
 int64_t approxifer_device_wait_timeouts(void) {
-  unsigned int n = 0, m = 0;
-  if (read_decode_wait_timeouts(&n) != cudaSuccess || read_pack_wait_timeouts(&m) != cudaSuccess) return -1;
-  return (int64_t)n + (int64_t)m;
+  unsigned int n = 0, m = 0, h = 0;
+  if (read_decode_wait_timeouts(&n) != cudaSuccess || read_pack_wait_timeouts(&m) != cudaSuccess || read_hosted_wait_timeouts(&h) != cudaSuccess) return -1;
+  return (int64_t)n + (int64_t)m + (int64_t)h;
 }
 
 const char* approxifer_strerror(int code) {

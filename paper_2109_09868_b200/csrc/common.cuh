@@ -108,6 +108,8 @@ bool pack_rotation_info(int K, int W, int64_t C, int mode, int* groups_per_item,
                         int* passes_plain, int* passes_chosen);
 cudaError_t reset_decode_wait_timeouts();
 cudaError_t reset_pack_wait_timeouts();
+cudaError_t read_hosted_wait_timeouts(unsigned int* out);  // all kernels of the hosted-model operators together
+cudaError_t reset_hosted_wait_timeouts();
 
 // Short-payload decoder (C <= 32, dense buffers); see decode_small.cu.
 bool decode_small_eligible(const DecodeArgs& a);

@@ -13,6 +13,10 @@ namespace approxifer {
 using bf16 = __nv_bfloat16;
 
 cudaError_t launch_linear(const approxifer_linear_args& a, cudaStream_t stream);
+bool linear_tile_eligible(const approxifer_linear_args& a);  // see linear_tile.cu
+cudaError_t launch_linear_tile(const approxifer_linear_args& a, cudaStream_t stream);
+cudaError_t read_linear_tile_wait_timeouts(unsigned int* out);
+cudaError_t reset_linear_tile_wait_timeouts();
 cudaError_t launch_norm_rope(const approxifer_norm_rope_args& a, cudaStream_t stream);
 cudaError_t launch_attention(const approxifer_attention_args& a, cudaStream_t stream);
 

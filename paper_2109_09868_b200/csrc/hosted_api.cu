@@ -12,6 +12,10 @@ bool known_type(int32_t type) { return type == APPROXIFER_TYPE_BF16 || type == A
 int from_cuda(cudaError_t e) { return e == cudaSuccess ? APPROXIFER_OK : APPROXIFER_E_CUDA; }
 
 }  // namespace
+
+cudaError_t read_hosted_wait_timeouts(unsigned int* out) { return read_linear_tile_wait_timeouts(out); }
+cudaError_t reset_hosted_wait_timeouts() { return reset_linear_tile_wait_timeouts(); }
+
 }  // namespace approxifer
 
 using namespace approxifer;

@@ -54,6 +54,7 @@ __global__ void __launch_bounds__(kThreads) linear_element_kernel(const __grid_c
 }  // namespace
 
 cudaError_t launch_linear(const approxifer_linear_args& a, cudaStream_t stream) {
+  if (linear_tile_eligible(a)) return launch_linear_tile(a, stream);
   const int64_t tiles_n = (a.N + kTile - 1) / kTile, tiles = tiles_n * ((a.M + kTile - 1) / kTile);
   if (tiles > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
   if (a.out_type == APPROXIFER_TYPE_F32)
