@@ -17,6 +17,9 @@ bool linear_tile_eligible(const approxifer_linear_args& a);  // see linear_tile.
 cudaError_t launch_linear_tile(const approxifer_linear_args& a, cudaStream_t stream);
 cudaError_t read_linear_tile_wait_timeouts(unsigned int* out);
 cudaError_t reset_linear_tile_wait_timeouts();
+cudaError_t launch_linear_pair(const approxifer_linear_args& a, cudaStream_t stream);  // see linear_pair.cu
+cudaError_t read_linear_pair_wait_timeouts(unsigned int* out);
+cudaError_t reset_linear_pair_wait_timeouts();
 cudaError_t launch_norm_rope(const approxifer_norm_rope_args& a, cudaStream_t stream);
 cudaError_t launch_attention(const approxifer_attention_args& a, cudaStream_t stream);
 
@@ -35,7 +38,7 @@ template <int ACT>
 __device__ __forceinline__ float activate(float x) {
   if constexpr (ACT == APPROXIFER_ACT_RELU) return x > 0.f ? x : (x == x ? 0.f : x);  // (a NaN stays one)
   if constexpr (ACT == APPROXIFER_ACT_GELU) return 0.5f * x * (1.f + erff(x * 0.70710678f));
-  if constexpr (ACT == APPROXIFER_ACT_GELU_TANH) return 0.5f * x * (1.f + tanhf(0.79788456f * (x + 0.044715f * x * x * x)));
+  if constexpr (ACT == APPROXIFER_ACT_GELU_TANH) return x / (1.f + __expf(-1.5957691f * (x + 0.044715f * x * x * x)));  // 0.5 (1 + tanh u) = 1 / (1 + e^-2u)
   if constexpr (ACT == APPROXIFER_ACT_SILU) return x / (1.f + __expf(-x));
   return x;
 }

@@ -13,8 +13,23 @@ int from_cuda(cudaError_t e) { return e == cudaSuccess ? APPROXIFER_OK : APPROXI
 
 }  // namespace
 
-cudaError_t read_hosted_wait_timeouts(unsigned int* out) { return read_linear_tile_wait_timeouts(out); }
-cudaError_t reset_hosted_wait_timeouts() { return reset_linear_tile_wait_timeouts(); }
+cudaError_t read_hosted_wait_timeouts(unsigned int* out) {
+  *out = 0;
+  for (auto read : {read_linear_tile_wait_timeouts, read_linear_pair_wait_timeouts}) {
+    unsigned int n = 0;
+    const cudaError_t e = read(&n);
+    if (e != cudaSuccess) return e;
+    *out += n;
+  }
+  return cudaSuccess;
+}
+cudaError_t reset_hosted_wait_timeouts() {
+  for (auto reset : {reset_linear_tile_wait_timeouts, reset_linear_pair_wait_timeouts}) {
+    const cudaError_t e = reset();
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
 
 }  // namespace approxifer
 

@@ -54,7 +54,11 @@ __global__ void __launch_bounds__(kThreads) linear_element_kernel(const __grid_c
 }  // namespace
 
 cudaError_t launch_linear(const approxifer_linear_args& a, cudaStream_t stream) {
-  if (linear_tile_eligible(a)) return launch_linear_tile(a, stream);
+  if (linear_tile_eligible(a)) {
+    // 256 x 256 tiles on pairs of CTAs once there are tiles for most of the pairs
+    if (a.M > 128 && a.N > 128 && ((a.M + 255) / 256) * ((a.N + 255) / 256) >= 48) return launch_linear_pair(a, stream);
+    return launch_linear_tile(a, stream);
+  }
   const int64_t tiles_n = (a.N + kTile - 1) / kTile, tiles = tiles_n * ((a.M + kTile - 1) / kTile);
   if (tiles > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
   if (a.out_type == APPROXIFER_TYPE_F32)

@@ -1,0 +1,243 @@
+// Matrix product with bias, activation and residual for many tiles: persistent pairs of CTAs, each pair one 256 x 256 tile
+// of Y at a time (tcgen05 with cta_group::2: every CTA keeps 128 rows of X and half of the tile's rows of Wt in shared
+// memory, the two tensor cores read both halves), accumulators double-buffered in tensor memory, so that the epilogue of a
+// tile runs under the products of the next.
+//
+//   warp 0      one lane: tensor-map copies of this CTA's operands, six stages of 64 columns (32 KB) in flight
+//   warp 1      one lane of the pair's first CTA: tcgen05.mma for the pair; allocates the tensor memory
+//   warps 2, 3  idle (the accumulator's lanes belong to warps by their index modulo 4)
+//   warps 4-11  epilogue: two warps to each quarter of the lanes, half of the columns each; bias, activation, residual,
+//               one rounding, 16-byte stores (a thread owns 64 bytes or more of one row at a time)
+#include "async.cuh"
+
+namespace approxifer {
+
+__device__ unsigned int g_linear_pair_wait_timeouts = 0;
+
+namespace {
+
+constexpr int kThreads = 384;
+constexpr int kEpilogueWarps = 8;
+constexpr int kTileM = 256, kTileN = 256, kDepth = 64;
+constexpr int kStages = 6;
+constexpr int kHalfBytes = 128 * kDepth * 2;      // one operand of one CTA per stage
+constexpr int kStageBytes = 2 * kHalfBytes;
+constexpr int kHeader = 1024;
+constexpr int kSmemBytes = kHeader + 1024 + kStages * kStageBytes;
+constexpr int kTmemCols = 512;
+constexpr int kGroupM = 8;  // rows of tiles that are walked together: their X stays in L2 while Wt streams by
+
+struct PairArgs {
+  int32_t M, N, K, steps, tiles_m, tiles_n, tiles;
+  const bf16* bias;
+  const void* R;
+  void* Y;
+  int64_t r_rstride, y_rstride;
+  int32_t vec;  // 16-byte accesses to Y, R and the bias
+};
+
+// Tiles in bands of kGroupM rows of tiles, down a band's columns of tiles.
+__device__ __forceinline__ void place(const PairArgs& a, int tile, int* m0, int* n0) {
+  const int per_band = kGroupM * a.tiles_n, band = tile / per_band, in = tile - band * per_band;
+  const int rows = min(kGroupM, a.tiles_m - band * kGroupM);
+  *m0 = (band * kGroupM + in % rows) * kTileM;
+  *n0 = (in / rows) * kTileN;
+}
+
+template <typename Out, int ACT>
+__device__ __forceinline__ void finish32(const PairArgs& a, int m, int n, const uint32_t (&v)[32]) {
+  if (m >= a.M || n >= a.N) return;
+  Out* y = static_cast<Out*>(a.Y) + (int64_t)m * a.y_rstride + n;
+  const Out* r = a.R ? static_cast<const Out*>(a.R) + (int64_t)m * a.r_rstride + n : nullptr;
+  if (a.vec && n + 32 <= a.N) {
+    constexpr int kPer = 16 / sizeof(Out);  // elements of 16 bytes
+#pragma unroll
+    for (int j = 0; j < 32; j += 8) {
+      float z[8];
+      uint4 b = make_uint4(0, 0, 0, 0);
+      if (a.bias) b = __ldg(reinterpret_cast<const uint4*>(a.bias + n + j));
+      const uint32_t bw[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        z[i] = activate<ACT>(__uint_as_float(v[j + i]) + __uint_as_float(i & 1 ? bw[i / 2] & 0xffff0000u : bw[i / 2] << 16));
+#pragma unroll
+      for (int i = 0; i < 8; i += kPer) {
+        if constexpr (sizeof(Out) == 2) {
+          if (r) {
+            const uint4 q = *reinterpret_cast<const uint4*>(r + j);
+            const uint32_t qw[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+            for (int e = 0; e < 8; ++e) z[e] += __uint_as_float(e & 1 ? qw[e / 2] & 0xffff0000u : qw[e / 2] << 16);
+          }
+          *reinterpret_cast<uint4*>(y + j) = make_uint4(pack_bf16x2(z[0], z[1]), pack_bf16x2(z[2], z[3]), pack_bf16x2(z[4], z[5]), pack_bf16x2(z[6], z[7]));
+        } else {
+          if (r) {
+            const float4 q = *reinterpret_cast<const float4*>(r + j + i);
+            z[i] += q.x, z[i + 1] += q.y, z[i + 2] += q.z, z[i + 3] += q.w;
+          }
+          *reinterpret_cast<float4*>(y + j + i) = make_float4(z[i], z[i + 1], z[i + 2], z[i + 3]);
+        }
+      }
+    }
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < 32; ++j) {
+    if (n + j < a.N) {
+      const float z = activate<ACT>(__uint_as_float(v[j]) + (a.bias ? widen(a.bias[n + j]) : 0.f));
+      y[j] = narrow<Out>(r ? z + widen(r[j]) : z);
+    }
+  }
+}
+
+template <typename Out, int ACT>
+__global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
+    linear_pair_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map, const __grid_constant__ PairArgs a) {
+  extern __shared__ unsigned char raw[];
+  unsigned char* base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
+  uint64_t* bars = reinterpret_cast<uint64_t*>(base);  // full[stages], empty[stages], ready[2], free[2]
+  volatile int* abort = reinterpret_cast<volatile int*>(base + 512);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(base + 516);
+  const uint32_t stages = smem_addr(base + kHeader);
+  const uint32_t full = smem_addr(bars), empty = full + 8 * kStages, ready = empty + 8 * kStages, drained = ready + 16;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int rank = (int)cluster_rank();
+  const int pair = blockIdx.x / 2, pairs = gridDim.x / 2;
+  unsigned int* count = &g_linear_pair_wait_timeouts;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) bar_init(full + 8 * s, 1), bar_init(empty + 8 * s, 1);
+    for (int s = 0; s < 2; ++s) bar_init(ready + 8 * s, 1), bar_init(drained + 8 * s, 2 * kEpilogueWarps);
+    *abort = 0;
+    bar_init_done();
+    prefetch_map(&x_map);
+    prefetch_map(&w_map);
+  }
+  if (warp == 1) tmem_alloc_pair(smem_addr(tmem_slot), kTmemCols);
+  tmem_fence_before();
+  __syncthreads();
+  cluster_sync();  // both CTAs' barriers stand before any is signalled from the other
+  tmem_fence_after();
+  const uint32_t tmem = *tmem_slot;
+
+  if (warp == 0 && lane == 0) {
+    int it = 0;
+    bool ok = true;
+    for (int tile = pair; tile < a.tiles && ok; tile += pairs) {
+      int m0, n0;
+      place(a, tile, &m0, &n0);
+      m0 += rank * 128, n0 += rank * 128;
+      for (int k = 0; k < a.steps; ++k, ++it) {
+        const int s = it % kStages, turn = it / kStages;
+        if (turn > 0 && !(ok = bar_wait(empty + 8 * s, (turn - 1) & 1, abort, count))) break;
+        if (rank == 0) bar_expect(full + 8 * s, 2 * kStageBytes);  // both CTAs' copies count on the first one's barrier
+        const uint32_t bar = peer_smem(full + 8 * s, 0), dst = stages + s * kStageBytes;
+        tma_2d_pair(dst, &x_map, k * kDepth, m0, bar);
+        tma_2d_pair(dst + kHalfBytes, &w_map, k * kDepth, n0, bar);
+      }
+    }
+  } else if (warp == 1 && lane == 0 && rank == 0) {
+    int it = 0, n = 0;
+    bool ok = true;
+    for (int tile = pair; tile < a.tiles && ok; tile += pairs, ++n) {
+      const int acc = n & 1;
+      if (n >= 2 && !(ok = bar_wait(drained + 8 * acc, (n / 2 - 1) & 1, abort, count))) break;
+      tmem_fence_after();
+      for (int k = 0; k < a.steps; ++k, ++it) {
+        const int s = it % kStages, turn = it / kStages;
+        if (!(ok = bar_wait(full + 8 * s, turn & 1, abort, count))) break;
+        tmem_fence_after();
+        const uint32_t src = stages + s * kStageBytes;
+        const uint64_t da = desc_k_major(src), db = desc_k_major(src + kHalfBytes);
+#pragma unroll
+        for (int j = 0; j < kDepth / 16; ++j) mma_ss_pair(tmem + acc * kTileN, da + 2 * j, db + 2 * j, mma_shape(kTileM, kTileN), k > 0 || j > 0);
+        mma_commit_pair(empty + 8 * s);
+      }
+      if (ok) mma_commit_pair(ready + 8 * acc);
+    }
+  } else if (warp >= 4) {
+    const int q = warp % 4, half = (warp - 4) / 4;
+    int n = 0;
+    for (int tile = pair; tile < a.tiles; tile += pairs, ++n) {
+      const int acc = n & 1;
+      int m0, n0;
+      place(a, tile, &m0, &n0);
+      if (!warp_wait(ready + 8 * acc, (n / 2) & 1, abort, count)) break;
+      tmem_fence_after();
+      const int m = m0 + rank * 128 + q * 32 + lane;
+      const uint32_t from = tmem + ((uint32_t)(q * 32) << 16) + acc * kTileN + half * (kTileN / 2);
+#pragma unroll 1
+      for (int c = 0; c < kTileN / 2; c += 32) {
+        uint32_t v[32];
+        tmem_ld32(from + c, v);
+        tmem_wait_ld();
+        if (c + 32 == kTileN / 2) {  // the accumulator has been read
+          tmem_fence_before();
+          __syncwarp();
+          if (lane == 0) bar_arrive_cluster(peer_smem(drained + 8 * acc, 0));
+        }
+        finish32<Out, ACT>(a, m, n0 + half * (kTileN / 2) + c, v);
+      }
+    }
+  }
+  __syncwarp();
+  tmem_fence_before();
+  __syncthreads();
+  drain_if_aborted(abort);
+  cluster_sync();  // neither CTA leaves while the other's copies, products or arrivals may still reach it
+  tmem_fence_after();
+  if (warp == 1) tmem_free_pair(tmem, kTmemCols);
+}
+
+template <typename Out, int ACT>
+cudaError_t launch_act(const PairArgs& t, const CUtensorMap& x, const CUtensorMap& w, const DeviceInfo& dev, cudaStream_t stream) {
+  auto kernel = linear_pair_kernel<Out, ACT>;
+  struct Tag {};
+  const cudaError_t e = ensure_dynamic_smem<Tag>(kernel, dev.ordinal, kSmemBytes);
+  if (e != cudaSuccess) return e;
+  const int pairs = t.tiles < dev.sms / 2 ? t.tiles : dev.sms / 2;
+  kernel<<<2 * pairs, kThreads, kSmemBytes, stream>>>(x, w, t);
+  count_launch();
+  return cudaGetLastError();
+}
+
+template <typename Out>
+cudaError_t launch_out(int act, const PairArgs& t, const CUtensorMap& x, const CUtensorMap& w, const DeviceInfo& dev, cudaStream_t stream) {
+  switch (act) {
+    case APPROXIFER_ACT_RELU: return launch_act<Out, APPROXIFER_ACT_RELU>(t, x, w, dev, stream);
+    case APPROXIFER_ACT_GELU: return launch_act<Out, APPROXIFER_ACT_GELU>(t, x, w, dev, stream);
+    case APPROXIFER_ACT_GELU_TANH: return launch_act<Out, APPROXIFER_ACT_GELU_TANH>(t, x, w, dev, stream);
+    case APPROXIFER_ACT_SILU: return launch_act<Out, APPROXIFER_ACT_SILU>(t, x, w, dev, stream);
+    default: return launch_act<Out, APPROXIFER_ACT_NONE>(t, x, w, dev, stream);
+  }
+}
+
+}  // namespace
+
+cudaError_t read_linear_pair_wait_timeouts(unsigned int* out) { return cudaMemcpyFromSymbol(out, g_linear_pair_wait_timeouts, sizeof(*out)); }
+cudaError_t reset_linear_pair_wait_timeouts() {
+  const unsigned int zero = 0;
+  return cudaMemcpyToSymbol(g_linear_pair_wait_timeouts, &zero, sizeof(zero));
+}
+
+cudaError_t launch_linear_pair(const approxifer_linear_args& a, cudaStream_t stream) {
+  const DeviceInfo* dev;
+  cudaError_t e = current_device_info(&dev);
+  if (e != cudaSuccess) return e;
+  PairArgs t{};
+  t.M = (int32_t)a.M, t.N = (int32_t)a.N, t.K = (int32_t)a.K;
+  t.steps = (int32_t)((a.K + kDepth - 1) / kDepth);
+  const int64_t tm = (a.M + kTileM - 1) / kTileM, tn = (a.N + kTileN - 1) / kTileN;
+  if (tm * tn > 0x3fffffffLL || tn > (1 << 27)) return cudaErrorInvalidConfiguration;
+  t.tiles_m = (int32_t)tm, t.tiles_n = (int32_t)tn, t.tiles = (int32_t)(tm * tn);
+  t.bias = reinterpret_cast<const bf16*>(a.bias), t.R = a.R, t.Y = a.Y, t.r_rstride = a.r_rstride, t.y_rstride = a.y_rstride;
+  const int per = a.out_type == APPROXIFER_TYPE_F32 ? 4 : 8;
+  t.vec = aligned16(a.Y) && a.y_rstride % per == 0 && (!a.R || (aligned16(a.R) && a.r_rstride % per == 0)) && (!a.bias || aligned16(a.bias));
+  const uint64_t xe[2] = {(uint64_t)a.K, (uint64_t)a.M}, xs[2] = {1, (uint64_t)a.x_rstride}, we[2] = {(uint64_t)a.K, (uint64_t)a.N}, ws[2] = {1, (uint64_t)a.w_rstride};
+  const uint32_t box[2] = {(uint32_t)kDepth, 128};
+  CUtensorMap x, w;
+  if ((e = make_tensor_map(&x, a.X, 2, xe, xs, box)) != cudaSuccess || (e = make_tensor_map(&w, a.Wt, 2, we, ws, box)) != cudaSuccess) return e;
+  return a.out_type == APPROXIFER_TYPE_F32 ? launch_out<float>(a.activation, t, x, w, *dev, stream) : launch_out<bf16>(a.activation, t, x, w, *dev, stream);
+}
+
+}  // namespace approxifer

@@ -38,6 +38,11 @@ CASES = [  # M, N, K, bias, activation, residual, out
     (1000, 1000, 160, False, "none", True, torch.float32),
     (2300, 1100, 320, True, "gelu", True, torch.bfloat16),
     (3000, 24, 64, False, "silu", False, torch.bfloat16),
+    (4000, 1100, 320, True, "gelu", True, torch.bfloat16),   # many tiles: pairs of CTAs
+    (4000, 1100, 72, True, "gelu_tanh", False, torch.float32),
+    (2049, 2305, 520, True, "silu", True, torch.float32),
+    (6500, 1029, 136, True, "relu", True, torch.bfloat16),
+    (1800, 3000, 64, False, "none", False, torch.bfloat16),
     (40, 33, 77, True, "gelu", True, torch.bfloat16),      # odd K: rows are not whole 16 bytes
     (300, 65, 13, False, "relu", False, torch.float32),
 ]
@@ -55,7 +60,7 @@ def test_linear_matches_the_plain_form(M, N, K, bias, act, residual, out):
     check(got, want, bound)
 
 
-@pytest.mark.parametrize("M,N,K", [(3, 200, 256), (150, 328, 200), (700, 512, 512)])
+@pytest.mark.parametrize("M,N,K", [(3, 200, 256), (150, 328, 200), (700, 512, 512), (2100, 1800, 200)])
 def test_linear_strides_guards_and_the_residual_in_place(M, N, K):
     x, w, r = normal((M, K), 1), normal((N, K), 2, std=K ** -0.5), normal((M, N), 3)
     want, bound = ref.linear(x, w, None, "none", r, torch.bfloat16)
@@ -79,7 +84,7 @@ def test_linear_strides_guards_and_the_residual_in_place(M, N, K):
 
 
 def test_linear_infinities_and_nan_stay_in_their_rows():
-    for M, N, K in ((5, 140, 128), (300, 200, 128)):
+    for M, N, K in ((5, 140, 128), (300, 200, 128), (2500, 1300, 128)):
         x, w = normal((M, K), 1), normal((N, K), 2, std=K ** -0.5)
         want, bound = ref.linear(x, w, None, "relu", None, torch.bfloat16)
         x[2, 5], x[4, 7] = float("nan"), float("inf")
