@@ -21,6 +21,8 @@ cudaError_t launch_linear_pair(const approxifer_linear_args& a, cudaStream_t str
 cudaError_t read_linear_pair_wait_timeouts(unsigned int* out);
 cudaError_t reset_linear_pair_wait_timeouts();
 cudaError_t launch_norm_rope(const approxifer_norm_rope_args& a, cudaStream_t stream);
+bool attention_token_eligible(const approxifer_attention_args& a);  // see attention_token.cu
+cudaError_t launch_attention_token(const approxifer_attention_args& a, cudaStream_t stream);
 cudaError_t launch_attention(const approxifer_attention_args& a, cudaStream_t stream);
 
 #ifdef __CUDACC__

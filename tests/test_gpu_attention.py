@@ -162,9 +162,11 @@ def test_attention_strides_guards_streams_and_repeatability():
         s = torch.cuda.Stream()
         qd = q.cuda()
         s.wait_stream(torch.cuda.current_stream())
-        y = ap.approxifer_attention(qd, *token_major, *rest, max(qs) + 5, stream=s, **args)
+        y = ap.approxifer_attention(qd, *token_major, *rest, max(qs), stream=s, **args)
         s.synchronize()
         assert torch.equal(y, first)
+        # a looser bound on the queries of a sequence may choose another kernel, with other roundings
+        check(ap.approxifer_attention(qd, *token_major, *rest, max(qs) + 5, **args), want, bound)
         # bases and rows that are not whole 16 bytes
         odd = torch.zeros((T, 4, 131), dtype=torch.bfloat16, device="cuda")
         odd[:, :, 1:129] = q.cuda()
