@@ -450,8 +450,17 @@ typedef struct approxifer_attention_args {
   const int32_t* kv_len;
   uint16_t* out;     /* [T][Hq][D] */
   int64_t o_tstride, o_hstride;
+  void* workspace;   /* device memory, 16-byte aligned, or NULL; free again when the call's work is done */
+  int64_t workspace_bytes;
 } approxifer_attention_args;
 int approxifer_attention(const approxifer_attention_args* args, void* cuda_stream);
+
+/*
+ * Bytes of workspace with which approxifer_attention runs these arguments best (only sizes are read: the pointers, the
+ * workspace among them, may be NULL): large calls of single tokens are cut into equal parts whose results it holds.  0:
+ * none is used.  With less, or none, the call is correct and slower.  Negative: APPROXIFER_E_*.
+ */
+int64_t approxifer_attention_workspace(const approxifer_attention_args* args);
 
 /*
  * Test hook (not on the hot path): the weights the kernels use, computed on

@@ -53,6 +53,7 @@ EXPORTS = (
     "approxifer_linear",
     "approxifer_qk_norm_rope",
     "approxifer_attention",
+    "approxifer_attention_workspace",
 )
 
 
@@ -154,6 +155,8 @@ def load() -> ctypes.CDLL:
     for name in ("approxifer_linear", "approxifer_qk_norm_rope", "approxifer_attention"):  # (packed struct, stream)
         getattr(lib, name).argtypes = [c_char_p, c_void_p]
         getattr(lib, name).restype = c_int
+    lib.approxifer_attention_workspace.argtypes = [c_char_p]
+    lib.approxifer_attention_workspace.restype = c_int64
     del pf, pu, pi
     _lib = lib
     return lib

@@ -56,6 +56,7 @@ __global__ void __launch_bounds__(kElementThreads) attention_element_kernel(cons
 
 cudaError_t launch_attention(const approxifer_attention_args& a, cudaStream_t stream) {
   if (attention_token_eligible(a)) return launch_attention_token(a, stream);
+  if (attention_tile_eligible(a)) return launch_attention_tile(a, stream);
   const int64_t units = a.T * a.Hq, per = kElementThreads / 32;
   const int64_t blocks = (units + per - 1) / per;
   if (blocks > 0x7fffffffLL) return cudaErrorInvalidConfiguration;

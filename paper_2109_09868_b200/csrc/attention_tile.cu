@@ -1,0 +1,512 @@
+// Attention of several tokens per sequence (prompts, chunks of prompts) over a paged cache, on the tensor cores.
+//
+// A CTA takes 256 query rows of one sequence and key head in two tiles of 128: the query heads that share the key head
+// stand side by side (row = token * group + head), so keys and values are read once for all of them.  It walks the tiles of
+// 128 keys that any of its rows sees (the sinks' tiles, then the window's), one pass with the running maximum and sum:
+//
+//   S = Q K^T       128 x 128 fp32 in tensor memory (tcgen05, both operands in shared memory)
+//   P = 2^(S' - m)  a thread owns a row: no shuffles; P (bfloat16) goes back to tensor memory over its S
+//   O += P V        P from tensor memory, V from shared memory as it lies in the cache (MN-major); O fp32 in tensor memory
+//
+// While the tensor cores work for one of the two tiles, the other's softmax runs.  The maximum in use is raised, and O
+// rescaled, only when a row's grows by more than 2^8 (P and O then still fit their types with room to spare; the final
+// division by the sum makes up for it), which after the first tiles is hardly ever.
+//
+//   warps 0-3, 4-7  softmax of tile 0, of tile 1, and their output
+//   warp 8          one lane: tcgen05.mma; allocates the tensor memory
+//   warp 9          tensor-map copies: keys and values by pages, a lane to a page; pages that are not there read as zeros
+//   warps 10, 11    look through the values of tiles that some rows see only in part: a weight of zero must meet no
+//                   infinity or NaN, so such elements are taken out, and where a row does see them the output adds them back
+#include "async.cuh"
+
+namespace approxifer {
+
+__device__ unsigned int g_attention_tile_wait_timeouts = 0;
+
+namespace {
+
+constexpr int kRows = 128;  // query rows per tile
+constexpr int kKeys = 128;  // keys per tile
+constexpr int kThreads = 12 * 32;
+constexpr int kCleanWarps = 2;
+constexpr int kBlock = kRows * 128;  // bytes of 64 columns of a tile
+constexpr float kGrowth = 8.f;       // log2 of what the maximum in use may lag behind
+
+constexpr int tile_bytes(int dp) { return kBlock * (dp / 64); }
+constexpr int stages_of(int dp) { return dp == 64 ? 8 : 5; }
+// Rings of one entry per tile of keys.  An entry is used again only after the products of four tiles before it have been
+// issued (the copies that lead there wait for their stages), and those wait for all that the tile's readers do.
+constexpr int kCleans = 4, kMasks = 8;
+constexpr int smem_bytes(int dp) { return 1024 + 1024 + (2 + stages_of(dp)) * tile_bytes(dp); }
+
+struct TileArgs {
+  approxifer_attention_args a;
+  int32_t group, tokens;  // query heads per key head; tokens per tile (128 / group)
+  int32_t blocks;         // query blocks (of two tiles) per sequence
+  int32_t page_shift;
+};
+
+// What the CTA works on; all roles derive it alike.
+struct Job {
+  int b, hk, token0;   // first token (in the packed array)
+  int left;            // tokens of the sequence from there on
+  int pos0;            // position of the first token (may be negative: fewer cached tokens than queries)
+  int lo, p1;          // lowest position in a window, highest position seen
+  int window, sinks;
+  int tokens;          // per tile
+  int sink_tiles, first_tile, steps;
+
+  __device__ __forceinline__ int tile(int j) const { return j < sink_tiles ? j : first_tile + (j - sink_tiles); }
+  __device__ __forceinline__ int first_pos(int t) const { return pos0 + t * tokens; }
+  __device__ __forceinline__ int last_pos(int t) const { return pos0 + min((t + 1) * tokens, left) - 1; }
+  // does any row of query tile t see any key of tile k; do all of them see all of it
+  __device__ __forceinline__ bool active(int t, int j) const {
+    if (t * tokens >= left) return false;
+    const int k0 = tile(j) * kKeys, k1 = k0 + kKeys - 1;
+    return k0 <= last_pos(t) && (window == 0 || k1 > first_pos(t) - window || k0 < sinks);
+  }
+  __device__ __forceinline__ bool full(int t, int j) const {
+    const int k0 = tile(j) * kKeys, k1 = k0 + kKeys - 1;
+    return k1 <= first_pos(t) && (window == 0 || k0 > last_pos(t) - window || k1 < sinks);
+  }
+};
+
+__device__ __forceinline__ bool find_job(const TileArgs& g, Job* job) {
+  const approxifer_attention_args& a = g.a;
+  // blocks of late queries see most: they come first
+  int x = blockIdx.x;
+  job->hk = x % a.Hkv;
+  x /= a.Hkv;
+  job->b = x % a.batch;
+  const int block = g.blocks - 1 - x / a.batch;
+  const int start = __ldg(a.q_start + job->b), queries = __ldg(a.q_start + job->b + 1) - start, held = __ldg(a.kv_len + job->b);
+  const int skip = block * 2 * g.tokens;
+  if (skip >= queries || start < 0 || (int64_t)start + queries > a.T) return false;
+  job->tokens = g.tokens;
+  job->token0 = start + skip;
+  job->left = queries - skip;
+  job->pos0 = held - queries + skip;
+  job->window = a.window, job->sinks = a.sinks;
+  const int last = job->pos0 + min(2 * g.tokens, job->left) - 1;
+  const int64_t room = a.table_pages << g.page_shift;
+  job->p1 = last < room ? last : (int)(room - 1);
+  job->lo = a.window && job->pos0 >= a.window ? job->pos0 - a.window + 1 : 0;
+  const int seen_sinks = min(min(a.sinks, job->lo), job->p1 + 1);  // sinks before the window
+  job->sink_tiles = seen_sinks > 0 ? (seen_sinks + kKeys - 1) / kKeys : 0;
+  job->first_tile = max(job->lo / kKeys, job->sink_tiles);
+  const int last_tile = job->p1 < 0 ? -1 : job->p1 / kKeys;
+  job->steps = job->p1 < 0 ? 0 : job->sink_tiles + max(0, last_tile - job->first_tile + 1);
+  return true;
+}
+
+__device__ __forceinline__ uint64_t pack2(float lo, float hi) {
+  uint64_t d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi));
+  return d;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ float pow2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+template <int DP>
+__global__ void __launch_bounds__(kThreads, 1)
+    attention_tile_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
+                          const __grid_constant__ TileArgs g) {
+  constexpr int kStages = stages_of(DP);
+  constexpr int kTile = tile_bytes(DP);
+  extern __shared__ unsigned char raw[];
+  unsigned char* base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
+  uint64_t* bars = reinterpret_cast<uint64_t*>(base);
+  volatile int* abort = reinterpret_cast<volatile int*>(base + 512);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(base + 516);
+  volatile int* poison = reinterpret_cast<volatile int*>(base + 520);
+  volatile uint32_t* pages_there = reinterpret_cast<volatile uint32_t*>(base + 576);  // [kMasks]: of tile j at j % kMasks, a bit per page
+  const uint32_t full = smem_addr(bars), empty = full + 8 * kStages, clean = empty + 8 * kStages, q_full = clean + 8 * kCleans, s_ready = q_full + 8,
+                 p_ready = s_ready + 16, o_ready = p_ready + 16;
+  const uint32_t q_at = smem_addr(base + 1024), ring = q_at + 2 * kTile;
+  const approxifer_attention_args& a = g.a;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  unsigned int* count = &g_attention_tile_wait_timeouts;
+
+  Job job;
+  if (!find_job(g, &job)) return;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) bar_init(full + 8 * s, 1), bar_init(empty + 8 * s, 1);
+    for (int s = 0; s < kCleans; ++s) bar_init(clean + 8 * s, kCleanWarps);
+    bar_init(q_full, 1);
+    for (int t = 0; t < 2; ++t) bar_init(s_ready + 8 * t, 1), bar_init(p_ready + 8 * t, 4), bar_init(o_ready + 8 * t, 1);
+    *abort = 0;
+    *poison = 0;
+    bar_init_done();
+    prefetch_map(&q_map);
+    prefetch_map(&k_map);
+    prefetch_map(&v_map);
+  }
+  if (warp == 8) tmem_alloc(smem_addr(tmem_slot), 512);
+  tmem_fence_before();
+  __syncthreads();
+  tmem_fence_after();
+  const uint32_t tmem = *tmem_slot;
+
+  if (warp == 9) {
+    // ---- copies ----
+    if (lane == 0) {
+      const int boxes = (job.tokens < job.left ? 2 : 1) * (DP / 64);  // (a second tile without rows is not read)
+      bar_expect(q_full, boxes * g.group * job.tokens * 128);
+      for (int t = 0; t < 2 && t * job.tokens < job.left; ++t)
+        for (int c = 0; c < DP / 64; ++c) tma_3d(q_at + t * kTile + c * kBlock, &q_map, c * 64, job.hk * g.group, job.token0 + t * job.tokens, q_full);
+    }
+    const int page_rows = 1 << g.page_shift, rows = min(page_rows, kKeys), per_tile = kKeys / rows;
+    const int32_t* table = a.block_table + (int64_t)job.b * a.table_stride;
+    bool ok = true;
+    for (int j = 0; j < job.steps && ok; ++j) {
+      const int k0 = job.tile(j) * kKeys;
+      const int64_t at = (int64_t)(k0 >> g.page_shift) + lane;
+      int32_t page = -1;
+      if (lane < per_tile && at < a.table_pages) page = __ldg(table + at);
+      const bool there = page >= 0 && page < a.num_pages;
+      if (!there) page = (int32_t)a.num_pages;  // beyond the array: zeros
+      const uint32_t mask = __ballot_sync(0xffffffffu, there);
+      const int row = k0 & (page_rows - 1);
+#pragma unroll
+      for (int v = 0; v < 2; ++v) {
+        const int i = 2 * j + v, s = i % kStages, turn = i / kStages;
+        if (turn > 0 && !(ok = warp_wait(empty + 8 * s, (turn - 1) & 1, abort, count))) break;
+        if (lane == 0) {
+          if (v == 0) pages_there[j % kMasks] = mask;
+          bar_expect(full + 8 * s, kTile);
+        }
+        __syncwarp();
+        if (lane < per_tile)
+          for (int c = 0; c < DP / 64; ++c)
+            tma_4d(ring + s * kTile + c * kBlock + lane * rows * 128, v ? &v_map : &k_map, c * 64, row, job.hk, page, full + 8 * s);
+      }
+    }
+  } else if (warp == 8) {
+    // ---- products ----
+    if (lane == 0 && job.steps > 0) {
+      bool ok = bar_wait(q_full, 0, abort, count);
+      int done[2] = {0, 0};  // rounds of the softmax of each tile
+      auto scores = [&](int t, int s) {
+#pragma unroll
+        for (int k = 0; k < DP / 16; ++k)
+          mma_ss(tmem + t * kKeys, desc_k_major(q_at + t * kTile + (k / 4) * kBlock) + 2 * (k % 4), desc_k_major(ring + s * kTile + (k / 4) * kBlock) + 2 * (k % 4),
+                 mma_shape(kRows, kKeys), k > 0);
+        mma_commit(s_ready + 8 * t);
+      };
+      auto wait_full = [&](int i) {
+        const bool got = bar_wait(full + 8 * (i % kStages), (i / kStages) & 1, abort, count);
+        tmem_fence_after();
+        return got;
+      };
+      ok = ok && wait_full(0);
+      if (ok) {
+        for (int t = 0; t < 2; ++t)
+          if (job.active(t, 0)) scores(t, 0);
+        mma_commit(empty);
+      }
+      for (int j = 0; j < job.steps && ok; ++j) {
+        const int vi = 2 * j + 1, vs = vi % kStages, ki = 2 * j + 2, ks = ki % kStages;
+        const bool more = j + 1 < job.steps;
+        if (!(ok = bar_wait(clean + 8 * (j % kCleans), (j / kCleans) & 1, abort, count))) break;
+        if (more && !(ok = wait_full(ki))) break;
+        for (int t = 0; t < 2 && ok; ++t) {
+          if (job.active(t, j)) {
+            if (!(ok = bar_wait(p_ready + 8 * t, done[t] & 1, abort, count))) break;
+            tmem_fence_after();
+#pragma unroll
+            for (int k = 0; k < kKeys / 16; ++k)
+              mma_ts(tmem + 2 * kKeys + t * 128, tmem + t * kKeys + k * 8, desc_mn_major(ring + vs * kTile, kBlock) + k * 128, mma_shape(kRows, DP, true),
+                     done[t] > 0 || k > 0);
+            ++done[t];
+          }
+          if (more && job.active(t, j + 1)) scores(t, ks);
+        }
+        if (!ok) break;
+        mma_commit(empty + 8 * vs);
+        if (more) mma_commit(empty + 8 * ks);
+      }
+      for (int t = 0; t < 2; ++t) mma_commit(o_ready + 8 * t);
+    }
+  } else if (warp >= 10) {
+    // ---- values of tiles that are seen in part ----
+    bool ok = true;
+    for (int j = 0; j < job.steps && ok; ++j) {
+      const int i = 2 * j + 1, s = i % kStages;
+      if (!(ok = warp_wait(full + 8 * s, (i / kStages) & 1, abort, count))) break;
+      const bool part = (job.active(0, j) && !job.full(0, j)) || (job.active(1, j) && !job.full(1, j));
+      if (part) {
+        uint4* v = reinterpret_cast<uint4*>(base + 1024 + (2 + s) * kTile);
+        const int k0 = job.tile(j) * kKeys;
+        for (int x = threadIdx.x - 320; x < kTile / 16; x += kCleanWarps * 32) {
+          uint4 u = v[x];
+          uint32_t w[4] = {u.x, u.y, u.z, u.w};
+          bool bad = false;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if ((w[e] & 0x7f80u) == 0x7f80u) w[e] &= 0xffff0000u, bad = true;
+            if ((w[e] & 0x7f800000u) == 0x7f800000u) w[e] &= 0xffffu, bad = true;
+          }
+          if (bad) {
+            v[x] = make_uint4(w[0], w[1], w[2], w[3]);
+            const int at = k0 + (x / 8) % kKeys;
+            if (at <= job.p1 && (at >= job.lo || at < job.sinks)) *poison = 1;  // (a row of this CTA may see it)
+          }
+        }
+        async_proxy_fence();
+      }
+      __syncwarp();
+      if (lane == 0) bar_arrive(clean + 8 * (j % kCleans));
+    }
+  } else {
+    // ---- softmax and output: one thread, one row ----
+    const int t = warp / 4, r = threadIdx.x % kRows;
+    const uint32_t lanes = (uint32_t)((warp % 4) * 32) << 16;
+    const uint32_t s_at = tmem + lanes + t * kKeys, o_at = tmem + lanes + 2 * kKeys + t * 128;
+    const int in_tile = r / g.group, token = t * job.tokens + in_tile;
+    const bool mine = in_tile < job.tokens && token < job.left;
+    const int pos = job.pos0 + token;
+    const bool flip = a.scale < 0.f;  // the running maximum is that of sign(scale) S
+    // (of a zero scale just enough is left to keep what a row does not see at minus infinity)
+    const float scale = fmaxf(fabsf(a.scale) * 1.4426950408889634f, 1e-37f);
+    float m = -CUDART_INF_F, l = 0.f;
+    int round = 0;
+    bool ok = true;
+    for (int j = 0; j < job.steps; ++j) {
+      if (!job.active(t, j)) continue;
+      if (!(ok = warp_wait(s_ready + 8 * t, round & 1, abort, count))) break;
+      ++round;
+      tmem_fence_after();
+      const uint32_t there = pages_there[j % kMasks];
+      const int per_tile = max(1, kKeys >> g.page_shift);
+      const bool part = !job.full(t, j) || there != (1u << per_tile) - 1u;
+      const int k0 = job.tile(j) * kKeys;
+      const int hi = pos - k0, lo = a.window ? hi - a.window + 1 : 0, sinks = a.window ? a.sinks - k0 : kKeys;
+      // The scores are read twice, 32 at a time -- once for the maximum, once for the weights -- which costs less than the
+      // registers that a whole row takes.
+      auto seen_scores = [&](int c, uint32_t (&v)[32]) {
+        if (flip) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) v[i] ^= 0x80000000u;
+        }
+        if (part) {
+          const int shift = min(g.page_shift, 7);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            const int k = c + i;
+            const bool sees = k <= hi && (k >= lo || k < sinks) && ((there >> (k >> shift)) & 1);
+            v[i] = sees ? v[i] : 0xff800000u;
+          }
+        }
+      };
+      float top = -CUDART_INF_F;
+      uint32_t v0[32], v1[32];
+      tmem_ld32(s_at, v0);
+      tmem_wait_ld(v0);
+#pragma unroll
+      for (int c = 0; c < kKeys; c += 64) {
+        tmem_ld32(s_at + c + 32, v1);
+        seen_scores(c, v0);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) top = fmaxf(top, __uint_as_float(v0[i]));
+        tmem_wait_ld(v1);
+        tmem_ld32(s_at + (c + 64) % kKeys, v0);  // (at the end: the first again)
+        seen_scores(c + 32, v1);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) top = fmaxf(top, __uint_as_float(v1[i]));
+        tmem_wait_ld(v0);
+      }
+      bool grow = false;
+      if (m == -CUDART_INF_F) {
+        m = top;  // (nothing summed yet but zeros)
+      } else if ((top - m) * scale > kGrowth) {
+        grow = true;
+      }
+      if (__any_sync(0xffffffffu, grow)) {
+        const float keep = grow ? pow2((m - top) * scale) : 1.f;
+        if (grow) m = top;
+        l *= keep;
+#pragma unroll 1
+        for (int c = 0; c < DP; c += 16) {
+          uint32_t v[16];
+          tmem_ld16(o_at + c, v);
+          tmem_wait_ld(v);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * keep);
+          tmem_st16(o_at + c, v);
+        }
+      }
+      const float shift_by = m == -CUDART_INF_F ? 0.f : -m * scale;
+      const uint64_t sc2 = pack2(scale, scale), sh2 = pack2(shift_by, shift_by);
+      uint64_t sum2[2] = {0, 0};
+      auto weights = [&](int c, uint32_t (&v)[32]) {  // P takes the place of scores that have been read
+        seen_scores(c, v);
+        uint32_t p[16];
+#pragma unroll
+        for (int i = 0; i < 32; i += 2) {
+          float x, y;
+          unpack2(fma2(pack2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), sc2, sh2), x, y);
+          x = pow2(x), y = pow2(y);
+          sum2[(i / 2) & 1] = add2(sum2[(i / 2) & 1], pack2(x, y));
+          p[i / 2] = pack_bf16x2(x, y);
+        }
+        tmem_st16(s_at + c / 2, p);
+      };
+#pragma unroll
+      for (int c = 0; c < kKeys; c += 64) {
+        tmem_ld32(s_at + c + 32, v1);
+        tmem_wait_ld(v1);
+        weights(c, v0);
+        if (c + 64 < kKeys) {
+          tmem_ld32(s_at + c + 64, v0);
+          tmem_wait_ld(v0);
+        }
+        weights(c + 32, v1);
+      }
+      tmem_wait_st();
+      tmem_fence_before();
+      __syncwarp();
+      if (lane == 0) bar_arrive(p_ready + 8 * t);
+      float u, v;
+      unpack2(add2(sum2[0], sum2[1]), u, v);
+      l += u + v;
+    }
+    bool have = false;
+    if (ok && job.steps > 0) {
+      ok = warp_wait(o_ready + 8 * t, 0, abort, count);
+      have = round > 0;
+      tmem_fence_after();
+    }
+    if (ok) {
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      const bool add_back = *poison != 0;
+      bf16* out = reinterpret_cast<bf16*>(a.out) + (int64_t)(job.token0 + token) * a.o_tstride + (int64_t)(job.hk * g.group + r % g.group) * a.o_hstride;
+#pragma unroll 1
+      for (int c = 0; c < DP; c += 32) {
+        float y[32];
+        if (have) {
+          uint32_t v[32];
+          tmem_ld32(o_at + c, v);
+          tmem_wait_ld(v);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) y[i] = l == 0.f ? 0.f : __uint_as_float(v[i]) * inv;
+        } else {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) y[i] = 0.f;
+        }
+        if (mine && add_back) {
+          // infinities and NaN that were taken out of tiles seen in part, for the rows that do see them
+          const int32_t* table = a.block_table + (int64_t)job.b * a.table_stride;
+#pragma unroll 1
+          for (int j = 0; j < job.steps; ++j) {
+            if ((!job.active(0, j) || job.full(0, j)) && (!job.active(1, j) || job.full(1, j))) continue;
+            const int k0 = job.tile(j) * kKeys;
+#pragma unroll 1
+            for (int k = k0; k < k0 + kKeys && k <= min(pos, job.p1); ++k) {
+              if (a.window && k <= pos - a.window && k >= a.sinks) continue;
+              const int32_t page = __ldg(table + (k >> g.page_shift));
+              if (page < 0 || page >= a.num_pages) continue;
+              const bf16* v = reinterpret_cast<const bf16*>(a.v_cache) + page * a.vc_pstride + job.hk * a.vc_hstride +
+                              (k & ((1 << g.page_shift) - 1)) * a.vc_rstride;
+#pragma unroll
+              for (int i = 0; i < 32; ++i) {
+                const float x = c + i < a.D ? widen(v[c + i]) : 0.f;
+                if (!isfinite(x)) y[i] += x;
+              }
+            }
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 32; i += 8)
+          if (mine && c + i < a.D)
+            *reinterpret_cast<uint4*>(out + c + i) =
+                make_uint4(pack_bf16x2(y[i], y[i + 1]), pack_bf16x2(y[i + 2], y[i + 3]), pack_bf16x2(y[i + 4], y[i + 5]), pack_bf16x2(y[i + 6], y[i + 7]));
+        __syncwarp();
+      }
+    }
+    tmem_fence_before();
+  }
+  __syncwarp();
+  __syncthreads();
+  drain_if_aborted(abort);
+  if (warp == 8) {
+    tmem_fence_after();
+    tmem_free(tmem, 512);
+  }
+}
+
+template <int DP>
+cudaError_t launch_one(const TileArgs& g, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, cudaStream_t stream) {
+  const DeviceInfo* dev;
+  cudaError_t e = current_device_info(&dev);
+  if (e != cudaSuccess) return e;
+  auto kernel = attention_tile_kernel<DP>;
+  struct Tag {};
+  if ((e = ensure_dynamic_smem<Tag>(kernel, dev->ordinal, smem_bytes(DP))) != cudaSuccess) return e;
+  const int64_t ctas = (int64_t)g.blocks * g.a.batch * g.a.Hkv;
+  if (ctas > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
+  kernel<<<(unsigned)ctas, kThreads, smem_bytes(DP), stream>>>(q, k, v, g);
+  count_launch();
+  return cudaGetLastError();
+}
+
+int log2_of(int v) {
+  int s = 0;
+  while ((1 << s) < v) ++s;
+  return (1 << s) == v ? s : -1;
+}
+
+}  // namespace
+
+cudaError_t read_attention_tile_wait_timeouts(unsigned int* out) { return cudaMemcpyFromSymbol(out, g_attention_tile_wait_timeouts, sizeof(*out)); }
+cudaError_t reset_attention_tile_wait_timeouts() {
+  const unsigned int zero = 0;
+  return cudaMemcpyToSymbol(g_attention_tile_wait_timeouts, &zero, sizeof(zero));
+}
+
+bool attention_tile_eligible(const approxifer_attention_args& a) {
+  const int64_t limit = 1LL << 38;
+  return a.D % 8 == 0 && a.D <= 128 && a.Hq / a.Hkv <= kRows && a.num_pages >= 1 && a.page_size >= 8 && log2_of(a.page_size) > 0 &&
+         a.table_pages * a.page_size < (1LL << 30) && aligned16(a.q) && aligned16(a.k_cache) && aligned16(a.v_cache) && aligned16(a.out) &&
+         (a.q_tstride | a.q_hstride | a.o_tstride | a.o_hstride | a.kc_pstride | a.kc_hstride | a.kc_rstride | a.vc_pstride | a.vc_hstride | a.vc_rstride) % 8 == 0 &&
+         a.q_tstride < limit && a.q_hstride < limit && a.kc_pstride < limit && a.kc_hstride < limit && a.kc_rstride < limit && a.vc_pstride < limit &&
+         a.vc_hstride < limit && a.vc_rstride < limit && a.sinks < (1 << 30) && a.window < (1 << 30);
+}
+
+cudaError_t launch_attention_tile(const approxifer_attention_args& a, cudaStream_t stream) {
+  TileArgs g{};
+  g.a = a;
+  g.group = a.Hq / a.Hkv;
+  g.tokens = kRows / g.group;
+  g.blocks = (a.max_q + 2 * g.tokens - 1) / (2 * g.tokens);
+  g.page_shift = log2_of(a.page_size);
+  const int dp = a.D <= 64 ? 64 : 128;
+  CUtensorMap q, k, v;
+  const uint64_t qe[3] = {(uint64_t)a.D, (uint64_t)a.Hq, (uint64_t)a.T}, qs[3] = {1, (uint64_t)a.q_hstride, (uint64_t)a.q_tstride};
+  const uint32_t qb[3] = {64, (uint32_t)g.group, (uint32_t)g.tokens};
+  const uint64_t ce[4] = {(uint64_t)a.D, (uint64_t)a.page_size, (uint64_t)a.Hkv, (uint64_t)a.num_pages};
+  const uint64_t kst[4] = {1, (uint64_t)a.kc_rstride, (uint64_t)a.kc_hstride, (uint64_t)a.kc_pstride};
+  const uint64_t vst[4] = {1, (uint64_t)a.vc_rstride, (uint64_t)a.vc_hstride, (uint64_t)a.vc_pstride};
+  const uint32_t cb[4] = {64, (uint32_t)(a.page_size < kKeys ? a.page_size : kKeys), 1, 1};
+  cudaError_t e;
+  if ((e = make_tensor_map(&q, a.q, 3, qe, qs, qb)) != cudaSuccess || (e = make_tensor_map(&k, a.k_cache, 4, ce, kst, cb)) != cudaSuccess ||
+      (e = make_tensor_map(&v, a.v_cache, 4, ce, vst, cb)) != cudaSuccess)
+    return e;
+  return dp == 64 ? launch_one<64>(g, q, k, v, stream) : launch_one<128>(g, q, k, v, stream);
+}
+
+}  // namespace approxifer

@@ -1,13 +1,18 @@
 // Attention of one token per sequence over a paged cache: every visible key and value is read once, so the call is bound
 // by HBM, and the work is cut along the cache.
 //
-// A cluster of S CTAs takes one (sequence, key head, 16 of the query heads that share it); its visible positions -- the
-// sinks, then the window -- are dealt to the cluster's warps in chunks of 16 keys.  Every WARP is a pipeline of its own:
-// it copies chunks into its private ring (16-byte asynchronous copies, pages looked up one chunk ahead, positions that are
-// not there filled with zeros) and reduces the oldest with mma.m16n8k16 (the query heads are the 16 rows; a tcgen05 tile
-// of 128 rows would be seven eighths padding, and the tensor pipes idle either way), keeping the running maximum and sum of
-// the softmax and the output in fp32 registers.  The warps' results meet in shared memory, the CTAs' in the shared memory
-// of their cluster, each time in a fixed order.
+// One unit of work = (sequence, key head, 16 of the query heads that share it); its visible positions -- the sinks, then
+// the window -- are cut into chunks of 8 KB of keys and values (16 keys up to D = 128, 32 up to D = 64).  Every WARP is a
+// pipeline of its own: it copies chunks into its private ring (16-byte asynchronous copies, pages looked up one chunk ahead,
+// positions that are not there filled with zeros) and reduces the oldest with mma.m16n8k16 (the query heads are the 16
+// rows; a tcgen05 tile of 128 rows would be seven eighths padding, and the tensor pipes idle either way), keeping the
+// running maximum and sum of the softmax and the output in fp32 registers.  Two ways to deal the chunks:
+//
+//   cluster form   a cluster of up to 8 CTAs takes one unit; its warps' results meet in the cluster's shared memory.  One
+//                  launch, no workspace: the form for small calls.
+//   balanced form  all chunks of the call in one row, cut into equal runs, one to each warp that the GPU holds: lengths may
+//                  differ as they like.  A run that covers a whole unit writes its output; the others leave partial sums
+//                  in the workspace, which a second small launch joins, in order.
 #include "async.cuh"
 
 namespace approxifer {
@@ -15,16 +20,19 @@ namespace {
 
 constexpr int kWarps = 4;
 constexpr int kThreads = kWarps * 32;
-constexpr int kKeys = 16;   // keys per chunk
-constexpr int kRows = 16;   // query heads per CTA
+constexpr int kCtasPerSm = 2;
+constexpr int kRows = 16;   // query heads per unit
 constexpr int kStages = 3;
+constexpr int kJoinWarps = 8;
 constexpr unsigned kFull = 0xffffffffu;
 
-constexpr int chunk_bytes(int dp) { return kKeys * dp * 2; }                            // keys, or values, of a chunk
-constexpr int smem_bytes(int dp) { return kWarps * kStages * 2 * chunk_bytes(dp) + 1024; }
-// After the loop the rings hold the results: float o[warp][16][DP], then m[warp][16], l[warp][16].
-static_assert(kWarps * kRows * 128 * 4 + kWarps * kRows * 8 <= kWarps * kStages * 2 * chunk_bytes(128), "results exceed the rings");
-static_assert(kWarps * kRows * 64 * 4 + kWarps * kRows * 8 <= kWarps * kStages * 2 * chunk_bytes(64), "results exceed the rings");
+constexpr int keys_of(int dp) { return dp <= 64 ? 32 : 16; }                 // keys per chunk
+constexpr int half_bytes(int dp) { return keys_of(dp) * dp * 2; }            // keys, or values, of a chunk
+constexpr int ring_bytes(int dp) { return kStages * 2 * half_bytes(dp); }    // of a warp
+constexpr int smem_bytes(int dp) { return kWarps * ring_bytes(dp); }
+// After the loop of the cluster form the rings hold the results: float o[warp][16][DP], then m[warp][16], l[warp][16].
+static_assert(kWarps * kRows * 128 * 4 + kWarps * kRows * 8 <= smem_bytes(128), "results exceed the rings");
+static_assert(kWarps * kRows * 64 * 4 + kWarps * kRows * 8 <= smem_bytes(64), "results exceed the rings");
 
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
@@ -48,65 +56,83 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-template <int DP>
-__global__ void __launch_bounds__(kThreads) attention_token_kernel(const __grid_constant__ approxifer_attention_args a, int row_tiles) {
-  extern __shared__ __align__(1024) unsigned char smem[];
-  constexpr int kCols = DP / 8;  // 16-byte columns of a row
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  const int S = (int)cluster_size(), rank = (int)cluster_rank();
-  int unit = blockIdx.x / S;
-  const int rt = unit % row_tiles;
-  unit /= row_tiles;
-  const int hk = unit % a.Hkv, b = unit / a.Hkv;
-  const int group = a.Hq / a.Hkv, row0 = rt * kRows, rows = min(kRows, group - row0);
-  const int t = __ldg(a.q_start + b), queries = __ldg(a.q_start + b + 1) - t;
-  const bool live = queries == 1 && t >= 0 && t < a.T;  // (max_q = 1; a sequence without a new token has no row)
-
-  // visible positions: 0 .. sinks-1, then first .. last
+// What one sequence's token sees: positions 0 .. sinks-1, then first .. last.
+struct Seen {
+  const int32_t* table;
+  int64_t first, last, sinks, count;
+  int32_t token, chunks;
+};
+// How many positions that is; the token's index, or -1 where the sequence has no new token (max_q = 1).
+__device__ __forceinline__ Seen seen_by(const approxifer_attention_args& a, int b, int keys) {
+  Seen s;
+  const int t = __ldg(a.q_start + b), end = __ldg(a.q_start + b + 1);
+  const bool live = end - t == 1 && t >= 0 && t < a.T;
+  s.token = live ? t : -1;
   const int64_t held = a.table_pages * a.page_size;
   const int64_t p = live ? (int64_t)__ldg(a.kv_len + b) - 1 : -1;
-  const int64_t last = p < held ? p : held - 1;
-  const int64_t first = a.window && p >= a.window ? p - a.window + 1 : 0;
-  const int64_t sinks = a.sinks < first ? a.sinks : first;
-  const int64_t span = last >= first ? last - first + 1 : 0;
-  const int64_t seen = sinks + span;  // (sinks may lie beyond `last` only where the table is too short: masked below)
-  const int chunks = (int)((seen + kKeys - 1) / kKeys);
-  const int32_t* table = a.block_table + (int64_t)b * a.table_stride;
+  s.last = p < held ? p : held - 1;
+  s.first = a.window && p >= a.window ? p - a.window + 1 : 0;
+  s.sinks = a.sinks < s.first ? a.sinks : s.first;
+  // (where the table is shorter than the cache claims to be, sinks may lie beyond `last`: such positions are not there)
+  s.count = live ? s.sinks + (s.last >= s.first ? s.last - s.first + 1 : 0) : 0;
+  s.chunks = (int32_t)((s.count + keys - 1) / keys);
+  s.table = a.block_table + (int64_t)b * a.table_stride;
+  return s;
+}
 
-  unsigned char* ring = smem + warp * (kStages * 2 * chunk_bytes(DP));
-  const uint32_t ring_addr = smem_addr(ring);
-  if (a.D < DP)  // columns beyond D are never copied: zero for good
-    for (int i = lane; i < kStages * 2 * chunk_bytes(DP) / 16; i += 32) reinterpret_cast<uint4*>(ring)[i] = make_uint4(0, 0, 0, 0);
-  __syncwarp();
+// One warp's share of a unit.
+template <int DP>
+struct Warp {
+  static constexpr int kKeys = keys_of(DP);
+  static constexpr int kCols = DP / 8;  // 16-byte columns of a row
+  uint32_t q[DP / 16][4];               // fragments of the 16 x DP queries
+  float o[DP / 8][4];
+  float m[2], l[2];
+  uint32_t ring;
+  int lane;
 
-  // queries: fragments of the 16 x DP matrix, scaled scores are formed after the product
-  uint32_t qf[DP / 16][4];
-  {
-    const bf16* q = reinterpret_cast<const bf16*>(a.q) + (int64_t)t * a.q_tstride + (int64_t)(hk * group + row0) * a.q_hstride;
+  __device__ __forceinline__ void setup(unsigned char* at, int D) {
+    lane = threadIdx.x % 32;
+    ring = smem_addr(at);
+    if (D < DP)  // columns beyond D are never copied: zero for good
+      for (int i = lane; i < ring_bytes(DP) / 16; i += 32) reinterpret_cast<uint4*>(at)[i] = make_uint4(0, 0, 0, 0);
+    __syncwarp();
+  }
+
+  __device__ __forceinline__ void start(const approxifer_attention_args& a, int token, int head0, int rows) {
+    const bf16* from = reinterpret_cast<const bf16*>(a.q) + (int64_t)token * a.q_tstride + (int64_t)head0 * a.q_hstride;
 #pragma unroll
     for (int ks = 0; ks < DP / 16; ++ks)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int r = lane / 4 + (i & 1) * 8, c = ks * 16 + (lane % 4) * 2 + (i >> 1) * 8;
-        qf[ks][i] = (live && r < rows && c < a.D) ? *reinterpret_cast<const uint32_t*>(q + (int64_t)r * a.q_hstride + c) : 0u;
+        q[ks][i] = (token >= 0 && r < rows && c < a.D) ? *reinterpret_cast<const uint32_t*>(from + (int64_t)r * a.q_hstride + c) : 0u;
       }
+#pragma unroll
+    for (int d = 0; d < DP / 8; ++d) o[d][0] = o[d][1] = o[d][2] = o[d][3] = 0.f;
+    m[0] = m[1] = -CUDART_INF_F;
+    l[0] = l[1] = 0.f;
   }
 
-  // lanes 0..15: where the rows of a chunk are (both caches), and which are there at all
-  const int stride = S * kWarps, c0 = rank * kWarps + warp;
-  auto look_up = [&](int c, int64_t* j) -> int32_t {  // page of this lane's position of chunk c, -1 if there is none
-    const int64_t u = (int64_t)c * kKeys + (lane % kKeys);
-    *j = u < sinks ? u : first + (u - sinks);
-    if (c >= chunks || u >= seen || *j > last) return -1;
-    const int32_t page = __ldg(table + *j / a.page_size);
+  // The page of this lane's key (lane % kKeys) of chunk c, -1 if there is none, and its row in the page.
+  __device__ __forceinline__ int32_t look_up(const approxifer_attention_args& a, const Seen& s, int c, int* row) const {
+    const int64_t u = (int64_t)c * kKeys + lane % kKeys;
+    const int64_t j = u < s.sinks ? u : s.first + (u - s.sinks);
+    *row = 0;
+    if (u >= s.count || j > s.last) return -1;
+    const uint32_t page_at = (uint32_t)j / (uint32_t)a.page_size;  // (positions are below 2^31)
+    *row = (int)((uint32_t)j - page_at * (uint32_t)a.page_size);
+    const int32_t page = __ldg(s.table + page_at);
     return page >= 0 && page < a.num_pages ? page : -1;
-  };
-  auto fetch = [&](int slot, int32_t page, int64_t j) -> uint32_t {  // starts the copies of a chunk; which keys are there
-    const uint32_t there = __ballot_sync(kFull, page >= 0) & 0xffffu;
-    const int64_t at = page >= 0 ? j % a.page_size : 0, pg = page >= 0 ? page : 0;
+  }
+
+  // Starts the copies of a chunk; which of its keys are there.
+  __device__ __forceinline__ uint32_t fetch(const approxifer_attention_args& a, int slot, int32_t page, int row_in_page, int hk) const {
+    const uint32_t there = __ballot_sync(kFull, page >= 0);
+    const int64_t pg = page >= 0 ? page : 0, at = page >= 0 ? row_in_page : 0;
     const int64_t ko = pg * a.kc_pstride + at * a.kc_rstride + (int64_t)hk * a.kc_hstride;
     const int64_t vo = pg * a.vc_pstride + at * a.vc_rstride + (int64_t)hk * a.vc_hstride;
-    const uint32_t kdst = ring_addr + slot * 2 * chunk_bytes(DP), vdst = kdst + chunk_bytes(DP);
+    const uint32_t kdst = ring + slot * 2 * half_bytes(DP), vdst = kdst + half_bytes(DP);
 #pragma unroll
     for (int i = 0; i < kKeys * kCols / 32; ++i) {
       const int row = (lane + 32 * i) / kCols, col = (lane + 32 * i) % kCols;
@@ -119,51 +145,31 @@ __global__ void __launch_bounds__(kThreads) attention_token_kernel(const __grid_
       }
     }
     return there;
-  };
-
-  float o[DP / 8][4] = {};
-  float m[2] = {-CUDART_INF_F, -CUDART_INF_F}, l[2] = {0.f, 0.f};
-  const float scale = a.scale * 1.4426950408889634f;  // the softmax runs on powers of two
-  uint32_t there[kStages];
-  int64_t j;
-  int32_t page;
-#pragma unroll
-  for (int s = 0; s < kStages - 1; ++s) {
-    page = look_up(c0 + s * stride, &j);
-    there[s] = fetch(s, page, j);
-    copy_commit();
   }
-  page = look_up(c0 + (kStages - 1) * stride, &j);
-  int slot = 0;
-  for (int c = c0; c < chunks; c += stride) {
-    // `there` and the ring turn together; kStages is small, so the rotation is three moves
-    const uint32_t newest = fetch((slot + kStages - 1) % kStages, page, j);
-    copy_commit();
-    page = look_up(c + kStages * stride, &j);
-    copy_wait<kStages - 1>();
-    __syncwarp();
-    const uint32_t mask = there[0];
-#pragma unroll
-    for (int s = 0; s + 1 < kStages - 1; ++s) there[s] = there[s + 1];
-    there[kStages - 2] = newest;
-    const uint32_t ks_addr = ring_addr + slot * 2 * chunk_bytes(DP), vs_addr = ks_addr + chunk_bytes(DP);
 
-    float s[2][4] = {};
+  // scale: of the scores, times log2 e (the softmax runs on powers of two).
+  __device__ __forceinline__ void reduce(int slot, uint32_t there, float scale) {
+    const uint32_t kat = ring + slot * 2 * half_bytes(DP), vat = kat + half_bytes(DP);
+    float s[kKeys / 8][4];
 #pragma unroll
-    for (int ks = 0; ks < DP / 16; ++ks) {
-      uint32_t kb[4];
-      const int key = (lane / 16) * 8 + lane % 8, col = ks * 2 + (lane / 8) % 2;
-      ldmatrix4(ks_addr + key * DP * 2 + ((col ^ (key & 7)) << 4), kb);
-      mma16816(s[0], qf[ks], kb[0], kb[1]);
-      mma16816(s[1], qf[ks], kb[2], kb[3]);
-    }
+    for (int n = 0; n < kKeys / 8; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < DP / 16; ++ks)
+#pragma unroll
+      for (int n = 0; n < kKeys / 16; ++n) {
+        uint32_t kb[4];
+        const int key = n * 16 + (lane / 16) * 8 + lane % 8, col = ks * 2 + (lane / 8) % 2;
+        ldmatrix4(kat + key * DP * 2 + ((col ^ (key & 7)) << 4), kb);
+        mma16816(s[2 * n], q[ks], kb[0], kb[1]);
+        mma16816(s[2 * n + 1], q[ks], kb[2], kb[3]);
+      }
     float top[2] = {m[0], m[1]};
 #pragma unroll
-    for (int n = 0; n < 2; ++n)
+    for (int n = 0; n < kKeys / 8; ++n)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int key = n * 8 + (lane % 4) * 2 + (i & 1);
-        s[n][i] = (mask >> key) & 1 ? s[n][i] * scale : -CUDART_INF_F;
+        s[n][i] = (there >> key) & 1 ? s[n][i] * scale : -CUDART_INF_F;
         top[i >> 1] = fmaxf(top[i >> 1], s[n][i]);
       }
 #pragma unroll
@@ -179,31 +185,79 @@ __global__ void __launch_bounds__(kThreads) attention_token_kernel(const __grid_
       for (int d = 0; d < DP / 8; ++d) o[d][0] *= keep[0], o[d][1] *= keep[0], o[d][2] *= keep[1], o[d][3] *= keep[1];
       m[0] = top[0], m[1] = top[1];
     }
-    uint32_t pf[4];
 #pragma unroll
-    for (int n = 0; n < 2; ++n) {
-      const float e0 = exp2f(s[n][0] - base[0]), e1 = exp2f(s[n][1] - base[0]), e2 = exp2f(s[n][2] - base[1]), e3 = exp2f(s[n][3] - base[1]);
-      l[0] += e0 + e1, l[1] += e2 + e3;
-      pf[2 * n] = pack_bf16x2(e0, e1), pf[2 * n + 1] = pack_bf16x2(e2, e3);
-    }
+    for (int kk = 0; kk < kKeys / 16; ++kk) {
+      uint32_t p[4];
 #pragma unroll
-    for (int dt = 0; dt < DP / 16; ++dt) {
-      uint32_t vb[4];
-      const int key = lane % 16, col = dt * 2 + lane / 16;
-      ldmatrix4_t(vs_addr + key * DP * 2 + ((col ^ (key & 7)) << 4), vb);
-      mma16816(o[2 * dt], pf, vb[0], vb[1]);
-      mma16816(o[2 * dt + 1], pf, vb[2], vb[3]);
+      for (int n = 0; n < 2; ++n) {
+        const float(&x)[4] = s[2 * kk + n];
+        const float e0 = exp2f(x[0] - base[0]), e1 = exp2f(x[1] - base[0]), e2 = exp2f(x[2] - base[1]), e3 = exp2f(x[3] - base[1]);
+        l[0] += e0 + e1, l[1] += e2 + e3;
+        p[2 * n] = pack_bf16x2(e0, e1), p[2 * n + 1] = pack_bf16x2(e2, e3);
+      }
+#pragma unroll
+      for (int dt = 0; dt < DP / 16; ++dt) {
+        uint32_t vb[4];
+        const int key = kk * 16 + lane % 16, col = dt * 2 + lane / 16;
+        ldmatrix4_t(vat + key * DP * 2 + ((col ^ (key & 7)) << 4), vb);
+        mma16816(o[2 * dt], p, vb[0], vb[1]);
+        mma16816(o[2 * dt + 1], p, vb[2], vb[3]);
+      }
     }
     __syncwarp();  // the slot may be filled again
+  }
+
+  __device__ __forceinline__ void finish() {  // the sums of the rows, from the four lanes that share them
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      l[r] += __shfl_xor_sync(kFull, l[r], 1);
+      l[r] += __shfl_xor_sync(kFull, l[r], 2);
+    }
+  }
+};
+
+template <int DP>
+__global__ void __launch_bounds__(kThreads, kCtasPerSm) attention_token_cluster_kernel(const __grid_constant__ approxifer_attention_args a, int row_tiles) {
+  extern __shared__ __align__(1024) unsigned char smem[];
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int S = (int)cluster_size(), rank = (int)cluster_rank();
+  int unit = blockIdx.x / S;
+  const int rt = unit % row_tiles;
+  unit /= row_tiles;
+  const int hk = unit % a.Hkv, b = unit / a.Hkv;
+  const int group = a.Hq / a.Hkv, head0 = hk * group + rt * kRows, rows = min(kRows, group - rt * kRows);
+  const Seen seen = seen_by(a, b, keys_of(DP));
+  const int stride = S * kWarps, c0 = rank * kWarps + warp;
+
+  Warp<DP> w;
+  w.setup(smem + warp * ring_bytes(DP), a.D);
+  uint32_t there[kStages];
+  int row;
+  int32_t page;
+#pragma unroll
+  for (int s = 0; s < kStages - 1; ++s) {
+    page = w.look_up(a, seen, c0 + s * stride, &row);
+    there[s] = w.fetch(a, s, page, row, hk);
+    copy_commit();
+  }
+  page = w.look_up(a, seen, c0 + (kStages - 1) * stride, &row);
+  w.start(a, seen.token, head0, rows);
+  const float scale = a.scale * 1.4426950408889634f;
+  int slot = 0;
+  for (int c = c0; c < seen.chunks; c += stride) {
+    there[kStages - 1] = w.fetch(a, (slot + kStages - 1) % kStages, page, row, hk);
+    copy_commit();
+    page = w.look_up(a, seen, c + kStages * stride, &row);
+    copy_wait<kStages - 1>();
+    __syncwarp();
+    w.reduce(slot, there[0], scale);
+#pragma unroll
+    for (int s = 0; s + 1 < kStages; ++s) there[s] = there[s + 1];
     slot = (slot + 1) % kStages;
   }
   copy_wait<0>();
-#pragma unroll
-  for (int r = 0; r < 2; ++r) {
-    l[r] += __shfl_xor_sync(kFull, l[r], 1);
-    l[r] += __shfl_xor_sync(kFull, l[r], 2);
-  }
-  // warps -> CTA.  o[16][DP], m[16], l[16] of warp 0's place receive the CTA's result.
+  w.finish();
+  // the warps' results, then every CTA joins its share of the rows' elements over all warps of the cluster, in order
   __syncthreads();
   float* so = reinterpret_cast<float*>(smem);
   float* sm = so + kWarps * kRows * DP;
@@ -211,57 +265,283 @@ __global__ void __launch_bounds__(kThreads) attention_token_kernel(const __grid_
 #pragma unroll
   for (int d = 0; d < DP / 8; ++d)
 #pragma unroll
-    for (int i = 0; i < 4; i += 2) {
-      const int r = lane / 4 + (i / 2) * 8;
-      *reinterpret_cast<float2*>(so + (warp * kRows + r) * DP + d * 8 + (lane % 4) * 2) = make_float2(o[d][i], o[d][i + 1]);
-    }
+    for (int i = 0; i < 4; i += 2)
+      *reinterpret_cast<float2*>(so + (warp * kRows + lane / 4 + i * 4) * DP + d * 8 + (lane % 4) * 2) = make_float2(w.o[d][i], w.o[d][i + 1]);
   if (lane % 4 == 0) {
-    sm[warp * kRows + lane / 4] = m[0], sm[warp * kRows + lane / 4 + 8] = m[1];
-    sl[warp * kRows + lane / 4] = l[0], sl[warp * kRows + lane / 4 + 8] = l[1];
+    sm[warp * kRows + lane / 4] = w.m[0], sm[warp * kRows + lane / 4 + 8] = w.m[1];
+    sl[warp * kRows + lane / 4] = w.l[0], sl[warp * kRows + lane / 4 + 8] = w.l[1];
   }
   __syncthreads();
-  bf16* out = reinterpret_cast<bf16*>(a.out) + (int64_t)t * a.o_tstride + (int64_t)(hk * group + row0) * a.o_hstride;
   if (S > 1) cluster_sync();
-  // every CTA joins its share of the rows' elements over all warps of the cluster, in order
-  const int cells = rows * (a.D / 2), x0 = cells * rank / S, x1 = cells * (rank + 1) / S;
-  const int parts = S * kWarps;
+  bf16* out = reinterpret_cast<bf16*>(a.out) + (int64_t)seen.token * a.o_tstride + (int64_t)head0 * a.o_hstride;
+  const int pairs = a.D / 2, cells = seen.token < 0 ? 0 : rows * pairs, x0 = cells * rank / S, x1 = cells * (rank + 1) / S;
   const uint32_t so_addr = smem_addr(so), sm_addr = smem_addr(sm), sl_addr = smem_addr(sl);
-  for (int x = x0 + threadIdx.x; x < x1 && live; x += kThreads) {
-    const int r = x / (a.D / 2), d = (x % (a.D / 2)) * 2;
-    auto far = [&](uint32_t addr, int part) { return S == 1 ? addr : peer_smem(addr, part / kWarps); };
-    auto get = [&](uint32_t addr) {
-      float v;
-      asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
-      return v;
-    };
+  auto get = [&](uint32_t addr) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    return v;
+  };
+  for (int x = x0 + threadIdx.x; x < x1; x += kThreads) {
+    const int r = x / pairs, d = (x % pairs) * 2;
     float best = -CUDART_INF_F;
-    for (int w = 0; w < parts; ++w) {
-      const float v = get(far(sm_addr + ((w % kWarps) * kRows + r) * 4, w));
-      best = fmaxf(best, v);
-    }
+    for (int p = 0; p < S * kWarps; ++p) best = fmaxf(best, get(peer_smem(sm_addr + ((p % kWarps) * kRows + r) * 4, p / kWarps)));
     if (best == -CUDART_INF_F) best = 0.f;
     float total = 0.f, y0 = 0.f, y1 = 0.f;
-    for (int w = 0; w < parts; ++w) {
-      const int at = (w % kWarps) * kRows + r;
-      const float k = exp2f(get(far(sm_addr + at * 4, w)) - best);
-      total = fmaf(k, get(far(sl_addr + at * 4, w)), total);
-      y0 = fmaf(k, get(far(so_addr + (at * DP + d) * 4, w)), y0);
-      y1 = fmaf(k, get(far(so_addr + (at * DP + d + 1) * 4, w)), y1);
+    for (int p = 0; p < S * kWarps; ++p) {
+      const int at = (p % kWarps) * kRows + r;
+      const float k = exp2f(get(peer_smem(sm_addr + at * 4, p / kWarps)) - best);
+      total = fmaf(k, get(peer_smem(sl_addr + at * 4, p / kWarps)), total);
+      y0 = fmaf(k, get(peer_smem(so_addr + (at * DP + d) * 4, p / kWarps)), y0);
+      y1 = fmaf(k, get(peer_smem(so_addr + (at * DP + d + 1) * 4, p / kWarps)), y1);
     }
     const float inv = total == 0.f ? 0.f : 1.f / total;
-    *reinterpret_cast<uint32_t*>(out + (int64_t)r * a.o_hstride + d) = pack_bf16x2(total == 0.f ? 0.f : y0 * inv, total == 0.f ? 0.f : y1 * inv);
+    *reinterpret_cast<uint32_t*>(out + (int64_t)r * a.o_hstride + d) = total == 0.f ? 0u : pack_bf16x2(y0 * inv, y1 * inv);
   }
   if (S > 1) cluster_sync();  // (a CTA's shared memory stays until all have read it)
 }
 
+// ---- balanced form ----
+
+// Workspace: two partial results for each warp (of a run's first unit, if the run starts inside it, and of its last, if it
+// ends inside it): float o[2 * warps][16][DP], then m, l [2 * warps][16].
+int64_t partial_floats(int dp) { return 2 * kRows * (dp + 2); }
+
+// All chunks of the call stand in a row: sequence after sequence, and of a sequence unit after unit.  The warp that finds a
+// place in the row: the sequence and the number of chunks before it.
+struct Place {
+  int b;
+  int64_t before;
+};
+// Adds up the chunks of all sequences (returned) and finds the one that holds chunk `x`, or, with x < 0, sequence `b_of`.
+__device__ __forceinline__ int64_t count_chunks(const approxifer_attention_args& a, int units, int keys, int64_t x, int b_of, Place* place) {
+  const int lane = threadIdx.x % 32;
+  int64_t total = 0;
+  place->b = -1;
+  place->before = 0;
+  for (int b0 = 0; b0 < a.batch; b0 += 32) {
+    const int b = b0 + lane;
+    const int64_t n = b < a.batch ? (int64_t)seen_by(a, b, keys).chunks * units : 0;
+    int64_t upto = n;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int64_t v = __shfl_up_sync(kFull, upto, d);
+      if (lane >= d) upto += v;
+    }
+    const bool here = x >= 0 ? (total + upto - n <= x && x < total + upto) : b == b_of;
+    const unsigned who = __ballot_sync(kFull, here);
+    if (who) {
+      place->b = b0 + __ffs(who) - 1;
+      place->before = total + __shfl_sync(kFull, upto - n, __ffs(who) - 1);
+    }
+    total += __shfl_sync(kFull, upto, 31);
+  }
+  return total;
+}
+
+// Where a warp stands in the row of chunks.
+struct Cursor {
+  Seen seen;
+  int b, unit, c;  // unit of the sequence: key head and row tile
+  __device__ __forceinline__ void next(const approxifer_attention_args& a, int units, int keys) {
+    if (++c < seen.chunks) return;
+    c = 0;
+    if (++unit < units) return;
+    unit = 0;
+    do {
+      ++b;
+      if (b >= a.batch) break;
+      seen = seen_by(a, b, keys);
+    } while (seen.chunks == 0);
+  }
+};
+
 template <int DP>
-cudaError_t launch_one(const approxifer_attention_args& a, int row_tiles, int64_t units, int split, cudaStream_t stream) {
-  const DeviceInfo* dev;
-  cudaError_t e = current_device_info(&dev);
-  if (e != cudaSuccess) return e;
-  auto kernel = attention_token_kernel<DP>;
+__global__ void __launch_bounds__(kThreads, kCtasPerSm) attention_token_balanced_kernel(const __grid_constant__ approxifer_attention_args a, int row_tiles,
+                                                                                         float* partial) {
+  extern __shared__ __align__(1024) unsigned char smem[];
+  const int warp = blockIdx.x * kWarps + threadIdx.x / 32, warps = gridDim.x * kWarps, lane = threadIdx.x % 32;
+  const int units = a.Hkv * row_tiles, group = a.Hq / a.Hkv;
+  asm volatile("griddepcontrol.launch_dependents;");
+  Place at;
+  const int64_t total = count_chunks(a, units, keys_of(DP), 0, 0, &at);
+  const int runs = total < warps ? (int)total : warps;  // (no empty runs)
+  if (warp >= runs) return;
+  const int64_t x0 = total * warp / runs, x1 = total * (warp + 1) / runs;
+  count_chunks(a, units, keys_of(DP), x0, 0, &at);
+  Cursor get, use;
+  get.b = at.b;
+  get.seen = seen_by(a, at.b, keys_of(DP));
+  get.unit = (int)((x0 - at.before) / get.seen.chunks);
+  get.c = (int)((x0 - at.before) % get.seen.chunks);
+  use = get;
+  int64_t to_get = x1 - x0;
+
+  Warp<DP> w;
+  w.setup(smem + (threadIdx.x / 32) * ring_bytes(DP), a.D);
+  uint32_t there[kStages];
+  int row = 0, hk = 0;
+  int32_t page = -1;
+  auto look_ahead = [&]() {
+    page = -1;
+    if (to_get-- > 0) {
+      page = w.look_up(a, get.seen, get.c, &row);
+      hk = get.unit / row_tiles;
+      if (to_get > 0) get.next(a, units, keys_of(DP));
+    }
+  };
+#pragma unroll
+  for (int s = 0; s < kStages - 1; ++s) {
+    look_ahead();
+    there[s] = w.fetch(a, s, page, row, hk);
+    copy_commit();
+  }
+  look_ahead();
+  const float scale = a.scale * 1.4426950408889634f;
+  int slot = 0;
+  bool from_start = use.c == 0;
+  int head0 = (use.unit / row_tiles) * group + (use.unit % row_tiles) * kRows;
+  int rows = min(kRows, group - (use.unit % row_tiles) * kRows);
+  w.start(a, use.seen.token, head0, rows);
+  for (int64_t x = x0; x < x1; ++x) {
+    there[kStages - 1] = w.fetch(a, (slot + kStages - 1) % kStages, page, row, hk);
+    copy_commit();
+    look_ahead();
+    copy_wait<kStages - 1>();
+    __syncwarp();
+    w.reduce(slot, there[0], scale);
+#pragma unroll
+    for (int s = 0; s + 1 < kStages; ++s) there[s] = there[s + 1];
+    slot = (slot + 1) % kStages;
+    const bool whole = use.c + 1 == use.seen.chunks;
+    if (whole || x + 1 == x1) {  // the end of the unit or of the run
+      w.finish();
+      if (whole && from_start) {
+        const float inv[2] = {w.l[0] == 0.f ? 0.f : 1.f / w.l[0], w.l[1] == 0.f ? 0.f : 1.f / w.l[1]};
+        bf16* out = reinterpret_cast<bf16*>(a.out) + (int64_t)use.seen.token * a.o_tstride + (int64_t)head0 * a.o_hstride;
+#pragma unroll
+        for (int d = 0; d < DP / 8; ++d)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int r = lane / 4 + h * 8, col = d * 8 + (lane % 4) * 2;
+            if (r < rows && col < a.D)
+              *reinterpret_cast<uint32_t*>(out + (int64_t)r * a.o_hstride + col) =
+                  w.l[h] == 0.f ? 0u : pack_bf16x2(w.o[d][2 * h] * inv[h], w.o[d][2 * h + 1] * inv[h]);
+          }
+      } else {
+        const int64_t part = 2 * (int64_t)warp + (from_start ? 1 : 0);
+        float* po = partial + part * kRows * DP;
+        float* pm = partial + 2 * (int64_t)warps * kRows * DP + part * kRows * 2;
+#pragma unroll
+        for (int d = 0; d < DP / 8; ++d)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int r = lane / 4 + h * 8;
+            if (r < rows) *reinterpret_cast<float2*>(po + r * DP + d * 8 + (lane % 4) * 2) = make_float2(w.o[d][2 * h], w.o[d][2 * h + 1]);
+          }
+        if (lane % 4 == 0)
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+            if (lane / 4 + h * 8 < rows) *reinterpret_cast<float2*>(pm + (lane / 4 + h * 8) * 2) = make_float2(w.m[h], w.l[h]);
+      }
+      if (x + 1 < x1) {
+        use.next(a, units, keys_of(DP));
+        from_start = true;
+        head0 = (use.unit / row_tiles) * group + (use.unit % row_tiles) * kRows;
+        rows = min(kRows, group - (use.unit % row_tiles) * kRows);
+        w.start(a, use.seen.token, head0, rows);
+      }
+    } else {
+      ++use.c;
+    }
+  }
+  copy_wait<0>();
+}
+
+// Joins the partial results of every unit that more than one run shares, and zeroes the rows that see nothing.  One CTA =
+// one row; its warps take every JW-th partial result, four loads ahead, and meet in shared memory.
+template <int DP, int JW>
+__global__ void __launch_bounds__(JW * 32) attention_token_join_kernel(const __grid_constant__ approxifer_attention_args a, int row_tiles, int warps,
+                                                                              const float* partial) {
+  __shared__ float sy[JW][DP], sm[JW], sl[JW];
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int units = a.Hkv * row_tiles, group = a.Hq / a.Hkv;
+  const int b = blockIdx.x / a.Hq, h = blockIdx.x % a.Hq, in_group = h % group;
+  Place at;
+  const int64_t total = count_chunks(a, units, keys_of(DP), -1, b, &at);
+  const Seen seen = seen_by(a, b, keys_of(DP));
+  asm volatile("griddepcontrol.wait;" ::: "memory");  // (before any way out: what follows this launch may count on the first kernel's end)
+  if (seen.token < 0) return;
+  bf16* out = reinterpret_cast<bf16*>(a.out) + (int64_t)seen.token * a.o_tstride + (int64_t)h * a.o_hstride;
+  if (seen.chunks == 0) {
+    for (int d = threadIdx.x; d < a.D; d += JW * 32) out[d] = narrow<bf16>(0.f);
+    return;
+  }
+  const int64_t x0 = at.before + (int64_t)((h / group) * row_tiles + in_group / kRows) * seen.chunks, x1 = x0 + seen.chunks;
+  const int64_t runs = total < warps ? total : warps;
+  const int w0 = (int)(((x0 + 1) * runs - 1) / total), w1 = (int)((x1 * runs - 1) / total);  // the runs that hold its first and its last chunk
+  if (w0 == w1) return;
+  const float* pm = partial + 2 * (int64_t)warps * kRows * DP;
+  const int r = in_group % kRows;
+  auto part = [&](int w) { return (2 * (int64_t)w + (w == w0 ? 1 : 0)) * kRows + r; };  // the first of them ends inside the unit
+  float m = -CUDART_INF_F, l = 0.f, y[DP / 32] = {};
+  for (int w = w0 + warp; w <= w1; w += 4 * JW) {
+    float2 ml[4], v[4][DP / 64];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int wi = w + i * JW;
+      const int64_t p = part(wi <= w1 ? wi : w1);
+      ml[i] = __ldcg(reinterpret_cast<const float2*>(pm + p * 2));
+      if (wi > w1) ml[i] = make_float2(-CUDART_INF_F, 0.f);
+#pragma unroll
+      for (int c = 0; c < DP / 64; ++c) v[i][c] = __ldcg(reinterpret_cast<const float2*>(partial + p * DP + c * 64 + lane * 2));
+    }
+    const float top = fmaxf(fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)), m), base = top == -CUDART_INF_F ? 0.f : top;
+    const float keep = exp2f(m - base);
+    l *= keep;
+#pragma unroll
+    for (int c = 0; c < DP / 32; ++c) y[c] *= keep;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (w + i * JW > w1) break;  // (what a row that has only NaN holds must not be scaled by zero)
+      const float k = exp2f(ml[i].x - base);
+      l = fmaf(k, ml[i].y, l);
+#pragma unroll
+      for (int c = 0; c < DP / 64; ++c) y[2 * c] = fmaf(k, v[i][c].x, y[2 * c]), y[2 * c + 1] = fmaf(k, v[i][c].y, y[2 * c + 1]);
+    }
+    m = top;
+  }
+  if (lane == 0) sm[warp] = m, sl[warp] = l;
+#pragma unroll
+  for (int c = 0; c < DP / 64; ++c) *reinterpret_cast<float2*>(&sy[warp][c * 64 + lane * 2]) = make_float2(y[2 * c], y[2 * c + 1]);
+  __syncthreads();
+  float best = sm[0];
+#pragma unroll
+  for (int w = 1; w < JW; ++w) best = fmaxf(best, sm[w]);
+  if (best == -CUDART_INF_F) best = 0.f;
+  for (int d = threadIdx.x; d < a.D; d += JW * 32) {
+    float sum = 0.f, z = 0.f;
+#pragma unroll
+    for (int w = 0; w < JW; ++w) {
+      const float k = exp2f(sm[w] - best);
+      sum = fmaf(k, sl[w], sum);
+      z = fmaf(k, sy[w][d], z);
+    }
+    out[d] = narrow<bf16>(sum == 0.f ? 0.f : z / sum);
+  }
+}
+
+// Chunks the call has at most (the lengths are on the device; the table's width and the window bound them).
+int64_t most_seen(const approxifer_attention_args& a) {
+  const int64_t held = a.table_pages * a.page_size;
+  return a.window && (int64_t)a.window + a.sinks < held ? (int64_t)a.window + a.sinks : held;
+}
+int64_t units_of(const approxifer_attention_args& a) { return (int64_t)a.batch * a.Hkv * ((a.Hq / a.Hkv + kRows - 1) / kRows); }
+template <int DP>
+cudaError_t launch_cluster(const approxifer_attention_args& a, const DeviceInfo& dev, int row_tiles, int64_t units, int split, cudaStream_t stream) {
+  auto kernel = attention_token_cluster_kernel<DP>;
   struct Tag {};
-  if ((e = ensure_dynamic_smem<Tag>(kernel, dev->ordinal, smem_bytes(DP))) != cudaSuccess) return e;
+  cudaError_t e = ensure_dynamic_smem<Tag>(kernel, dev.ordinal, smem_bytes(DP));
+  if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(units * split));
   cfg.blockDim = dim3(kThreads);
@@ -277,6 +557,37 @@ cudaError_t launch_one(const approxifer_attention_args& a, int row_tiles, int64_
   return e;
 }
 
+template <int DP>
+cudaError_t launch_balanced(const approxifer_attention_args& a, const DeviceInfo& dev, int row_tiles, cudaStream_t stream) {
+  auto kernel = attention_token_balanced_kernel<DP>;
+  struct Tag {};
+  cudaError_t e = ensure_dynamic_smem<Tag>(kernel, dev.ordinal, smem_bytes(DP));
+  if (e != cudaSuccess) return e;
+  const int ctas = dev.sms * kCtasPerSm;
+  float* partial = static_cast<float*>(a.workspace);
+  kernel<<<ctas, kThreads, smem_bytes(DP), stream>>>(a, row_tiles, partial);
+  count_launch();
+  if ((e = cudaGetLastError()) != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)((int64_t)a.batch * a.Hq));
+  // a unit's share of the runs: one warp joins a few partial results, eight many
+  const bool few = units_of(a) * 8 >= (int64_t)ctas * kWarps;
+  cfg.blockDim = dim3(few ? 32 : kJoinWarps * 32);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;  // its launch and its counting overlap the first kernel
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  e = cudaLaunchKernelEx(&cfg, few ? attention_token_join_kernel<DP, 1> : attention_token_join_kernel<DP, kJoinWarps>, a, row_tiles, ctas * kWarps,
+                         (const float*)partial);
+  count_launch();
+  return e;
+}
+
+// The balanced form from 128 MB ... on
+bool wants_balance(const approxifer_attention_args& a) { return units_of(a) * most_seen(a) > 512 * 1024 / (a.D <= 64 ? 1 : 2); }
+
 }  // namespace
 
 bool attention_token_eligible(const approxifer_attention_args& a) {
@@ -285,20 +596,27 @@ bool attention_token_eligible(const approxifer_attention_args& a) {
          (a.kc_pstride | a.kc_hstride | a.kc_rstride | a.vc_pstride | a.vc_hstride | a.vc_rstride) % 8 == 0;
 }
 
+int64_t attention_token_workspace(const approxifer_attention_args& a) {
+  const DeviceInfo* dev;
+  if (!wants_balance(a) || current_device_info(&dev) != cudaSuccess) return 0;
+  return (int64_t)dev->sms * kCtasPerSm * kWarps * partial_floats(a.D <= 64 ? 64 : 128) * 4;
+}
+
 cudaError_t launch_attention_token(const approxifer_attention_args& a, cudaStream_t stream) {
   const DeviceInfo* dev;
   const cudaError_t e = current_device_info(&dev);
   if (e != cudaSuccess) return e;
-  const int group = a.Hq / a.Hkv, row_tiles = (group + kRows - 1) / kRows;
-  const int64_t units = (int64_t)a.batch * a.Hkv * row_tiles;
-  // The lengths are on the device; what a sequence can see at most says how far it is worth cutting: until there are
-  // about four CTAs for every place on the GPU, none with less than two chunks for each warp.
-  int64_t most = a.table_pages * a.page_size;
-  if (a.window && (int64_t)a.window + a.sinks < most) most = (int64_t)a.window + a.sinks;
+  const int row_tiles = (a.Hq / a.Hkv + kRows - 1) / kRows;
+  const int64_t need = attention_token_workspace(a);
+  if (need > 0 && a.workspace_bytes >= need && (int64_t)a.batch * a.Hq < (1LL << 31) && (int64_t)a.Hkv * row_tiles < (1LL << 31))
+    return a.D <= 64 ? launch_balanced<64>(a, *dev, row_tiles, stream) : launch_balanced<128>(a, *dev, row_tiles, stream);
+  // Until there are about four CTAs for every place on the GPU, none with less than two chunks for each warp.
+  const int64_t units = units_of(a), most = most_seen(a);
+  const int keys = keys_of(a.D <= 64 ? 64 : 128);
   int split = 1;
-  while (split < 8 && units * split < 4LL * 2 * dev->sms && most >= (int64_t)split * 2 * kWarps * kKeys * 2) split *= 2;
+  while (split < 8 && units * split < 4LL * kCtasPerSm * dev->sms && most >= (int64_t)split * 2 * kWarps * keys * 2) split *= 2;
   if (units * split > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
-  return a.D <= 64 ? launch_one<64>(a, row_tiles, units, split, stream) : launch_one<128>(a, row_tiles, units, split, stream);
+  return a.D <= 64 ? launch_cluster<64>(a, *dev, row_tiles, units, split, stream) : launch_cluster<128>(a, *dev, row_tiles, units, split, stream);
 }
 
 }  // namespace approxifer

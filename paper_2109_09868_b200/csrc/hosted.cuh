@@ -22,7 +22,12 @@ cudaError_t read_linear_pair_wait_timeouts(unsigned int* out);
 cudaError_t reset_linear_pair_wait_timeouts();
 cudaError_t launch_norm_rope(const approxifer_norm_rope_args& a, cudaStream_t stream);
 bool attention_token_eligible(const approxifer_attention_args& a);  // see attention_token.cu
+int64_t attention_token_workspace(const approxifer_attention_args& a);
 cudaError_t launch_attention_token(const approxifer_attention_args& a, cudaStream_t stream);
+bool attention_tile_eligible(const approxifer_attention_args& a);  // see attention_tile.cu
+cudaError_t launch_attention_tile(const approxifer_attention_args& a, cudaStream_t stream);
+cudaError_t read_attention_tile_wait_timeouts(unsigned int* out);
+cudaError_t reset_attention_tile_wait_timeouts();
 cudaError_t launch_attention(const approxifer_attention_args& a, cudaStream_t stream);
 
 #ifdef __CUDACC__

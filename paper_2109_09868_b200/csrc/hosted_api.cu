@@ -13,9 +13,24 @@ int from_cuda(cudaError_t e) { return e == cudaSuccess ? APPROXIFER_OK : APPROXI
 
 }  // namespace
 
+namespace {
+// Everything but the pointers.
+int check_attention(const approxifer_attention_args& a) {
+  if (a.T < 0 || a.T > kMaxExtent || a.batch < 0 || a.max_q < 0 || a.Hq < 1 || a.Hq > 65535 || a.Hkv < 1 || a.D < 1 || a.D > 256) return APPROXIFER_E_RANGE;
+  if (a.page_size < 1 || a.window < 0 || a.sinks < 0 || a.num_pages < 0 || a.num_pages > kMaxExtent || a.table_pages < 0 || a.workspace_bytes < 0)
+    return APPROXIFER_E_RANGE;
+  if (a.q_tstride < 0 || a.q_hstride < a.D || a.o_tstride < 0 || a.o_hstride < a.D || a.kc_rstride < a.D || a.kc_hstride < a.D || a.kc_pstride < a.D ||
+      a.vc_rstride < a.D || a.vc_hstride < a.D || a.vc_pstride < a.D || a.table_stride < 0)
+    return APPROXIFER_E_RANGE;
+  if (a.Hq % a.Hkv != 0 || a.reserved != 0 || !isfinite(a.scale)) return APPROXIFER_E_PARAM;
+  if (a.T > 0 && (a.batch < 1 || a.max_q < 1)) return APPROXIFER_E_RANGE;
+  return APPROXIFER_OK;
+}
+}  // namespace
+
 cudaError_t read_hosted_wait_timeouts(unsigned int* out) {
   *out = 0;
-  for (auto read : {read_linear_tile_wait_timeouts, read_linear_pair_wait_timeouts}) {
+  for (auto read : {read_linear_tile_wait_timeouts, read_linear_pair_wait_timeouts, read_attention_tile_wait_timeouts}) {
     unsigned int n = 0;
     const cudaError_t e = read(&n);
     if (e != cudaSuccess) return e;
@@ -24,7 +39,7 @@ cudaError_t read_hosted_wait_timeouts(unsigned int* out) {
   return cudaSuccess;
 }
 cudaError_t reset_hosted_wait_timeouts() {
-  for (auto reset : {reset_linear_tile_wait_timeouts, reset_linear_pair_wait_timeouts}) {
+  for (auto reset : {reset_linear_tile_wait_timeouts, reset_linear_pair_wait_timeouts, reset_attention_tile_wait_timeouts}) {
     const cudaError_t e = reset();
     if (e != cudaSuccess) return e;
   }
@@ -67,19 +82,20 @@ int approxifer_qk_norm_rope(const approxifer_norm_rope_args* a, void* cuda_strea
   return from_cuda(launch_norm_rope(*a, static_cast<cudaStream_t>(cuda_stream)));
 }
 
+int64_t approxifer_attention_workspace(const approxifer_attention_args* a) {
+  if (a == nullptr) return APPROXIFER_E_NULL;
+  const int rc = check_attention(*a);
+  if (rc) return rc;
+  return a->T > 0 && attention_token_eligible(*a) ? attention_token_workspace(*a) : 0;
+}
+
 int approxifer_attention(const approxifer_attention_args* a, void* cuda_stream) {
   if (a == nullptr) return APPROXIFER_E_NULL;
-  if (a->T < 0 || a->T > kMaxExtent || a->batch < 0 || a->max_q < 0 || a->Hq < 1 || a->Hq > 65535 || a->Hkv < 1 || a->D < 1 || a->D > 256)
-    return APPROXIFER_E_RANGE;
-  if (a->page_size < 1 || a->window < 0 || a->sinks < 0 || a->num_pages < 0 || a->num_pages > kMaxExtent || a->table_pages < 0) return APPROXIFER_E_RANGE;
-  if (a->q_tstride < 0 || a->q_hstride < a->D || a->o_tstride < 0 || a->o_hstride < a->D || a->kc_rstride < a->D || a->kc_hstride < a->D ||
-      a->kc_pstride < a->D || a->vc_rstride < a->D || a->vc_hstride < a->D || a->vc_pstride < a->D || a->table_stride < 0)
-    return APPROXIFER_E_RANGE;
-  if (a->Hq % a->Hkv != 0 || a->reserved != 0 || !isfinite(a->scale)) return APPROXIFER_E_PARAM;
-  if (a->T > 0 && (a->batch < 1 || a->max_q < 1)) return APPROXIFER_E_RANGE;
+  const int rc = check_attention(*a);
+  if (rc) return rc;
   if (a->T == 0) return APPROXIFER_OK;
   if (!a->q || !a->k_cache || !a->v_cache || !a->q_start || !a->kv_len || !a->out || (a->table_pages > 0 && !a->block_table)) return APPROXIFER_E_NULL;
-  if (!whole(a->q, 2) || !whole(a->k_cache, 2) || !whole(a->v_cache, 2) || !whole(a->out, 2)) return APPROXIFER_E_PARAM;
+  if (!whole(a->q, 2) || !whole(a->k_cache, 2) || !whole(a->v_cache, 2) || !whole(a->out, 2) || !whole(a->workspace, 16)) return APPROXIFER_E_PARAM;
   return from_cuda(launch_attention(*a, static_cast<cudaStream_t>(cuda_stream)));
 }
 

@@ -170,7 +170,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
       for (int c = 0; c < kTileN / 2; c += 32) {
         uint32_t v[32];
         tmem_ld32(from + c, v);
-        tmem_wait_ld();
+        tmem_wait_ld(v);
         if (c + 32 == kTileN / 2) {  // the accumulator has been read
           tmem_fence_before();
           __syncwarp();

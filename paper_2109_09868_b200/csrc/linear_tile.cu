@@ -153,7 +153,7 @@ __global__ void __launch_bounds__(kThreads) linear_tile_kernel(const __grid_cons
       for (int c = 0; c < BN; c += 16) {
         uint32_t v[16];
         tmem_ld16(tmem + ((uint32_t)(q * 32) << 16) + c, v);
-        tmem_wait_ld();
+        tmem_wait_ld(v);
         if (step0 == step1) {  // (more CTAs than stages of K: this one has nothing to add)
 #pragma unroll
           for (int j = 0; j < 16; ++j) v[j] = 0;

@@ -21,7 +21,8 @@ ST_POSITION, ST_SLOT = 32, 64
 
 _LINEAR = struct.Struct("@qqqPqPqPPqPqii")
 _NORM_ROPE = struct.Struct("@qiiiiiiPqqPqqPqqPPPqPPqqPqqqPqqqqPifP")
-_ATTENTION = struct.Struct("@qiiiiiiiifiPqqPqqqPqqqqPqqPPPqq")
+_ATTENTION = struct.Struct("@qiiiiiiiifiPqqPqqqPqqqqPqqPPPqqPq")
+_WORKSPACE = struct.Struct("@Pq")  # the last two fields of the attention arguments
 
 _entry = {}
 
@@ -153,8 +154,12 @@ def approxifer_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.
     tp = _check(block_table, torch.int32, (batch, table_pages), "block_table", dev)
     sp, lp = _vector(q_start, torch.int32, batch + 1, "q_start", dev), _vector(kv_len, torch.int32, batch, "kv_len", dev)
     qs, ks, vs, os = q.stride(), k_cache.stride(), v_cache.stride(), out.stride()
-    _call("approxifer_attention",
-          _ATTENTION.pack(T, batch, max_q, Hq, Hkv, D, page, window, sinks, 1 / math.sqrt(D) if scale is None else scale, 0, qp, qs[0], qs[1],
-                          kp, ks[0], ks[1], ks[2], vp, vs[0], vs[1], vs[2], pages, tp, block_table.stride(0), table_pages, sp, lp, op, os[0], os[1]),
-          dev, stream)
+    packed = _ATTENTION.pack(T, batch, max_q, Hq, Hkv, D, page, window, sinks, 1 / math.sqrt(D) if scale is None else scale, 0, qp, qs[0], qs[1],
+                             kp, ks[0], ks[1], ks[2], vp, vs[0], vs[1], vs[2], pages, tp, block_table.stride(0), table_pages, sp, lp, op, os[0], os[1], 0, 0)
+    if max_q == 1:
+        need = load().approxifer_attention_workspace(packed)
+        if need > 0:
+            room = _new((need,), q, torch.uint8, stream)
+            packed = packed[:-_WORKSPACE.size] + _WORKSPACE.pack(room.data_ptr(), need)
+    _call("approxifer_attention", packed, dev, stream)
     return out

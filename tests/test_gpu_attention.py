@@ -56,6 +56,9 @@ CASES = [  # queries, cached tokens, Hq, Hkv, D, page, window, sinks
     ([1, 1], [0, 40], 4, 2, 64, 16, 8, 2),     # a sequence with nothing cached: its row is zero
     ([1, 1], [130, 260], 2, 2, 40, 16, 1, 0),  # a window of the token itself
     ([1], [260], 2, 1, 64, 16, 100, 300),      # more sinks than tokens before the window
+    ([1] * 40, [37 * i for i in range(40)], 4, 1, 64, 16, 0, 0),                # many sequences of all lengths, the first empty
+    ([1] * 35, [1 + 61 * (i % 7) for i in range(35)], 2, 2, 128, 8, 90, 3),
+    ([1, 0, 1, 1], [300, 50, 0, 4100], 20, 1, 64, 64, 0, 0),                    # a sequence without a new token; two row tiles
     # prompts and chunks
     ([5], [5], 1, 1, 64, 16, 0, 0),
     ([130], [130], 4, 2, 128, 16, 0, 0),
@@ -172,6 +175,22 @@ def test_attention_strides_guards_streams_and_repeatability():
         odd[:, :, 1:129] = q.cuda()
         yo = torch.zeros((T, 4, 129), dtype=torch.bfloat16, device="cuda")
         check(ap.approxifer_attention(odd[:, :, 1:129], *token_major, *rest, max(qs), out=yo[:, :, 1:], **args), want, bound)
+
+
+@pytest.mark.parametrize("D,Hq,Hkv", [(128, 4, 1), (64, 20, 1), (96, 2, 2)])
+def test_attention_single_tokens_with_and_without_workspace(D, Hq, Hkv):
+    """The balanced form (with the workspace the library asks for) and the cluster form (without) agree with the plain form.  The
+    table is much wider than the sequences are long, so that the library expects a large call."""
+    kvs = [5, 700, 0, 333, 64, 1, 1500, 16, 15, 17, 800]
+    q, k, v, table, start, lens = inputs([1] * len(kvs), kvs, Hq, Hkv, D, 16, seed=D)
+    wide = torch.full((len(kvs), 8192), -1, dtype=torch.int32)
+    wide[:, : table.shape[1]] = table
+    for window, sinks in ((0, 0), (200, 4)):
+        want, bound = ref.attention(q, k, v, table, start, lens, window, sinks, D ** -0.5)
+        check(run((q, k, v, table, start, lens), 1, window, sinks, D ** -0.5), want, bound)
+        got = run((q, k, v, wide, start, lens), 1, window, sinks, D ** -0.5)
+        check(got, want, bound)
+        assert torch.equal(got, run((q, k, v, wide, start, lens), 1, window, sinks, D ** -0.5))
 
 
 def test_attention_of_no_tokens():

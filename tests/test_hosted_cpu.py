@@ -42,17 +42,18 @@ def test_norm_rope_refusals():
 
 
 def attention_rc(T=3, batch=1, max_q=3, Hq=4, Hkv=2, D=8, page=8, window=0, sinks=0, scale=1.0, reserved=0, q=16, qs=(32, 8), kc=16, kcs=(128, 64, 8), vc=16,
-                 vcs=(128, 64, 8), pages=5, table=16, ts=4, tp=4, start=16, lens=16, out=16, os=(32, 8)):
+                 vcs=(128, 64, 8), pages=5, table=16, ts=4, tp=4, start=16, lens=16, out=16, os=(32, 8),
+                 ws=0, wb=0):
     return ap.load().approxifer_attention(hosted._ATTENTION.pack(
-        T, batch, max_q, Hq, Hkv, D, page, window, sinks, scale, reserved, q, *qs, kc, *kcs, vc, *vcs, pages, table, ts, tp, start, lens, out, *os), None)
+        T, batch, max_q, Hq, Hkv, D, page, window, sinks, scale, reserved, q, *qs, kc, *kcs, vc, *vcs, pages, table, ts, tp, start, lens, out, *os, ws, wb), None)
 
 
 def test_attention_refusals():
     assert attention_rc(T=0, batch=0, q=0, kc=0, vc=0, out=0) == binding.OK
     for bad in (dict(T=-1), dict(batch=0), dict(max_q=0), dict(Hq=0), dict(Hkv=0), dict(D=0), dict(D=257), dict(page=0), dict(window=-1), dict(sinks=-1),
-                dict(pages=-1), dict(tp=-1), dict(qs=(32, 7)), dict(os=(-32, 8)), dict(kcs=(128, 64, 7)), dict(vcs=(128, 7, 8)), dict(ts=-4)):
+                dict(pages=-1), dict(tp=-1), dict(qs=(32, 7)), dict(os=(-32, 8)), dict(kcs=(128, 64, 7)), dict(vcs=(128, 7, 8)), dict(ts=-4), dict(wb=-1)):
         assert attention_rc(**bad) == binding.E_RANGE, bad
-    for bad in (dict(Hq=5), dict(scale=float("nan")), dict(scale=float("inf")), dict(reserved=1), dict(q=17), dict(vc=17)):
+    for bad in (dict(Hq=5), dict(scale=float("nan")), dict(scale=float("inf")), dict(reserved=1), dict(q=17), dict(vc=17), dict(ws=8, wb=64)):
         assert attention_rc(**bad) == binding.E_PARAM, bad
     for bad in (dict(q=0), dict(kc=0), dict(vc=0), dict(table=0), dict(start=0), dict(lens=0), dict(out=0)):
         assert attention_rc(**bad) == binding.E_NULL, bad
@@ -63,7 +64,7 @@ def test_packed_structs_are_as_long_as_the_header_says():
     # eight bytes a pointer or 64-bit integer, four the others
     assert hosted._LINEAR.size == 12 * 8 + 2 * 4
     assert hosted._NORM_ROPE.size == 29 * 8 + 8 * 4
-    assert hosted._ATTENTION.size == 21 * 8 + 10 * 4
+    assert hosted._ATTENTION.size == 23 * 8 + 10 * 4
     assert ctypes.sizeof(ctypes.c_void_p) == 8
 
 
