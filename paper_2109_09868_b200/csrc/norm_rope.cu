@@ -74,18 +74,201 @@ __global__ void __launch_bounds__(kElementThreads) norm_rope_element_kernel(cons
   }
 }
 
-}  // namespace
+// The path for whole 16-byte columns: one pass over HBM.  A head's row is spread over L lanes (the power of two that holds
+// its columns), a warp takes 32 / L rows at a time and up to kAhead of those in one go, all of one token and of one kind
+// (queries, keys or values), so that the cosines, sines and weights are read once for many rows:
+//     y_d = r (x_d A_d + x_p(d) B_d),    A_d = w_d cos,  B_d = -+ w_p(d) sin,   p(d) the other element of d's pair,
+// with r the reciprocal root mean square of the row.  The pair's other element comes from another lane (halves) or from
+// the lane's own column (neighbouring pairs).  All rows' loads are in flight before the first is used.
+constexpr int kThreads = 256;
+constexpr int kAhead = 8;
 
-cudaError_t launch_norm_rope(const approxifer_norm_rope_args& a, cudaStream_t stream) {
+template <typename T>
+struct Column;
+template <>
+struct Column<bf16> {
+  static constexpr int kElems = 8;
+  static __device__ __forceinline__ void widen8(const uint4& u, float (&x)[8]) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(w[i] << 16), x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+  static __device__ __forceinline__ uint4 narrow8(const float (&x)[8]) {
+    return make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+  }
+};
+template <>
+struct Column<float> {
+  static constexpr int kElems = 4;
+  static __device__ __forceinline__ void widen8(const uint4& u, float (&x)[4]) {
+    x[0] = __uint_as_float(u.x), x[1] = __uint_as_float(u.y), x[2] = __uint_as_float(u.z), x[3] = __uint_as_float(u.w);
+  }
+  static __device__ __forceinline__ uint4 narrow8(const float (&x)[4]) {
+    return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+  }
+};
+
+template <typename T, int L>
+__global__ void __launch_bounds__(kThreads) norm_rope_kernel(const __grid_constant__ approxifer_norm_rope_args a, int q_units, int kv_units) {
+  constexpr int E = Column<T>::kElems, kSide = 32 / L;  // elements of a column, rows side by side
+  const int lane = threadIdx.x % 32, at = lane % L, side = lane / L;
+  const int units = q_units + (a.k ? kv_units : 0) + (a.v ? kv_units : 0);
+  const int64_t u = (int64_t)blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
+  if (u >= a.T * units) return;
+  const int64_t t = a.T < (1 << 24) && units < 128 ? (uint32_t)u / (uint32_t)units : u / units;
+  int unit = (int)(u - t * units);
+  const bool is_q = unit < q_units, is_k = !is_q && a.k && unit < q_units + kv_units;
+  const bool head_unit = unit == 0;
+  unit -= is_q ? 0 : is_k || !a.k ? q_units : q_units + kv_units;
+  const int heads = is_q ? a.Hq : a.Hkv, h0 = unit * (kSide * kAhead) + side;
+  const T* in = is_q ? static_cast<const T*>(a.q) + t * a.q_tstride : is_k ? static_cast<const T*>(a.k) + t * a.k_tstride : static_cast<const T*>(a.v) + t * a.v_tstride;
+  const int64_t in_h = is_q ? a.q_hstride : is_k ? a.k_hstride : a.v_hstride;
+  const int d0 = at * E;
+  const bool live = d0 < a.D;
+  uint4 x[kAhead];
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) {
+    const int h = h0 + i * kSide;
+    x[i] = live && h < heads ? __ldcs(reinterpret_cast<const uint4*>(in + h * in_h + d0)) : make_uint4(0, 0, 0, 0);
+  }
+  const int32_t pos = a.rot ? __ldg(a.positions + t) : 0;
+  const bool placed = a.rot == 0 || (pos >= 0 && pos < a.positions_max);
+  const int64_t slot = a.slots ? __ldg(a.slots + t) : -1;
+  const bool fits = slot < a.num_pages * a.page_size;
+  if (head_unit && lane == 0 && a.status) a.status[t] = (placed ? 0u : APPROXIFER_ST_POSITION) | (fits ? 0u : APPROXIFER_ST_SLOT);
+
+  T* out;
+  int64_t out_h;
+  if (is_q) {
+    out = static_cast<T*>(a.q_out) + t * a.qo_tstride;
+    out_h = a.qo_hstride;
+  } else {
+    if (!placed || !fits || slot < 0) return;
+    int64_t page, row;
+    if (slot < (1LL << 31)) {
+      page = (uint32_t)slot / (uint32_t)a.page_size;
+      row = (uint32_t)slot - (uint32_t)page * (uint32_t)a.page_size;
+    } else {
+      page = slot / a.page_size;
+      row = slot % a.page_size;
+    }
+    out = is_k ? static_cast<T*>(a.k_cache) + page * a.kc_pstride + row * a.kc_rstride : static_cast<T*>(a.v_cache) + page * a.vc_pstride + row * a.vc_rstride;
+    out_h = is_k ? a.kc_hstride : a.vc_hstride;
+  }
+  if (!is_q && !is_k) {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int h = h0 + i * kSide;
+      if (live && h < heads) *reinterpret_cast<uint4*>(out + h * out_h + d0) = x[i];
+    }
+    return;
+  }
+
+  // A, B of this lane's elements, and the lane that holds their pairs
+  const T* weight = static_cast<const T*>(is_q ? a.q_weight : a.k_weight);
+  const int half = a.rot / 2;
+  const bool turned = placed && d0 < a.rot, second = d0 >= half;
+  const int partner = (turned && !a.interleaved) ? (second ? d0 - half : d0 + half) : d0;
+  const int from = side * L + partner / E;
+  float A[E], B[E];
+  {
+    float w[E], wp[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) w[e] = wp[e] = 1.f;
+    if (weight && live) {
+      Column<T>::widen8(__ldg(reinterpret_cast<const uint4*>(weight + d0)), w);
+      Column<T>::widen8(__ldg(reinterpret_cast<const uint4*>(weight + partner)), wp);
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) A[e] = w[e], B[e] = 0.f;
+    if (turned) {
+      const float* cs = a.cos_sin + (int64_t)pos * a.rot + (a.interleaved ? d0 / 2 : second ? d0 - half : d0);
+      if (a.interleaved) {
+#pragma unroll
+        for (int e = 0; e < E; e += 2) {
+          const float c = __ldg(cs + e / 2), s = __ldg(cs + half + e / 2);
+          A[e] = w[e] * c, A[e + 1] = w[e + 1] * c;
+          B[e] = -wp[e + 1] * s, B[e + 1] = wp[e] * s;
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; e += 4) {
+          const float4 c = __ldg(reinterpret_cast<const float4*>(cs + e)), s = __ldg(reinterpret_cast<const float4*>(cs + half + e));
+          const float sign = second ? 1.f : -1.f;
+          A[e] = w[e] * c.x, A[e + 1] = w[e + 1] * c.y, A[e + 2] = w[e + 2] * c.z, A[e + 3] = w[e + 3] * c.w;
+          B[e] = sign * wp[e] * s.x, B[e + 1] = sign * wp[e + 1] * s.y, B[e + 2] = sign * wp[e + 2] * s.z, B[e + 3] = sign * wp[e + 3] * s.w;
+        }
+      }
+    }
+  }
+  const float inv_d = 1.f / (float)a.D;
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) {
+    const int h = h0 + i * kSide;
+    if (h - side >= heads) break;  // (the whole warp)
+    float v[E], p[E], sq = 0.f;
+    Column<T>::widen8(x[i], v);
+#pragma unroll
+    for (int e = 0; e < E; ++e) sq = fmaf(v[e], v[e], sq);
+#pragma unroll
+    for (int d = L / 2; d > 0; d >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, d);
+    const float r = weight ? rsqrtf(sq * inv_d + a.eps) : 1.f;
+    if (a.interleaved) {
+#pragma unroll
+      for (int e = 0; e < E; e += 2) p[e] = v[e + 1], p[e + 1] = v[e];
+    } else {
+      uint4 other;
+      other.x = __shfl_sync(0xffffffffu, x[i].x, from), other.y = __shfl_sync(0xffffffffu, x[i].y, from);
+      other.z = __shfl_sync(0xffffffffu, x[i].z, from), other.w = __shfl_sync(0xffffffffu, x[i].w, from);
+      Column<T>::widen8(other, p);
+    }
+    // (an element that is not turned has no part in its pair, even where that is infinite)
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = placed ? r * (turned ? fmaf(v[e], A[e], p[e] * B[e]) : v[e] * A[e]) : 0.f;
+    if (live && h < heads) *reinterpret_cast<uint4*>(out + h * out_h + d0) = Column<T>::narrow8(v);
+  }
+}
+
+template <typename T>
+bool columns_fit(const approxifer_norm_rope_args& a) {
+  constexpr int E = Column<T>::kElems;
+  const int64_t strides = a.q_tstride | a.q_hstride | a.qo_tstride | a.qo_hstride | (a.k ? a.k_tstride | a.k_hstride | a.kc_pstride | a.kc_hstride | a.kc_rstride : 0) |
+                          (a.v ? a.v_tstride | a.v_hstride | a.vc_pstride | a.vc_hstride | a.vc_rstride : 0);
+  return a.D % E == 0 && a.D / E <= 32 && (a.interleaved ? a.rot % E == 0 : a.rot % (2 * E) == 0) && strides % E == 0 && aligned16(a.q) && aligned16(a.q_out) &&
+         aligned16(a.k) && aligned16(a.v) && aligned16(a.k_cache) && aligned16(a.v_cache) && aligned16(a.q_weight) && aligned16(a.k_weight) && aligned16(a.cos_sin);
+}
+
+template <typename T, int L>
+cudaError_t launch_columns(const approxifer_norm_rope_args& a, cudaStream_t stream) {
+  constexpr int kRowsPerUnit = (32 / L) * kAhead;
+  const int q_units = (a.Hq + kRowsPerUnit - 1) / kRowsPerUnit, kv_units = (a.Hkv + kRowsPerUnit - 1) / kRowsPerUnit;
+  const int64_t warps = a.T * (q_units + (a.k ? kv_units : 0) + (a.v ? kv_units : 0)), blocks = (warps + kThreads / 32 - 1) / (kThreads / 32);
+  if (blocks > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
+  norm_rope_kernel<T, L><<<(unsigned)blocks, kThreads, 0, stream>>>(a, q_units, kv_units);
+  count_launch();
+  return cudaGetLastError();
+}
+
+template <typename T>
+cudaError_t launch_type(const approxifer_norm_rope_args& a, cudaStream_t stream) {
+  if (columns_fit<T>(a)) {
+    const int columns = a.D / Column<T>::kElems;
+    if (columns <= 8) return launch_columns<T, 8>(a, stream);
+    if (columns <= 16) return launch_columns<T, 16>(a, stream);
+    return launch_columns<T, 32>(a, stream);
+  }
   const int64_t units = a.T * (a.Hq + 2 * a.Hkv), per = kElementThreads / 32;
   const int64_t blocks = (units + per - 1) / per;
   if (blocks > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
-  if (a.type == APPROXIFER_TYPE_F32)
-    norm_rope_element_kernel<float><<<(unsigned)blocks, kElementThreads, 0, stream>>>(a);
-  else
-    norm_rope_element_kernel<bf16><<<(unsigned)blocks, kElementThreads, 0, stream>>>(a);
+  norm_rope_element_kernel<T><<<(unsigned)blocks, kElementThreads, 0, stream>>>(a);
   count_launch();
   return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_norm_rope(const approxifer_norm_rope_args& a, cudaStream_t stream) {
+  return a.type == APPROXIFER_TYPE_F32 ? launch_type<float>(a, stream) : launch_type<bf16>(a, stream);
 }
 
 }  // namespace approxifer
