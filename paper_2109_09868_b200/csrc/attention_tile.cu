@@ -65,11 +65,28 @@ struct Job {
     const int k0 = tile(j) * kKeys, k1 = k0 + kKeys - 1;
     return k0 <= last_pos(t) && (window == 0 || k1 > first_pos(t) - window || k0 < sinks);
   }
+  // which of the 32 keys from position k on the row at `pos` sees, a bit per key
+  __device__ __forceinline__ uint32_t sees(int pos, int k) const {
+    auto below = [](int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; };  // bits 0 .. n-1
+    const uint32_t past = below(pos + 1 - k);
+    return window == 0 ? past : past & (~below(pos + 1 - window - k) | below(sinks - k));
+  }
   __device__ __forceinline__ bool full(int t, int j) const {
     const int k0 = tile(j) * kKeys, k1 = k0 + kKeys - 1;
     return k1 <= first_pos(t) && (window == 0 || k0 > last_pos(t) - window || k1 < sinks);
   }
 };
+
+// The page bits of a tile, spread over its 32 keys from column c on.
+__device__ __forceinline__ uint32_t pages_of(uint32_t there, int c, int page_shift) {
+  if (page_shift >= 7) return there ? 0xffffffffu : 0u;
+  if (page_shift >= 5) return (there >> (c >> page_shift)) & 1 ? 0xffffffffu : 0u;
+  uint32_t bits = 0;
+  const int rows = 1 << page_shift;
+  for (int q = 0; q < 32; q += rows)
+    if ((there >> ((c + q) >> page_shift)) & 1) bits |= ((1u << rows) - 1u) << q;
+  return bits;
+}
 
 __device__ __forceinline__ bool find_job(const TileArgs& g, Job* job) {
   const approxifer_attention_args& a = g.a;
@@ -115,6 +132,11 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
 }
+__device__ __forceinline__ float max3(float a, float b, float c) {  // (a NaN is passed over; it makes its row NaN as a weight)
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
 __device__ __forceinline__ float pow2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -135,7 +157,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   volatile int* poison = reinterpret_cast<volatile int*>(base + 520);
   volatile uint32_t* pages_there = reinterpret_cast<volatile uint32_t*>(base + 576);  // [kMasks]: of tile j at j % kMasks, a bit per page
   const uint32_t full = smem_addr(bars), empty = full + 8 * kStages, clean = empty + 8 * kStages, q_full = clean + 8 * kCleans, s_ready = q_full + 8,
-                 p_ready = s_ready + 16, o_ready = p_ready + 16;
+                 p_ready = s_ready + 16, o_ready = p_ready + 32;
   const uint32_t q_at = smem_addr(base + 1024), ring = q_at + 2 * kTile;
   const approxifer_attention_args& a = g.a;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -148,7 +170,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int s = 0; s < kStages; ++s) bar_init(full + 8 * s, 1), bar_init(empty + 8 * s, 1);
     for (int s = 0; s < kCleans; ++s) bar_init(clean + 8 * s, kCleanWarps);
     bar_init(q_full, 1);
-    for (int t = 0; t < 2; ++t) bar_init(s_ready + 8 * t, 1), bar_init(p_ready + 8 * t, 4), bar_init(o_ready + 8 * t, 1);
+    for (int t = 0; t < 2; ++t) bar_init(s_ready + 8 * t, 1), bar_init(p_ready + 16 * t, 4), bar_init(p_ready + 16 * t + 8, 4), bar_init(o_ready + 8 * t, 1);
     *abort = 0;
     *poison = 0;
     bar_init_done();
@@ -162,117 +184,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   tmem_fence_after();
   const uint32_t tmem = *tmem_slot;
 
-  if (warp == 9) {
-    // ---- copies ----
-    if (lane == 0) {
-      const int boxes = (job.tokens < job.left ? 2 : 1) * (DP / 64);  // (a second tile without rows is not read)
-      bar_expect(q_full, boxes * g.group * job.tokens * 128);
-      for (int t = 0; t < 2 && t * job.tokens < job.left; ++t)
-        for (int c = 0; c < DP / 64; ++c) tma_3d(q_at + t * kTile + c * kBlock, &q_map, c * 64, job.hk * g.group, job.token0 + t * job.tokens, q_full);
-    }
-    const int page_rows = 1 << g.page_shift, rows = min(page_rows, kKeys), per_tile = kKeys / rows;
-    const int32_t* table = a.block_table + (int64_t)job.b * a.table_stride;
-    bool ok = true;
-    for (int j = 0; j < job.steps && ok; ++j) {
-      const int k0 = job.tile(j) * kKeys;
-      const int64_t at = (int64_t)(k0 >> g.page_shift) + lane;
-      int32_t page = -1;
-      if (lane < per_tile && at < a.table_pages) page = __ldg(table + at);
-      const bool there = page >= 0 && page < a.num_pages;
-      if (!there) page = (int32_t)a.num_pages;  // beyond the array: zeros
-      const uint32_t mask = __ballot_sync(0xffffffffu, there);
-      const int row = k0 & (page_rows - 1);
-#pragma unroll
-      for (int v = 0; v < 2; ++v) {
-        const int i = 2 * j + v, s = i % kStages, turn = i / kStages;
-        if (turn > 0 && !(ok = warp_wait(empty + 8 * s, (turn - 1) & 1, abort, count))) break;
-        if (lane == 0) {
-          if (v == 0) pages_there[j % kMasks] = mask;
-          bar_expect(full + 8 * s, kTile);
-        }
-        __syncwarp();
-        if (lane < per_tile)
-          for (int c = 0; c < DP / 64; ++c)
-            tma_4d(ring + s * kTile + c * kBlock + lane * rows * 128, v ? &v_map : &k_map, c * 64, row, job.hk, page, full + 8 * s);
-      }
-    }
-  } else if (warp == 8) {
-    // ---- products ----
-    if (lane == 0 && job.steps > 0) {
-      bool ok = bar_wait(q_full, 0, abort, count);
-      int done[2] = {0, 0};  // rounds of the softmax of each tile
-      auto scores = [&](int t, int s) {
-#pragma unroll
-        for (int k = 0; k < DP / 16; ++k)
-          mma_ss(tmem + t * kKeys, desc_k_major(q_at + t * kTile + (k / 4) * kBlock) + 2 * (k % 4), desc_k_major(ring + s * kTile + (k / 4) * kBlock) + 2 * (k % 4),
-                 mma_shape(kRows, kKeys), k > 0);
-        mma_commit(s_ready + 8 * t);
-      };
-      auto wait_full = [&](int i) {
-        const bool got = bar_wait(full + 8 * (i % kStages), (i / kStages) & 1, abort, count);
-        tmem_fence_after();
-        return got;
-      };
-      ok = ok && wait_full(0);
-      if (ok) {
-        for (int t = 0; t < 2; ++t)
-          if (job.active(t, 0)) scores(t, 0);
-        mma_commit(empty);
-      }
-      for (int j = 0; j < job.steps && ok; ++j) {
-        const int vi = 2 * j + 1, vs = vi % kStages, ki = 2 * j + 2, ks = ki % kStages;
-        const bool more = j + 1 < job.steps;
-        if (!(ok = bar_wait(clean + 8 * (j % kCleans), (j / kCleans) & 1, abort, count))) break;
-        if (more && !(ok = wait_full(ki))) break;
-        for (int t = 0; t < 2 && ok; ++t) {
-          if (job.active(t, j)) {
-            if (!(ok = bar_wait(p_ready + 8 * t, done[t] & 1, abort, count))) break;
-            tmem_fence_after();
-#pragma unroll
-            for (int k = 0; k < kKeys / 16; ++k)
-              mma_ts(tmem + 2 * kKeys + t * 128, tmem + t * kKeys + k * 8, desc_mn_major(ring + vs * kTile, kBlock) + k * 128, mma_shape(kRows, DP, true),
-                     done[t] > 0 || k > 0);
-            ++done[t];
-          }
-          if (more && job.active(t, j + 1)) scores(t, ks);
-        }
-        if (!ok) break;
-        mma_commit(empty + 8 * vs);
-        if (more) mma_commit(empty + 8 * ks);
-      }
-      for (int t = 0; t < 2; ++t) mma_commit(o_ready + 8 * t);
-    }
-  } else if (warp >= 10) {
-    // ---- values of tiles that are seen in part ----
-    bool ok = true;
-    for (int j = 0; j < job.steps && ok; ++j) {
-      const int i = 2 * j + 1, s = i % kStages;
-      if (!(ok = warp_wait(full + 8 * s, (i / kStages) & 1, abort, count))) break;
-      const bool part = (job.active(0, j) && !job.full(0, j)) || (job.active(1, j) && !job.full(1, j));
-      if (part) {
-        uint4* v = reinterpret_cast<uint4*>(base + 1024 + (2 + s) * kTile);
-        const int k0 = job.tile(j) * kKeys;
-        for (int x = threadIdx.x - 320; x < kTile / 16; x += kCleanWarps * 32) {
-          uint4 u = v[x];
-          uint32_t w[4] = {u.x, u.y, u.z, u.w};
-          bool bad = false;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            if ((w[e] & 0x7f80u) == 0x7f80u) w[e] &= 0xffff0000u, bad = true;
-            if ((w[e] & 0x7f800000u) == 0x7f800000u) w[e] &= 0xffffu, bad = true;
-          }
-          if (bad) {
-            v[x] = make_uint4(w[0], w[1], w[2], w[3]);
-            const int at = k0 + (x / 8) % kKeys;
-            if (at <= job.p1 && (at >= job.lo || at < job.sinks)) *poison = 1;  // (a row of this CTA may see it)
-          }
-        }
-        async_proxy_fence();
-      }
-      __syncwarp();
-      if (lane == 0) bar_arrive(clean + 8 * (j % kCleans));
-    }
-  } else {
+  // The softmax warps keep a row of scores in registers; the four others give up theirs (2 x 128 x 200 + 128 x 104 = 384 x 168).
+  if (warp < 8) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
     // ---- softmax and output: one thread, one row ----
     const int t = warp / 4, r = threadIdx.x % kRows;
     const uint32_t lanes = (uint32_t)((warp % 4) * 32) << 16;
@@ -292,44 +206,28 @@ __global__ void __launch_bounds__(kThreads, 1)
       ++round;
       tmem_fence_after();
       const uint32_t there = pages_there[j % kMasks];
-      const int per_tile = max(1, kKeys >> g.page_shift);
-      const bool part = !job.full(t, j) || there != (1u << per_tile) - 1u;
-      const int k0 = job.tile(j) * kKeys;
-      const int hi = pos - k0, lo = a.window ? hi - a.window + 1 : 0, sinks = a.window ? a.sinks - k0 : kKeys;
-      // The scores are read twice, 32 at a time -- once for the maximum, once for the weights -- which costs less than the
-      // registers that a whole row takes.
-      auto seen_scores = [&](int c, uint32_t (&v)[32]) {
-        if (flip) {
+      float s[kKeys];
 #pragma unroll
-          for (int i = 0; i < 32; ++i) v[i] ^= 0x80000000u;
-        }
-        if (part) {
-          const int shift = min(g.page_shift, 7);
+      for (int c = 0; c < kKeys; c += 32) tmem_ld32(s_at + c, *reinterpret_cast<uint32_t(*)[32]>(s + c));
 #pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            const int k = c + i;
-            const bool sees = k <= hi && (k >= lo || k < sinks) && ((there >> (k >> shift)) & 1);
-            v[i] = sees ? v[i] : 0xff800000u;
-          }
-        }
-      };
-      float top = -CUDART_INF_F;
-      uint32_t v0[32], v1[32];
-      tmem_ld32(s_at, v0);
-      tmem_wait_ld(v0);
+      for (int c = 0; c < kKeys; c += 32) tmem_wait_ld(*reinterpret_cast<uint32_t(*)[32]>(s + c));
+      if (flip) {
 #pragma unroll
-      for (int c = 0; c < kKeys; c += 64) {
-        tmem_ld32(s_at + c + 32, v1);
-        seen_scores(c, v0);
-#pragma unroll
-        for (int i = 0; i < 32; ++i) top = fmaxf(top, __uint_as_float(v0[i]));
-        tmem_wait_ld(v1);
-        tmem_ld32(s_at + (c + 64) % kKeys, v0);  // (at the end: the first again)
-        seen_scores(c + 32, v1);
-#pragma unroll
-        for (int i = 0; i < 32; ++i) top = fmaxf(top, __uint_as_float(v1[i]));
-        tmem_wait_ld(v0);
+        for (int i = 0; i < kKeys; ++i) s[i] = -s[i];
       }
+      if (!job.full(t, j) || there != (1u << max(1, kKeys >> g.page_shift)) - 1u) {
+#pragma unroll
+        for (int c = 0; c < kKeys; c += 32) {
+          const uint32_t sees = job.sees(pos, job.tile(j) * kKeys + c) & pages_of(there, c, g.page_shift);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) s[c + i] = (sees >> i) & 1 ? s[c + i] : -CUDART_INF_F;
+        }
+      }
+      float top = max3(s[0], s[1], s[2]), top2 = max3(s[3], s[4], s[5]);
+#pragma unroll
+      for (int i = 6; i + 4 <= kKeys; i += 4) top = max3(top, s[i], s[i + 1]), top2 = max3(top2, s[i + 2], s[i + 3]);
+      top = max3(top, s[kKeys - 2], s[kKeys - 1]);
+      top = fmaxf(top, top2);
       bool grow = false;
       if (m == -CUDART_INF_F) {
         m = top;  // (nothing summed yet but zeros)
@@ -353,34 +251,26 @@ __global__ void __launch_bounds__(kThreads, 1)
       const float shift_by = m == -CUDART_INF_F ? 0.f : -m * scale;
       const uint64_t sc2 = pack2(scale, scale), sh2 = pack2(shift_by, shift_by);
       uint64_t sum2[2] = {0, 0};
-      auto weights = [&](int c, uint32_t (&v)[32]) {  // P takes the place of scores that have been read
-        seen_scores(c, v);
-        uint32_t p[16];
 #pragma unroll
-        for (int i = 0; i < 32; i += 2) {
-          float x, y;
-          unpack2(fma2(pack2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), sc2, sh2), x, y);
-          x = pow2(x), y = pow2(y);
-          sum2[(i / 2) & 1] = add2(sum2[(i / 2) & 1], pack2(x, y));
-          p[i / 2] = pack_bf16x2(x, y);
-        }
-        tmem_st16(s_at + c / 2, p);
-      };
+      for (int half = 0; half < 2; ++half) {
 #pragma unroll
-      for (int c = 0; c < kKeys; c += 64) {
-        tmem_ld32(s_at + c + 32, v1);
-        tmem_wait_ld(v1);
-        weights(c, v0);
-        if (c + 64 < kKeys) {
-          tmem_ld32(s_at + c + 64, v0);
-          tmem_wait_ld(v0);
+        for (int c = half * 64; c < half * 64 + 64; c += 32) {
+          uint32_t p[16];
+#pragma unroll
+          for (int i = 0; i < 32; i += 2) {
+            float x, y;
+            unpack2(fma2(pack2(s[c + i], s[c + i + 1]), sc2, sh2), x, y);
+            x = pow2(x), y = pow2(y);
+            sum2[(i / 2) & 1] = add2(sum2[(i / 2) & 1], pack2(x, y));
+            p[i / 2] = pack_bf16x2(x, y);
+          }
+          tmem_st16(s_at + c / 2, p);  // P takes the place of scores that have been read
         }
-        weights(c + 32, v1);
+        tmem_wait_st();
+        tmem_fence_before();
+        __syncwarp();
+        if (lane == 0) bar_arrive(p_ready + 16 * t + 8 * half);
       }
-      tmem_wait_st();
-      tmem_fence_before();
-      __syncwarp();
-      if (lane == 0) bar_arrive(p_ready + 8 * t);
       float u, v;
       unpack2(add2(sum2[0], sum2[1]), u, v);
       l += u + v;
@@ -439,6 +329,124 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
     }
     tmem_fence_before();
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
+    if (warp == 9) {
+      // ---- copies ----
+      if (lane == 0) {
+        const int boxes = (job.tokens < job.left ? 2 : 1) * (DP / 64);  // (a second tile without rows is not read)
+        bar_expect(q_full, boxes * g.group * job.tokens * 128);
+        for (int t = 0; t < 2 && t * job.tokens < job.left; ++t)
+          for (int c = 0; c < DP / 64; ++c) tma_3d(q_at + t * kTile + c * kBlock, &q_map, c * 64, job.hk * g.group, job.token0 + t * job.tokens, q_full);
+      }
+      const int page_rows = 1 << g.page_shift, rows = min(page_rows, kKeys), per_tile = kKeys / rows;
+      const int32_t* table = a.block_table + (int64_t)job.b * a.table_stride;
+      bool ok = true;
+      for (int j = 0; j < job.steps && ok; ++j) {
+        const int k0 = job.tile(j) * kKeys;
+        const int64_t at = (int64_t)(k0 >> g.page_shift) + lane;
+        int32_t page = -1;
+        if (lane < per_tile && at < a.table_pages) page = __ldg(table + at);
+        const bool there = page >= 0 && page < a.num_pages;
+        if (!there) page = (int32_t)a.num_pages;  // beyond the array: zeros
+        const uint32_t mask = __ballot_sync(0xffffffffu, there);
+        const int row = k0 & (page_rows - 1);
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+          const int i = 2 * j + v, s = i % kStages, turn = i / kStages;
+          if (turn > 0 && !(ok = warp_wait(empty + 8 * s, (turn - 1) & 1, abort, count))) break;
+          if (lane == 0) {
+            if (v == 0) pages_there[j % kMasks] = mask;
+            bar_expect(full + 8 * s, kTile);
+          }
+          __syncwarp();
+          if (lane < per_tile)
+            for (int c = 0; c < DP / 64; ++c)
+              tma_4d(ring + s * kTile + c * kBlock + lane * rows * 128, v ? &v_map : &k_map, c * 64, row, job.hk, page, full + 8 * s);
+        }
+      }
+    } else if (warp == 8) {
+      // ---- products ----
+      if (lane == 0 && job.steps > 0) {
+        bool ok = bar_wait(q_full, 0, abort, count);
+        int done[2] = {0, 0};  // rounds of the softmax of each tile
+        auto scores = [&](int t, int s) {
+#pragma unroll
+          for (int k = 0; k < DP / 16; ++k)
+            mma_ss(tmem + t * kKeys, desc_k_major(q_at + t * kTile + (k / 4) * kBlock) + 2 * (k % 4), desc_k_major(ring + s * kTile + (k / 4) * kBlock) + 2 * (k % 4),
+                   mma_shape(kRows, kKeys), k > 0);
+          mma_commit(s_ready + 8 * t);
+        };
+        auto wait_full = [&](int i) {
+          const bool got = bar_wait(full + 8 * (i % kStages), (i / kStages) & 1, abort, count);
+          tmem_fence_after();
+          return got;
+        };
+        ok = ok && wait_full(0);
+        if (ok) {
+          for (int t = 0; t < 2; ++t)
+            if (job.active(t, 0)) scores(t, 0);
+          mma_commit(empty);
+        }
+        for (int j = 0; j < job.steps && ok; ++j) {
+          const int vi = 2 * j + 1, vs = vi % kStages, ki = 2 * j + 2, ks = ki % kStages;
+          const bool more = j + 1 < job.steps;
+          if (!(ok = bar_wait(clean + 8 * (j % kCleans), (j / kCleans) & 1, abort, count))) break;
+          if (more && !(ok = wait_full(ki))) break;
+          for (int t = 0; t < 2 && ok; ++t) {
+            if (job.active(t, j)) {
+              for (int half = 0; half < 2 && ok; ++half) {  // the first half of the keys while the second's weights are formed
+                if (!(ok = bar_wait(p_ready + 16 * t + 8 * half, done[t] & 1, abort, count))) break;
+                tmem_fence_after();
+#pragma unroll
+                for (int k = 0; k < kKeys / 32; ++k) {
+                  const int kk = half * (kKeys / 32) + k;
+                  mma_ts(tmem + 2 * kKeys + t * 128, tmem + t * kKeys + kk * 8, desc_mn_major(ring + vs * kTile, kBlock) + kk * 128, mma_shape(kRows, DP, true),
+                         done[t] > 0 || kk > 0);
+                }
+              }
+              if (!ok) break;
+              ++done[t];
+            }
+            if (more && job.active(t, j + 1)) scores(t, ks);
+          }
+          if (!ok) break;
+          mma_commit(empty + 8 * vs);
+          if (more) mma_commit(empty + 8 * ks);
+        }
+        for (int t = 0; t < 2; ++t) mma_commit(o_ready + 8 * t);
+      }
+    } else if (warp >= 10) {
+      // ---- values of tiles that are seen in part ----
+      bool ok = true;
+      for (int j = 0; j < job.steps && ok; ++j) {
+        const int i = 2 * j + 1, s = i % kStages;
+        if (!(ok = warp_wait(full + 8 * s, (i / kStages) & 1, abort, count))) break;
+        const bool part = (job.active(0, j) && !job.full(0, j)) || (job.active(1, j) && !job.full(1, j));
+        if (part) {
+          uint4* v = reinterpret_cast<uint4*>(base + 1024 + (2 + s) * kTile);
+          const int k0 = job.tile(j) * kKeys;
+          for (int x = threadIdx.x - 320; x < kTile / 16; x += kCleanWarps * 32) {
+            uint4 u = v[x];
+            uint32_t w[4] = {u.x, u.y, u.z, u.w};
+            bool bad = false;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              if ((w[e] & 0x7f80u) == 0x7f80u) w[e] &= 0xffff0000u, bad = true;
+              if ((w[e] & 0x7f800000u) == 0x7f800000u) w[e] &= 0xffffu, bad = true;
+            }
+            if (bad) {
+              v[x] = make_uint4(w[0], w[1], w[2], w[3]);
+              const int at = k0 + (x / 8) % kKeys;
+              if (at <= job.p1 && (at >= job.lo || at < job.sinks)) *poison = 1;  // (a row of this CTA may see it)
+            }
+          }
+          async_proxy_fence();
+        }
+        __syncwarp();
+        if (lane == 0) bar_arrive(clean + 8 * (j % kCleans));
+      }
+    }
   }
   __syncwarp();
   __syncthreads();

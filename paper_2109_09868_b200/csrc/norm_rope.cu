@@ -75,13 +75,15 @@ __global__ void __launch_bounds__(kElementThreads) norm_rope_element_kernel(cons
 }
 
 // The path for whole 16-byte columns: one pass over HBM.  A head's row is spread over L lanes (the power of two that holds
-// its columns), a warp takes 32 / L rows at a time and up to kAhead of those in one go, all of one token and of one kind
-// (queries, keys or values), so that the cosines, sines and weights are read once for many rows:
+// its columns), a warp takes 32 / L rows at a time, kAhead of those loaded together and kBatches of these one after the
+// other, all of one token and of one kind (queries, keys or values), so that the cosines, sines and weights are read once
+// for many rows:
 //     y_d = r (x_d A_d + x_p(d) B_d),    A_d = w_d cos,  B_d = -+ w_p(d) sin,   p(d) the other element of d's pair,
 // with r the reciprocal root mean square of the row.  The pair's other element comes from another lane (halves) or from
-// the lane's own column (neighbouring pairs).  All rows' loads are in flight before the first is used.
+// the lane's own column (neighbouring pairs).
 constexpr int kThreads = 256;
-constexpr int kAhead = 8;
+constexpr int kAhead = 4;
+constexpr int kBatches = 2;
 
 template <typename T>
 struct Column;
@@ -109,7 +111,7 @@ struct Column<float> {
 };
 
 template <typename T, int L>
-__global__ void __launch_bounds__(kThreads) norm_rope_kernel(const __grid_constant__ approxifer_norm_rope_args a, int q_units, int kv_units) {
+__global__ void __launch_bounds__(kThreads, 4) norm_rope_kernel(const __grid_constant__ approxifer_norm_rope_args a, int q_units, int kv_units) {
   constexpr int E = Column<T>::kElems, kSide = 32 / L;  // elements of a column, rows side by side
   const int lane = threadIdx.x % 32, at = lane % L, side = lane / L;
   const int units = q_units + (a.k ? kv_units : 0) + (a.v ? kv_units : 0);
@@ -120,17 +122,20 @@ __global__ void __launch_bounds__(kThreads) norm_rope_kernel(const __grid_consta
   const bool is_q = unit < q_units, is_k = !is_q && a.k && unit < q_units + kv_units;
   const bool head_unit = unit == 0;
   unit -= is_q ? 0 : is_k || !a.k ? q_units : q_units + kv_units;
-  const int heads = is_q ? a.Hq : a.Hkv, h0 = unit * (kSide * kAhead) + side;
+  const int heads = is_q ? a.Hq : a.Hkv, h0 = unit * (kSide * kAhead * kBatches) + side;
   const T* in = is_q ? static_cast<const T*>(a.q) + t * a.q_tstride : is_k ? static_cast<const T*>(a.k) + t * a.k_tstride : static_cast<const T*>(a.v) + t * a.v_tstride;
   const int64_t in_h = is_q ? a.q_hstride : is_k ? a.k_hstride : a.v_hstride;
   const int d0 = at * E;
   const bool live = d0 < a.D;
   uint4 x[kAhead];
+  auto load = [&](int batch) {
 #pragma unroll
-  for (int i = 0; i < kAhead; ++i) {
-    const int h = h0 + i * kSide;
-    x[i] = live && h < heads ? __ldcs(reinterpret_cast<const uint4*>(in + h * in_h + d0)) : make_uint4(0, 0, 0, 0);
-  }
+    for (int i = 0; i < kAhead; ++i) {
+      const int h = h0 + (batch * kAhead + i) * kSide;
+      x[i] = live && h < heads ? __ldcs(reinterpret_cast<const uint4*>(in + h * in_h + d0)) : make_uint4(0, 0, 0, 0);
+    }
+  };
+  load(0);
   const int32_t pos = a.rot ? __ldg(a.positions + t) : 0;
   const bool placed = a.rot == 0 || (pos >= 0 && pos < a.positions_max);
   const int64_t slot = a.slots ? __ldg(a.slots + t) : -1;
@@ -156,18 +161,26 @@ __global__ void __launch_bounds__(kThreads) norm_rope_kernel(const __grid_consta
     out_h = is_k ? a.kc_hstride : a.vc_hstride;
   }
   if (!is_q && !is_k) {
+    for (int batch = 0; batch < kBatches; ++batch) {
+      if (batch) load(batch);
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      const int h = h0 + i * kSide;
-      if (live && h < heads) *reinterpret_cast<uint4*>(out + h * out_h + d0) = x[i];
+      for (int i = 0; i < kAhead; ++i) {
+        const int h = h0 + (batch * kAhead + i) * kSide;
+        if (live && h < heads) *reinterpret_cast<uint4*>(out + h * out_h + d0) = x[i];
+      }
     }
+    return;
+  }
+  if (!placed) {  // (queries: keys have left above)
+    for (int h = h0; h < min(heads, h0 + kAhead * kBatches * kSide); h += kSide)
+      if (live) *reinterpret_cast<uint4*>(out + h * out_h + d0) = make_uint4(0, 0, 0, 0);
     return;
   }
 
   // A, B of this lane's elements, and the lane that holds their pairs
   const T* weight = static_cast<const T*>(is_q ? a.q_weight : a.k_weight);
   const int half = a.rot / 2;
-  const bool turned = placed && d0 < a.rot, second = d0 >= half;
+  const bool turned = d0 < a.rot, second = d0 >= half;
   const int partner = (turned && !a.interleaved) ? (second ? d0 - half : d0 + half) : d0;
   const int from = side * L + partner / E;
   float A[E], B[E];
@@ -202,30 +215,38 @@ __global__ void __launch_bounds__(kThreads) norm_rope_kernel(const __grid_consta
     }
   }
   const float inv_d = 1.f / (float)a.D;
+#pragma unroll 1
+  for (int batch = 0; batch < kBatches; ++batch) {
+    if (batch) load(batch);
 #pragma unroll
-  for (int i = 0; i < kAhead; ++i) {
-    const int h = h0 + i * kSide;
-    if (h - side >= heads) break;  // (the whole warp)
-    float v[E], p[E], sq = 0.f;
-    Column<T>::widen8(x[i], v);
+    for (int i = 0; i < kAhead; ++i) {
+      const int h = h0 + (batch * kAhead + i) * kSide;
+      if (h - side >= heads) break;  // (the whole warp)
+      float v[E], p[E], sq = 0.f;
+      Column<T>::widen8(x[i], v);
 #pragma unroll
-    for (int e = 0; e < E; ++e) sq = fmaf(v[e], v[e], sq);
+      for (int e = 0; e < E; ++e) sq = fmaf(v[e], v[e], sq);
 #pragma unroll
-    for (int d = L / 2; d > 0; d >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, d);
-    const float r = weight ? rsqrtf(sq * inv_d + a.eps) : 1.f;
-    if (a.interleaved) {
-#pragma unroll
-      for (int e = 0; e < E; e += 2) p[e] = v[e + 1], p[e + 1] = v[e];
-    } else {
-      uint4 other;
-      other.x = __shfl_sync(0xffffffffu, x[i].x, from), other.y = __shfl_sync(0xffffffffu, x[i].y, from);
-      other.z = __shfl_sync(0xffffffffu, x[i].z, from), other.w = __shfl_sync(0xffffffffu, x[i].w, from);
+      for (int d = L / 2; d > 0; d >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, d);
+      const float r = weight ? rsqrtf(sq * inv_d + a.eps) : 1.f;
+      uint4 other = x[i];
+      if (!a.interleaved) {
+        other.x = __shfl_sync(0xffffffffu, other.x, from), other.y = __shfl_sync(0xffffffffu, other.y, from);
+        other.z = __shfl_sync(0xffffffffu, other.z, from), other.w = __shfl_sync(0xffffffffu, other.w, from);
+      }
+      if (!turned) other = make_uint4(0, 0, 0, 0);  // (an element that is not turned has no part in a pair, even where it is infinite)
       Column<T>::widen8(other, p);
-    }
-    // (an element that is not turned has no part in its pair, even where that is infinite)
+      if (a.interleaved) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) v[e] = placed ? r * (turned ? fmaf(v[e], A[e], p[e] * B[e]) : v[e] * A[e]) : 0.f;
-    if (live && h < heads) *reinterpret_cast<uint4*>(out + h * out_h + d0) = Column<T>::narrow8(v);
+        for (int e = 0; e < E; e += 2) {
+          const float q = p[e];
+          p[e] = p[e + 1], p[e + 1] = q;
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[e] = r * fmaf(v[e], A[e], p[e] * B[e]);
+      if (live && h < heads) *reinterpret_cast<uint4*>(out + h * out_h + d0) = Column<T>::narrow8(v);
+    }
   }
 }
 
@@ -240,7 +261,7 @@ bool columns_fit(const approxifer_norm_rope_args& a) {
 
 template <typename T, int L>
 cudaError_t launch_columns(const approxifer_norm_rope_args& a, cudaStream_t stream) {
-  constexpr int kRowsPerUnit = (32 / L) * kAhead;
+  constexpr int kRowsPerUnit = (32 / L) * kAhead * kBatches;
   const int q_units = (a.Hq + kRowsPerUnit - 1) / kRowsPerUnit, kv_units = (a.Hkv + kRowsPerUnit - 1) / kRowsPerUnit;
   const int64_t warps = a.T * (q_units + (a.k ? kv_units : 0) + (a.v ? kv_units : 0)), blocks = (warps + kThreads / 32 - 1) / (kThreads / 32);
   if (blocks > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
