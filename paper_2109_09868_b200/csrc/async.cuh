@@ -69,6 +69,12 @@ __device__ __forceinline__ void drain_if_aborted(volatile int* abort) {
     for (int i = 0; i < 4000; ++i) __nanosleep(1000);
 }
 
+__device__ __forceinline__ float pow2(float x) {  // 2^x
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));

@@ -37,6 +37,9 @@ static_assert(kWarps * kRows * 64 * 4 + kWarps * kRows * 8 <= smem_bytes(64), "r
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
 }
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
@@ -56,35 +59,54 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// What one sequence's token sees: positions 0 .. sinks-1, then first .. last.
+__device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
+
+// What one sequence's token sees -- positions 0 .. sinks-1 and first .. last -- as chunks of `keys` positions that start at
+// multiples of `keys`: those that hold sinks, then those that hold the window.
 struct Seen {
   const int32_t* table;
-  int64_t first, last, sinks, count;
-  int32_t token, chunks;
+  int32_t first, last, sinks;
+  int32_t token;  // its index, or -1 where the sequence has no new token (max_q = 1)
+  int32_t sink_chunks, skip, chunks;
+  __device__ __forceinline__ int32_t position(int c, int keys) const { return (c < sink_chunks ? c : c + skip) * keys; }
+  // which of the keys of the chunk at `pos` are seen, a bit per key
+  __device__ __forceinline__ uint32_t sees(int32_t pos, int keys) const {
+    return bits_below(keys) & bits_below(last + 1 - pos) & (~bits_below(first - pos) | bits_below(sinks - pos));
+  }
 };
-// How many positions that is; the token's index, or -1 where the sequence has no new token (max_q = 1).
 __device__ __forceinline__ Seen seen_by(const approxifer_attention_args& a, int b, int keys) {
   Seen s;
   const int t = __ldg(a.q_start + b), end = __ldg(a.q_start + b + 1);
   const bool live = end - t == 1 && t >= 0 && t < a.T;
   s.token = live ? t : -1;
   const int64_t held = a.table_pages * a.page_size;
-  const int64_t p = live ? (int64_t)__ldg(a.kv_len + b) - 1 : -1;
-  s.last = p < held ? p : held - 1;
+  const int p = live ? __ldg(a.kv_len + b) - 1 : -1;
+  s.last = p < held ? p : (int)held - 1;
   s.first = a.window && p >= a.window ? p - a.window + 1 : 0;
   s.sinks = a.sinks < s.first ? a.sinks : s.first;
-  // (where the table is shorter than the cache claims to be, sinks may lie beyond `last`: such positions are not there)
-  s.count = live ? s.sinks + (s.last >= s.first ? s.last - s.first + 1 : 0) : 0;
-  s.chunks = (int32_t)((s.count + keys - 1) / keys);
+  s.sinks = s.sinks < s.last + 1 ? s.sinks : s.last + 1;
+  s.sink_chunks = s.sinks > 0 ? (s.sinks + keys - 1) / keys : 0;
+  const int from = s.first / keys > s.sink_chunks ? s.first / keys : s.sink_chunks;
+  s.skip = from - s.sink_chunks;
+  const int in_window = s.last >= 0 ? s.last / keys - from + 1 : 0;
+  s.chunks = s.last >= 0 ? s.sink_chunks + (in_window > 0 ? in_window : 0) : 0;
   s.table = a.block_table + (int64_t)b * a.table_stride;
   return s;
 }
 
+// Where the keys of a chunk lie.  WHOLE (pages of whole chunks): the chunk's page and first row, the same in all lanes.
+// Else: those of this lane's key (lane % keys).
+struct Spot {
+  int32_t page, row;
+  uint32_t sees;
+};
+
 // One warp's share of a unit.
-template <int DP>
+template <int DP, bool WHOLE>
 struct Warp {
   static constexpr int kKeys = keys_of(DP);
   static constexpr int kCols = DP / 8;  // 16-byte columns of a row
+  static constexpr uint32_t kAll = kKeys == 32 ? 0xffffffffu : (1u << kKeys) - 1u;
   uint32_t q[DP / 16][4];               // fragments of the 16 x DP queries
   float o[DP / 8][4];
   float m[2], l[2];
@@ -114,42 +136,74 @@ struct Warp {
     l[0] = l[1] = 0.f;
   }
 
-  // The page of this lane's key (lane % kKeys) of chunk c, -1 if there is none, and its row in the page.
-  __device__ __forceinline__ int32_t look_up(const approxifer_attention_args& a, const Seen& s, int c, int* row) const {
-    const int64_t u = (int64_t)c * kKeys + lane % kKeys;
-    const int64_t j = u < s.sinks ? u : s.first + (u - s.sinks);
-    *row = 0;
-    if (u >= s.count || j > s.last) return -1;
-    const uint32_t page_at = (uint32_t)j / (uint32_t)a.page_size;  // (positions are below 2^31)
-    *row = (int)((uint32_t)j - page_at * (uint32_t)a.page_size);
-    const int32_t page = __ldg(s.table + page_at);
-    return page >= 0 && page < a.num_pages ? page : -1;
+  __device__ __forceinline__ Spot look_up(const approxifer_attention_args& a, int page_shift, const Seen& s, int c) const {
+    Spot at{0, 0, 0};
+    if (c >= s.chunks) return at;
+    const int32_t pos = s.position(c, kKeys);
+    at.sees = s.sees(pos, kKeys);
+    if constexpr (WHOLE) {
+      at.page = __ldg(s.table + (pos >> page_shift));
+      at.row = pos & ((1 << page_shift) - 1);
+      if (at.page < 0 || at.page >= a.num_pages) at.page = 0, at.sees = 0;
+    } else {
+      const uint32_t j = (uint32_t)pos + lane % kKeys, entry = j / (uint32_t)a.page_size;
+      at.row = (int32_t)(j - entry * (uint32_t)a.page_size);
+      at.page = -1;
+      if ((at.sees >> (lane % kKeys)) & 1) at.page = __ldg(s.table + entry);
+      if (at.page >= a.num_pages) at.page = -1;
+    }
+    return at;
   }
 
   // Starts the copies of a chunk; which of its keys are there.
-  __device__ __forceinline__ uint32_t fetch(const approxifer_attention_args& a, int slot, int32_t page, int row_in_page, int hk) const {
-    const uint32_t there = __ballot_sync(kFull, page >= 0);
-    const int64_t pg = page >= 0 ? page : 0, at = page >= 0 ? row_in_page : 0;
-    const int64_t ko = pg * a.kc_pstride + at * a.kc_rstride + (int64_t)hk * a.kc_hstride;
-    const int64_t vo = pg * a.vc_pstride + at * a.vc_rstride + (int64_t)hk * a.vc_hstride;
-    const uint32_t kdst = ring + slot * 2 * half_bytes(DP), vdst = kdst + half_bytes(DP);
+  __device__ __forceinline__ uint32_t fetch(const approxifer_attention_args& a, int slot, const Spot& at, int hk) const {
+    constexpr int kStep = 32 / kCols;  // rows from one copy of a lane to its next
+    const int r0 = lane / kCols, col = lane % kCols;
+    const uint32_t kdst = ring + slot * 2 * half_bytes(DP) + r0 * DP * 2, x = (col ^ r0) << 4;
+    const bool in = col * 8 < a.D;
+    if constexpr (WHOLE) {
+      const bf16* k = reinterpret_cast<const bf16*>(a.k_cache) + at.page * a.kc_pstride + hk * a.kc_hstride + (at.row + r0) * a.kc_rstride + col * 8;
+      const bf16* v = reinterpret_cast<const bf16*>(a.v_cache) + at.page * a.vc_pstride + hk * a.vc_hstride + (at.row + r0) * a.vc_rstride + col * 8;
+      const int64_t kst = kStep * a.kc_rstride, vst = kStep * a.vc_rstride;
+      if (at.sees == kAll) {
 #pragma unroll
-    for (int i = 0; i < kKeys * kCols / 32; ++i) {
-      const int row = (lane + 32 * i) / kCols, col = (lane + 32 * i) % kCols;
-      const int64_t k = __shfl_sync(kFull, ko, row), v = __shfl_sync(kFull, vo, row);
-      const uint32_t to = row * DP * 2 + ((col ^ (row & 7)) << 4);
-      if (col * 8 < a.D) {
-        const bool ok = (there >> row) & 1;
-        copy16(kdst + to, reinterpret_cast<const bf16*>(a.k_cache) + k + col * 8, ok);
-        copy16(vdst + to, reinterpret_cast<const bf16*>(a.v_cache) + v + col * 8, ok);
+        for (int i = 0; i < kKeys / kStep; ++i, k += kst, v += vst) {
+          const uint32_t to = kdst + i * kStep * DP * 2 + (x ^ (((i * kStep) & 7) << 4));
+          if (in) copy16(to, k), copy16(to + half_bytes(DP), v);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < kKeys / kStep; ++i, k += kst, v += vst) {
+          const uint32_t to = kdst + i * kStep * DP * 2 + (x ^ (((i * kStep) & 7) << 4));
+          const bool ok = (at.sees >> (r0 + i * kStep)) & 1;
+          if (in) copy16(to, k, ok), copy16(to + half_bytes(DP), v, ok);
+        }
       }
+      return at.sees;
+    } else {
+      const uint32_t there = __ballot_sync(kFull, at.page >= 0);
+      const int64_t pg = at.page >= 0 ? at.page : 0, row = at.page >= 0 ? at.row : 0;
+      const int64_t ko = pg * a.kc_pstride + row * a.kc_rstride + (int64_t)hk * a.kc_hstride;
+      const int64_t vo = pg * a.vc_pstride + row * a.vc_rstride + (int64_t)hk * a.vc_hstride;
+#pragma unroll
+      for (int i = 0; i < kKeys / kStep; ++i) {
+        const int r = r0 + i * kStep;
+        const int64_t k = __shfl_sync(kFull, ko, r), v = __shfl_sync(kFull, vo, r);
+        const uint32_t to = kdst + i * kStep * DP * 2 + (x ^ (((i * kStep) & 7) << 4));
+        const bool ok = (there >> r) & 1;
+        if (in) {
+          copy16(to, reinterpret_cast<const bf16*>(a.k_cache) + k + col * 8, ok);
+          copy16(to + half_bytes(DP), reinterpret_cast<const bf16*>(a.v_cache) + v + col * 8, ok);
+        }
+      }
+      return there & kAll;
     }
-    return there;
   }
 
   // scale: of the scores, times log2 e (the softmax runs on powers of two).
   __device__ __forceinline__ void reduce(int slot, uint32_t there, float scale) {
-    const uint32_t kat = ring + slot * 2 * half_bytes(DP), vat = kat + half_bytes(DP);
+    const uint32_t kat = ring + slot * 2 * half_bytes(DP) + ((lane / 16) * 8 + lane % 8) * DP * 2, kx = ((lane / 8) % 2 ^ (lane & 7)) << 4;
+    const uint32_t vat = ring + slot * 2 * half_bytes(DP) + half_bytes(DP) + (lane % 16) * DP * 2, vx = (lane / 16 ^ (lane & 7)) << 4;
     float s[kKeys / 8][4];
 #pragma unroll
     for (int n = 0; n < kKeys / 8; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
@@ -158,20 +212,25 @@ struct Warp {
 #pragma unroll
       for (int n = 0; n < kKeys / 16; ++n) {
         uint32_t kb[4];
-        const int key = n * 16 + (lane / 16) * 8 + lane % 8, col = ks * 2 + (lane / 8) % 2;
-        ldmatrix4(kat + key * DP * 2 + ((col ^ (key & 7)) << 4), kb);
+        ldmatrix4(kat + n * 16 * DP * 2 + (kx ^ (ks << 5)), kb);
         mma16816(s[2 * n], q[ks], kb[0], kb[1]);
         mma16816(s[2 * n + 1], q[ks], kb[2], kb[3]);
       }
+#pragma unroll
+    for (int n = 0; n < kKeys / 8; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[n][i] *= scale;
+    if (there != kAll) {
+#pragma unroll
+      for (int n = 0; n < kKeys / 8; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[n][i] = (there >> (n * 8 + (lane % 4) * 2 + (i & 1))) & 1 ? s[n][i] : -CUDART_INF_F;
+    }
     float top[2] = {m[0], m[1]};
 #pragma unroll
     for (int n = 0; n < kKeys / 8; ++n)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int key = n * 8 + (lane % 4) * 2 + (i & 1);
-        s[n][i] = (there >> key) & 1 ? s[n][i] * scale : -CUDART_INF_F;
-        top[i >> 1] = fmaxf(top[i >> 1], s[n][i]);
-      }
+      for (int i = 0; i < 4; ++i) top[i >> 1] = fmaxf(top[i >> 1], s[n][i]);
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
       top[r] = fmaxf(top[r], __shfl_xor_sync(kFull, top[r], 1));
@@ -179,7 +238,7 @@ struct Warp {
     }
     const float base[2] = {top[0] == -CUDART_INF_F ? 0.f : top[0], top[1] == -CUDART_INF_F ? 0.f : top[1]};
     if (__any_sync(kFull, top[0] != m[0] || top[1] != m[1])) {
-      const float keep[2] = {exp2f(m[0] - base[0]), exp2f(m[1] - base[1])};
+      const float keep[2] = {pow2(m[0] - base[0]), pow2(m[1] - base[1])};
       l[0] *= keep[0], l[1] *= keep[1];
 #pragma unroll
       for (int d = 0; d < DP / 8; ++d) o[d][0] *= keep[0], o[d][1] *= keep[0], o[d][2] *= keep[1], o[d][3] *= keep[1];
@@ -191,15 +250,14 @@ struct Warp {
 #pragma unroll
       for (int n = 0; n < 2; ++n) {
         const float(&x)[4] = s[2 * kk + n];
-        const float e0 = exp2f(x[0] - base[0]), e1 = exp2f(x[1] - base[0]), e2 = exp2f(x[2] - base[1]), e3 = exp2f(x[3] - base[1]);
+        const float e0 = pow2(x[0] - base[0]), e1 = pow2(x[1] - base[0]), e2 = pow2(x[2] - base[1]), e3 = pow2(x[3] - base[1]);
         l[0] += e0 + e1, l[1] += e2 + e3;
         p[2 * n] = pack_bf16x2(e0, e1), p[2 * n + 1] = pack_bf16x2(e2, e3);
       }
 #pragma unroll
       for (int dt = 0; dt < DP / 16; ++dt) {
         uint32_t vb[4];
-        const int key = kk * 16 + lane % 16, col = dt * 2 + lane / 16;
-        ldmatrix4_t(vat + key * DP * 2 + ((col ^ (key & 7)) << 4), vb);
+        ldmatrix4_t(vat + kk * 16 * DP * 2 + (vx ^ (dt << 5)), vb);
         mma16816(o[2 * dt], p, vb[0], vb[1]);
         mma16816(o[2 * dt + 1], p, vb[2], vb[3]);
       }
@@ -216,8 +274,9 @@ struct Warp {
   }
 };
 
-template <int DP>
-__global__ void __launch_bounds__(kThreads, kCtasPerSm) attention_token_cluster_kernel(const __grid_constant__ approxifer_attention_args a, int row_tiles) {
+template <int DP, bool WHOLE>
+__global__ void __launch_bounds__(kThreads, kCtasPerSm) attention_token_cluster_kernel(const __grid_constant__ approxifer_attention_args a, int row_tiles,
+                                                                                        int page_shift) {
   extern __shared__ __align__(1024) unsigned char smem[];
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const int S = (int)cluster_size(), rank = (int)cluster_rank();
@@ -229,25 +288,22 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) attention_token_cluster_
   const Seen seen = seen_by(a, b, keys_of(DP));
   const int stride = S * kWarps, c0 = rank * kWarps + warp;
 
-  Warp<DP> w;
+  Warp<DP, WHOLE> w;
   w.setup(smem + warp * ring_bytes(DP), a.D);
   uint32_t there[kStages];
-  int row;
-  int32_t page;
 #pragma unroll
   for (int s = 0; s < kStages - 1; ++s) {
-    page = w.look_up(a, seen, c0 + s * stride, &row);
-    there[s] = w.fetch(a, s, page, row, hk);
+    there[s] = w.fetch(a, s, w.look_up(a, page_shift, seen, c0 + s * stride), hk);
     copy_commit();
   }
-  page = w.look_up(a, seen, c0 + (kStages - 1) * stride, &row);
+  Spot ahead = w.look_up(a, page_shift, seen, c0 + (kStages - 1) * stride);
   w.start(a, seen.token, head0, rows);
   const float scale = a.scale * 1.4426950408889634f;
   int slot = 0;
   for (int c = c0; c < seen.chunks; c += stride) {
-    there[kStages - 1] = w.fetch(a, (slot + kStages - 1) % kStages, page, row, hk);
+    there[kStages - 1] = w.fetch(a, (slot + kStages - 1) % kStages, ahead, hk);
     copy_commit();
-    page = w.look_up(a, seen, c + kStages * stride, &row);
+    ahead = w.look_up(a, page_shift, seen, c + kStages * stride);
     copy_wait<kStages - 1>();
     __syncwarp();
     w.reduce(slot, there[0], scale);
@@ -289,7 +345,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) attention_token_cluster_
     float total = 0.f, y0 = 0.f, y1 = 0.f;
     for (int p = 0; p < S * kWarps; ++p) {
       const int at = (p % kWarps) * kRows + r;
-      const float k = exp2f(get(peer_smem(sm_addr + at * 4, p / kWarps)) - best);
+      const float k = pow2(get(peer_smem(sm_addr + at * 4, p / kWarps)) - best);
       total = fmaf(k, get(peer_smem(sl_addr + at * 4, p / kWarps)), total);
       y0 = fmaf(k, get(peer_smem(so_addr + (at * DP + d) * 4, p / kWarps)), y0);
       y1 = fmaf(k, get(peer_smem(so_addr + (at * DP + d + 1) * 4, p / kWarps)), y1);
@@ -355,9 +411,9 @@ struct Cursor {
   }
 };
 
-template <int DP>
+template <int DP, bool WHOLE>
 __global__ void __launch_bounds__(kThreads, kCtasPerSm) attention_token_balanced_kernel(const __grid_constant__ approxifer_attention_args a, int row_tiles,
-                                                                                         float* partial) {
+                                                                                         int page_shift, float* partial) {
   extern __shared__ __align__(1024) unsigned char smem[];
   const int warp = blockIdx.x * kWarps + threadIdx.x / 32, warps = gridDim.x * kWarps, lane = threadIdx.x % 32;
   const int units = a.Hkv * row_tiles, group = a.Hq / a.Hkv;
@@ -376,23 +432,24 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) attention_token_balanced
   use = get;
   int64_t to_get = x1 - x0;
 
-  Warp<DP> w;
+  Warp<DP, WHOLE> w;
   w.setup(smem + (threadIdx.x / 32) * ring_bytes(DP), a.D);
   uint32_t there[kStages];
-  int row = 0, hk = 0;
-  int32_t page = -1;
+  Spot ahead;
+  int hk = 0;
   auto look_ahead = [&]() {
-    page = -1;
     if (to_get-- > 0) {
-      page = w.look_up(a, get.seen, get.c, &row);
+      ahead = w.look_up(a, page_shift, get.seen, get.c);
       hk = get.unit / row_tiles;
       if (to_get > 0) get.next(a, units, keys_of(DP));
+    } else {
+      ahead = Spot{WHOLE ? 0 : -1, 0, 0};
     }
   };
 #pragma unroll
   for (int s = 0; s < kStages - 1; ++s) {
     look_ahead();
-    there[s] = w.fetch(a, s, page, row, hk);
+    there[s] = w.fetch(a, s, ahead, hk);
     copy_commit();
   }
   look_ahead();
@@ -403,7 +460,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) attention_token_balanced
   int rows = min(kRows, group - (use.unit % row_tiles) * kRows);
   w.start(a, use.seen.token, head0, rows);
   for (int64_t x = x0; x < x1; ++x) {
-    there[kStages - 1] = w.fetch(a, (slot + kStages - 1) % kStages, page, row, hk);
+    there[kStages - 1] = w.fetch(a, (slot + kStages - 1) % kStages, ahead, hk);
     copy_commit();
     look_ahead();
     copy_wait<kStages - 1>();
@@ -496,14 +553,14 @@ __global__ void __launch_bounds__(JW * 32) attention_token_join_kernel(const __g
       for (int c = 0; c < DP / 64; ++c) v[i][c] = __ldcg(reinterpret_cast<const float2*>(partial + p * DP + c * 64 + lane * 2));
     }
     const float top = fmaxf(fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)), m), base = top == -CUDART_INF_F ? 0.f : top;
-    const float keep = exp2f(m - base);
+    const float keep = pow2(m - base);
     l *= keep;
 #pragma unroll
     for (int c = 0; c < DP / 32; ++c) y[c] *= keep;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       if (w + i * JW > w1) break;  // (what a row that has only NaN holds must not be scaled by zero)
-      const float k = exp2f(ml[i].x - base);
+      const float k = pow2(ml[i].x - base);
       l = fmaf(k, ml[i].y, l);
 #pragma unroll
       for (int c = 0; c < DP / 64; ++c) y[2 * c] = fmaf(k, v[i][c].x, y[2 * c]), y[2 * c + 1] = fmaf(k, v[i][c].y, y[2 * c + 1]);
@@ -522,7 +579,7 @@ __global__ void __launch_bounds__(JW * 32) attention_token_join_kernel(const __g
     float sum = 0.f, z = 0.f;
 #pragma unroll
     for (int w = 0; w < JW; ++w) {
-      const float k = exp2f(sm[w] - best);
+      const float k = pow2(sm[w] - best);
       sum = fmaf(k, sl[w], sum);
       z = fmaf(k, sy[w][d], z);
     }
@@ -536,9 +593,9 @@ int64_t most_seen(const approxifer_attention_args& a) {
   return a.window && (int64_t)a.window + a.sinks < held ? (int64_t)a.window + a.sinks : held;
 }
 int64_t units_of(const approxifer_attention_args& a) { return (int64_t)a.batch * a.Hkv * ((a.Hq / a.Hkv + kRows - 1) / kRows); }
-template <int DP>
-cudaError_t launch_cluster(const approxifer_attention_args& a, const DeviceInfo& dev, int row_tiles, int64_t units, int split, cudaStream_t stream) {
-  auto kernel = attention_token_cluster_kernel<DP>;
+template <int DP, bool WHOLE>
+cudaError_t launch_cluster(const approxifer_attention_args& a, const DeviceInfo& dev, int row_tiles, int page_shift, int64_t units, int split, cudaStream_t stream) {
+  auto kernel = attention_token_cluster_kernel<DP, WHOLE>;
   struct Tag {};
   cudaError_t e = ensure_dynamic_smem<Tag>(kernel, dev.ordinal, smem_bytes(DP));
   if (e != cudaSuccess) return e;
@@ -552,20 +609,20 @@ cudaError_t launch_cluster(const approxifer_attention_args& a, const DeviceInfo&
   attr[0].val.clusterDim.x = split, attr[0].val.clusterDim.y = 1, attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  e = cudaLaunchKernelEx(&cfg, kernel, a, row_tiles);
+  e = cudaLaunchKernelEx(&cfg, kernel, a, row_tiles, page_shift);
   count_launch();
   return e;
 }
 
-template <int DP>
-cudaError_t launch_balanced(const approxifer_attention_args& a, const DeviceInfo& dev, int row_tiles, cudaStream_t stream) {
-  auto kernel = attention_token_balanced_kernel<DP>;
+template <int DP, bool WHOLE>
+cudaError_t launch_balanced(const approxifer_attention_args& a, const DeviceInfo& dev, int row_tiles, int page_shift, cudaStream_t stream) {
+  auto kernel = attention_token_balanced_kernel<DP, WHOLE>;
   struct Tag {};
   cudaError_t e = ensure_dynamic_smem<Tag>(kernel, dev.ordinal, smem_bytes(DP));
   if (e != cudaSuccess) return e;
   const int ctas = dev.sms * kCtasPerSm;
   float* partial = static_cast<float*>(a.workspace);
-  kernel<<<ctas, kThreads, smem_bytes(DP), stream>>>(a, row_tiles, partial);
+  kernel<<<ctas, kThreads, smem_bytes(DP), stream>>>(a, row_tiles, page_shift, partial);
   count_launch();
   if ((e = cudaGetLastError()) != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
@@ -591,7 +648,7 @@ bool wants_balance(const approxifer_attention_args& a) { return units_of(a) * mo
 }  // namespace
 
 bool attention_token_eligible(const approxifer_attention_args& a) {
-  return a.max_q == 1 && a.D % 8 == 0 && a.D <= 128 && aligned16(a.k_cache) && aligned16(a.v_cache) && (reinterpret_cast<uintptr_t>(a.q) & 3) == 0 &&
+  return a.max_q == 1 && a.table_pages * a.page_size < (1LL << 31) && a.D % 8 == 0 && a.D <= 128 && aligned16(a.k_cache) && aligned16(a.v_cache) && (reinterpret_cast<uintptr_t>(a.q) & 3) == 0 &&
          (reinterpret_cast<uintptr_t>(a.out) & 3) == 0 && a.q_tstride % 2 == 0 && a.q_hstride % 2 == 0 && a.o_tstride % 2 == 0 && a.o_hstride % 2 == 0 &&
          (a.kc_pstride | a.kc_hstride | a.kc_rstride | a.vc_pstride | a.vc_hstride | a.vc_rstride) % 8 == 0;
 }
@@ -607,16 +664,22 @@ cudaError_t launch_attention_token(const approxifer_attention_args& a, cudaStrea
   const cudaError_t e = current_device_info(&dev);
   if (e != cudaSuccess) return e;
   const int row_tiles = (a.Hq / a.Hkv + kRows - 1) / kRows;
+  const int dp = a.D <= 64 ? 64 : 128, keys = keys_of(dp);
+  int page_shift = 0;  // pages of whole chunks and a power of two: one look-up a chunk
+  while ((1 << page_shift) < a.page_size) ++page_shift;
+  const bool is_whole = (1 << page_shift) == a.page_size && a.page_size >= keys;
   const int64_t need = attention_token_workspace(a);
-  if (need > 0 && a.workspace_bytes >= need && (int64_t)a.batch * a.Hq < (1LL << 31) && (int64_t)a.Hkv * row_tiles < (1LL << 31))
-    return a.D <= 64 ? launch_balanced<64>(a, *dev, row_tiles, stream) : launch_balanced<128>(a, *dev, row_tiles, stream);
+  if (need > 0 && a.workspace_bytes >= need && (int64_t)a.batch * a.Hq < (1LL << 31)) {
+    auto launch = is_whole ? (dp == 64 ? launch_balanced<64, true> : launch_balanced<128, true>) : dp == 64 ? launch_balanced<64, false> : launch_balanced<128, false>;
+    return launch(a, *dev, row_tiles, page_shift, stream);
+  }
   // Until there are about four CTAs for every place on the GPU, none with less than two chunks for each warp.
   const int64_t units = units_of(a), most = most_seen(a);
-  const int keys = keys_of(a.D <= 64 ? 64 : 128);
   int split = 1;
   while (split < 8 && units * split < 4LL * kCtasPerSm * dev->sms && most >= (int64_t)split * 2 * kWarps * keys * 2) split *= 2;
   if (units * split > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
-  return a.D <= 64 ? launch_cluster<64>(a, *dev, row_tiles, units, split, stream) : launch_cluster<128>(a, *dev, row_tiles, units, split, stream);
+  auto launch = is_whole ? (dp == 64 ? launch_cluster<64, true> : launch_cluster<128, true>) : dp == 64 ? launch_cluster<64, false> : launch_cluster<128, false>;
+  return launch(a, *dev, row_tiles, page_shift, units, split, stream);
 }
 
 }  // namespace approxifer
