@@ -57,12 +57,15 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
   return false;
 }
 
-// Whole warp: true if every lane's wait succeeded and nothing was aborted (the tensor-memory accesses that follow need the
-// warp together).
+// Whole warp: true if every lane's wait succeeded (the tensor-memory accesses that follow need the warp together).
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort, unsigned int* count) {
-  const bool ok = bar_wait(bar, parity, abort, count);
-  return __all_sync(0xffffffffu, ok && *abort == 0);
+  bool ok = bar_try(bar, parity);
+  if (__all_sync(0xffffffffu, ok)) return true;
+  if (!ok) ok = bar_wait(bar, parity, abort, count);
+  return __all_sync(0xffffffffu, ok);
 }
+// The warp's index, known to be the same in all its lanes.
+__device__ __forceinline__ int warp_index() { return __shfl_sync(0xffffffffu, (int)threadIdx.x / 32, 0); }
 // Before the CTA gives up its memory after an aborted wait: time (bounded) for its copies and products in flight to land.
 __device__ __forceinline__ void drain_if_aborted(volatile int* abort) {
   if (*abort)
@@ -137,6 +140,18 @@ __device__ __forceinline__ uint64_t desc_mn_major(uint32_t addr, uint32_t block)
 // bfloat16 x bfloat16 -> fp32; b_mn: the second operand is MN-major.
 __host__ __device__ constexpr uint32_t mma_shape(int m, int n, bool b_mn = false) {
   return 1u << 4 | 1u << 7 | 1u << 10 | (b_mn ? 1u << 16 : 0u) | (uint32_t)(n >> 3) << 17 | (uint32_t)(m >> 4) << 24;
+}
+// The products and their commits are issued from a branch on elect_one() that the whole warp reaches in the same state: the
+// operands then live in uniform registers, which is what the instruction takes (from a branch on a lane index each issue costs
+// some 200 cycles).
+__device__ __forceinline__ bool elect_one() {  // one lane of the warp, the same every time
+  uint32_t ok;
+  asm volatile(
+      "{\n.reg .pred p;\n"
+      "elect.sync _|p, 0xffffffff;\n"
+      "selp.u32 %0, 1, 0, p;\n}\n"
+      : "=r"(ok));
+  return ok != 0;
 }
 __device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t shape, bool add) {
   asm volatile(

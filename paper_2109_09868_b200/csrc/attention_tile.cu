@@ -1,22 +1,24 @@
 // Attention of several tokens per sequence (prompts, chunks of prompts) over a paged cache, on the tensor cores.
 //
-// A CTA takes 256 query rows of one sequence and key head in two tiles of 128: the query heads that share the key head
-// stand side by side (row = token * group + head), so keys and values are read once for all of them.  It walks the tiles of
-// 128 keys that any of its rows sees (the sinks' tiles, then the window's), one pass with the running maximum and sum:
+// Query rows come in tiles of 128 of one sequence and key head: the query heads that share the key head stand side by side
+// (row = token * group + head), so keys and values are read once for all of them.  A CTA walks the tiles of 128 keys that
+// any of its rows sees (the sinks' tiles, then the window's), one pass with the running maximum and sum:
 //
 //   S = Q K^T       128 x 128 fp32 in tensor memory (tcgen05, both operands in shared memory)
-//   P = 2^(S' - m)  a thread owns a row: no shuffles; P (bfloat16) goes back to tensor memory over its S
+//   P = 2^(S' - m)  a thread owns a row and holds it in registers: no shuffles; P (bfloat16) goes to tensor memory
 //   O += P V        P from tensor memory, V from shared memory as it lies in the cache (MN-major); O fp32 in tensor memory
 //
-// While the tensor cores work for one of the two tiles, the other's softmax runs.  The maximum in use is raised, and O
+// What a tile's rows wait for is the chain S -> softmax -> P, not any one unit, so S is free again as soon as it has been
+// loaded into registers, and the next S is formed while the softmax works on the last one.  With P beside S that leaves
+// tensor memory for one S, which the two tiles of a CTA (D > 64) take in turn.  The maximum in use is raised, and O
 // rescaled, only when a row's grows by more than 2^8 (P and O then still fit their types with room to spare; the final
 // division by the sum makes up for it), which after the first tiles is hardly ever.
 //
-//   warps 0-3, 4-7  softmax of tile 0, of tile 1, and their output
-//   warp 8          one lane: tcgen05.mma; allocates the tensor memory
-//   warp 9          tensor-map copies: keys and values by pages, a lane to a page; pages that are not there read as zeros
-//   warps 10, 11    look through the values of tiles that some rows see only in part: a weight of zero must meet no
-//                   infinity or NaN, so such elements are taken out, and where a row does see them the output adds them back
+//   4 warps a tile   softmax and output
+//   1 warp           tcgen05.mma; allocates the tensor memory
+//   1 warp           tensor-map copies: keys and values by pages, a lane to a page; pages that are not there read as zeros
+//   2 warps          look through the values of tiles that some rows see only in part: a weight of zero must meet no
+//                    infinity or NaN, so such elements are taken out, and where a row does see them the output adds them back
 #include "async.cuh"
 
 namespace approxifer {
@@ -27,22 +29,26 @@ namespace {
 
 constexpr int kRows = 128;  // query rows per tile
 constexpr int kKeys = 128;  // keys per tile
-constexpr int kThreads = 12 * 32;
 constexpr int kCleanWarps = 2;
+constexpr int kOtherWarps = 2 + kCleanWarps;
 constexpr int kBlock = kRows * 128;  // bytes of 64 columns of a tile
 constexpr float kGrowth = 8.f;       // log2 of what the maximum in use may lag behind
 
 constexpr int tile_bytes(int dp) { return kBlock * (dp / 64); }
-constexpr int stages_of(int dp) { return dp == 64 ? 8 : 5; }
+// Query tiles per CTA and CTAs per SM.  Up to D = 64 a CTA has one tile and two CTAs share an SM: each fills the gaps of the
+// other, its start and end included.  Beyond, shared memory holds one CTA, and its two tiles share the keys and values.
+constexpr int tiles_of(int dp) { return dp == 64 ? 1 : 2; }
+constexpr int threads_of(int dp) { return (4 * tiles_of(dp) + kOtherWarps) * 32; }
+constexpr int kStages = 5;
 // Rings of one entry per tile of keys.  An entry is used again only after the products of four tiles before it have been
 // issued (the copies that lead there wait for their stages), and those wait for all that the tile's readers do.
 constexpr int kCleans = 4, kMasks = 8;
-constexpr int smem_bytes(int dp) { return 1024 + 1024 + (2 + stages_of(dp)) * tile_bytes(dp); }
+constexpr int smem_bytes(int dp) { return 1024 + 1024 + (tiles_of(dp) + kStages) * tile_bytes(dp); }
 
 struct TileArgs {
   approxifer_attention_args a;
   int32_t group, tokens;  // query heads per key head; tokens per tile (128 / group)
-  int32_t blocks;         // query blocks (of two tiles) per sequence
+  int32_t blocks;         // query blocks (a CTA's tiles) per sequence
   int32_t page_shift;
 };
 
@@ -55,16 +61,14 @@ struct Job {
   int window, sinks;
   int tokens;          // per tile
   int sink_tiles, first_tile, steps;
+  int steps0, steps1;  // of the two query tiles
 
   __device__ __forceinline__ int tile(int j) const { return j < sink_tiles ? j : first_tile + (j - sink_tiles); }
   __device__ __forceinline__ int first_pos(int t) const { return pos0 + t * tokens; }
   __device__ __forceinline__ int last_pos(int t) const { return pos0 + min((t + 1) * tokens, left) - 1; }
-  // does any row of query tile t see any key of tile k; do all of them see all of it
-  __device__ __forceinline__ bool active(int t, int j) const {
-    if (t * tokens >= left) return false;
-    const int k0 = tile(j) * kKeys, k1 = k0 + kKeys - 1;
-    return k0 <= last_pos(t) && (window == 0 || k1 > first_pos(t) - window || k0 < sinks);
-  }
+  // Which steps a query tile takes part in: tile 0 up to the last key its rows see, tile 1 all (the window of its first row
+  // may start a tile or two later than tile 0's; there it finds nothing).
+  __device__ __forceinline__ int steps_of(int t) const { return t == 0 ? steps0 : steps1; }
   // which of the 32 keys from position k on the row at `pos` sees, a bit per key
   __device__ __forceinline__ uint32_t sees(int pos, int k) const {
     auto below = [](int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; };  // bits 0 .. n-1
@@ -74,6 +78,9 @@ struct Job {
   __device__ __forceinline__ bool full(int t, int j) const {
     const int k0 = tile(j) * kKeys, k1 = k0 + kKeys - 1;
     return k1 <= first_pos(t) && (window == 0 || k0 > last_pos(t) - window || k1 < sinks);
+  }
+  __device__ __forceinline__ bool part(int j, int tiles) const {  // some row of a tile that is worked on does not see all of it
+    return (j < steps0 && !full(0, j)) || (tiles == 2 && j < steps1 && !full(1, j));
   }
 };
 
@@ -88,6 +95,7 @@ __device__ __forceinline__ uint32_t pages_of(uint32_t there, int c, int page_shi
   return bits;
 }
 
+template <int TQ>
 __device__ __forceinline__ bool find_job(const TileArgs& g, Job* job) {
   const approxifer_attention_args& a = g.a;
   // blocks of late queries see most: they come first
@@ -97,14 +105,14 @@ __device__ __forceinline__ bool find_job(const TileArgs& g, Job* job) {
   job->b = x % a.batch;
   const int block = g.blocks - 1 - x / a.batch;
   const int start = __ldg(a.q_start + job->b), queries = __ldg(a.q_start + job->b + 1) - start, held = __ldg(a.kv_len + job->b);
-  const int skip = block * 2 * g.tokens;
+  const int skip = block * TQ * g.tokens;
   if (skip >= queries || start < 0 || (int64_t)start + queries > a.T) return false;
   job->tokens = g.tokens;
   job->token0 = start + skip;
   job->left = queries - skip;
   job->pos0 = held - queries + skip;
   job->window = a.window, job->sinks = a.sinks;
-  const int last = job->pos0 + min(2 * g.tokens, job->left) - 1;
+  const int last = job->pos0 + min(TQ * g.tokens, job->left) - 1;
   const int64_t room = a.table_pages << g.page_shift;
   job->p1 = last < room ? last : (int)(room - 1);
   job->lo = a.window && job->pos0 >= a.window ? job->pos0 - a.window + 1 : 0;
@@ -113,36 +121,24 @@ __device__ __forceinline__ bool find_job(const TileArgs& g, Job* job) {
   job->first_tile = max(job->lo / kKeys, job->sink_tiles);
   const int last_tile = job->p1 < 0 ? -1 : job->p1 / kKeys;
   job->steps = job->p1 < 0 ? 0 : job->sink_tiles + max(0, last_tile - job->first_tile + 1);
+  const int last0 = job->last_pos(0);  // (of tile 0's rows)
+  job->steps1 = TQ == 2 && job->tokens < job->left ? job->steps : 0;
+  job->steps0 = job->steps1 == 0 ? job->steps : last0 < 0 ? 0 : min(job->steps, job->sink_tiles + max(0, last0 / kKeys - job->first_tile + 1));
   return true;
 }
 
-__device__ __forceinline__ uint64_t pack2(float lo, float hi) {
-  uint64_t d;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi));
-  return d;
-}
-__device__ __forceinline__ void unpack2(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-  return d;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
 __device__ __forceinline__ float max3(float a, float b, float c) {  // (a NaN is passed over; it makes its row NaN as a weight)
   float d;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
 template <int DP>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
     attention_tile_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
                           const __grid_constant__ TileArgs g) {
-  constexpr int kStages = stages_of(DP);
-  constexpr int kTile = tile_bytes(DP);
+  constexpr int TQ = tiles_of(DP), kTile = tile_bytes(DP);
+  constexpr int kMmaWarp = 4 * TQ, kCopyWarp = kMmaWarp + 1, kCleanWarp0 = kMmaWarp + 2;
+  constexpr uint32_t kPCol = kKeys, kOutCol = kPCol + TQ * (kKeys / 2), kTmemCols = TQ * 256;  // tensor memory: S, P of the tiles, O of the tiles
   extern __shared__ unsigned char raw[];
   unsigned char* base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
   uint64_t* bars = reinterpret_cast<uint64_t*>(base);
@@ -151,20 +147,21 @@ __global__ void __launch_bounds__(kThreads, 1)
   volatile int* poison = reinterpret_cast<volatile int*>(base + 520);
   volatile uint32_t* pages_there = reinterpret_cast<volatile uint32_t*>(base + 576);  // [kMasks]: of tile j at j % kMasks, a bit per page
   const uint32_t full = smem_addr(bars), empty = full + 8 * kStages, clean = empty + 8 * kStages, q_full = clean + 8 * kCleans, s_ready = q_full + 8,
-                 p_ready = s_ready + 16, o_ready = p_ready + 32;
-  const uint32_t q_at = smem_addr(base + 1024), ring = q_at + 2 * kTile;
+                 s_free = s_ready + 16, p_ready = s_free + 8, pv_done = p_ready + 32;
+  const uint32_t q_at = smem_addr(base + 1024), ring = q_at + TQ * kTile;
   const approxifer_attention_args& a = g.a;
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int warp = warp_index(), lane = threadIdx.x % 32;
   unsigned int* count = &g_attention_tile_wait_timeouts;
 
   Job job;
-  if (!find_job(g, &job)) return;
+  if (!find_job<TQ>(g, &job)) return;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) bar_init(full + 8 * s, 1), bar_init(empty + 8 * s, 1);
     for (int s = 0; s < kCleans; ++s) bar_init(clean + 8 * s, kCleanWarps);
     bar_init(q_full, 1);
-    for (int t = 0; t < 2; ++t) bar_init(s_ready + 8 * t, 1), bar_init(p_ready + 16 * t, 4), bar_init(p_ready + 16 * t + 8, 4), bar_init(o_ready + 8 * t, 1);
+    bar_init(s_free, 4);
+    for (int t = 0; t < TQ; ++t) bar_init(s_ready + 8 * t, 1), bar_init(p_ready + 16 * t, 4), bar_init(p_ready + 16 * t + 8, 4), bar_init(pv_done + 8 * t, 1);
     *abort = 0;
     *poison = 0;
     bar_init_done();
@@ -172,19 +169,21 @@ __global__ void __launch_bounds__(kThreads, 1)
     prefetch_map(&k_map);
     prefetch_map(&v_map);
   }
-  if (warp == 8) tmem_alloc(smem_addr(tmem_slot), 512);
+  if (warp == kMmaWarp) tmem_alloc(smem_addr(tmem_slot), kTmemCols);
   tmem_fence_before();
   __syncthreads();
   tmem_fence_after();
-  const uint32_t tmem = *tmem_slot;
+  const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
 
-  // The softmax warps keep a row of scores in registers; the four others give up theirs (2 x 128 x 200 + 128 x 104 = 384 x 168).
-  if (warp < 8) {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+  // The softmax warps keep a row of scores in registers; the four others give up theirs (two tiles: 2 x 128 x 200 + 128 x 104
+  // = 384 x 168 registers at the launch; one: 128 x 184 + 128 x 72 = 256 x 128).
+  if (warp < kMmaWarp) {
+    if constexpr (TQ == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+    else asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
     // ---- softmax and output: one thread, one row ----
     const int t = warp / 4, r = threadIdx.x % kRows;
     const uint32_t lanes = (uint32_t)((warp % 4) * 32) << 16;
-    const uint32_t s_at = tmem + lanes + t * kKeys, o_at = tmem + lanes + 2 * kKeys + t * 128;
+    const uint32_t s_at = tmem + lanes, p_at = tmem + lanes + kPCol + t * (kKeys / 2), o_at = tmem + lanes + kOutCol + t * DP;
     const int in_tile = r / g.group, token = t * job.tokens + in_tile;
     const bool mine = in_tile < job.tokens && token < job.left;
     const int pos = job.pos0 + token;
@@ -194,43 +193,57 @@ __global__ void __launch_bounds__(kThreads, 1)
     float m = -CUDART_INF_F, l = 0.f;
     int round = 0;
     bool ok = true;
-    for (int j = 0; j < job.steps; ++j) {
-      if (!job.active(t, j)) continue;
+    for (int j = 0; j < job.steps_of(t); ++j) {
       if (!(ok = warp_wait(s_ready + 8 * t, round & 1, abort, count))) break;
       ++round;
       tmem_fence_after();
       const uint32_t there = pages_there[j % kMasks];
-      float s[kKeys];
+      if (flip || !job.full(t, j) || there != (1u << max(1, kKeys >> g.page_shift)) - 1u) {
+        // what a row does not see becomes minus infinity, in place and in a short loop: few tiles come here, and the code that
+        // all tiles run stays small
+#pragma unroll 1
+        for (int c = 0; c < kKeys; c += 16) {
+          uint32_t v[16];
+          tmem_ld16(s_at + c, v);
+          const uint32_t sees = job.sees(pos, job.tile(j) * kKeys + c) & pages_of(there, c, g.page_shift), sign = flip ? 0x80000000u : 0u;
+          tmem_wait_ld(v);
 #pragma unroll
-      for (int c = 0; c < kKeys; c += 32) tmem_ld32(s_at + c, *reinterpret_cast<uint32_t(*)[32]>(s + c));
-#pragma unroll
-      for (int c = 0; c < kKeys; c += 32) tmem_wait_ld(*reinterpret_cast<uint32_t(*)[32]>(s + c));
-      if (flip) {
-#pragma unroll
-        for (int i = 0; i < kKeys; ++i) s[i] = -s[i];
-      }
-      if (!job.full(t, j) || there != (1u << max(1, kKeys >> g.page_shift)) - 1u) {
-#pragma unroll
-        for (int c = 0; c < kKeys; c += 32) {
-          const uint32_t sees = job.sees(pos, job.tile(j) * kKeys + c) & pages_of(there, c, g.page_shift);
-#pragma unroll
-          for (int i = 0; i < 32; ++i) s[c + i] = (sees >> i) & 1 ? s[c + i] : -CUDART_INF_F;
+          for (int i = 0; i < 16; ++i) v[i] = (sees >> i) & 1 ? v[i] ^ sign : 0xff800000u;
+          tmem_st16(s_at + c, v);
         }
+        tmem_wait_st();
       }
-      float top = max3(s[0], s[1], s[2]), top2 = max3(s[3], s[4], s[5]);
+      float s[kKeys];
+      auto load = [&](int c) { tmem_ld32(s_at + c, *reinterpret_cast<uint32_t(*)[32]>(s + c)); };
+      auto loaded = [&](int c) { tmem_wait_ld(*reinterpret_cast<uint32_t(*)[32]>(s + c)); };
+      float top[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
+      auto maximum = [&](int c) {
 #pragma unroll
-      for (int i = 6; i + 4 <= kKeys; i += 4) top = max3(top, s[i], s[i + 1]), top2 = max3(top2, s[i + 2], s[i + 3]);
-      top = max3(top, s[kKeys - 2], s[kKeys - 1]);
-      top = fmaxf(top, top2);
+        for (int i = 0; i < 64; i += 8)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) top[k] = max3(top[k], s[c + i + 2 * k], s[c + i + 2 * k + 1]);
+      };
+      load(0), load(32);
+      loaded(0), loaded(32);
+      load(64), load(96);
+      maximum(0);
+      loaded(64), loaded(96);
+      tmem_fence_before();
+      __syncwarp();
+      if (lane == 0) bar_arrive(s_free);
+      maximum(64);
+      top[0] = fmaxf(max3(top[0], top[1], top[2]), top[3]);
+      if (round > 1 && !(ok = warp_wait(pv_done + 8 * t, round & 1, abort, count))) break;  // (the last P has been used, O is whole)
+      tmem_fence_after();
       bool grow = false;
       if (m == -CUDART_INF_F) {
-        m = top;  // (nothing summed yet but zeros)
-      } else if ((top - m) * scale > kGrowth) {
+        m = top[0];  // (nothing summed yet but zeros)
+      } else if ((top[0] - m) * scale > kGrowth) {
         grow = true;
       }
       if (__any_sync(0xffffffffu, grow)) {
-        const float keep = grow ? pow2((m - top) * scale) : 1.f;
-        if (grow) m = top;
+        const float keep = grow ? pow2((m - top[0]) * scale) : 1.f;
+        if (grow) m = top[0];
         l *= keep;
 #pragma unroll 1
         for (int c = 0; c < DP; c += 16) {
@@ -258,7 +271,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             sum2[(i / 2) & 1] = add2(sum2[(i / 2) & 1], pack2(x, y));
             p[i / 2] = pack_bf16x2(x, y);
           }
-          tmem_st16(s_at + c / 2, p);  // P takes the place of scores that have been read
+          tmem_st16(p_at + c / 2, p);
         }
         tmem_wait_st();
         tmem_fence_before();
@@ -269,35 +282,35 @@ __global__ void __launch_bounds__(kThreads, 1)
       unpack2(add2(sum2[0], sum2[1]), u, v);
       l += u + v;
     }
-    bool have = false;
-    if (ok && job.steps > 0) {
-      ok = warp_wait(o_ready + 8 * t, 0, abort, count);
-      have = round > 0;
+    const bool have = round > 0;
+    if (ok && have) {
+      ok = warp_wait(pv_done + 8 * t, (round - 1) & 1, abort, count);
       tmem_fence_after();
     }
     if (ok) {
+      // O / sum, by way of the tile's queries' place in shared memory (a warp keeps to its own rows) into whole rows
       const float inv = l == 0.f ? 0.f : 1.f / l;
       const bool add_back = *poison != 0;
-      bf16* out = reinterpret_cast<bf16*>(a.out) + (int64_t)(job.token0 + token) * a.o_tstride + (int64_t)(job.hk * g.group + r % g.group) * a.o_hstride;
+      unsigned char* rows = base + 1024 + t * kTile + (warp % 4) * 32 * DP * 2;
 #pragma unroll 1
-      for (int c = 0; c < DP; c += 32) {
-        float y[32];
+      for (int c = 0; c < DP; c += 16) {
+        float y[16];
         if (have) {
-          uint32_t v[32];
-          tmem_ld32(o_at + c, v);
+          uint32_t v[16];
+          tmem_ld16(o_at + c, v);
           tmem_wait_ld(v);
 #pragma unroll
-          for (int i = 0; i < 32; ++i) y[i] = l == 0.f ? 0.f : __uint_as_float(v[i]) * inv;
+          for (int i = 0; i < 16; ++i) y[i] = l == 0.f ? 0.f : __uint_as_float(v[i]) * inv;
         } else {
 #pragma unroll
-          for (int i = 0; i < 32; ++i) y[i] = 0.f;
+          for (int i = 0; i < 16; ++i) y[i] = 0.f;
         }
         if (mine && add_back) {
           // infinities and NaN that were taken out of tiles seen in part, for the rows that do see them
           const int32_t* table = a.block_table + (int64_t)job.b * a.table_stride;
 #pragma unroll 1
           for (int j = 0; j < job.steps; ++j) {
-            if ((!job.active(0, j) || job.full(0, j)) && (!job.active(1, j) || job.full(1, j))) continue;
+            if (!job.part(j, TQ)) continue;
             const int k0 = job.tile(j) * kKeys;
 #pragma unroll 1
             for (int k = k0; k < k0 + kKeys && k <= min(pos, job.p1); ++k) {
@@ -307,7 +320,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               const bf16* v = reinterpret_cast<const bf16*>(a.v_cache) + page * a.vc_pstride + job.hk * a.vc_hstride +
                               (k & ((1 << g.page_shift) - 1)) * a.vc_rstride;
 #pragma unroll
-              for (int i = 0; i < 32; ++i) {
+              for (int i = 0; i < 16; ++i) {
                 const float x = c + i < a.D ? widen(v[c + i]) : 0.f;
                 if (!isfinite(x)) y[i] += x;
               }
@@ -315,22 +328,31 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
 #pragma unroll
-        for (int i = 0; i < 32; i += 8)
-          if (mine && c + i < a.D)
-            *reinterpret_cast<uint4*>(out + c + i) =
-                make_uint4(pack_bf16x2(y[i], y[i + 1]), pack_bf16x2(y[i + 2], y[i + 3]), pack_bf16x2(y[i + 4], y[i + 5]), pack_bf16x2(y[i + 6], y[i + 7]));
+        for (int i = 0; i < 16; i += 8)
+          *reinterpret_cast<uint4*>(rows + lane * DP * 2 + ((((c + i) / 8) ^ (lane & 7)) << 4)) =
+              make_uint4(pack_bf16x2(y[i], y[i + 1]), pack_bf16x2(y[i + 2], y[i + 3]), pack_bf16x2(y[i + 4], y[i + 5]), pack_bf16x2(y[i + 6], y[i + 7]));
         __syncwarp();
+      }
+      const int64_t to = mine ? (int64_t)(job.token0 + token) * a.o_tstride + (int64_t)(job.hk * g.group + r % g.group) * a.o_hstride : -1;
+      constexpr int kCols = DP / 8;
+#pragma unroll 4
+      for (int x = lane; x < 32 * kCols; x += 32) {
+        const int row = x / kCols, col = x % kCols;
+        const int64_t at = __shfl_sync(0xffffffffu, to, row);
+        if (at >= 0 && col * 8 < a.D)
+          *reinterpret_cast<uint4*>(reinterpret_cast<bf16*>(a.out) + at + col * 8) = *reinterpret_cast<const uint4*>(rows + row * DP * 2 + ((col ^ (row & 7)) << 4));
       }
     }
     tmem_fence_before();
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
-    if (warp == 9) {
+    if constexpr (TQ == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
+    else asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    if (warp == kCopyWarp) {
       // ---- copies ----
       if (lane == 0) {
-        const int boxes = (job.tokens < job.left ? 2 : 1) * (DP / 64);  // (a second tile without rows is not read)
+        const int boxes = (TQ == 2 && job.tokens < job.left ? 2 : 1) * (DP / 64);  // (a second tile without rows is not read)
         bar_expect(q_full, boxes * g.group * job.tokens * 128);
-        for (int t = 0; t < 2 && t * job.tokens < job.left; ++t)
+        for (int t = 0; t < TQ && t * job.tokens < job.left; ++t)
           for (int c = 0; c < DP / 64; ++c) tma_3d(q_at + t * kTile + c * kBlock, &q_map, c * 64, job.hk * g.group, job.token0 + t * job.tokens, q_full);
       }
       const int page_rows = 1 << g.page_shift, rows = min(page_rows, kKeys), per_tile = kKeys / rows;
@@ -359,68 +381,80 @@ __global__ void __launch_bounds__(kThreads, 1)
               tma_4d(ring + s * kTile + c * kBlock + lane * rows * 128, v ? &v_map : &k_map, c * 64, row, job.hk, page, full + 8 * s);
         }
       }
-    } else if (warp == 8) {
+    } else if (warp == kMmaWarp) {
       // ---- products ----
-      if (lane == 0 && job.steps > 0) {
-        bool ok = bar_wait(q_full, 0, abort, count);
-        int done[2] = {0, 0};  // rounds of the softmax of each tile
-        auto scores = [&](int t, int s) {
-#pragma unroll
-          for (int k = 0; k < DP / 16; ++k)
-            mma_ss(tmem + t * kKeys, desc_k_major(q_at + t * kTile + (k / 4) * kBlock) + 2 * (k % 4), desc_k_major(ring + s * kTile + (k / 4) * kBlock) + 2 * (k % 4),
-                   mma_shape(kRows, kKeys), k > 0);
-          mma_commit(s_ready + 8 * t);
+      if (job.steps > 0 && warp_wait(q_full, 0, abort, count)) {
+        // Items: (query tile, key tile) pairs in the order of the key tiles, both query tiles of a key tile while both take
+        // part, then those of tile 1.  S runs TQ items ahead of O.  Every key tile has an item; keys and values are given back
+        // as soon as their last item is issued (what S needs next may be waiting for that place).  This loop feeds the tensor
+        // cores from one warp: it has some 250 instructions' time to an item.
+        const int both = TQ == 2 ? min(job.steps0, job.steps1) : 0, items = job.steps0 + job.steps1;
+        auto place = [&](int n, int& t, int& j, bool& first, bool& last) {
+          const bool two = n < 2 * both;
+          t = TQ == 1 ? 0 : two ? n & 1 : job.steps1 > 0 ? 1 : 0;
+          j = TQ == 1 ? n : two ? n >> 1 : n - both;
+          first = !two || t == 0, last = !two || t == 1;
         };
-        auto wait_full = [&](int i) {
-          const bool got = bar_wait(full + 8 * (i % kStages), (i / kStages) & 1, abort, count);
+        bool ok = true;
+        auto scores = [&](int n) {
+          int t, j;
+          bool first, last;
+          place(n, t, j, first, last);
+          const int i = 2 * j, turn = i / kStages, stage = i - turn * kStages;
+          if (first) ok = warp_wait(full + 8 * stage, turn & 1, abort, count);
+          if (ok && n > 0) ok = warp_wait(s_free, (n - 1) & 1, abort, count);  // the last S is in registers
+          if (!ok) return;
           tmem_fence_after();
-          return got;
-        };
-        ok = ok && wait_full(0);
-        if (ok) {
-          for (int t = 0; t < 2; ++t)
-            if (job.active(t, 0)) scores(t, 0);
-          mma_commit(empty);
-        }
-        for (int j = 0; j < job.steps && ok; ++j) {
-          const int vi = 2 * j + 1, vs = vi % kStages, ki = 2 * j + 2, ks = ki % kStages;
-          const bool more = j + 1 < job.steps;
-          if (!(ok = bar_wait(clean + 8 * (j % kCleans), (j / kCleans) & 1, abort, count))) break;
-          if (more && !(ok = wait_full(ki))) break;
-          for (int t = 0; t < 2 && ok; ++t) {
-            if (job.active(t, j)) {
-              for (int half = 0; half < 2 && ok; ++half) {  // the first half of the keys while the second's weights are formed
-                if (!(ok = bar_wait(p_ready + 16 * t + 8 * half, done[t] & 1, abort, count))) break;
-                tmem_fence_after();
+          const uint64_t qs = desc_k_major(q_at + t * kTile), ks = desc_k_major(ring + stage * kTile);
+          if (elect_one()) {
+            constexpr int kBlock16 = kBlock >> 4;
 #pragma unroll
-                for (int k = 0; k < kKeys / 32; ++k) {
-                  const int kk = half * (kKeys / 32) + k;
-                  mma_ts(tmem + 2 * kKeys + t * 128, tmem + t * kKeys + kk * 8, desc_mn_major(ring + vs * kTile, kBlock) + kk * 128, mma_shape(kRows, DP, true),
-                         done[t] > 0 || kk > 0);
-                }
-              }
-              if (!ok) break;
-              ++done[t];
-            }
-            if (more && job.active(t, j + 1)) scores(t, ks);
+            for (int k = 0; k < DP / 16; ++k)
+              mma_ss(tmem, qs + (k / 4) * kBlock16 + 2 * (k % 4), ks + (k / 4) * kBlock16 + 2 * (k % 4), mma_shape(kRows, kKeys), k > 0);
+            mma_commit(s_ready + 8 * t);
+            if (last) mma_commit(empty + 8 * stage);
           }
+          __syncwarp();
+        };
+        for (int n = 0; n < TQ && n < items && ok; ++n) scores(n);
+        for (int n = 0; n < items && ok; ++n) {
+          if (n + TQ < items) scores(n + TQ);
           if (!ok) break;
-          mma_commit(empty + 8 * vs);
-          if (more) mma_commit(empty + 8 * ks);
+          int t, j;
+          bool first, last;
+          place(n, t, j, first, last);
+          const int i = 2 * j + 1, stage = i % kStages, round = j;  // (a query tile takes part from its first step on)
+          if (first && !(ok = warp_wait(clean + 8 * (j % kCleans), (j / kCleans) & 1, abort, count))) break;
+          const uint64_t vs = desc_mn_major(ring + stage * kTile, kBlock);
+          const uint32_t to = tmem + kOutCol + t * DP, from = tmem + kPCol + t * (kKeys / 2);
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {  // the first half of the keys while the second's weights are formed
+            if (!(ok = warp_wait(p_ready + 16 * t + 8 * half, round & 1, abort, count))) break;
+            tmem_fence_after();
+            if (elect_one()) {
+#pragma unroll
+              for (int k = 0; k < kKeys / 32; ++k)
+                mma_ts(to, from + (half * (kKeys / 32) + k) * 8, vs + (half * (kKeys / 32) + k) * 128, mma_shape(kRows, DP, true), round > 0 || half > 0 || k > 0);
+              if (half == 1) {
+                mma_commit(pv_done + 8 * t);
+                if (last) mma_commit(empty + 8 * stage);
+              }
+            }
+            __syncwarp();
+          }
         }
-        for (int t = 0; t < 2; ++t) mma_commit(o_ready + 8 * t);
       }
-    } else if (warp >= 10) {
+    } else {
       // ---- values of tiles that are seen in part ----
       bool ok = true;
       for (int j = 0; j < job.steps && ok; ++j) {
         const int i = 2 * j + 1, s = i % kStages;
         if (!(ok = warp_wait(full + 8 * s, (i / kStages) & 1, abort, count))) break;
-        const bool part = (job.active(0, j) && !job.full(0, j)) || (job.active(1, j) && !job.full(1, j));
+        const bool part = job.part(j, TQ);
         if (part) {
-          uint4* v = reinterpret_cast<uint4*>(base + 1024 + (2 + s) * kTile);
+          uint4* v = reinterpret_cast<uint4*>(base + 1024 + (TQ + s) * kTile);
           const int k0 = job.tile(j) * kKeys;
-          for (int x = threadIdx.x - 320; x < kTile / 16; x += kCleanWarps * 32) {
+          for (int x = threadIdx.x - kCleanWarp0 * 32; x < kTile / 16; x += kCleanWarps * 32) {
             uint4 u = v[x];
             uint32_t w[4] = {u.x, u.y, u.z, u.w};
             bool bad = false;
@@ -445,9 +479,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   __syncwarp();
   __syncthreads();
   drain_if_aborted(abort);
-  if (warp == 8) {
+  if (warp == kMmaWarp) {
     tmem_fence_after();
-    tmem_free(tmem, 512);
+    tmem_free(tmem, kTmemCols);
   }
 }
 
@@ -461,7 +495,7 @@ cudaError_t launch_one(const TileArgs& g, const CUtensorMap& q, const CUtensorMa
   if ((e = ensure_dynamic_smem<Tag>(kernel, dev->ordinal, smem_bytes(DP))) != cudaSuccess) return e;
   const int64_t ctas = (int64_t)g.blocks * g.a.batch * g.a.Hkv;
   if (ctas > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
-  kernel<<<(unsigned)ctas, kThreads, smem_bytes(DP), stream>>>(q, k, v, g);
+  kernel<<<(unsigned)ctas, threads_of(DP), smem_bytes(DP), stream>>>(q, k, v, g);
   count_launch();
   return cudaGetLastError();
 }
@@ -494,7 +528,8 @@ cudaError_t launch_attention_tile(const approxifer_attention_args& a, cudaStream
   g.a = a;
   g.group = a.Hq / a.Hkv;
   g.tokens = kRows / g.group;
-  g.blocks = (a.max_q + 2 * g.tokens - 1) / (2 * g.tokens);
+  const int per_cta = tiles_of(a.D <= 64 ? 64 : 128) * g.tokens;
+  g.blocks = (int)(((int64_t)a.max_q + per_cta - 1) / per_cta);
   g.page_shift = log2_of(a.page_size);
   const int dp = a.D <= 64 ? 64 : 128;
   CUtensorMap q, k, v;

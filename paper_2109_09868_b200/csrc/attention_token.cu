@@ -23,7 +23,7 @@ constexpr int kThreads = kWarps * 32;
 constexpr int kCtasPerSm = 2;
 constexpr int kRows = 16;   // query heads per unit
 constexpr int kStages = 3;
-constexpr int kJoinWarps = 8;
+constexpr int kJoinWarps = 8, kJoinAhead = 6;
 constexpr unsigned kFull = 0xffffffffu;
 
 constexpr int keys_of(int dp) { return dp <= 64 ? 32 : 16; }                 // keys per chunk
@@ -412,7 +412,7 @@ struct Cursor {
 };
 
 template <int DP, bool WHOLE>
-__global__ void __launch_bounds__(kThreads, kCtasPerSm) attention_token_balanced_kernel(const __grid_constant__ approxifer_attention_args a, int row_tiles,
+__global__ void __launch_bounds__(kThreads, 3) attention_token_balanced_kernel(const __grid_constant__ approxifer_attention_args a, int row_tiles,
                                                                                          int page_shift, float* partial) {
   extern __shared__ __align__(1024) unsigned char smem[];
   const int warp = blockIdx.x * kWarps + threadIdx.x / 32, warps = gridDim.x * kWarps, lane = threadIdx.x % 32;
@@ -515,12 +515,15 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) attention_token_balanced
 }
 
 // Joins the partial results of every unit that more than one run shares, and zeroes the rows that see nothing.  One CTA =
-// one row; its warps take every JW-th partial result, four loads ahead, and meet in shared memory.
+// one row; its warps (for short rows their halves) take the partial results in turn, kJoinAhead loads in flight, and meet in
+// shared memory.
 template <int DP, int JW>
 __global__ void __launch_bounds__(JW * 32) attention_token_join_kernel(const __grid_constant__ approxifer_attention_args a, int row_tiles, int warps,
                                                                               const float* partial) {
-  __shared__ float sy[JW][DP], sm[JW], sl[JW];
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  constexpr int kLanes = DP / 4, kTeams = JW * 32 / kLanes;  // lanes to a partial row, partial rows at a time
+  __shared__ __align__(16) float sy[kTeams][DP];
+  __shared__ float sm[kTeams], sl[kTeams];
+  const int team = threadIdx.x / kLanes, at4 = (threadIdx.x % kLanes) * 4;
   const int units = a.Hkv * row_tiles, group = a.Hq / a.Hkv;
   const int b = blockIdx.x / a.Hq, h = blockIdx.x % a.Hq, in_group = h % group;
   Place at;
@@ -540,45 +543,46 @@ __global__ void __launch_bounds__(JW * 32) attention_token_join_kernel(const __g
   const float* pm = partial + 2 * (int64_t)warps * kRows * DP;
   const int r = in_group % kRows;
   auto part = [&](int w) { return (2 * (int64_t)w + (w == w0 ? 1 : 0)) * kRows + r; };  // the first of them ends inside the unit
-  float m = -CUDART_INF_F, l = 0.f, y[DP / 32] = {};
-  for (int w = w0 + warp; w <= w1; w += 4 * JW) {
-    float2 ml[4], v[4][DP / 64];
+  float m = -CUDART_INF_F, l = 0.f;
+  float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int w = w0 + team; w <= w1; w += kJoinAhead * kTeams) {
+    float2 ml[kJoinAhead];
+    float4 v[kJoinAhead];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int wi = w + i * JW;
-      const int64_t p = part(wi <= w1 ? wi : w1);
-      ml[i] = __ldcg(reinterpret_cast<const float2*>(pm + p * 2));
-      if (wi > w1) ml[i] = make_float2(-CUDART_INF_F, 0.f);
-#pragma unroll
-      for (int c = 0; c < DP / 64; ++c) v[i][c] = __ldcg(reinterpret_cast<const float2*>(partial + p * DP + c * 64 + lane * 2));
+    for (int i = 0; i < kJoinAhead; ++i) {
+      const int wi = w + i * kTeams;
+      ml[i] = make_float2(-CUDART_INF_F, 0.f);
+      v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (wi <= w1) {
+        const int64_t p = part(wi);
+        ml[i] = __ldcg(reinterpret_cast<const float2*>(pm + p * 2));
+        v[i] = __ldcg(reinterpret_cast<const float4*>(partial + p * DP + at4));
+      }
     }
-    const float top = fmaxf(fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)), m), base = top == -CUDART_INF_F ? 0.f : top;
-    const float keep = pow2(m - base);
-    l *= keep;
+    float top = m;
 #pragma unroll
-    for (int c = 0; c < DP / 32; ++c) y[c] *= keep;
+    for (int i = 0; i < kJoinAhead; ++i) top = fmaxf(top, ml[i].x);
+    const float base = top == -CUDART_INF_F ? 0.f : top, keep = pow2(m - base);
+    l *= keep, y.x *= keep, y.y *= keep, y.z *= keep, y.w *= keep;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (w + i * JW > w1) break;  // (what a row that has only NaN holds must not be scaled by zero)
+    for (int i = 0; i < kJoinAhead; ++i) {
       const float k = pow2(ml[i].x - base);
       l = fmaf(k, ml[i].y, l);
-#pragma unroll
-      for (int c = 0; c < DP / 64; ++c) y[2 * c] = fmaf(k, v[i][c].x, y[2 * c]), y[2 * c + 1] = fmaf(k, v[i][c].y, y[2 * c + 1]);
+      y.x = fmaf(k, v[i].x, y.x), y.y = fmaf(k, v[i].y, y.y), y.z = fmaf(k, v[i].z, y.z), y.w = fmaf(k, v[i].w, y.w);
     }
     m = top;
   }
-  if (lane == 0) sm[warp] = m, sl[warp] = l;
-#pragma unroll
-  for (int c = 0; c < DP / 64; ++c) *reinterpret_cast<float2*>(&sy[warp][c * 64 + lane * 2]) = make_float2(y[2 * c], y[2 * c + 1]);
+  if (at4 == 0) sm[team] = m, sl[team] = l;
+  *reinterpret_cast<float4*>(&sy[team][at4]) = y;
   __syncthreads();
   float best = sm[0];
 #pragma unroll
-  for (int w = 1; w < JW; ++w) best = fmaxf(best, sm[w]);
+  for (int w = 1; w < kTeams; ++w) best = fmaxf(best, sm[w]);
   if (best == -CUDART_INF_F) best = 0.f;
   for (int d = threadIdx.x; d < a.D; d += JW * 32) {
     float sum = 0.f, z = 0.f;
 #pragma unroll
-    for (int w = 0; w < JW; ++w) {
+    for (int w = 0; w < kTeams; ++w) {
       const float k = pow2(sm[w] - best);
       sum = fmaf(k, sl[w], sum);
       z = fmaf(k, sy[w][d], z);

@@ -4,7 +4,7 @@
 // tile runs under the products of the next.
 //
 //   warp 0      one lane: tensor-map copies of this CTA's operands, six stages of 64 columns (32 KB) in flight
-//   warp 1      one lane of the pair's first CTA: tcgen05.mma for the pair; allocates the tensor memory
+//   warp 1      of the pair's first CTA: tcgen05.mma for the pair; allocates the tensor memory
 //   warps 2, 3  idle (the accumulator's lanes belong to warps by their index modulo 4)
 //   warps 4-11  epilogue: two warps to each quarter of the lanes, half of the columns each; bias, activation, residual,
 //               one rounding, 16-byte stores (a thread owns 64 bytes or more of one row at a time)
@@ -100,7 +100,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(base + 516);
   const uint32_t stages = smem_addr(base + kHeader);
   const uint32_t full = smem_addr(bars), empty = full + 8 * kStages, ready = empty + 8 * kStages, drained = ready + 16;
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int warp = warp_index(), lane = threadIdx.x % 32;
   const int rank = (int)cluster_rank();
   const int pair = blockIdx.x / 2, pairs = gridDim.x / 2;
   unsigned int* count = &g_linear_pair_wait_timeouts;
@@ -118,7 +118,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
   __syncthreads();
   cluster_sync();  // both CTAs' barriers stand before any is signalled from the other
   tmem_fence_after();
-  const uint32_t tmem = *tmem_slot;
+  const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
 
   if (warp == 0 && lane == 0) {
     int it = 0;
@@ -136,24 +136,28 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
         tma_2d_pair(dst + kHalfBytes, &w_map, k * kDepth, n0, bar);
       }
     }
-  } else if (warp == 1 && lane == 0 && rank == 0) {
+  } else if (warp == 1 && rank == 0) {
     int it = 0, n = 0;
     bool ok = true;
     for (int tile = pair; tile < a.tiles && ok; tile += pairs, ++n) {
       const int acc = n & 1;
-      if (n >= 2 && !(ok = bar_wait(drained + 8 * acc, (n / 2 - 1) & 1, abort, count))) break;
+      if (n >= 2 && !(ok = warp_wait(drained + 8 * acc, (n / 2 - 1) & 1, abort, count))) break;
       tmem_fence_after();
       for (int k = 0; k < a.steps; ++k, ++it) {
         const int s = it % kStages, turn = it / kStages;
-        if (!(ok = bar_wait(full + 8 * s, turn & 1, abort, count))) break;
+        if (!(ok = warp_wait(full + 8 * s, turn & 1, abort, count))) break;
         tmem_fence_after();
         const uint32_t src = stages + s * kStageBytes;
         const uint64_t da = desc_k_major(src), db = desc_k_major(src + kHalfBytes);
+        if (elect_one()) {
 #pragma unroll
-        for (int j = 0; j < kDepth / 16; ++j) mma_ss_pair(tmem + acc * kTileN, da + 2 * j, db + 2 * j, mma_shape(kTileM, kTileN), k > 0 || j > 0);
-        mma_commit_pair(empty + 8 * s);
+          for (int j = 0; j < kDepth / 16; ++j) mma_ss_pair(tmem + acc * kTileN, da + 2 * j, db + 2 * j, mma_shape(kTileM, kTileN), k > 0 || j > 0);
+          mma_commit_pair(empty + 8 * s);
+        }
+        __syncwarp();
       }
-      if (ok) mma_commit_pair(ready + 8 * acc);
+      if (ok && elect_one()) mma_commit_pair(ready + 8 * acc);
+      __syncwarp();
     }
   } else if (warp >= 4) {
     const int q = warp % 4, half = (warp - 4) / 4;

@@ -10,7 +10,7 @@
 // over its share of the tile (the same order every time) and applies the epilogue to it.
 //
 //   warp 0     one lane: tensor-map copies, 64 columns of both operands per stage, up to 10 stages in flight
-//   warp 1     one lane: tcgen05.mma; allocates the tensor memory
+//   warp 1     tcgen05.mma; allocates the tensor memory
 //   warps 2-5  accumulator -> shared memory; all warps: sum, epilogue, stores
 #include "async.cuh"
 
@@ -94,7 +94,7 @@ __global__ void __launch_bounds__(kThreads) linear_tile_kernel(const __grid_cons
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(base + 516);
   unsigned char* stages = base + kHeader;
   const uint32_t full = smem_addr(bars), empty = full + 8 * kStages, done = empty + 8 * kStages;
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int warp = warp_index(), lane = threadIdx.x % 32;
 
   const int S = (int)cluster_size(), rank = (int)cluster_rank();
   const int tile = blockIdx.x / S;
@@ -113,7 +113,7 @@ __global__ void __launch_bounds__(kThreads) linear_tile_kernel(const __grid_cons
   tmem_fence_before();
   __syncthreads();
   tmem_fence_after();
-  const uint32_t tmem = *tmem_slot;
+  const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
 
   if (warp == 0 && lane == 0) {
     for (int i = step0; i < step1; ++i) {
@@ -124,20 +124,21 @@ __global__ void __launch_bounds__(kThreads) linear_tile_kernel(const __grid_cons
       tma_2d(dst, &rows_map, i * kDepth, row0, full + 8 * s);
       tma_2d(dst + kLanes * kDepth * 2, &cols_map, i * kDepth, col0, full + 8 * s);
     }
-  } else if (warp == 1 && lane == 0) {
-    bool ok = true;
-    for (int i = step0; i < step1 && ok; ++i) {
+  } else if (warp == 1) {
+    for (int i = step0; i < step1; ++i) {
       const int s = (i - step0) % kStages, turn = (i - step0) / kStages;
-      ok = bar_wait(full + 8 * s, turn & 1, abort, &g_linear_tile_wait_timeouts);
-      if (!ok) break;
+      if (!warp_wait(full + 8 * s, turn & 1, abort, &g_linear_tile_wait_timeouts)) break;
       tmem_fence_after();
       const uint32_t src = smem_addr(stages) + s * stage_bytes(BN);
       const uint64_t da = desc_k_major(src), db = desc_k_major(src + kLanes * kDepth * 2);
+      if (elect_one()) {
 #pragma unroll
-      for (int k = 0; k < kDepth / 16; ++k) mma_ss(tmem, da + 2 * k, db + 2 * k, mma_shape(kLanes, BN), i > step0 || k > 0);
-      mma_commit(empty + 8 * s);
+        for (int k = 0; k < kDepth / 16; ++k) mma_ss(tmem, da + 2 * k, db + 2 * k, mma_shape(kLanes, BN), i > step0 || k > 0);
+        mma_commit(empty + 8 * s);
+      }
+      __syncwarp();
     }
-    mma_commit(done);
+    if (elect_one()) mma_commit(done);
   }
   __syncwarp();
   // Accumulator -> shared memory, in the order of the output: [m][n], n contiguous.  (`done` also says that every copy has

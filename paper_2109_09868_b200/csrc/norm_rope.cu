@@ -81,37 +81,46 @@ __global__ void __launch_bounds__(kElementThreads) norm_rope_element_kernel(cons
 //     y_d = r (x_d A_d + x_p(d) B_d),    A_d = w_d cos,  B_d = -+ w_p(d) sin,   p(d) the other element of d's pair,
 // with r the reciprocal root mean square of the row.  The pair's other element comes from another lane (halves) or from
 // the lane's own column (neighbouring pairs).
-constexpr int kThreads = 256;
+constexpr int kThreads = 128;
 constexpr int kAhead = 4;
-constexpr int kBatches = 2;
+constexpr int kBatches = 1;
 
 template <typename T>
 struct Column;
 template <>
 struct Column<bf16> {
   static constexpr int kElems = 8;
-  static __device__ __forceinline__ void widen8(const uint4& u, float (&x)[8]) {
+  static __device__ __forceinline__ void get(const uint4& u, uint64_t (&x)[4]) {
     const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(w[i] << 16), x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    for (int i = 0; i < 4; ++i) x[i] = pack2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
   }
-  static __device__ __forceinline__ uint4 narrow8(const float (&x)[8]) {
-    return make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+  static __device__ __forceinline__ uint4 put(const uint64_t (&x)[4]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float lo, hi;
+      unpack2(x[i], lo, hi);
+      w[i] = pack_bf16x2(lo, hi);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
   }
 };
 template <>
 struct Column<float> {
   static constexpr int kElems = 4;
-  static __device__ __forceinline__ void widen8(const uint4& u, float (&x)[4]) {
-    x[0] = __uint_as_float(u.x), x[1] = __uint_as_float(u.y), x[2] = __uint_as_float(u.z), x[3] = __uint_as_float(u.w);
+  static __device__ __forceinline__ void get(const uint4& u, uint64_t (&x)[2]) {
+    x[0] = pack2(__uint_as_float(u.x), __uint_as_float(u.y)), x[1] = pack2(__uint_as_float(u.z), __uint_as_float(u.w));
   }
-  static __device__ __forceinline__ uint4 narrow8(const float (&x)[4]) {
-    return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+  static __device__ __forceinline__ uint4 put(const uint64_t (&x)[2]) {
+    float a, b, c, d;
+    unpack2(x[0], a, b), unpack2(x[1], c, d);
+    return make_uint4(__float_as_uint(a), __float_as_uint(b), __float_as_uint(c), __float_as_uint(d));
   }
 };
 
 template <typename T, int L>
-__global__ void __launch_bounds__(kThreads, 4) norm_rope_kernel(const __grid_constant__ approxifer_norm_rope_args a, int q_units, int kv_units) {
+__global__ void __launch_bounds__(kThreads, 8) norm_rope_kernel(const __grid_constant__ approxifer_norm_rope_args a, int q_units, int kv_units) {
   constexpr int E = Column<T>::kElems, kSide = 32 / L;  // elements of a column, rows side by side
   const int lane = threadIdx.x % 32, at = lane % L, side = lane / L;
   const int units = q_units + (a.k ? kv_units : 0) + (a.v ? kv_units : 0);
@@ -183,33 +192,34 @@ __global__ void __launch_bounds__(kThreads, 4) norm_rope_kernel(const __grid_con
   const bool turned = d0 < a.rot, second = d0 >= half;
   const int partner = (turned && !a.interleaved) ? (second ? d0 - half : d0 + half) : d0;
   const int from = side * L + partner / E;
-  float A[E], B[E];
+  uint64_t A[E / 2], B[E / 2];
   {
-    float w[E], wp[E];
+    uint64_t w[E / 2], wp[E / 2];
 #pragma unroll
-    for (int e = 0; e < E; ++e) w[e] = wp[e] = 1.f;
+    for (int e = 0; e < E / 2; ++e) w[e] = wp[e] = pack2(1.f, 1.f);
     if (weight && live) {
-      Column<T>::widen8(__ldg(reinterpret_cast<const uint4*>(weight + d0)), w);
-      Column<T>::widen8(__ldg(reinterpret_cast<const uint4*>(weight + partner)), wp);
+      Column<T>::get(__ldg(reinterpret_cast<const uint4*>(weight + d0)), w);
+      Column<T>::get(__ldg(reinterpret_cast<const uint4*>(weight + partner)), wp);
     }
 #pragma unroll
-    for (int e = 0; e < E; ++e) A[e] = w[e], B[e] = 0.f;
+    for (int e = 0; e < E / 2; ++e) A[e] = w[e], B[e] = 0;
     if (turned) {
       const float* cs = a.cos_sin + (int64_t)pos * a.rot + (a.interleaved ? d0 / 2 : second ? d0 - half : d0);
       if (a.interleaved) {
 #pragma unroll
-        for (int e = 0; e < E; e += 2) {
-          const float c = __ldg(cs + e / 2), s = __ldg(cs + half + e / 2);
-          A[e] = w[e] * c, A[e + 1] = w[e + 1] * c;
-          B[e] = -wp[e + 1] * s, B[e + 1] = wp[e] * s;
+        for (int e = 0; e < E / 2; ++e) {
+          const float c = __ldg(cs + e), s = __ldg(cs + half + e);
+          float x, y;
+          unpack2(wp[e], x, y);
+          A[e] = mul2(w[e], pack2(c, c)), B[e] = pack2(-y * s, x * s);
         }
       } else {
+        const float sign = second ? 1.f : -1.f;
 #pragma unroll
-        for (int e = 0; e < E; e += 4) {
-          const float4 c = __ldg(reinterpret_cast<const float4*>(cs + e)), s = __ldg(reinterpret_cast<const float4*>(cs + half + e));
-          const float sign = second ? 1.f : -1.f;
-          A[e] = w[e] * c.x, A[e + 1] = w[e + 1] * c.y, A[e + 2] = w[e + 2] * c.z, A[e + 3] = w[e + 3] * c.w;
-          B[e] = sign * wp[e] * s.x, B[e + 1] = sign * wp[e + 1] * s.y, B[e + 2] = sign * wp[e + 2] * s.z, B[e + 3] = sign * wp[e + 3] * s.w;
+        for (int e = 0; e < E / 2; e += 2) {
+          const float4 c = __ldg(reinterpret_cast<const float4*>(cs + 2 * e)), s = __ldg(reinterpret_cast<const float4*>(cs + half + 2 * e));
+          A[e] = mul2(w[e], pack2(c.x, c.y)), A[e + 1] = mul2(w[e + 1], pack2(c.z, c.w));
+          B[e] = mul2(wp[e], pack2(sign * s.x, sign * s.y)), B[e + 1] = mul2(wp[e + 1], pack2(sign * s.z, sign * s.w));
         }
       }
     }
@@ -222,10 +232,13 @@ __global__ void __launch_bounds__(kThreads, 4) norm_rope_kernel(const __grid_con
     for (int i = 0; i < kAhead; ++i) {
       const int h = h0 + (batch * kAhead + i) * kSide;
       if (h - side >= heads) break;  // (the whole warp)
-      float v[E], p[E], sq = 0.f;
-      Column<T>::widen8(x[i], v);
+      uint64_t v[E / 2], p[E / 2], sq2 = 0;
+      Column<T>::get(x[i], v);
 #pragma unroll
-      for (int e = 0; e < E; ++e) sq = fmaf(v[e], v[e], sq);
+      for (int e = 0; e < E / 2; ++e) sq2 = fma2(v[e], v[e], sq2);
+      float sq, sq_hi;
+      unpack2(sq2, sq, sq_hi);
+      sq += sq_hi;
 #pragma unroll
       for (int d = L / 2; d > 0; d >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, d);
       const float r = weight ? rsqrtf(sq * inv_d + a.eps) : 1.f;
@@ -235,17 +248,19 @@ __global__ void __launch_bounds__(kThreads, 4) norm_rope_kernel(const __grid_con
         other.z = __shfl_sync(0xffffffffu, other.z, from), other.w = __shfl_sync(0xffffffffu, other.w, from);
       }
       if (!turned) other = make_uint4(0, 0, 0, 0);  // (an element that is not turned has no part in a pair, even where it is infinite)
-      Column<T>::widen8(other, p);
+      Column<T>::get(other, p);
       if (a.interleaved) {
 #pragma unroll
-        for (int e = 0; e < E; e += 2) {
-          const float q = p[e];
-          p[e] = p[e + 1], p[e + 1] = q;
+        for (int e = 0; e < E / 2; ++e) {
+          float lo, hi;
+          unpack2(p[e], lo, hi);
+          p[e] = pack2(hi, lo);
         }
       }
+      const uint64_t r2 = pack2(r, r);
 #pragma unroll
-      for (int e = 0; e < E; ++e) v[e] = r * fmaf(v[e], A[e], p[e] * B[e]);
-      if (live && h < heads) *reinterpret_cast<uint4*>(out + h * out_h + d0) = Column<T>::narrow8(v);
+      for (int e = 0; e < E / 2; ++e) v[e] = mul2(r2, fma2(v[e], A[e], mul2(p[e], B[e])));
+      if (live && h < heads) *reinterpret_cast<uint4*>(out + h * out_h + d0) = Column<T>::put(v);
     }
   }
 }
