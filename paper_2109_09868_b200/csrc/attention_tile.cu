@@ -15,9 +15,10 @@
 // division by the sum makes up for it), which after the first tiles is hardly ever.
 //
 //   4 warps a tile   softmax and output
-//   1 warp           tcgen05.mma; allocates the tensor memory
+//   1 warp           tcgen05.mma for S; allocates the tensor memory
+//   1 warp           tcgen05.mma for O (one warp for both has too much to do between two products)
 //   1 warp           tensor-map copies: keys and values by pages, a lane to a page; pages that are not there read as zeros
-//   2 warps          look through the values of tiles that some rows see only in part: a weight of zero must meet no
+//   1 warp           looks through the values of tiles that some rows see only in part: a weight of zero must meet no
 //                    infinity or NaN, so such elements are taken out, and where a row does see them the output adds them back
 #include "async.cuh"
 
@@ -29,8 +30,7 @@ namespace {
 
 constexpr int kRows = 128;  // query rows per tile
 constexpr int kKeys = 128;  // keys per tile
-constexpr int kCleanWarps = 2;
-constexpr int kOtherWarps = 2 + kCleanWarps;
+constexpr int kOtherWarps = 4;
 constexpr int kBlock = kRows * 128;  // bytes of 64 columns of a tile
 constexpr float kGrowth = 8.f;       // log2 of what the maximum in use may lag behind
 
@@ -40,8 +40,8 @@ constexpr int tile_bytes(int dp) { return kBlock * (dp / 64); }
 constexpr int tiles_of(int dp) { return dp == 64 ? 1 : 2; }
 constexpr int threads_of(int dp) { return (4 * tiles_of(dp) + kOtherWarps) * 32; }
 constexpr int kStages = 5;
-// Rings of one entry per tile of keys.  An entry is used again only after the products of four tiles before it have been
-// issued (the copies that lead there wait for their stages), and those wait for all that the tile's readers do.
+// Rings of one entry per tile of keys.  The copies go in order through kStages places, so that the values of tile j + 4, or
+// the keys of tile j + 8, are asked for only after those of tile j have been used and given back.
 constexpr int kCleans = 4, kMasks = 8;
 constexpr int smem_bytes(int dp) { return 1024 + 1024 + (tiles_of(dp) + kStages) * tile_bytes(dp); }
 
@@ -132,12 +132,31 @@ __device__ __forceinline__ float max3(float a, float b, float c) {  // (a NaN is
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
+// All ones over the elements of a pair of bfloat16 that are infinite or NaN.
+__device__ __forceinline__ uint32_t bad_elements(uint32_t w) {
+  const uint32_t e = (w & 0x7f807f80u) + 0x00800080u;  // an exponent of all ones carries into the sign's place
+  return ((e >> 15) & 0x00010001u) * 0xffffu;
+}
+
+// The n-th (query tile, key tile) pair; the first or the last of its key tile.  (A query tile takes part from step 0 on.)
+struct Item {
+  int t, j;
+  bool first, last;
+};
+template <int TQ>
+__device__ __forceinline__ Item item_at(const Job& job, int n) {
+  if (TQ == 1) return {0, n, true, true};
+  const int both = min(job.steps0, job.steps1);
+  if (n < 2 * both) return {n & 1, n >> 1, (n & 1) == 0, (n & 1) == 1};
+  return {job.steps1 > 0 ? 1 : 0, n - both, true, true};
+}
+
 template <int DP>
 __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
     attention_tile_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
                           const __grid_constant__ TileArgs g) {
   constexpr int TQ = tiles_of(DP), kTile = tile_bytes(DP);
-  constexpr int kMmaWarp = 4 * TQ, kCopyWarp = kMmaWarp + 1, kCleanWarp0 = kMmaWarp + 2;
+  constexpr int kScoreWarp = 4 * TQ, kOutWarp = kScoreWarp + 1, kCopyWarp = kScoreWarp + 2;
   constexpr uint32_t kPCol = kKeys, kOutCol = kPCol + TQ * (kKeys / 2), kTmemCols = TQ * 256;  // tensor memory: S, P of the tiles, O of the tiles
   extern __shared__ unsigned char raw[];
   unsigned char* base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
@@ -153,12 +172,9 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
   const int warp = warp_index(), lane = threadIdx.x % 32;
   unsigned int* count = &g_attention_tile_wait_timeouts;
 
-  Job job;
-  if (!find_job<TQ>(g, &job)) return;
-
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) bar_init(full + 8 * s, 1), bar_init(empty + 8 * s, 1);
-    for (int s = 0; s < kCleans; ++s) bar_init(clean + 8 * s, kCleanWarps);
+    for (int s = 0; s < kCleans; ++s) bar_init(clean + 8 * s, 1);
     bar_init(q_full, 1);
     bar_init(s_free, 4);
     for (int t = 0; t < TQ; ++t) bar_init(s_ready + 8 * t, 1), bar_init(p_ready + 16 * t, 4), bar_init(p_ready + 16 * t + 8, 4), bar_init(pv_done + 8 * t, 1);
@@ -169,7 +185,18 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
     prefetch_map(&k_map);
     prefetch_map(&v_map);
   }
-  if (warp == kMmaWarp) tmem_alloc(smem_addr(tmem_slot), kTmemCols);
+  Job job;
+  if (!find_job<TQ>(g, &job)) return;
+  // (copies) the page of this lane's rows of a key tile, looked up a tile ahead
+  const int32_t* table = a.block_table + (int64_t)job.b * a.table_stride;
+  const int page_rows = 1 << g.page_shift, rows = min(page_rows, kKeys), per_tile = kKeys / rows;
+  auto page_of = [&](int j) -> int32_t {
+    if (j >= job.steps || lane >= per_tile) return -1;
+    const int64_t at = (int64_t)((job.tile(j) * kKeys) >> g.page_shift) + lane;
+    return at < a.table_pages ? __ldg(table + at) : -1;
+  };
+  int32_t page_ahead = warp == kCopyWarp ? page_of(0) : -1;
+  if (warp == kScoreWarp) tmem_alloc(smem_addr(tmem_slot), kTmemCols);
   tmem_fence_before();
   __syncthreads();
   tmem_fence_after();
@@ -177,7 +204,7 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
 
   // The softmax warps keep a row of scores in registers; the four others give up theirs (two tiles: 2 x 128 x 200 + 128 x 104
   // = 384 x 168 registers at the launch; one: 128 x 184 + 128 x 72 = 256 x 128).
-  if (warp < kMmaWarp) {
+  if (warp < kScoreWarp) {
     if constexpr (TQ == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
     else asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
     // ---- softmax and output: one thread, one row ----
@@ -201,15 +228,16 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
       if (flip || !job.full(t, j) || there != (1u << max(1, kKeys >> g.page_shift)) - 1u) {
         // what a row does not see becomes minus infinity, in place and in a short loop: few tiles come here, and the code that
         // all tiles run stays small
+        const uint32_t sign = flip ? 0x80000000u : 0u;
 #pragma unroll 1
-        for (int c = 0; c < kKeys; c += 16) {
-          uint32_t v[16];
-          tmem_ld16(s_at + c, v);
-          const uint32_t sees = job.sees(pos, job.tile(j) * kKeys + c) & pages_of(there, c, g.page_shift), sign = flip ? 0x80000000u : 0u;
+        for (int c = 0; c < kKeys; c += 32) {
+          uint32_t v[32];
+          tmem_ld32(s_at + c, v);
+          const uint32_t sees = job.sees(pos, job.tile(j) * kKeys + c) & pages_of(there, c, g.page_shift);
           tmem_wait_ld(v);
 #pragma unroll
-          for (int i = 0; i < 16; ++i) v[i] = (sees >> i) & 1 ? v[i] ^ sign : 0xff800000u;
-          tmem_st16(s_at + c, v);
+          for (int i = 0; i < 32; ++i) v[i] = sees & (1u << i) ? v[i] ^ sign : 0xff800000u;
+          tmem_st32(s_at + c, v);
         }
         tmem_wait_st();
       }
@@ -291,7 +319,7 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
       // O / sum, by way of the tile's queries' place in shared memory (a warp keeps to its own rows) into whole rows
       const float inv = l == 0.f ? 0.f : 1.f / l;
       const bool add_back = *poison != 0;
-      unsigned char* rows = base + 1024 + t * kTile + (warp % 4) * 32 * DP * 2;
+      unsigned char* own_rows = base + 1024 + t * kTile + (warp % 4) * 32 * DP * 2;
 #pragma unroll 1
       for (int c = 0; c < DP; c += 16) {
         float y[16];
@@ -307,7 +335,6 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
         }
         if (mine && add_back) {
           // infinities and NaN that were taken out of tiles seen in part, for the rows that do see them
-          const int32_t* table = a.block_table + (int64_t)job.b * a.table_stride;
 #pragma unroll 1
           for (int j = 0; j < job.steps; ++j) {
             if (!job.part(j, TQ)) continue;
@@ -329,7 +356,7 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
         }
 #pragma unroll
         for (int i = 0; i < 16; i += 8)
-          *reinterpret_cast<uint4*>(rows + lane * DP * 2 + ((((c + i) / 8) ^ (lane & 7)) << 4)) =
+          *reinterpret_cast<uint4*>(own_rows + lane * DP * 2 + ((((c + i) / 8) ^ (lane & 7)) << 4)) =
               make_uint4(pack_bf16x2(y[i], y[i + 1]), pack_bf16x2(y[i + 2], y[i + 3]), pack_bf16x2(y[i + 4], y[i + 5]), pack_bf16x2(y[i + 6], y[i + 7]));
         __syncwarp();
       }
@@ -340,7 +367,7 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
         const int row = x / kCols, col = x % kCols;
         const int64_t at = __shfl_sync(0xffffffffu, to, row);
         if (at >= 0 && col * 8 < a.D)
-          *reinterpret_cast<uint4*>(reinterpret_cast<bf16*>(a.out) + at + col * 8) = *reinterpret_cast<const uint4*>(rows + row * DP * 2 + ((col ^ (row & 7)) << 4));
+          *reinterpret_cast<uint4*>(reinterpret_cast<bf16*>(a.out) + at + col * 8) = *reinterpret_cast<const uint4*>(own_rows + row * DP * 2 + ((col ^ (row & 7)) << 4));
       }
     }
     tmem_fence_before();
@@ -355,14 +382,11 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
         for (int t = 0; t < TQ && t * job.tokens < job.left; ++t)
           for (int c = 0; c < DP / 64; ++c) tma_3d(q_at + t * kTile + c * kBlock, &q_map, c * 64, job.hk * g.group, job.token0 + t * job.tokens, q_full);
       }
-      const int page_rows = 1 << g.page_shift, rows = min(page_rows, kKeys), per_tile = kKeys / rows;
-      const int32_t* table = a.block_table + (int64_t)job.b * a.table_stride;
       bool ok = true;
       for (int j = 0; j < job.steps && ok; ++j) {
         const int k0 = job.tile(j) * kKeys;
-        const int64_t at = (int64_t)(k0 >> g.page_shift) + lane;
-        int32_t page = -1;
-        if (lane < per_tile && at < a.table_pages) page = __ldg(table + at);
+        int32_t page = page_ahead;
+        page_ahead = page_of(j + 1);
         const bool there = page >= 0 && page < a.num_pages;
         if (!there) page = (int32_t)a.num_pages;  // beyond the array: zeros
         const uint32_t mask = __ballot_sync(0xffffffffu, there);
@@ -381,67 +405,54 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
               tma_4d(ring + s * kTile + c * kBlock + lane * rows * 128, v ? &v_map : &k_map, c * 64, row, job.hk, page, full + 8 * s);
         }
       }
-    } else if (warp == kMmaWarp) {
-      // ---- products ----
+    } else if (warp == kScoreWarp) {
+      // ---- S ----
+      // Items: (query tile, key tile) pairs in the order of the key tiles, both query tiles of a key tile while both take part,
+      // then those of tile 1.  Every key tile has an item; its keys, and its values, are given back with the last.
       if (job.steps > 0 && warp_wait(q_full, 0, abort, count)) {
-        // Items: (query tile, key tile) pairs in the order of the key tiles, both query tiles of a key tile while both take
-        // part, then those of tile 1.  S runs TQ items ahead of O.  Every key tile has an item; keys and values are given back
-        // as soon as their last item is issued (what S needs next may be waiting for that place).  This loop feeds the tensor
-        // cores from one warp: it has some 250 instructions' time to an item.
-        const int both = TQ == 2 ? min(job.steps0, job.steps1) : 0, items = job.steps0 + job.steps1;
-        auto place = [&](int n, int& t, int& j, bool& first, bool& last) {
-          const bool two = n < 2 * both;
-          t = TQ == 1 ? 0 : two ? n & 1 : job.steps1 > 0 ? 1 : 0;
-          j = TQ == 1 ? n : two ? n >> 1 : n - both;
-          first = !two || t == 0, last = !two || t == 1;
-        };
-        bool ok = true;
-        auto scores = [&](int n) {
-          int t, j;
-          bool first, last;
-          place(n, t, j, first, last);
-          const int i = 2 * j, turn = i / kStages, stage = i - turn * kStages;
-          if (first) ok = warp_wait(full + 8 * stage, turn & 1, abort, count);
-          if (ok && n > 0) ok = warp_wait(s_free, (n - 1) & 1, abort, count);  // the last S is in registers
-          if (!ok) return;
+        const int items = job.steps0 + job.steps1;
+        for (int n = 0; n < items; ++n) {
+          const Item x = item_at<TQ>(job, n);
+          const int i = 2 * x.j, turn = i / kStages, stage = i - turn * kStages;
+          if (x.first && !warp_wait(full + 8 * stage, turn & 1, abort, count)) break;
+          if (n > 0 && !warp_wait(s_free, (n - 1) & 1, abort, count)) break;  // the last S is in registers
           tmem_fence_after();
-          const uint64_t qs = desc_k_major(q_at + t * kTile), ks = desc_k_major(ring + stage * kTile);
+          const uint64_t qs = desc_k_major(q_at + x.t * kTile), ks = desc_k_major(ring + stage * kTile);
           if (elect_one()) {
             constexpr int kBlock16 = kBlock >> 4;
 #pragma unroll
             for (int k = 0; k < DP / 16; ++k)
               mma_ss(tmem, qs + (k / 4) * kBlock16 + 2 * (k % 4), ks + (k / 4) * kBlock16 + 2 * (k % 4), mma_shape(kRows, kKeys), k > 0);
-            mma_commit(s_ready + 8 * t);
-            if (last) mma_commit(empty + 8 * stage);
+            mma_commit(s_ready + 8 * x.t);
+            if (x.last) mma_commit(empty + 8 * stage);
           }
           __syncwarp();
-        };
-        for (int n = 0; n < TQ && n < items && ok; ++n) scores(n);
-        for (int n = 0; n < items && ok; ++n) {
-          if (n + TQ < items) scores(n + TQ);
-          if (!ok) break;
-          int t, j;
-          bool first, last;
-          place(n, t, j, first, last);
-          const int i = 2 * j + 1, stage = i % kStages, round = j;  // (a query tile takes part from its first step on)
-          if (first && !(ok = warp_wait(clean + 8 * (j % kCleans), (j / kCleans) & 1, abort, count))) break;
-          const uint64_t vs = desc_mn_major(ring + stage * kTile, kBlock);
-          const uint32_t to = tmem + kOutCol + t * DP, from = tmem + kPCol + t * (kKeys / 2);
+        }
+      }
+    } else if (warp == kOutWarp) {
+      // ---- O ----
+      const int items = job.steps0 + job.steps1;
+      bool ok = true;
+      for (int n = 0; n < items && ok; ++n) {
+        const Item x = item_at<TQ>(job, n);
+        const int stage = (2 * x.j + 1) % kStages;
+        if (x.first && !(ok = warp_wait(clean + 8 * (x.j % kCleans), (x.j / kCleans) & 1, abort, count))) break;
+        const uint64_t vs = desc_mn_major(ring + stage * kTile, kBlock);
+        const uint32_t to = tmem + kOutCol + x.t * DP, from = tmem + kPCol + x.t * (kKeys / 2);
 #pragma unroll
-          for (int half = 0; half < 2; ++half) {  // the first half of the keys while the second's weights are formed
-            if (!(ok = warp_wait(p_ready + 16 * t + 8 * half, round & 1, abort, count))) break;
-            tmem_fence_after();
-            if (elect_one()) {
+        for (int half = 0; half < 2; ++half) {  // the first half of the keys while the second's weights are formed
+          if (!(ok = warp_wait(p_ready + 16 * x.t + 8 * half, x.j & 1, abort, count))) break;
+          tmem_fence_after();
+          if (elect_one()) {
 #pragma unroll
-              for (int k = 0; k < kKeys / 32; ++k)
-                mma_ts(to, from + (half * (kKeys / 32) + k) * 8, vs + (half * (kKeys / 32) + k) * 128, mma_shape(kRows, DP, true), round > 0 || half > 0 || k > 0);
-              if (half == 1) {
-                mma_commit(pv_done + 8 * t);
-                if (last) mma_commit(empty + 8 * stage);
-              }
+            for (int k = 0; k < kKeys / 32; ++k)
+              mma_ts(to, from + (half * (kKeys / 32) + k) * 8, vs + (half * (kKeys / 32) + k) * 128, mma_shape(kRows, DP, true), x.j > 0 || half > 0 || k > 0);
+            if (half == 1) {
+              mma_commit(pv_done + 8 * x.t);
+              if (x.last) mma_commit(empty + 8 * stage);
             }
-            __syncwarp();
           }
+          __syncwarp();
         }
       }
     } else {
@@ -454,17 +465,22 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
         if (part) {
           uint4* v = reinterpret_cast<uint4*>(base + 1024 + (TQ + s) * kTile);
           const int k0 = job.tile(j) * kKeys;
-          for (int x = threadIdx.x - kCleanWarp0 * 32; x < kTile / 16; x += kCleanWarps * 32) {
-            uint4 u = v[x];
-            uint32_t w[4] = {u.x, u.y, u.z, u.w};
-            bool bad = false;
+#pragma unroll 1
+          for (int x0 = lane; x0 < kTile / 16; x0 += 32 * 8) {
+            uint4 u[8];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              if ((w[e] & 0x7f80u) == 0x7f80u) w[e] &= 0xffff0000u, bad = true;
-              if ((w[e] & 0x7f800000u) == 0x7f800000u) w[e] &= 0xffffu, bad = true;
-            }
-            if (bad) {
-              v[x] = make_uint4(w[0], w[1], w[2], w[3]);
+            for (int e = 0; e < 8; ++e) u[e] = v[x0 + 32 * e];
+            uint32_t any = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) any |= bad_elements(u[e].x) | bad_elements(u[e].y) | bad_elements(u[e].z) | bad_elements(u[e].w);
+            if (any == 0) continue;
+#pragma unroll 1
+            for (int x = x0; x < x0 + 32 * 8; x += 32) {
+              uint4 w = v[x];
+              const uint32_t b0 = bad_elements(w.x), b1 = bad_elements(w.y), b2 = bad_elements(w.z), b3 = bad_elements(w.w);
+              if ((b0 | b1 | b2 | b3) == 0) continue;
+              w.x &= ~b0, w.y &= ~b1, w.z &= ~b2, w.w &= ~b3;
+              v[x] = w;
               const int at = k0 + (x / 8) % kKeys;
               if (at <= job.p1 && (at >= job.lo || at < job.sinks)) *poison = 1;  // (a row of this CTA may see it)
             }
@@ -479,7 +495,7 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
   __syncwarp();
   __syncthreads();
   drain_if_aborted(abort);
-  if (warp == kMmaWarp) {
+  if (warp == kScoreWarp) {
     tmem_fence_after();
     tmem_free(tmem, kTmemCols);
   }
