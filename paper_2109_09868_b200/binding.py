@@ -88,9 +88,9 @@ def load() -> ctypes.CDLL:
     have_nvcc = shutil.which("nvcc") is not None or os.path.exists("/usr/local/cuda/bin/nvcc")
     if have_nvcc and _build.is_stale():
         _build.build()
-    if not os.path.exists(_build.LIB):
+    if not os.path.exists(_build.LIB) or not os.path.exists(_build.BINDING):
         raise RuntimeError(
-            "libapproxifer.so is missing and cannot be built (no nvcc): run `python -m paper_2109_09868_b200.build`"
+            "libapproxifer.so or _hosted.so is missing and cannot be built (no nvcc): run `python -m paper_2109_09868_b200.build`"
         )
     lib = ctypes.CDLL(_build.LIB)
     pf, pu, pi = POINTER(c_float), POINTER(c_uint32), POINTER(c_int32)
@@ -152,10 +152,10 @@ def load() -> ctypes.CDLL:
     lib.approxifer_locate_host.restype = c_int
     lib.approxifer_encode_host_static.argtypes = [pp, c_int64, c_int64, c_void_p, c_void_p, c_void_p]
     lib.approxifer_encode_host_static.restype = c_int
-    for name in ("approxifer_linear", "approxifer_qk_norm_rope", "approxifer_attention"):  # (packed struct, stream)
-        getattr(lib, name).argtypes = [c_char_p, c_void_p]
+    for name in ("approxifer_linear", "approxifer_qk_norm_rope", "approxifer_attention"):  # (args struct, stream); see hosted.py
+        getattr(lib, name).argtypes = [c_void_p, c_void_p]
         getattr(lib, name).restype = c_int
-    lib.approxifer_attention_workspace.argtypes = [c_char_p]
+    lib.approxifer_attention_workspace.argtypes = [c_void_p]
     lib.approxifer_attention_workspace.restype = c_int64
     del pf, pu, pi
     _lib = lib

@@ -19,6 +19,7 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 OBJDIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libapproxifer.so")
+BINDING = os.path.join(HERE, "_hosted.so")  # the hosted-model operators' Python binding (hosted_binding.cpp)
 
 SOURCES = ["api.cu", "tables.cpp", "encode.cu", "decode.cu", "decode_small.cu", "decode_pack.cu", "decode_staged.cu", "locate.cu", "locate_rows.cu", "locate_rows_n8.cu", "locate_rows_n16.cu", "locate_rows_n24.cu", "locate_rows_n32.cu", "host_api.cu", "no_alloc.cu", "hosted_api.cu", "tensor_map.cu", "linear.cu", "linear_tile.cu", "linear_pair.cu", "norm_rope.cu", "attention.cu", "attention_token.cu", "attention_tile.cu"]
 ARCH = ["-gencode", "arch=compute_100a,code=sm_100a"]
@@ -52,7 +53,28 @@ def _deps_mtime() -> float:
 
 
 def is_stale() -> bool:
-    return (not os.path.exists(LIB)) or os.path.getmtime(LIB) < _deps_mtime()
+    return any(not os.path.exists(f) or os.path.getmtime(f) < _deps_mtime() for f in (LIB, BINDING))
+
+
+def _build_binding(verbose: bool) -> None:
+    """Compiles hosted_binding.cpp against the installed torch's headers (host code only)."""
+    import sysconfig
+
+    import torch
+
+    root = os.path.join(os.path.dirname(torch.__file__), "include")
+    tmp = BINDING + ".tmp.%d" % os.getpid()
+    cuda = os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(nvcc()))), "include")
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
+           "-isystem", root, "-isystem", os.path.join(root, "torch", "csrc", "api", "include"), "-isystem", sysconfig.get_paths()["include"], "-isystem", cuda,
+           os.path.join(CSRC, "hosted_binding.cpp"), "-o", tmp, "-L", os.path.join(os.path.dirname(root), "lib"),
+           "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]  # (all loaded by then: importing torch comes first)
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError("g++ failed on hosted_binding.cpp:\n%s\n%s" % (r.stdout, r.stderr))
+    os.replace(tmp, BINDING)
 
 
 def _compile(src: str, verbose: bool) -> str:
@@ -75,8 +97,10 @@ def build(force: bool = False, verbose: bool = False) -> str:
         return LIB
     check_toolkit()
     os.makedirs(OBJDIR, exist_ok=True)
-    with concurrent.futures.ThreadPoolExecutor(max_workers=len(SOURCES)) as ex:
+    with concurrent.futures.ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
+        binding = ex.submit(_build_binding, verbose)
         objs = list(ex.map(lambda s: _compile(s, verbose), SOURCES))
+        binding.result()
     tmp = LIB + ".tmp.%d" % os.getpid()
     cmd = [nvcc(), *ARCH, "-shared", "-o", tmp, *objs]
     r = subprocess.run(cmd, capture_output=True, text=True)

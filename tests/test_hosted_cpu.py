@@ -1,15 +1,21 @@
 """What the hosted-model operators refuse, found on the host before anything is launched."""
 import ctypes
+import struct
 
 import pytest
 import torch
 
 import paper_2109_09868_b200 as ap
-from paper_2109_09868_b200 import binding, hosted
+from paper_2109_09868_b200 import binding
+
+# the argument structs of the header, field by field (native alignment)
+LINEAR = struct.Struct("@qqqPqPqPPqPqii")
+NORM_ROPE = struct.Struct("@qiiiiiiPqqPqqPqqPPPqPPqqPqqqPqqqqPifP")
+ATTENTION = struct.Struct("@qiiiiiiiifiPqqPqqqPqqqqPqqPPPqqPq")
 
 
 def linear_rc(M=4, N=8, K=16, X=16, xs=16, W=16, ws=16, bias=0, R=0, rs=0, Y=16, ys=8, act=0, kind=0):
-    return ap.load().approxifer_linear(hosted._LINEAR.pack(M, N, K, X, xs, W, ws, bias, R, rs, Y, ys, act, kind), None)
+    return ap.load().approxifer_linear(LINEAR.pack(M, N, K, X, xs, W, ws, bias, R, rs, Y, ys, act, kind), None)
 
 
 def test_linear_refusals():
@@ -25,7 +31,7 @@ def test_linear_refusals():
 
 def norm_rope_rc(T=3, Hq=4, Hkv=2, D=8, rot=8, inter=0, kind=0, q=16, qs=(32, 8), k=16, ks=(16, 8), v=16, vs=(16, 8), qw=0, kw=0, cs=16, npos=9,
                  pos=16, qo=16, qos=(32, 8), kc=16, kcs=(128, 64, 8), vc=16, vcs=(128, 64, 8), pages=5, slots=16, page=8, eps=1e-6, status=0):
-    return ap.load().approxifer_qk_norm_rope(hosted._NORM_ROPE.pack(
+    return ap.load().approxifer_qk_norm_rope(NORM_ROPE.pack(
         T, Hq, Hkv, D, rot, inter, kind, q, *qs, k, *ks, v, *vs, qw, kw, cs, npos, pos, qo, *qos, kc, *kcs, vc, *vcs, pages, slots, page, eps, status), None)
 
 
@@ -44,7 +50,7 @@ def test_norm_rope_refusals():
 def attention_rc(T=3, batch=1, max_q=3, Hq=4, Hkv=2, D=8, page=8, window=0, sinks=0, scale=1.0, reserved=0, q=16, qs=(32, 8), kc=16, kcs=(128, 64, 8), vc=16,
                  vcs=(128, 64, 8), pages=5, table=16, ts=4, tp=4, start=16, lens=16, out=16, os=(32, 8),
                  ws=0, wb=0):
-    return ap.load().approxifer_attention(hosted._ATTENTION.pack(
+    return ap.load().approxifer_attention(ATTENTION.pack(
         T, batch, max_q, Hq, Hkv, D, page, window, sinks, scale, reserved, q, *qs, kc, *kcs, vc, *vcs, pages, table, ts, tp, start, lens, out, *os, ws, wb), None)
 
 
@@ -62,9 +68,9 @@ def test_attention_refusals():
 
 def test_packed_structs_are_as_long_as_the_header_says():
     # eight bytes a pointer or 64-bit integer, four the others
-    assert hosted._LINEAR.size == 12 * 8 + 2 * 4
-    assert hosted._NORM_ROPE.size == 29 * 8 + 8 * 4
-    assert hosted._ATTENTION.size == 23 * 8 + 10 * 4
+    assert LINEAR.size == 12 * 8 + 2 * 4
+    assert NORM_ROPE.size == 29 * 8 + 8 * 4
+    assert ATTENTION.size == 23 * 8 + 10 * 4
     assert ctypes.sizeof(ctypes.c_void_p) == 8
 
 
