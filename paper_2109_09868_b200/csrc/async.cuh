@@ -11,6 +11,30 @@
 
 namespace approxifer {
 
+// Launches a kernel of these operators: as a cluster of `cluster` CTAs (1: none), and so that its CTAs may start, set up
+// their barriers and tensor memory and wait in wait_for_inputs() while the kernel before it on the stream still drains.
+// (A kernel so launched calls wait_for_inputs() in every thread that goes on to read or write global memory, and in at
+// least one of every CTA: what follows it on the stream may count on its end alone.)
+template <typename... Params, typename... Args>
+cudaError_t launch_kernel(void (*kernel)(Params...), int64_t grid, int block, int smem, int cluster, cudaStream_t stream, Args&&... args) {
+  if (grid > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)grid);
+  cfg.blockDim = dim3(block);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = cluster, attr[1].val.clusterDim.y = 1, attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, Params(args)...);
+  count_launch();
+  return e;
+}
+
 // Tensor map of a bfloat16 array of `rank` dimensions (innermost first; extents and strides in elements, strides[0] = 1
 // implied) read in boxes whose rows are 64 elements = 128 bytes wide, stored with the 128-byte swizzle.  Elements outside
 // the array read as zero.
@@ -19,6 +43,9 @@ cudaError_t make_tensor_map(CUtensorMap* map, const void* base, int rank, const 
 #ifdef __CUDACC__
 
 constexpr uint32_t kWaitLimit = 1u << 21;  // try_wait attempts (each may block for a while) before a wait gives up
+
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_inputs() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 __device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
@@ -100,6 +127,12 @@ __device__ __forceinline__ uint32_t peer_smem(uint32_t addr, uint32_t rank) {
 __device__ __forceinline__ float4 peer_load(uint32_t addr) {
   float4 v;
   asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+
+__device__ __forceinline__ float2 peer_load2(uint32_t addr) {
+  float2 v;
+  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
   return v;
 }
 

@@ -171,6 +171,7 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
   const approxifer_attention_args& a = g.a;
   const int warp = warp_index(), lane = threadIdx.x % 32;
   unsigned int* count = &g_attention_tile_wait_timeouts;
+  let_next_start();
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) bar_init(full + 8 * s, 1), bar_init(empty + 8 * s, 1);
@@ -185,6 +186,7 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
     prefetch_map(&k_map);
     prefetch_map(&v_map);
   }
+  wait_for_inputs();
   Job job;
   if (!find_job<TQ>(g, &job)) return;
   // (copies) the page of this lane's rows of a key tile, looked up a tile ahead
@@ -510,10 +512,7 @@ cudaError_t launch_one(const TileArgs& g, const CUtensorMap& q, const CUtensorMa
   struct Tag {};
   if ((e = ensure_dynamic_smem<Tag>(kernel, dev->ordinal, smem_bytes(DP))) != cudaSuccess) return e;
   const int64_t ctas = (int64_t)g.blocks * g.a.batch * g.a.Hkv;
-  if (ctas > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
-  kernel<<<(unsigned)ctas, threads_of(DP), smem_bytes(DP), stream>>>(q, k, v, g);
-  count_launch();
-  return cudaGetLastError();
+  return launch_kernel(kernel, ctas, threads_of(DP), smem_bytes(DP), 1, stream, q, k, v, g);
 }
 
 int log2_of(int v) {

@@ -24,15 +24,16 @@ constexpr int kCtasPerSm = 2;
 constexpr int kRows = 16;   // query heads per unit
 constexpr int kStages = 3;
 constexpr int kJoinWarps = 8, kJoinAhead = 6;
+constexpr int kMaxSplit = 8;  // CTAs of a cluster
 constexpr unsigned kFull = 0xffffffffu;
 
 constexpr int keys_of(int dp) { return dp <= 64 ? 32 : 16; }                 // keys per chunk
 constexpr int half_bytes(int dp) { return keys_of(dp) * dp * 2; }            // keys, or values, of a chunk
 constexpr int ring_bytes(int dp) { return kStages * 2 * half_bytes(dp); }    // of a warp
 constexpr int smem_bytes(int dp) { return kWarps * ring_bytes(dp); }
-// After the loop of the cluster form the rings hold the results: float o[warp][16][DP], then m[warp][16], l[warp][16].
-static_assert(kWarps * kRows * 128 * 4 + kWarps * kRows * 8 <= smem_bytes(128), "results exceed the rings");
-static_assert(kWarps * kRows * 64 * 4 + kWarps * kRows * 8 <= smem_bytes(64), "results exceed the rings");
+// After the loop of the cluster form the rings hold the results of the warps and of the CTA.
+constexpr int result_bytes(int dp) { return (kWarps + 1) * kRows * (dp * 4 + 8); }
+static_assert(result_bytes(128) <= smem_bytes(128) && result_bytes(64) <= smem_bytes(64), "results exceed the rings");
 
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
@@ -274,12 +275,34 @@ struct Warp {
   }
 };
 
+// N partial results (maximum and sum, two elements) as one.
+struct Joined {
+  float m, l;
+  float2 v;
+};
+template <int N>
+__device__ __forceinline__ Joined join(const float2 (&ml)[N], const float2 (&v)[N]) {
+  Joined j{ml[0].x, 0.f, make_float2(0.f, 0.f)};
+#pragma unroll
+  for (int p = 1; p < N; ++p) j.m = fmaxf(j.m, ml[p].x);
+  const float base = j.m == -CUDART_INF_F ? 0.f : j.m;
+#pragma unroll
+  for (int p = 0; p < N; ++p) {
+    const float k = pow2(ml[p].x - base);
+    j.l = fmaf(k, ml[p].y, j.l);
+    j.v.x = fmaf(k, v[p].x, j.v.x), j.v.y = fmaf(k, v[p].y, j.v.y);
+  }
+  return j;
+}
+
 template <int DP, bool WHOLE>
 __global__ void __launch_bounds__(kThreads, kCtasPerSm) attention_token_cluster_kernel(const __grid_constant__ approxifer_attention_args a, int row_tiles,
                                                                                         int page_shift) {
   extern __shared__ __align__(1024) unsigned char smem[];
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const int S = (int)cluster_size(), rank = (int)cluster_rank();
+  let_next_start();
+  wait_for_inputs();
   int unit = blockIdx.x / S;
   const int rt = unit % row_tiles;
   unit /= row_tiles;
@@ -313,45 +336,48 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) attention_token_cluster_
   }
   copy_wait<0>();
   w.finish();
-  // the warps' results, then every CTA joins its share of the rows' elements over all warps of the cluster, in order
+  // The warps' results meet in the CTA, the CTAs' in the cluster: every CTA takes its share of the rows' elements (pairs of
+  // them), all the loads of one side by side.
   __syncthreads();
-  float* so = reinterpret_cast<float*>(smem);
-  float* sm = so + kWarps * kRows * DP;
-  float* sl = sm + kWarps * kRows;
+  float* so = reinterpret_cast<float*>(smem);                      // [warp][16][DP]
+  float2* sml = reinterpret_cast<float2*>(so + kWarps * kRows * DP);  // [warp][16] m, l
+  float2* cta_o = sml + kWarps * kRows;                            // [16][DP / 2] of this CTA
+  float2* cta_ml = cta_o + kRows * DP / 2;                         // [16]
 #pragma unroll
   for (int d = 0; d < DP / 8; ++d)
 #pragma unroll
     for (int i = 0; i < 4; i += 2)
       *reinterpret_cast<float2*>(so + (warp * kRows + lane / 4 + i * 4) * DP + d * 8 + (lane % 4) * 2) = make_float2(w.o[d][i], w.o[d][i + 1]);
   if (lane % 4 == 0) {
-    sm[warp * kRows + lane / 4] = w.m[0], sm[warp * kRows + lane / 4 + 8] = w.m[1];
-    sl[warp * kRows + lane / 4] = w.l[0], sl[warp * kRows + lane / 4 + 8] = w.l[1];
+    sml[warp * kRows + lane / 4] = make_float2(w.m[0], w.l[0]);
+    sml[warp * kRows + lane / 4 + 8] = make_float2(w.m[1], w.l[1]);
   }
   __syncthreads();
+  const int pairs = a.D / 2, cells = seen.token < 0 ? 0 : rows * pairs;
+  for (int x = threadIdx.x; x < cells; x += kThreads) {
+    const int r = x / pairs, d = x % pairs;
+    float2 ml[kWarps], v[kWarps];
+#pragma unroll
+    for (int p = 0; p < kWarps; ++p) ml[p] = sml[p * kRows + r], v[p] = *reinterpret_cast<const float2*>(so + (p * kRows + r) * DP + 2 * d);
+    const Joined j = join<kWarps>(ml, v);
+    cta_o[r * (DP / 2) + d] = j.v;
+    if (d == 0) cta_ml[r] = make_float2(j.m, j.l);
+  }
   if (S > 1) cluster_sync();
+  else __syncthreads();
   bf16* out = reinterpret_cast<bf16*>(a.out) + (int64_t)seen.token * a.o_tstride + (int64_t)head0 * a.o_hstride;
-  const int pairs = a.D / 2, cells = seen.token < 0 ? 0 : rows * pairs, x0 = cells * rank / S, x1 = cells * (rank + 1) / S;
-  const uint32_t so_addr = smem_addr(so), sm_addr = smem_addr(sm), sl_addr = smem_addr(sl);
-  auto get = [&](uint32_t addr) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
-    return v;
-  };
+  const int x0 = cells * rank / S, x1 = cells * (rank + 1) / S;
   for (int x = x0 + threadIdx.x; x < x1; x += kThreads) {
-    const int r = x / pairs, d = (x % pairs) * 2;
-    float best = -CUDART_INF_F;
-    for (int p = 0; p < S * kWarps; ++p) best = fmaxf(best, get(peer_smem(sm_addr + ((p % kWarps) * kRows + r) * 4, p / kWarps)));
-    if (best == -CUDART_INF_F) best = 0.f;
-    float total = 0.f, y0 = 0.f, y1 = 0.f;
-    for (int p = 0; p < S * kWarps; ++p) {
-      const int at = (p % kWarps) * kRows + r;
-      const float k = pow2(get(peer_smem(sm_addr + at * 4, p / kWarps)) - best);
-      total = fmaf(k, get(peer_smem(sl_addr + at * 4, p / kWarps)), total);
-      y0 = fmaf(k, get(peer_smem(so_addr + (at * DP + d) * 4, p / kWarps)), y0);
-      y1 = fmaf(k, get(peer_smem(so_addr + (at * DP + d + 1) * 4, p / kWarps)), y1);
+    const int r = x / pairs, d = x % pairs;
+    float2 ml[kMaxSplit], v[kMaxSplit];
+#pragma unroll
+    for (int p = 0; p < kMaxSplit; ++p) {
+      ml[p] = make_float2(-CUDART_INF_F, 0.f), v[p] = make_float2(0.f, 0.f);
+      if (p < S) ml[p] = peer_load2(peer_smem(smem_addr(cta_ml + r), p)), v[p] = peer_load2(peer_smem(smem_addr(cta_o + r * (DP / 2) + d), p));
     }
-    const float inv = total == 0.f ? 0.f : 1.f / total;
-    *reinterpret_cast<uint32_t*>(out + (int64_t)r * a.o_hstride + d) = total == 0.f ? 0u : pack_bf16x2(y0 * inv, y1 * inv);
+    const Joined j = join<kMaxSplit>(ml, v);
+    const float inv = j.l == 0.f ? 0.f : 1.f / j.l;
+    *reinterpret_cast<uint32_t*>(out + (int64_t)r * a.o_hstride + 2 * d) = j.l == 0.f ? 0u : pack_bf16x2(j.v.x * inv, j.v.y * inv);
   }
   if (S > 1) cluster_sync();  // (a CTA's shared memory stays until all have read it)
 }
@@ -417,7 +443,8 @@ __global__ void __launch_bounds__(kThreads, 3) attention_token_balanced_kernel(c
   extern __shared__ __align__(1024) unsigned char smem[];
   const int warp = blockIdx.x * kWarps + threadIdx.x / 32, warps = gridDim.x * kWarps, lane = threadIdx.x % 32;
   const int units = a.Hkv * row_tiles, group = a.Hq / a.Hkv;
-  asm volatile("griddepcontrol.launch_dependents;");
+  wait_for_inputs();
+  let_next_start();  // (only now: the kernel that joins counts the chunks, from the call's inputs, before it waits for this one)
   Place at;
   const int64_t total = count_chunks(a, units, keys_of(DP), 0, 0, &at);
   const int runs = total < warps ? (int)total : warps;  // (no empty runs)
@@ -523,13 +550,14 @@ __global__ void __launch_bounds__(JW * 32) attention_token_join_kernel(const __g
   constexpr int kLanes = DP / 4, kTeams = JW * 32 / kLanes;  // lanes to a partial row, partial rows at a time
   __shared__ __align__(16) float sy[kTeams][DP];
   __shared__ float sm[kTeams], sl[kTeams];
+  let_next_start();
   const int team = threadIdx.x / kLanes, at4 = (threadIdx.x % kLanes) * 4;
   const int units = a.Hkv * row_tiles, group = a.Hq / a.Hkv;
   const int b = blockIdx.x / a.Hq, h = blockIdx.x % a.Hq, in_group = h % group;
   Place at;
   const int64_t total = count_chunks(a, units, keys_of(DP), -1, b, &at);
   const Seen seen = seen_by(a, b, keys_of(DP));
-  asm volatile("griddepcontrol.wait;" ::: "memory");  // (before any way out: what follows this launch may count on the first kernel's end)
+  wait_for_inputs();
   if (seen.token < 0) return;
   bf16* out = reinterpret_cast<bf16*>(a.out) + (int64_t)seen.token * a.o_tstride + (int64_t)h * a.o_hstride;
   if (seen.chunks == 0) {
@@ -603,19 +631,7 @@ cudaError_t launch_cluster(const approxifer_attention_args& a, const DeviceInfo&
   struct Tag {};
   cudaError_t e = ensure_dynamic_smem<Tag>(kernel, dev.ordinal, smem_bytes(DP));
   if (e != cudaSuccess) return e;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(units * split));
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = smem_bytes(DP);
-  cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = split, attr[0].val.clusterDim.y = 1, attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  e = cudaLaunchKernelEx(&cfg, kernel, a, row_tiles, page_shift);
-  count_launch();
-  return e;
+  return launch_kernel(kernel, units * split, kThreads, smem_bytes(DP), split, stream, a, row_tiles, page_shift);
 }
 
 template <int DP, bool WHOLE>
@@ -626,24 +642,11 @@ cudaError_t launch_balanced(const approxifer_attention_args& a, const DeviceInfo
   if (e != cudaSuccess) return e;
   const int ctas = dev.sms * kCtasPerSm;
   float* partial = static_cast<float*>(a.workspace);
-  kernel<<<ctas, kThreads, smem_bytes(DP), stream>>>(a, row_tiles, page_shift, partial);
-  count_launch();
-  if ((e = cudaGetLastError()) != cudaSuccess) return e;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)((int64_t)a.batch * a.Hq));
+  if ((e = launch_kernel(kernel, ctas, kThreads, smem_bytes(DP), 1, stream, a, row_tiles, page_shift, partial)) != cudaSuccess) return e;
   // a unit's share of the runs: one warp joins a few partial results, eight many
   const bool few = units_of(a) * 8 >= (int64_t)ctas * kWarps;
-  cfg.blockDim = dim3(few ? 32 : kJoinWarps * 32);
-  cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;  // its launch and its counting overlap the first kernel
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  e = cudaLaunchKernelEx(&cfg, few ? attention_token_join_kernel<DP, 1> : attention_token_join_kernel<DP, kJoinWarps>, a, row_tiles, ctas * kWarps,
-                         (const float*)partial);
-  count_launch();
-  return e;
+  return launch_kernel(few ? attention_token_join_kernel<DP, 1> : attention_token_join_kernel<DP, kJoinWarps>, (int64_t)a.batch * a.Hq,
+                       few ? 32 : kJoinWarps * 32, 0, 1, stream, a, row_tiles, ctas * kWarps, partial);
 }
 
 // The balanced form from 128 MB ... on
@@ -680,8 +683,7 @@ cudaError_t launch_attention_token(const approxifer_attention_args& a, cudaStrea
   // Until there are about four CTAs for every place on the GPU, none with less than two chunks for each warp.
   const int64_t units = units_of(a), most = most_seen(a);
   int split = 1;
-  while (split < 8 && units * split < 4LL * kCtasPerSm * dev->sms && most >= (int64_t)split * 2 * kWarps * keys * 2) split *= 2;
-  if (units * split > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
+  while (split < kMaxSplit && units * split < 4LL * kCtasPerSm * dev->sms && most >= (int64_t)split * 2 * kWarps * keys * 2) split *= 2;
   auto launch = is_whole ? (dp == 64 ? launch_cluster<64, true> : launch_cluster<128, true>) : dp == 64 ? launch_cluster<64, false> : launch_cluster<128, false>;
   return launch(a, *dev, row_tiles, page_shift, units, split, stream);
 }

@@ -91,7 +91,7 @@ __device__ __forceinline__ void finish32(const PairArgs& a, int m, int n, const 
 }
 
 template <typename Out, int ACT>
-__global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
+__global__ void __launch_bounds__(kThreads, 1)
     linear_pair_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map, const __grid_constant__ PairArgs a) {
   extern __shared__ unsigned char raw[];
   unsigned char* base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
@@ -104,6 +104,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
   const int rank = (int)cluster_rank();
   const int pair = blockIdx.x / 2, pairs = gridDim.x / 2;
   unsigned int* count = &g_linear_pair_wait_timeouts;
+  let_next_start();
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) bar_init(full + 8 * s, 1), bar_init(empty + 8 * s, 1);
@@ -119,6 +120,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
   cluster_sync();  // both CTAs' barriers stand before any is signalled from the other
   tmem_fence_after();
   const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
+  wait_for_inputs();
 
   if (warp == 0 && lane == 0) {
     int it = 0;
@@ -200,9 +202,7 @@ cudaError_t launch_act(const PairArgs& t, const CUtensorMap& x, const CUtensorMa
   const cudaError_t e = ensure_dynamic_smem<Tag>(kernel, dev.ordinal, kSmemBytes);
   if (e != cudaSuccess) return e;
   const int pairs = t.tiles < dev.sms / 2 ? t.tiles : dev.sms / 2;
-  kernel<<<2 * pairs, kThreads, kSmemBytes, stream>>>(x, w, t);
-  count_launch();
-  return cudaGetLastError();
+  return launch_kernel(kernel, 2 * pairs, kThreads, kSmemBytes, 2, stream, x, w, t);
 }
 
 template <typename Out>

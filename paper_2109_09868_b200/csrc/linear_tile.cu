@@ -95,6 +95,7 @@ __global__ void __launch_bounds__(kThreads) linear_tile_kernel(const __grid_cons
   unsigned char* stages = base + kHeader;
   const uint32_t full = smem_addr(bars), empty = full + 8 * kStages, done = empty + 8 * kStages;
   const int warp = warp_index(), lane = threadIdx.x % 32;
+  let_next_start();
 
   const int S = (int)cluster_size(), rank = (int)cluster_rank();
   const int tile = blockIdx.x / S;
@@ -114,6 +115,7 @@ __global__ void __launch_bounds__(kThreads) linear_tile_kernel(const __grid_cons
   __syncthreads();
   tmem_fence_after();
   const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
+  wait_for_inputs();
 
   if (warp == 0 && lane == 0) {
     for (int i = step0; i < step1; ++i) {
@@ -210,19 +212,7 @@ cudaError_t launch_one(const TileArgs& t, const CUtensorMap& rows, const CUtenso
   auto kernel = linear_tile_kernel<BN, SWAP, Out>;
   struct Tag {};
   if ((e = ensure_dynamic_smem<Tag>(kernel, dev->ordinal, smem_bytes(BN))) != cudaSuccess) return e;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(tiles * split));
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = smem_bytes(BN);
-  cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = split, attr[0].val.clusterDim.y = 1, attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  e = cudaLaunchKernelEx(&cfg, kernel, rows, cols, t);
-  count_launch();
-  return e;
+  return launch_kernel(kernel, tiles * split, kThreads, smem_bytes(BN), split, stream, rows, cols, t);
 }
 
 template <int BN, bool SWAP>
