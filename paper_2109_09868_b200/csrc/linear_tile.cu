@@ -9,7 +9,7 @@
 // workspace and no second launch); the partial tiles meet in shared memory, and every CTA sums S of them in rank order
 // over its share of the tile (the same order every time) and applies the epilogue to it.
 //
-//   warp 0     one lane: tensor-map copies, 64 columns of both operands per stage, up to 10 stages in flight
+//   warp 0     one lane: tensor-map copies, 64 columns of both operands per stage, 6 to 10 stages in flight
 //   warp 1     tcgen05.mma; allocates the tensor memory
 //   warps 2-5  accumulator -> shared memory; all warps: sum, epilogue, stores
 #include "async.cuh"
@@ -21,14 +21,13 @@ __device__ unsigned int g_linear_tile_wait_timeouts = 0;
 namespace {
 
 constexpr int kThreads = 192;
-constexpr int kLanes = 128;   // rows of the first operand per tile
+constexpr int kLanes = 128;   // rows of the first operand per tile ...
+constexpr int kMinLanes = 96; // ... and the fewest worth having (with less a copy is too short to keep HBM busy)
 constexpr int kDepth = 64;    // columns of both operands per stage: one 128-byte swizzle row
 constexpr int kHeader = 1024; // mbarriers, flags; keeps the stages 1,024-byte aligned
-constexpr int kMaxStages = 10;
-constexpr int kStageBudget = 196 * 1024;
 
 constexpr int stage_bytes(int bn) { return (kLanes + bn) * kDepth * 2; }
-constexpr int stages_of(int bn) { return kStageBudget / stage_bytes(bn) < kMaxStages ? kStageBudget / stage_bytes(bn) : kMaxStages; }
+constexpr int stages_of(int bn) { return 196 * 1024 / stage_bytes(bn); }
 constexpr int smem_bytes(int bn) { return kHeader + 1024 + stages_of(bn) * stage_bytes(bn); }
 constexpr int tmem_cols(int bn) { return bn < 32 ? 32 : bn; }
 
@@ -36,6 +35,7 @@ struct TileArgs {
   int32_t M, N, K;
   int32_t steps;  // stages of K in all
   int32_t tiles_cols;
+  int32_t lanes;  // rows of the first operand per tile: a multiple of 8, up to 128 (the accumulator's other lanes are not used)
   const bf16* bias;
   const void* R;
   void* Y;
@@ -99,7 +99,7 @@ __global__ void __launch_bounds__(kThreads) linear_tile_kernel(const __grid_cons
 
   const int S = (int)cluster_size(), rank = (int)cluster_rank();
   const int tile = blockIdx.x / S;
-  const int row0 = (tile / a.tiles_cols) * kLanes, col0 = (tile % a.tiles_cols) * BN;
+  const int row0 = (tile / a.tiles_cols) * a.lanes, col0 = (tile % a.tiles_cols) * BN;
   const int step0 = (int)((int64_t)a.steps * rank / S), step1 = (int)((int64_t)a.steps * (rank + 1) / S);
 
   if (threadIdx.x == 0) {
@@ -122,7 +122,7 @@ __global__ void __launch_bounds__(kThreads) linear_tile_kernel(const __grid_cons
       const int s = (i - step0) % kStages, turn = (i - step0) / kStages;
       if (turn > 0 && !bar_wait(empty + 8 * s, (turn - 1) & 1, abort, &g_linear_tile_wait_timeouts)) break;
       const uint32_t dst = smem_addr(stages) + s * stage_bytes(BN);
-      bar_expect(full + 8 * s, stage_bytes(BN));
+      bar_expect(full + 8 * s, (a.lanes + BN) * kDepth * 2);
       tma_2d(dst, &rows_map, i * kDepth, row0, full + 8 * s);
       tma_2d(dst + kLanes * kDepth * 2, &cols_map, i * kDepth, col0, full + 8 * s);
     }
@@ -181,13 +181,12 @@ __global__ void __launch_bounds__(kThreads) linear_tile_kernel(const __grid_cons
   if (S > 1) cluster_sync();
   // This CTA's share of the tile: consecutive groups of four columns.
   const int m0 = SWAP ? col0 : row0, n0 = SWAP ? row0 : col0;
-  constexpr int kRowsOut = SWAP ? BN : kLanes, kColsOut = SWAP ? kLanes : BN;
-  const int rows_here = min(kRowsOut, a.M - m0);
-  const int groups = rows_here * (kColsOut / 4);
+  const int rows_here = min(SWAP ? BN : a.lanes, a.M - m0), quads = (SWAP ? a.lanes : BN) / 4;  // groups of four columns in a row
+  const int groups = rows_here * quads;
   const int g0 = (int)((int64_t)groups * rank / S), g1 = (int)((int64_t)groups * (rank + 1) / S);
   const uint32_t part_addr = smem_addr(part);
   for (int g = g0 + threadIdx.x; g < g1; g += kThreads) {
-    const int m = g / (kColsOut / 4), n = (g % (kColsOut / 4)) * 4;
+    const int m = g / quads, n = (g % quads) * 4;
     if (n0 + n >= a.N) continue;
     const uint32_t at = part_addr + (m * kPitch + n) * 4;
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -252,7 +251,7 @@ cudaError_t launch_linear_tile(const approxifer_linear_args& a, cudaStream_t str
   const int64_t across = swap ? a.M : a.N;
   const int bn = across <= 16 ? 16 : across <= 32 ? 32 : across <= 64 ? 64 : 128;
   const int64_t lanes = swap ? a.N : a.M;
-  const int64_t tiles_rows = (lanes + kLanes - 1) / kLanes, tiles_cols = (across + bn - 1) / bn, tiles = tiles_rows * tiles_cols;
+  const int64_t tiles_cols = (across + bn - 1) / bn;
   TileArgs t{};
   t.M = (int32_t)a.M, t.N = (int32_t)a.N, t.K = (int32_t)a.K;
   t.steps = (int32_t)((a.K + kDepth - 1) / kDepth);
@@ -262,12 +261,26 @@ cudaError_t launch_linear_tile(const approxifer_linear_args& a, cudaStream_t str
   const int size = a.out_type == APPROXIFER_TYPE_F32 ? 4 : 2, quad = 4 * size;
   auto fits = [](const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) % bytes) == 0; };
   t.vec = fits(a.Y, quad) && a.y_rstride % 4 == 0 && (!a.R || (fits(a.R, quad) && a.r_rstride % 4 == 0)) && (!a.bias || fits(a.bias, 8));
-  // As many CTAs to a tile as keep every SM busy, each with four stages of K or more.
-  int split = 1;
-  while (split < 8 && tiles * split * 2 <= dev->sms && t.steps >= split * 2 * 4) split *= 2;
+  // CTAs to a tile (each with four stages of K or more), and rows to a tile: full tiles, or as many fewer as give every SM
+  // one of the same size.  A CTA's time is that of reading its rows over its part of K, plus some eight stages' worth for
+  // its start and its end (with the cluster's meeting, ten); what counts is how many of those follow each other on an SM.
+  int split = 1, per_tile = kLanes;
+  int64_t tiles = 0;
+  double best = 0;
+  for (int s = 1; s <= 8 && (s == 1 || t.steps >= 4 * s); s *= 2) {
+    const int64_t places = (s == 1 ? dev->sms : dev->sms * 7 / 8) / s / tiles_cols;  // tiles along the rows that run at once
+    const int64_t even = places > 0 ? ((lanes + places - 1) / places + 7) / 8 * 8 : kLanes;
+    for (const int64_t rows : {(int64_t)kLanes, even}) {
+      if (rows > kLanes || rows < kMinLanes) continue;
+      const int64_t n = (lanes + rows - 1) / rows * tiles_cols, turns = (n * s + dev->sms - 1) / dev->sms;
+      const double time = turns * ((double)rows / kLanes * ((t.steps + s - 1) / s) + (s == 1 ? 8 : 10));
+      if (tiles == 0 || time < best) best = time, split = s, per_tile = (int)rows, tiles = n;
+    }
+  }
+  t.lanes = per_tile;
   if (tiles * split > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
   CUtensorMap rows, cols;
-  if ((e = operand_map(&rows, swap ? a.Wt : a.X, lanes, a.K, swap ? a.w_rstride : a.x_rstride, kLanes)) != cudaSuccess) return e;
+  if ((e = operand_map(&rows, swap ? a.Wt : a.X, lanes, a.K, swap ? a.w_rstride : a.x_rstride, per_tile)) != cudaSuccess) return e;
   if ((e = operand_map(&cols, swap ? a.X : a.Wt, across, a.K, swap ? a.x_rstride : a.w_rstride, bn)) != cudaSuccess) return e;
   if (swap) {
     switch (bn) {

@@ -1,5 +1,5 @@
 // Per-head norm of queries and keys with the position rotation, keys and values written to the paged cache.
-#include "hosted.cuh"
+#include "async.cuh"
 
 namespace approxifer {
 namespace {
@@ -74,55 +74,66 @@ __global__ void __launch_bounds__(kElementThreads) norm_rope_element_kernel(cons
   }
 }
 
-// The path for whole 16-byte columns: one pass over HBM.  A head's row is spread over L lanes (the power of two that holds
-// its columns), a warp takes 32 / L rows at a time, kAhead of those loaded together and kBatches of these one after the
-// other, all of one token and of one kind (queries, keys or values), so that the cosines, sines and weights are read once
-// for many rows:
-//     y_d = r (x_d A_d + x_p(d) B_d),    A_d = w_d cos,  B_d = -+ w_p(d) sin,   p(d) the other element of d's pair,
-// with r the reciprocal root mean square of the row.  The pair's other element comes from another lane (halves) or from
-// the lane's own column (neighbouring pairs).
+// The path for whole columns: one pass over HBM.  A lane holds eight elements of a row, so that a pair's two elements are in
+// the same lane: four and the four that they are turned with (rot/2 further on, or, of neighbouring pairs, the next four),
+// beyond rot eight that are not turned.  A row is spread over L lanes, a warp takes 32 / L rows at a time and kAhead of
+// those together, all of one token and of one kind (queries, keys or values), so that the cosines, sines and weights are
+// read once for many rows:
+//     y = r (x A + x' B),    A = w cos,  B = -+ w' sin,   x' the other element of the pair and w' its weight,
+// with r the reciprocal root mean square of the row.  All rows' loads are in flight before the first is used.
+//
+// With 400 MB to move this is bound by instruction issue as much as by HBM: hence the pairs within a lane (exchanging them
+// between lanes cost 16 instructions of 78 a row pair) and the packed fp32 arithmetic.
 constexpr int kThreads = 128;
 constexpr int kAhead = 4;
-constexpr int kBatches = 1;
 
+// Four elements: a half of what a lane holds of a row.
 template <typename T>
-struct Column;
+struct Four;
 template <>
-struct Column<bf16> {
-  static constexpr int kElems = 8;
-  static __device__ __forceinline__ void get(const uint4& u, uint64_t (&x)[4]) {
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = pack2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+struct Four<bf16> {
+  using Raw = uint2;
+  static constexpr int kCtas = 8;  // per SM
+  static __device__ __forceinline__ void get(const Raw& u, uint64_t (&x)[2]) {
+    x[0] = pack2(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u));
+    x[1] = pack2(__uint_as_float(u.y << 16), __uint_as_float(u.y & 0xffff0000u));
   }
-  static __device__ __forceinline__ uint4 put(const uint64_t (&x)[4]) {
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float lo, hi;
-      unpack2(x[i], lo, hi);
-      w[i] = pack_bf16x2(lo, hi);
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
+  static __device__ __forceinline__ Raw put(const uint64_t (&x)[2]) {
+    float a, b, c, d;
+    unpack2(x[0], a, b), unpack2(x[1], c, d);
+    return make_uint2(pack_bf16x2(a, b), pack_bf16x2(c, d));
   }
+  static __device__ __forceinline__ Raw none() { return make_uint2(0, 0); }
 };
 template <>
-struct Column<float> {
-  static constexpr int kElems = 4;
-  static __device__ __forceinline__ void get(const uint4& u, uint64_t (&x)[2]) {
+struct Four<float> {
+  using Raw = uint4;
+  static constexpr int kCtas = 6;
+  static __device__ __forceinline__ void get(const Raw& u, uint64_t (&x)[2]) {
     x[0] = pack2(__uint_as_float(u.x), __uint_as_float(u.y)), x[1] = pack2(__uint_as_float(u.z), __uint_as_float(u.w));
   }
-  static __device__ __forceinline__ uint4 put(const uint64_t (&x)[2]) {
+  static __device__ __forceinline__ Raw put(const uint64_t (&x)[2]) {
     float a, b, c, d;
     unpack2(x[0], a, b), unpack2(x[1], c, d);
     return make_uint4(__float_as_uint(a), __float_as_uint(b), __float_as_uint(c), __float_as_uint(d));
   }
+  static __device__ __forceinline__ Raw none() { return make_uint4(0, 0, 0, 0); }
 };
 
+__device__ __forceinline__ uint64_t swapped(uint64_t v) {
+  float a, b;
+  unpack2(v, a, b);
+  return pack2(b, a);
+}
+
 template <typename T, int L>
-__global__ void __launch_bounds__(kThreads, 8) norm_rope_kernel(const __grid_constant__ approxifer_norm_rope_args a, int q_units, int kv_units) {
-  constexpr int E = Column<T>::kElems, kSide = 32 / L;  // elements of a column, rows side by side
+__global__ void __launch_bounds__(kThreads, Four<T>::kCtas) norm_rope_kernel(const __grid_constant__ approxifer_norm_rope_args a, int q_units, int kv_units) {
+  using F = Four<T>;
+  using Raw = typename F::Raw;
+  constexpr int kSide = 32 / L;  // rows side by side
   const int lane = threadIdx.x % 32, at = lane % L, side = lane / L;
+  let_next_start();
+  wait_for_inputs();
   const int units = q_units + (a.k ? kv_units : 0) + (a.v ? kv_units : 0);
   const int64_t u = (int64_t)blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
   if (u >= a.T * units) return;
@@ -131,20 +142,23 @@ __global__ void __launch_bounds__(kThreads, 8) norm_rope_kernel(const __grid_con
   const bool is_q = unit < q_units, is_k = !is_q && a.k && unit < q_units + kv_units;
   const bool head_unit = unit == 0;
   unit -= is_q ? 0 : is_k || !a.k ? q_units : q_units + kv_units;
-  const int heads = is_q ? a.Hq : a.Hkv, h0 = unit * (kSide * kAhead * kBatches) + side;
-  const T* in = is_q ? static_cast<const T*>(a.q) + t * a.q_tstride : is_k ? static_cast<const T*>(a.k) + t * a.k_tstride : static_cast<const T*>(a.v) + t * a.v_tstride;
+  const int heads = (is_q ? a.Hq : a.Hkv) - unit * (kSide * kAhead) - side, h0 = unit * (kSide * kAhead) + side;
+  // where this lane's two fours are
+  const int half = a.rot / 2, turning = a.interleaved ? a.rot / 8 : half / 4;
+  const bool turned = at < turning;
+  const int d1 = a.interleaved ? 8 * at : turned ? 4 * at : a.rot + 8 * (at - turning), d2 = turned && !a.interleaved ? half + d1 : d1 + 4;
+  const bool live = at * 8 < a.D;
+
   const int64_t in_h = is_q ? a.q_hstride : is_k ? a.k_hstride : a.v_hstride;
-  const int d0 = at * E;
-  const bool live = d0 < a.D;
-  uint4 x[kAhead];
-  auto load = [&](int batch) {
+  const T* in = (is_q ? static_cast<const T*>(a.q) + t * a.q_tstride : is_k ? static_cast<const T*>(a.k) + t * a.k_tstride : static_cast<const T*>(a.v) + t * a.v_tstride) +
+                h0 * in_h;
+  Raw x1[kAhead], x2[kAhead];
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      const int h = h0 + (batch * kAhead + i) * kSide;
-      x[i] = live && h < heads ? __ldcs(reinterpret_cast<const uint4*>(in + h * in_h + d0)) : make_uint4(0, 0, 0, 0);
-    }
-  };
-  load(0);
+  for (int i = 0; i < kAhead; ++i, in += kSide * in_h) {
+    const bool there = live && i * kSide < heads;
+    x1[i] = there ? __ldcs(reinterpret_cast<const Raw*>(in + d1)) : F::none();
+    x2[i] = there ? __ldcs(reinterpret_cast<const Raw*>(in + d2)) : F::none();
+  }
   const int32_t pos = a.rot ? __ldg(a.positions + t) : 0;
   const bool placed = a.rot == 0 || (pos >= 0 && pos < a.positions_max);
   const int64_t slot = a.slots ? __ldg(a.slots + t) : -1;
@@ -169,126 +183,93 @@ __global__ void __launch_bounds__(kThreads, 8) norm_rope_kernel(const __grid_con
     out = is_k ? static_cast<T*>(a.k_cache) + page * a.kc_pstride + row * a.kc_rstride : static_cast<T*>(a.v_cache) + page * a.vc_pstride + row * a.vc_rstride;
     out_h = is_k ? a.kc_hstride : a.vc_hstride;
   }
-  if (!is_q && !is_k) {
-    for (int batch = 0; batch < kBatches; ++batch) {
-      if (batch) load(batch);
+  out += h0 * out_h;
+  if ((!is_q && !is_k) || !placed) {  // values as they are; queries without a place (keys have left above) zero
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        const int h = h0 + (batch * kAhead + i) * kSide;
-        if (live && h < heads) *reinterpret_cast<uint4*>(out + h * out_h + d0) = x[i];
+    for (int i = 0; i < kAhead; ++i, out += kSide * out_h)
+      if (live && i * kSide < heads) {
+        *reinterpret_cast<Raw*>(out + d1) = placed ? x1[i] : F::none();
+        *reinterpret_cast<Raw*>(out + d2) = placed ? x2[i] : F::none();
       }
-    }
-    return;
-  }
-  if (!placed) {  // (queries: keys have left above)
-    for (int h = h0; h < min(heads, h0 + kAhead * kBatches * kSide); h += kSide)
-      if (live) *reinterpret_cast<uint4*>(out + h * out_h + d0) = make_uint4(0, 0, 0, 0);
     return;
   }
 
-  // A, B of this lane's elements, and the lane that holds their pairs
+  // A, B of this lane's elements.  (An element that is not turned has no part in a pair, even where that is infinite: such
+  // lanes take the pair as zero below.)
   const T* weight = static_cast<const T*>(is_q ? a.q_weight : a.k_weight);
-  const int half = a.rot / 2;
-  const bool turned = d0 < a.rot, second = d0 >= half;
-  const int partner = (turned && !a.interleaved) ? (second ? d0 - half : d0 + half) : d0;
-  const int from = side * L + partner / E;
-  uint64_t A[E / 2], B[E / 2];
+  uint64_t A1[2], A2[2], B1[2], B2[2];
   {
-    uint64_t w[E / 2], wp[E / 2];
-#pragma unroll
-    for (int e = 0; e < E / 2; ++e) w[e] = wp[e] = pack2(1.f, 1.f);
-    if (weight && live) {
-      Column<T>::get(__ldg(reinterpret_cast<const uint4*>(weight + d0)), w);
-      Column<T>::get(__ldg(reinterpret_cast<const uint4*>(weight + partner)), wp);
-    }
-#pragma unroll
-    for (int e = 0; e < E / 2; ++e) A[e] = w[e], B[e] = 0;
+    A1[0] = A1[1] = A2[0] = A2[1] = pack2(1.f, 1.f);
+    B1[0] = B1[1] = B2[0] = B2[1] = 0;
+    if (weight && live) F::get(__ldg(reinterpret_cast<const Raw*>(weight + d1)), A1), F::get(__ldg(reinterpret_cast<const Raw*>(weight + d2)), A2);
     if (turned) {
-      const float* cs = a.cos_sin + (int64_t)pos * a.rot + (a.interleaved ? d0 / 2 : second ? d0 - half : d0);
+      const float* cs = a.cos_sin + (int64_t)pos * a.rot + 4 * at;
+      const float4 c = __ldg(reinterpret_cast<const float4*>(cs)), s = __ldg(reinterpret_cast<const float4*>(cs + half));
       if (a.interleaved) {
-#pragma unroll
-        for (int e = 0; e < E / 2; ++e) {
-          const float c = __ldg(cs + e), s = __ldg(cs + half + e);
-          float x, y;
-          unpack2(wp[e], x, y);
-          A[e] = mul2(w[e], pack2(c, c)), B[e] = pack2(-y * s, x * s);
-        }
+        auto turn = [](uint64_t& A, uint64_t& B, float c, float s) {
+          B = mul2(swapped(A), pack2(-s, s));
+          A = mul2(A, pack2(c, c));
+        };
+        turn(A1[0], B1[0], c.x, s.x), turn(A1[1], B1[1], c.y, s.y), turn(A2[0], B2[0], c.z, s.z), turn(A2[1], B2[1], c.w, s.w);
       } else {
-        const float sign = second ? 1.f : -1.f;
+        const uint64_t c2[2] = {pack2(c.x, c.y), pack2(c.z, c.w)}, s2[2] = {pack2(s.x, s.y), pack2(s.z, s.w)}, n2[2] = {pack2(-s.x, -s.y), pack2(-s.z, -s.w)};
 #pragma unroll
-        for (int e = 0; e < E / 2; e += 2) {
-          const float4 c = __ldg(reinterpret_cast<const float4*>(cs + 2 * e)), s = __ldg(reinterpret_cast<const float4*>(cs + half + 2 * e));
-          A[e] = mul2(w[e], pack2(c.x, c.y)), A[e + 1] = mul2(w[e + 1], pack2(c.z, c.w));
-          B[e] = mul2(wp[e], pack2(sign * s.x, sign * s.y)), B[e + 1] = mul2(wp[e + 1], pack2(sign * s.z, sign * s.w));
+        for (int e = 0; e < 2; ++e) {
+          B1[e] = mul2(A2[e], n2[e]), B2[e] = mul2(A1[e], s2[e]);
+          A1[e] = mul2(A1[e], c2[e]), A2[e] = mul2(A2[e], c2[e]);
         }
       }
     }
   }
   const float inv_d = 1.f / (float)a.D;
-#pragma unroll 1
-  for (int batch = 0; batch < kBatches; ++batch) {
-    if (batch) load(batch);
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      const int h = h0 + (batch * kAhead + i) * kSide;
-      if (h - side >= heads) break;  // (the whole warp)
-      uint64_t v[E / 2], p[E / 2], sq2 = 0;
-      Column<T>::get(x[i], v);
+  for (int i = 0; i < kAhead; ++i, out += kSide * out_h) {
+    if (i * kSide >= heads + side) break;  // (the whole warp)
+    uint64_t v1[2], v2[2];
+    F::get(x1[i], v1), F::get(x2[i], v2);
+    uint64_t sq2 = fma2(v2[1], v2[1], fma2(v2[0], v2[0], fma2(v1[1], v1[1], mul2(v1[0], v1[0]))));
+    float sq, sq_hi;
+    unpack2(sq2, sq, sq_hi);
+    sq += sq_hi;
 #pragma unroll
-      for (int e = 0; e < E / 2; ++e) sq2 = fma2(v[e], v[e], sq2);
-      float sq, sq_hi;
-      unpack2(sq2, sq, sq_hi);
-      sq += sq_hi;
+    for (int d = L / 2; d > 0; d >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, d);
+    const float r = weight ? rsqrtf(sq * inv_d + a.eps) : 1.f;
+    const uint64_t r2 = pack2(r, r);
+    uint64_t p1[2] = {v2[0], v2[1]}, p2[2] = {v1[0], v1[1]};
+    if (a.interleaved) p1[0] = swapped(v1[0]), p1[1] = swapped(v1[1]), p2[0] = swapped(v2[0]), p2[1] = swapped(v2[1]);
+    if (!turned) p1[0] = p1[1] = p2[0] = p2[1] = 0;
 #pragma unroll
-      for (int d = L / 2; d > 0; d >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, d);
-      const float r = weight ? rsqrtf(sq * inv_d + a.eps) : 1.f;
-      uint4 other = x[i];
-      if (!a.interleaved) {
-        other.x = __shfl_sync(0xffffffffu, other.x, from), other.y = __shfl_sync(0xffffffffu, other.y, from);
-        other.z = __shfl_sync(0xffffffffu, other.z, from), other.w = __shfl_sync(0xffffffffu, other.w, from);
-      }
-      if (!turned) other = make_uint4(0, 0, 0, 0);  // (an element that is not turned has no part in a pair, even where it is infinite)
-      Column<T>::get(other, p);
-      if (a.interleaved) {
-#pragma unroll
-        for (int e = 0; e < E / 2; ++e) {
-          float lo, hi;
-          unpack2(p[e], lo, hi);
-          p[e] = pack2(hi, lo);
-        }
-      }
-      const uint64_t r2 = pack2(r, r);
-#pragma unroll
-      for (int e = 0; e < E / 2; ++e) v[e] = mul2(r2, fma2(v[e], A[e], mul2(p[e], B[e])));
-      if (live && h < heads) *reinterpret_cast<uint4*>(out + h * out_h + d0) = Column<T>::put(v);
+    for (int e = 0; e < 2; ++e) {
+      p1[e] = mul2(r2, fma2(v1[e], A1[e], mul2(p1[e], B1[e])));
+      p2[e] = mul2(r2, fma2(v2[e], A2[e], mul2(p2[e], B2[e])));
+    }
+    if (live && i * kSide < heads) {
+      *reinterpret_cast<Raw*>(out + d1) = F::put(p1);
+      *reinterpret_cast<Raw*>(out + d2) = F::put(p2);
     }
   }
 }
 
 template <typename T>
 bool columns_fit(const approxifer_norm_rope_args& a) {
-  constexpr int E = Column<T>::kElems;
   const int64_t strides = a.q_tstride | a.q_hstride | a.qo_tstride | a.qo_hstride | (a.k ? a.k_tstride | a.k_hstride | a.kc_pstride | a.kc_hstride | a.kc_rstride : 0) |
                           (a.v ? a.v_tstride | a.v_hstride | a.vc_pstride | a.vc_hstride | a.vc_rstride : 0);
-  return a.D % E == 0 && a.D / E <= 32 && (a.interleaved ? a.rot % E == 0 : a.rot % (2 * E) == 0) && strides % E == 0 && aligned16(a.q) && aligned16(a.q_out) &&
-         aligned16(a.k) && aligned16(a.v) && aligned16(a.k_cache) && aligned16(a.v_cache) && aligned16(a.q_weight) && aligned16(a.k_weight) && aligned16(a.cos_sin);
+  return a.D % 8 == 0 && a.rot % 8 == 0 && strides % 4 == 0 && aligned16(a.q) && aligned16(a.q_out) && aligned16(a.k) && aligned16(a.v) && aligned16(a.k_cache) &&
+         aligned16(a.v_cache) && aligned16(a.q_weight) && aligned16(a.k_weight) && aligned16(a.cos_sin);
 }
 
 template <typename T, int L>
 cudaError_t launch_columns(const approxifer_norm_rope_args& a, cudaStream_t stream) {
-  constexpr int kRowsPerUnit = (32 / L) * kAhead * kBatches;
+  constexpr int kRowsPerUnit = (32 / L) * kAhead;
   const int q_units = (a.Hq + kRowsPerUnit - 1) / kRowsPerUnit, kv_units = (a.Hkv + kRowsPerUnit - 1) / kRowsPerUnit;
   const int64_t warps = a.T * (q_units + (a.k ? kv_units : 0) + (a.v ? kv_units : 0)), blocks = (warps + kThreads / 32 - 1) / (kThreads / 32);
-  if (blocks > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
-  norm_rope_kernel<T, L><<<(unsigned)blocks, kThreads, 0, stream>>>(a, q_units, kv_units);
-  count_launch();
-  return cudaGetLastError();
+  return launch_kernel(norm_rope_kernel<T, L>, blocks, kThreads, 0, 1, stream, a, q_units, kv_units);
 }
 
 template <typename T>
 cudaError_t launch_type(const approxifer_norm_rope_args& a, cudaStream_t stream) {
   if (columns_fit<T>(a)) {
-    const int columns = a.D / Column<T>::kElems;
+    const int columns = a.D / 8;
     if (columns <= 8) return launch_columns<T, 8>(a, stream);
     if (columns <= 16) return launch_columns<T, 16>(a, stream);
     return launch_columns<T, 32>(a, stream);
