@@ -5,18 +5,21 @@
 // any of its rows sees (the sinks' tiles, then the window's), one pass with the running maximum and sum:
 //
 //   S = Q K^T       128 x 128 fp32 in tensor memory (tcgen05, both operands in shared memory)
-//   P = 2^(S' - m)  a thread owns a row and holds it in registers: no shuffles; P (bfloat16) goes to tensor memory
+//   P = 2^(S' - m)  two threads share a row, 64 scores each in registers; P (bfloat16) goes to tensor memory
 //   O += P V        P from tensor memory, V from shared memory as it lies in the cache (MN-major); O fp32 in tensor memory
 //
-// What a tile's rows wait for is the chain S -> softmax -> P, not any one unit, so S is free again as soon as it has been
-// loaded into registers, and the next S is formed while the softmax works on the last one.  With P beside S that leaves
-// tensor memory for one S, which the two tiles of a CTA (D > 64) take in turn.  The maximum in use is raised, and O
-// rescaled, only when a row's grows by more than 2^8 (P and O then still fit their types with room to spare; the final
-// division by the sum makes up for it), which after the first tiles is hardly ever.
+// What a tile's rows wait for is the chain S -> softmax -> P -> O, not any one unit.  Up to D = 64 tensor memory holds S, P
+// and O of a tile side by side for two CTAs on an SM: S is free again as soon as it has been loaded into registers, and the
+// next one is formed while the softmax works on the last.  Beyond, P lies over S, and the two tiles of a CTA take turns: the
+// tensor cores work for one while the other's softmax runs.  The maximum in use is raised, and O rescaled, only when a row's
+// grows by more than 2^8 (P and O then still fit their types with room to spare; the final division by the sum makes up
+// for it), which after the first tiles is hardly ever.
 //
-//   4 warps a tile   softmax and output
-//   1 warp           tcgen05.mma for S; allocates the tensor memory
-//   1 warp           tcgen05.mma for O (one warp for both has too much to do between two products)
+//   8 warps a tile   softmax and output: four for the first 64 keys and columns, four for the others.  Two threads to a row
+//                    halve the chain and double the warps that hide it; they need agree on the maximum only when one of
+//                    them wants it raised (a vote of the two warps that share rows; the value only then)
+//   1 warp           tcgen05.mma for S of one tile; allocates the tensor memory
+//   1 warp           tcgen05.mma for O, of two tiles also for S
 //   1 warp           tensor-map copies: keys and values by pages, a lane to a page; pages that are not there read as zeros
 //   1 warp           looks through the values of tiles that some rows see only in part: a weight of zero must meet no
 //                    infinity or NaN, so such elements are taken out, and where a row does see them the output adds them back
@@ -38,12 +41,13 @@ constexpr int tile_bytes(int dp) { return kBlock * (dp / 64); }
 // Query tiles per CTA and CTAs per SM.  Up to D = 64 a CTA has one tile and two CTAs share an SM: each fills the gaps of the
 // other, its start and end included.  Beyond, shared memory holds one CTA, and its two tiles share the keys and values.
 constexpr int tiles_of(int dp) { return dp == 64 ? 1 : 2; }
-constexpr int threads_of(int dp) { return (4 * tiles_of(dp) + kOtherWarps) * 32; }
+constexpr int threads_of(int dp) { return (8 * tiles_of(dp) + kOtherWarps) * 32; }
 constexpr int kStages = 5;
 // Rings of one entry per tile of keys.  The copies go in order through kStages places, so that the values of tile j + 4, or
 // the keys of tile j + 8, are asked for only after those of tile j have been used and given back.
 constexpr int kCleans = 4, kMasks = 8;
-constexpr int smem_bytes(int dp) { return 1024 + 1024 + (tiles_of(dp) + kStages) * tile_bytes(dp); }
+// alignment, barriers and flags, what the threads of a row exchange, queries, ring
+constexpr int smem_bytes(int dp) { return 1024 + 1024 + tiles_of(dp) * kRows * 4 + (tiles_of(dp) + kStages) * tile_bytes(dp); }
 
 struct TileArgs {
   approxifer_attention_args a;
@@ -78,6 +82,12 @@ struct Job {
   __device__ __forceinline__ bool full(int t, int j) const {
     const int k0 = tile(j) * kKeys, k1 = k0 + kKeys - 1;
     return k1 <= first_pos(t) && (window == 0 || k0 > last_pos(t) - window || k1 < sinks);
+  }
+  // steps from `from` up to `to` are full for query tile t (tiles that hold sinks are left to the masked way)
+  __device__ __forceinline__ void full_steps(int t, int* from, int* to) const {
+    const int past = last_pos(t) - window, k0 = window && past >= 0 ? past / kKeys + 1 : 0, k1 = first_pos(t) < 0 ? 0 : (first_pos(t) + 1) / kKeys;
+    *from = sink_tiles + max(0, k0 - first_tile);
+    *to = sink_tiles + k1 - first_tile;
   }
   __device__ __forceinline__ bool part(int j, int tiles) const {  // some row of a tile that is worked on does not see all of it
     return (j < steps0 && !full(0, j)) || (tiles == 2 && j < steps1 && !full(1, j));
@@ -138,6 +148,29 @@ __device__ __forceinline__ uint32_t bad_elements(uint32_t w) {
   return ((e >> 15) & 0x00010001u) * 0xffffu;
 }
 
+// S of a query tile and a key tile, both K-major in blocks of 64 columns.
+template <int DP>
+__device__ __forceinline__ void form_scores(uint32_t to, uint64_t q, uint64_t k) {
+  constexpr int kBlock16 = kBlock >> 4;
+#pragma unroll
+  for (int i = 0; i < DP / 16; ++i) mma_ss(to, q + (i / 4) * kBlock16 + 2 * (i % 4), k + (i / 4) * kBlock16 + 2 * (i % 4), mma_shape(kRows, kKeys), i > 0);
+}
+
+// Two warps meet (named barriers 1 .. 8); the second form says whether any of their threads wants something.
+__device__ __forceinline__ void warps_meet(int id) { asm volatile("barrier.cta.sync.aligned %0, 64;" ::"r"(id) : "memory"); }
+__device__ __forceinline__ bool any_of_both(int id, bool want) {
+  uint32_t any;
+  asm volatile(
+      "{\n.reg .pred p, q;\n"
+      "setp.ne.u32 p, %2, 0;\n"
+      "barrier.cta.red.or.pred.aligned q, %1, 64, p;\n"
+      "selp.u32 %0, 1, 0, q;\n}\n"
+      : "=r"(any)
+      : "r"(id), "r"((uint32_t)want)
+      : "memory");
+  return any != 0;
+}
+
 // The n-th (query tile, key tile) pair; the first or the last of its key tile.  (A query tile takes part from step 0 on.)
 struct Item {
   int t, j;
@@ -156,8 +189,9 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
     attention_tile_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
                           const __grid_constant__ TileArgs g) {
   constexpr int TQ = tiles_of(DP), kTile = tile_bytes(DP);
-  constexpr int kScoreWarp = 4 * TQ, kOutWarp = kScoreWarp + 1, kCopyWarp = kScoreWarp + 2;
-  constexpr uint32_t kPCol = kKeys, kOutCol = kPCol + TQ * (kKeys / 2), kTmemCols = TQ * 256;  // tensor memory: S, P of the tiles, O of the tiles
+  constexpr int kScoreWarp = 8 * TQ, kOutWarp = kScoreWarp + 1, kCopyWarp = kScoreWarp + 2;
+  // tensor memory: one tile S, P, O; two tiles S (with P over its first half) of each, O of each
+  constexpr uint32_t kPCol = TQ == 1 ? kKeys : 0, kPStep = kKeys, kOutCol = TQ == 1 ? kKeys + kKeys / 2 : 2 * kKeys, kTmemCols = TQ * 256;
   extern __shared__ unsigned char raw[];
   unsigned char* base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
   uint64_t* bars = reinterpret_cast<uint64_t*>(base);
@@ -168,6 +202,7 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
   const uint32_t full = smem_addr(bars), empty = full + 8 * kStages, clean = empty + 8 * kStages, q_full = clean + 8 * kCleans, s_ready = q_full + 8,
                  s_free = s_ready + 16, p_ready = s_free + 8, pv_done = p_ready + 32;
   const uint32_t q_at = smem_addr(base + 1024), ring = q_at + TQ * kTile;
+  float* exchange = reinterpret_cast<float*>(base + 1024 + (TQ + kStages) * kTile);  // [tile][row]
   const approxifer_attention_args& a = g.a;
   const int warp = warp_index(), lane = threadIdx.x % 32;
   unsigned int* count = &g_attention_tile_wait_timeouts;
@@ -177,7 +212,7 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
     for (int s = 0; s < kStages; ++s) bar_init(full + 8 * s, 1), bar_init(empty + 8 * s, 1);
     for (int s = 0; s < kCleans; ++s) bar_init(clean + 8 * s, 1);
     bar_init(q_full, 1);
-    bar_init(s_free, 4);
+    bar_init(s_free, 8);
     for (int t = 0; t < TQ; ++t) bar_init(s_ready + 8 * t, 1), bar_init(p_ready + 16 * t, 4), bar_init(p_ready + 16 * t + 8, 4), bar_init(pv_done + 8 * t, 1);
     *abort = 0;
     *poison = 0;
@@ -204,38 +239,56 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
   tmem_fence_after();
   const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
 
-  // The softmax warps keep a row of scores in registers; the four others give up theirs (two tiles: 2 x 128 x 200 + 128 x 104
-  // = 384 x 168 registers at the launch; one: 128 x 184 + 128 x 72 = 256 x 128).
+  // The softmax warps keep scores in registers; the four others give up theirs (two tiles: 512 x 104 + 128 x 64 = 640 x 96
+  // registers at the launch; one: 256 x 96 + 128 x 48 = 384 x 80).
   if (warp < kScoreWarp) {
-    if constexpr (TQ == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
-    else asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
-    // ---- softmax and output: one thread, one row ----
-    const int t = warp / 4, r = threadIdx.x % kRows;
-    const uint32_t lanes = (uint32_t)((warp % 4) * 32) << 16;
-    const uint32_t s_at = tmem + lanes, p_at = tmem + lanes + kPCol + t * (kKeys / 2), o_at = tmem + lanes + kOutCol + t * DP;
+    if constexpr (TQ == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
+    else asm volatile("setmaxnreg.inc.sync.aligned.u32 96;");
+    // ---- softmax and output: two threads to a row ----
+    constexpr int kMine = kKeys / 2;  // keys, and kOut columns of the output, of a thread
+    constexpr int kOut = DP / 2;
+    const int t = warp / 8, half = warp / 4 % 2, quarter = warp % 4, r = quarter * 32 + lane;
+    const int meet = 1 + t * 4 + quarter;  // the barrier of the two warps that share these rows
+    const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+    const uint32_t s_at = tmem + lanes + t * kKeys + half * kMine, p_at = tmem + lanes + kPCol + t * kPStep + half * (kMine / 2), o_at = tmem + lanes + kOutCol + t * DP + half * kOut;
+    float* row_value = exchange + t * kRows + r;
+    // the largest (or the sum) of what the row's two threads hold; both warps together
+    auto of_both = [&](float v, auto combine) {
+      if (half == 1) *row_value = v;
+      warps_meet(meet);
+      if (half == 0) *row_value = v = combine(v, *row_value);
+      warps_meet(meet);
+      if (half == 1) v = *row_value;
+      return v;
+    };
     const int in_tile = r / g.group, token = t * job.tokens + in_tile;
     const bool mine = in_tile < job.tokens && token < job.left;
     const int pos = job.pos0 + token;
     const bool flip = a.scale < 0.f;  // the running maximum is that of sign(scale) S
     // (of a zero scale just enough is left to keep what a row does not see at minus infinity)
     const float scale = fmaxf(fabsf(a.scale) * 1.4426950408889634f, 1e-37f);
-    float m = -CUDART_INF_F, l = 0.f;
-    int round = 0;
+    const uint64_t sc2 = pack2(scale, scale);
+    const uint32_t all_pages = (1u << max(1, kKeys >> g.page_shift)) - 1u;
+    int full_from, full_to;  // the steps in which every row of the tile sees every key
+    job.full_steps(t, &full_from, &full_to);
+    if (flip) full_to = 0;
+    const int steps = job.steps_of(t);
+    float m = mine ? -CUDART_INF_F : 0.f, l = 0.f;  // (rows that are not there never ask for another maximum)
     bool ok = true;
-    for (int j = 0; j < job.steps_of(t); ++j) {
-      if (!(ok = warp_wait(s_ready + 8 * t, round & 1, abort, count))) break;
-      ++round;
+    for (int j = 0; j < steps; ++j) {
+      if (!(ok = warp_wait(s_ready + 8 * t, j & 1, abort, count))) break;
       tmem_fence_after();
       const uint32_t there = pages_there[j % kMasks];
-      if (flip || !job.full(t, j) || there != (1u << max(1, kKeys >> g.page_shift)) - 1u) {
+      if (j < full_from || j >= full_to || there != all_pages) {
         // what a row does not see becomes minus infinity, in place and in a short loop: few tiles come here, and the code that
         // all tiles run stays small
         const uint32_t sign = flip ? 0x80000000u : 0u;
 #pragma unroll 1
-        for (int c = 0; c < kKeys; c += 32) {
+        for (int c = 0; c < kMine; c += 32) {
           uint32_t v[32];
           tmem_ld32(s_at + c, v);
-          const uint32_t sees = job.sees(pos, job.tile(j) * kKeys + c) & pages_of(there, c, g.page_shift);
+          const int k = half * kMine + c;
+          const uint32_t sees = job.sees(pos, job.tile(j) * kKeys + k) & pages_of(there, k, g.page_shift);
           tmem_wait_ld(v);
 #pragma unroll
           for (int i = 0; i < 32; ++i) v[i] = sees & (1u << i) ? v[i] ^ sign : 0xff800000u;
@@ -243,89 +296,87 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
         }
         tmem_wait_st();
       }
-      float s[kKeys];
-      auto load = [&](int c) { tmem_ld32(s_at + c, *reinterpret_cast<uint32_t(*)[32]>(s + c)); };
-      auto loaded = [&](int c) { tmem_wait_ld(*reinterpret_cast<uint32_t(*)[32]>(s + c)); };
-      float top[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
-      auto maximum = [&](int c) {
-#pragma unroll
-        for (int i = 0; i < 64; i += 8)
-#pragma unroll
-          for (int k = 0; k < 4; ++k) top[k] = max3(top[k], s[c + i + 2 * k], s[c + i + 2 * k + 1]);
-      };
-      load(0), load(32);
-      loaded(0), loaded(32);
-      load(64), load(96);
-      maximum(0);
-      loaded(64), loaded(96);
+      float s[kMine];
+      tmem_ld32(s_at, *reinterpret_cast<uint32_t(*)[32]>(s));
+      tmem_ld32(s_at + 32, *reinterpret_cast<uint32_t(*)[32]>(s + 32));
+      tmem_wait_ld(*reinterpret_cast<uint32_t(*)[32]>(s));
+      tmem_wait_ld(*reinterpret_cast<uint32_t(*)[32]>(s + 32));
       tmem_fence_before();
-      __syncwarp();
-      if (lane == 0) bar_arrive(s_free);
-      maximum(64);
-      top[0] = fmaxf(max3(top[0], top[1], top[2]), top[3]);
-      if (round > 1 && !(ok = warp_wait(pv_done + 8 * t, round & 1, abort, count))) break;  // (the last P has been used, O is whole)
-      tmem_fence_after();
-      bool grow = false;
-      if (m == -CUDART_INF_F) {
-        m = top[0];  // (nothing summed yet but zeros)
-      } else if ((top[0] - m) * scale > kGrowth) {
-        grow = true;
+      if constexpr (TQ == 1) {
+        __syncwarp();
+        if (lane == 0) bar_arrive(s_free);
       }
-      if (__any_sync(0xffffffffu, grow)) {
-        const float keep = grow ? pow2((m - top[0]) * scale) : 1.f;
-        if (grow) m = top[0];
-        l *= keep;
-#pragma unroll 1
-        for (int c = 0; c < DP; c += 16) {
-          uint32_t v[16];
-          tmem_ld16(o_at + c, v);
-          tmem_wait_ld(v);
+      float top[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
 #pragma unroll
-          for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * keep);
-          tmem_st16(o_at + c, v);
+      for (int i = 0; i < kMine; i += 8)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) top[k] = max3(top[k], s[i + 2 * k], s[i + 2 * k + 1]);
+      top[0] = fmaxf(max3(top[0], top[1], top[2]), top[3]);
+      // the last P has been used, O is whole (two tiles: so S says already, which follows them on the tensor cores)
+      if (TQ == 1 && j > 0 && !(ok = warp_wait(pv_done, (j - 1) & 1, abort, count))) break;
+      tmem_fence_after();
+      // (the vote also keeps P from being written before both warps have read the scores that it may lie over)
+      if (any_of_both(meet, mine && (m == -CUDART_INF_F || (top[0] - m) * scale > kGrowth))) {
+        const float most = of_both(top[0], [](float x, float y) { return fmaxf(x, y); });
+        const bool grow = mine && m != -CUDART_INF_F && (most - m) * scale > kGrowth;
+        const float keep = grow ? pow2((m - most) * scale) : 1.f;
+        if (mine && (grow || m == -CUDART_INF_F)) m = most;  // (at minus infinity nothing is summed yet but zeros)
+        l *= keep;
+        if (j > 0 && __any_sync(0xffffffffu, grow)) {
+#pragma unroll 1
+          for (int c = 0; c < kOut; c += 16) {
+            uint32_t v[16];
+            tmem_ld16(o_at + c, v);
+            tmem_wait_ld(v);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * keep);
+            tmem_st16(o_at + c, v);
+          }
+          tmem_wait_st();
+          tmem_fence_before();
         }
+        warps_meet(meet);  // O is whole again before either warp hands over its weights
+        tmem_fence_after();
       }
       const float shift_by = m == -CUDART_INF_F ? 0.f : -m * scale;
-      const uint64_t sc2 = pack2(scale, scale), sh2 = pack2(shift_by, shift_by);
+      const uint64_t sh2 = pack2(shift_by, shift_by);
       uint64_t sum2[2] = {0, 0};
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
+      for (int c = 0; c < kMine; c += 32) {
+        uint32_t p[16];
 #pragma unroll
-        for (int c = half * 64; c < half * 64 + 64; c += 32) {
-          uint32_t p[16];
-#pragma unroll
-          for (int i = 0; i < 32; i += 2) {
-            float x, y;
-            unpack2(fma2(pack2(s[c + i], s[c + i + 1]), sc2, sh2), x, y);
-            x = pow2(x), y = pow2(y);
-            sum2[(i / 2) & 1] = add2(sum2[(i / 2) & 1], pack2(x, y));
-            p[i / 2] = pack_bf16x2(x, y);
-          }
-          tmem_st16(p_at + c / 2, p);
+        for (int i = 0; i < 32; i += 2) {
+          float x, y;
+          unpack2(fma2(pack2(s[c + i], s[c + i + 1]), sc2, sh2), x, y);
+          x = pow2(x), y = pow2(y);
+          sum2[(i / 2) & 1] = add2(sum2[(i / 2) & 1], pack2(x, y));
+          p[i / 2] = pack_bf16x2(x, y);
         }
-        tmem_wait_st();
-        tmem_fence_before();
-        __syncwarp();
-        if (lane == 0) bar_arrive(p_ready + 16 * t + 8 * half);
+        tmem_st16(p_at + c / 2, p);
       }
+      tmem_wait_st();
+      tmem_fence_before();
+      __syncwarp();
+      if (lane == 0) bar_arrive(p_ready + 16 * t + 8 * half);
       float u, v;
       unpack2(add2(sum2[0], sum2[1]), u, v);
       l += u + v;
     }
-    const bool have = round > 0;
-    if (ok && have) {
-      ok = warp_wait(pv_done + 8 * t, (round - 1) & 1, abort, count);
+    if (ok && steps > 0) {
+      l = of_both(l, [](float x, float y) { return x + y; });
+      ok = warp_wait(pv_done + 8 * t, TQ == 1 ? (steps - 1) & 1 : 0, abort, count);
       tmem_fence_after();
     }
     if (ok) {
-      // O / sum, by way of the tile's queries' place in shared memory (a warp keeps to its own rows) into whole rows
+      // O / sum, by way of the tile's queries' place in shared memory (a warp keeps to its own rows and columns) into whole rows
       const float inv = l == 0.f ? 0.f : 1.f / l;
       const bool add_back = *poison != 0;
-      unsigned char* own_rows = base + 1024 + t * kTile + (warp % 4) * 32 * DP * 2;
+      unsigned char* own_rows = base + 1024 + t * kTile + (half * 4 + quarter) * 32 * kOut * 2;
+      constexpr int kCols = kOut / 8;  // 16-byte columns
 #pragma unroll 1
-      for (int c = 0; c < DP; c += 16) {
+      for (int c = 0; c < kOut; c += 16) {
         float y[16];
-        if (have) {
+        if (steps > 0) {
           uint32_t v[16];
           tmem_ld16(o_at + c, v);
           tmem_wait_ld(v);
@@ -337,6 +388,7 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
         }
         if (mine && add_back) {
           // infinities and NaN that were taken out of tiles seen in part, for the rows that do see them
+          const int d0 = half * kOut + c;
 #pragma unroll 1
           for (int j = 0; j < job.steps; ++j) {
             if (!job.part(j, TQ)) continue;
@@ -350,7 +402,7 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
                               (k & ((1 << g.page_shift) - 1)) * a.vc_rstride;
 #pragma unroll
               for (int i = 0; i < 16; ++i) {
-                const float x = c + i < a.D ? widen(v[c + i]) : 0.f;
+                const float x = d0 + i < a.D ? widen(v[d0 + i]) : 0.f;
                 if (!isfinite(x)) y[i] += x;
               }
             }
@@ -358,24 +410,23 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
         }
 #pragma unroll
         for (int i = 0; i < 16; i += 8)
-          *reinterpret_cast<uint4*>(own_rows + lane * DP * 2 + ((((c + i) / 8) ^ (lane & 7)) << 4)) =
+          *reinterpret_cast<uint4*>(own_rows + lane * kOut * 2 + ((((c + i) / 8) ^ (lane & (kCols - 1))) << 4)) =
               make_uint4(pack_bf16x2(y[i], y[i + 1]), pack_bf16x2(y[i + 2], y[i + 3]), pack_bf16x2(y[i + 4], y[i + 5]), pack_bf16x2(y[i + 6], y[i + 7]));
         __syncwarp();
       }
       const int64_t to = mine ? (int64_t)(job.token0 + token) * a.o_tstride + (int64_t)(job.hk * g.group + r % g.group) * a.o_hstride : -1;
-      constexpr int kCols = DP / 8;
 #pragma unroll 4
       for (int x = lane; x < 32 * kCols; x += 32) {
-        const int row = x / kCols, col = x % kCols;
+        const int row = x / kCols, col = x % kCols, d = half * kOut + col * 8;
         const int64_t at = __shfl_sync(0xffffffffu, to, row);
-        if (at >= 0 && col * 8 < a.D)
-          *reinterpret_cast<uint4*>(reinterpret_cast<bf16*>(a.out) + at + col * 8) = *reinterpret_cast<const uint4*>(own_rows + row * DP * 2 + ((col ^ (row & 7)) << 4));
+        if (at >= 0 && d < a.D)
+          *reinterpret_cast<uint4*>(reinterpret_cast<bf16*>(a.out) + at + d) = *reinterpret_cast<const uint4*>(own_rows + row * kOut * 2 + ((col ^ (row & (kCols - 1))) << 4));
       }
     }
     tmem_fence_before();
   } else {
-    if constexpr (TQ == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
-    else asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    if constexpr (TQ == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    else asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
     if (warp == kCopyWarp) {
       // ---- copies ----
       if (lane == 0) {
@@ -408,41 +459,55 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
         }
       }
     } else if (warp == kScoreWarp) {
-      // ---- S ----
-      // Items: (query tile, key tile) pairs in the order of the key tiles, both query tiles of a key tile while both take part,
-      // then those of tile 1.  Every key tile has an item; its keys, and its values, are given back with the last.
-      if (job.steps > 0 && warp_wait(q_full, 0, abort, count)) {
-        const int items = job.steps0 + job.steps1;
-        for (int n = 0; n < items; ++n) {
-          const Item x = item_at<TQ>(job, n);
-          const int i = 2 * x.j, turn = i / kStages, stage = i - turn * kStages;
-          if (x.first && !warp_wait(full + 8 * stage, turn & 1, abort, count)) break;
-          if (n > 0 && !warp_wait(s_free, (n - 1) & 1, abort, count)) break;  // the last S is in registers
+      // ---- S (one tile) ----
+      if (TQ == 1 && job.steps > 0 && warp_wait(q_full, 0, abort, count)) {
+        for (int j = 0; j < job.steps; ++j) {
+          const int i = 2 * j, turn = i / kStages, stage = i - turn * kStages;
+          const uint64_t ks = desc_k_major(ring + stage * kTile);
+          if (!warp_wait(full + 8 * stage, turn & 1, abort, count)) break;
+          if (j > 0 && !warp_wait(s_free, (j - 1) & 1, abort, count)) break;  // the last S is in registers
           tmem_fence_after();
-          const uint64_t qs = desc_k_major(q_at + x.t * kTile), ks = desc_k_major(ring + stage * kTile);
           if (elect_one()) {
-            constexpr int kBlock16 = kBlock >> 4;
-#pragma unroll
-            for (int k = 0; k < DP / 16; ++k)
-              mma_ss(tmem, qs + (k / 4) * kBlock16 + 2 * (k % 4), ks + (k / 4) * kBlock16 + 2 * (k % 4), mma_shape(kRows, kKeys), k > 0);
-            mma_commit(s_ready + 8 * x.t);
-            if (x.last) mma_commit(empty + 8 * stage);
+            form_scores<DP>(tmem, desc_k_major(q_at), ks);
+            mma_commit(s_ready);
+            mma_commit(empty + 8 * stage);
           }
           __syncwarp();
         }
       }
     } else if (warp == kOutWarp) {
-      // ---- O ----
+      // ---- O (one tile); S and O (two) ----
+      // Items: (query tile, key tile) pairs in the order of the key tiles, both query tiles of a key tile while both take part,
+      // then those of tile 1.  Every key tile has an item; its values are given back with the last, its keys with its last S.
       const int items = job.steps0 + job.steps1;
-      bool ok = true;
+      bool ok = items > 0;
+      int keys_in = 1;
+      if (TQ == 2 && ok) {
+        ok = warp_wait(q_full, 0, abort, count) && warp_wait(full, 0, abort, count);
+        if (ok && elect_one()) {
+#pragma unroll
+          for (int t = 0; t < TQ; ++t)
+            if (job.steps_of(t) > 0) {
+              form_scores<DP>(tmem + t * kKeys, desc_k_major(q_at + t * kTile), desc_k_major(ring));
+              mma_commit(s_ready + 8 * t);
+            }
+          mma_commit(empty);
+        }
+        __syncwarp();
+      }
       for (int n = 0; n < items && ok; ++n) {
         const Item x = item_at<TQ>(job, n);
-        const int stage = (2 * x.j + 1) % kStages;
+        const int stage = (2 * x.j + 1) % kStages, next_key = (2 * x.j + 2) % kStages;
+        const bool more = x.j + 1 < job.steps_of(x.t);
         if (x.first && !(ok = warp_wait(clean + 8 * (x.j % kCleans), (x.j / kCleans) & 1, abort, count))) break;
+        if (TQ == 2 && more && keys_in == x.j + 1) {
+          if (!(ok = warp_wait(full + 8 * next_key, ((2 * x.j + 2) / kStages) & 1, abort, count))) break;
+          ++keys_in;
+        }
         const uint64_t vs = desc_mn_major(ring + stage * kTile, kBlock);
-        const uint32_t to = tmem + kOutCol + x.t * DP, from = tmem + kPCol + x.t * (kKeys / 2);
+        const uint32_t to = tmem + kOutCol + x.t * DP, from = tmem + kPCol + x.t * kPStep;
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {  // the first half of the keys while the second's weights are formed
+        for (int half = 0; half < 2; ++half) {
           if (!(ok = warp_wait(p_ready + 16 * x.t + 8 * half, x.j & 1, abort, count))) break;
           tmem_fence_after();
           if (elect_one()) {
@@ -450,8 +515,13 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
             for (int k = 0; k < kKeys / 32; ++k)
               mma_ts(to, from + (half * (kKeys / 32) + k) * 8, vs + (half * (kKeys / 32) + k) * 128, mma_shape(kRows, DP, true), x.j > 0 || half > 0 || k > 0);
             if (half == 1) {
-              mma_commit(pv_done + 8 * x.t);
+              if (TQ == 1 || !more) mma_commit(pv_done + 8 * x.t);
               if (x.last) mma_commit(empty + 8 * stage);
+              if (TQ == 2 && more) {  // over the P that has just been used
+                form_scores<DP>(tmem + x.t * kKeys, desc_k_major(q_at + x.t * kTile), desc_k_major(ring + next_key * kTile));
+                mma_commit(s_ready + 8 * x.t);
+                if (x.t == 1 || x.j + 1 >= job.steps1) mma_commit(empty + 8 * next_key);
+              }
             }
           }
           __syncwarp();
@@ -468,16 +538,16 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
           uint4* v = reinterpret_cast<uint4*>(base + 1024 + (TQ + s) * kTile);
           const int k0 = job.tile(j) * kKeys;
 #pragma unroll 1
-          for (int x0 = lane; x0 < kTile / 16; x0 += 32 * 8) {
-            uint4 u[8];
+          for (int x0 = lane; x0 < kTile / 16; x0 += 32 * 4) {
+            uint4 u[4];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) u[e] = v[x0 + 32 * e];
+            for (int e = 0; e < 4; ++e) u[e] = v[x0 + 32 * e];
             uint32_t any = 0;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) any |= bad_elements(u[e].x) | bad_elements(u[e].y) | bad_elements(u[e].z) | bad_elements(u[e].w);
+            for (int e = 0; e < 4; ++e) any |= bad_elements(u[e].x) | bad_elements(u[e].y) | bad_elements(u[e].z) | bad_elements(u[e].w);
             if (any == 0) continue;
 #pragma unroll 1
-            for (int x = x0; x < x0 + 32 * 8; x += 32) {
+            for (int x = x0; x < x0 + 32 * 4; x += 32) {
               uint4 w = v[x];
               const uint32_t b0 = bad_elements(w.x), b1 = bad_elements(w.y), b2 = bad_elements(w.z), b3 = bad_elements(w.w);
               if ((b0 | b1 | b2 | b3) == 0) continue;
