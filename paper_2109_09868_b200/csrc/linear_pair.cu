@@ -3,11 +3,13 @@
 // memory, the two tensor cores read both halves), accumulators double-buffered in tensor memory, so that the epilogue of a
 // tile runs under the products of the next.
 //
-//   warp 0      one lane: tensor-map copies of this CTA's operands, six stages of 64 columns (32 KB) in flight
+//   warp 0      one lane: tensor-map copies of this CTA's operands, five stages of 64 columns (32 KB) in flight
 //   warp 1      of the pair's first CTA: tcgen05.mma for the pair; allocates the tensor memory
 //   warps 2, 3  idle (the accumulator's lanes belong to warps by their index modulo 4)
 //   warps 4-11  epilogue: two warps to each quarter of the lanes, half of the columns each; bias, activation, residual,
-//               one rounding, 16-byte stores (a thread owns 64 bytes or more of one row at a time)
+//               one rounding.  A thread has one row of the accumulator; through 4 KB of shared memory a warp turns 32 of
+//               its columns so that eight lanes write, or read of the residual, a row's piece together (a store of 32
+//               rows takes 32 passes; with short K the epilogue is all that is seen)
 #include "async.cuh"
 
 namespace approxifer {
@@ -19,11 +21,12 @@ namespace {
 constexpr int kThreads = 384;
 constexpr int kEpilogueWarps = 8;
 constexpr int kTileM = 256, kTileN = 256, kDepth = 64;
-constexpr int kStages = 6;
+constexpr int kStages = 5;
+constexpr int kTurnBytes = 32 * 32 * 4;           // of an epilogue warp
 constexpr int kHalfBytes = 128 * kDepth * 2;      // one operand of one CTA per stage
 constexpr int kStageBytes = 2 * kHalfBytes;
 constexpr int kHeader = 1024;
-constexpr int kSmemBytes = kHeader + 1024 + kStages * kStageBytes;
+constexpr int kSmemBytes = kHeader + 1024 + kStages * kStageBytes + kEpilogueWarps * kTurnBytes;
 constexpr int kTmemCols = 512;
 constexpr int kGroupM = 8;  // rows of tiles that are walked together: their X stays in L2 while Wt streams by
 
@@ -33,7 +36,7 @@ struct PairArgs {
   const void* R;
   void* Y;
   int64_t r_rstride, y_rstride;
-  int32_t vec;  // 16-byte accesses to Y, R and the bias
+  int32_t vec;  // Y and R can be accessed four elements at a time
 };
 
 // Tiles in bands of kGroupM rows of tiles, down a band's columns of tiles.
@@ -44,48 +47,51 @@ __device__ __forceinline__ void place(const PairArgs& a, int tile, int* m0, int*
   *n0 = (in / rows) * kTileN;
 }
 
+// Rows m0 .. m0+31 and columns n .. n+31: v is this lane's row of the accumulator.
 template <typename Out, int ACT>
-__device__ __forceinline__ void finish32(const PairArgs& a, int m, int n, const uint32_t (&v)[32]) {
-  if (m >= a.M || n >= a.N) return;
-  Out* y = static_cast<Out*>(a.Y) + (int64_t)m * a.y_rstride + n;
-  const Out* r = a.R ? static_cast<const Out*>(a.R) + (int64_t)m * a.r_rstride + n : nullptr;
-  if (a.vec && n + 32 <= a.N) {
-    constexpr int kPer = 16 / sizeof(Out);  // elements of 16 bytes
+__device__ __forceinline__ void finish32(const PairArgs& a, int m0, int n, const uint32_t (&v)[32], float4* turn, int lane) {
+  __syncwarp();  // the last piece has been read
 #pragma unroll
-    for (int j = 0; j < 32; j += 8) {
-      float z[8];
-      uint4 b = make_uint4(0, 0, 0, 0);
-      if (a.bias) b = __ldg(reinterpret_cast<const uint4*>(a.bias + n + j));
-      const uint32_t bw[4] = {b.x, b.y, b.z, b.w};
+  for (int j = 0; j < 8; ++j)
+    turn[lane * 8 + (j ^ (lane & 7))] =
+        make_float4(__uint_as_float(v[4 * j]), __uint_as_float(v[4 * j + 1]), __uint_as_float(v[4 * j + 2]), __uint_as_float(v[4 * j + 3]));
+  __syncwarp();
+  const int col = n + (lane % 8) * 4;
+  if (col >= a.N) return;
+  const bool vec = a.vec && col + 4 <= a.N;
+  float b[4] = {0.f, 0.f, 0.f, 0.f};
+  if (a.bias) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        z[i] = activate<ACT>(__uint_as_float(v[j + i]) + __uint_as_float(i & 1 ? bw[i / 2] & 0xffff0000u : bw[i / 2] << 16));
-#pragma unroll
-      for (int i = 0; i < 8; i += kPer) {
-        if constexpr (sizeof(Out) == 2) {
-          if (r) {
-            const uint4 q = *reinterpret_cast<const uint4*>(r + j);
-            const uint32_t qw[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-            for (int e = 0; e < 8; ++e) z[e] += __uint_as_float(e & 1 ? qw[e / 2] & 0xffff0000u : qw[e / 2] << 16);
-          }
-          *reinterpret_cast<uint4*>(y + j) = make_uint4(pack_bf16x2(z[0], z[1]), pack_bf16x2(z[2], z[3]), pack_bf16x2(z[4], z[5]), pack_bf16x2(z[6], z[7]));
-        } else {
-          if (r) {
-            const float4 q = *reinterpret_cast<const float4*>(r + j + i);
-            z[i] += q.x, z[i + 1] += q.y, z[i + 2] += q.z, z[i + 3] += q.w;
-          }
-          *reinterpret_cast<float4*>(y + j + i) = make_float4(z[i], z[i + 1], z[i + 2], z[i + 3]);
-        }
-      }
-    }
-    return;
+    for (int i = 0; i < 4; ++i)
+      if (col + i < a.N) b[i] = widen(a.bias[col + i]);
   }
+  const int left = a.M - m0;
 #pragma unroll
-  for (int j = 0; j < 32; ++j) {
-    if (n + j < a.N) {
-      const float z = activate<ACT>(__uint_as_float(v[j]) + (a.bias ? widen(a.bias[n + j]) : 0.f));
-      y[j] = narrow<Out>(r ? z + widen(r[j]) : z);
+  for (int i = 0; i < 8; ++i) {
+    const int row = i * 4 + lane / 8;
+    if (row >= left) break;
+    const float4 x = turn[row * 8 + ((lane % 8) ^ (row & 7))];
+    float z[4] = {activate<ACT>(x.x + b[0]), activate<ACT>(x.y + b[1]), activate<ACT>(x.z + b[2]), activate<ACT>(x.w + b[3])};
+    Out* y = static_cast<Out*>(a.Y) + (int64_t)(m0 + row) * a.y_rstride + col;
+    const Out* r = a.R ? static_cast<const Out*>(a.R) + (int64_t)(m0 + row) * a.r_rstride + col : nullptr;
+    if (vec) {
+      if constexpr (sizeof(Out) == 2) {
+        if (r) {
+          const uint2 q = *reinterpret_cast<const uint2*>(r);
+          z[0] += __uint_as_float(q.x << 16), z[1] += __uint_as_float(q.x & 0xffff0000u), z[2] += __uint_as_float(q.y << 16), z[3] += __uint_as_float(q.y & 0xffff0000u);
+        }
+        *reinterpret_cast<uint2*>(y) = make_uint2(pack_bf16x2(z[0], z[1]), pack_bf16x2(z[2], z[3]));
+      } else {
+        if (r) {
+          const float4 q = *reinterpret_cast<const float4*>(r);
+          z[0] += q.x, z[1] += q.y, z[2] += q.z, z[3] += q.w;
+        }
+        *reinterpret_cast<float4*>(y) = make_float4(z[0], z[1], z[2], z[3]);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (col + e < a.N) y[e] = narrow<Out>(r ? z[e] + widen(r[e]) : z[e]);
     }
   }
 }
@@ -170,7 +176,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       place(a, tile, &m0, &n0);
       if (!warp_wait(ready + 8 * acc, (n / 2) & 1, abort, count)) break;
       tmem_fence_after();
-      const int m = m0 + rank * 128 + q * 32 + lane;
+      float4* turn = reinterpret_cast<float4*>(base + kHeader + kStages * kStageBytes + (warp - 4) * kTurnBytes);
       const uint32_t from = tmem + ((uint32_t)(q * 32) << 16) + acc * kTileN + half * (kTileN / 2);
 #pragma unroll 1
       for (int c = 0; c < kTileN / 2; c += 32) {
@@ -182,7 +188,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           __syncwarp();
           if (lane == 0) bar_arrive_cluster(peer_smem(drained + 8 * acc, 0));
         }
-        finish32<Out, ACT>(a, m, n0 + half * (kTileN / 2) + c, v);
+        finish32<Out, ACT>(a, m0 + rank * 128 + q * 32, n0 + half * (kTileN / 2) + c, v, turn, lane);
       }
     }
   }
@@ -235,8 +241,9 @@ cudaError_t launch_linear_pair(const approxifer_linear_args& a, cudaStream_t str
   if (tm * tn > 0x3fffffffLL || tn > (1 << 27)) return cudaErrorInvalidConfiguration;
   t.tiles_m = (int32_t)tm, t.tiles_n = (int32_t)tn, t.tiles = (int32_t)(tm * tn);
   t.bias = reinterpret_cast<const bf16*>(a.bias), t.R = a.R, t.Y = a.Y, t.r_rstride = a.r_rstride, t.y_rstride = a.y_rstride;
-  const int per = a.out_type == APPROXIFER_TYPE_F32 ? 4 : 8;
-  t.vec = aligned16(a.Y) && a.y_rstride % per == 0 && (!a.R || (aligned16(a.R) && a.r_rstride % per == 0)) && (!a.bias || aligned16(a.bias));
+  const int quad = a.out_type == APPROXIFER_TYPE_F32 ? 16 : 8;
+  auto fits = [&](const void* p) { return reinterpret_cast<uintptr_t>(p) % quad == 0; };
+  t.vec = fits(a.Y) && a.y_rstride % 4 == 0 && (!a.R || (fits(a.R) && a.r_rstride % 4 == 0));
   const uint64_t xe[2] = {(uint64_t)a.K, (uint64_t)a.M}, xs[2] = {1, (uint64_t)a.x_rstride}, we[2] = {(uint64_t)a.K, (uint64_t)a.N}, ws[2] = {1, (uint64_t)a.w_rstride};
   const uint32_t box[2] = {(uint32_t)kDepth, 128};
   CUtensorMap x, w;

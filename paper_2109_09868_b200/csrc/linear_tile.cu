@@ -41,7 +41,7 @@ struct TileArgs {
   void* Y;
   int64_t r_rstride, y_rstride;
   int32_t activation;
-  int32_t vec;  // rows of Y, R and the bias can be accessed four elements at a time
+  int32_t vec, bias_vec;  // rows of Y and R, the bias, can be accessed four elements at a time
 };
 
 template <typename Out>
@@ -56,35 +56,26 @@ __device__ __forceinline__ float4 load4<bf16>(const bf16* p) {
 __device__ __forceinline__ void store4(float* p, float4 v) { *reinterpret_cast<float4*>(p) = v; }
 __device__ __forceinline__ void store4(bf16* p, float4 v) { *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w)); }
 
-// Four consecutive columns n .. n+3 of row m.
+// Four consecutive columns from p on, of which the first `count` are there.
 template <typename Out>
-__device__ __forceinline__ void finish4(const TileArgs& a, int m, int n, float4 v) {
-  Out* y = static_cast<Out*>(a.Y) + (int64_t)m * a.y_rstride + n;
-  const Out* r = a.R ? static_cast<const Out*>(a.R) + (int64_t)m * a.r_rstride + n : nullptr;
-  if (a.vec && n + 4 <= a.N) {
-    if (a.bias) {
-      const float4 b = load4<bf16>(a.bias + n);
-      v.x += b.x, v.y += b.y, v.z += b.z, v.w += b.w;
-    }
-    v.x = activate(a.activation, v.x), v.y = activate(a.activation, v.y), v.z = activate(a.activation, v.z), v.w = activate(a.activation, v.w);
-    if (r) {
-      const float4 q = load4<Out>(r);
-      v.x += q.x, v.y += q.y, v.z += q.z, v.w += q.w;
-    }
-    store4(y, v);
+__device__ __forceinline__ float4 read4(const Out* p, bool vec, int count) {
+  if (vec && count >= 4) return load4<Out>(p);
+  return make_float4(count > 0 ? widen(p[0]) : 0.f, count > 1 ? widen(p[1]) : 0.f, count > 2 ? widen(p[2]) : 0.f, count > 3 ? widen(p[3]) : 0.f);
+}
+template <typename Out>
+__device__ __forceinline__ void write4(Out* p, float4 v, bool vec, int count) {
+  if (vec && count >= 4) {
+    store4(p, v);
     return;
   }
-  const float e[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (n + i >= a.N) break;
-    const float z = activate(a.activation, e[i] + (a.bias ? widen(a.bias[n + i]) : 0.f));
-    y[i] = narrow<Out>(r ? z + widen(r[i]) : z);
-  }
+  if (count > 0) p[0] = narrow<Out>(v.x);
+  if (count > 1) p[1] = narrow<Out>(v.y);
+  if (count > 2) p[2] = narrow<Out>(v.z);
+  if (count > 3) p[3] = narrow<Out>(v.w);
 }
 
 template <int BN, bool SWAP, typename Out>
-__global__ void __launch_bounds__(kThreads) linear_tile_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_constant__ CUtensorMap cols_map,
+__global__ void __launch_bounds__(kThreads, 1) linear_tile_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_constant__ CUtensorMap cols_map,
                                                                const __grid_constant__ TileArgs a) {
   constexpr int kStages = stages_of(BN);
   extern __shared__ unsigned char raw[];
@@ -152,21 +143,24 @@ __global__ void __launch_bounds__(kThreads) linear_tile_kernel(const __grid_cons
     tmem_fence_after();
     const int q = warp % 4, l = q * 32 + lane;
     if (ok) {
-#pragma unroll 1
-      for (int c = 0; c < BN; c += 16) {
-        uint32_t v[16];
-        tmem_ld16(tmem + ((uint32_t)(q * 32) << 16) + c, v);
+      constexpr int kAt = BN < 32 ? 16 : 32;  // columns at a time
+#pragma unroll 2
+      for (int c = 0; c < BN; c += kAt) {
+        uint32_t v[kAt];
+        const uint32_t from = tmem + ((uint32_t)(q * 32) << 16) + c;
+        if constexpr (kAt == 16) tmem_ld16(from, v);
+        else tmem_ld32(from, v);
         tmem_wait_ld(v);
         if (step0 == step1) {  // (more CTAs than stages of K: this one has nothing to add)
 #pragma unroll
-          for (int j = 0; j < 16; ++j) v[j] = 0;
+          for (int j = 0; j < kAt; ++j) v[j] = 0;
         }
         if constexpr (SWAP) {
 #pragma unroll
-          for (int j = 0; j < 16; ++j) part[(c + j) * kPitch + l] = __uint_as_float(v[j]);
+          for (int j = 0; j < kAt; ++j) part[(c + j) * kPitch + l] = __uint_as_float(v[j]);
         } else {
 #pragma unroll
-          for (int j = 0; j < 16; j += 4) *reinterpret_cast<uint4*>(part + l * kPitch + c + j) = make_uint4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+          for (int j = 0; j < kAt; j += 4) *reinterpret_cast<uint4*>(part + l * kPitch + c + j) = make_uint4(v[j], v[j + 1], v[j + 2], v[j + 3]);
         }
       }
     }
@@ -179,26 +173,51 @@ __global__ void __launch_bounds__(kThreads) linear_tile_kernel(const __grid_cons
     tmem_free(tmem, tmem_cols(BN));
   }
   if (S > 1) cluster_sync();
-  // This CTA's share of the tile: consecutive groups of four columns.
+  // This CTA's share of the tile's rows, a warp to a row of up to 128 columns (or several shorter ones), a lane to four
+  // columns, kAhead rows' loads side by side.
   const int m0 = SWAP ? col0 : row0, n0 = SWAP ? row0 : col0;
-  const int rows_here = min(SWAP ? BN : a.lanes, a.M - m0), quads = (SWAP ? a.lanes : BN) / 4;  // groups of four columns in a row
-  const int groups = rows_here * quads;
-  const int g0 = (int)((int64_t)groups * rank / S), g1 = (int)((int64_t)groups * (rank + 1) / S);
-  const uint32_t part_addr = smem_addr(part);
-  for (int g = g0 + threadIdx.x; g < g1; g += kThreads) {
-    const int m = g / quads, n = (g % quads) * 4;
-    if (n0 + n >= a.N) continue;
-    const uint32_t at = part_addr + (m * kPitch + n) * 4;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (S == 1) {
-      v = *reinterpret_cast<const float4*>(part + m * kPitch + n);
-    } else {
-      for (int s = 0; s < S; ++s) {
-        const float4 u = peer_load(peer_smem(at, s));
-        v.x += u.x, v.y += u.y, v.z += u.z, v.w += u.w;
+  const int rows_here = min(SWAP ? BN : a.lanes, a.M - m0);
+  const int m_from = rows_here * rank / S, m_to = rows_here * (rank + 1) / S;
+  constexpr int kQuads = SWAP ? 32 : BN / 4, kSide = 32 / kQuads, kAhead = 4, kWarps = kThreads / 32;
+  const int n = (lane % kQuads) * 4, count = a.N - (n0 + n);
+  if (n < (SWAP ? a.lanes : BN) && count > 0) {
+    const uint32_t part_addr = smem_addr(part) + n * 4;
+    const float4 b = a.bias ? read4<bf16>(a.bias + n0 + n, a.bias_vec, count) : make_float4(0.f, 0.f, 0.f, 0.f);
+    const Out* R = static_cast<const Out*>(a.R) + n0 + n;
+    Out* Y = static_cast<Out*>(a.Y) + n0 + n;
+    for (int m = m_from + warp * kSide + lane / kQuads; m < m_to; m += kWarps * kSide * kAhead) {
+      float4 v[kAhead], r[kAhead];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const int mi = m + i * kWarps * kSide;
+        v[i] = r[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (mi >= m_to) continue;
+        if (S == 1) v[i] = *reinterpret_cast<const float4*>(part + mi * kPitch + n);
+        if (a.R) r[i] = read4<Out>(R + (int64_t)(m0 + mi) * a.r_rstride, a.vec, count);
+      }
+      if (S > 1) {
+#pragma unroll 2
+        for (int s = 0; s < S; ++s) {
+          const uint32_t peer = peer_smem(part_addr, s);
+#pragma unroll
+          for (int i = 0; i < kAhead; ++i) {
+            const int mi = m + i * kWarps * kSide;
+            if (mi >= m_to) continue;
+            const float4 u = peer_load(peer + mi * kPitch * 4);
+            v[i].x += u.x, v[i].y += u.y, v[i].z += u.z, v[i].w += u.w;
+          }
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const int mi = m + i * kWarps * kSide;
+        if (mi >= m_to) continue;
+        float4 z = make_float4(v[i].x + b.x, v[i].y + b.y, v[i].z + b.z, v[i].w + b.w);
+        if (a.activation != APPROXIFER_ACT_NONE)
+          z = make_float4(activate(a.activation, z.x), activate(a.activation, z.y), activate(a.activation, z.z), activate(a.activation, z.w));
+        write4<Out>(Y + (int64_t)(m0 + mi) * a.y_rstride, make_float4(z.x + r[i].x, z.y + r[i].y, z.z + r[i].z, z.w + r[i].w), a.vec, count);
       }
     }
-    finish4<Out>(a, m0 + m, n0 + n, v);
   }
   if (S > 1) cluster_sync();  // (a CTA's shared memory stays until all have read it)
 }
@@ -260,7 +279,8 @@ cudaError_t launch_linear_tile(const approxifer_linear_args& a, cudaStream_t str
   t.activation = a.activation;
   const int size = a.out_type == APPROXIFER_TYPE_F32 ? 4 : 2, quad = 4 * size;
   auto fits = [](const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) % bytes) == 0; };
-  t.vec = fits(a.Y, quad) && a.y_rstride % 4 == 0 && (!a.R || (fits(a.R, quad) && a.r_rstride % 4 == 0)) && (!a.bias || fits(a.bias, 8));
+  t.vec = fits(a.Y, quad) && a.y_rstride % 4 == 0 && (!a.R || (fits(a.R, quad) && a.r_rstride % 4 == 0));
+  t.bias_vec = fits(a.bias, 8);
   // CTAs to a tile (each with four stages of K or more), and rows to a tile: full tiles, or as many fewer as give every SM
   // one of the same size.  A CTA's time is that of reading its rows over its part of K, plus some eight stages' worth for
   // its start and its end (with the cluster's meeting, ten); what counts is how many of those follow each other on an SM.
@@ -268,11 +288,13 @@ cudaError_t launch_linear_tile(const approxifer_linear_args& a, cudaStream_t str
   int64_t tiles = 0;
   double best = 0;
   for (int s = 1; s <= 8 && (s == 1 || t.steps >= 4 * s); s *= 2) {
-    const int64_t places = (s == 1 ? dev->sms : dev->sms * 7 / 8) / s / tiles_cols;  // tiles along the rows that run at once
+    // (a cluster sits within one GPC: of its SMs some are left over, more the larger the cluster)
+    const int usable = s == 1 ? dev->sms : s == 2 ? dev->sms - 4 : s == 4 ? dev->sms * 7 / 8 : dev->sms * 3 / 4;
+    const int64_t places = usable / s / tiles_cols;  // tiles along the rows that run at once
     const int64_t even = places > 0 ? ((lanes + places - 1) / places + 7) / 8 * 8 : kLanes;
     for (const int64_t rows : {(int64_t)kLanes, even}) {
       if (rows > kLanes || rows < kMinLanes) continue;
-      const int64_t n = (lanes + rows - 1) / rows * tiles_cols, turns = (n * s + dev->sms - 1) / dev->sms;
+      const int64_t n = (lanes + rows - 1) / rows * tiles_cols, turns = (n * s + usable - 1) / usable;
       const double time = turns * ((double)rows / kLanes * ((t.steps + s - 1) / s) + (s == 1 ? 8 : 10));
       if (tiles == 0 || time < best) best = time, split = s, per_tile = (int)rows, tiles = n;
     }
