@@ -16,10 +16,9 @@ namespace approxifer {
 // (A kernel so launched calls wait_for_inputs() in every thread that goes on to read or write global memory, and in at
 // least one of every CTA: what follows it on the stream may count on its end alone.)
 template <typename... Params, typename... Args>
-cudaError_t launch_kernel(void (*kernel)(Params...), int64_t grid, int block, int smem, int cluster, cudaStream_t stream, Args&&... args) {
-  if (grid > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
+cudaError_t launch_kernel(void (*kernel)(Params...), dim3 grid, int block, int smem, int cluster, cudaStream_t stream, Args&&... args) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)grid);
+  cfg.gridDim = grid;
   cfg.blockDim = dim3(block);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
@@ -33,6 +32,16 @@ cudaError_t launch_kernel(void (*kernel)(Params...), int64_t grid, int block, in
   const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, Params(args)...);
   count_launch();
   return e;
+}
+
+template <typename... Params, typename... Args>
+cudaError_t launch_kernel(void (*kernel)(Params...), int64_t grid, int block, int smem, int cluster, cudaStream_t stream, Args&&... args) {
+  if (grid > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
+  return launch_kernel(kernel, dim3((unsigned)grid), block, smem, cluster, stream, args...);
+}
+template <typename... Params, typename... Args>
+cudaError_t launch_kernel(void (*kernel)(Params...), int grid, int block, int smem, int cluster, cudaStream_t stream, Args&&... args) {
+  return launch_kernel(kernel, (int64_t)grid, block, smem, cluster, stream, args...);
 }
 
 // Tensor map of a bfloat16 array of `rank` dimensions (innermost first; extents and strides in elements, strides[0] = 1

@@ -83,8 +83,9 @@ __global__ void __launch_bounds__(kElementThreads) norm_rope_element_kernel(cons
 // with r the reciprocal root mean square of the row.  All rows' loads are in flight before the first is used.
 //
 // With 400 MB to move this is bound by instruction issue as much as by HBM: hence the pairs within a lane (exchanging them
-// between lanes cost 16 instructions of 78 a row pair) and the packed fp32 arithmetic.
-constexpr int kThreads = 128;
+// between lanes cost 16 instructions of 78 a row pair), the packed fp32 arithmetic, a token to a CTA (no division to find
+// it), and the two template parameters (INTER: neighbouring pairs; PARTIAL: some elements are not turned).
+constexpr int kMaxWarps = 8;  // units of a token per CTA
 constexpr int kAhead = 4;
 
 // Four elements: a half of what a lane holds of a row.
@@ -93,7 +94,7 @@ struct Four;
 template <>
 struct Four<bf16> {
   using Raw = uint2;
-  static constexpr int kCtas = 8;  // per SM
+  static constexpr int kCtas = 4;  // per SM
   static __device__ __forceinline__ void get(const Raw& u, uint64_t (&x)[2]) {
     x[0] = pack2(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u));
     x[1] = pack2(__uint_as_float(u.y << 16), __uint_as_float(u.y & 0xffff0000u));
@@ -108,7 +109,7 @@ struct Four<bf16> {
 template <>
 struct Four<float> {
   using Raw = uint4;
-  static constexpr int kCtas = 6;
+  static constexpr int kCtas = 3;
   static __device__ __forceinline__ void get(const Raw& u, uint64_t (&x)[2]) {
     x[0] = pack2(__uint_as_float(u.x), __uint_as_float(u.y)), x[1] = pack2(__uint_as_float(u.z), __uint_as_float(u.w));
   }
@@ -126,8 +127,9 @@ __device__ __forceinline__ uint64_t swapped(uint64_t v) {
   return pack2(b, a);
 }
 
-template <typename T, int L>
-__global__ void __launch_bounds__(kThreads, Four<T>::kCtas) norm_rope_kernel(const __grid_constant__ approxifer_norm_rope_args a, int q_units, int kv_units) {
+template <typename T, int L, bool INTER, bool PARTIAL>
+__global__ void __launch_bounds__(kMaxWarps * 32, Four<T>::kCtas) norm_rope_kernel(const __grid_constant__ approxifer_norm_rope_args a, int q_units, int kv_units,
+                                                                                   int page_shift) {
   using F = Four<T>;
   using Raw = typename F::Raw;
   constexpr int kSide = 32 / L;  // rows side by side
@@ -135,18 +137,17 @@ __global__ void __launch_bounds__(kThreads, Four<T>::kCtas) norm_rope_kernel(con
   let_next_start();
   wait_for_inputs();
   const int units = q_units + (a.k ? kv_units : 0) + (a.v ? kv_units : 0);
-  const int64_t u = (int64_t)blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
-  if (u >= a.T * units) return;
-  const int64_t t = a.T < (1 << 24) && units < 128 ? (uint32_t)u / (uint32_t)units : u / units;
-  int unit = (int)(u - t * units);
+  const int64_t t = blockIdx.x;
+  int unit = (int)(blockIdx.y * (blockDim.x / 32) + threadIdx.x / 32);
+  if (unit >= units) return;
   const bool is_q = unit < q_units, is_k = !is_q && a.k && unit < q_units + kv_units;
   const bool head_unit = unit == 0;
   unit -= is_q ? 0 : is_k || !a.k ? q_units : q_units + kv_units;
   const int heads = (is_q ? a.Hq : a.Hkv) - unit * (kSide * kAhead) - side, h0 = unit * (kSide * kAhead) + side;
   // where this lane's two fours are
-  const int half = a.rot / 2, turning = a.interleaved ? a.rot / 8 : half / 4;
-  const bool turned = at < turning;
-  const int d1 = a.interleaved ? 8 * at : turned ? 4 * at : a.rot + 8 * (at - turning), d2 = turned && !a.interleaved ? half + d1 : d1 + 4;
+  const int half = a.rot / 2, turning = a.rot / 8;
+  const bool turned = !PARTIAL || at < turning;
+  const int d1 = INTER ? 8 * at : turned ? 4 * at : a.rot + 8 * (at - turning), d2 = turned && !INTER ? half + d1 : d1 + 4;
   const bool live = at * 8 < a.D;
 
   const int64_t in_h = is_q ? a.q_hstride : is_k ? a.k_hstride : a.v_hstride;
@@ -172,14 +173,7 @@ __global__ void __launch_bounds__(kThreads, Four<T>::kCtas) norm_rope_kernel(con
     out_h = a.qo_hstride;
   } else {
     if (!placed || !fits || slot < 0) return;
-    int64_t page, row;
-    if (slot < (1LL << 31)) {
-      page = (uint32_t)slot / (uint32_t)a.page_size;
-      row = (uint32_t)slot - (uint32_t)page * (uint32_t)a.page_size;
-    } else {
-      page = slot / a.page_size;
-      row = slot % a.page_size;
-    }
+    const int64_t page = page_shift >= 0 ? slot >> page_shift : slot / a.page_size, row = slot - page * a.page_size;
     out = is_k ? static_cast<T*>(a.k_cache) + page * a.kc_pstride + row * a.kc_rstride : static_cast<T*>(a.v_cache) + page * a.vc_pstride + row * a.vc_rstride;
     out_h = is_k ? a.kc_hstride : a.vc_hstride;
   }
@@ -202,10 +196,10 @@ __global__ void __launch_bounds__(kThreads, Four<T>::kCtas) norm_rope_kernel(con
     A1[0] = A1[1] = A2[0] = A2[1] = pack2(1.f, 1.f);
     B1[0] = B1[1] = B2[0] = B2[1] = 0;
     if (weight && live) F::get(__ldg(reinterpret_cast<const Raw*>(weight + d1)), A1), F::get(__ldg(reinterpret_cast<const Raw*>(weight + d2)), A2);
-    if (turned) {
+    if (turned && a.rot > 0 && live) {
       const float* cs = a.cos_sin + (int64_t)pos * a.rot + 4 * at;
       const float4 c = __ldg(reinterpret_cast<const float4*>(cs)), s = __ldg(reinterpret_cast<const float4*>(cs + half));
-      if (a.interleaved) {
+      if constexpr (INTER) {
         auto turn = [](uint64_t& A, uint64_t& B, float c, float s) {
           B = mul2(swapped(A), pack2(-s, s));
           A = mul2(A, pack2(c, c));
@@ -236,8 +230,8 @@ __global__ void __launch_bounds__(kThreads, Four<T>::kCtas) norm_rope_kernel(con
     const float r = weight ? rsqrtf(sq * inv_d + a.eps) : 1.f;
     const uint64_t r2 = pack2(r, r);
     uint64_t p1[2] = {v2[0], v2[1]}, p2[2] = {v1[0], v1[1]};
-    if (a.interleaved) p1[0] = swapped(v1[0]), p1[1] = swapped(v1[1]), p2[0] = swapped(v2[0]), p2[1] = swapped(v2[1]);
-    if (!turned) p1[0] = p1[1] = p2[0] = p2[1] = 0;
+    if constexpr (INTER) p1[0] = swapped(v1[0]), p1[1] = swapped(v1[1]), p2[0] = swapped(v2[0]), p2[1] = swapped(v2[1]);
+    if (PARTIAL && !turned) p1[0] = p1[1] = p2[0] = p2[1] = 0;
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       p1[e] = mul2(r2, fma2(v1[e], A1[e], mul2(p1[e], B1[e])));
@@ -262,8 +256,15 @@ template <typename T, int L>
 cudaError_t launch_columns(const approxifer_norm_rope_args& a, cudaStream_t stream) {
   constexpr int kRowsPerUnit = (32 / L) * kAhead;
   const int q_units = (a.Hq + kRowsPerUnit - 1) / kRowsPerUnit, kv_units = (a.Hkv + kRowsPerUnit - 1) / kRowsPerUnit;
-  const int64_t warps = a.T * (q_units + (a.k ? kv_units : 0) + (a.v ? kv_units : 0)), blocks = (warps + kThreads / 32 - 1) / (kThreads / 32);
-  return launch_kernel(norm_rope_kernel<T, L>, blocks, kThreads, 0, 1, stream, a, q_units, kv_units);
+  const int units = q_units + (a.k ? kv_units : 0) + (a.v ? kv_units : 0);
+  const int parts = (units + kMaxWarps - 1) / kMaxWarps, warps = (units + parts - 1) / parts;
+  int page_shift = 0;
+  while ((1 << page_shift) < a.page_size && page_shift < 30) ++page_shift;
+  if ((1 << page_shift) != a.page_size) page_shift = -1;
+  const bool partial = a.rot < a.D;
+  auto kernel = a.interleaved ? (partial ? norm_rope_kernel<T, L, true, true> : norm_rope_kernel<T, L, true, false>)
+                              : (partial ? norm_rope_kernel<T, L, false, true> : norm_rope_kernel<T, L, false, false>);
+  return launch_kernel(kernel, dim3((unsigned)a.T, (unsigned)parts), warps * 32, 0, 1, stream, a, q_units, kv_units, page_shift);
 }
 
 template <typename T>
