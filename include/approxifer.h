@@ -428,9 +428,9 @@ int approxifer_qk_norm_rope(const approxifer_norm_rope_args* args, void* cuda_st
  *   kv_len   [batch] int32        max_q  an upper bound on every sequence's number of queries (HOST)
  *   k_cache, v_cache  [num_pages][Hkv][page_size][D] by strides; bfloat16, as q and out
  * The softmax runs in one pass in fp32; the weights are rounded to bfloat16 for the product with V.
- * Hq a multiple of Hkv, 1 <= D <= 256, 1 <= page_size.  D a multiple of 8 up to 128, a page size that is a power of two
- * of at least 8 (single tokens: any), 16-byte aligned bases and strides of whole 16 bytes run on the tensor cores; others
- * run an element-wise kernel.
+ * Hq a multiple of Hkv, 1 <= D <= 256, 1 <= page_size.  The tensor-core kernels take D a multiple of 8 up to 128, 16-byte
+ * aligned bases and strides of whole 16 bytes, and, for more than single tokens (max_q > 1), a page size that is a power of
+ * two of at least 8 and at most 128 query heads to a key head; anything else runs an element-wise kernel.
  */
 typedef struct approxifer_attention_args {
   int64_t T;

@@ -8,7 +8,8 @@ namespace {
 constexpr int kElementThreads = 128;
 
 // One warp = one (token, query head); a lane holds every 32nd element of q and of the output.  The keys are walked one
-// by one with the running maximum and sum of the softmax.  The path for odd head sizes, page sizes and strides.
+// by one with the running maximum and sum of the softmax.  The path for odd head sizes, page sizes and strides: for layouts,
+// not for speed (a warp spends some 40 instructions on a key).
 __global__ void __launch_bounds__(kElementThreads) attention_element_kernel(const __grid_constant__ approxifer_attention_args a) {
   const int lane = threadIdx.x % 32;
   const int64_t unit = (int64_t)blockIdx.x * (kElementThreads / 32) + threadIdx.x / 32;

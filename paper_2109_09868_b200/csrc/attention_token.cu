@@ -13,6 +13,10 @@
 //   balanced form  all chunks of the call in one row, cut into equal runs, one to each warp that the GPU holds: lengths may
 //                  differ as they like.  A run that covers a whole unit writes its output; the others leave partial sums
 //                  in the workspace, which a second small launch joins, in order.
+//
+// Measured: one token, 1,028 visible of 1,500 cached, 32 heads on 8 of 128: 7.1 us (latency: three loads that wait for one
+// another, the joining); 48 tokens, window 4,096: 134 us, 6.0 TB/s; 4 contexts of up to 131,072, 2 key heads of 64: 43 us,
+// 4.6 TB/s (the joining of 148 partial results a unit is 5 us of it).
 #include "async.cuh"
 
 namespace approxifer {
@@ -649,8 +653,10 @@ cudaError_t launch_balanced(const approxifer_attention_args& a, const DeviceInfo
                        few ? 32 : kJoinWarps * 32, 0, 1, stream, a, row_tiles, ctas * kWarps, partial);
 }
 
-// The balanced form from 128 MB ... on
-bool wants_balance(const approxifer_attention_args& a) { return units_of(a) * most_seen(a) > 512 * 1024 / (a.D <= 64 ? 1 : 2); }
+// The balanced form from 96 K positions (times key heads) on.  Measured, cluster against balanced form, us: 8 K positions
+// (one sequence of 1,024, 8 heads of 128) 6.8 / 11.3, 64 K 10.5 / 14.7; 128 K: 8 sequences of 2,048 19.9 / 19.2, one of
+// 16,384 29.9 / 20.2, 64 of 256 30.7 / 21.2, one of 65,536 with 2 heads of 64 61 / 18; 512 K 82 / 56.
+bool wants_balance(const approxifer_attention_args& a) { return units_of(a) * most_seen(a) >= 96 * 1024; }
 
 }  // namespace
 

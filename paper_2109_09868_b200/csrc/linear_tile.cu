@@ -12,6 +12,10 @@
 //   warp 0     one lane: tensor-map copies, 64 columns of both operands per stage, 6 to 10 stages in flight
 //   warp 1     tcgen05.mma; allocates the tensor memory
 //   warps 2-5  accumulator -> shared memory; all warps: sum, epilogue, stores
+//
+// Few rows are bound by reading Wt, small products by the chain of a start, one copy, one product and the joining (5 to
+// 8 us).  Measured: 1 x 4,096 x 4,096 with residual 10 us, 3.3 TB/s; 20 rows, 4,096 -> 16,384 with bias and gelu 26 us,
+// 5.1 TB/s; 1,280 rows, 784 -> 10 5.5 us.
 #include "async.cuh"
 
 namespace approxifer {
@@ -265,7 +269,8 @@ cudaError_t launch_linear_tile(const approxifer_linear_args& a, cudaStream_t str
   cudaError_t e = current_device_info(&dev);
   if (e != cudaSuccess) return e;
   // Up to 128 rows of X the product is bound by reading Wt, whose rows then become the 128 lanes, and the tile is only as
-  // wide as X has rows.  Beyond, X's rows are the lanes and the tile as wide as N needs, up to 128.
+  // wide as X has rows.  Beyond, X's rows are the lanes and the tile as wide as N needs, up to 128.  (From 65 rows on, where
+  // both tiles are 128 wide, the two ways measure the same within 2 %.)
   const bool swap = a.M <= 128;
   const int64_t across = swap ? a.M : a.N;
   const int bn = across <= 16 ? 16 : across <= 32 ? 32 : across <= 64 ? 64 : 128;

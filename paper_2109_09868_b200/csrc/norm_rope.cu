@@ -85,6 +85,10 @@ __global__ void __launch_bounds__(kElementThreads) norm_rope_element_kernel(cons
 // With 400 MB to move this is bound by instruction issue as much as by HBM: hence the pairs within a lane (exchanging them
 // between lanes cost 16 instructions of 78 a row pair), the packed fp32 arithmetic, a token to a CTA (no division to find
 // it), and the two template parameters (INTER: neighbouring pairs; PARTIAL: some elements are not turned).
+//
+// Measured: 16,384 tokens, 32 + 8 + 8 heads of 128 in bfloat16: 81 us, 5.0 TB/s (a plain copy of as many bytes takes 66);
+// 1,237 tokens, 15 + 5 + 5 heads of 80 in fp32: 5.5 us; one token 2.8 us.  Tried and slower: copying ahead into shared
+// memory by persistent warps (113 us), eight rows in flight (86), two (93).
 constexpr int kMaxWarps = 8;  // units of a token per CTA
 constexpr int kAhead = 4;
 
