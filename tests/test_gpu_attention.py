@@ -197,3 +197,66 @@ def test_attention_of_no_tokens():
     x = inputs([1], [8], 2, 1, 64, 16)
     none = (x[0][:0], x[1], x[2], x[3], torch.zeros(2, dtype=torch.int32), x[5])
     assert run(none, 1, 0, 0, 0.1).shape == (0, 2, 64)
+
+
+@pytest.mark.parametrize("qs,kvs,page", [([1, 1], [700, 40], 256), ([200], [700], 256), ([200], [1400], 1024), ([130, 20], [300, 900], 128)])
+def test_attention_pages_longer_than_a_tile(qs, kvs, page):
+    for D in (64, 128):
+        x = inputs(qs, kvs, 4, 2, D, page, seed=page + D)
+        want, bound = ref.attention(*x, 150, 3, D ** -0.5)
+        check(run(x, max(qs), 150, 3, D ** -0.5), want, bound)
+
+
+@pytest.mark.parametrize("nq", [1, 40])
+def test_attention_cache_offsets_beyond_32_bits(nq):
+    """A cache of more than 2^32 bytes, and 2^31 elements, whose tokens lie at its end."""
+    Hkv, page, D, n = 4, 16, 128, 90
+    pages = (1 << 31) // (Hkv * page * D) + 64
+    caches = [torch.empty((pages, Hkv, page, D), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    g = torch.Generator().manual_seed(8)
+    table = torch.arange(pages - 1, pages - 1 - (n + page - 1) // page, -1, dtype=torch.int32)[None]
+    small = [torch.randn((table.shape[1], Hkv, page, D), generator=g).bfloat16() for _ in range(2)]
+    for c, s in zip(caches, small):
+        c[table[0].long().cuda()] = s.cuda()
+    q = torch.randn((nq, 8, D), generator=g).bfloat16()
+    start, lens = torch.tensor([0, nq], dtype=torch.int32), torch.tensor([n], dtype=torch.int32)
+    want, bound = ref.attention(q, *small, torch.arange(table.shape[1], dtype=torch.int32)[None], start, lens, 50, 2, 0.1)
+    got = ap.approxifer_attention(q.cuda(), *caches, table.cuda(), start.cuda(), lens.cuda(), nq, window=50, sinks=2, scale=0.1)
+    check(got, want, bound)
+    # and the same slots written by the norm and rotation
+    cs = torch.cat([torch.ones(4, D // 2), torch.zeros(4, D // 2)], 1).cuda()
+    slots = (table[0].long() * page + 3).cuda()
+    T = len(slots)
+    new = torch.randn((T, Hkv, D), generator=g).bfloat16().cuda()
+    pos = torch.zeros(T, dtype=torch.int32, device="cuda")
+    ap.approxifer_qk_norm_rope(q[:1].expand(T, -1, -1).contiguous().cuda(), new, new, None, None, cs, pos, *caches, slots)
+    for c in caches:
+        assert torch.equal(c[table[0].long().cuda(), :, 3], new)
+
+
+def test_attention_large_finite_values_behind_the_mask_do_not_reach_a_row():
+    """Values of the type's largest magnitude in positions that a row does not see: their weight is zero exactly."""
+    n, window = 260, 70
+    x = list(inputs([n], [n], 4, 2, 64, 16, seed=4))
+    want, bound = ref.attention(*x, window, 0, 0.125)
+    for at in (0, 129, 259):
+        y = list(x)
+        y[2] = x[2].clone()
+        y[2][x[3][0, at // 16].long(), :, at % 16] = 3.3e38
+        got = run(y, n, window, 0, 0.125).double().cpu()
+        sees = torch.tensor([at <= p < at + window for p in range(n)])
+        check(got[~sees], want[~sees], bound[~sees])
+
+
+def test_attention_refuses_what_the_library_cannot_take():
+    q, k, v, table, start, lens = [t.cuda() for t in inputs([1], [20], 4, 2, 64, 16)]
+    for bad in (dict(q=q.float()), dict(k=k.float()), dict(v=v[:-1]), dict(table=table.long()), dict(start=start[:1]), dict(lens=lens.float()), dict(q=q.cpu()),
+                dict(k=k[..., :32]), dict(q=q.transpose(1, 2))):
+        args = dict(dict(q=q, k=k, v=v, table=table, start=start, lens=lens), **bad)
+        with pytest.raises(ValueError):
+            ap.approxifer_attention(*args.values(), 1)
+    for bad in (dict(window=-1), dict(sinks=-2), dict(scale=float("nan"))):
+        with pytest.raises(ap.ApproxiferError):
+            ap.approxifer_attention(q, k, v, table, start, lens, 1, **bad)
+    with pytest.raises(ap.ApproxiferError):
+        ap.approxifer_attention(q[:, :3], k, v, table, start, lens, 1)  # 3 query heads on 2 key heads

@@ -116,3 +116,20 @@ def test_linear_is_repeatable_and_runs_on_a_stream_and_in_a_graph():
 
 def test_linear_of_no_rows():
     assert ap.approxifer_linear(torch.empty((0, 64), dtype=torch.bfloat16, device="cuda"), torch.empty((5, 64), dtype=torch.bfloat16, device="cuda")).shape == (0, 5)
+
+
+def test_linear_output_offsets_beyond_32_bits():
+    M, N, K = 66000, 33000, 64  # 2.18e9 elements
+    x, w = normal((M, K), 1), normal((N, K), 2, std=K ** -0.5)
+    y = ap.approxifer_linear(x.cuda(), w.cuda())
+    rows = [0, 1, 40000, 65071, 65072, M - 1]
+    want, bound = ref.linear(x[rows], w, None, "none", None, torch.bfloat16)
+    check(y[rows], want, bound)
+
+
+def test_linear_refuses_what_the_library_cannot_take():
+    x, w = normal((4, 64), 1).cuda(), normal((8, 64), 2).cuda()
+    for bad in (dict(X=x.float()), dict(weight=w[:, :32]), dict(bias=x[0]), dict(residual=x), dict(activation="tanh"), dict(out_dtype=torch.float16), dict(X=x.cpu()),
+                dict(X=x[0]), dict(Y=torch.empty((4, 8), device="cuda").bfloat16(), out_dtype=torch.float32), dict(X=x.t().contiguous().t())):
+        with pytest.raises(ValueError):
+            ap.approxifer_linear(**dict(dict(X=x, weight=w), **bad))

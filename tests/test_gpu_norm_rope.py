@@ -131,3 +131,18 @@ def test_norm_rope_of_zero_rows_and_of_no_tokens():
     w = torch.ones(64, dtype=torch.bfloat16, device="cuda")
     assert not ap.approxifer_qk_norm_rope(x, None, None, w, None, cs, pos, None, None, None, eps=EPS).any()
     assert ap.approxifer_qk_norm_rope(x[:0], None, None, w, None, cs, pos[:0], None, None, None).shape == (0, 2, 64)
+
+
+def test_norm_rope_refuses_what_the_library_cannot_take():
+    x = inputs(5, 4, 2, 64, 64, 16, torch.bfloat16)
+    d = {n: t.cuda() for n, t in x.items()}
+    q, k, v = split(d["qkv"], 4, 2, 64)
+    good = dict(q=q, k=k, v=v, q_weight=d["qw"], k_weight=d["kw"], cos_sin=d["cs"], positions=d["pos"], k_cache=d["kc"], v_cache=d["vc"], slots=d["slots"])
+    for bad in (dict(q=q.float()), dict(k=k.float()), dict(q_weight=d["qw"][:32]), dict(cos_sin=d["cs"].bfloat16()), dict(positions=d["pos"].long()),
+                dict(slots=d["slots"].int()), dict(k=None), dict(v_cache=None), dict(slots=None), dict(k_cache=d["kc"][:, :1]), dict(q=q.cpu())):
+        with pytest.raises(ValueError):
+            ap.approxifer_qk_norm_rope(**dict(good, **bad))
+    with pytest.raises(ap.ApproxiferError):
+        ap.approxifer_qk_norm_rope(**dict(good, cos_sin=d["cs"][:, :33].contiguous()))  # an odd rotation
+    with pytest.raises(ap.ApproxiferError):
+        ap.approxifer_qk_norm_rope(**good, eps=-1.0)
