@@ -24,6 +24,9 @@
 //   1 warp           looks through the values of tiles that some rows see only in part: a weight of zero must meet no
 //                    infinity or NaN, so such elements are taken out, and where a row does see them the output adds them back
 //
+// Where a call has few query blocks, a cluster of CTAs shares one: each walks a part of the key tiles, and at the end they join
+// their rows' maxima, sums and outputs in shared memory, in order.
+//
 // What bounds it is that chain and its issue, not a unit: at 4,096 causal tokens, D = 128, the tensor cores are busy 48 % of
 // the cycles, the special-function unit (a weight is one exponential) 49 %, instructions issue in 43 %.  Measured: 2 x 8,192
 // tokens causal, 32 heads on 4 of 128: 949 us, 1,159 TFLOP/s; prompts of 1,828 .. 4,096 under a window of 1,024, 32 heads
@@ -41,6 +44,7 @@ namespace {
 constexpr int kRows = 128;  // query rows per tile
 constexpr int kKeys = 128;  // keys per tile
 constexpr int kOtherWarps = 4;
+constexpr int kMaxSplit = 8;  // CTAs of a cluster that share a query block
 constexpr int kBlock = kRows * 128;  // bytes of 64 columns of a tile
 constexpr float kGrowth = 8.f;       // log2 of what the maximum in use may lag behind
 
@@ -71,10 +75,11 @@ struct Job {
   int lo, p1;          // lowest position in a window, highest position seen
   int window, sinks;
   int tokens;          // per tile
-  int sink_tiles, first_tile, steps;
+  int sink_tiles, first_tile;
+  int skip, steps;       // this CTA's steps of the cluster's: from `skip` on
   int steps0, steps1;  // of the two query tiles
 
-  __device__ __forceinline__ int tile(int j) const { return j < sink_tiles ? j : first_tile + (j - sink_tiles); }
+  __device__ __forceinline__ int tile(int j) const { return j + skip < sink_tiles ? j + skip : first_tile + (j + skip - sink_tiles); }
   __device__ __forceinline__ int first_pos(int t) const { return pos0 + t * tokens; }
   __device__ __forceinline__ int last_pos(int t) const { return pos0 + min((t + 1) * tokens, left) - 1; }
   // Which steps a query tile takes part in: tile 0 up to the last key its rows see, tile 1 all (the window of its first row
@@ -93,8 +98,8 @@ struct Job {
   // steps from `from` up to `to` are full for query tile t (tiles that hold sinks are left to the masked way)
   __device__ __forceinline__ void full_steps(int t, int* from, int* to) const {
     const int past = last_pos(t) - window, k0 = window && past >= 0 ? past / kKeys + 1 : 0, k1 = first_pos(t) < 0 ? 0 : (first_pos(t) + 1) / kKeys;
-    *from = sink_tiles + max(0, k0 - first_tile);
-    *to = sink_tiles + k1 - first_tile;
+    *from = sink_tiles + max(0, k0 - first_tile) - skip;
+    *to = sink_tiles + k1 - first_tile - skip;
   }
   __device__ __forceinline__ bool part(int j, int tiles) const {  // some row of a tile that is worked on does not see all of it
     return (j < steps0 && !full(0, j)) || (tiles == 2 && j < steps1 && !full(1, j));
@@ -113,10 +118,10 @@ __device__ __forceinline__ uint32_t pages_of(uint32_t there, int c, int page_shi
 }
 
 template <int TQ>
-__device__ __forceinline__ bool find_job(const TileArgs& g, Job* job) {
+__device__ __forceinline__ bool find_job(const TileArgs& g, int S, int rank, Job* job) {
   const approxifer_attention_args& a = g.a;
   // blocks of late queries see most: they come first
-  int x = blockIdx.x;
+  int x = blockIdx.x / S;
   job->hk = x % a.Hkv;
   x /= a.Hkv;
   job->b = x % a.batch;
@@ -141,6 +146,11 @@ __device__ __forceinline__ bool find_job(const TileArgs& g, Job* job) {
   const int last0 = job->last_pos(0);  // (of tile 0's rows)
   job->steps1 = TQ == 2 && job->tokens < job->left ? job->steps : 0;
   job->steps0 = job->steps1 == 0 ? job->steps : last0 < 0 ? 0 : min(job->steps, job->sink_tiles + max(0, last0 / kKeys - job->first_tile + 1));
+  // a cluster's CTAs take consecutive parts of the steps; a query tile takes part in a first part of each as it does of all
+  job->skip = (int)((int64_t)job->steps * rank / S);
+  job->steps = (int)((int64_t)job->steps * (rank + 1) / S) - job->skip;
+  job->steps0 = min(max(job->steps0 - job->skip, 0), job->steps);
+  job->steps1 = min(max(job->steps1 - job->skip, 0), job->steps);
   return true;
 }
 
@@ -178,6 +188,10 @@ __device__ __forceinline__ bool any_of_both(int id, bool want) {
   return any != 0;
 }
 
+// All softmax warps.
+template <int TQ>
+__device__ __forceinline__ void softmax_warps_meet() { asm volatile("barrier.cta.sync.aligned 15, %0;" ::"n"(TQ * 256) : "memory"); }
+
 // The n-th (query tile, key tile) pair; the first or the last of its key tile.  (A query tile takes part from step 0 on.)
 struct Item {
   int t, j;
@@ -191,7 +205,7 @@ __device__ __forceinline__ Item item_at(const Job& job, int n) {
   return {job.steps1 > 0 ? 1 : 0, n - both, true, true};
 }
 
-template <int DP>
+template <int DP, bool CLUSTER>
 __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
     attention_tile_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
                           const __grid_constant__ TileArgs g) {
@@ -210,6 +224,10 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
                  s_free = s_ready + 16, p_ready = s_free + 8, pv_done = p_ready + 32;
   const uint32_t q_at = smem_addr(base + 1024), ring = q_at + TQ * kTile;
   float* exchange = reinterpret_cast<float*>(base + 1024 + (TQ + kStages) * kTile);  // [tile][row]
+  // (a cluster, at the end, over queries and ring) O of this CTA's part [tile][row][DP], maximum and sum [tile][row]
+  float4* part_rows = reinterpret_cast<float4*>(base + 1024);
+  float2* row_sums = reinterpret_cast<float2*>(base + 1024 + TQ * kRows * DP * 4);
+  static_assert(TQ * kRows * (DP * 4 + 8) <= (TQ + kStages) * kTile, "a CTA's part exceeds queries and ring");
   const approxifer_attention_args& a = g.a;
   const int warp = warp_index(), lane = threadIdx.x % 32;
   unsigned int* count = &g_attention_tile_wait_timeouts;
@@ -230,7 +248,8 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
   }
   wait_for_inputs();
   Job job;
-  if (!find_job<TQ>(g, &job)) return;
+  const int S = CLUSTER ? (int)cluster_size() : 1, rank = CLUSTER ? (int)cluster_rank() : 0;
+  if (!find_job<TQ>(g, S, rank, &job)) return;  // (all CTAs of a cluster or none)
   // (copies) the page of this lane's rows of a key tile, looked up a tile ahead
   const int32_t* table = a.block_table + (int64_t)job.b * a.table_stride;
   const int page_rows = 1 << g.page_shift, rows = min(page_rows, kKeys), per_tile = kKeys / rows;
@@ -374,12 +393,15 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
       ok = warp_wait(pv_done + 8 * t, TQ == 1 ? (steps - 1) & 1 : 0, abort, count);
       tmem_fence_after();
     }
+    if constexpr (CLUSTER) softmax_warps_meet<TQ>();  // no product reads shared memory any more, of either tile
     if (ok) {
-      // O / sum, by way of the tile's queries' place in shared memory (a warp keeps to its own rows and columns) into whole rows
-      const float inv = l == 0.f ? 0.f : 1.f / l;
+      // One CTA: O / sum, by way of the tile's queries' place in shared memory (a warp keeps to its own rows and columns) into
+      // whole rows.  A cluster: O as it is into shared memory, with the row's maximum and sum.
+      const float inv = CLUSTER ? 1.f : l == 0.f ? 0.f : 1.f / l;
       const bool add_back = *poison != 0;
       unsigned char* own_rows = base + 1024 + t * kTile + (half * 4 + quarter) * 32 * kOut * 2;
       constexpr int kCols = kOut / 8;  // 16-byte columns
+      if (CLUSTER && half == 0) row_sums[t * kRows + r] = make_float2(m, l);
 #pragma unroll 1
       for (int c = 0; c < kOut; c += 16) {
         float y[16];
@@ -415,15 +437,21 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
             }
           }
         }
+        if constexpr (CLUSTER) {
 #pragma unroll
-        for (int i = 0; i < 16; i += 8)
-          *reinterpret_cast<uint4*>(own_rows + lane * kOut * 2 + ((((c + i) / 8) ^ (lane & (kCols - 1))) << 4)) =
-              make_uint4(pack_bf16x2(y[i], y[i + 1]), pack_bf16x2(y[i + 2], y[i + 3]), pack_bf16x2(y[i + 4], y[i + 5]), pack_bf16x2(y[i + 6], y[i + 7]));
+          for (int i = 0; i < 16; i += 4)
+            part_rows[(t * kRows + r) * (DP / 4) + (((half * kOut + c + i) / 4) ^ (r & 7))] = make_float4(y[i], y[i + 1], y[i + 2], y[i + 3]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 16; i += 8)
+            *reinterpret_cast<uint4*>(own_rows + lane * kOut * 2 + ((((c + i) / 8) ^ (lane & (kCols - 1))) << 4)) =
+                make_uint4(pack_bf16x2(y[i], y[i + 1]), pack_bf16x2(y[i + 2], y[i + 3]), pack_bf16x2(y[i + 4], y[i + 5]), pack_bf16x2(y[i + 6], y[i + 7]));
+        }
         __syncwarp();
       }
       const int64_t to = mine ? (int64_t)(job.token0 + token) * a.o_tstride + (int64_t)(job.hk * g.group + r % g.group) * a.o_hstride : -1;
 #pragma unroll 4
-      for (int x = lane; x < 32 * kCols; x += 32) {
+      for (int x = lane; !CLUSTER && x < 32 * kCols; x += 32) {
         const int row = x / kCols, col = x % kCols, d = half * kOut + col * 8;
         const int64_t at = __shfl_sync(0xffffffffu, to, row);
         if (at >= 0 && d < a.D)
@@ -578,18 +606,78 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
     tmem_fence_after();
     tmem_free(tmem, kTmemCols);
   }
+  if constexpr (CLUSTER) {
+    // The CTAs' parts of every row, in order: each CTA joins its share of the rows, a warp to a row.
+    cluster_sync();
+    if (warp < kScoreWarp) {
+      const float scale = fmaxf(fabsf(a.scale) * 1.4426950408889634f, 1e-37f);
+      const uint32_t parts = smem_addr(part_rows), sums = smem_addr(row_sums);
+      for (int x = TQ * kRows * rank / S + warp; x < TQ * kRows * (rank + 1) / S; x += kScoreWarp) {
+        const int t = x / kRows, r = x % kRows, token = t * job.tokens + r / g.group;
+        if (r / g.group >= job.tokens || token >= job.left) continue;
+        float2 ml[kMaxSplit];
+        float best = -CUDART_INF_F;
+#pragma unroll
+        for (int s = 0; s < kMaxSplit; ++s) {
+          ml[s] = s < S ? peer_load2(peer_smem(sums + x * 8, s)) : make_float2(-CUDART_INF_F, 0.f);
+          best = fmaxf(best, ml[s].x);
+        }
+        if (best == -CUDART_INF_F) best = 0.f;
+        const int c = lane * (DP / 32);  // this lane's columns
+        const uint32_t at = parts + (x * (DP / 4) + ((c / 4) ^ (r & 7))) * 16 + (c % 4) * 4;
+        float total = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < kMaxSplit; ++s) {
+          if (s >= S) continue;
+          const float k = pow2((ml[s].x - best) * scale);
+          total = fmaf(k, ml[s].y, total);
+          if constexpr (DP == 128) {
+            const float4 v = peer_load(peer_smem(at, s));
+            y[0] = fmaf(k, v.x, y[0]), y[1] = fmaf(k, v.y, y[1]), y[2] = fmaf(k, v.z, y[2]), y[3] = fmaf(k, v.w, y[3]);
+          } else {
+            const float2 v = peer_load2(peer_smem(at, s));
+            y[0] = fmaf(k, v.x, y[0]), y[1] = fmaf(k, v.y, y[1]);
+          }
+        }
+        const float inv = total == 0.f ? 0.f : 1.f / total;
+        bf16* out = reinterpret_cast<bf16*>(a.out) + (int64_t)(job.token0 + token) * a.o_tstride + (int64_t)(job.hk * g.group + r % g.group) * a.o_hstride + c;
+        if (c < a.D) {
+          if constexpr (DP == 128) *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(y[0] * inv, y[1] * inv), pack_bf16x2(y[2] * inv, y[3] * inv));
+          else *reinterpret_cast<uint32_t*>(out) = pack_bf16x2(y[0] * inv, y[1] * inv);
+        }
+      }
+    }
+    cluster_sync();  // (a CTA's shared memory stays until all have read it)
+  }
+}
+
+template <int DP, bool CLUSTER>
+cudaError_t launch_split(const TileArgs& g, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const DeviceInfo& dev, int64_t ctas, int split,
+                         cudaStream_t stream) {
+  auto kernel = attention_tile_kernel<DP, CLUSTER>;
+  struct Tag {};
+  const cudaError_t e = ensure_dynamic_smem<Tag>(kernel, dev.ordinal, smem_bytes(DP));
+  if (e != cudaSuccess) return e;
+  return launch_kernel(kernel, ctas * split, threads_of(DP), smem_bytes(DP), split, stream, q, k, v, g);
 }
 
 template <int DP>
 cudaError_t launch_one(const TileArgs& g, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, cudaStream_t stream) {
   const DeviceInfo* dev;
-  cudaError_t e = current_device_info(&dev);
+  const cudaError_t e = current_device_info(&dev);
   if (e != cudaSuccess) return e;
-  auto kernel = attention_tile_kernel<DP>;
-  struct Tag {};
-  if ((e = ensure_dynamic_smem<Tag>(kernel, dev->ordinal, smem_bytes(DP))) != cudaSuccess) return e;
-  const int64_t ctas = (int64_t)g.blocks * g.a.batch * g.a.Hkv;
-  return launch_kernel(kernel, ctas, threads_of(DP), smem_bytes(DP), 1, stream, q, k, v, g);
+  const approxifer_attention_args& a = g.a;
+  const int64_t ctas = (int64_t)g.blocks * a.batch * a.Hkv;
+  // Few query blocks: as many CTAs to each, along the keys, as the GPU holds, each with three tiles of keys or more.  (The
+  // lengths are on the device: what a block can see at most says how far it is worth cutting.)  Measured, one CTA a block
+  // against the cluster, us: 2 queries at 4,000 keys, 1 key head of 128: 62 / 16; 10 at 4,000, 8 heads of 64: 44 / 13; 64 at
+  // 2,048, 2 heads of 128: 38 / 22; 80 blocks of 64 cut in two for two CTAs on every SM: 31 / 35, hence one CTA to an SM.
+  int64_t most = a.table_pages * a.page_size;
+  if (a.window && (int64_t)a.window + a.max_q + a.sinks < most) most = (int64_t)a.window + a.max_q + a.sinks;
+  const int held = dev->sms * 3 / 4;
+  int split = 1;
+  while (split < kMaxSplit && ctas * split * 2 <= held && most >= (int64_t)split * 2 * 3 * kKeys) split *= 2;
+  return split > 1 ? launch_split<DP, true>(g, q, k, v, *dev, ctas, split, stream) : launch_split<DP, false>(g, q, k, v, *dev, ctas, 1, stream);
 }
 
 int log2_of(int v) {

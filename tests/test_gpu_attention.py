@@ -75,6 +75,13 @@ CASES = [  # queries, cached tokens, Hq, Hkv, D, page, window, sinks
     ([140], [140], 2, 1, 256, 16, 0, 0),
     ([6], [50], 2, 1, 33, 16, 10, 1),
     ([400], [400], 2, 1, 128, 16, 5, 40),      # sinks that reach past the window's start
+    # few queries at long contexts: the keys are cut over a cluster
+    ([7], [3000], 2, 1, 96, 16, 0, 0),
+    ([2], [1100], 4, 4, 64, 64, 0, 0),
+    ([33, 100], [1700, 2500], 8, 2, 64, 16, 0, 0),
+    ([160], [2600], 4, 2, 128, 32, 900, 5),
+    ([90, 2, 0], [1600, 900, 70], 6, 2, 128, 16, 1000, 20),
+    ([20], [10], 2, 2, 128, 16, 0, 0),
 ]
 
 
@@ -197,6 +204,33 @@ def test_attention_of_no_tokens():
     x = inputs([1], [8], 2, 1, 64, 16)
     none = (x[0][:0], x[1], x[2], x[3], torch.zeros(2, dtype=torch.int32), x[5])
     assert run(none, 1, 0, 0, 0.1).shape == (0, 2, 64)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_attention_cut_over_a_cluster_keeps_what_a_row_sees(D):
+    """Few queries at a long context: NaN values reach the rows that see them, freed pages are left out, results repeat."""
+    nq, n, window, sinks = 70, 2000, 1200, 3
+    x = list(inputs([nq], [n], 4, 2, D, 16, seed=6))
+    want, bound = ref.attention(*x, window, sinks, D ** -0.5)
+    got = run(x, nq, window, sinks, D ** -0.5)
+    check(got, want, bound)
+    assert torch.equal(got, run(x, nq, window, sinks, D ** -0.5))
+    for at in (n - nq - window + 20, n - 30, 1):
+        y = list(x)
+        y[2] = x[2].clone()
+        y[2][x[3][0, at // 16].long(), 1, at % 16, 5] = float("nan")
+        bad = run(y, nq, window, sinks, D ** -0.5).double().cpu()
+        sees = torch.tensor([at <= p and (at > p - window or at < sinks) for p in range(n - nq, n)])
+        assert torch.isnan(bad[sees][:, 2:, 5]).all()
+        rest = [d for d in range(D) if d != 5]
+        check(bad[..., rest], want[..., rest], bound[..., rest])
+        if not sees.all():
+            check(bad[~sees], want[~sees], bound[~sees])
+    y = list(x)
+    y[3] = x[3].clone()
+    y[3][0, [70, 90, 110]] = -1
+    want, bound = ref.attention(*y, window, sinks, D ** -0.5)
+    check(run(y, nq, window, sinks, D ** -0.5), want, bound)
 
 
 @pytest.mark.parametrize("qs,kvs,page", [([1, 1], [700, 40], 256), ([200], [700], 256), ([200], [1400], 1024), ([130, 20], [300, 900], 128)])
