@@ -305,23 +305,6 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
       if (!(ok = warp_wait(s_ready + 8 * t, j & 1, abort, count))) break;
       tmem_fence_after();
       const uint32_t there = pages_there[j % kMasks];
-      if (j < full_from || j >= full_to || there != all_pages) {
-        // what a row does not see becomes minus infinity, in place and in a short loop: few tiles come here, and the code that
-        // all tiles run stays small
-        const uint32_t sign = flip ? 0x80000000u : 0u;
-#pragma unroll 1
-        for (int c = 0; c < kMine; c += 32) {
-          uint32_t v[32];
-          tmem_ld32(s_at + c, v);
-          const int k = half * kMine + c;
-          const uint32_t sees = job.sees(pos, job.tile(j) * kKeys + k) & pages_of(there, k, g.page_shift);
-          tmem_wait_ld(v);
-#pragma unroll
-          for (int i = 0; i < 32; ++i) v[i] = sees & (1u << i) ? v[i] ^ sign : 0xff800000u;
-          tmem_st32(s_at + c, v);
-        }
-        tmem_wait_st();
-      }
       float s[kMine];
       tmem_ld32(s_at, *reinterpret_cast<uint32_t(*)[32]>(s));
       tmem_ld32(s_at + 32, *reinterpret_cast<uint32_t(*)[32]>(s + 32));
@@ -331,6 +314,21 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
       if constexpr (TQ == 1) {
         __syncwarp();
         if (lane == 0) bar_arrive(s_free);
+      }
+      if (j < full_from || j >= full_to || there != all_pages) {  // what a row does not see becomes minus infinity
+        if (flip) {
+#pragma unroll
+          for (int i = 0; i < kMine; ++i) s[i] = -s[i];
+        }
+#pragma unroll
+        for (int c = 0; c < kMine; c += 32) {
+          const int k = half * kMine + c;
+          const uint32_t sees = job.sees(pos, job.tile(j) * kKeys + k) & pages_of(there, k, g.page_shift);
+          if (__any_sync(0xffffffffu, sees != 0xffffffffu)) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) s[c + i] = sees & (1u << i) ? s[c + i] : -CUDART_INF_F;
+          }
+        }
       }
       float top[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
 #pragma unroll
