@@ -17,6 +17,8 @@ bool linear_tile_eligible(const approxifer_linear_args& a);  // see linear_tile.
 cudaError_t launch_linear_tile(const approxifer_linear_args& a, cudaStream_t stream);
 cudaError_t read_linear_tile_wait_timeouts(unsigned int* out);
 cudaError_t reset_linear_tile_wait_timeouts();
+bool linear_few_wanted(const approxifer_linear_args& a, int sms);  // see linear_few.cu
+cudaError_t launch_linear_few(const approxifer_linear_args& a, cudaStream_t stream);
 cudaError_t launch_linear_pair(const approxifer_linear_args& a, cudaStream_t stream);  // see linear_pair.cu
 cudaError_t read_linear_pair_wait_timeouts(unsigned int* out);
 cudaError_t reset_linear_pair_wait_timeouts();

@@ -55,13 +55,14 @@ __global__ void __launch_bounds__(kThreads) linear_element_kernel(const __grid_c
 
 cudaError_t launch_linear(const approxifer_linear_args& a, cudaStream_t stream) {
   if (linear_tile_eligible(a)) {
+    const DeviceInfo* dev;
+    const cudaError_t e = current_device_info(&dev);
+    if (e != cudaSuccess) return e;
+    if (linear_few_wanted(a, dev->sms)) return launch_linear_few(a, stream);
     // 256 x 256 tiles on pairs of CTAs once the 128 x 128 tiles of the other kernel would need a second turn.  Measured, tile
     // against pair kernel, us, 256 x 256 tiles: 32 (2,048 x 1,024 x 4,096) 22.4 / 26.9, 40 (1,024 x 2,560 x 4,096) 43.3 / 28.3,
     // 48 (1,536 x 2,048 x 4,096) 44.2 / 28.6, 256 (4,096^2 x 512) 55 / 25.  (Pairs with 256 x 128 tiles, to leave fewer of them
     // idle in the last turn, reach 70 % of the rate and win nowhere.)
-    const DeviceInfo* dev;
-    const cudaError_t e = current_device_info(&dev);
-    if (e != cudaSuccess) return e;
     if (a.M > 128 && a.N > 128 && ((a.M + 127) / 128) * ((a.N + 127) / 128) > dev->sms) return launch_linear_pair(a, stream);
     return launch_linear_tile(a, stream);
   }

@@ -14,8 +14,7 @@
 //   warps 2-5  accumulator -> shared memory; all warps: sum, epilogue, stores
 //
 // Few rows are bound by reading Wt, small products by the chain of a start, one copy, one product and the joining (5 to
-// 8 us).  Measured: 1 x 4,096 x 4,096 with residual 10 us, 3.3 TB/s; 20 rows, 4,096 -> 16,384 with bias and gelu 26 us,
-// 5.1 TB/s; 1,280 rows, 784 -> 10 5.5 us.
+// 8 us).  Measured: 20 rows, 4,096 -> 16,384 with bias and gelu 26 us, 5.1 TB/s; 1,280 rows, 784 -> 10 5.5 us.
 #include "async.cuh"
 
 namespace approxifer {

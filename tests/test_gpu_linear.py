@@ -38,6 +38,10 @@ CASES = [  # M, N, K, bias, activation, residual, out
     (1000, 1000, 160, False, "none", True, torch.float32),
     (2300, 1100, 320, True, "gelu", True, torch.bfloat16),
     (3000, 24, 64, False, "silu", False, torch.bfloat16),
+    (3, 1003, 2056, True, "gelu", True, torch.float32),      # few rows: K in turns of 1,024, odd N
+    (8, 4700, 136, False, "silu", True, torch.bfloat16),
+    (5, 40, 8192, True, "relu", False, torch.bfloat16),
+    (8, 50, 8200, True, "none", True, torch.float32),
     (4000, 1100, 320, True, "gelu", True, torch.bfloat16),   # many tiles: pairs of CTAs
     (4000, 1100, 72, True, "gelu_tanh", False, torch.float32),
     (2049, 2305, 520, True, "silu", True, torch.float32),
