@@ -53,6 +53,9 @@ cudaError_t make_tensor_map(CUtensorMap* map, const void* base, int rank, const 
 
 constexpr uint32_t kWaitLimit = 1u << 21;  // try_wait attempts (each may block for a while) before a wait gives up
 
+// Lets the next kernel's CTAs start once all of this one's have come here.  A kernel that allocates tensor memory comes here
+// only when it holds it: a CTA of the next kernel on the same SM could take it first and then wait for this kernel to end,
+// while a CTA of this one waits for the memory.
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_inputs() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 

@@ -232,7 +232,6 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
   const approxifer_attention_args& a = g.a;
   const int warp = warp_index(), lane = threadIdx.x % 32;
   unsigned int* count = &g_attention_tile_wait_timeouts;
-  let_next_start();
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) bar_init(full + 8 * s, 1), bar_init(empty + 8 * s, 1);
@@ -265,6 +264,7 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
   __syncthreads();
   tmem_fence_after();
   const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
+  let_next_start();  // not before: the tensor memory is held
 
   // The softmax warps keep scores in registers; the four others give up theirs (two tiles: 512 x 104 + 128 x 64 = 640 x 96
   // registers at the launch; one: 256 x 96 + 128 x 48 = 384 x 80).

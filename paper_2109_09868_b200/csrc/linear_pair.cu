@@ -114,7 +114,6 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int rank = (int)cluster_rank();
   const int pair = blockIdx.x / 2, pairs = gridDim.x / 2;
   unsigned int* count = &g_linear_pair_wait_timeouts;
-  let_next_start();
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) bar_init(full + 8 * s, 1), bar_init(empty + 8 * s, 1);
@@ -130,6 +129,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   cluster_sync();  // both CTAs' barriers stand before any is signalled from the other
   tmem_fence_after();
   const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
+  let_next_start();  // not before: the tensor memory is held
   wait_for_inputs();
 
   if (warp == 0 && lane == 0) {

@@ -89,7 +89,6 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tile_kernel(const __grid_c
   unsigned char* stages = base + kHeader;
   const uint32_t full = smem_addr(bars), empty = full + 8 * kStages, done = empty + 8 * kStages;
   const int warp = warp_index(), lane = threadIdx.x % 32;
-  let_next_start();
 
   const int S = (int)cluster_size(), rank = (int)cluster_rank();
   const int tile = blockIdx.x / S;
@@ -109,6 +108,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tile_kernel(const __grid_c
   __syncthreads();
   tmem_fence_after();
   const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
+  let_next_start();  // not before: the tensor memory is held
   wait_for_inputs();
 
   if (warp == 0 && lane == 0) {
