@@ -463,11 +463,13 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
     else asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
     if (warp == kCopyWarp) {
       // ---- copies ----
-      if (lane == 0) {
-        const int boxes = (TQ == 2 && job.tokens < job.left ? 2 : 1) * (DP / 64);  // (a second tile without rows is not read)
-        bar_expect(q_full, boxes * g.group * job.tokens * 128);
-        for (int t = 0; t < TQ && t * job.tokens < job.left; ++t)
-          for (int c = 0; c < DP / 64; ++c) tma_3d(q_at + t * kTile + c * kBlock, &q_map, c * 64, job.hk * g.group, job.token0 + t * job.tokens, q_full);
+      // The queries of the tiles that have a step, and of no other: the first product is what waits for them.  A copy that nothing
+      // waits for would land in rows that the output is staged in meanwhile, or in the memory of the SM's next CTA.
+      if (lane == 0 && job.steps > 0) {
+        bar_expect(q_full, ((job.steps0 > 0) + (job.steps1 > 0)) * (DP / 64) * g.group * job.tokens * 128);
+        for (int t = 0; t < TQ; ++t)
+          for (int c = 0; c < DP / 64 && job.steps_of(t) > 0; ++c)
+            tma_3d(q_at + t * kTile + c * kBlock, &q_map, c * 64, job.hk * g.group, job.token0 + t * job.tokens, q_full);
       }
       bool ok = true;
       for (int j = 0; j < job.steps && ok; ++j) {

@@ -282,6 +282,49 @@ def test_attention_large_finite_values_behind_the_mask_do_not_reach_a_row():
         check(got[~sees], want[~sees], bound[~sees])
 
 
+def widened(x, columns):
+    """The same inputs with a table that has room for far longer sequences: the library then expects long ones."""
+    q, k, v, table, start, lens = x
+    wide = torch.full((table.shape[0], columns), -1, dtype=torch.int32)
+    wide[:, : table.shape[1]] = table
+    return q, k, v, wide, start, lens
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("columns", [0, 1024])
+def test_attention_of_queries_before_the_first_cached_token_is_zero(D, columns):
+    """Blocks of queries that no key is there for, beside others: with 64 tokens to a query tile, 300 queries on nothing, 200 on 40
+    (the first tiles see nothing) and on 100 (of a pair of tiles only the second does)."""
+    qs, kvs = [300, 130, 200, 200], [0, 130, 40, 100]
+    x = inputs(qs, kvs, 4, 2, D, 16, seed=D)
+    want, bound = ref.attention(*x, 60, 3, D ** -0.5)
+    none = (want == 0).flatten(1).all(dim=1)
+    assert int(none.sum()) == 300 + 160 + 100
+    y = widened(x, columns) if columns else x
+    ap.reset_device_wait_timeouts()
+    first = run(y, max(qs), 60, 3, D ** -0.5)
+    for _ in range(5):
+        got = run(y, max(qs), 60, 3, D ** -0.5)
+        check(got, want, bound)
+        assert not got.cpu()[none].any()
+        assert torch.equal(got, first)
+    assert ap.device_wait_timeouts() == 0
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_attention_cut_over_a_cluster_keeps_a_bad_query_to_its_row(D, bad):
+    """Short sequences under a wide table: CTAs of the cluster that have no key to walk.  One query is NaN or infinite."""
+    qs, kvs = [70, 20, 5], [90, 20, 0]
+    x = list(inputs(qs, kvs, 4, 2, D, 16, seed=D + 1))
+    want, bound = ref.attention(*x, 0, 0, D ** -0.5)
+    x[0][33, 1] = bad
+    got = run(widened(x, 1024), max(qs), 0, 0, D ** -0.5).double().cpu()
+    assert torch.isnan(got[33, 1]).all()
+    got[33, 1], want[33, 1], bound[33, 1] = 0, 0, 1
+    check(got, want, bound)
+
+
 def test_attention_refuses_what_the_library_cannot_take():
     q, k, v, table, start, lens = [t.cuda() for t in inputs([1], [20], 4, 2, 64, 16)]
     for bad in (dict(q=q.float()), dict(k=k.float()), dict(v=v[:-1]), dict(table=table.long()), dict(start=start[:1]), dict(lens=lens.float()), dict(q=q.cpu()),
