@@ -58,6 +58,13 @@ constexpr int kStages = 5;
 // Rings of one entry per tile of keys.  The copies go in order through kStages places, so that the values of tile j + 4, or
 // the keys of tile j + 8, are asked for only after those of tile j have been used and given back.
 constexpr int kCleans = 4, kMasks = 8;
+// The ring's entries are keys and values in turn: entry 2j the keys of tile j, 2j + 1 its values, entry i in place i % kStages.  A
+// place thus holds both kinds in turn, but the warps that look through the values, or form S, wait for one kind only.  A wait by
+// parity tells two phases apart, no more: on a barrier that both kinds used, such a warp could take the entry before the last for
+// the last while the one between, which it never asks for, is still on its way.  So a place has two barriers for what has landed,
+// taken in turn, one for each kind (entry i: i % kFulls), and who waits on one has waited for each of its phases.
+constexpr int kFulls = 2 * kStages;
+static_assert(kStages % 2 == 1 && kFulls % 2 == 0, "a barrier is used by one kind of entry");
 // alignment, barriers and flags, what the threads of a row exchange, queries, ring
 constexpr int smem_bytes(int dp) { return 1024 + 1024 + tiles_of(dp) * kRows * 4 + (tiles_of(dp) + kStages) * tile_bytes(dp); }
 
@@ -221,9 +228,11 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(base + 516);
   volatile int* poison = reinterpret_cast<volatile int*>(base + 520);
   volatile uint32_t* pages_there = reinterpret_cast<volatile uint32_t*>(base + 576);  // [kMasks]: of tile j at j % kMasks, a bit per page
-  const uint32_t full = smem_addr(bars), empty = full + 8 * kStages, clean = empty + 8 * kStages, q_full = clean + 8 * kCleans, s_ready = q_full + 8,
+  const uint32_t full = smem_addr(bars), empty = full + 8 * kFulls, clean = empty + 8 * kStages, q_full = clean + 8 * kCleans, s_ready = q_full + 8,
                  s_free = s_ready + 16, p_ready = s_free + 8, pv_done = p_ready + 32;
   const uint32_t q_at = smem_addr(base + 1024), ring = q_at + TQ * kTile;
+  auto landed = [&](int i) { return full + 8 * (i % kFulls); };
+  auto landed_parity = [](int i) { return (uint32_t)(i / kFulls) & 1; };
   float* exchange = reinterpret_cast<float*>(base + 1024 + (TQ + kStages) * kTile);  // [tile][row]
   // (a cluster, at the end, over queries and ring) O of this CTA's part [tile][row][DP], maximum and sum [tile][row]
   float4* part_rows = reinterpret_cast<float4*>(base + 1024);
@@ -234,7 +243,8 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
   unsigned int* count = &g_attention_tile_wait_timeouts;
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kStages; ++s) bar_init(full + 8 * s, 1), bar_init(empty + 8 * s, 1);
+    for (int s = 0; s < kFulls; ++s) bar_init(full + 8 * s, 1);
+    for (int s = 0; s < kStages; ++s) bar_init(empty + 8 * s, 1);
     for (int s = 0; s < kCleans; ++s) bar_init(clean + 8 * s, 1);
     bar_init(q_full, 1);
     bar_init(s_free, 8);
@@ -486,21 +496,21 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
           if (turn > 0 && !(ok = warp_wait(empty + 8 * s, (turn - 1) & 1, abort, count))) break;
           if (lane == 0) {
             if (v == 0) pages_there[j % kMasks] = mask;
-            bar_expect(full + 8 * s, kTile);
+            bar_expect(landed(i), kTile);
           }
           __syncwarp();
           if (lane < per_tile)
             for (int c = 0; c < DP / 64; ++c)
-              tma_4d(ring + s * kTile + c * kBlock + lane * rows * 128, v ? &v_map : &k_map, c * 64, row, job.hk, page, full + 8 * s);
+              tma_4d(ring + s * kTile + c * kBlock + lane * rows * 128, v ? &v_map : &k_map, c * 64, row, job.hk, page, landed(i));
         }
       }
     } else if (warp == kScoreWarp) {
       // ---- S (one tile) ----
       if (TQ == 1 && job.steps > 0 && warp_wait(q_full, 0, abort, count)) {
         for (int j = 0; j < job.steps; ++j) {
-          const int i = 2 * j, turn = i / kStages, stage = i - turn * kStages;
+          const int i = 2 * j, stage = i % kStages;
           const uint64_t ks = desc_k_major(ring + stage * kTile);
-          if (!warp_wait(full + 8 * stage, turn & 1, abort, count)) break;
+          if (!warp_wait(landed(i), landed_parity(i), abort, count)) break;
           if (j > 0 && !warp_wait(s_free, (j - 1) & 1, abort, count)) break;  // the last S is in registers
           tmem_fence_after();
           if (elect_one()) {
@@ -519,7 +529,7 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
       bool ok = items > 0;
       int keys_in = 1;
       if (TQ == 2 && ok) {
-        ok = warp_wait(q_full, 0, abort, count) && warp_wait(full, 0, abort, count);
+        ok = warp_wait(q_full, 0, abort, count) && warp_wait(landed(0), landed_parity(0), abort, count);
         if (ok && elect_one()) {
 #pragma unroll
           for (int t = 0; t < TQ; ++t)
@@ -533,11 +543,13 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
       }
       for (int n = 0; n < items && ok; ++n) {
         const Item x = item_at<TQ>(job, n);
-        const int stage = (2 * x.j + 1) % kStages, next_key = (2 * x.j + 2) % kStages;
+        const int value = 2 * x.j + 1, stage = value % kStages, next_key = (value + 1) % kStages;
         const bool more = x.j + 1 < job.steps_of(x.t);
-        if (x.first && !(ok = warp_wait(clean + 8 * (x.j % kCleans), (x.j / kCleans) & 1, abort, count))) break;
+        if (x.first && !(ok = warp_wait(landed(value), landed_parity(value), abort, count) &&
+                              warp_wait(clean + 8 * (x.j % kCleans), (x.j / kCleans) & 1, abort, count)))
+          break;
         if (TQ == 2 && more && keys_in == x.j + 1) {
-          if (!(ok = warp_wait(full + 8 * next_key, ((2 * x.j + 2) / kStages) & 1, abort, count))) break;
+          if (!(ok = warp_wait(landed(value + 1), landed_parity(value + 1), abort, count))) break;
           ++keys_in;
         }
         const uint64_t vs = desc_mn_major(ring + stage * kTile, kBlock);
@@ -568,7 +580,7 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
       bool ok = true;
       for (int j = 0; j < job.steps && ok; ++j) {
         const int i = 2 * j + 1, s = i % kStages;
-        if (!(ok = warp_wait(full + 8 * s, (i / kStages) & 1, abort, count))) break;
+        if (!(ok = warp_wait(landed(i), landed_parity(i), abort, count))) break;
         const bool part = job.part(j, TQ);
         if (part) {
           uint4* v = reinterpret_cast<uint4*>(base + 1024 + (TQ + s) * kTile);

@@ -16,6 +16,7 @@ def constant(name):
 
 
 STAGES, CLEANS, MASKS = constant("kStages"), constant("kCleans"), constant("kMasks")
+FULLS = int(re.search(r"\bkFulls = (\d+) \* kStages\b", SOURCE).group(1)) * STAGES
 
 
 class Unsound(Exception):
@@ -70,12 +71,12 @@ class Cta:
     """One CTA of `tiles` query tiles that take part in `steps` of the key tiles; the two warps of one quarter of the rows stand
     for all softmax warps of a tile."""
 
-    def __init__(self, rng, steps, queries="steps", rows=None, cluster=False):
+    def __init__(self, rng, steps, queries="steps", rows=None, cluster=False, fulls=FULLS):
         self.rng, self.steps_of, self.TQ, self.cluster = rng, steps, len(steps), cluster
         self.steps = max(steps)
         self.rows = rows or [True] * self.TQ  # tiles that have rows at all
         self.queries = queries
-        self.full, self.empty = [Bar(1) for _ in range(STAGES)], [Bar(1) for _ in range(STAGES)]
+        self.full, self.empty = [Bar(1) for _ in range(fulls)], [Bar(1) for _ in range(STAGES)]
         self.clean, self.q_full, self.s_free = [Bar(1) for _ in range(CLEANS)], Bar(1), Bar(2)
         self.s_ready = [Bar(1) for _ in steps]
         self.p_ready = [[Bar(1), Bar(1)] for _ in steps]
@@ -92,7 +93,7 @@ class Cta:
 
     # entry i = 2 j (keys of tile j) or 2 j + 1 (values)
     def full_of(self, i):
-        return self.full[i % STAGES], (i // STAGES) & 1
+        return self.full[i % len(self.full)], (i // len(self.full)) & 1
 
     def here(self, i):
         return self.place[i % STAGES] == (i, True)
@@ -195,6 +196,7 @@ class Cta:
                 t, j, first, last = (1 if self.steps_of[1] > 0 else 0), n - both, True, True
             more = j + 1 < self.steps_of[t]
             if first:
+                yield self.full_of(2 * j + 1)
                 yield self.clean[j % CLEANS], (j // CLEANS) & 1
             if self.TQ == 2 and more and keys_in == j + 1:
                 yield self.full_of(2 * j + 2)
@@ -296,6 +298,7 @@ def trial(steps, rows, cluster, order, seed, **variant):
 def test_every_access_waits_for_what_it_needs(steps, rows, cluster):
     for seed in range(60):
         trial(steps, rows, cluster, "in turn", seed)
+        trial(steps, rows, cluster, "any", seed)
 
 
 def finds(what, **variant):
@@ -316,3 +319,9 @@ def test_queries_of_tiles_without_steps_must_not_be_asked_for():
     # the copies' byte count and their loop go by the tiles' steps
     assert "((job.steps0 > 0) + (job.steps1 > 0)) * (DP / 64) * g.group * job.tokens * 128" in SOURCE
     assert "job.steps_of(t) > 0; ++c)" in SOURCE
+
+
+def test_keys_and_values_must_not_land_on_one_barrier():
+    # (the copies of one CTA may land in any order)
+    assert finds("values are looked through before they have landed", fulls=STAGES, order="any")
+    assert SOURCE.count("landed(i), landed_parity(i)") == 2 and "landed(value), landed_parity(value)" in SOURCE and "full + 8 * s," not in SOURCE.replace("bar_init(full + 8 * s, 1)", "")
