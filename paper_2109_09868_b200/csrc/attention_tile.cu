@@ -311,9 +311,10 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
     if (flip) full_to = 0;
     const int steps = job.steps_of(t);
     float m = mine ? -CUDART_INF_F : 0.f, l = 0.f;  // (rows that are not there never ask for another maximum)
-    bool ok = true;
+    // After a wait that gave up the warp goes on through its steps (its next waits end soon, and what it forms is not written): the
+    // other warp of its rows may be on its way to a meeting of the two, and those have no limit of their own.
     for (int j = 0; j < steps; ++j) {
-      if (!(ok = warp_wait(s_ready + 8 * t, j & 1, abort, count))) break;
+      warp_wait(s_ready + 8 * t, j & 1, abort, count);
       tmem_fence_after();
       const uint32_t there = pages_there[j % kMasks];
       float s[kMine];
@@ -348,7 +349,7 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
         for (int k = 0; k < 4; ++k) top[k] = max3(top[k], s[i + 2 * k], s[i + 2 * k + 1]);
       top[0] = fmaxf(max3(top[0], top[1], top[2]), top[3]);
       // the last P has been used, O is whole (two tiles: so S says already, which follows them on the tensor cores)
-      if (TQ == 1 && j > 0 && !(ok = warp_wait(pv_done, (j - 1) & 1, abort, count))) break;
+      if (TQ == 1 && j > 0) warp_wait(pv_done, (j - 1) & 1, abort, count);
       tmem_fence_after();
       // (the vote also keeps P from being written before both warps have read the scores that it may lie over)
       if (any_of_both(meet, mine && (m == -CUDART_INF_F || (top[0] - m) * scale > kGrowth))) {
@@ -397,13 +398,13 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
       unpack2(add2(sum2[0], sum2[1]), u, v);
       l += u + v;
     }
-    if (ok && steps > 0) {
+    if (steps > 0) {
       l = of_both(l, [](float x, float y) { return x + y; });
-      ok = warp_wait(pv_done + 8 * t, TQ == 1 ? (steps - 1) & 1 : 0, abort, count);
+      warp_wait(pv_done + 8 * t, TQ == 1 ? (steps - 1) & 1 : 0, abort, count);
       tmem_fence_after();
     }
     if constexpr (CLUSTER) softmax_warps_meet<TQ>();  // no product reads shared memory any more, of either tile
-    if (ok) {
+    if (__all_sync(0xffffffffu, *abort == 0)) {
       // One CTA: O / sum, by way of the tile's queries' place in shared memory (a warp keeps to its own rows and columns) into
       // whole rows.  A cluster: O as it is into shared memory, with the row's maximum and sum.
       const float inv = CLUSTER ? 1.f : l == 0.f ? 0.f : 1.f / l;

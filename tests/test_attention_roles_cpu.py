@@ -1,6 +1,6 @@
 """The prompt attention's warp roles (csrc/attention_tile.cu) as a model on the host: barriers with phases, copies and products
-that land later, warps that run in any order.  The model checks, at every access, that what is read has landed and what is
-written over has been used, and that a CTA ends with no copy in flight.  Each design that was found unsound is a variant of the
+that land later or never, warps that run in any order.  The model checks, at every access, that what is read has landed and what is
+written over has been used, that a CTA ends with no copy in flight, and that it ends at all when a copy never lands.  Each design that was found unsound is a variant of the
 model that has to fail, which shows that the model would see it."""
 import os
 import random
@@ -71,11 +71,13 @@ class Cta:
     """One CTA of `tiles` query tiles that take part in `steps` of the key tiles; the two warps of one quarter of the rows stand
     for all softmax warps of a tile."""
 
-    def __init__(self, rng, steps, queries="steps", rows=None, cluster=False, fulls=FULLS):
+    def __init__(self, rng, steps, queries="steps", rows=None, cluster=False, fulls=FULLS, lost=None, softmax="goes on"):
         self.rng, self.steps_of, self.TQ, self.cluster = rng, steps, len(steps), cluster
         self.steps = max(steps)
         self.rows = rows or [True] * self.TQ  # tiles that have rows at all
-        self.queries = queries
+        self.queries, self.softmax = queries, softmax
+        self.lost = lost         # the copy that never lands: an entry of the ring, or "queries"
+        self.gave_up = False     # a wait has run out: the CTA's flag; from then on nothing that is read or written counts
         self.full, self.empty = [Bar(1) for _ in range(fulls)], [Bar(1) for _ in range(STAGES)]
         self.clean, self.q_full, self.s_free = [Bar(1) for _ in range(CLEANS)], Bar(1), Bar(2)
         self.s_ready = [Bar(1) for _ in steps]
@@ -95,13 +97,16 @@ class Cta:
     def full_of(self, i):
         return self.full[i % len(self.full)], (i // len(self.full)) & 1
 
+    def need(self, ok, what):
+        need(ok or self.gave_up, what)
+
     def here(self, i):
         return self.place[i % STAGES] == (i, True)
 
     def copy_in(self, i):
         at, bar = i % STAGES, self.full_of(i)[0]
         if self.place[at] is not None:
-            need(self.place[at][1] and self.place[at][0] in self.used, "entry %d is copied over what is still needed" % i)
+            self.need(self.place[at][1] and self.place[at][0] in self.used, "entry %d is copied over what is still needed" % i)
         self.place[at] = (i, False)
 
         def landed():
@@ -109,7 +114,8 @@ class Cta:
             bar.land(1)
 
         bar.arrive(expect=1)
-        self.flying.append(landed)
+        if i != self.lost:
+            self.flying.append(landed)
 
     # ---- roles: what they yield they wait for ----
     def copies(self):
@@ -126,11 +132,13 @@ class Cta:
                 self.q[t] = "here"
                 self.q_full.land(1)
 
-            self.flying.append(landed)
+            if self.lost != "queries":
+                self.flying.append(landed)
             yield
         for i in range(2 * self.steps):
             if i >= STAGES:
-                yield self.empty[i % STAGES], (i // STAGES - 1) & 1
+                if not (yield self.empty[i % STAGES], (i // STAGES - 1) & 1):
+                    return
             if i % 2 == 0:
                 self.masks[i // 2 % MASKS] = i // 2
             self.copy_in(i)
@@ -138,20 +146,20 @@ class Cta:
 
     def scores(self, t, j):  # the product S, when it runs
         def run():
-            need(self.q[t] == "here", "S of queries that have not landed")
-            need(self.here(2 * j), "S of keys that have not landed")
-            need(j == 0 or min(self.read[t]) == j - 1, "S over scores that have not been read")
+            self.need(self.q[t] == "here", "S of queries that have not landed")
+            self.need(self.here(2 * j), "S of keys that have not landed")
+            self.need(j == 0 or min(self.read[t]) == j - 1, "S over scores that have not been read")
             if self.TQ == 2:
-                need(j == 0 or self.o[t] == j - 1, "S over weights that have not been used")
+                self.need(j == 0 or self.o[t] == j - 1, "S over weights that have not been used")
             self.s[t] = j
 
         return run
 
     def values(self, t, j, half):
         def run():
-            need(self.here(2 * j + 1), "O of values that have not landed")
-            need(j in self.cleaned, "O of values that have not been looked through")
-            need(self.p[t][half] == j, "O of other weights")
+            self.need(self.here(2 * j + 1), "O of values that have not landed")
+            self.need(j in self.cleaned, "O of values that have not been looked through")
+            self.need(self.p[t][half] == j, "O of other weights")
             if half == 1:
                 self.o[t] = j
 
@@ -167,11 +175,13 @@ class Cta:
     def score_warp(self):
         if self.TQ != 1 or self.steps == 0:
             return
-        yield self.q_full, 0
+        if not (yield self.q_full, 0):
+            return
         for j in range(self.steps):
-            yield self.full_of(2 * j)
-            if j > 0:
-                yield self.s_free, (j - 1) & 1
+            if not (yield self.full_of(2 * j)):
+                return
+            if j > 0 and not (yield self.s_free, (j - 1) & 1):
+                return
             self.queues["score"] += [self.scores(0, j), self.s_ready[0].arrive, self.give_back(2 * j)]
 
     def out_warp(self):
@@ -180,8 +190,8 @@ class Cta:
             return
         keys_in = 1
         if self.TQ == 2:
-            yield self.q_full, 0
-            yield self.full_of(0)
+            if not (yield self.q_full, 0) or not (yield self.full_of(0)):
+                return
             for t in range(2):
                 if self.steps_of[t] > 0:
                     queue += [self.scores(t, 0), self.s_ready[t].arrive]
@@ -196,13 +206,15 @@ class Cta:
                 t, j, first, last = (1 if self.steps_of[1] > 0 else 0), n - both, True, True
             more = j + 1 < self.steps_of[t]
             if first:
-                yield self.full_of(2 * j + 1)
-                yield self.clean[j % CLEANS], (j // CLEANS) & 1
+                if not (yield self.full_of(2 * j + 1)) or not (yield self.clean[j % CLEANS], (j // CLEANS) & 1):
+                    return
             if self.TQ == 2 and more and keys_in == j + 1:
-                yield self.full_of(2 * j + 2)
+                if not (yield self.full_of(2 * j + 2)):
+                    return
                 keys_in += 1
             for half in range(2):
-                yield self.p_ready[t][half], j & 1
+                if not (yield self.p_ready[t][half], j & 1):
+                    return
                 queue.append(self.values(t, j, half))
             if self.TQ == 1 or not more:
                 queue.append(self.pv_done[t].arrive)
@@ -215,10 +227,11 @@ class Cta:
 
     def clean_warp(self):
         for j in range(self.steps):
-            yield self.full_of(2 * j + 1)
-            need(self.here(2 * j + 1), "values are looked through before they have landed")
+            if not (yield self.full_of(2 * j + 1)):
+                return
+            self.need(self.here(2 * j + 1), "values are looked through before they have landed")
             yield
-            need(self.here(2 * j + 1), "values are looked through before they have landed")
+            self.need(self.here(2 * j + 1), "values are looked through before they have landed")
             self.cleaned.add(j)
             self.clean[j % CLEANS].arrive()
 
@@ -226,37 +239,42 @@ class Cta:
         def together(want=False):
             return self.meet[t].come(want), self.meet[t]
 
+        ok = True
         for j in range(self.steps_of[t]):
-            yield self.s_ready[t], j & 1
-            need(self.s[t] == j, "scores are read before they are there")
-            need(self.masks[j % MASKS] == j, "the pages of another tile of keys")
+            ok = yield self.s_ready[t], j & 1
+            if not ok and self.softmax == "leaves":
+                break
+            self.need(self.s[t] == j, "scores are read before they are there")
+            self.need(self.masks.get(j % MASKS) == j, "the pages of another tile of keys")
             self.read[t][half] = j
             if self.TQ == 1:
                 self.s_free.arrive()
                 if j > 0:
-                    yield self.pv_done[0], (j - 1) & 1
+                    ok = yield self.pv_done[0], (j - 1) & 1
+                    if not ok and self.softmax == "leaves":
+                        break
             turn, meeting = together(self.rng.random() < 0.3)
             yield meeting, turn
             if meeting.said[turn]:
                 for _ in range(2):
                     yield tuple(reversed(together()))
-                need(self.o[t] == j - 1, "O is scaled while products are added to it")
+                self.need(self.o[t] == j - 1, "O is scaled while products are added to it")
                 yield tuple(reversed(together()))
-            need(self.o[t] == j - 1, "weights are written over those in use")
+            self.need(self.o[t] == j - 1, "weights are written over those in use")
             if self.TQ == 2:
-                need(min(self.read[t]) == j, "weights are written over scores that have not been read")
+                self.need(min(self.read[t]) == j, "weights are written over scores that have not been read")
             self.p[t][half] = j
             self.p_ready[t][half].arrive()
-        if self.steps_of[t] > 0:
+        if self.steps_of[t] > 0 and (ok or self.softmax == "goes on"):
             for _ in range(2):
                 yield tuple(reversed(together()))
             yield self.pv_done[t], (self.steps_of[t] - 1) & 1 if self.TQ == 1 else 0
-            need(self.o[t] == self.steps_of[t] - 1, "O is read before it is whole")
+            self.need(self.o[t] == self.steps_of[t] - 1, "O is read before it is whole")
         if self.cluster:
             turn = self.all_meet.come()
             yield self.all_meet, turn
         for u in range(self.TQ) if self.cluster else [t]:  # the output is staged where the queries were (a cluster: over all)
-            need(self.q[u] != "flying", "the output is staged where queries still land")
+            self.need(self.q[u] != "flying", "the output is staged where queries still land")
 
     def run(self, order):
         roles = [self.copies(), self.score_warp(), self.out_warp(), self.clean_warp()] + [self.softmax_warp(t, h) for t in range(self.TQ) for h in range(2)]
@@ -265,23 +283,32 @@ class Cta:
         def ready(w):
             return w is None or (w[0].over(w[1]) if isinstance(w[0], Bar) else w[1] in w[0].said)
 
+        def step(r, ok):
+            try:
+                waits[r] = next(r) if waits[r] is None else r.send(ok)
+            except StopIteration:
+                del waits[r]
+
         while waits:
             can = [("role", r) for r, w in waits.items() if ready(w)]
             can += [("queue", q) for q in self.queues.values() if q]
             can += [("land", n) for n in range(len(self.flying) if order == "any" else min(1, len(self.flying)))]
+            late = [r for r, w in waits.items() if w is not None and isinstance(w[0], Bar) and not ready(w)]
+            # a wait runs out: where nothing else happens, now and then before; once one has, the others may soon
+            if late and (not can or self.rng.random() < (0.2 if self.gave_up else 0.01 if self.lost is not None else 0)):
+                self.gave_up = True
+                step(late[self.rng.randrange(len(late))], False)
+                continue
             need(can, "everything waits")
             # copies are slow or fast against the rest, by the draw
             kind, x = can[self.rng.randrange(len(can))] if self.rng.random() < 0.7 else can[0]
             if kind == "role":
-                try:
-                    waits[x] = next(x)
-                except StopIteration:
-                    del waits[x]
+                step(x, True)
             elif kind == "queue":
                 x.pop(0)()
             else:
                 self.flying.pop(x)()
-        need(not self.flying, "the CTA ends with a copy in flight")
+        self.need(not self.flying, "the CTA ends with a copy in flight")
 
 
 JOBS = [([n], [True]) for n in (0, 1, 2, 3, 5, 8, 13)] + [
@@ -299,6 +326,14 @@ def test_every_access_waits_for_what_it_needs(steps, rows, cluster):
     for seed in range(60):
         trial(steps, rows, cluster, "in turn", seed)
         trial(steps, rows, cluster, "any", seed)
+
+
+@pytest.mark.parametrize("steps,rows", JOBS)
+def test_a_copy_that_never_lands_ends_the_kernel(steps, rows):
+    for seed in range(60):
+        lost = random.Random(seed).choice(["queries"] + list(range(2 * max(steps))))
+        for cluster in (False, True):
+            trial(steps, rows, cluster, "any", seed, lost=lost)
 
 
 def finds(what, **variant):
@@ -325,3 +360,9 @@ def test_keys_and_values_must_not_land_on_one_barrier():
     # (the copies of one CTA may land in any order)
     assert finds("values are looked through before they have landed", fulls=STAGES, order="any")
     assert SOURCE.count("landed(i), landed_parity(i)") == 2 and "landed(value), landed_parity(value)" in SOURCE and "full + 8 * s," not in SOURCE.replace("bar_init(full + 8 * s, 1)", "")
+
+
+def test_a_softmax_warp_must_not_leave_the_warp_it_meets():
+    assert finds("everything waits", softmax="leaves", lost=4, order="any")
+    softmax = SOURCE[SOURCE.index("---- softmax and output"): SOURCE.index("---- copies ----")]
+    assert softmax.count("warp_wait(") == 3 and "break;" not in softmax and "__all_sync(0xffffffffu, *abort == 0)" in softmax
