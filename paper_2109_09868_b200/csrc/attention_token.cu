@@ -99,12 +99,16 @@ __device__ __forceinline__ Seen seen_by(const approxifer_attention_args& a, int 
   return s;
 }
 
-// Where the keys of a chunk lie.  WHOLE (pages of whole chunks): the chunk's page and first row, the same in all lanes.
-// Else: those of this lane's key (lane % keys).
+// Where the keys of a chunk lie.  WHOLE (pages of whole chunks): the chunk's page and first row, the same in all lanes, and which
+// keys are there (none: page 0, never read).  Else: those of this lane's key (lane % keys), page -1 where it is not there.
 struct Spot {
   int32_t page, row;
   uint32_t sees;
 };
+template <bool WHOLE>
+__device__ __forceinline__ Spot nowhere() {
+  return Spot{WHOLE ? 0 : -1, 0, 0};
+}
 
 // One warp's share of a unit.
 template <int DP, bool WHOLE>
@@ -142,7 +146,7 @@ struct Warp {
   }
 
   __device__ __forceinline__ Spot look_up(const approxifer_attention_args& a, int page_shift, const Seen& s, int c) const {
-    Spot at{0, 0, 0};
+    Spot at = nowhere<WHOLE>();
     if (c >= s.chunks) return at;
     const int32_t pos = s.position(c, kKeys);
     at.sees = s.sees(pos, kKeys);
@@ -153,7 +157,6 @@ struct Warp {
     } else {
       const uint32_t j = (uint32_t)pos + lane % kKeys, entry = j / (uint32_t)a.page_size;
       at.row = (int32_t)(j - entry * (uint32_t)a.page_size);
-      at.page = -1;
       if ((at.sees >> (lane % kKeys)) & 1) at.page = __ldg(s.table + entry);
       if (at.page >= a.num_pages) at.page = -1;
     }
@@ -474,7 +477,7 @@ __global__ void __launch_bounds__(kThreads, 3) attention_token_balanced_kernel(c
       hk = get.unit / row_tiles;
       if (to_get > 0) get.next(a, units, keys_of(DP));
     } else {
-      ahead = Spot{WHOLE ? 0 : -1, 0, 0};
+      ahead = nowhere<WHOLE>();
     }
   };
 #pragma unroll

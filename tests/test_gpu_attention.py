@@ -5,6 +5,7 @@ import torch
 
 import hosted_reference as ref
 import paper_2109_09868_b200 as ap
+from test_hosted_cpu import ATTENTION
 
 pytestmark = pytest.mark.gpu
 
@@ -323,6 +324,30 @@ def test_attention_cut_over_a_cluster_keeps_a_bad_query_to_its_row(D, bad):
     assert torch.isnan(got[33, 1]).all()
     got[33, 1], want[33, 1], bound[33, 1] = 0, 0, 1
     check(got, want, bound)
+
+
+@pytest.mark.parametrize("D", [64, 72, 128])
+def test_attention_single_tokens_shorter_than_the_copies_ahead(D):
+    """Pages that are no power of two, sequences of no token and of less than a chunk for every warp: the copies that run ahead
+    find nothing.  The table names few pages and has room for many, so that a cluster shares a sequence."""
+    kvs = [0, 1, 2, 15, 16, 33, 70]
+    x = inputs([1] * len(kvs), kvs, 4, 2, D, 24, seed=D + 2)
+    want, bound = ref.attention(*x, 0, 0, D ** -0.5)
+    check(run(x, 1, 0, 0, D ** -0.5), want, bound)
+    check(run(widened(x, 40), 1, 0, 0, D ** -0.5), want, bound)
+
+
+@pytest.mark.parametrize("page", [16, 24])
+def test_attention_over_a_cache_of_no_pages_is_zero(page):
+    """No page is valid: whatever the table says, nothing is there (the pointer still names memory, full of NaN)."""
+    q, k, v, table, start, lens = [t.cuda() for t in inputs([1, 1], [40, 3], 4, 2, 64, page, seed=1)]
+    k.fill_(float("nan"))
+    out = torch.full_like(q, 7.0)
+    T, Hq, D = q.shape
+    args = ATTENTION.pack(T, 2, 1, Hq, 2, D, page, 0, 0, 0.125, 0, q.data_ptr(), *q.stride()[:2], k.data_ptr(), *k.stride()[:3], k.data_ptr(), *k.stride()[:3], 0,
+                          table.data_ptr(), table.stride(0), table.shape[1], start.data_ptr(), lens.data_ptr(), out.data_ptr(), *out.stride()[:2], 0, 0)
+    assert ap.load().approxifer_attention(args, torch.cuda.current_stream().cuda_stream) == 0
+    assert not out.any()
 
 
 def test_attention_refuses_what_the_library_cannot_take():
