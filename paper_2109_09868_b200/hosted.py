@@ -4,6 +4,11 @@ The calls go through ``_hosted`` (``csrc/hosted_binding.cpp``), which marshals t
 ``include/approxifer.h`` and calls the C entry point of the same name: in C++, because a single-token call is short enough
 for marshalling in Python to cost more than the call.  There is no fallback: a missing library, a CPU tensor or a layout the
 library cannot take raises.
+
+``stream``: the stream that the work is enqueued on (None: the current one).  As everywhere in CUDA it is the caller who makes it
+wait for what the inputs come from, and who waits for it before the outputs are used elsewhere.  An output that is not given is
+allocated on that stream, so its memory is free there, and kept for the current stream too.  The operators serve: they compute no
+gradients, and their outputs have none, whatever the inputs ask for.
 """
 from __future__ import annotations
 
@@ -36,10 +41,15 @@ def _load():
     return module
 
 
-def _ordered(out: torch.Tensor, given, stream) -> torch.Tensor:
-    """Tells the allocator where a new output is written, if that is not the current stream."""
-    if given is None:
-        out.record_stream(stream)
+def _on(stream, call, given, *args) -> torch.Tensor:
+    """``call`` on a stream that need not be the current one.  A new output is taken from that stream's memory: a block of the
+    current stream's may still be in use there by work that `stream` does not wait for."""
+    if given is not None:
+        return call(*args, int(stream.cuda_stream))
+    user = torch.cuda.current_stream()
+    with torch.cuda.stream(stream):
+        out = call(*args, int(stream.cuda_stream))
+    out.record_stream(user)  # (it is used there: its memory goes back to `stream` only after that)
     return out
 
 
@@ -51,9 +61,10 @@ def approxifer_linear(X: torch.Tensor, weight: torch.Tensor, bias: Optional[torc
     act = ACTIVATIONS.get(activation)
     if act is None:
         raise ValueError("activation must be one of %s" % sorted(ACTIVATIONS))
+    args = (X, weight, bias, act, residual, out_dtype, Y)
     if stream is None:
-        return (_native or _load()).linear(X, weight, bias, act, residual, out_dtype, Y, None)
-    return _ordered((_native or _load()).linear(X, weight, bias, act, residual, out_dtype, Y, int(stream.cuda_stream)), Y, stream)
+        return (_native or _load()).linear(*args, None)
+    return _on(stream, (_native or _load()).linear, Y, *args)
 
 
 def approxifer_qk_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor], v: Optional[torch.Tensor], q_weight: Optional[torch.Tensor],
@@ -67,7 +78,7 @@ def approxifer_qk_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor], v: Optio
     args = (q, k, v, q_weight, k_weight, cos_sin, positions, k_cache, v_cache, slots, q_out, eps, interleaved, status)
     if stream is None:
         return (_native or _load()).norm_rope(*args, None)
-    return _ordered((_native or _load()).norm_rope(*args, int(stream.cuda_stream)), q_out, stream)
+    return _on(stream, (_native or _load()).norm_rope, q_out, *args)
 
 
 def approxifer_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, block_table: torch.Tensor, q_start: torch.Tensor,
@@ -81,4 +92,4 @@ def approxifer_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.
     args = (q, k_cache, v_cache, block_table, q_start, kv_len, max_q, window, sinks, scale, out, workspace)
     if stream is None:
         return (_native or _load()).attention(*args, None)
-    return _ordered((_native or _load()).attention(*args, int(stream.cuda_stream)), out, stream)
+    return _on(stream, (_native or _load()).attention, out, *args)

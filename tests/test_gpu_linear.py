@@ -118,6 +118,24 @@ def test_linear_is_repeatable_and_runs_on_a_stream_and_in_a_graph():
     assert torch.equal(out, first)
 
 
+def test_linear_on_another_stream_leaves_memory_alone_that_the_current_one_still_reads():
+    x, w = normal((512, 512), 1).cuda(), normal((1024, 512), 2, std=0.05).cuda()
+    s = torch.cuda.Stream()
+    want = ap.approxifer_linear(x, w)
+    torch.cuda.synchronize()
+    for _ in range(5):
+        held = torch.full((512, 1024), 3.0, dtype=torch.bfloat16, device="cuda")
+        copy = torch.empty_like(held)
+        s.wait_stream(torch.cuda.current_stream())
+        torch.cuda._sleep(20_000_000)  # (some 10 ms)
+        copy.copy_(held)               # still to come when the block is given back ...
+        del held
+        y = ap.approxifer_linear(x, w, stream=s)  # ... and an output of the same size is asked for
+        s.synchronize()
+        torch.cuda.synchronize()
+        assert bool((copy == 3.0).all()) and torch.equal(y, want)
+
+
 def test_linear_of_no_rows():
     assert ap.approxifer_linear(torch.empty((0, 64), dtype=torch.bfloat16, device="cuda"), torch.empty((5, 64), dtype=torch.bfloat16, device="cuda")).shape == (0, 5)
 

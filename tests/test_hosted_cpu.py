@@ -83,3 +83,48 @@ def test_binding_refuses_what_the_library_cannot_take():
     with pytest.raises(ValueError):
         ap.approxifer_attention(x.view(2, 1, 8), x.view(1, 1, 2, 8), x.view(1, 1, 2, 8), torch.zeros(1, 1, dtype=torch.int32),
                                 torch.zeros(2, dtype=torch.int32), torch.zeros(1, dtype=torch.int32), 2)
+
+
+def test_outputs_for_another_stream_come_from_that_streams_memory(monkeypatch):
+    """A block of the current stream's memory may be in use there by work that the other stream does not wait for."""
+    from paper_2109_09868_b200 import hosted
+
+    seen = []
+
+    class Stream:
+        cuda_stream = 77
+
+    class On:
+        def __init__(self, stream):
+            self.stream = stream
+
+        def __enter__(self):
+            seen.append(("on", self.stream))
+
+        def __exit__(self, *a):
+            seen.append("off")
+
+    class Out:
+        def record_stream(self, stream):
+            seen.append(("kept for", stream))
+
+    class Native:
+        def __getattr__(self, name):
+            return lambda *args: (seen.append((name, args[-1])), Out())[1]
+
+    monkeypatch.setattr(hosted, "_native", Native())
+    monkeypatch.setattr(torch.cuda, "stream", On)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: "user")
+    s = Stream()
+    calls = {"linear": lambda **k: ap.approxifer_linear(1, 2, **k), "norm_rope": lambda **k: ap.approxifer_qk_norm_rope(*range(10), **k),
+             "attention": lambda **k: ap.approxifer_attention(*range(7), **k)}
+    for name, call in calls.items():
+        del seen[:]
+        call(stream=s)
+        assert seen == [("on", s), (name, 77), "off", ("kept for", "user")]
+        del seen[:]
+        call(stream=s, **{{"linear": "Y", "norm_rope": "q_out", "attention": "out"}[name]: "given"})
+        assert seen == [(name, 77)]
+        del seen[:]
+        call()
+        assert seen == [(name, None)]
