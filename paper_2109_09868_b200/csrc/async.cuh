@@ -86,7 +86,6 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
 }
 // Bounded wait.  `abort`: the CTA's flag in shared memory; `count`: the translation unit's counter of waits that gave up.
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* abort, unsigned int* count) {
-  if (bar_try(bar, parity)) return true;
   for (uint32_t it = 0; it < kWaitLimit; ++it) {
     if (bar_try(bar, parity)) return true;
     if (*abort) return false;

@@ -62,9 +62,10 @@ constexpr int kCleans = 4, kMasks = 8;
 // place thus holds both kinds in turn, but the warps that look through the values, or form S, wait for one kind only.  A wait by
 // parity tells two phases apart, no more: on a barrier that both kinds used, such a warp could take the entry before the last for
 // the last while the one between, which it never asks for, is still on its way.  So a place has two barriers for what has landed,
-// taken in turn, one for each kind (entry i: i % kFulls), and who waits on one has waited for each of its phases.
+// one for each kind, and who waits on one has waited for each of its phases.  (The products with the values wait for the look
+// through them, which has waited for the values: a wait of their own for the values too cost 6 % of the windowed prompts.)
 constexpr int kFulls = 2 * kStages;
-static_assert(kStages % 2 == 1 && kFulls % 2 == 0, "a barrier is used by one kind of entry");
+static_assert(kStages % 2 == 1, "a place holds keys and values in turn");
 // alignment, barriers and flags, what the threads of a row exchange, queries, ring
 constexpr int smem_bytes(int dp) { return 1024 + 1024 + tiles_of(dp) * kRows * 4 + (tiles_of(dp) + kStages) * tile_bytes(dp); }
 
@@ -231,8 +232,8 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
   const uint32_t full = smem_addr(bars), empty = full + 8 * kFulls, clean = empty + 8 * kStages, q_full = clean + 8 * kCleans, s_ready = q_full + 8,
                  s_free = s_ready + 16, p_ready = s_free + 8, pv_done = p_ready + 32;
   const uint32_t q_at = smem_addr(base + 1024), ring = q_at + TQ * kTile;
-  auto landed = [&](int i) { return full + 8 * (i % kFulls); };
-  auto landed_parity = [](int i) { return (uint32_t)(i / kFulls) & 1; };
+  auto landed = [&](int i) { return full + 8 * (i % kStages + (i & 1) * kStages); };
+  auto landed_parity = [](int i) { return (uint32_t)(i / kStages >> 1) & 1; };  // (every second turn of a place is of the entry's kind)
   float* exchange = reinterpret_cast<float*>(base + 1024 + (TQ + kStages) * kTile);  // [tile][row]
   // (a cluster, at the end, over queries and ring) O of this CTA's part [tile][row][DP], maximum and sum [tile][row]
   float4* part_rows = reinterpret_cast<float4*>(base + 1024);
@@ -311,10 +312,10 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
     if (flip) full_to = 0;
     const int steps = job.steps_of(t);
     float m = mine ? -CUDART_INF_F : 0.f, l = 0.f;  // (rows that are not there never ask for another maximum)
-    // After a wait that gave up the warp goes on through its steps (its next waits end soon, and what it forms is not written): the
-    // other warp of its rows may be on its way to a meeting of the two, and those have no limit of their own.
-    for (int j = 0; j < steps; ++j) {
-      warp_wait(s_ready + 8 * t, j & 1, abort, count);
+    bool ok = true;
+    int j = 0;
+    for (; j < steps; ++j) {
+      if (!(ok = warp_wait(s_ready + 8 * t, j & 1, abort, count))) break;
       tmem_fence_after();
       const uint32_t there = pages_there[j % kMasks];
       float s[kMine];
@@ -349,7 +350,7 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
         for (int k = 0; k < 4; ++k) top[k] = max3(top[k], s[i + 2 * k], s[i + 2 * k + 1]);
       top[0] = fmaxf(max3(top[0], top[1], top[2]), top[3]);
       // the last P has been used, O is whole (two tiles: so S says already, which follows them on the tensor cores)
-      if (TQ == 1 && j > 0) warp_wait(pv_done, (j - 1) & 1, abort, count);
+      if (TQ == 1 && j > 0 && !(ok = warp_wait(pv_done, (j - 1) & 1, abort, count))) break;
       tmem_fence_after();
       // (the vote also keeps P from being written before both warps have read the scores that it may lie over)
       if (any_of_both(meet, mine && (m == -CUDART_INF_F || (top[0] - m) * scale > kGrowth))) {
@@ -398,13 +399,17 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
       unpack2(add2(sum2[0], sum2[1]), u, v);
       l += u + v;
     }
+    // After a wait that gave up the warp keeps the meetings of the steps that it leaves out: the other warp of its rows may be on
+    // its way to them, and they have no limit of their own.
+    for (; j < steps; ++j)
+      if (any_of_both(meet, false)) warps_meet(meet), warps_meet(meet), warps_meet(meet);
     if (steps > 0) {
       l = of_both(l, [](float x, float y) { return x + y; });
-      warp_wait(pv_done + 8 * t, TQ == 1 ? (steps - 1) & 1 : 0, abort, count);
+      if (ok) ok = warp_wait(pv_done + 8 * t, TQ == 1 ? (steps - 1) & 1 : 0, abort, count);
       tmem_fence_after();
     }
     if constexpr (CLUSTER) softmax_warps_meet<TQ>();  // no product reads shared memory any more, of either tile
-    if (__all_sync(0xffffffffu, *abort == 0)) {
+    if (ok) {
       // One CTA: O / sum, by way of the tile's queries' place in shared memory (a warp keeps to its own rows and columns) into
       // whole rows.  A cluster: O as it is into shared memory, with the row's maximum and sum.
       const float inv = CLUSTER ? 1.f : l == 0.f ? 0.f : 1.f / l;
@@ -546,9 +551,7 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
         const Item x = item_at<TQ>(job, n);
         const int value = 2 * x.j + 1, stage = value % kStages, next_key = (value + 1) % kStages;
         const bool more = x.j + 1 < job.steps_of(x.t);
-        if (x.first && !(ok = warp_wait(landed(value), landed_parity(value), abort, count) &&
-                              warp_wait(clean + 8 * (x.j % kCleans), (x.j / kCleans) & 1, abort, count)))
-          break;
+        if (x.first && !(ok = warp_wait(clean + 8 * (x.j % kCleans), (x.j / kCleans) & 1, abort, count))) break;  // landed, and looked through
         if (TQ == 2 && more && keys_in == x.j + 1) {
           if (!(ok = warp_wait(landed(value + 1), landed_parity(value + 1), abort, count))) break;
           ++keys_in;

@@ -71,7 +71,7 @@ class Cta:
     """One CTA of `tiles` query tiles that take part in `steps` of the key tiles; the two warps of one quarter of the rows stand
     for all softmax warps of a tile."""
 
-    def __init__(self, rng, steps, queries="steps", rows=None, cluster=False, fulls=FULLS, lost=None, softmax="goes on"):
+    def __init__(self, rng, steps, queries="steps", rows=None, cluster=False, fulls=FULLS, lost=None, softmax="keeps meetings"):
         self.rng, self.steps_of, self.TQ, self.cluster = rng, steps, len(steps), cluster
         self.steps = max(steps)
         self.rows = rows or [True] * self.TQ  # tiles that have rows at all
@@ -95,7 +95,9 @@ class Cta:
 
     # entry i = 2 j (keys of tile j) or 2 j + 1 (values)
     def full_of(self, i):
-        return self.full[i % len(self.full)], (i // len(self.full)) & 1
+        if len(self.full) == STAGES:  # one barrier to a place
+            return self.full[i % STAGES], (i // STAGES) & 1
+        return self.full[i % STAGES + (i & 1) * STAGES], (i // STAGES >> 1) & 1
 
     def need(self, ok, what):
         need(ok or self.gave_up, what)
@@ -206,7 +208,7 @@ class Cta:
                 t, j, first, last = (1 if self.steps_of[1] > 0 else 0), n - both, True, True
             more = j + 1 < self.steps_of[t]
             if first:
-                if not (yield self.full_of(2 * j + 1)) or not (yield self.clean[j % CLEANS], (j // CLEANS) & 1):
+                if not (yield self.clean[j % CLEANS], (j // CLEANS) & 1):
                     return
             if self.TQ == 2 and more and keys_in == j + 1:
                 if not (yield self.full_of(2 * j + 2)):
@@ -239,10 +241,11 @@ class Cta:
         def together(want=False):
             return self.meet[t].come(want), self.meet[t]
 
-        ok = True
+        ok, left = True, 0  # left: steps that a wait which gave up leaves out
         for j in range(self.steps_of[t]):
+            left = self.steps_of[t] - j
             ok = yield self.s_ready[t], j & 1
-            if not ok and self.softmax == "leaves":
+            if not ok:
                 break
             self.need(self.s[t] == j, "scores are read before they are there")
             self.need(self.masks.get(j % MASKS) == j, "the pages of another tile of keys")
@@ -251,7 +254,7 @@ class Cta:
                 self.s_free.arrive()
                 if j > 0:
                     ok = yield self.pv_done[0], (j - 1) & 1
-                    if not ok and self.softmax == "leaves":
+                    if not ok:
                         break
             turn, meeting = together(self.rng.random() < 0.3)
             yield meeting, turn
@@ -265,10 +268,16 @@ class Cta:
                 self.need(min(self.read[t]) == j, "weights are written over scores that have not been read")
             self.p[t][half] = j
             self.p_ready[t][half].arrive()
-        if self.steps_of[t] > 0 and (ok or self.softmax == "goes on"):
+        for _ in range(0 if ok or self.softmax == "leaves" else left):
+            turn, meeting = together()
+            yield meeting, turn
+            for _ in range(3 if meeting.said[turn] else 0):
+                yield tuple(reversed(together()))
+        if self.steps_of[t] > 0 and (ok or self.softmax != "leaves"):
             for _ in range(2):
                 yield tuple(reversed(together()))
-            yield self.pv_done[t], (self.steps_of[t] - 1) & 1 if self.TQ == 1 else 0
+            if ok:
+                ok = yield self.pv_done[t], (self.steps_of[t] - 1) & 1 if self.TQ == 1 else 0
             self.need(self.o[t] == self.steps_of[t] - 1, "O is read before it is whole")
         if self.cluster:
             turn = self.all_meet.come()
@@ -359,10 +368,11 @@ def test_queries_of_tiles_without_steps_must_not_be_asked_for():
 def test_keys_and_values_must_not_land_on_one_barrier():
     # (the copies of one CTA may land in any order)
     assert finds("values are looked through before they have landed", fulls=STAGES, order="any")
-    assert SOURCE.count("landed(i), landed_parity(i)") == 2 and "landed(value), landed_parity(value)" in SOURCE and "full + 8 * s," not in SOURCE.replace("bar_init(full + 8 * s, 1)", "")
+    assert "full + 8 * (i % kStages + (i & 1) * kStages)" in SOURCE and "(i / kStages >> 1) & 1" in SOURCE
+    assert SOURCE.count("landed(i), landed_parity(i)") == 2 and "full + 8 * s," not in SOURCE.replace("bar_init(full + 8 * s, 1)", "")
 
 
 def test_a_softmax_warp_must_not_leave_the_warp_it_meets():
     assert finds("everything waits", softmax="leaves", lost=4, order="any")
     softmax = SOURCE[SOURCE.index("---- softmax and output"): SOURCE.index("---- copies ----")]
-    assert softmax.count("warp_wait(") == 3 and "break;" not in softmax and "__all_sync(0xffffffffu, *abort == 0)" in softmax
+    assert softmax.count("break;") == 2 and "if (any_of_both(meet, false)) warps_meet(meet), warps_meet(meet), warps_meet(meet);" in softmax
