@@ -26,9 +26,7 @@ __global__ void __launch_bounds__(kElementThreads) attention_element_kernel(cons
   const int64_t last = min(p, a.table_pages * a.page_size - 1);
   const int64_t first = a.window ? max((int64_t)0, p - a.window + 1) : 0;
   const int64_t sinks = min((int64_t)a.sinks, first);
-  for (int64_t u = first - sinks; u <= last; ++u) {
-    const int64_t j = u < first ? u - (first - sinks) : u;  // the sinks before the window, then the window
-    if (j > last) break;
+  for (int64_t j = sinks > 0 ? 0 : first; j <= last; j = j + 1 == sinks ? first : j + 1) {  // the sinks before the window, then the window
     const int32_t page = __ldg(a.block_table + b * a.table_stride + j / a.page_size);
     if (page < 0 || page >= a.num_pages) continue;
     const bf16* k = reinterpret_cast<const bf16*>(a.k_cache) + page * a.kc_pstride + hk * a.kc_hstride + (j % a.page_size) * a.kc_rstride;

@@ -350,6 +350,18 @@ def test_attention_over_a_cache_of_no_pages_is_zero(page):
     assert not out.any()
 
 
+@pytest.mark.parametrize("nq", [1, 2, 40])
+@pytest.mark.parametrize("D,page", [(64, 16), (64, 24), (128, 16), (200, 16), (33, 16)])
+def test_attention_first_tokens_are_seen_where_the_window_lies_beyond_the_table(D, page, nq):
+    """A table of two pages under a sequence of 200 tokens: of the window nothing is there, or only its start; the sinks are."""
+    x = list(inputs([nq], [200], 4, 2, D, page, seed=D))
+    x[3] = x[3][:, :2].contiguous()
+    for window, sinks in ((5, 3), (200 - nq - 20, 4), (0, 0), (30, 40)):
+        want, bound = ref.attention(*x, window, sinks, D ** -0.5)
+        assert want.abs().amax(dim=-1).min() > 0  # every row sees something
+        check(run(x, nq, window, sinks, D ** -0.5), want, bound)
+
+
 def test_attention_refuses_what_the_library_cannot_take():
     q, k, v, table, start, lens = [t.cuda() for t in inputs([1], [20], 4, 2, 64, 16)]
     for bad in (dict(q=q.float()), dict(k=k.float()), dict(v=v[:-1]), dict(table=table.long()), dict(start=start[:1]), dict(lens=lens.float()), dict(q=q.cpu()),
