@@ -723,10 +723,11 @@ bool attention_tile_eligible(const approxifer_attention_args& a) {
 cudaError_t launch_attention_tile(const approxifer_attention_args& a, cudaStream_t stream) {
   TileArgs g{};
   g.a = a;
+  if (g.a.max_q > a.T) g.a.max_q = (int32_t)a.T;  // (no sequence has more queries than the call: a loose bound launches no CTAs for nothing)
   g.group = a.Hq / a.Hkv;
   g.tokens = kRows / g.group;
   const int per_cta = tiles_of(a.D <= 64 ? 64 : 128) * g.tokens;
-  g.blocks = (int)(((int64_t)a.max_q + per_cta - 1) / per_cta);
+  g.blocks = (int)(((int64_t)g.a.max_q + per_cta - 1) / per_cta);
   g.page_shift = log2_of(a.page_size);
   const int dp = a.D <= 64 ? 64 : 128;
   CUtensorMap q, k, v;

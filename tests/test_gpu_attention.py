@@ -362,6 +362,16 @@ def test_attention_first_tokens_are_seen_where_the_window_lies_beyond_the_table(
         check(run(x, nq, window, sinks, D ** -0.5), want, bound)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+def test_attention_takes_any_upper_bound_on_the_queries(D):
+    """The bound may be as loose as the type allows: the call costs what its tokens cost."""
+    Hkv, batch = 16, 12
+    x = inputs([3] + [1] * (batch - 1), [20 + b for b in range(batch)], Hkv, Hkv, D, 16, seed=D + 3)
+    want, bound = ref.attention(*x, 0, 0, D ** -0.5)
+    for max_q in (3, 1000, 2 ** 31 - 1):
+        check(run(x, max_q, 0, 0, D ** -0.5), want, bound)
+
+
 def test_attention_refuses_what_the_library_cannot_take():
     q, k, v, table, start, lens = [t.cuda() for t in inputs([1], [20], 4, 2, 64, 16)]
     for bad in (dict(q=q.float()), dict(k=k.float()), dict(v=v[:-1]), dict(table=table.long()), dict(start=start[:1]), dict(lens=lens.float()), dict(q=q.cpu()),
