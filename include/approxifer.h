@@ -425,7 +425,7 @@ int approxifer_qk_norm_rope(const approxifer_norm_rope_args* args, void* cuda_st
  * A row without a visible position (also: kv_len[b] shorter than the queries) is zero.  What lies in positions that
  * a query does not see, NaN included, never influences it.
  *   q_start  [batch+1] int32, ascending, q_start[0] = 0, q_start[batch] = T
- *   kv_len   [batch] int32        max_q  an upper bound on every sequence's number of queries (HOST)
+ *   kv_len   [batch] int32        max_q  an upper bound on every sequence's number of queries (HOST; T <= batch * max_q)
  *   k_cache, v_cache  [num_pages][Hkv][page_size][D] by strides; bfloat16, as q and out
  * The softmax runs in one pass in fp32; the weights are rounded to bfloat16 for the product with V.
  * Hq a multiple of Hkv, 1 <= D <= 256, 1 <= page_size.  The tensor-core kernels take D a multiple of 8 up to 128, 16-byte

@@ -23,7 +23,7 @@ int check_attention(const approxifer_attention_args& a) {
       a.vc_rstride < a.D || a.vc_hstride < a.D || a.vc_pstride < a.D || a.table_stride < 0)
     return APPROXIFER_E_RANGE;
   if (a.Hq % a.Hkv != 0 || a.reserved != 0 || !isfinite(a.scale)) return APPROXIFER_E_PARAM;
-  if (a.T > 0 && (a.batch < 1 || a.max_q < 1)) return APPROXIFER_E_RANGE;
+  if (a.T > (int64_t)a.batch * a.max_q) return APPROXIFER_E_RANGE;  // (some sequence has more queries than max_q: their rows would not be written)
   return APPROXIFER_OK;
 }
 }  // namespace

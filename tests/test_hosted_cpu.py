@@ -128,3 +128,11 @@ def test_outputs_for_another_stream_come_from_that_streams_memory(monkeypatch):
         del seen[:]
         call()
         assert seen == [(name, None)]
+
+
+def test_attention_refuses_more_tokens_than_the_bound_on_the_queries_allows():
+    # (such a call would leave rows unwritten)
+    assert attention_rc(T=7, batch=2, max_q=3) == binding.E_RANGE
+    assert attention_rc(T=7, batch=2, max_q=3, q=0) == binding.E_RANGE
+    assert attention_rc(T=6, batch=2, max_q=3, q=0) == binding.E_NULL
+    assert attention_rc(T=6, batch=2 ** 31 - 1, max_q=2 ** 31 - 1, q=0) == binding.E_NULL
