@@ -17,7 +17,8 @@ namespace {
 // Everything but the pointers.
 int check_attention(const approxifer_attention_args& a) {
   if (a.T < 0 || a.T > kMaxExtent || a.batch < 0 || a.max_q < 0 || a.Hq < 1 || a.Hq > 65535 || a.Hkv < 1 || a.D < 1 || a.D > 256) return APPROXIFER_E_RANGE;
-  if (a.page_size < 1 || a.window < 0 || a.sinks < 0 || a.num_pages < 0 || a.num_pages > kMaxExtent || a.table_pages < 0 || a.workspace_bytes < 0)
+  if (a.page_size < 1 || a.window < 0 || a.sinks < 0 || a.num_pages < 0 || a.num_pages > kMaxExtent || a.table_pages < 0 || a.table_pages > kMaxExtent ||
+      a.workspace_bytes < 0)
     return APPROXIFER_E_RANGE;
   if (a.q_tstride < 0 || a.q_hstride < a.D || a.o_tstride < 0 || a.o_hstride < a.D || a.kc_rstride < a.D || a.kc_hstride < a.D || a.kc_pstride < a.D ||
       a.vc_rstride < a.D || a.vc_hstride < a.D || a.vc_pstride < a.D || a.table_stride < 0)
@@ -67,7 +68,7 @@ int approxifer_linear(const approxifer_linear_args* a, void* cuda_stream) {
 int approxifer_qk_norm_rope(const approxifer_norm_rope_args* a, void* cuda_stream) {
   if (a == nullptr) return APPROXIFER_E_NULL;
   if (a->T < 0 || a->T > kMaxExtent || a->Hq < 1 || a->Hq > 65535 || a->Hkv < 1 || a->Hkv > 65535 || a->D < 1 || a->D > 256) return APPROXIFER_E_RANGE;
-  if (a->rot < 0 || a->rot > a->D || a->page_size < 1 || a->num_pages < 0 || a->positions_max < 0) return APPROXIFER_E_RANGE;
+  if (a->rot < 0 || a->rot > a->D || a->page_size < 1 || a->num_pages < 0 || a->num_pages > kMaxExtent || a->positions_max < 0) return APPROXIFER_E_RANGE;
   if (a->rot % 2 != 0 || !known_type(a->type) || !(a->eps >= 0.f)) return APPROXIFER_E_PARAM;
   if ((a->k == nullptr) != (a->k_cache == nullptr) || (a->v == nullptr) != (a->v_cache == nullptr)) return APPROXIFER_E_NULL;
   if (a->q_tstride < 0 || a->q_hstride < a->D || a->qo_tstride < 0 || a->qo_hstride < a->D) return APPROXIFER_E_RANGE;

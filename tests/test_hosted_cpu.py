@@ -136,3 +136,12 @@ def test_attention_refuses_more_tokens_than_the_bound_on_the_queries_allows():
     assert attention_rc(T=7, batch=2, max_q=3, q=0) == binding.E_RANGE
     assert attention_rc(T=6, batch=2, max_q=3, q=0) == binding.E_NULL
     assert attention_rc(T=6, batch=2 ** 31 - 1, max_q=2 ** 31 - 1, q=0) == binding.E_NULL
+
+
+def test_extents_whose_products_overflow_are_refused():
+    assert attention_rc(tp=2 ** 31) == binding.E_RANGE
+    assert attention_rc(tp=2 ** 40, page=2 ** 31 - 1) == binding.E_RANGE
+    assert attention_rc(tp=2 ** 31 - 1, page=2 ** 31 - 1, q=0) == binding.E_NULL
+    assert norm_rope_rc(pages=2 ** 31) == binding.E_RANGE
+    assert norm_rope_rc(pages=2 ** 62) == binding.E_RANGE
+    assert norm_rope_rc(pages=2 ** 31 - 1, q=0) == binding.E_NULL
