@@ -697,12 +697,6 @@ cudaError_t launch_one(const TileArgs& g, const CUtensorMap& q, const CUtensorMa
   return split > 1 ? launch_split<DP, true>(g, q, k, v, *dev, ctas, split, stream) : launch_split<DP, false>(g, q, k, v, *dev, ctas, 1, stream);
 }
 
-int log2_of(int v) {
-  int s = 0;
-  while ((1 << s) < v) ++s;
-  return (1 << s) == v ? s : -1;
-}
-
 }  // namespace
 
 cudaError_t read_attention_tile_wait_timeouts(unsigned int* out) { return cudaMemcpyFromSymbol(out, g_attention_tile_wait_timeouts, sizeof(*out)); }
@@ -713,7 +707,7 @@ cudaError_t reset_attention_tile_wait_timeouts() {
 
 bool attention_tile_eligible(const approxifer_attention_args& a) {
   const int64_t limit = 1LL << 38;
-  return a.D % 8 == 0 && a.D <= 128 && a.Hq / a.Hkv <= kRows && a.num_pages >= 1 && a.page_size >= 8 && log2_of(a.page_size) > 0 &&
+  return a.D % 8 == 0 && a.D <= 128 && a.Hq / a.Hkv <= kRows && a.num_pages >= 1 && a.page_size >= 8 && exact_log2(a.page_size) > 0 &&
          a.table_pages * a.page_size < (1LL << 30) && aligned16(a.q) && aligned16(a.k_cache) && aligned16(a.v_cache) && aligned16(a.out) &&
          (a.q_tstride | a.q_hstride | a.o_tstride | a.o_hstride | a.kc_pstride | a.kc_hstride | a.kc_rstride | a.vc_pstride | a.vc_hstride | a.vc_rstride) % 8 == 0 &&
          a.q_tstride < limit && a.q_hstride < limit && a.kc_pstride < limit && a.kc_hstride < limit && a.kc_rstride < limit && a.vc_pstride < limit &&
@@ -728,7 +722,7 @@ cudaError_t launch_attention_tile(const approxifer_attention_args& a, cudaStream
   g.tokens = kRows / g.group;
   const int per_cta = tiles_of(a.D <= 64 ? 64 : 128) * g.tokens;
   g.blocks = (int)(((int64_t)g.a.max_q + per_cta - 1) / per_cta);
-  g.page_shift = log2_of(a.page_size);
+  g.page_shift = exact_log2(a.page_size);
   const int dp = a.D <= 64 ? 64 : 128;
   CUtensorMap q, k, v;
   const uint64_t qe[3] = {(uint64_t)a.D, (uint64_t)a.Hq, (uint64_t)a.T}, qs[3] = {1, (uint64_t)a.q_hstride, (uint64_t)a.q_tstride};

@@ -681,9 +681,8 @@ cudaError_t launch_attention_token(const approxifer_attention_args& a, cudaStrea
   if (e != cudaSuccess) return e;
   const int row_tiles = (a.Hq / a.Hkv + kRows - 1) / kRows;
   const int dp = a.D <= 64 ? 64 : 128, keys = keys_of(dp);
-  int page_shift = 0;  // pages of whole chunks and a power of two: one look-up a chunk
-  while ((1 << page_shift) < a.page_size) ++page_shift;
-  const bool is_whole = (1 << page_shift) == a.page_size && a.page_size >= keys;
+  const int page_shift = exact_log2(a.page_size);  // pages of whole chunks and a power of two: one look-up a chunk
+  const bool is_whole = page_shift >= 0 && a.page_size >= keys;
   const int64_t need = attention_token_workspace(a);
   if (need > 0 && a.workspace_bytes >= need && (int64_t)a.batch * a.Hq < (1LL << 31)) {
     auto launch = is_whole ? (dp == 64 ? launch_balanced<64, true> : launch_balanced<128, true>) : dp == 64 ? launch_balanced<64, false> : launch_balanced<128, false>;

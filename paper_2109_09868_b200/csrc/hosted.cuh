@@ -12,6 +12,13 @@ namespace approxifer {
 
 using bf16 = __nv_bfloat16;
 
+// s with 2^s = v, or -1.
+inline int exact_log2(int32_t v) {
+  for (int s = 0; s < 31; ++s)
+    if ((1 << s) == v) return s;
+  return -1;
+}
+
 cudaError_t launch_linear(const approxifer_linear_args& a, cudaStream_t stream);
 bool linear_tile_eligible(const approxifer_linear_args& a);  // see linear_tile.cu
 cudaError_t launch_linear_tile(const approxifer_linear_args& a, cudaStream_t stream);

@@ -262,9 +262,7 @@ cudaError_t launch_columns(const approxifer_norm_rope_args& a, cudaStream_t stre
   const int q_units = (a.Hq + kRowsPerUnit - 1) / kRowsPerUnit, kv_units = (a.Hkv + kRowsPerUnit - 1) / kRowsPerUnit;
   const int units = q_units + (a.k ? kv_units : 0) + (a.v ? kv_units : 0);
   const int parts = (units + kMaxWarps - 1) / kMaxWarps, warps = (units + parts - 1) / parts;
-  int page_shift = 0;
-  while ((1 << page_shift) < a.page_size && page_shift < 30) ++page_shift;
-  if ((1 << page_shift) != a.page_size) page_shift = -1;
+  const int page_shift = exact_log2(a.page_size);
   const bool partial = a.rot < a.D;
   auto kernel = a.interleaved ? (partial ? norm_rope_kernel<T, L, true, true> : norm_rope_kernel<T, L, true, false>)
                               : (partial ? norm_rope_kernel<T, L, false, true> : norm_rope_kernel<T, L, false, false>);

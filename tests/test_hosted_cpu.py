@@ -1,12 +1,17 @@
 """What the hosted-model operators refuse, found on the host before anything is launched."""
 import ctypes
+import os
 import struct
+import subprocess
+import sys
 
 import pytest
 import torch
 
 import paper_2109_09868_b200 as ap
 from paper_2109_09868_b200 import binding
+
+HERE = os.path.dirname(os.path.abspath(__file__))
 
 # the argument structs of the header, field by field (native alignment)
 LINEAR = struct.Struct("@qqqPqPqPPqPqii")
@@ -145,3 +150,12 @@ def test_extents_whose_products_overflow_are_refused():
     assert norm_rope_rc(pages=2 ** 31) == binding.E_RANGE
     assert norm_rope_rc(pages=2 ** 62) == binding.E_RANGE
     assert norm_rope_rc(pages=2 ** 31 - 1, q=0) == binding.E_NULL
+
+
+@pytest.mark.parametrize("page", [2 ** 30 + 1, 2 ** 31 - 1])
+@pytest.mark.parametrize("max_q,T", [(1, 1), (3, 3)])
+def test_the_choice_of_kernel_ends_for_the_longest_pages(page, max_q, T):
+    """In a process without a device, so that nothing can be launched: the call gets as far as that."""
+    code = ("import sys; sys.path[:0] = [%r, %r]\nimport test_hosted_cpu as t\n"
+            "assert t.attention_rc(T=%d, max_q=%d, tp=1, page=%d) == t.binding.E_CUDA" % (os.path.dirname(HERE), HERE, T, max_q, page))
+    subprocess.run([sys.executable, "-c", code], check=True, timeout=120, env=dict(os.environ, CUDA_VISIBLE_DEVICES=""))
