@@ -110,6 +110,12 @@ double real(PyObject* o) {
   return v;
 }
 
+bool truth(PyObject* o) {
+  const int v = PyObject_IsTrue(o);
+  if (v < 0) throw Raised();
+  return v != 0;
+}
+
 int32_t type_code(at::ScalarType t, const char* name) {
   if (t == at::kBFloat16) return APPROXIFER_TYPE_BF16;
   if (t == at::kFloat) return APPROXIFER_TYPE_F32;
@@ -234,7 +240,7 @@ PyObject* norm_rope(PyObject*, PyObject* const* arg, Py_ssize_t n) {
     }
     a.q_out = out.data_ptr(), a.qo_tstride = out.stride(0), a.qo_hstride = out.stride(1);
     a.eps = (float)real(arg[11]);
-    a.interleaved = PyObject_IsTrue(arg[12]);
+    a.interleaved = truth(arg[12]);
     if (arg[13] != Py_None) a.status = reinterpret_cast<uint32_t*>(data<int32_t>(vec(arg[13], at::kInt, a.T, "status")));
     return finish(entry.norm_rope(&a, stream_of(arg[14], device)), "approxifer_qk_norm_rope", out, arg[10]);
   });

@@ -146,3 +146,10 @@ def test_norm_rope_refuses_what_the_library_cannot_take():
         ap.approxifer_qk_norm_rope(**dict(good, cos_sin=d["cs"][:, :33].contiguous()))  # an odd rotation
     with pytest.raises(ap.ApproxiferError):
         ap.approxifer_qk_norm_rope(**good, eps=-1.0)
+
+
+def test_norm_rope_passes_on_the_error_of_an_argument_without_a_truth_value():
+    x = torch.zeros((3, 2, 64), dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(RuntimeError, match="ambiguous"):
+        ap.approxifer_qk_norm_rope(x, None, None, None, None, table(4, 64).cuda(), torch.arange(3, dtype=torch.int32, device="cuda"), None, None, None,
+                                   interleaved=torch.ones(2))
