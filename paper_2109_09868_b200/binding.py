@@ -86,11 +86,11 @@ def load() -> ctypes.CDLL:
     if _lib is not None:
         return _lib
     have_nvcc = shutil.which("nvcc") is not None or os.path.exists("/usr/local/cuda/bin/nvcc")
-    if have_nvcc and _build.is_stale():
-        _build.build()
-    if not os.path.exists(_build.LIB) or not os.path.exists(_build.BINDING):
+    if have_nvcc and _build.library_is_stale():
+        _build.build_library()
+    if not os.path.exists(_build.LIB):
         raise RuntimeError(
-            "libapproxifer.so or _hosted.so is missing and cannot be built (no nvcc): run `python -m paper_2109_09868_b200.build`"
+            "libapproxifer.so is missing and cannot be built (no nvcc): run `python -m paper_2109_09868_b200.build`"
         )
     lib = ctypes.CDLL(_build.LIB)
     pf, pu, pi = POINTER(c_float), POINTER(c_uint32), POINTER(c_int32)

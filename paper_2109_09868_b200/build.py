@@ -1,9 +1,10 @@
-"""Builds ``libapproxifer.so`` (sm_100a) in-tree with nvcc.
+"""Builds ``libapproxifer.so`` (sm_100a) in-tree with nvcc, and ``_hosted.so`` (the hosted-model operators' Python binding) with g++.
 
     python -m paper_2109_09868_b200.build [--force] [--verbose]
 
-Objects go to ``paper_2109_09868_b200/_build/``; the shared library is written
-next to this file.  nvcc cross-compiles, so no GPU is needed to build.
+Objects go to ``paper_2109_09868_b200/_build/``; the shared libraries are written
+next to this file.  nvcc cross-compiles, so no GPU is needed to build.  The two are
+built apart: what does not call the hosted-model operators does without the second.
 """
 from __future__ import annotations
 
@@ -47,16 +48,24 @@ def check_toolkit() -> None:
                            "parameter blocks of up to 32 KB)" % (m.group(1), m.group(2), *MIN_CUDA))
 
 
-def _deps_mtime() -> float:
-    paths = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(INCLUDE, "approxifer.h"), __file__]
-    return max(os.path.getmtime(p) for p in paths)
+def _stale(target: str, sources) -> bool:
+    paths = [os.path.join(CSRC, f) for f in sources] + [os.path.join(INCLUDE, "approxifer.h"), __file__]
+    return not os.path.exists(target) or os.path.getmtime(target) < max(os.path.getmtime(p) for p in paths)
+
+
+def library_is_stale() -> bool:
+    return _stale(LIB, [f for f in os.listdir(CSRC) if f != "hosted_binding.cpp"])
+
+
+def binding_is_stale() -> bool:
+    return _stale(BINDING, ["hosted_binding.cpp"])
 
 
 def is_stale() -> bool:
-    return any(not os.path.exists(f) or os.path.getmtime(f) < _deps_mtime() for f in (LIB, BINDING))
+    return library_is_stale() or binding_is_stale()
 
 
-def _build_binding(verbose: bool) -> None:
+def build_binding(verbose: bool = False) -> str:
     """Compiles hosted_binding.cpp against the installed torch's headers (host code only)."""
     import sysconfig
 
@@ -75,6 +84,7 @@ def _build_binding(verbose: bool) -> None:
     if r.returncode != 0:
         raise RuntimeError("g++ failed on hosted_binding.cpp:\n%s\n%s" % (r.stdout, r.stderr))
     os.replace(tmp, BINDING)
+    return BINDING
 
 
 def _compile(src: str, verbose: bool) -> str:
@@ -92,21 +102,28 @@ def _compile(src: str, verbose: bool) -> str:
     return obj
 
 
-def build(force: bool = False, verbose: bool = False) -> str:
-    if not force and not is_stale():
-        return LIB
+def build_library(verbose: bool = False) -> str:
     check_toolkit()
     os.makedirs(OBJDIR, exist_ok=True)
-    with concurrent.futures.ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
-        binding = ex.submit(_build_binding, verbose)
+    with concurrent.futures.ThreadPoolExecutor(max_workers=len(SOURCES)) as ex:
         objs = list(ex.map(lambda s: _compile(s, verbose), SOURCES))
-        binding.result()
     tmp = LIB + ".tmp.%d" % os.getpid()
     cmd = [nvcc(), *ARCH, "-shared", "-o", tmp, *objs]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError("link failed:\n%s\n%s" % (r.stdout, r.stderr))
     os.replace(tmp, LIB)
+    return LIB
+
+
+def build(force: bool = False, verbose: bool = False) -> str:
+    """Both, where they are older than their sources."""
+    with concurrent.futures.ThreadPoolExecutor(max_workers=1) as ex:
+        binding = ex.submit(build_binding, verbose) if force or binding_is_stale() else None
+        if force or library_is_stale():
+            build_library(verbose)
+        if binding:
+            binding.result()
     return LIB
 
 

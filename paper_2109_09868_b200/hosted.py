@@ -15,6 +15,8 @@ from __future__ import annotations
 import ctypes
 import importlib.machinery
 import importlib.util
+import os
+import shutil
 from typing import Optional
 
 import torch
@@ -31,7 +33,12 @@ _native = None
 def _load():
     """The native binding, with the loaded library's entry points."""
     global _native
-    lib = load()  # (builds both if they are older than their sources)
+    lib = load()
+    have_compilers = shutil.which("g++") is not None and (shutil.which("nvcc") is not None or os.path.exists("/usr/local/cuda/bin/nvcc"))
+    if have_compilers and _build.binding_is_stale():
+        _build.build_binding()
+    if not os.path.exists(_build.BINDING):
+        raise RuntimeError("_hosted.so is missing and cannot be built (no g++ or no CUDA headers): run `python -m paper_2109_09868_b200.build`")
     loader = importlib.machinery.ExtensionFileLoader("_hosted", _build.BINDING)
     module = importlib.util.module_from_spec(importlib.util.spec_from_loader("_hosted", loader))
     loader.exec_module(module)

@@ -159,3 +159,39 @@ def test_the_choice_of_kernel_ends_for_the_longest_pages(page, max_q, T):
     code = ("import sys; sys.path[:0] = [%r, %r]\nimport test_hosted_cpu as t\n"
             "assert t.attention_rc(T=%d, max_q=%d, tp=1, page=%d) == t.binding.E_CUDA" % (os.path.dirname(HERE), HERE, T, max_q, page))
     subprocess.run([sys.executable, "-c", code], check=True, timeout=120, env=dict(os.environ, CUDA_VISIBLE_DEVICES=""))
+
+
+def test_only_the_hosted_operators_need_their_binding(monkeypatch, tmp_path):
+    """Without _hosted.so, and without what it takes to build it, the library loads; the hosted operators say what is missing."""
+    from paper_2109_09868_b200 import build, hosted
+
+    def refuse(*a, **k):
+        raise RuntimeError("no g++ here")
+
+    monkeypatch.setattr(build, "BINDING", str(tmp_path / "_hosted.so"))
+    monkeypatch.setattr(build, "build_binding", refuse)
+    monkeypatch.setattr(binding, "_lib", None)
+    monkeypatch.setattr(hosted, "_native", None)
+    assert ap.load().approxifer_version() == ap.version() >= 100
+    x = torch.zeros(2, 8, dtype=torch.bfloat16)
+    with pytest.raises(RuntimeError, match="no g"):
+        ap.approxifer_linear(x, x)
+    monkeypatch.setattr(hosted.shutil, "which", lambda name: None)
+    with pytest.raises(RuntimeError, match="_hosted.so is missing"):
+        ap.approxifer_linear(x, x)
+
+
+def test_a_binding_that_does_not_build_keeps_nobody_from_the_library(monkeypatch, tmp_path):
+    from paper_2109_09868_b200 import build
+
+    def refuse(*a, **k):
+        raise RuntimeError("no g++ here")
+
+    built = []
+    monkeypatch.setattr(build, "BINDING", str(tmp_path / "_hosted.so"))
+    monkeypatch.setattr(build, "build_binding", refuse)
+    monkeypatch.setattr(build, "library_is_stale", lambda: True)
+    monkeypatch.setattr(build, "build_library", lambda verbose=False: built.append(1))
+    with pytest.raises(RuntimeError, match="no g"):
+        build.build()
+    assert built == [1]
