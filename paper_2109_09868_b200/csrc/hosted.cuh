@@ -49,21 +49,30 @@ __device__ __forceinline__ float narrow<float>(float v) { return v; }
 template <>
 __device__ __forceinline__ bf16 narrow<bf16>(float v) { return __float2bfloat16_rn(v); }
 
-// The activations of approxifer_linear, in fp32.
-template <int ACT>
+// e^x to the accuracy that an output of type Out shows.  __expf errs by some 1.2 |x| units in the last place: 5e-6 relative at
+// |x| = 40, which bfloat16 (4e-3) hides and fp32 does not.
+template <typename Out>
+__device__ __forceinline__ float exponential(float x) {
+  if constexpr (sizeof(Out) == 4) return expf(x);
+  return __expf(x);
+}
+
+// The activations of approxifer_linear, in fp32, for an output of type Out.
+template <int ACT, typename Out>
 __device__ __forceinline__ float activate(float x) {
   if constexpr (ACT == APPROXIFER_ACT_RELU) return x > 0.f ? x : (x == x ? 0.f : x);  // (a NaN stays one)
   if constexpr (ACT == APPROXIFER_ACT_GELU) return 0.5f * x * (1.f + erff(x * 0.70710678f));
-  if constexpr (ACT == APPROXIFER_ACT_GELU_TANH) return x / (1.f + __expf(-1.5957691f * (x + 0.044715f * x * x * x)));  // 0.5 (1 + tanh u) = 1 / (1 + e^-2u)
-  if constexpr (ACT == APPROXIFER_ACT_SILU) return x / (1.f + __expf(-x));
+  if constexpr (ACT == APPROXIFER_ACT_GELU_TANH) return x / (1.f + exponential<Out>(-1.5957691f * (x + 0.044715f * x * x * x)));  // 0.5 (1 + tanh u) = 1 / (1 + e^-2u)
+  if constexpr (ACT == APPROXIFER_ACT_SILU) return x / (1.f + exponential<Out>(-x));
   return x;
 }
+template <typename Out>
 __device__ __forceinline__ float activate(int act, float x) {
   switch (act) {
-    case APPROXIFER_ACT_RELU: return activate<APPROXIFER_ACT_RELU>(x);
-    case APPROXIFER_ACT_GELU: return activate<APPROXIFER_ACT_GELU>(x);
-    case APPROXIFER_ACT_GELU_TANH: return activate<APPROXIFER_ACT_GELU_TANH>(x);
-    case APPROXIFER_ACT_SILU: return activate<APPROXIFER_ACT_SILU>(x);
+    case APPROXIFER_ACT_RELU: return activate<APPROXIFER_ACT_RELU, Out>(x);
+    case APPROXIFER_ACT_GELU: return activate<APPROXIFER_ACT_GELU, Out>(x);
+    case APPROXIFER_ACT_GELU_TANH: return activate<APPROXIFER_ACT_GELU_TANH, Out>(x);
+    case APPROXIFER_ACT_SILU: return activate<APPROXIFER_ACT_SILU, Out>(x);
     default: return x;
   }
 }

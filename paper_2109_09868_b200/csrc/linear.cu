@@ -45,7 +45,7 @@ __global__ void __launch_bounds__(kThreads) linear_element_kernel(const __grid_c
       if (m >= a.M || n >= a.N) continue;
       float y = acc[i][j];
       if (a.bias) y += widen(reinterpret_cast<const bf16*>(a.bias)[n]);
-      y = activate(a.activation, y);
+      y = activate<Out>(a.activation, y);
       if (a.R) y += widen(static_cast<const Out*>(a.R)[m * a.r_rstride + n]);
       static_cast<Out*>(a.Y)[m * a.y_rstride + n] = narrow<Out>(y);
     }

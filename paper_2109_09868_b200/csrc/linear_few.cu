@@ -79,7 +79,7 @@ __global__ void __launch_bounds__(kThreads, 2) linear_few_kernel(const __grid_co
 #pragma unroll
   for (int w = 1; w < kWarps; ++w) y += sums[w][row][m];
   if (a.bias) y += widen(reinterpret_cast<const bf16*>(a.bias)[n]);
-  y = activate(a.activation, y);
+  y = activate<Out>(a.activation, y);
   if (a.R) y += widen(static_cast<const Out*>(a.R)[m * a.r_rstride + n]);
   static_cast<Out*>(a.Y)[m * a.y_rstride + n] = narrow<Out>(y);
 }

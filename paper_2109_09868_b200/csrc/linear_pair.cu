@@ -75,7 +75,7 @@ __device__ __forceinline__ void finish32(const PairArgs& a, int m0, int n, const
     const int row = i * 4 + lane / 8;
     if (row >= left) break;
     const float4 x = turn[row * 8 + ((lane % 8) ^ (row & 7))];
-    float z[4] = {activate<ACT>(x.x + b[0]), activate<ACT>(x.y + b[1]), activate<ACT>(x.z + b[2]), activate<ACT>(x.w + b[3])};
+    float z[4] = {activate<ACT, Out>(x.x + b[0]), activate<ACT, Out>(x.y + b[1]), activate<ACT, Out>(x.z + b[2]), activate<ACT, Out>(x.w + b[3])};
     Out* y = static_cast<Out*>(a.Y) + (int64_t)(m0 + row) * a.y_rstride + col;
     const Out* r = a.R ? static_cast<const Out*>(a.R) + (int64_t)(m0 + row) * a.r_rstride + col : nullptr;
     if (vec) {

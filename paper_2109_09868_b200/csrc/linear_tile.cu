@@ -218,7 +218,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tile_kernel(const __grid_c
         if (mi >= m_to) continue;
         float4 z = make_float4(v[i].x + b.x, v[i].y + b.y, v[i].z + b.z, v[i].w + b.w);
         if (a.activation != APPROXIFER_ACT_NONE)
-          z = make_float4(activate(a.activation, z.x), activate(a.activation, z.y), activate(a.activation, z.z), activate(a.activation, z.w));
+          z = make_float4(activate<Out>(a.activation, z.x), activate<Out>(a.activation, z.y), activate<Out>(a.activation, z.z), activate<Out>(a.activation, z.w));
         write4<Out>(Y + (int64_t)(m0 + mi) * a.y_rstride, make_float4(z.x + r[i].x, z.y + r[i].y, z.z + r[i].z, z.w + r[i].w), a.vec, count);
       }
     }

@@ -1,5 +1,7 @@
 """approxifer_linear against its 64-bit plain form: shapes from one row to several tiles, odd sizes, strides, unaligned
 bases, every activation, bias and residual present or not, both output types."""
+import math
+
 import pytest
 import torch
 
@@ -134,6 +136,29 @@ def test_linear_on_another_stream_leaves_memory_alone_that_the_current_one_still
         s.synchronize()
         torch.cuda.synchronize()
         assert bool((copy == 3.0).all()) and torch.equal(y, want)
+
+
+@pytest.mark.parametrize("M,K", [(2, 64), (40, 64), (300, 64), (2600, 64), (20, 13)])
+def test_linear_activations_keep_their_relative_accuracy_in_fp32(M, K):
+    """Sums that are exact (one element of each row of X is 1), so that only the activation errs: x / (1 + e^-x) by at most 2^-23 for
+    each of the exponential (twice that), the sum and the quotient, relative to the result, also where that is small."""
+    N = 1200 if M == 2600 else 200
+    x = torch.zeros((M, K))
+    x[:, 3] = 1
+    w = torch.zeros((N, K))
+    w[:, 3] = torch.linspace(-80, 12, N)
+    x, w = x.bfloat16(), w.bfloat16()
+    z = w[:, 3].double()
+    want = (z / (1 + torch.exp(-z))).expand(M, N)
+    got = ap.approxifer_linear(x.cuda(), w.cuda(), activation="silu", out_dtype=torch.float32).double().cpu()
+    assert ((got - want).abs() <= 4 * 2.0 ** -23 * want.abs() + 2.0 ** -130).all()
+    # gelu by tanh: x / (1 + e^u) with u = -2 sqrt(2/pi) (x + 0.044715 x^3) in some six operations, each an error of e^u that grows with |u|
+    u = -2 * math.sqrt(2 / math.pi) * (z + 0.044715 * z ** 3)
+    want = (z / (1 + torch.exp(u))).expand(M, N)
+    got = ap.approxifer_linear(x.cuda(), w.cuda(), activation="gelu_tanh", out_dtype=torch.float32).double().cpu()
+    near = u.expand(M, N) < 80
+    over = (got - want).abs() - ((6 * u.abs() + 4) * 2.0 ** -23 * want.abs() + 2.0 ** -100)
+    assert (over[near] <= 0).all()
 
 
 def test_linear_of_no_rows():
