@@ -710,7 +710,7 @@ bool attention_tile_eligible(const approxifer_attention_args& a) {
   return a.D % 8 == 0 && a.D <= 128 && a.Hq / a.Hkv <= kRows && a.num_pages >= 1 && a.page_size >= 8 && exact_log2(a.page_size) > 0 &&
          a.table_pages * a.page_size < (1LL << 30) && aligned16(a.q) && aligned16(a.k_cache) && aligned16(a.v_cache) && aligned16(a.out) &&
          (a.q_tstride | a.q_hstride | a.o_tstride | a.o_hstride | a.kc_pstride | a.kc_hstride | a.kc_rstride | a.vc_pstride | a.vc_hstride | a.vc_rstride) % 8 == 0 &&
-         a.q_tstride < limit && a.q_hstride < limit && a.kc_pstride < limit && a.kc_hstride < limit && a.kc_rstride < limit && a.vc_pstride < limit &&
+         a.q_tstride > 0 /* (a tensor map's strides; one query for all tokens is the element-wise kernel's) */ && a.q_tstride < limit && a.q_hstride < limit && a.kc_pstride < limit && a.kc_hstride < limit && a.kc_rstride < limit && a.vc_pstride < limit &&
          a.vc_hstride < limit && a.vc_rstride < limit && a.sinks < (1 << 30) && a.window < (1 << 30);
 }
 

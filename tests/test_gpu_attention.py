@@ -372,6 +372,19 @@ def test_attention_takes_any_upper_bound_on_the_queries(D):
         check(run(x, max_q, 0, 0, D ** -0.5), want, bound)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+def test_attention_of_one_query_for_all_tokens(D):
+    """Queries broadcast over the tokens: a token stride of zero."""
+    q, k, v, table, start, lens = inputs([20, 1], [50, 9], 4, 2, D, 16, seed=D + 5)
+    q = q[:1].expand(21, -1, -1)
+    want, bound = ref.attention(q, k, v, table, start, lens, 30, 2, D ** -0.5)
+    wide = q[:1].cuda().expand(21, -1, -1)
+    assert wide.stride(0) == 0
+    check(run((wide, k, v, table, start, lens), 20, 30, 2, D ** -0.5), want, bound)
+    one = (wide[19:], k, v, table, torch.tensor([0, 1, 2], dtype=torch.int32), lens)
+    check(run(one, 1, 30, 2, D ** -0.5), want[19:], bound[19:])
+
+
 def test_attention_refuses_what_the_library_cannot_take():
     q, k, v, table, start, lens = [t.cuda() for t in inputs([1], [20], 4, 2, 64, 16)]
     for bad in (dict(q=q.float()), dict(k=k.float()), dict(v=v[:-1]), dict(table=table.long()), dict(start=start[:1]), dict(lens=lens.float()), dict(q=q.cpu()),
