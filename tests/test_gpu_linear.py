@@ -161,6 +161,19 @@ def test_linear_activations_keep_their_relative_accuracy_in_fp32(M, K):
     assert (over[near] <= 0).all()
 
 
+@pytest.mark.parametrize("M,N", [(3, 70), (40, 70), (300, 200), (2500, 1300)])
+@pytest.mark.parametrize("K", [1, 13, 77, 201])
+def test_linear_rows_of_odd_length_in_whole_columns(M, N, K):
+    """Rows of any length K at strides of whole 16 bytes run on the tensor cores; what lies behind a row is NaN."""
+    x, w = normal((M, K), 1), normal((N, K), 2, std=K ** -0.5)
+    want, bound = ref.linear(x, w, None, "silu", None, torch.float32)
+    wide = (K + 15) // 8 * 8
+    xp = torch.full((M, wide), float("nan"), dtype=torch.bfloat16, device="cuda")
+    wp = torch.full((N, wide), float("nan"), dtype=torch.bfloat16, device="cuda")
+    xp[:, :K], wp[:, :K] = x.cuda(), w.cuda()
+    check(ap.approxifer_linear(xp[:, :K], wp[:, :K], activation="silu", out_dtype=torch.float32), want, bound)
+
+
 def test_linear_of_no_rows():
     assert ap.approxifer_linear(torch.empty((0, 64), dtype=torch.bfloat16, device="cuda"), torch.empty((5, 64), dtype=torch.bfloat16, device="cuda")).shape == (0, 5)
 
