@@ -29,9 +29,9 @@
 //
 // What bounds it is that chain and its issue, not a unit: at 4,096 causal tokens, D = 128, the tensor cores are busy 48 % of
 // the cycles, the special-function unit (a weight is one exponential) 49 %, instructions issue in 43 %.  Measured: 2 x 8,192
-// tokens causal, 32 heads on 4 of 128: 944 us, 1,165 TFLOP/s; prompts of 1,828 .. 4,096 under a window of 1,024, 32 heads
-// on 8 of 64: 198 us, 379 TFLOP/s (a CTA lives ten steps, four of them masked, and its start and end take the time of
-// three).  Tried and not faster: forming a quarter of the exponentials by a polynomial (the loop's code grows past what the
+// tokens causal, 32 heads on 4 of 128: 925 us, 1,188 TFLOP/s, and 1,080 to 1,100 us, 1,010 TFLOP/s, repeated at the power
+// limit; prompts of 1,828 .. 4,096 under a window of 1,024, 32 heads on 8 of 64: 195 to 200 us, 380 TFLOP/s (a CTA lives ten
+// steps, four of them masked, and its start and end take the time of three).  Tried and not faster: forming a quarter of the exponentials by a polynomial (the loop's code grows past what the
 // instruction caches take well), leaving out the exponentials of keys that no row of a warp sees, one thread to a row, one
 // tile to a CTA at D = 128.
 #include "async.cuh"

@@ -14,9 +14,9 @@
 //                  differ as they like.  A run that covers a whole unit writes its output; the others leave partial sums
 //                  in the workspace, which a second small launch joins, in order.
 //
-// Measured: one token, 1,028 visible of 1,500 cached, 32 heads on 8 of 128: 7.1 us (latency: three loads that wait for one
-// another, the joining); 48 tokens, window 4,096: 134 us, 6.0 TB/s; 4 contexts of up to 131,072, 2 key heads of 64: 43 us,
-// 4.6 TB/s (the joining of 148 partial results a unit is 5 us of it).
+// Measured: one token, 1,028 visible of 1,500 cached, 32 heads on 8 of 128: 7.0 us (latency: three loads that wait for one
+// another, the joining); 48 tokens, window 4,096: 134 us, 6.0 TB/s, from a graph, 142 to 145 us, 5.6 TB/s, call by call; 4
+// contexts of up to 131,072, 2 key heads of 64: 43 us, 4.6 TB/s (the joining of 148 partial results a unit is 5 us of it).
 #include "async.cuh"
 
 namespace approxifer {

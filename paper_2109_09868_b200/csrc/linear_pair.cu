@@ -12,8 +12,8 @@
 //               rows takes 32 passes; with short K the epilogue is all that is seen)
 //
 // Bound by the tensor cores, for seconds on end by the power limit.  Measured: 8,192 x 16,384 x 4,096 with bias and gelu
-// 725 us, 1,517 TFLOP/s (1,619 is what a library product of 8,192^3 reaches); repeated for a second 817 to 857 us, with
-// the SM clock.  With K = 64 (130 us) the epilogue is what is left.
+// 709 us, 1,551 TFLOP/s (1,619 is what a library product of 8,192^3 reaches); repeated for a second 817 to 872 us, 1.26 to 1.35
+// PFLOP/s, with the SM clock.  With K = 64 (130 us) the epilogue is what is left.
 #include "async.cuh"
 
 namespace approxifer {

@@ -2,7 +2,8 @@
 // axis split over the CTAs of the cluster.
 //
 //   Y = act(X Wt^T + bias) + R, fp32 accumulators in tensor memory (an fp32 output shows their sums: error against 64
-//   bits 2.2e-7 at K = 784, four times that of elementary fp32 operations; a bfloat16 output hides it).
+//   bits 3.6e-7 at 300 x 1,000 x 784, 1.0e-6 at 300 x 1,000 x 4,096, where elementary fp32 operations err by 2.1e-7 and
+//   6.1e-7; a bfloat16 output hides it).
 //
 // A CTA forms a 128 x BN tile.  The operand whose rows become the 128 lanes of the accumulator is X, or -- SWAP, for few
 // rows of X, where the call is bound by reading Wt -- Wt: the tile is then the transposed one and BN needs only to cover

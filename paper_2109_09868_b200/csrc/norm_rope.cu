@@ -87,7 +87,7 @@ __global__ void __launch_bounds__(kElementThreads) norm_rope_element_kernel(cons
 // it), and the two template parameters (INTER: neighbouring pairs; PARTIAL: some elements are not turned).
 //
 // Measured: 16,384 tokens, 32 + 8 + 8 heads of 128 in bfloat16: 81 us, 5.0 TB/s (a plain copy of as many bytes takes 66);
-// 1,237 tokens, 15 + 5 + 5 heads of 80 in fp32: 5.5 us; one token 2.8 us.  Tried and slower: copying ahead into shared
+// 1,237 tokens, 15 + 5 + 5 heads of 80 in fp32: 5.6 us; one token 2.7 us.  Tried and slower: copying ahead into shared
 // memory by persistent warps (113 us), eight rows in flight (86), two (93).
 constexpr int kMaxWarps = 8;  // units of a token per CTA
 constexpr int kAhead = 4;
