@@ -464,6 +464,137 @@ int approxifer_attention(const approxifer_attention_args* args, void* cuda_strea
  */
 int64_t approxifer_attention_workspace(const approxifer_attention_args* args);
 
+/* norms of approxifer_block_norm */
+#define APPROXIFER_NORM_NONE 0
+#define APPROXIFER_NORM_RMS 1   /* x / sqrt(mean x^2 + eps) * w + bias */
+#define APPROXIFER_NORM_LAYER 2 /* (x - mean x) / sqrt(mean (x - mean x)^2 + eps) * w + bias */
+
+/* activations of a gate */
+#define APPROXIFER_GATE_NONE 0
+#define APPROXIFER_GATE_SIGMOID 1
+#define APPROXIFER_GATE_TANH 2
+
+/*
+ * What lies between two blocks of a layer, in one pass: the norm of a block's output, its gate, its way into the stream of
+ * residuals, and the norm before the next block.  For every token t
+ *     r' = residual_scale * R[t] + block_scale * act(gate) * norm_after(Y[t])          -> R_out[t]
+ *     x  = norm_before(r')                                                             -> X[t]
+ * in fp32, each result rounded once (x is of r' before its rounding).  The norms run over the N elements of a token; their
+ * weights and biases [N] may be NULL (ones, zeros).
+ *   Y     [T][N] or NULL (no block yet: r' = R[t], residual_scale = 1, no gate, after = NONE; R_out is not written)
+ *   gate  by strides: g_rstride = 0 one row for all tokens, g_cstride = 0 one value for all elements of a token (else 1); or NULL
+ *   X     [T][N]; with before = NONE it is not written and may be NULL
+ * R and R_out are of stream_type; Y, gate, weights, biases and X of `type`.  R_out may be R, and X may be Y (same strides); else
+ * outputs overlap nothing.  T = 0 is a valid no-op; 1 <= N <= 16384.  Rows of whole 16 bytes (N a multiple of 8, strides and bases
+ * of 16 bytes) are read and written 16 bytes at a time, others element by element.
+ */
+typedef struct approxifer_block_norm_args {
+  int64_t T;
+  int32_t N, stream_type, type; /* APPROXIFER_TYPE_* */
+  int32_t after, before;        /* APPROXIFER_NORM_* */
+  int32_t gate_activation;      /* APPROXIFER_GATE_* */
+  float residual_scale, block_scale, eps;
+  int32_t reserved;             /* 0 */
+  const void* R;
+  int64_t r_rstride;
+  const void* Y;
+  int64_t y_rstride;
+  const void* gate;
+  int64_t g_rstride, g_cstride;
+  const void* after_weight;
+  const void* after_bias;
+  const void* before_weight;
+  const void* before_bias;
+  void* R_out;
+  int64_t ro_rstride;
+  void* X;
+  int64_t x_rstride;
+} approxifer_block_norm_args;
+int approxifer_block_norm(const approxifer_block_norm_args* args, void* cuda_stream);
+
+/*
+ * The 4-bit microscaled form of an array [M][K] (K a multiple of 32): every 32 neighbours of a row share a scale, a power of two.
+ * With m the largest of their magnitudes and 2^e <= m < 2^(e+1) the scale is 2^(e-2), at least 2^-127 (also where m = 0), and an
+ * element is held as the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (with sign) times the scale: ties go to the even code, what lies
+ * beyond 6 becomes 6.  A group that holds an infinity or a NaN has the scale NaN and zeros for codes.
+ *   codes   [M][K/2] bytes: two elements each, the first in the low half; a code is sign * 8 + the index in the list above.  Rows
+ *           c_rstride bytes apart, a multiple of 16, at a base of 16 bytes
+ *   scales  ceil(M/128) x ceil(K/128) blocks of 512 bytes, at a base of 16 bytes: row r, group g of a block (g of four) at byte
+ *           (r % 32) * 16 + (r / 32) * 4 + g; the byte is the scale's exponent + 127, 255 for NaN.  Rows and groups beyond the array
+ *           are zero (written so by approxifer_mx_quantize; approxifer_mx_linear needs the groups beyond K to be other than 255)
+ * approxifer_mx_quantize reads X and writes codes and scales; approxifer_mx_dequantize reads those and writes X, exactly where
+ * `type` can hold it (nearest otherwise: bfloat16 and fp32 hold all but 6, 4, 3 and 2 times 2^127, which become infinite).
+ */
+typedef struct approxifer_mx_array_args {
+  int64_t M, K;
+  int32_t type;     /* APPROXIFER_TYPE_* of X */
+  int32_t reserved; /* 0 */
+  void* X;          /* [M][K]; only read by approxifer_mx_quantize */
+  int64_t x_rstride;
+  uint8_t* codes;   /* only read by approxifer_mx_dequantize, as are the scales */
+  int64_t c_rstride;
+  uint8_t* scales;
+} approxifer_mx_array_args;
+int approxifer_mx_quantize(const approxifer_mx_array_args* args, void* cuda_stream);
+int approxifer_mx_dequantize(const approxifer_mx_array_args* args, void* cuda_stream);
+
+/*
+ * Matrix product of 4-bit microscaled operands with bias, activation and residual:
+ *     Y[m][n] = act( sum_k Xq[m][k] Wq[n][k] + bias[n] ) + R[m][n],
+ * the sums in fp32, the result rounded once, to out_type.  Wq is held as codes and scales (above).  Xq too, where x_scales is
+ * given; where it is NULL, X is bfloat16 and Xq its 4-bit form, as approxifer_mx_quantize would make it, made within the call.
+ * bias [N] is bfloat16, R and Y are of out_type; bias and R may be NULL; R may be Y itself (same stride).  Y must not overlap any
+ * other operand.  M = 0 is a valid no-op; K a multiple of 32, 1 <= N.  A NaN scale makes NaN of the rows (columns) of its operand.
+ * With X in bfloat16 and more rows than a single pass takes, the 4-bit form goes to the workspace
+ * (approxifer_mx_linear_workspace).
+ */
+typedef struct approxifer_mx_linear_args {
+  int64_t M, N, K;
+  const void* X;           /* [M][K] bfloat16 (any stride of elements) or [M][K/2] codes (stride in bytes, as above) */
+  int64_t x_rstride;
+  const uint8_t* x_scales; /* or NULL */
+  const uint8_t* Wt;       /* [N][K/2] codes */
+  int64_t w_rstride;
+  const uint8_t* w_scales;
+  const uint16_t* bias;
+  const void* R;
+  int64_t r_rstride;
+  void* Y;
+  int64_t y_rstride;
+  int32_t activation; /* APPROXIFER_ACT_* */
+  int32_t out_type;   /* APPROXIFER_TYPE_* of R and Y */
+  void* workspace;    /* device memory, 16-byte aligned; free again when the call's work is done */
+  int64_t workspace_bytes;
+} approxifer_mx_linear_args;
+int approxifer_mx_linear(const approxifer_mx_linear_args* args, void* cuda_stream);
+
+/* Bytes of workspace that approxifer_mx_linear needs for these sizes (pointers but x_scales are not looked at).  Negative:
+ * APPROXIFER_E_*. */
+int64_t approxifer_mx_linear_workspace(const approxifer_mx_linear_args* args);
+
+/*
+ * Attention of a batch of sequences that begin with the same prefix: its keys and values lie in the caches once and are read once
+ * for the batch.  (Where all K queries of a group begin alike, so do the coded queries: the encoder's weights of a coded query sum
+ * to one.)  `own` is as for approxifer_attention, with kv_len, block_table and the positions counted from the prefix's end, window
+ * and sinks 0: for a query at its sequence's own position p >= 0
+ *     out = sum_j softmax_j(scale q.k_j) v_j   over all prefix_len positions of the prefix and the own positions j <= p.
+ * Position j of the prefix lies in page prefix_table[j / page_size], row j % page_size.  A page outside 0 .. num_pages-1, or beyond
+ * its table, holds nothing.  A row with p < 0 (kv_len[b] shorter than the queries) is zero, as is one that sees nothing.
+ * prefix_len = 0 is allowed.  The layouts that approxifer_attention runs on the tensor cores are run so here, in two steps that
+ * meet in own.workspace, which has to hold approxifer_prefix_attention_workspace bytes; others run an element-wise kernel.
+ */
+typedef struct approxifer_prefix_attention_args {
+  approxifer_attention_args own;
+  const int32_t* prefix_table; /* [prefix_pages] */
+  int64_t prefix_pages;
+  int64_t prefix_len;          /* HOST */
+} approxifer_prefix_attention_args;
+int approxifer_prefix_attention(const approxifer_prefix_attention_args* args, void* cuda_stream);
+
+/* Bytes of workspace that approxifer_prefix_attention needs for these arguments (their sizes, alignments and strides; the
+ * workspace itself may be NULL).  Negative: APPROXIFER_E_*. */
+int64_t approxifer_prefix_attention_workspace(const approxifer_prefix_attention_args* args);
+
 /*
  * Test hook (not on the hot path): the weights the kernels use, computed on
  * the device by the same code.

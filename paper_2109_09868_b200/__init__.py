@@ -39,6 +39,11 @@ from .binding import (  # noqa: F401
 )
 from .hosted import (  # noqa: F401
     approxifer_attention,
+    approxifer_block_norm,
     approxifer_linear,
+    approxifer_mx_dequantize,
+    approxifer_mx_linear,
+    approxifer_mx_quantize,
+    approxifer_prefix_attention,
     approxifer_qk_norm_rope,
 )

@@ -54,6 +54,13 @@ EXPORTS = (
     "approxifer_qk_norm_rope",
     "approxifer_attention",
     "approxifer_attention_workspace",
+    "approxifer_block_norm",
+    "approxifer_mx_quantize",
+    "approxifer_mx_dequantize",
+    "approxifer_mx_linear",
+    "approxifer_mx_linear_workspace",
+    "approxifer_prefix_attention",
+    "approxifer_prefix_attention_workspace",
 )
 
 
@@ -152,11 +159,13 @@ def load() -> ctypes.CDLL:
     lib.approxifer_locate_host.restype = c_int
     lib.approxifer_encode_host_static.argtypes = [pp, c_int64, c_int64, c_void_p, c_void_p, c_void_p]
     lib.approxifer_encode_host_static.restype = c_int
-    for name in ("approxifer_linear", "approxifer_qk_norm_rope", "approxifer_attention"):  # (args struct, stream); see hosted.py
+    for name in ("approxifer_linear", "approxifer_qk_norm_rope", "approxifer_attention", "approxifer_block_norm", "approxifer_mx_quantize",
+                 "approxifer_mx_dequantize", "approxifer_mx_linear", "approxifer_prefix_attention"):  # (args struct, stream); see hosted.py
         getattr(lib, name).argtypes = [c_void_p, c_void_p]
         getattr(lib, name).restype = c_int
-    lib.approxifer_attention_workspace.argtypes = [c_void_p]
-    lib.approxifer_attention_workspace.restype = c_int64
+    for name in ("approxifer_attention_workspace", "approxifer_mx_linear_workspace", "approxifer_prefix_attention_workspace"):
+        getattr(lib, name).argtypes = [c_void_p]
+        getattr(lib, name).restype = c_int64
     del pf, pu, pi
     _lib = lib
     return lib

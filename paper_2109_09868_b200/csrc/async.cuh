@@ -16,10 +16,10 @@ namespace approxifer {
 // (A kernel so launched calls wait_for_inputs() in every thread that goes on to read or write global memory, and in at
 // least one of every CTA: what follows it on the stream may count on its end alone.)
 template <typename... Params, typename... Args>
-cudaError_t launch_kernel(void (*kernel)(Params...), dim3 grid, int block, int smem, int cluster, cudaStream_t stream, Args&&... args) {
+cudaError_t launch_kernel(void (*kernel)(Params...), dim3 grid, dim3 block, int smem, int cluster, cudaStream_t stream, Args&&... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
-  cfg.blockDim = dim3(block);
+  cfg.blockDim = block;
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
@@ -37,7 +37,7 @@ cudaError_t launch_kernel(void (*kernel)(Params...), dim3 grid, int block, int s
 template <typename... Params, typename... Args>
 cudaError_t launch_kernel(void (*kernel)(Params...), int64_t grid, int block, int smem, int cluster, cudaStream_t stream, Args&&... args) {
   if (grid > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
-  return launch_kernel(kernel, dim3((unsigned)grid), block, smem, cluster, stream, args...);
+  return launch_kernel(kernel, dim3((unsigned)grid), dim3(block), smem, cluster, stream, args...);
 }
 template <typename... Params, typename... Args>
 cudaError_t launch_kernel(void (*kernel)(Params...), int grid, int block, int smem, int cluster, cudaStream_t stream, Args&&... args) {

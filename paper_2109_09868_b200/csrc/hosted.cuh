@@ -1,8 +1,9 @@
 // Shared declarations of the hosted-model operators (linear, per-head norm with rotary positions, attention over a
-// paged cache).  The C structs of include/approxifer.h are what the launchers take: they hold device pointers and
+// paged cache, also behind a common prefix, norms around a block, 4-bit arrays and their products).  The C structs of include/approxifer.h are what the launchers take: they hold device pointers and
 // strides, already checked by hosted_api.cu.
 #pragma once
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 #include <math_constants.h>
 
 #include "../../include/approxifer.h"
@@ -38,6 +39,15 @@ cudaError_t launch_attention_tile(const approxifer_attention_args& a, cudaStream
 cudaError_t read_attention_tile_wait_timeouts(unsigned int* out);
 cudaError_t reset_attention_tile_wait_timeouts();
 cudaError_t launch_attention(const approxifer_attention_args& a, cudaStream_t stream);
+cudaError_t launch_block_norm(const approxifer_block_norm_args& a, cudaStream_t stream);
+cudaError_t read_block_norm_wait_timeouts(unsigned int* out);
+cudaError_t reset_block_norm_wait_timeouts();
+cudaError_t launch_mx_quantize(const approxifer_mx_array_args& a, cudaStream_t stream);
+cudaError_t launch_mx_dequantize(const approxifer_mx_array_args& a, cudaStream_t stream);
+int64_t mx_linear_workspace(const approxifer_mx_linear_args& a);
+cudaError_t launch_mx_linear(const approxifer_mx_linear_args& a, cudaStream_t stream);
+int64_t prefix_attention_workspace(const approxifer_prefix_attention_args& a);
+cudaError_t launch_prefix_attention(const approxifer_prefix_attention_args& a, cudaStream_t stream);
 
 #ifdef __CUDACC__
 __device__ __forceinline__ float widen(float v) { return v; }
