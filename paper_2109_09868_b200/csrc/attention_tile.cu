@@ -35,6 +35,7 @@
 // instruction caches take well), leaving out the exponentials of keys that no row of a warp sees, one thread to a row, one
 // tile to a CTA at D = 128.
 #include "async.cuh"
+#include "prefix.cuh"
 
 namespace approxifer {
 
@@ -74,9 +75,12 @@ struct TileArgs {
   int32_t group, tokens;  // query heads per key head; tokens per tile (128 / group)
   int32_t blocks;         // query blocks (a CTA's tiles) per sequence
   int32_t page_shift;
+  PrefixParts prior;      // kOverPrefix: to write; kBehindPrefix: to join
+  int32_t prefix_last;    // kOverPrefix: the prefix's last position
 };
 
-// What the CTA works on; all roles derive it alike.
+// What the CTA works on; all roles derive it alike.  FLAT: all rows stand at the same position.
+template <bool FLAT>
 struct Job {
   int b, hk, token0;   // first token (in the packed array)
   int left;            // tokens of the sequence from there on
@@ -87,10 +91,12 @@ struct Job {
   int sink_tiles, first_tile;
   int skip, steps;       // this CTA's steps of the cluster's: from `skip` on
   int steps0, steps1;  // of the two query tiles
+  int piece;           // (over a prefix) which part of it
 
   __device__ __forceinline__ int tile(int j) const { return j + skip < sink_tiles ? j + skip : first_tile + (j + skip - sink_tiles); }
-  __device__ __forceinline__ int first_pos(int t) const { return pos0 + t * tokens; }
-  __device__ __forceinline__ int last_pos(int t) const { return pos0 + min((t + 1) * tokens, left) - 1; }
+  __device__ __forceinline__ int pos_of(int token) const { return FLAT ? pos0 : pos0 + token; }
+  __device__ __forceinline__ int first_pos(int t) const { return pos_of(t * tokens); }
+  __device__ __forceinline__ int last_pos(int t) const { return pos_of(min((t + 1) * tokens, left) - 1); }
   // Which steps a query tile takes part in: tile 0 up to the last key its rows see, tile 1 all (the window of its first row
   // may start a tile or two later than tile 0's; there it finds nothing).
   __device__ __forceinline__ int steps_of(int t) const { return t == 0 ? steps0 : steps1; }
@@ -127,7 +133,29 @@ __device__ __forceinline__ uint32_t pages_of(uint32_t there, int c, int page_shi
 }
 
 template <int TQ>
-__device__ __forceinline__ bool find_job(const TileArgs& g, int S, int rank, Job* job) {
+__device__ __forceinline__ bool find_job(const TileArgs& g, int S, int rank, Job<true>* job) {  // over a common prefix
+  const approxifer_attention_args& a = g.a;
+  // of every key head and query block so many parts of the prefix, of the last block, if it has one tile only, fewer
+  const int per_head = (g.blocks - 1) * g.prior.parts + g.prior.last_parts;
+  const int x = blockIdx.x / S, in_head = x % per_head, block = min(in_head / g.prior.parts, g.blocks - 1);
+  const int part = in_head - block * g.prior.parts, parts = block == g.blocks - 1 ? g.prior.last_parts : g.prior.parts;
+  job->hk = x / per_head;
+  job->b = 0;
+  job->piece = part;
+  job->tokens = g.tokens;
+  job->token0 = block * TQ * g.tokens;
+  job->left = (int)a.T - job->token0;
+  job->pos0 = job->p1 = g.prefix_last;
+  job->window = job->sinks = job->lo = job->sink_tiles = job->first_tile = 0;
+  const int steps = job->p1 / kKeys + 1;
+  job->skip = (int)((int64_t)steps * (part * S + rank) / (parts * S));
+  job->steps = job->steps0 = (int)((int64_t)steps * (part * S + rank + 1) / (parts * S)) - job->skip;
+  job->steps1 = TQ == 2 && job->tokens < job->left ? job->steps : 0;
+  return true;
+}
+
+template <int TQ>
+__device__ __forceinline__ bool find_job(const TileArgs& g, int S, int rank, Job<false>* job) {
   const approxifer_attention_args& a = g.a;
   // blocks of late queries see most: they come first
   int x = blockIdx.x / S;
@@ -206,15 +234,19 @@ struct Item {
   int t, j;
   bool first, last;
 };
-template <int TQ>
-__device__ __forceinline__ Item item_at(const Job& job, int n) {
+template <int TQ, bool FLAT>
+__device__ __forceinline__ Item item_at(const Job<FLAT>& job, int n) {
   if (TQ == 1) return {0, n, true, true};
   const int both = min(job.steps0, job.steps1);
   if (n < 2 * both) return {n & 1, n >> 1, (n & 1) == 0, (n & 1) == 1};
   return {job.steps1 > 0 ? 1 : 0, n - both, true, true};
 }
 
-template <int DP, bool CLUSTER>
+// kOverPrefix: all tokens over the common prefix, into partial results; kBehindPrefix: tokens over their sequences' own keys, joined
+// with those.
+enum Form { kPlain, kOverPrefix, kBehindPrefix };
+
+template <int DP, bool CLUSTER, Form FORM>
 __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
     attention_tile_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
                           const __grid_constant__ TileArgs g) {
@@ -257,10 +289,15 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
     prefetch_map(&k_map);
     prefetch_map(&v_map);
   }
-  wait_for_inputs();
-  Job job;
+  // (Behind a prefix: the kernel before this one lets it start only once it has waited for what came before, so the call's inputs
+  // are there; what that kernel leaves is waited for where it is needed, and by each CTA.)
+  if constexpr (FORM != kBehindPrefix) wait_for_inputs();
+  Job<FORM == kOverPrefix> job;
   const int S = CLUSTER ? (int)cluster_size() : 1, rank = CLUSTER ? (int)cluster_rank() : 0;
-  if (!find_job<TQ>(g, S, rank, &job)) return;  // (all CTAs of a cluster or none)
+  if (!find_job<TQ>(g, S, rank, &job)) {  // (all CTAs of a cluster or none)
+    if constexpr (FORM == kBehindPrefix) wait_for_inputs();
+    return;
+  }
   // (copies) the page of this lane's rows of a key tile, looked up a tile ahead
   const int32_t* table = a.block_table + (int64_t)job.b * a.table_stride;
   const int page_rows = 1 << g.page_shift, rows = min(page_rows, kKeys), per_tile = kKeys / rows;
@@ -301,7 +338,7 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
     };
     const int in_tile = r / g.group, token = t * job.tokens + in_tile;
     const bool mine = in_tile < job.tokens && token < job.left;
-    const int pos = job.pos0 + token;
+    const int pos = job.pos_of(token);
     const bool flip = a.scale < 0.f;  // the running maximum is that of sign(scale) S
     // (of a zero scale just enough is left to keep what a row does not see at minus infinity)
     const float scale = fmaxf(fabsf(a.scale) * 1.4426950408889634f, 1e-37f);
@@ -409,10 +446,21 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
       tmem_fence_after();
     }
     if constexpr (CLUSTER) softmax_warps_meet<TQ>();  // no product reads shared memory any more, of either tile
+    if constexpr (FORM == kBehindPrefix) wait_for_inputs();
     if (ok) {
       // One CTA: O / sum, by way of the tile's queries' place in shared memory (a warp keeps to its own rows and columns) into
       // whole rows.  A cluster: O as it is into shared memory, with the row's maximum and sum.
-      const float inv = CLUSTER ? 1.f : l == 0.f ? 0.f : 1.f / l;
+      float inv = CLUSTER || FORM == kOverPrefix ? 1.f : l == 0.f ? 0.f : 1.f / l;
+      const int64_t row_at = (int64_t)(job.token0 + token) * a.Hq + job.hk * g.group + r % g.group;  // (of the partial results)
+      PriorRow prior;
+      if constexpr (FORM == kBehindPrefix && !CLUSTER) {
+        prior.parts = 0;
+        if (mine && pos >= 0) {
+          prior.load(g.prior, row_at, job.token0 + token);
+          const float own = prior.weigh(m == -CUDART_INF_F ? m : m * scale, l);
+          inv = l == 0.f ? 0.f : own;
+        }
+      }
       const bool add_back = *poison != 0;
       unsigned char* own_rows = base + 1024 + t * kTile + (half * 4 + quarter) * 32 * kOut * 2;
       constexpr int kCols = kOut / 8;  // 16-byte columns
@@ -452,10 +500,17 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
             }
           }
         }
+        if constexpr (FORM == kBehindPrefix && !CLUSTER) prior.template add<16>(g.prior, row_at, DP, half * kOut + c, y);
         if constexpr (CLUSTER) {
 #pragma unroll
           for (int i = 0; i < 16; i += 4)
             part_rows[(t * kRows + r) * (DP / 4) + (((half * kOut + c + i) / 4) ^ (r & 7))] = make_float4(y[i], y[i + 1], y[i + 2], y[i + 3]);
+        } else if constexpr (FORM == kOverPrefix) {
+          if (mine) {
+            float4* to = reinterpret_cast<float4*>(g.prior.o + (job.piece * g.prior.rows + row_at) * DP + half * kOut + c);
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) to[i / 4] = make_float4(y[i], y[i + 1], y[i + 2], y[i + 3]);
+          }
         } else {
 #pragma unroll
           for (int i = 0; i < 16; i += 8)
@@ -464,9 +519,10 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
         }
         __syncwarp();
       }
+      if (FORM == kOverPrefix && !CLUSTER && mine && half == 0) g.prior.ml[job.piece * g.prior.rows + row_at] = make_float2(m == -CUDART_INF_F ? m : m * scale, l);
       const int64_t to = mine ? (int64_t)(job.token0 + token) * a.o_tstride + (int64_t)(job.hk * g.group + r % g.group) * a.o_hstride : -1;
 #pragma unroll 4
-      for (int x = lane; !CLUSTER && x < 32 * kCols; x += 32) {
+      for (int x = lane; !CLUSTER && FORM != kOverPrefix && x < 32 * kCols; x += 32) {
         const int row = x / kCols, col = x % kCols, d = half * kOut + col * 8;
         const int64_t at = __shfl_sync(0xffffffffu, to, row);
         if (at >= 0 && d < a.D)
@@ -656,7 +712,31 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
             y[0] = fmaf(k, v.x, y[0]), y[1] = fmaf(k, v.y, y[1]);
           }
         }
-        const float inv = total == 0.f ? 0.f : 1.f / total;
+        const int64_t row_at = (int64_t)(job.token0 + token) * a.Hq + job.hk * g.group + r % g.group;
+        if constexpr (FORM == kOverPrefix) {
+          float* to = g.prior.o + (job.piece * g.prior.rows + row_at) * DP + c;
+          if constexpr (DP == 128) *reinterpret_cast<float4*>(to) = make_float4(y[0], y[1], y[2], y[3]);
+          else *reinterpret_cast<float2*>(to) = make_float2(y[0], y[1]);
+          if (lane == 0) g.prior.ml[job.piece * g.prior.rows + row_at] = make_float2(total == 0.f ? -CUDART_INF_F : best * scale, total);
+          continue;
+        }
+        float inv = total == 0.f ? 0.f : 1.f / total;
+        if constexpr (FORM == kBehindPrefix) {
+          PriorRow prior;
+          prior.parts = 0;
+          if (job.pos_of(token) >= 0) {
+            prior.load(g.prior, row_at, job.token0 + token);
+            const float own = prior.weigh(total == 0.f ? -CUDART_INF_F : best * scale, total);
+            inv = total == 0.f ? 0.f : own;
+          }
+#pragma unroll
+          for (int i = 0; i < DP / 32; ++i) y[i] *= inv;
+          inv = 1.f;
+          float z[DP / 32] = {};
+          prior.template add<DP / 32>(g.prior, row_at, DP, c, z);
+#pragma unroll
+          for (int i = 0; i < DP / 32; ++i) y[i] += z[i];
+        }
         bf16* out = reinterpret_cast<bf16*>(a.out) + (int64_t)(job.token0 + token) * a.o_tstride + (int64_t)(job.hk * g.group + r % g.group) * a.o_hstride + c;
         if (c < a.D) {
           if constexpr (DP == 128) *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(y[0] * inv, y[1] * inv), pack_bf16x2(y[2] * inv, y[3] * inv));
@@ -668,22 +748,23 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
   }
 }
 
-template <int DP, bool CLUSTER>
+template <int DP, bool CLUSTER, Form FORM>
 cudaError_t launch_split(const TileArgs& g, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const DeviceInfo& dev, int64_t ctas, int split,
                          cudaStream_t stream) {
-  auto kernel = attention_tile_kernel<DP, CLUSTER>;
+  auto kernel = attention_tile_kernel<DP, CLUSTER, FORM>;
   struct Tag {};
   const cudaError_t e = ensure_dynamic_smem<Tag>(kernel, dev.ordinal, smem_bytes(DP));
   if (e != cudaSuccess) return e;
   return launch_kernel(kernel, ctas * split, threads_of(DP), smem_bytes(DP), split, stream, q, k, v, g);
 }
 
-template <int DP>
-cudaError_t launch_one(const TileArgs& g, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, cudaStream_t stream) {
-  const DeviceInfo* dev;
-  const cudaError_t e = current_device_info(&dev);
-  if (e != cudaSuccess) return e;
+template <int DP, Form FORM>
+cudaError_t launch_one(const TileArgs& g, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const DeviceInfo& dev, cudaStream_t stream) {
   const approxifer_attention_args& a = g.a;
+  if constexpr (FORM == kOverPrefix) {
+    const int64_t ctas = ((int64_t)(g.blocks - 1) * g.prior.parts + g.prior.last_parts) * a.Hkv;
+    return launch_split<DP, false, FORM>(g, q, k, v, dev, ctas, 1, stream);
+  }
   const int64_t ctas = (int64_t)g.blocks * a.batch * a.Hkv;
   // Few query blocks: as many CTAs to each, along the keys, as the GPU holds, each with three tiles of keys or more.  (The
   // lengths are on the device: what a block can see at most says how far it is worth cutting.)  Measured, one CTA a block
@@ -691,10 +772,41 @@ cudaError_t launch_one(const TileArgs& g, const CUtensorMap& q, const CUtensorMa
   // 2,048, 2 heads of 128: 38 / 22; 80 blocks of 64 cut in two for two CTAs on every SM: 31 / 35, hence one CTA to an SM.
   int64_t most = a.table_pages * a.page_size;
   if (a.window && (int64_t)a.window + a.max_q + a.sinks < most) most = (int64_t)a.window + a.max_q + a.sinks;
-  const int held = dev->sms * 3 / 4;
+  const int held = dev.sms * 3 / 4;
   int split = 1;
   while (split < kMaxSplit && ctas * split * 2 <= held && most >= (int64_t)split * 2 * 3 * kKeys) split *= 2;
-  return split > 1 ? launch_split<DP, true>(g, q, k, v, *dev, ctas, split, stream) : launch_split<DP, false>(g, q, k, v, *dev, ctas, 1, stream);
+  return split > 1 ? launch_split<DP, true, FORM>(g, q, k, v, dev, ctas, split, stream) : launch_split<DP, false, FORM>(g, q, k, v, dev, ctas, 1, stream);
+}
+
+// Tensor maps, and the launch.
+template <Form FORM>
+cudaError_t launch_form(const TileArgs& g, const DeviceInfo& dev, cudaStream_t stream) {
+  const approxifer_attention_args& a = g.a;
+  CUtensorMap q, k, v;
+  const uint64_t qe[3] = {(uint64_t)a.D, (uint64_t)a.Hq, (uint64_t)a.T}, qs[3] = {1, (uint64_t)a.q_hstride, (uint64_t)a.q_tstride};
+  const uint32_t qb[3] = {64, (uint32_t)g.group, (uint32_t)g.tokens};
+  const uint64_t ce[4] = {(uint64_t)a.D, (uint64_t)a.page_size, (uint64_t)a.Hkv, (uint64_t)a.num_pages};
+  const uint64_t kst[4] = {1, (uint64_t)a.kc_rstride, (uint64_t)a.kc_hstride, (uint64_t)a.kc_pstride};
+  const uint64_t vst[4] = {1, (uint64_t)a.vc_rstride, (uint64_t)a.vc_hstride, (uint64_t)a.vc_pstride};
+  const uint32_t cb[4] = {64, (uint32_t)(a.page_size < kKeys ? a.page_size : kKeys), 1, 1};
+  cudaError_t e;
+  if ((e = make_tensor_map(&q, a.q, 3, qe, qs, qb)) != cudaSuccess || (e = make_tensor_map(&k, a.k_cache, 4, ce, kst, cb)) != cudaSuccess ||
+      (e = make_tensor_map(&v, a.v_cache, 4, ce, vst, cb)) != cudaSuccess)
+    return e;
+  return a.D <= 64 ? launch_one<64, FORM>(g, q, k, v, dev, stream) : launch_one<128, FORM>(g, q, k, v, dev, stream);
+}
+
+int padded_head(const approxifer_attention_args& a) { return a.D <= 64 ? 64 : 128; }
+TileArgs tile_args(const approxifer_attention_args& a) {
+  TileArgs g{};
+  g.a = a;
+  if (g.a.max_q > a.T) g.a.max_q = (int32_t)a.T;  // (no sequence has more queries than the call: a loose bound launches no CTAs for nothing)
+  g.group = a.Hq / a.Hkv;
+  g.tokens = kRows / g.group;
+  const int per_cta = tiles_of(padded_head(a)) * g.tokens;
+  g.blocks = (int)(((int64_t)g.a.max_q + per_cta - 1) / per_cta);
+  g.page_shift = exact_log2(a.page_size);
+  return g;
 }
 
 }  // namespace
@@ -715,27 +827,53 @@ bool attention_tile_eligible(const approxifer_attention_args& a) {
 }
 
 cudaError_t launch_attention_tile(const approxifer_attention_args& a, cudaStream_t stream) {
-  TileArgs g{};
-  g.a = a;
-  if (g.a.max_q > a.T) g.a.max_q = (int32_t)a.T;  // (no sequence has more queries than the call: a loose bound launches no CTAs for nothing)
-  g.group = a.Hq / a.Hkv;
-  g.tokens = kRows / g.group;
-  const int per_cta = tiles_of(a.D <= 64 ? 64 : 128) * g.tokens;
-  g.blocks = (int)(((int64_t)g.a.max_q + per_cta - 1) / per_cta);
-  g.page_shift = exact_log2(a.page_size);
-  const int dp = a.D <= 64 ? 64 : 128;
-  CUtensorMap q, k, v;
-  const uint64_t qe[3] = {(uint64_t)a.D, (uint64_t)a.Hq, (uint64_t)a.T}, qs[3] = {1, (uint64_t)a.q_hstride, (uint64_t)a.q_tstride};
-  const uint32_t qb[3] = {64, (uint32_t)g.group, (uint32_t)g.tokens};
-  const uint64_t ce[4] = {(uint64_t)a.D, (uint64_t)a.page_size, (uint64_t)a.Hkv, (uint64_t)a.num_pages};
-  const uint64_t kst[4] = {1, (uint64_t)a.kc_rstride, (uint64_t)a.kc_hstride, (uint64_t)a.kc_pstride};
-  const uint64_t vst[4] = {1, (uint64_t)a.vc_rstride, (uint64_t)a.vc_hstride, (uint64_t)a.vc_pstride};
-  const uint32_t cb[4] = {64, (uint32_t)(a.page_size < kKeys ? a.page_size : kKeys), 1, 1};
-  cudaError_t e;
-  if ((e = make_tensor_map(&q, a.q, 3, qe, qs, qb)) != cudaSuccess || (e = make_tensor_map(&k, a.k_cache, 4, ce, kst, cb)) != cudaSuccess ||
-      (e = make_tensor_map(&v, a.v_cache, 4, ce, vst, cb)) != cudaSuccess)
-    return e;
-  return dp == 64 ? launch_one<64>(g, q, k, v, stream) : launch_one<128>(g, q, k, v, stream);
+  const DeviceInfo* dev;
+  const cudaError_t e = current_device_info(&dev);
+  return e != cudaSuccess ? e : launch_form<kPlain>(tile_args(a), *dev, stream);
+}
+
+// The parts that the prefix is cut into.  All CTAs of a turn run at once; a CTA's time is that of its steps and some four more for
+// its start and end, and every part is written and read once more by those who join them.
+PrefixParts prefix_parts(const approxifer_prefix_attention_args& p, const DeviceInfo& dev) {
+  const approxifer_attention_args& a = p.own;
+  const int dp = padded_head(a), tiles = tiles_of(dp), tokens = kRows / (a.Hq / a.Hkv), per_cta = tiles * tokens;
+  const int64_t blocks = (a.T + per_cta - 1) / per_cta, places = (int64_t)dev.sms * (3 - tiles);
+  const int64_t room = p.prefix_pages * a.page_size, steps = ((p.prefix_len < room ? p.prefix_len : room) + kKeys - 1) / kKeys;
+  const bool half = tiles == 2 && a.T - (blocks - 1) * per_cta <= tokens;  // the last block has one tile
+  PrefixParts best{};
+  best.rows = a.T * a.Hq;
+  const double join = (double)best.rows * dp * 8 / 5e12 / (dp == 128 ? 2.3e-6 : 1.2e-6);  // in steps
+  double least = 0;
+  for (int64_t n = 1; n <= steps && n <= 64; ++n) {
+    const int64_t last = half && n > 1 ? (2 * n + 2) / 3 : n;
+    const int64_t turns = (((blocks - 1) * n + last) * a.Hkv + places - 1) / places;
+    const double time = turns * ((double)steps / n + 4) + n * join;
+    if (best.parts == 0 || time < least) least = time, best.parts = (int32_t)n, best.last_parts = (int32_t)last;
+  }
+  best.last_token = (blocks - 1) * per_cta;
+  return best;
+}
+
+cudaError_t launch_attention_over_prefix(const approxifer_prefix_attention_args& p, const PrefixParts& parts, cudaStream_t stream) {
+  const DeviceInfo* dev;
+  const cudaError_t e = current_device_info(&dev);
+  if (e != cudaSuccess) return e;
+  approxifer_attention_args a = p.own;
+  a.batch = 1, a.max_q = (int32_t)a.T, a.block_table = p.prefix_table, a.table_pages = p.prefix_pages, a.table_stride = 0;
+  TileArgs g = tile_args(a);
+  g.prior = parts;
+  const int64_t room = p.prefix_pages * a.page_size;
+  g.prefix_last = (int32_t)((p.prefix_len < room ? p.prefix_len : room) - 1);
+  return launch_form<kOverPrefix>(g, *dev, stream);
+}
+
+cudaError_t launch_attention_tile_behind(const approxifer_attention_args& a, const PrefixParts& parts, cudaStream_t stream) {
+  const DeviceInfo* dev;
+  const cudaError_t e = current_device_info(&dev);
+  if (e != cudaSuccess) return e;
+  TileArgs g = tile_args(a);
+  g.prior = parts;
+  return launch_form<kBehindPrefix>(g, *dev, stream);
 }
 
 }  // namespace approxifer

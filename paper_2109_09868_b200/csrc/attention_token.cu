@@ -18,6 +18,7 @@
 // another, the joining); 48 tokens, window 4,096: 134 us, 6.0 TB/s, from a graph, 142 to 145 us, 5.6 TB/s, call by call; 4
 // contexts of up to 131,072, 2 key heads of 64: 43 us, 4.6 TB/s (the joining of 148 partial results a unit is 5 us of it).
 #include "async.cuh"
+#include "prefix.cuh"
 
 namespace approxifer {
 namespace {
@@ -72,6 +73,7 @@ struct Seen {
   const int32_t* table;
   int32_t first, last, sinks;
   int32_t token;  // its index, or -1 where the sequence has no new token (max_q = 1)
+  bool placed;    // (behind a prefix) it has a position of its own
   int32_t sink_chunks, skip, chunks;
   __device__ __forceinline__ int32_t position(int c, int keys) const { return (c < sink_chunks ? c : c + skip) * keys; }
   // which of the keys of the chunk at `pos` are seen, a bit per key
@@ -86,6 +88,7 @@ __device__ __forceinline__ Seen seen_by(const approxifer_attention_args& a, int 
   s.token = live ? t : -1;
   const int64_t held = a.table_pages * a.page_size;
   const int p = live ? __ldg(a.kv_len + b) - 1 : -1;
+  s.placed = p >= 0;
   s.last = p < held ? p : (int)held - 1;
   s.first = a.window && p >= a.window ? p - a.window + 1 : 0;
   s.sinks = a.sinks < s.first ? a.sinks : s.first;
@@ -302,14 +305,16 @@ __device__ __forceinline__ Joined join(const float2 (&ml)[N], const float2 (&v)[
   return j;
 }
 
-template <int DP, bool WHOLE>
+// BEHIND (here and below): the row's partial results over a common prefix are joined in.  The kernel before, which makes them, lets
+// this one start only once it has waited for what came before it: the call's inputs are there from the start.
+template <int DP, bool WHOLE, bool BEHIND>
 __global__ void __launch_bounds__(kThreads, kCtasPerSm) attention_token_cluster_kernel(const __grid_constant__ approxifer_attention_args a, int row_tiles,
-                                                                                        int page_shift) {
+                                                                                        int page_shift, const __grid_constant__ PrefixParts prior) {
   extern __shared__ __align__(1024) unsigned char smem[];
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const int S = (int)cluster_size(), rank = (int)cluster_rank();
   let_next_start();
-  wait_for_inputs();
+  if constexpr (!BEHIND) wait_for_inputs();
   int unit = blockIdx.x / S;
   const int rt = unit % row_tiles;
   unit /= row_tiles;
@@ -372,6 +377,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) attention_token_cluster_
   }
   if (S > 1) cluster_sync();
   else __syncthreads();
+  if constexpr (BEHIND) wait_for_inputs();
   bf16* out = reinterpret_cast<bf16*>(a.out) + (int64_t)seen.token * a.o_tstride + (int64_t)head0 * a.o_hstride;
   const int x0 = cells * rank / S, x1 = cells * (rank + 1) / S;
   for (int x = x0 + threadIdx.x; x < x1; x += kThreads) {
@@ -383,8 +389,22 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) attention_token_cluster_
       if (p < S) ml[p] = peer_load2(peer_smem(smem_addr(cta_ml + r), p)), v[p] = peer_load2(peer_smem(smem_addr(cta_o + r * (DP / 2) + d), p));
     }
     const Joined j = join<kMaxSplit>(ml, v);
-    const float inv = j.l == 0.f ? 0.f : 1.f / j.l;
-    *reinterpret_cast<uint32_t*>(out + (int64_t)r * a.o_hstride + 2 * d) = j.l == 0.f ? 0u : pack_bf16x2(j.v.x * inv, j.v.y * inv);
+    float inv = j.l == 0.f ? 0.f : 1.f / j.l, y[2];
+    if constexpr (BEHIND) {
+      PriorRow before;
+      before.parts = 0;
+      const int64_t row_at = (int64_t)seen.token * a.Hq + head0 + r;
+      if (seen.placed) {
+        before.load(prior, row_at, seen.token);
+        const float own = before.weigh(j.m, j.l);
+        inv = j.l == 0.f ? 0.f : own;
+      }
+      y[0] = j.l == 0.f ? 0.f : j.v.x * inv, y[1] = j.l == 0.f ? 0.f : j.v.y * inv;
+      before.add<2>(prior, row_at, DP, 2 * d, y);
+    } else {
+      y[0] = j.l == 0.f ? 0.f : j.v.x * inv, y[1] = j.l == 0.f ? 0.f : j.v.y * inv;
+    }
+    *reinterpret_cast<uint32_t*>(out + (int64_t)r * a.o_hstride + 2 * d) = pack_bf16x2(y[0], y[1]);
   }
   if (S > 1) cluster_sync();  // (a CTA's shared memory stays until all have read it)
 }
@@ -444,18 +464,21 @@ struct Cursor {
   }
 };
 
-template <int DP, bool WHOLE>
+template <int DP, bool WHOLE, bool BEHIND>
 __global__ void __launch_bounds__(kThreads, 3) attention_token_balanced_kernel(const __grid_constant__ approxifer_attention_args a, int row_tiles,
-                                                                                         int page_shift, float* partial) {
+                                                                                         int page_shift, float* partial, const __grid_constant__ PrefixParts prior) {
   extern __shared__ __align__(1024) unsigned char smem[];
   const int warp = blockIdx.x * kWarps + threadIdx.x / 32, warps = gridDim.x * kWarps, lane = threadIdx.x % 32;
   const int units = a.Hkv * row_tiles, group = a.Hq / a.Hkv;
-  wait_for_inputs();
+  if constexpr (!BEHIND) wait_for_inputs();
   let_next_start();  // (only now: the kernel that joins counts the chunks, from the call's inputs, before it waits for this one)
   Place at;
   const int64_t total = count_chunks(a, units, keys_of(DP), 0, 0, &at);
   const int runs = total < warps ? (int)total : warps;  // (no empty runs)
-  if (warp >= runs) return;
+  if (warp >= runs) {
+    if constexpr (BEHIND) wait_for_inputs();
+    return;
+  }
   const int64_t x0 = total * warp / runs, x1 = total * (warp + 1) / runs;
   count_chunks(a, units, keys_of(DP), x0, 0, &at);
   Cursor get, use;
@@ -507,8 +530,28 @@ __global__ void __launch_bounds__(kThreads, 3) attention_token_balanced_kernel(c
     if (whole || x + 1 == x1) {  // the end of the unit or of the run
       w.finish();
       if (whole && from_start) {
-        const float inv[2] = {w.l[0] == 0.f ? 0.f : 1.f / w.l[0], w.l[1] == 0.f ? 0.f : 1.f / w.l[1]};
+        float inv[2] = {w.l[0] == 0.f ? 0.f : 1.f / w.l[0], w.l[1] == 0.f ? 0.f : 1.f / w.l[1]};
         bf16* out = reinterpret_cast<bf16*>(a.out) + (int64_t)use.seen.token * a.o_tstride + (int64_t)head0 * a.o_hstride;
+        if constexpr (BEHIND) {
+          wait_for_inputs();
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int r = lane / 4 + h * 8;
+            if (r >= rows) continue;
+            PriorRow before;
+            const int64_t row_at = (int64_t)use.seen.token * a.Hq + head0 + r;
+            before.load(prior, row_at, use.seen.token);
+            const float own = before.weigh(w.m[h], w.l[h]);
+            inv[h] = w.l[h] == 0.f ? 0.f : own;
+#pragma unroll
+            for (int d = 0; d < DP / 8; ++d) {
+              float y[2] = {w.l[h] == 0.f ? 0.f : w.o[d][2 * h] * inv[h], w.l[h] == 0.f ? 0.f : w.o[d][2 * h + 1] * inv[h]};
+              before.add<2>(prior, row_at, DP, d * 8 + (lane % 4) * 2, y);
+              w.o[d][2 * h] = y[0], w.o[d][2 * h + 1] = y[1];
+            }
+            inv[h] = 1.f;
+          }
+        }
 #pragma unroll
         for (int d = 0; d < DP / 8; ++d)
 #pragma unroll
@@ -516,7 +559,7 @@ __global__ void __launch_bounds__(kThreads, 3) attention_token_balanced_kernel(c
             const int r = lane / 4 + h * 8, col = d * 8 + (lane % 4) * 2;
             if (r < rows && col < a.D)
               *reinterpret_cast<uint32_t*>(out + (int64_t)r * a.o_hstride + col) =
-                  w.l[h] == 0.f ? 0u : pack_bf16x2(w.o[d][2 * h] * inv[h], w.o[d][2 * h + 1] * inv[h]);
+                  !BEHIND && w.l[h] == 0.f ? 0u : pack_bf16x2(w.o[d][2 * h] * inv[h], w.o[d][2 * h + 1] * inv[h]);
           }
       } else {
         const int64_t part = 2 * (int64_t)warp + (from_start ? 1 : 0);
@@ -546,14 +589,15 @@ __global__ void __launch_bounds__(kThreads, 3) attention_token_balanced_kernel(c
     }
   }
   copy_wait<0>();
+  if constexpr (BEHIND) wait_for_inputs();
 }
 
 // Joins the partial results of every unit that more than one run shares, and zeroes the rows that see nothing.  One CTA =
 // one row; its warps (for short rows their halves) take the partial results in turn, kJoinAhead loads in flight, and meet in
 // shared memory.
-template <int DP, int JW>
+template <int DP, int JW, bool BEHIND>
 __global__ void __launch_bounds__(JW * 32) attention_token_join_kernel(const __grid_constant__ approxifer_attention_args a, int row_tiles, int warps,
-                                                                              const float* partial) {
+                                                                              const float* partial, const __grid_constant__ PrefixParts prior) {
   constexpr int kLanes = DP / 4, kTeams = JW * 32 / kLanes;  // lanes to a partial row, partial rows at a time
   __shared__ __align__(16) float sy[kTeams][DP];
   __shared__ float sm[kTeams], sl[kTeams];
@@ -567,8 +611,17 @@ __global__ void __launch_bounds__(JW * 32) attention_token_join_kernel(const __g
   wait_for_inputs();
   if (seen.token < 0) return;
   bf16* out = reinterpret_cast<bf16*>(a.out) + (int64_t)seen.token * a.o_tstride + (int64_t)h * a.o_hstride;
+  PriorRow before;
+  before.parts = 0;
+  const int64_t row_at = (int64_t)seen.token * a.Hq + h;
+  if (BEHIND && seen.placed) before.load(prior, row_at, seen.token);
   if (seen.chunks == 0) {
-    for (int d = threadIdx.x; d < a.D; d += JW * 32) out[d] = narrow<bf16>(0.f);
+    if (BEHIND && seen.placed) before.weigh(-CUDART_INF_F, 0.f);
+    for (int d = threadIdx.x; d < a.D; d += JW * 32) {
+      float y[1] = {0.f};
+      if constexpr (BEHIND) before.add<1>(prior, row_at, DP, d, y);
+      out[d] = narrow<bf16>(y[0]);
+    }
     return;
   }
   const int64_t x0 = at.before + (int64_t)((h / group) * row_tiles + in_group / kRows) * seen.chunks, x1 = x0 + seen.chunks;
@@ -622,7 +675,15 @@ __global__ void __launch_bounds__(JW * 32) attention_token_join_kernel(const __g
       sum = fmaf(k, sl[w], sum);
       z = fmaf(k, sy[w][d], z);
     }
-    out[d] = narrow<bf16>(sum == 0.f ? 0.f : z / sum);
+    if constexpr (BEHIND) {
+      PriorRow all = before;
+      const float own = all.weigh(sum == 0.f ? -CUDART_INF_F : best, sum);
+      float y[1] = {sum == 0.f ? 0.f : z * own};
+      all.add<1>(prior, row_at, DP, d, y);
+      out[d] = narrow<bf16>(y[0]);
+    } else {
+      out[d] = narrow<bf16>(sum == 0.f ? 0.f : z / sum);
+    }
   }
 }
 
@@ -632,28 +693,29 @@ int64_t most_seen(const approxifer_attention_args& a) {
   return a.window && (int64_t)a.window + a.sinks < held ? (int64_t)a.window + a.sinks : held;
 }
 int64_t units_of(const approxifer_attention_args& a) { return (int64_t)a.batch * a.Hkv * ((a.Hq / a.Hkv + kRows - 1) / kRows); }
-template <int DP, bool WHOLE>
-cudaError_t launch_cluster(const approxifer_attention_args& a, const DeviceInfo& dev, int row_tiles, int page_shift, int64_t units, int split, cudaStream_t stream) {
-  auto kernel = attention_token_cluster_kernel<DP, WHOLE>;
+template <int DP, bool WHOLE, bool BEHIND>
+cudaError_t launch_cluster(const approxifer_attention_args& a, const PrefixParts& prior, const DeviceInfo& dev, int row_tiles, int page_shift, int64_t units, int split,
+                           cudaStream_t stream) {
+  auto kernel = attention_token_cluster_kernel<DP, WHOLE, BEHIND>;
   struct Tag {};
   cudaError_t e = ensure_dynamic_smem<Tag>(kernel, dev.ordinal, smem_bytes(DP));
   if (e != cudaSuccess) return e;
-  return launch_kernel(kernel, units * split, kThreads, smem_bytes(DP), split, stream, a, row_tiles, page_shift);
+  return launch_kernel(kernel, units * split, kThreads, smem_bytes(DP), split, stream, a, row_tiles, page_shift, prior);
 }
 
-template <int DP, bool WHOLE>
-cudaError_t launch_balanced(const approxifer_attention_args& a, const DeviceInfo& dev, int row_tiles, int page_shift, cudaStream_t stream) {
-  auto kernel = attention_token_balanced_kernel<DP, WHOLE>;
+template <int DP, bool WHOLE, bool BEHIND>
+cudaError_t launch_balanced(const approxifer_attention_args& a, const PrefixParts& prior, const DeviceInfo& dev, int row_tiles, int page_shift, cudaStream_t stream) {
+  auto kernel = attention_token_balanced_kernel<DP, WHOLE, BEHIND>;
   struct Tag {};
   cudaError_t e = ensure_dynamic_smem<Tag>(kernel, dev.ordinal, smem_bytes(DP));
   if (e != cudaSuccess) return e;
   const int ctas = dev.sms * kCtasPerSm;
   float* partial = static_cast<float*>(a.workspace);
-  if ((e = launch_kernel(kernel, ctas, kThreads, smem_bytes(DP), 1, stream, a, row_tiles, page_shift, partial)) != cudaSuccess) return e;
+  if ((e = launch_kernel(kernel, ctas, kThreads, smem_bytes(DP), 1, stream, a, row_tiles, page_shift, partial, prior)) != cudaSuccess) return e;
   // a unit's share of the runs: one warp joins a few partial results, eight many
   const bool few = units_of(a) * 8 >= (int64_t)ctas * kWarps;
-  return launch_kernel(few ? attention_token_join_kernel<DP, 1> : attention_token_join_kernel<DP, kJoinWarps>, (int64_t)a.batch * a.Hq,
-                       few ? 32 : kJoinWarps * 32, 0, 1, stream, a, row_tiles, ctas * kWarps, partial);
+  return launch_kernel(few ? attention_token_join_kernel<DP, 1, BEHIND> : attention_token_join_kernel<DP, kJoinWarps, BEHIND>, (int64_t)a.batch * a.Hq,
+                       few ? 32 : kJoinWarps * 32, 0, 1, stream, a, row_tiles, ctas * kWarps, partial, prior);
 }
 
 // The balanced form from 96 K positions (times key heads) on.  Measured, cluster against balanced form, us: 8 K positions
@@ -675,7 +737,9 @@ int64_t attention_token_workspace(const approxifer_attention_args& a) {
   return (int64_t)dev->sms * kCtasPerSm * kWarps * partial_floats(a.D <= 64 ? 64 : 128) * 4;
 }
 
-cudaError_t launch_attention_token(const approxifer_attention_args& a, cudaStream_t stream) {
+namespace {
+template <bool BEHIND>
+cudaError_t launch_form(const approxifer_attention_args& a, const PrefixParts& prior, cudaStream_t stream) {
   const DeviceInfo* dev;
   const cudaError_t e = current_device_info(&dev);
   if (e != cudaSuccess) return e;
@@ -685,15 +749,21 @@ cudaError_t launch_attention_token(const approxifer_attention_args& a, cudaStrea
   const bool is_whole = page_shift >= 0 && a.page_size >= keys;
   const int64_t need = attention_token_workspace(a);
   if (need > 0 && a.workspace_bytes >= need && (int64_t)a.batch * a.Hq < (1LL << 31)) {
-    auto launch = is_whole ? (dp == 64 ? launch_balanced<64, true> : launch_balanced<128, true>) : dp == 64 ? launch_balanced<64, false> : launch_balanced<128, false>;
-    return launch(a, *dev, row_tiles, page_shift, stream);
+    auto launch = is_whole ? (dp == 64 ? launch_balanced<64, true, BEHIND> : launch_balanced<128, true, BEHIND>)
+                           : dp == 64 ? launch_balanced<64, false, BEHIND> : launch_balanced<128, false, BEHIND>;
+    return launch(a, prior, *dev, row_tiles, page_shift, stream);
   }
   // Until there are about four CTAs for every place on the GPU, none with less than two chunks for each warp.
   const int64_t units = units_of(a), most = most_seen(a);
   int split = 1;
   while (split < kMaxSplit && units * split < 4LL * kCtasPerSm * dev->sms && most >= (int64_t)split * 2 * kWarps * keys * 2) split *= 2;
-  auto launch = is_whole ? (dp == 64 ? launch_cluster<64, true> : launch_cluster<128, true>) : dp == 64 ? launch_cluster<64, false> : launch_cluster<128, false>;
-  return launch(a, *dev, row_tiles, page_shift, units, split, stream);
+  auto launch = is_whole ? (dp == 64 ? launch_cluster<64, true, BEHIND> : launch_cluster<128, true, BEHIND>)
+                         : dp == 64 ? launch_cluster<64, false, BEHIND> : launch_cluster<128, false, BEHIND>;
+  return launch(a, prior, *dev, row_tiles, page_shift, units, split, stream);
 }
+}  // namespace
+
+cudaError_t launch_attention_token(const approxifer_attention_args& a, cudaStream_t stream) { return launch_form<false>(a, PrefixParts{}, stream); }
+cudaError_t launch_attention_token_behind(const approxifer_attention_args& a, const PrefixParts& prior, cudaStream_t stream) { return launch_form<true>(a, prior, stream); }
 
 }  // namespace approxifer

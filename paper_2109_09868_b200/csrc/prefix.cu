@@ -1,6 +1,6 @@
 // Attention of a batch behind a common prefix: choice of kernels, and the element-wise kernel for layouts that the others cannot
 // take.
-#include "hosted.cuh"
+#include "prefix.cuh"
 
 namespace approxifer {
 namespace {
@@ -57,13 +57,45 @@ __global__ void __launch_bounds__(kElementThreads) prefix_element_kernel(const _
 
 }  // namespace
 
-int64_t prefix_attention_workspace(const approxifer_prefix_attention_args&) { return 0; }
+namespace {
+// Whether the call runs on the tensor cores: what the kernel over the prefix takes, the ones over the own keys take too.
+bool on_tensor_cores(const approxifer_prefix_attention_args& p) {
+  approxifer_attention_args a = p.own;
+  if (!attention_tile_eligible(a)) return false;
+  a.table_pages = p.prefix_pages;
+  return attention_tile_eligible(a);
+}
+int64_t parts_bytes(const PrefixParts& p, const approxifer_attention_args& a) { return p.parts * p.rows * ((a.D <= 64 ? 64 : 128) + 2) * (int64_t)sizeof(float); }
+bool has_prefix(const approxifer_prefix_attention_args& p) { return p.prefix_len > 0 && p.prefix_pages > 0; }
+}  // namespace
 
-cudaError_t launch_prefix_attention(const approxifer_prefix_attention_args& a, cudaStream_t stream) {
-  const int64_t units = a.own.T * a.own.Hq, per = kElementThreads / 32;
+int64_t prefix_attention_workspace(const approxifer_prefix_attention_args& p) {
+  const DeviceInfo* dev;
+  if (!on_tensor_cores(p) || current_device_info(&dev) != cudaSuccess) return 0;
+  int64_t bytes = attention_token_eligible(p.own) ? attention_token_workspace(p.own) : 0;
+  if (has_prefix(p)) bytes += (parts_bytes(prefix_parts(p, *dev), p.own) + 15) / 16 * 16;
+  return bytes;
+}
+
+cudaError_t launch_prefix_attention(const approxifer_prefix_attention_args& p, cudaStream_t stream) {
+  if (on_tensor_cores(p)) {
+    if (!has_prefix(p)) return launch_attention(p.own, stream);
+    const DeviceInfo* dev;
+    cudaError_t e = current_device_info(&dev);
+    if (e != cudaSuccess) return e;
+    PrefixParts parts = prefix_parts(p, *dev);
+    approxifer_attention_args own = p.own;
+    parts.o = static_cast<float*>(own.workspace);
+    parts.ml = reinterpret_cast<float2*>(parts.o + parts.parts * parts.rows * (own.D <= 64 ? 64 : 128));
+    const int64_t used = (parts_bytes(parts, own) + 15) / 16 * 16;
+    own.workspace = static_cast<char*>(own.workspace) + used, own.workspace_bytes -= used;
+    if ((e = launch_attention_over_prefix(p, parts, stream)) != cudaSuccess) return e;
+    return attention_token_eligible(own) ? launch_attention_token_behind(own, parts, stream) : launch_attention_tile_behind(own, parts, stream);
+  }
+  const int64_t units = p.own.T * p.own.Hq, per = kElementThreads / 32;
   const int64_t blocks = (units + per - 1) / per;
   if (blocks > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
-  prefix_element_kernel<<<(unsigned)blocks, kElementThreads, 0, stream>>>(a);
+  prefix_element_kernel<<<(unsigned)blocks, kElementThreads, 0, stream>>>(p);
   count_launch();
   return cudaGetLastError();
 }
