@@ -763,7 +763,7 @@ cudaError_t launch_one(const TileArgs& g, const CUtensorMap& q, const CUtensorMa
   const approxifer_attention_args& a = g.a;
   if constexpr (FORM == kOverPrefix) {
     const int64_t ctas = ((int64_t)(g.blocks - 1) * g.prior.parts + g.prior.last_parts) * a.Hkv;
-    return launch_split<DP, false, FORM>(g, q, k, v, dev, ctas, 1, stream);
+    return g.prior.split > 1 ? launch_split<DP, true, FORM>(g, q, k, v, dev, ctas, g.prior.split, stream) : launch_split<DP, false, FORM>(g, q, k, v, dev, ctas, 1, stream);
   }
   const int64_t ctas = (int64_t)g.blocks * a.batch * a.Hkv;
   // Few query blocks: as many CTAs to each, along the keys, as the GPU holds, each with three tiles of keys or more.  (The
@@ -832,25 +832,32 @@ cudaError_t launch_attention_tile(const approxifer_attention_args& a, cudaStream
   return e != cudaSuccess ? e : launch_form<kPlain>(tile_args(a), *dev, stream);
 }
 
-// The parts that the prefix is cut into.  All CTAs of a turn run at once; a CTA's time is that of its steps and some four more for
-// its start and end, and every part is written and read once more by those who join them.
+// The parts that the prefix is cut into, and how many CTAs (a cluster, which joins their results) share one.  All CTAs of a turn run
+// at once; a CTA's time is that of its steps and some four more for its start and end, a cluster's meeting one more, and every part is
+// written and read once by those who join them.  A block of one tile takes 0.62 of the time of one of two.
 PrefixParts prefix_parts(const approxifer_prefix_attention_args& p, const DeviceInfo& dev) {
   const approxifer_attention_args& a = p.own;
-  const int dp = padded_head(a), tiles = tiles_of(dp), tokens = kRows / (a.Hq / a.Hkv), per_cta = tiles * tokens;
-  const int64_t blocks = (a.T + per_cta - 1) / per_cta, places = (int64_t)dev.sms * (3 - tiles);
+  const int dp = padded_head(a), tiles = tiles_of(dp), tokens = kRows / (a.Hq / a.Hkv), per_cta = tiles * tokens, per_sm = 3 - tiles;
+  const int64_t blocks = (a.T + per_cta - 1) / per_cta;
   const int64_t room = p.prefix_pages * a.page_size, steps = ((p.prefix_len < room ? p.prefix_len : room) + kKeys - 1) / kKeys;
   const bool half = tiles == 2 && a.T - (blocks - 1) * per_cta <= tokens;  // the last block has one tile
   PrefixParts best{};
   best.rows = a.T * a.Hq;
-  const double join = (double)best.rows * dp * 8 / 5e12 / (dp == 128 ? 2.3e-6 : 1.2e-6);  // in steps
-  double least = 0;
-  for (int64_t n = 1; n <= steps && n <= 64; ++n) {
-    const int64_t last = half && n > 1 ? (2 * n + 2) / 3 : n;
-    const int64_t turns = (((blocks - 1) * n + last) * a.Hkv + places - 1) / places;
-    const double time = turns * ((double)steps / n + 4) + n * join;
-    if (best.parts == 0 || time < least) least = time, best.parts = (int32_t)n, best.last_parts = (int32_t)last;
-  }
   best.last_token = (blocks - 1) * per_cta;
+  const double step = dp == 128 ? 2.1e-6 : 1.1e-6;  // s
+  const double join = ((double)best.rows * dp * 8 / 5e12 + 0.1e-6) / step;
+  double least = 0;
+  for (int s = 1; s <= kMaxSplit && s <= steps; s *= 2) {
+    // (a cluster sits within one GPC: of its SMs some are left over, more the larger the cluster)
+    const int64_t places = (int64_t)(s == 1 ? dev.sms : s == 2 ? dev.sms - 4 : s == 4 ? dev.sms * 7 / 8 : dev.sms * 3 / 4) * per_sm / s;
+    for (int64_t n = 1; n * s <= steps && n <= 64; ++n) {
+      const int64_t last = half ? (n * 62 + 99) / 100 : n;
+      const int64_t turns = (((blocks - 1) * n + last) * a.Hkv + places - 1) / places;
+      const double longest = (double)steps / s / (blocks > 1 ? n : last) * (blocks > 1 || !half ? 1.0 : 0.62);
+      const double time = turns * (longest + (s > 1 ? 5 : 4)) + n * join;
+      if (best.parts == 0 || time < least) least = time, best.parts = (int32_t)n, best.last_parts = (int32_t)last, best.split = s;
+    }
+  }
   return best;
 }
 

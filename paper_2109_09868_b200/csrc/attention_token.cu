@@ -412,8 +412,10 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) attention_token_cluster_
 // ---- balanced form ----
 
 // Workspace: two partial results for each warp (of a run's first unit, if the run starts inside it, and of its last, if it
-// ends inside it): float o[2 * warps][16][DP], then m, l [2 * warps][16].
+// ends inside it): float o[2 * warps][16][DP], then m, l [2 * warps][16].  Behind a prefix a unit that lies in one run is left as a
+// partial result too: after those, o[units][16][DP] and m, l [units][16] (of 16 rows, or as many as query heads share a key head).
 int64_t partial_floats(int dp) { return 2 * kRows * (dp + 2); }
+__host__ __device__ __forceinline__ int rows_of_unit(const approxifer_attention_args& a) { return a.Hq / a.Hkv < kRows ? a.Hq / a.Hkv : kRows; }
 
 // All chunks of the call stand in a row: sequence after sequence, and of a sequence unit after unit.  The warp that finds a
 // place in the row: the sequence and the number of chunks before it.
@@ -466,7 +468,7 @@ struct Cursor {
 
 template <int DP, bool WHOLE, bool BEHIND>
 __global__ void __launch_bounds__(kThreads, 3) attention_token_balanced_kernel(const __grid_constant__ approxifer_attention_args a, int row_tiles,
-                                                                                         int page_shift, float* partial, const __grid_constant__ PrefixParts prior) {
+                                                                                         int page_shift, float* partial) {
   extern __shared__ __align__(1024) unsigned char smem[];
   const int warp = blockIdx.x * kWarps + threadIdx.x / 32, warps = gridDim.x * kWarps, lane = threadIdx.x % 32;
   const int units = a.Hkv * row_tiles, group = a.Hq / a.Hkv;
@@ -529,29 +531,9 @@ __global__ void __launch_bounds__(kThreads, 3) attention_token_balanced_kernel(c
     const bool whole = use.c + 1 == use.seen.chunks;
     if (whole || x + 1 == x1) {  // the end of the unit or of the run
       w.finish();
-      if (whole && from_start) {
-        float inv[2] = {w.l[0] == 0.f ? 0.f : 1.f / w.l[0], w.l[1] == 0.f ? 0.f : 1.f / w.l[1]};
+      if (!BEHIND && whole && from_start) {
+        const float inv[2] = {w.l[0] == 0.f ? 0.f : 1.f / w.l[0], w.l[1] == 0.f ? 0.f : 1.f / w.l[1]};
         bf16* out = reinterpret_cast<bf16*>(a.out) + (int64_t)use.seen.token * a.o_tstride + (int64_t)head0 * a.o_hstride;
-        if constexpr (BEHIND) {
-          wait_for_inputs();
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int r = lane / 4 + h * 8;
-            if (r >= rows) continue;
-            PriorRow before;
-            const int64_t row_at = (int64_t)use.seen.token * a.Hq + head0 + r;
-            before.load(prior, row_at, use.seen.token);
-            const float own = before.weigh(w.m[h], w.l[h]);
-            inv[h] = w.l[h] == 0.f ? 0.f : own;
-#pragma unroll
-            for (int d = 0; d < DP / 8; ++d) {
-              float y[2] = {w.l[h] == 0.f ? 0.f : w.o[d][2 * h] * inv[h], w.l[h] == 0.f ? 0.f : w.o[d][2 * h + 1] * inv[h]};
-              before.add<2>(prior, row_at, DP, d * 8 + (lane % 4) * 2, y);
-              w.o[d][2 * h] = y[0], w.o[d][2 * h + 1] = y[1];
-            }
-            inv[h] = 1.f;
-          }
-        }
 #pragma unroll
         for (int d = 0; d < DP / 8; ++d)
 #pragma unroll
@@ -559,12 +541,18 @@ __global__ void __launch_bounds__(kThreads, 3) attention_token_balanced_kernel(c
             const int r = lane / 4 + h * 8, col = d * 8 + (lane % 4) * 2;
             if (r < rows && col < a.D)
               *reinterpret_cast<uint32_t*>(out + (int64_t)r * a.o_hstride + col) =
-                  !BEHIND && w.l[h] == 0.f ? 0u : pack_bf16x2(w.o[d][2 * h] * inv[h], w.o[d][2 * h + 1] * inv[h]);
+                  w.l[h] == 0.f ? 0u : pack_bf16x2(w.o[d][2 * h] * inv[h], w.o[d][2 * h + 1] * inv[h]);
           }
       } else {
         const int64_t part = 2 * (int64_t)warp + (from_start ? 1 : 0);
         float* po = partial + part * kRows * DP;
         float* pm = partial + 2 * (int64_t)warps * kRows * DP + part * kRows * 2;
+        if (BEHIND && whole && from_start) {
+          const int64_t unit = (int64_t)use.b * units + use.unit, all = (int64_t)a.batch * units * rows_of_unit(a);
+          po = partial + 2 * (int64_t)warps * kRows * (DP + 2);
+          pm = po + all * DP + unit * rows_of_unit(a) * 2;
+          po += unit * rows_of_unit(a) * DP;
+        }
 #pragma unroll
         for (int d = 0; d < DP / 8; ++d)
 #pragma unroll
@@ -611,29 +599,39 @@ __global__ void __launch_bounds__(JW * 32) attention_token_join_kernel(const __g
   wait_for_inputs();
   if (seen.token < 0) return;
   bf16* out = reinterpret_cast<bf16*>(a.out) + (int64_t)seen.token * a.o_tstride + (int64_t)h * a.o_hstride;
-  PriorRow before;
-  before.parts = 0;
-  const int64_t row_at = (int64_t)seen.token * a.Hq + h;
-  if (BEHIND && seen.placed) before.load(prior, row_at, seen.token);
-  if (seen.chunks == 0) {
-    if (BEHIND && seen.placed) before.weigh(-CUDART_INF_F, 0.f);
-    for (int d = threadIdx.x; d < a.D; d += JW * 32) {
-      float y[1] = {0.f};
-      if constexpr (BEHIND) before.add<1>(prior, row_at, DP, d, y);
-      out[d] = narrow<bf16>(y[0]);
-    }
+  const int prior_parts = !BEHIND || !seen.placed ? 0 : seen.token >= prior.last_token ? prior.last_parts : prior.parts;
+  if (seen.chunks == 0 && prior_parts == 0) {
+    for (int d = threadIdx.x; d < a.D; d += JW * 32) out[d] = narrow<bf16>(0.f);
     return;
   }
   const int64_t x0 = at.before + (int64_t)((h / group) * row_tiles + in_group / kRows) * seen.chunks, x1 = x0 + seen.chunks;
   const int64_t runs = total < warps ? total : warps;
-  const int w0 = (int)(((x0 + 1) * runs - 1) / total), w1 = (int)((x1 * runs - 1) / total);  // the runs that hold its first and its last chunk
-  if (w0 == w1) return;
+  // the runs that hold its first and its last chunk
+  const int w0 = seen.chunks ? (int)(((x0 + 1) * runs - 1) / total) : 0, w1 = seen.chunks ? (int)((x1 * runs - 1) / total) : -1;
+  if (!BEHIND && w0 == w1) return;
   const float* pm = partial + 2 * (int64_t)warps * kRows * DP;
   const int r = in_group % kRows;
   auto part = [&](int w) { return (2 * (int64_t)w + (w == w0 ? 1 : 0)) * kRows + r; };  // the first of them ends inside the unit
+  auto sums_of = [&](int w) -> const float2* {
+    if (BEHIND && w > w1) return prior.ml + (w - w1 - 1) * prior.rows + (int64_t)seen.token * a.Hq + h;
+    if (BEHIND && w0 == w1) {
+      const int64_t rows = rows_of_unit(a), unit = (int64_t)b * units + (h / group) * row_tiles + in_group / kRows;
+      return reinterpret_cast<const float2*>(partial + 2 * (int64_t)warps * kRows * (DP + 2) + (int64_t)a.batch * units * rows * DP) + unit * rows + r;
+    }
+    return reinterpret_cast<const float2*>(pm + part(w) * 2);
+  };
+  auto values_of = [&](int w) -> const float* {
+    if (BEHIND && w > w1) return prior.o + ((w - w1 - 1) * prior.rows + (int64_t)seen.token * a.Hq + h) * DP;
+    if (BEHIND && w0 == w1) {
+      const int64_t rows = rows_of_unit(a), unit = (int64_t)b * units + (h / group) * row_tiles + in_group / kRows;
+      return partial + 2 * (int64_t)warps * kRows * (DP + 2) + (unit * rows + r) * DP;
+    }
+    return partial + part(w) * DP;
+  };
+  const int last = w1 + prior_parts;
   float m = -CUDART_INF_F, l = 0.f;
   float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int w = w0 + team; w <= w1; w += kJoinAhead * kTeams) {
+  for (int w = w0 + team; w <= last; w += kJoinAhead * kTeams) {
     float2 ml[kJoinAhead];
     float4 v[kJoinAhead];
 #pragma unroll
@@ -641,10 +639,9 @@ __global__ void __launch_bounds__(JW * 32) attention_token_join_kernel(const __g
       const int wi = w + i * kTeams;
       ml[i] = make_float2(-CUDART_INF_F, 0.f);
       v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (wi <= w1) {
-        const int64_t p = part(wi);
-        ml[i] = __ldcg(reinterpret_cast<const float2*>(pm + p * 2));
-        v[i] = __ldcg(reinterpret_cast<const float4*>(partial + p * DP + at4));
+      if (wi <= last) {
+        ml[i] = __ldcg(sums_of(wi));
+        v[i] = __ldcg(reinterpret_cast<const float4*>(values_of(wi) + at4));
       }
     }
     float top = m;
@@ -675,15 +672,7 @@ __global__ void __launch_bounds__(JW * 32) attention_token_join_kernel(const __g
       sum = fmaf(k, sl[w], sum);
       z = fmaf(k, sy[w][d], z);
     }
-    if constexpr (BEHIND) {
-      PriorRow all = before;
-      const float own = all.weigh(sum == 0.f ? -CUDART_INF_F : best, sum);
-      float y[1] = {sum == 0.f ? 0.f : z * own};
-      all.add<1>(prior, row_at, DP, d, y);
-      out[d] = narrow<bf16>(y[0]);
-    } else {
-      out[d] = narrow<bf16>(sum == 0.f ? 0.f : z / sum);
-    }
+    out[d] = narrow<bf16>(sum == 0.f ? 0.f : z / sum);
   }
 }
 
@@ -711,7 +700,7 @@ cudaError_t launch_balanced(const approxifer_attention_args& a, const PrefixPart
   if (e != cudaSuccess) return e;
   const int ctas = dev.sms * kCtasPerSm;
   float* partial = static_cast<float*>(a.workspace);
-  if ((e = launch_kernel(kernel, ctas, kThreads, smem_bytes(DP), 1, stream, a, row_tiles, page_shift, partial, prior)) != cudaSuccess) return e;
+  if ((e = launch_kernel(kernel, ctas, kThreads, smem_bytes(DP), 1, stream, a, row_tiles, page_shift, partial)) != cudaSuccess) return e;
   // a unit's share of the runs: one warp joins a few partial results, eight many
   const bool few = units_of(a) * 8 >= (int64_t)ctas * kWarps;
   return launch_kernel(few ? attention_token_join_kernel<DP, 1, BEHIND> : attention_token_join_kernel<DP, kJoinWarps, BEHIND>, (int64_t)a.batch * a.Hq,
@@ -737,6 +726,11 @@ int64_t attention_token_workspace(const approxifer_attention_args& a) {
   return (int64_t)dev->sms * kCtasPerSm * kWarps * partial_floats(a.D <= 64 ? 64 : 128) * 4;
 }
 
+int64_t attention_token_behind_workspace(const approxifer_attention_args& a) {
+  const int64_t bytes = attention_token_workspace(a);
+  return bytes == 0 ? 0 : bytes + units_of(a) * rows_of_unit(a) * ((a.D <= 64 ? 64 : 128) + 2) * 4;
+}
+
 namespace {
 template <bool BEHIND>
 cudaError_t launch_form(const approxifer_attention_args& a, const PrefixParts& prior, cudaStream_t stream) {
@@ -747,7 +741,7 @@ cudaError_t launch_form(const approxifer_attention_args& a, const PrefixParts& p
   const int dp = a.D <= 64 ? 64 : 128, keys = keys_of(dp);
   const int page_shift = exact_log2(a.page_size);  // pages of whole chunks and a power of two: one look-up a chunk
   const bool is_whole = page_shift >= 0 && a.page_size >= keys;
-  const int64_t need = attention_token_workspace(a);
+  const int64_t need = BEHIND ? attention_token_behind_workspace(a) : attention_token_workspace(a);
   if (need > 0 && a.workspace_bytes >= need && (int64_t)a.batch * a.Hq < (1LL << 31)) {
     auto launch = is_whole ? (dp == 64 ? launch_balanced<64, true, BEHIND> : launch_balanced<128, true, BEHIND>)
                            : dp == 64 ? launch_balanced<64, false, BEHIND> : launch_balanced<128, false, BEHIND>;

@@ -72,8 +72,9 @@ bool has_prefix(const approxifer_prefix_attention_args& p) { return p.prefix_len
 int64_t prefix_attention_workspace(const approxifer_prefix_attention_args& p) {
   const DeviceInfo* dev;
   if (!on_tensor_cores(p) || current_device_info(&dev) != cudaSuccess) return 0;
-  int64_t bytes = attention_token_eligible(p.own) ? attention_token_workspace(p.own) : 0;
-  if (has_prefix(p)) bytes += (parts_bytes(prefix_parts(p, *dev), p.own) + 15) / 16 * 16;
+  const bool behind = has_prefix(p), token = attention_token_eligible(p.own);
+  int64_t bytes = !token ? 0 : behind ? attention_token_behind_workspace(p.own) : attention_token_workspace(p.own);
+  if (behind) bytes += (parts_bytes(prefix_parts(p, *dev), p.own) + 15) / 16 * 16;
   return bytes;
 }
 

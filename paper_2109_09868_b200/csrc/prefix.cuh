@@ -13,56 +13,79 @@ struct PrefixParts {
   int64_t rows;
   int64_t last_token;          // from this token on (the last query block of the kernel over the prefix)
   int32_t parts, last_parts;   // so many parts instead
+  int32_t split;               // CTAs that share a part, as a cluster
 };
 
 #ifdef __CUDACC__
-// A row's partial results: their weights in the joined row, divided by its sum.
+__device__ __forceinline__ float power_of_two(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// A row's partial results: their weights in the joined row, divided by its sum.  Loads go out several parts at a time.
 struct PriorRow {
   int parts;
   float top, inv;
 
   __device__ __forceinline__ void load(const PrefixParts& p, int64_t row, int64_t token) {
+    constexpr int kAt = 8;
     parts = token >= p.last_token ? p.last_parts : p.parts;
     top = -CUDART_INF_F, inv = 0.f;
-    for (int i = 0; i < parts; ++i) {
-      const float2 v = __ldcg(p.ml + i * p.rows + row);
-      if (v.x > top) inv *= pow2_of(top - v.x), top = v.x;
-      inv += v.y * pow2_of(v.x - (top == -CUDART_INF_F ? 0.f : top));
+    for (int i = 0; i < parts; i += kAt) {
+      float2 v[kAt];
+#pragma unroll
+      for (int e = 0; e < kAt; ++e) v[e] = i + e < parts ? __ldcg(p.ml + (i + e) * p.rows + row) : make_float2(-CUDART_INF_F, 0.f);
+      float most = top;
+#pragma unroll
+      for (int e = 0; e < kAt; ++e) most = fmaxf(most, v[e].x);
+      const float base = most == -CUDART_INF_F ? 0.f : most;
+      inv *= power_of_two(top - base);
+#pragma unroll
+      for (int e = 0; e < kAt; ++e) inv = fmaf(v[e].y, power_of_two(v[e].x - base), inv);
+      top = most;
     }
   }
   // Joins the row's own maximum and sum; what its own sums are to be multiplied with.
   __device__ __forceinline__ float weigh(float m, float l) {
     const float most = fmaxf(top, m), base = most == -CUDART_INF_F ? 0.f : most;
-    const float sum = inv * pow2_of(top - base) + l * pow2_of(m - base);
+    const float sum = inv * power_of_two(top - base) + l * power_of_two(m - base);
     top = base;
     inv = sum == 0.f ? 0.f : 1.f / sum;
-    return pow2_of(m - base) * inv;
+    return power_of_two(m - base) * inv;
   }
   // Adds columns col .. col + N - 1 of the partial results.
   template <int N>
   __device__ __forceinline__ void add(const PrefixParts& p, int64_t row, int width, int col, float (&y)[N]) const {
-    constexpr int kWide = N >= 4 ? 4 : N;
-    for (int i = 0; i < parts; ++i) {
-      const float w = pow2_of(__ldcg(p.ml + i * p.rows + row).x - top) * inv;
-      const float* from = p.o + (i * p.rows + row) * width + col;
+    constexpr int kWide = N >= 4 ? 4 : 2, kAt = N >= 16 ? 2 : 8;
+    static_assert(N % kWide == 0, "whole pairs or fours");
+    for (int i = 0; i < parts; i += kAt) {
+      float m[kAt], v[kAt][N];
 #pragma unroll
-      for (int c = 0; c < N; c += kWide) {
-        if constexpr (kWide == 4) {
-          const float4 v = __ldcg(reinterpret_cast<const float4*>(from + c));
-          y[c] = fmaf(w, v.x, y[c]), y[c + 1] = fmaf(w, v.y, y[c + 1]), y[c + 2] = fmaf(w, v.z, y[c + 2]), y[c + 3] = fmaf(w, v.w, y[c + 3]);
-        } else if constexpr (kWide == 1) {
-          y[c] = fmaf(w, __ldcg(from + c), y[c]);
-        } else {
-          const float2 v = __ldcg(reinterpret_cast<const float2*>(from + c));
-          y[c] = fmaf(w, v.x, y[c]), y[c + 1] = fmaf(w, v.y, y[c + 1]);
+      for (int e = 0; e < kAt; ++e) {
+        const bool there = i + e < parts;
+        const int64_t at = there ? (i + e) * p.rows + row : row;
+        m[e] = there ? __ldcg(p.ml + at).x : -CUDART_INF_F;
+        const float* from = p.o + at * width + col;
+#pragma unroll
+        for (int c = 0; c < N; c += kWide) {
+          if constexpr (kWide == 4) {
+            const float4 u = there ? __ldcg(reinterpret_cast<const float4*>(from + c)) : make_float4(0.f, 0.f, 0.f, 0.f);
+            v[e][c] = u.x, v[e][c + 1] = u.y, v[e][c + 2] = u.z, v[e][c + 3] = u.w;
+          } else {
+            const float2 u = there ? __ldcg(reinterpret_cast<const float2*>(from + c)) : make_float2(0.f, 0.f);
+            v[e][c] = u.x, v[e][c + 1] = u.y;
+          }
         }
       }
+#pragma unroll
+      for (int e = 0; e < kAt; ++e) {
+        if (i + e >= parts) break;
+        const float w = power_of_two(m[e] - top) * inv;
+#pragma unroll
+        for (int c = 0; c < N; ++c) y[c] = fmaf(w, v[e][c], y[c]);
+      }
     }
-  }
-  static __device__ __forceinline__ float pow2_of(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
   }
 };
 #endif
@@ -70,6 +93,7 @@ struct PriorRow {
 PrefixParts prefix_parts(const approxifer_prefix_attention_args& a, const DeviceInfo& dev);  // (pointers left out); see attention_tile.cu
 cudaError_t launch_attention_over_prefix(const approxifer_prefix_attention_args& a, const PrefixParts& parts, cudaStream_t stream);
 cudaError_t launch_attention_tile_behind(const approxifer_attention_args& a, const PrefixParts& parts, cudaStream_t stream);
+int64_t attention_token_behind_workspace(const approxifer_attention_args& a);
 cudaError_t launch_attention_token_behind(const approxifer_attention_args& a, const PrefixParts& parts, cudaStream_t stream);
 
 }  // namespace approxifer
