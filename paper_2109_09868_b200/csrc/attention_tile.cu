@@ -445,11 +445,13 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
       if (ok) ok = warp_wait(pv_done + 8 * t, TQ == 1 ? (steps - 1) & 1 : 0, abort, count);
       tmem_fence_after();
     }
-    if constexpr (CLUSTER) softmax_warps_meet<TQ>();  // no product reads shared memory any more, of either tile
+    constexpr bool kWide = FORM != kPlain && !CLUSTER;  // rows in fp32 for the partial results, or to be joined with them
+    if constexpr (CLUSTER || kWide) softmax_warps_meet<TQ>();  // no product reads shared memory any more, of either tile
     if constexpr (FORM == kBehindPrefix) wait_for_inputs();
     if (ok) {
       // One CTA: O / sum, by way of the tile's queries' place in shared memory (a warp keeps to its own rows and columns) into
-      // whole rows.  A cluster: O as it is into shared memory, with the row's maximum and sum.
+      // whole rows; around a prefix in fp32, over queries and ring.  A cluster: O as it is into shared memory, with the row's maximum
+      // and sum.
       float inv = CLUSTER || FORM == kOverPrefix ? 1.f : l == 0.f ? 0.f : 1.f / l;
       const int64_t row_at = (int64_t)(job.token0 + token) * a.Hq + job.hk * g.group + r % g.group;  // (of the partial results)
       PriorRow prior;
@@ -462,8 +464,8 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
         }
       }
       const bool add_back = *poison != 0;
-      unsigned char* own_rows = base + 1024 + t * kTile + (half * 4 + quarter) * 32 * kOut * 2;
-      constexpr int kCols = kOut / 8;  // 16-byte columns
+      constexpr int kCols = kOut / (kWide ? 4 : 8);  // 16-byte columns
+      unsigned char* own_rows = kWide ? base + 1024 + warp * 32 * kOut * 4 : base + 1024 + t * kTile + (half * 4 + quarter) * 32 * kOut * 2;
       if (CLUSTER && half == 0) row_sums[t * kRows + r] = make_float2(m, l);
 #pragma unroll 1
       for (int c = 0; c < kOut; c += 16) {
@@ -500,17 +502,14 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
             }
           }
         }
-        if constexpr (FORM == kBehindPrefix && !CLUSTER) prior.template add<16>(g.prior, row_at, DP, half * kOut + c, y);
         if constexpr (CLUSTER) {
 #pragma unroll
           for (int i = 0; i < 16; i += 4)
             part_rows[(t * kRows + r) * (DP / 4) + (((half * kOut + c + i) / 4) ^ (r & 7))] = make_float4(y[i], y[i + 1], y[i + 2], y[i + 3]);
-        } else if constexpr (FORM == kOverPrefix) {
-          if (mine) {
-            float4* to = reinterpret_cast<float4*>(g.prior.o + (job.piece * g.prior.rows + row_at) * DP + half * kOut + c);
+        } else if constexpr (kWide) {
 #pragma unroll
-            for (int i = 0; i < 16; i += 4) to[i / 4] = make_float4(y[i], y[i + 1], y[i + 2], y[i + 3]);
-          }
+          for (int i = 0; i < 16; i += 4)
+            *reinterpret_cast<float4*>(own_rows + lane * kOut * 4 + ((((c + i) / 4) ^ (lane & (kCols - 1))) << 4)) = make_float4(y[i], y[i + 1], y[i + 2], y[i + 3]);
         } else {
 #pragma unroll
           for (int i = 0; i < 16; i += 8)
@@ -519,10 +518,52 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
         }
         __syncwarp();
       }
-      if (FORM == kOverPrefix && !CLUSTER && mine && half == 0) g.prior.ml[job.piece * g.prior.rows + row_at] = make_float2(m == -CUDART_INF_F ? m : m * scale, l);
+      if constexpr (kWide) {
+        // Rows of this warp, a lane to four columns: out of shared memory into the partial results, or with those into the output.
+        constexpr int kTogether = 8, kSide = 32 / kCols;  // rows at a time, side by side
+        const int col = lane % kCols, d = half * kOut + col * 4;
+        if (FORM == kOverPrefix && mine && half == 0) g.prior.ml[job.piece * g.prior.rows + row_at] = make_float2(m == -CUDART_INF_F ? m : m * scale, l);
+        const int64_t to = !mine ? -1 : FORM == kOverPrefix ? (job.piece * g.prior.rows + row_at) * DP
+                                                             : (int64_t)(job.token0 + token) * a.o_tstride + (int64_t)(job.hk * g.group + r % g.group) * a.o_hstride;
+        const int parts = FORM == kBehindPrefix ? g.prior.parts : 0;  // (a row of fewer gives the others no weight)
+#pragma unroll 1
+        for (int x = 0; x < 32; x += kTogether * kSide) {
+          float4 y[kTogether];
+#pragma unroll
+          for (int e = 0; e < kTogether; ++e) {
+            const int row = x + e * kSide + lane / kCols;
+            y[e] = *reinterpret_cast<const float4*>(own_rows + row * kOut * 4 + ((col ^ (row & (kCols - 1))) << 4));
+          }
+          if constexpr (FORM == kBehindPrefix) {
+#pragma unroll 1
+            for (int p = 0; p < parts; ++p) {
+              const float mine_w = p < prior.parts ? prior.weight(__ldcg(g.prior.ml + p * g.prior.rows + row_at).x) : 0.f;
+              float4 v[kTogether];
+              float w[kTogether];
+#pragma unroll
+              for (int e = 0; e < kTogether; ++e) {
+                const int row = x + e * kSide + lane / kCols;
+                const int64_t at = __shfl_sync(0xffffffffu, p < prior.parts ? row_at : -1, row);
+                w[e] = __shfl_sync(0xffffffffu, mine_w, row);
+                v[e] = at >= 0 ? __ldcg(reinterpret_cast<const float4*>(g.prior.o + (p * g.prior.rows + at) * DP + d)) : make_float4(0.f, 0.f, 0.f, 0.f);
+              }
+#pragma unroll
+              for (int e = 0; e < kTogether; ++e)
+                y[e] = make_float4(fmaf(w[e], v[e].x, y[e].x), fmaf(w[e], v[e].y, y[e].y), fmaf(w[e], v[e].z, y[e].z), fmaf(w[e], v[e].w, y[e].w));
+            }
+          }
+#pragma unroll
+          for (int e = 0; e < kTogether; ++e) {
+            const int64_t at = __shfl_sync(0xffffffffu, to, x + e * kSide + lane / kCols);
+            if (at < 0) continue;
+            if constexpr (FORM == kOverPrefix) *reinterpret_cast<float4*>(g.prior.o + at + d) = y[e];
+            else if (d < a.D) *reinterpret_cast<uint2*>(reinterpret_cast<bf16*>(a.out) + at + d) = make_uint2(pack_bf16x2(y[e].x, y[e].y), pack_bf16x2(y[e].z, y[e].w));
+          }
+        }
+      }
       const int64_t to = mine ? (int64_t)(job.token0 + token) * a.o_tstride + (int64_t)(job.hk * g.group + r % g.group) * a.o_hstride : -1;
 #pragma unroll 4
-      for (int x = lane; !CLUSTER && FORM != kOverPrefix && x < 32 * kCols; x += 32) {
+      for (int x = lane; !CLUSTER && !kWide && x < 32 * kCols; x += 32) {
         const int row = x / kCols, col = x % kCols, d = half * kOut + col * 8;
         const int64_t at = __shfl_sync(0xffffffffu, to, row);
         if (at >= 0 && d < a.D)
@@ -685,62 +726,79 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
     if (warp < kScoreWarp) {
       const float scale = fmaxf(fabsf(a.scale) * 1.4426950408889634f, 1e-37f);
       const uint32_t parts = smem_addr(part_rows), sums = smem_addr(row_sums);
-      for (int x = TQ * kRows * rank / S + warp; x < TQ * kRows * (rank + 1) / S; x += kScoreWarp) {
-        const int t = x / kRows, r = x % kRows, token = t * job.tokens + r / g.group;
-        if (r / g.group >= job.tokens || token >= job.left) continue;
-        float2 ml[kMaxSplit];
-        float best = -CUDART_INF_F;
+      constexpr int kAt = 2;  // rows whose loads are in flight together
+      const int end = TQ * kRows * (rank + 1) / S, c = lane * (DP / 32);  // this lane's columns
+      for (int x0 = TQ * kRows * rank / S + warp; x0 < end; x0 += kScoreWarp * kAt) {
+        float2 ml[kAt][kMaxSplit];
+        float best[kAt], total[kAt], y[kAt][4];
 #pragma unroll
-        for (int s = 0; s < kMaxSplit; ++s) {
-          ml[s] = s < S ? peer_load2(peer_smem(sums + x * 8, s)) : make_float2(-CUDART_INF_F, 0.f);
-          best = fmaxf(best, ml[s].x);
+        for (int e = 0; e < kAt; ++e) {
+          const int x = min(x0 + e * kScoreWarp, TQ * kRows - 1);
+          best[e] = -CUDART_INF_F, total[e] = y[e][0] = y[e][1] = y[e][2] = y[e][3] = 0.f;
+#pragma unroll
+          for (int s = 0; s < kMaxSplit; ++s) ml[e][s] = s < S ? peer_load2(peer_smem(sums + x * 8, s)) : make_float2(-CUDART_INF_F, 0.f);
         }
-        if (best == -CUDART_INF_F) best = 0.f;
-        const int c = lane * (DP / 32);  // this lane's columns
-        const uint32_t at = parts + (x * (DP / 4) + ((c / 4) ^ (r & 7))) * 16 + (c % 4) * 4;
-        float total = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int e = 0; e < kAt; ++e) {
+#pragma unroll
+          for (int s = 0; s < kMaxSplit; ++s) best[e] = fmaxf(best[e], ml[e][s].x);
+          if (best[e] == -CUDART_INF_F) best[e] = 0.f;
+        }
 #pragma unroll
         for (int s = 0; s < kMaxSplit; ++s) {
           if (s >= S) continue;
-          const float k = pow2((ml[s].x - best) * scale);
-          total = fmaf(k, ml[s].y, total);
-          if constexpr (DP == 128) {
-            const float4 v = peer_load(peer_smem(at, s));
-            y[0] = fmaf(k, v.x, y[0]), y[1] = fmaf(k, v.y, y[1]), y[2] = fmaf(k, v.z, y[2]), y[3] = fmaf(k, v.w, y[3]);
+          float4 v[kAt];
+#pragma unroll
+          for (int e = 0; e < kAt; ++e) {
+            const int x = min(x0 + e * kScoreWarp, TQ * kRows - 1);
+            const uint32_t at = parts + (x * (DP / 4) + ((c / 4) ^ (x % kRows & 7))) * 16 + (c % 4) * 4;
+            if constexpr (DP == 128) {
+              v[e] = peer_load(peer_smem(at, s));
+            } else {
+              const float2 u = peer_load2(peer_smem(at, s));
+              v[e] = make_float4(u.x, u.y, 0.f, 0.f);
+            }
+          }
+#pragma unroll
+          for (int e = 0; e < kAt; ++e) {
+            const float k = pow2((ml[e][s].x - best[e]) * scale);
+            total[e] = fmaf(k, ml[e][s].y, total[e]);
+            y[e][0] = fmaf(k, v[e].x, y[e][0]), y[e][1] = fmaf(k, v[e].y, y[e][1]);
+            if constexpr (DP == 128) y[e][2] = fmaf(k, v[e].z, y[e][2]), y[e][3] = fmaf(k, v[e].w, y[e][3]);
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < kAt; ++e) {
+          const int x = x0 + e * kScoreWarp, t = x / kRows, r = x % kRows, token = t * job.tokens + r / g.group;
+          if (x >= end || r / g.group >= job.tokens || token >= job.left) continue;
+          const int64_t row_at = (int64_t)(job.token0 + token) * a.Hq + job.hk * g.group + r % g.group;
+          if constexpr (FORM == kOverPrefix) {
+            float* to = g.prior.o + (job.piece * g.prior.rows + row_at) * DP + c;
+            if constexpr (DP == 128) *reinterpret_cast<float4*>(to) = make_float4(y[e][0], y[e][1], y[e][2], y[e][3]);
+            else *reinterpret_cast<float2*>(to) = make_float2(y[e][0], y[e][1]);
+            if (lane == 0) g.prior.ml[job.piece * g.prior.rows + row_at] = make_float2(total[e] == 0.f ? -CUDART_INF_F : best[e] * scale, total[e]);
           } else {
-            const float2 v = peer_load2(peer_smem(at, s));
-            y[0] = fmaf(k, v.x, y[0]), y[1] = fmaf(k, v.y, y[1]);
-          }
-        }
-        const int64_t row_at = (int64_t)(job.token0 + token) * a.Hq + job.hk * g.group + r % g.group;
-        if constexpr (FORM == kOverPrefix) {
-          float* to = g.prior.o + (job.piece * g.prior.rows + row_at) * DP + c;
-          if constexpr (DP == 128) *reinterpret_cast<float4*>(to) = make_float4(y[0], y[1], y[2], y[3]);
-          else *reinterpret_cast<float2*>(to) = make_float2(y[0], y[1]);
-          if (lane == 0) g.prior.ml[job.piece * g.prior.rows + row_at] = make_float2(total == 0.f ? -CUDART_INF_F : best * scale, total);
-          continue;
-        }
-        float inv = total == 0.f ? 0.f : 1.f / total;
-        if constexpr (FORM == kBehindPrefix) {
-          PriorRow prior;
-          prior.parts = 0;
-          if (job.pos_of(token) >= 0) {
-            prior.load(g.prior, row_at, job.token0 + token);
-            const float own = prior.weigh(total == 0.f ? -CUDART_INF_F : best * scale, total);
-            inv = total == 0.f ? 0.f : own;
-          }
+            float inv = total[e] == 0.f ? 0.f : 1.f / total[e];
+            if constexpr (FORM == kBehindPrefix) {
+              PriorRow prior;
+              prior.parts = 0;
+              if (job.pos_of(token) >= 0) {
+                prior.load(g.prior, row_at, job.token0 + token);
+                const float own = prior.weigh(total[e] == 0.f ? -CUDART_INF_F : best[e] * scale, total[e]);
+                inv = total[e] == 0.f ? 0.f : own;
+              }
+              float z[DP / 32] = {};
+              prior.template add<DP / 32>(g.prior, row_at, DP, c, z);
 #pragma unroll
-          for (int i = 0; i < DP / 32; ++i) y[i] *= inv;
-          inv = 1.f;
-          float z[DP / 32] = {};
-          prior.template add<DP / 32>(g.prior, row_at, DP, c, z);
-#pragma unroll
-          for (int i = 0; i < DP / 32; ++i) y[i] += z[i];
-        }
-        bf16* out = reinterpret_cast<bf16*>(a.out) + (int64_t)(job.token0 + token) * a.o_tstride + (int64_t)(job.hk * g.group + r % g.group) * a.o_hstride + c;
-        if (c < a.D) {
-          if constexpr (DP == 128) *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(y[0] * inv, y[1] * inv), pack_bf16x2(y[2] * inv, y[3] * inv));
-          else *reinterpret_cast<uint32_t*>(out) = pack_bf16x2(y[0] * inv, y[1] * inv);
+              for (int i = 0; i < DP / 32; ++i) y[e][i] = fmaf(y[e][i], inv, z[i]);
+              inv = 1.f;
+            }
+            bf16* out = reinterpret_cast<bf16*>(a.out) + (int64_t)(job.token0 + token) * a.o_tstride + (int64_t)(job.hk * g.group + r % g.group) * a.o_hstride + c;
+            if (c < a.D) {
+              if constexpr (DP == 128) *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(y[e][0] * inv, y[e][1] * inv), pack_bf16x2(y[e][2] * inv, y[e][3] * inv));
+              else *reinterpret_cast<uint32_t*>(out) = pack_bf16x2(y[e][0] * inv, y[e][1] * inv);
+            }
+          }
         }
       }
     }
@@ -834,7 +892,8 @@ cudaError_t launch_attention_tile(const approxifer_attention_args& a, cudaStream
 
 // The parts that the prefix is cut into, and how many CTAs (a cluster, which joins their results) share one.  All CTAs of a turn run
 // at once; a CTA's time is that of its steps and some four more for its start and end, a cluster's meeting one more, and every part is
-// written and read once by those who join them.  A block of one tile takes 0.62 of the time of one of two.
+// written and read once by those who join them.  Of two tiles in turn each hides the other's softmax:
+// a block of one takes nearly as long (1.75 us a step, two 1.98).
 PrefixParts prefix_parts(const approxifer_prefix_attention_args& p, const DeviceInfo& dev) {
   const approxifer_attention_args& a = p.own;
   const int dp = padded_head(a), tiles = tiles_of(dp), tokens = kRows / (a.Hq / a.Hkv), per_cta = tiles * tokens, per_sm = 3 - tiles;
@@ -844,17 +903,17 @@ PrefixParts prefix_parts(const approxifer_prefix_attention_args& p, const Device
   PrefixParts best{};
   best.rows = a.T * a.Hq;
   best.last_token = (blocks - 1) * per_cta;
-  const double step = dp == 128 ? 2.1e-6 : 1.1e-6;  // s
+  const double step = dp == 128 ? 2.0e-6 : 1.0e-6;  // s
   const double join = ((double)best.rows * dp * 8 / 5e12 + 0.1e-6) / step;
   double least = 0;
   for (int s = 1; s <= kMaxSplit && s <= steps; s *= 2) {
     // (a cluster sits within one GPC: of its SMs some are left over, more the larger the cluster)
     const int64_t places = (int64_t)(s == 1 ? dev.sms : s == 2 ? dev.sms - 4 : s == 4 ? dev.sms * 7 / 8 : dev.sms * 3 / 4) * per_sm / s;
     for (int64_t n = 1; n * s <= steps && n <= 64; ++n) {
-      const int64_t last = half ? (n * 62 + 99) / 100 : n;
+      const int64_t last = half ? (n * 4 + 4) / 5 : n;
       const int64_t turns = (((blocks - 1) * n + last) * a.Hkv + places - 1) / places;
-      const double longest = (double)steps / s / (blocks > 1 ? n : last) * (blocks > 1 || !half ? 1.0 : 0.62);
-      const double time = turns * (longest + (s > 1 ? 5 : 4)) + n * join;
+      const double longest = (double)steps / s / (blocks > 1 ? n : last) * (blocks > 1 || !half ? 1.0 : 0.88);
+      const double time = turns * (longest + (s > 1 ? 8 : 4)) + n * join;
       if (best.parts == 0 || time < least) least = time, best.parts = (int32_t)n, best.last_parts = (int32_t)last, best.split = s;
     }
   }

@@ -54,10 +54,12 @@ struct PriorRow {
     inv = sum == 0.f ? 0.f : 1.f / sum;
     return power_of_two(m - base) * inv;
   }
+  // The weight of a part whose maximum is m.
+  __device__ __forceinline__ float weight(float m) const { return power_of_two(m - top) * inv; }
   // Adds columns col .. col + N - 1 of the partial results.
   template <int N>
   __device__ __forceinline__ void add(const PrefixParts& p, int64_t row, int width, int col, float (&y)[N]) const {
-    constexpr int kWide = N >= 4 ? 4 : 2, kAt = N >= 16 ? 2 : 8;
+    constexpr int kWide = N >= 4 ? 4 : 2, kAt = 8;
     static_assert(N % kWide == 0, "whole pairs or fours");
     for (int i = 0; i < parts; i += kAt) {
       float m[kAt], v[kAt][N];
@@ -81,7 +83,7 @@ struct PriorRow {
 #pragma unroll
       for (int e = 0; e < kAt; ++e) {
         if (i + e >= parts) break;
-        const float w = power_of_two(m[e] - top) * inv;
+        const float w = weight(m[e]);
 #pragma unroll
         for (int c = 0; c < N; ++c) y[c] = fmaf(w, v[e][c], y[c]);
       }
