@@ -49,6 +49,10 @@ cudaError_t launch_kernel(void (*kernel)(Params...), int grid, int block, int sm
 // the array read as zero.
 cudaError_t make_tensor_map(CUtensorMap* map, const void* base, int rank, const uint64_t* extent, const uint64_t* stride, const uint32_t* box);
 
+// Tensor map of the blocks of scales (512 bytes each) of a 4-bit microscaled array, [row_blocks][col_blocks] of them, read two
+// neighbours of a row of blocks at a time (of `rows` such rows together), as they lie.  Blocks outside the array read as zero.
+cudaError_t make_scales_map(CUtensorMap* map, const void* base, int64_t row_blocks, int64_t col_blocks, int rows);
+
 #ifdef __CUDACC__
 
 constexpr uint32_t kWaitLimit = 1u << 21;  // try_wait attempts (each may block for a while) before a wait gives up
@@ -164,6 +168,11 @@ __device__ __forceinline__ void tma_3d(uint32_t dst, const CUtensorMap* map, int
                "r"(y), "r"(z), "r"(bar)
                : "memory");
 }
+__device__ __forceinline__ void tma_3d_pair(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+               "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+               : "memory");
+}
 __device__ __forceinline__ void tma_4d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int w, uint32_t bar) {
   asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst), "l"(map),
                "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar)
@@ -220,6 +229,38 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint3
       "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d),
       "r"(a), "l"(b), "r"(shape), "r"((uint32_t)add)
       : "memory");
+}
+// 4-bit microscaled operands (E2M1, a power of two to 32 of them): both K-major, 64 of K an instruction, two to a byte, so that a
+// swizzled row of 128 bytes holds 256 and the operands' descriptors move on as those of bfloat16 do.  The scales lie in tensor
+// memory, copied there from a block of 512 bytes as approxifer_mx_quantize lays it out: four columns, of which column c holds,
+// in lane l, the four scales (128 of K) of row 32 c + l; `half` says which two of the four the instruction takes.
+__host__ __device__ constexpr uint32_t mx_shape(int m, int n, int half) {
+  return (uint32_t)(2 * half) << 4 | 1u << 7 | 1u << 10 | (uint32_t)(n >> 3) << 17 | 1u << 23 | (uint32_t)(m >> 7) << 27 | (uint32_t)(2 * half) << 29;
+}
+__device__ __forceinline__ void mma_mx(uint32_t d, uint64_t a, uint64_t b, uint32_t shape, uint32_t scales_a, uint32_t scales_b, bool add) {
+  asm volatile(
+      "{\n.reg .pred p;\n"
+      "setp.ne.b32 p, %6, 0;\n"
+      "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}\n" ::"r"(d),
+      "l"(a), "l"(b), "r"(shape), "r"(scales_a), "r"(scales_b), "r"((uint32_t)add)
+      : "memory");
+}
+__device__ __forceinline__ void mma_mx_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t shape, uint32_t scales_a, uint32_t scales_b, bool add) {
+  asm volatile(
+      "{\n.reg .pred p;\n"
+      "setp.ne.b32 p, %6, 0;\n"
+      "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}\n" ::"r"(d),
+      "l"(a), "l"(b), "r"(shape), "r"(scales_a), "r"(scales_b), "r"((uint32_t)add)
+      : "memory");
+}
+// A block of scales, 512 bytes of shared memory as they lie (32 rows of 16 bytes, eight to a group), to four columns of tensor
+// memory, in all four quarters of its lanes.
+__device__ __forceinline__ uint64_t desc_scales(uint32_t addr) { return (uint64_t)((addr & 0x3ffff) >> 4) | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46; }
+__device__ __forceinline__ void copy_scales(uint32_t to, uint32_t from) {
+  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(to), "l"(desc_scales(from)) : "memory");
+}
+__device__ __forceinline__ void copy_scales_pair(uint32_t to, uint32_t from) {  // in both CTAs, each from its own shared memory
+  asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(to), "l"(desc_scales(from)) : "memory");
 }
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");

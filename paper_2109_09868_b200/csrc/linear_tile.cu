@@ -17,7 +17,7 @@
 //
 // Few rows are bound by reading Wt, small products by the chain of a start, one copy, one product and the joining (5 to
 // 8 us).  Measured: 20 rows, 4,096 -> 16,384 with bias and gelu 26 us, 5.1 TB/s; 1,280 rows, 784 -> 10 5.5 us.
-#include "async.cuh"
+#include "mx.cuh"
 
 namespace approxifer {
 
@@ -31,10 +31,17 @@ constexpr int kMinLanes = 96; // ... and the fewest worth having (with less a co
 constexpr int kDepth = 64;    // columns of both operands per stage: one 128-byte swizzle row
 constexpr int kHeader = 1024; // mbarriers, flags; keeps the stages 1,024-byte aligned
 
-constexpr int stage_bytes(int bn) { return (kLanes + bn) * kDepth * 2; }
-constexpr int stages_of(int bn) { return 196 * 1024 / stage_bytes(bn); }
-constexpr int smem_bytes(int bn) { return kHeader + 1024 + stages_of(bn) * stage_bytes(bn); }
-constexpr int tmem_cols(int bn) { return bn < 32 ? 32 : bn; }
+// MX: both operands 4-bit microscaled, 256 columns and two blocks of each operand's scales a stage.
+constexpr int operand_bytes(int bn) { return (kLanes + bn) * kDepth * 2; }
+constexpr int stage_bytes(int bn, bool mx) { return operand_bytes(bn) + (mx ? 4 * kMxBlock : 0); }
+constexpr int stages_of(int bn, bool mx) { return 196 * 1024 / stage_bytes(bn, mx); }
+constexpr int smem_bytes(int bn, bool mx) { return kHeader + 1024 + stages_of(bn, mx) * stage_bytes(bn, mx); }
+constexpr int acc_cols(int bn) { return bn < 32 ? 32 : bn; }
+// (MX: behind the accumulator sixteen columns of scales a stage)
+constexpr int tmem_cols(int bn, bool mx) { return mx ? 256 : acc_cols(bn); }
+static_assert(acc_cols(16) + 16 * stages_of(16, true) <= 256 && acc_cols(32) + 16 * stages_of(32, true) <= 256 && acc_cols(64) + 16 * stages_of(64, true) <= 256 &&
+                  acc_cols(128) + 16 * stages_of(128, true) <= 256,
+              "the scales exceed the tensor memory");
 
 struct TileArgs {
   int32_t M, N, K;
@@ -46,6 +53,7 @@ struct TileArgs {
   void* Y;
   int64_t r_rstride, y_rstride;
   int32_t activation;
+  int32_t mx_blocks;      // (MX) blocks of 128 columns
   int32_t vec, bias_vec;  // rows of Y and R, the bias, can be accessed four elements at a time
 };
 
@@ -79,10 +87,11 @@ __device__ __forceinline__ void write4(Out* p, float4 v, bool vec, int count) {
   if (count > 3) p[3] = narrow<Out>(v.w);
 }
 
-template <int BN, bool SWAP, typename Out>
+template <int BN, bool SWAP, typename Out, bool MX>
 __global__ void __launch_bounds__(kThreads, 1) linear_tile_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_constant__ CUtensorMap cols_map,
+                                                               const __grid_constant__ CUtensorMap row_scales, const __grid_constant__ CUtensorMap col_scales,
                                                                const __grid_constant__ TileArgs a) {
-  constexpr int kStages = stages_of(BN);
+  constexpr int kStages = stages_of(BN, MX), kStageBytes = stage_bytes(BN, MX);
   extern __shared__ unsigned char raw[];
   unsigned char* base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
   uint64_t* bars = reinterpret_cast<uint64_t*>(base);  // full[stages], empty[stages], done
@@ -104,8 +113,9 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tile_kernel(const __grid_c
     bar_init_done();
     prefetch_map(&rows_map);
     prefetch_map(&cols_map);
+    if constexpr (MX) prefetch_map(&row_scales), prefetch_map(&col_scales);
   }
-  if (warp == 1) tmem_alloc(smem_addr(tmem_slot), tmem_cols(BN));
+  if (warp == 1) tmem_alloc(smem_addr(tmem_slot), tmem_cols(BN, MX));
   tmem_fence_before();
   __syncthreads();
   tmem_fence_after();
@@ -117,21 +127,38 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tile_kernel(const __grid_c
     for (int i = step0; i < step1; ++i) {
       const int s = (i - step0) % kStages, turn = (i - step0) / kStages;
       if (turn > 0 && !bar_wait(empty + 8 * s, (turn - 1) & 1, abort, &g_linear_tile_wait_timeouts)) break;
-      const uint32_t dst = smem_addr(stages) + s * stage_bytes(BN);
-      bar_expect(full + 8 * s, (a.lanes + BN) * kDepth * 2);
+      const uint32_t dst = smem_addr(stages) + s * kStageBytes;
+      bar_expect(full + 8 * s, (a.lanes + BN) * kDepth * 2 + kStageBytes - operand_bytes(BN));
       tma_2d(dst, &rows_map, i * kDepth, row0, full + 8 * s);
       tma_2d(dst + kLanes * kDepth * 2, &cols_map, i * kDepth, col0, full + 8 * s);
+      if constexpr (MX) {
+        tma_3d(dst + operand_bytes(BN), &row_scales, 0, 2 * i, row0 / kMxRows, full + 8 * s);
+        tma_3d(dst + operand_bytes(BN) + 2 * kMxBlock, &col_scales, 0, 2 * i, col0 / kMxRows, full + 8 * s);
+      }
     }
   } else if (warp == 1) {
     for (int i = step0; i < step1; ++i) {
       const int s = (i - step0) % kStages, turn = (i - step0) / kStages;
       if (!warp_wait(full + 8 * s, turn & 1, abort, &g_linear_tile_wait_timeouts)) break;
       tmem_fence_after();
-      const uint32_t src = smem_addr(stages) + s * stage_bytes(BN);
+      const uint32_t src = smem_addr(stages) + s * kStageBytes;
       const uint64_t da = desc_k_major(src), db = desc_k_major(src + kLanes * kDepth * 2);
       if (elect_one()) {
+        if constexpr (MX) {
+          // (what a block of scales holds beyond K's last 64 columns is not used: it need not be there)
+          const uint32_t sa = tmem + acc_cols(BN) + s * 16, sb = sa + 8;
 #pragma unroll
-        for (int k = 0; k < kDepth / 16; ++k) mma_ss(tmem, da + 2 * k, db + 2 * k, mma_shape(kLanes, BN), i > step0 || k > 0);
+          for (int k = 0; k < 4; ++k) {
+            if (k % 2 == 0 && 2 * i + k / 2 < a.mx_blocks) {
+              copy_scales(sa + 2 * k, src + operand_bytes(BN) + k / 2 * kMxBlock);
+              copy_scales(sb + 2 * k, src + operand_bytes(BN) + (2 + k / 2) * kMxBlock);
+            }
+            if (i * 4 + k < (a.K + 15) / 16) mma_mx(tmem, da + 2 * k, db + 2 * k, mx_shape(kLanes, BN, k % 2), sa + k / 2 * 4, sb + k / 2 * 4, i > step0 || k > 0);
+          }
+        } else {
+#pragma unroll
+          for (int k = 0; k < kDepth / 16; ++k) mma_ss(tmem, da + 2 * k, db + 2 * k, mma_shape(kLanes, BN), i > step0 || k > 0);
+        }
         mma_commit(empty + 8 * s);
       }
       __syncwarp();
@@ -175,7 +202,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tile_kernel(const __grid_c
   drain_if_aborted(abort);
   if (warp == 1) {
     tmem_fence_after();
-    tmem_free(tmem, tmem_cols(BN));
+    tmem_free(tmem, tmem_cols(BN, MX));
   }
   if (S > 1) cluster_sync();
   // This CTA's share of the tile's rows, a warp to a row of up to 128 columns (or several shorter ones), a lane to four
@@ -227,22 +254,26 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tile_kernel(const __grid_c
   if (S > 1) cluster_sync();  // (a CTA's shared memory stays until all have read it)
 }
 
-template <int BN, bool SWAP, typename Out>
-cudaError_t launch_one(const TileArgs& t, const CUtensorMap& rows, const CUtensorMap& cols, int64_t tiles, int split, cudaStream_t stream) {
+struct Maps {
+  CUtensorMap rows, cols, row_scales, col_scales;
+};
+
+template <int BN, bool SWAP, typename Out, bool MX>
+cudaError_t launch_one(const TileArgs& t, const Maps& m, int64_t tiles, int split, cudaStream_t stream) {
   const DeviceInfo* dev;
   cudaError_t e = current_device_info(&dev);
   if (e != cudaSuccess) return e;
-  auto kernel = linear_tile_kernel<BN, SWAP, Out>;
+  auto kernel = linear_tile_kernel<BN, SWAP, Out, MX>;
   struct Tag {};
-  if ((e = ensure_dynamic_smem<Tag>(kernel, dev->ordinal, smem_bytes(BN))) != cudaSuccess) return e;
-  return launch_kernel(kernel, tiles * split, kThreads, smem_bytes(BN), split, stream, rows, cols, t);
+  if ((e = ensure_dynamic_smem<Tag>(kernel, dev->ordinal, smem_bytes(BN, MX))) != cudaSuccess) return e;
+  return launch_kernel(kernel, tiles * split, kThreads, smem_bytes(BN, MX), split, stream, m.rows, m.cols, m.row_scales, m.col_scales, t);
 }
 
 template <int BN, bool SWAP>
-cudaError_t launch_out(const approxifer_linear_args& a, const TileArgs& t, const CUtensorMap& rows, const CUtensorMap& cols, int64_t tiles, int split,
-                       cudaStream_t stream) {
-  return a.out_type == APPROXIFER_TYPE_F32 ? launch_one<BN, SWAP, float>(t, rows, cols, tiles, split, stream)
-                                           : launch_one<BN, SWAP, bf16>(t, rows, cols, tiles, split, stream);
+cudaError_t launch_out(const approxifer_linear_args& a, const TileArgs& t, const Maps& m, bool mx, int64_t tiles, int split, cudaStream_t stream) {
+  if (a.out_type == APPROXIFER_TYPE_F32)
+    return mx ? launch_one<BN, SWAP, float, true>(t, m, tiles, split, stream) : launch_one<BN, SWAP, float, false>(t, m, tiles, split, stream);
+  return mx ? launch_one<BN, SWAP, bf16, true>(t, m, tiles, split, stream) : launch_one<BN, SWAP, bf16, false>(t, m, tiles, split, stream);
 }
 
 cudaError_t operand_map(CUtensorMap* map, const uint16_t* base, int64_t rows, int64_t cols, int64_t rstride, int box_rows) {
@@ -265,7 +296,7 @@ bool linear_tile_eligible(const approxifer_linear_args& a) {
          a.w_rstride < (1LL << 38);
 }
 
-cudaError_t launch_linear_tile(const approxifer_linear_args& a, cudaStream_t stream) {
+cudaError_t launch_linear_tile(const approxifer_linear_args& a, const MxScales* mx, cudaStream_t stream) {
   const DeviceInfo* dev;
   cudaError_t e = current_device_info(&dev);
   if (e != cudaSuccess) return e;
@@ -299,7 +330,7 @@ cudaError_t launch_linear_tile(const approxifer_linear_args& a, cudaStream_t str
     const int64_t places = usable / s / tiles_cols;  // tiles along the rows that run at once
     const int64_t even = places > 0 ? ((lanes + places - 1) / places + 7) / 8 * 8 : kLanes;
     for (const int64_t rows : {(int64_t)kLanes, even}) {
-      if (rows > kLanes || rows < kMinLanes) continue;
+      if (rows > kLanes || rows < (mx ? kLanes : kMinLanes)) continue;  // (blocks of scales have 128 rows)
       const int64_t n = (lanes + rows - 1) / rows * tiles_cols, turns = (n * s + usable - 1) / usable;
       const double time = turns * ((double)rows / kLanes * ((t.steps + s - 1) / s) + (s == 1 ? 8 : 10));
       if (tiles == 0 || time < best) best = time, split = s, per_tile = (int)rows, tiles = n;
@@ -307,22 +338,28 @@ cudaError_t launch_linear_tile(const approxifer_linear_args& a, cudaStream_t str
   }
   t.lanes = per_tile;
   if (tiles * split > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
-  CUtensorMap rows, cols;
-  if ((e = operand_map(&rows, swap ? a.Wt : a.X, lanes, a.K, swap ? a.w_rstride : a.x_rstride, per_tile)) != cudaSuccess) return e;
-  if ((e = operand_map(&cols, swap ? a.X : a.Wt, across, a.K, swap ? a.x_rstride : a.w_rstride, bn)) != cudaSuccess) return e;
+  Maps m{};
+  if ((e = operand_map(&m.rows, swap ? a.Wt : a.X, lanes, a.K, swap ? a.w_rstride : a.x_rstride, per_tile)) != cudaSuccess) return e;
+  if ((e = operand_map(&m.cols, swap ? a.X : a.Wt, across, a.K, swap ? a.x_rstride : a.w_rstride, bn)) != cudaSuccess) return e;
+  if (mx) {
+    t.mx_blocks = (int32_t)((mx->K + kMxCols - 1) / kMxCols);
+    auto scales_map = [&](CUtensorMap* map, const uint8_t* base, int64_t n) { return make_scales_map(map, base, (n + kMxRows - 1) / kMxRows, t.mx_blocks, 1); };
+    if ((e = scales_map(&m.row_scales, swap ? mx->w : mx->x, lanes)) != cudaSuccess || (e = scales_map(&m.col_scales, swap ? mx->x : mx->w, across)) != cudaSuccess) return e;
+  }
+  const bool is_mx = mx != nullptr;
   if (swap) {
     switch (bn) {
-      case 16: return launch_out<16, true>(a, t, rows, cols, tiles, split, stream);
-      case 32: return launch_out<32, true>(a, t, rows, cols, tiles, split, stream);
-      case 64: return launch_out<64, true>(a, t, rows, cols, tiles, split, stream);
-      default: return launch_out<128, true>(a, t, rows, cols, tiles, split, stream);
+      case 16: return launch_out<16, true>(a, t, m, is_mx, tiles, split, stream);
+      case 32: return launch_out<32, true>(a, t, m, is_mx, tiles, split, stream);
+      case 64: return launch_out<64, true>(a, t, m, is_mx, tiles, split, stream);
+      default: return launch_out<128, true>(a, t, m, is_mx, tiles, split, stream);
     }
   }
   switch (bn) {
-    case 16: return launch_out<16, false>(a, t, rows, cols, tiles, split, stream);
-    case 32: return launch_out<32, false>(a, t, rows, cols, tiles, split, stream);
-    case 64: return launch_out<64, false>(a, t, rows, cols, tiles, split, stream);
-    default: return launch_out<128, false>(a, t, rows, cols, tiles, split, stream);
+    case 16: return launch_out<16, false>(a, t, m, is_mx, tiles, split, stream);
+    case 32: return launch_out<32, false>(a, t, m, is_mx, tiles, split, stream);
+    case 64: return launch_out<64, false>(a, t, m, is_mx, tiles, split, stream);
+    default: return launch_out<128, false>(a, t, m, is_mx, tiles, split, stream);
   }
 }
 
