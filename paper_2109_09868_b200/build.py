@@ -22,7 +22,7 @@ OBJDIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libapproxifer.so")
 BINDING = os.path.join(HERE, "_hosted.so")  # the hosted-model operators' Python binding (hosted_binding.cpp)
 
-SOURCES = ["api.cu", "tables.cpp", "encode.cu", "decode.cu", "decode_small.cu", "decode_pack.cu", "decode_staged.cu", "locate.cu", "locate_rows.cu", "locate_rows_n8.cu", "locate_rows_n16.cu", "locate_rows_n24.cu", "locate_rows_n32.cu", "host_api.cu", "no_alloc.cu", "hosted_api.cu", "tensor_map.cu", "linear.cu", "linear_tile.cu", "linear_pair.cu", "linear_few.cu", "norm_rope.cu", "attention.cu", "attention_token.cu", "attention_tile.cu", "block_norm.cu", "mx_array.cu", "mx_linear.cu", "prefix.cu"]
+SOURCES = ["api.cu", "tables.cpp", "encode.cu", "decode.cu", "decode_small.cu", "decode_pack.cu", "decode_staged.cu", "locate.cu", "locate_rows.cu", "locate_rows_n8.cu", "locate_rows_n16.cu", "locate_rows_n24.cu", "locate_rows_n32.cu", "host_api.cu", "no_alloc.cu", "hosted_api.cu", "tensor_map.cu", "linear.cu", "linear_tile.cu", "linear_pair.cu", "linear_few.cu", "norm_rope.cu", "attention.cu", "attention_token.cu", "attention_tile.cu", "block_norm.cu", "mx_array.cu", "mx_linear.cu", "mx_pair.cu", "prefix.cu"]
 ARCH = ["-gencode", "arch=compute_100a,code=sm_100a"]
 CFLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall", "--expt-relaxed-constexpr"]
 

@@ -53,6 +53,10 @@ cudaError_t make_tensor_map(CUtensorMap* map, const void* base, int rank, const 
 // neighbours of a row of blocks at a time (of `rows` such rows together), as they lie.  Blocks outside the array read as zero.
 cudaError_t make_scales_map(CUtensorMap* map, const void* base, int64_t row_blocks, int64_t col_blocks, int rows);
 
+// Tensor map of an output [rows][cols] (fp32 or bfloat16) written in pieces of 32 rows of 64 bytes, taken from shared memory with the
+// 64-byte swizzle.  Elements outside the array are not written.
+cudaError_t make_store_map(CUtensorMap* map, void* base, bool f32, int64_t rows, int64_t cols, int64_t rstride);
+
 #ifdef __CUDACC__
 
 constexpr uint32_t kWaitLimit = 1u << 21;  // try_wait attempts (each may block for a while) before a wait gives up

@@ -20,7 +20,7 @@ inline int exact_log2(int32_t v) {
   return -1;
 }
 
-// The scales of a product's 4-bit microscaled operands.  Such a product goes through the kernels below as one of rows of K / 4
+// The scales of a product's 4-bit microscaled operands.  Such a product goes through linear_tile.cu as one of rows of K / 4
 // 16-bit elements (the same bytes), with these.
 struct MxScales {
   const uint8_t *x, *w;
@@ -33,7 +33,7 @@ cudaError_t read_linear_tile_wait_timeouts(unsigned int* out);
 cudaError_t reset_linear_tile_wait_timeouts();
 bool linear_few_wanted(const approxifer_linear_args& a, int sms);  // see linear_few.cu
 cudaError_t launch_linear_few(const approxifer_linear_args& a, cudaStream_t stream);
-cudaError_t launch_linear_pair(const approxifer_linear_args& a, const MxScales* mx, cudaStream_t stream);  // see linear_pair.cu
+cudaError_t launch_linear_pair(const approxifer_linear_args& a, cudaStream_t stream);  // see linear_pair.cu
 cudaError_t read_linear_pair_wait_timeouts(unsigned int* out);
 cudaError_t reset_linear_pair_wait_timeouts();
 cudaError_t launch_norm_rope(const approxifer_norm_rope_args& a, cudaStream_t stream);
@@ -52,6 +52,9 @@ cudaError_t launch_mx_quantize(const approxifer_mx_array_args& a, cudaStream_t s
 cudaError_t launch_mx_dequantize(const approxifer_mx_array_args& a, cudaStream_t stream);
 int64_t mx_linear_workspace(const approxifer_mx_linear_args& a);
 cudaError_t launch_mx_linear(const approxifer_mx_linear_args& a, cudaStream_t stream);
+cudaError_t launch_mx_pair(const approxifer_mx_linear_args& a, cudaStream_t stream);  // X as codes
+cudaError_t read_mx_pair_wait_timeouts(unsigned int* out);
+cudaError_t reset_mx_pair_wait_timeouts();
 int64_t prefix_attention_workspace(const approxifer_prefix_attention_args& a);
 cudaError_t launch_prefix_attention(const approxifer_prefix_attention_args& a, cudaStream_t stream);
 

@@ -59,7 +59,7 @@ int check_prefix_attention(const approxifer_prefix_attention_args& a) {
 
 cudaError_t read_hosted_wait_timeouts(unsigned int* out) {
   *out = 0;
-  for (auto read : {read_linear_tile_wait_timeouts, read_linear_pair_wait_timeouts, read_attention_tile_wait_timeouts, read_block_norm_wait_timeouts}) {
+  for (auto read : {read_linear_tile_wait_timeouts, read_linear_pair_wait_timeouts, read_attention_tile_wait_timeouts, read_block_norm_wait_timeouts, read_mx_pair_wait_timeouts}) {
     unsigned int n = 0;
     const cudaError_t e = read(&n);
     if (e != cudaSuccess) return e;
@@ -68,7 +68,7 @@ cudaError_t read_hosted_wait_timeouts(unsigned int* out) {
   return cudaSuccess;
 }
 cudaError_t reset_hosted_wait_timeouts() {
-  for (auto reset : {reset_linear_tile_wait_timeouts, reset_linear_pair_wait_timeouts, reset_attention_tile_wait_timeouts, reset_block_norm_wait_timeouts}) {
+  for (auto reset : {reset_linear_tile_wait_timeouts, reset_linear_pair_wait_timeouts, reset_attention_tile_wait_timeouts, reset_block_norm_wait_timeouts, reset_mx_pair_wait_timeouts}) {
     const cudaError_t e = reset();
     if (e != cudaSuccess) return e;
   }

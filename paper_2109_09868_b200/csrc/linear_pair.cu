@@ -14,7 +14,7 @@
 // Bound by the tensor cores, for seconds on end by the power limit.  Measured: 8,192 x 16,384 x 4,096 with bias and gelu
 // 709 us, 1,551 TFLOP/s (1,619 is what a library product of 8,192^3 reaches); repeated for a second 817 to 872 us, 1.26 to 1.35
 // PFLOP/s, with the SM clock.  With K = 64 (130 us) the epilogue is what is left.
-#include "mx.cuh"
+#include "async.cuh"
 
 namespace approxifer {
 
@@ -24,25 +24,14 @@ namespace {
 
 constexpr int kThreads = 384;
 constexpr int kEpilogueWarps = 8;
-constexpr int kTileM = 256, kDepth = 64;
+constexpr int kTileM = 256, kTileN = 256, kDepth = 64;
 constexpr int kStages = 5;
 constexpr int kTurnBytes = 32 * 32 * 4;           // of an epilogue warp
-constexpr int kRowBytes = kDepth * 2;
-constexpr int kHalfBytes = 128 * kRowBytes;       // rows of X of one CTA per stage
+constexpr int kHalfBytes = 128 * kDepth * 2;      // one operand of one CTA per stage
+constexpr int kStageBytes = 2 * kHalfBytes;
 constexpr int kHeader = 1024;
+constexpr int kSmemBytes = kHeader + 1024 + kStages * kStageBytes + kEpilogueWarps * kTurnBytes;
 constexpr int kTmemCols = 512;
-// MX: both operands 4-bit microscaled, 256 columns a stage, tiles of 192 columns: two accumulators and, of each stage, 24 columns
-// of scales (two blocks for the CTA's rows of X, two times two for the tile's rows of Wt, of which each CTA needs all) fill the
-// tensor memory.
-template <bool MX>
-struct Plan {
-  static constexpr int kTileN = MX ? 192 : 256;
-  static constexpr int kOperandBytes = kHalfBytes + kTileN / 2 * kRowBytes;
-  static constexpr int kStageBytes = kOperandBytes + (MX ? 6 * kMxBlock : 0);
-  static constexpr int kSmemBytes = kHeader + 1024 + kStages * kStageBytes + kEpilogueWarps * kTurnBytes;
-  static constexpr int kScaleCols = 24;
-};
-static_assert(2 * Plan<true>::kTileN + kStages * Plan<true>::kScaleCols <= kTmemCols, "the scales exceed the tensor memory");
 constexpr int kGroupM = 8;  // rows of tiles that are walked together: their X stays in L2 while Wt streams by
 
 struct PairArgs {
@@ -51,12 +40,10 @@ struct PairArgs {
   const void* R;
   void* Y;
   int64_t r_rstride, y_rstride;
-  int32_t mx_blocks;  // (MX) blocks of 128 columns
   int32_t vec;  // Y and R can be accessed four elements at a time
 };
 
 // Tiles in bands of kGroupM rows of tiles, down a band's columns of tiles.
-template <int kTileN>
 __device__ __forceinline__ void place(const PairArgs& a, int tile, int* m0, int* n0) {
   const int per_band = kGroupM * a.tiles_n, band = tile / per_band, in = tile - band * per_band;
   const int rows = min(kGroupM, a.tiles_m - band * kGroupM);
@@ -113,11 +100,9 @@ __device__ __forceinline__ void finish32(const PairArgs& a, int m0, int n, const
   }
 }
 
-template <typename Out, int ACT, bool MX>
+template <typename Out, int ACT>
 __global__ void __launch_bounds__(kThreads, 1)
-    linear_pair_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap x_scales,
-                       const __grid_constant__ CUtensorMap w_scales, const __grid_constant__ PairArgs a) {
-  constexpr int kTileN = Plan<MX>::kTileN, kOperandBytes = Plan<MX>::kOperandBytes, kStageBytes = Plan<MX>::kStageBytes;
+    linear_pair_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map, const __grid_constant__ PairArgs a) {
   extern __shared__ unsigned char raw[];
   unsigned char* base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
   uint64_t* bars = reinterpret_cast<uint64_t*>(base);  // full[stages], empty[stages], ready[2], free[2]
@@ -137,7 +122,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     bar_init_done();
     prefetch_map(&x_map);
     prefetch_map(&w_map);
-    if constexpr (MX) prefetch_map(&x_scales), prefetch_map(&w_scales);
   }
   if (warp == 1) tmem_alloc_pair(smem_addr(tmem_slot), kTmemCols);
   tmem_fence_before();
@@ -153,9 +137,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     bool ok = true;
     for (int tile = pair; tile < a.tiles && ok; tile += pairs) {
       int m0, n0;
-      place<kTileN>(a, tile, &m0, &n0);
-      const int tile_n = n0;
-      m0 += rank * 128, n0 += rank * (kTileN / 2);
+      place(a, tile, &m0, &n0);
+      m0 += rank * 128, n0 += rank * 128;
       for (int k = 0; k < a.steps; ++k, ++it) {
         const int s = it % kStages, turn = it / kStages;
         if (turn > 0 && !(ok = bar_wait(empty + 8 * s, (turn - 1) & 1, abort, count))) break;
@@ -163,10 +146,6 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t bar = peer_smem(full + 8 * s, 0), dst = stages + s * kStageBytes;
         tma_2d_pair(dst, &x_map, k * kDepth, m0, bar);
         tma_2d_pair(dst + kHalfBytes, &w_map, k * kDepth, n0, bar);
-        if constexpr (MX) {
-          tma_3d_pair(dst + kOperandBytes, &x_scales, 0, 2 * k, m0 / kMxRows, bar);
-          tma_3d_pair(dst + kOperandBytes + 2 * kMxBlock, &w_scales, 0, 2 * k, tile_n / kMxRows, bar);
-        }
       }
     }
   } else if (warp == 1 && rank == 0) {
@@ -174,12 +153,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     bool ok = true;
     for (int tile = pair; tile < a.tiles && ok; tile += pairs, ++n) {
       const int acc = n & 1;
-      uint32_t skip = 0;  // (MX) columns of scales of rows of Wt before the tile's: it starts at the block's first row or in its middle
-      if constexpr (MX) {
-        int m0, n0;
-        place<kTileN>(a, tile, &m0, &n0);
-        skip = n0 % kMxRows / 32;
-      }
       if (n >= 2 && !(ok = warp_wait(drained + 8 * acc, (n / 2 - 1) & 1, abort, count))) break;
       tmem_fence_after();
       for (int k = 0; k < a.steps; ++k, ++it) {
@@ -189,19 +162,6 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t src = stages + s * kStageBytes;
         const uint64_t da = desc_k_major(src), db = desc_k_major(src + kHalfBytes);
         if (elect_one()) {
-          if constexpr (MX) {
-            const uint32_t sa = tmem + 2 * kTileN + s * Plan<MX>::kScaleCols, sb = sa + 8, from = src + kOperandBytes;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              if (j % 2 == 0 && 2 * k + j / 2 < a.mx_blocks) {
-                copy_scales_pair(sa + 2 * j, from + j / 2 * kMxBlock);
-                copy_scales_pair(sb + 4 * j, from + (2 + j / 2) * kMxBlock);
-                copy_scales_pair(sb + 4 * j + 4, from + (4 + j / 2) * kMxBlock);
-              }
-              if (k * 4 + j < (a.K + 15) / 16)
-                mma_mx_pair(tmem + acc * kTileN, da + 2 * j, db + 2 * j, mx_shape(kTileM, kTileN, j % 2), sa + j / 2 * 4, sb + j / 2 * 8 + skip, k > 0 || j > 0);
-            }
-          } else
 #pragma unroll
           for (int j = 0; j < kDepth / 16; ++j) mma_ss_pair(tmem + acc * kTileN, da + 2 * j, db + 2 * j, mma_shape(kTileM, kTileN), k > 0 || j > 0);
           mma_commit_pair(empty + 8 * s);
@@ -217,7 +177,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int tile = pair; tile < a.tiles; tile += pairs, ++n) {
       const int acc = n & 1;
       int m0, n0;
-      place<kTileN>(a, tile, &m0, &n0);
+      place(a, tile, &m0, &n0);
       if (!warp_wait(ready + 8 * acc, (n / 2) & 1, abort, count)) break;
       tmem_fence_after();
       float4* turn = reinterpret_cast<float4*>(base + kHeader + kStages * kStageBytes + (warp - 4) * kTurnBytes);
@@ -245,28 +205,24 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (warp == 1) tmem_free_pair(tmem, kTmemCols);
 }
 
-struct Maps {
-  CUtensorMap x, w, x_scales, w_scales;
-};
-
-template <typename Out, int ACT, bool MX>
-cudaError_t launch_kind(const PairArgs& t, const Maps& m, const DeviceInfo& dev, cudaStream_t stream) {
-  auto kernel = linear_pair_kernel<Out, ACT, MX>;
+template <typename Out, int ACT>
+cudaError_t launch_act(const PairArgs& t, const CUtensorMap& x, const CUtensorMap& w, const DeviceInfo& dev, cudaStream_t stream) {
+  auto kernel = linear_pair_kernel<Out, ACT>;
   struct Tag {};
-  const cudaError_t e = ensure_dynamic_smem<Tag>(kernel, dev.ordinal, Plan<MX>::kSmemBytes);
+  const cudaError_t e = ensure_dynamic_smem<Tag>(kernel, dev.ordinal, kSmemBytes);
   if (e != cudaSuccess) return e;
   const int pairs = t.tiles < dev.sms / 2 ? t.tiles : dev.sms / 2;
-  return launch_kernel(kernel, 2 * pairs, kThreads, Plan<MX>::kSmemBytes, 2, stream, m.x, m.w, m.x_scales, m.w_scales, t);
+  return launch_kernel(kernel, 2 * pairs, kThreads, kSmemBytes, 2, stream, x, w, t);
 }
 
-template <typename Out, bool MX>
-cudaError_t launch_out(int act, const PairArgs& t, const Maps& m, const DeviceInfo& dev, cudaStream_t stream) {
+template <typename Out>
+cudaError_t launch_out(int act, const PairArgs& t, const CUtensorMap& x, const CUtensorMap& w, const DeviceInfo& dev, cudaStream_t stream) {
   switch (act) {
-    case APPROXIFER_ACT_RELU: return launch_kind<Out, APPROXIFER_ACT_RELU, MX>(t, m, dev, stream);
-    case APPROXIFER_ACT_GELU: return launch_kind<Out, APPROXIFER_ACT_GELU, MX>(t, m, dev, stream);
-    case APPROXIFER_ACT_GELU_TANH: return launch_kind<Out, APPROXIFER_ACT_GELU_TANH, MX>(t, m, dev, stream);
-    case APPROXIFER_ACT_SILU: return launch_kind<Out, APPROXIFER_ACT_SILU, MX>(t, m, dev, stream);
-    default: return launch_kind<Out, APPROXIFER_ACT_NONE, MX>(t, m, dev, stream);
+    case APPROXIFER_ACT_RELU: return launch_act<Out, APPROXIFER_ACT_RELU>(t, x, w, dev, stream);
+    case APPROXIFER_ACT_GELU: return launch_act<Out, APPROXIFER_ACT_GELU>(t, x, w, dev, stream);
+    case APPROXIFER_ACT_GELU_TANH: return launch_act<Out, APPROXIFER_ACT_GELU_TANH>(t, x, w, dev, stream);
+    case APPROXIFER_ACT_SILU: return launch_act<Out, APPROXIFER_ACT_SILU>(t, x, w, dev, stream);
+    default: return launch_act<Out, APPROXIFER_ACT_NONE>(t, x, w, dev, stream);
   }
 }
 
@@ -278,15 +234,14 @@ cudaError_t reset_linear_pair_wait_timeouts() {
   return cudaMemcpyToSymbol(g_linear_pair_wait_timeouts, &zero, sizeof(zero));
 }
 
-cudaError_t launch_linear_pair(const approxifer_linear_args& a, const MxScales* mx, cudaStream_t stream) {
+cudaError_t launch_linear_pair(const approxifer_linear_args& a, cudaStream_t stream) {
   const DeviceInfo* dev;
   cudaError_t e = current_device_info(&dev);
   if (e != cudaSuccess) return e;
   PairArgs t{};
   t.M = (int32_t)a.M, t.N = (int32_t)a.N, t.K = (int32_t)a.K;
   t.steps = (int32_t)((a.K + kDepth - 1) / kDepth);
-  const int tile_n = mx ? Plan<true>::kTileN : Plan<false>::kTileN;
-  const int64_t tm = (a.M + kTileM - 1) / kTileM, tn = (a.N + tile_n - 1) / tile_n;
+  const int64_t tm = (a.M + kTileM - 1) / kTileM, tn = (a.N + kTileN - 1) / kTileN;
   if (tm * tn > 0x3fffffffLL || tn > (1 << 27)) return cudaErrorInvalidConfiguration;
   t.tiles_m = (int32_t)tm, t.tiles_n = (int32_t)tn, t.tiles = (int32_t)(tm * tn);
   t.bias = reinterpret_cast<const bf16*>(a.bias), t.R = a.R, t.Y = a.Y, t.r_rstride = a.r_rstride, t.y_rstride = a.y_rstride;
@@ -294,18 +249,10 @@ cudaError_t launch_linear_pair(const approxifer_linear_args& a, const MxScales* 
   auto fits = [&](const void* p) { return reinterpret_cast<uintptr_t>(p) % quad == 0; };
   t.vec = fits(a.Y) && a.y_rstride % 4 == 0 && (!a.R || (fits(a.R) && a.r_rstride % 4 == 0));
   const uint64_t xe[2] = {(uint64_t)a.K, (uint64_t)a.M}, xs[2] = {1, (uint64_t)a.x_rstride}, we[2] = {(uint64_t)a.K, (uint64_t)a.N}, ws[2] = {1, (uint64_t)a.w_rstride};
-  const uint32_t x_box[2] = {(uint32_t)kDepth, 128}, w_box[2] = {(uint32_t)kDepth, (uint32_t)tile_n / 2};
-  Maps m{};
-  if ((e = make_tensor_map(&m.x, a.X, 2, xe, xs, x_box)) != cudaSuccess || (e = make_tensor_map(&m.w, a.Wt, 2, we, ws, w_box)) != cudaSuccess) return e;
-  const bool f32 = a.out_type == APPROXIFER_TYPE_F32;
-  if (mx) {
-    t.mx_blocks = (int32_t)((mx->K + kMxCols - 1) / kMxCols);
-    if ((e = make_scales_map(&m.x_scales, mx->x, (a.M + kMxRows - 1) / kMxRows, t.mx_blocks, 1)) != cudaSuccess ||
-        (e = make_scales_map(&m.w_scales, mx->w, (a.N + kMxRows - 1) / kMxRows, t.mx_blocks, 2)) != cudaSuccess)
-      return e;
-    return f32 ? launch_out<float, true>(a.activation, t, m, *dev, stream) : launch_out<bf16, true>(a.activation, t, m, *dev, stream);
-  }
-  return f32 ? launch_out<float, false>(a.activation, t, m, *dev, stream) : launch_out<bf16, false>(a.activation, t, m, *dev, stream);
+  const uint32_t box[2] = {(uint32_t)kDepth, 128};
+  CUtensorMap x, w;
+  if ((e = make_tensor_map(&x, a.X, 2, xe, xs, box)) != cudaSuccess || (e = make_tensor_map(&w, a.Wt, 2, we, ws, box)) != cudaSuccess) return e;
+  return a.out_type == APPROXIFER_TYPE_F32 ? launch_out<float>(a.activation, t, x, w, *dev, stream) : launch_out<bf16>(a.activation, t, x, w, *dev, stream);
 }
 
 }  // namespace approxifer

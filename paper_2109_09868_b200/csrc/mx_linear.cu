@@ -28,7 +28,7 @@ cudaError_t launch_mx_linear(const approxifer_mx_linear_args& given, cudaStream_
   b.bias = a.bias, b.R = a.R, b.r_rstride = a.r_rstride, b.Y = a.Y, b.y_rstride = a.y_rstride, b.activation = a.activation, b.out_type = a.out_type;
   const MxScales scales{a.x_scales, a.w_scales, a.K};
   // As for bfloat16: pairs of CTAs once the tiles of one CTA would need a second turn.
-  if (a.M > 128 && a.N > 128 && ((a.M + 127) / 128) * ((a.N + 127) / 128) > dev->sms) return launch_linear_pair(b, &scales, stream);
+  if (a.M > 128 && a.N > 128 && ((a.M + 127) / 128) * ((a.N + 127) / 128) > dev->sms) return launch_mx_pair(a, stream);
   return launch_linear_tile(b, &scales, stream);
 }
 

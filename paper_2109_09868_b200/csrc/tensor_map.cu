@@ -46,4 +46,15 @@ cudaError_t make_scales_map(CUtensorMap* map, const void* base, int64_t row_bloc
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
+cudaError_t make_store_map(CUtensorMap* map, void* base, bool f32, int64_t rows, int64_t cols, int64_t rstride) {
+  Encode encode;
+  const cudaError_t e = find_encode(&encode);
+  if (e != cudaSuccess) return e;
+  const cuuint64_t ext[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, bytes[1] = {(cuuint64_t)rstride * (f32 ? 4 : 2)};
+  const cuuint32_t box[2] = {f32 ? 16u : 32u, 32}, ones[2] = {1, 1};
+  const CUresult r = encode(map, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, ext, bytes, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                            CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
 }  // namespace approxifer
