@@ -20,15 +20,17 @@ inline int exact_log2(int32_t v) {
   return -1;
 }
 
+constexpr int kMxRawRows = 32;
 // The scales of a product's 4-bit microscaled operands.  Such a product goes through linear_tile.cu as one of rows of K / 4
 // 16-bit elements (the same bytes), with these.
 struct MxScales {
-  const uint8_t *x, *w;
+  const uint8_t *x, *w;  // x NULL: X is bfloat16 and brought into the 4-bit form within the kernel, which takes few rows of it
   int64_t K;  // in 4-bit elements
 };
 cudaError_t launch_linear(const approxifer_linear_args& a, cudaStream_t stream);
 bool linear_tile_eligible(const approxifer_linear_args& a);  // see linear_tile.cu
 cudaError_t launch_linear_tile(const approxifer_linear_args& a, const MxScales* mx, cudaStream_t stream);
+bool linear_tile_takes_raw(const approxifer_linear_args& a, int sms);
 cudaError_t read_linear_tile_wait_timeouts(unsigned int* out);
 cudaError_t reset_linear_tile_wait_timeouts();
 bool linear_few_wanted(const approxifer_linear_args& a, int sms);  // see linear_few.cu

@@ -25,22 +25,28 @@ __device__ unsigned int g_linear_tile_wait_timeouts = 0;
 
 namespace {
 
-constexpr int kThreads = 192;
+// What the operands are: bfloat16; both 4-bit microscaled (256 columns, and two blocks of each operand's scales, a stage); the same
+// with X in bfloat16, brought into the 4-bit form on its way into shared memory, where all of this CTA's part of it stays.
+enum Kind { kBf16, kMx, kMxRaw };
+constexpr int kRawWarps = 16;  // at most, that do so, after the first two
+constexpr int kRawSteps = 16;  // stages of K that there is room for
+constexpr int threads_of(Kind kind) { return kind == kMxRaw ? (2 + kRawWarps) * 32 : 192; }  // (at most)
 constexpr int kLanes = 128;   // rows of the first operand per tile ...
 constexpr int kMinLanes = 96; // ... and the fewest worth having (with less a copy is too short to keep HBM busy)
 constexpr int kDepth = 64;    // columns of both operands per stage: one 128-byte swizzle row
 constexpr int kHeader = 1024; // mbarriers, flags; keeps the stages 1,024-byte aligned
 
-// MX: both operands 4-bit microscaled, 256 columns and two blocks of each operand's scales a stage.
-constexpr int operand_bytes(int bn) { return (kLanes + bn) * kDepth * 2; }
-constexpr int stage_bytes(int bn, bool mx) { return operand_bytes(bn) + (mx ? 4 * kMxBlock : 0); }
-constexpr int stages_of(int bn, bool mx) { return 196 * 1024 / stage_bytes(bn, mx); }
-constexpr int smem_bytes(int bn, bool mx) { return kHeader + 1024 + stages_of(bn, mx) * stage_bytes(bn, mx); }
+constexpr int rows_bytes(Kind kind) { return kLanes * kDepth * 2 + (kind == kBf16 ? 0 : 2 * kMxBlock); }
+constexpr int cols_bytes(int bn, Kind kind) { return bn * kDepth * 2 + (kind == kBf16 ? 0 : 2 * kMxBlock); }
+constexpr int raw_bytes(int bn, Kind kind) { return kind == kMxRaw ? kRawSteps * cols_bytes(bn, kind) : 0; }
+constexpr int stage_bytes(int bn, Kind kind) { return rows_bytes(kind) + (kind == kMxRaw ? 0 : cols_bytes(bn, kind)); }
+constexpr int stages_of(int bn, Kind kind) { return (196 * 1024 - raw_bytes(bn, kind)) / stage_bytes(bn, kind); }
+constexpr int smem_bytes(int bn, Kind kind) { return kHeader + 1024 + stages_of(bn, kind) * stage_bytes(bn, kind) + raw_bytes(bn, kind); }
 constexpr int acc_cols(int bn) { return bn < 32 ? 32 : bn; }
-// (MX: behind the accumulator sixteen columns of scales a stage)
-constexpr int tmem_cols(int bn, bool mx) { return mx ? 256 : acc_cols(bn); }
-static_assert(acc_cols(16) + 16 * stages_of(16, true) <= 256 && acc_cols(32) + 16 * stages_of(32, true) <= 256 && acc_cols(64) + 16 * stages_of(64, true) <= 256 &&
-                  acc_cols(128) + 16 * stages_of(128, true) <= 256,
+// (4 bits: behind the accumulator sixteen columns of scales a stage)
+constexpr int tmem_cols(int bn, Kind kind) { return kind == kBf16 ? acc_cols(bn) : 256; }
+static_assert(acc_cols(16) + 16 * stages_of(16, kMx) <= 256 && acc_cols(32) + 16 * stages_of(32, kMx) <= 256 && acc_cols(64) + 16 * stages_of(64, kMx) <= 256 &&
+                  acc_cols(128) + 16 * stages_of(128, kMx) <= 256,
               "the scales exceed the tensor memory");
 
 struct TileArgs {
@@ -53,7 +59,10 @@ struct TileArgs {
   void* Y;
   int64_t r_rstride, y_rstride;
   int32_t activation;
-  int32_t mx_blocks;      // (MX) blocks of 128 columns
+  int32_t mx_blocks;      // (4 bits) blocks of 128 columns
+  const bf16* raw;        // (kMxRaw) X
+  int64_t raw_rstride;
+  int32_t raw_columns, raw_whole;  // ... its columns; 16 bytes at a time
   int32_t vec, bias_vec;  // rows of Y and R, the bias, can be accessed four elements at a time
 };
 
@@ -87,18 +96,77 @@ __device__ __forceinline__ void write4(Out* p, float4 v, bool vec, int count) {
   if (count > 3) p[3] = narrow<Out>(v.w);
 }
 
-template <int BN, bool SWAP, typename Out, bool MX>
-__global__ void __launch_bounds__(kThreads, 1) linear_tile_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_constant__ CUtensorMap cols_map,
+// (kMxRaw) This warp's share of X's columns of stages step0 .. step1-1, brought into the 4-bit form.  Half a warp takes a row's 128
+// columns (one of the stage's two blocks) at a time, rows and then stages in turn, with the other warps; the
+// loads of the next four are in flight meanwhile.
+template <int BN>
+__device__ __forceinline__ void bring_raw(const TileArgs& a, unsigned char* to, uint32_t landed, int step0, int step1, int warps, int warp, int lane) {
+  constexpr int kAhead = 4;
+  struct Place {
+    int stage, row;
+    __device__ __forceinline__ void next(int stages_on, int rows_on, int rows) {
+      stage += stages_on, row += rows_on;
+      if (row >= rows) row -= rows, ++stage;
+    }
+  };
+  const int M = a.M, half = lane / 16, at = lane % 16 * 8, stages = step1 - step0, stages_on = warps / M, rows_on = warps % M;
+  const bf16* from = a.raw + (int64_t)step0 * 4 * kDepth + half * kMxCols + at;
+  const int columns = a.raw_columns - step0 * 4 * kDepth - half * kMxCols - at;  // from there on
+  Place get{warp / M, warp % M}, use = get;
+  MxRow<bf16> v[kAhead];
+  auto load = [&](MxRow<bf16>& x) {
+    x.none();
+    const int col = get.stage * 4 * kDepth;
+    if (get.stage < stages && col < columns) {
+      const bf16* p = from + get.row * a.raw_rstride + col;
+      if (a.raw_whole) x.load<true>(p);
+      else x.load<false>(p);
+    }
+    get.next(stages_on, rows_on, M);
+  };
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) load(v[i]);
+  unsigned char* codes_to = to + ((half * kMxCols + at) / 32 << 4) + at / 2 % 16;
+  unsigned char* scales_to = to + BN * 128 + half * kMxBlock + at / 32;
+  int told = 0;  // stages that this warp has said to be there
+  while (told < stages) {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      uint32_t byte;
+      const uint32_t codes = mx_quantize8(v[i].widened(), &byte);
+      load(v[i]);
+      if (use.stage < stages) {
+        const int offset = use.stage * cols_bytes(BN, kMxRaw);
+        *reinterpret_cast<uint32_t*>(to + offset + use.row * 128 + ((int)(codes_to - to) ^ ((use.row & 7) << 4))) = codes;  // (the 128-byte swizzle)
+        if (lane % 4 == 0) scales_to[offset + use.row * 16] = (unsigned char)byte;
+      }
+      use.next(stages_on, rows_on, M);
+      const int whole = min(use.stage, stages);
+      if (told < whole) {
+        async_proxy_fence();
+        __syncwarp();
+        if (lane == 0)
+          for (int x = told; x < whole; ++x) bar_arrive(landed + 8 * x);
+        told = whole;
+      }
+    }
+  }
+}
+
+template <int BN, bool SWAP, typename Out, Kind KIND>
+__global__ void __launch_bounds__(threads_of(KIND), 1) linear_tile_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_constant__ CUtensorMap cols_map,
                                                                const __grid_constant__ CUtensorMap row_scales, const __grid_constant__ CUtensorMap col_scales,
                                                                const __grid_constant__ TileArgs a) {
-  constexpr int kStages = stages_of(BN, MX), kStageBytes = stage_bytes(BN, MX);
+  const int warps = KIND == kMxRaw ? (int)blockDim.x / 32 : threads_of(KIND) / 32;
+  constexpr int kStages = stages_of(BN, KIND), kStageBytes = stage_bytes(BN, KIND);
   extern __shared__ unsigned char raw[];
   unsigned char* base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
-  uint64_t* bars = reinterpret_cast<uint64_t*>(base);  // full[stages], empty[stages], done
+  uint64_t* bars = reinterpret_cast<uint64_t*>(base);  // full[stages], empty[stages], done, (kMxRaw) landed[steps]
   volatile int* abort = reinterpret_cast<volatile int*>(base + 512);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(base + 516);
   unsigned char* stages = base + kHeader;
-  const uint32_t full = smem_addr(bars), empty = full + 8 * kStages, done = empty + 8 * kStages;
+  unsigned char* raw_at = stages + kStages * kStageBytes;
+  const uint32_t full = smem_addr(bars), empty = full + 8 * kStages, done = empty + 8 * kStages, landed = done + 8;
   const int warp = warp_index(), lane = threadIdx.x % 32;
 
   const int S = (int)cluster_size(), rank = (int)cluster_rank();
@@ -109,13 +177,15 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tile_kernel(const __grid_c
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) bar_init(full + 8 * s, 1), bar_init(empty + 8 * s, 1);
     bar_init(done, 1);
+    for (int s = 0; KIND == kMxRaw && s < kRawSteps; ++s) bar_init(landed + 8 * s, warps - 2);
     *abort = 0;
     bar_init_done();
     prefetch_map(&rows_map);
-    prefetch_map(&cols_map);
-    if constexpr (MX) prefetch_map(&row_scales), prefetch_map(&col_scales);
+    if constexpr (KIND != kMxRaw) prefetch_map(&cols_map);
+    if constexpr (KIND != kBf16) prefetch_map(&row_scales);
+    if constexpr (KIND == kMx) prefetch_map(&col_scales);
   }
-  if (warp == 1) tmem_alloc(smem_addr(tmem_slot), tmem_cols(BN, MX));
+  if (warp == 1) tmem_alloc(smem_addr(tmem_slot), tmem_cols(BN, KIND));
   tmem_fence_before();
   __syncthreads();
   tmem_fence_after();
@@ -128,31 +198,33 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tile_kernel(const __grid_c
       const int s = (i - step0) % kStages, turn = (i - step0) / kStages;
       if (turn > 0 && !bar_wait(empty + 8 * s, (turn - 1) & 1, abort, &g_linear_tile_wait_timeouts)) break;
       const uint32_t dst = smem_addr(stages) + s * kStageBytes;
-      bar_expect(full + 8 * s, (a.lanes + BN) * kDepth * 2 + kStageBytes - operand_bytes(BN));
+      bar_expect(full + 8 * s, kStageBytes - (kLanes - a.lanes) * kDepth * 2);
       tma_2d(dst, &rows_map, i * kDepth, row0, full + 8 * s);
-      tma_2d(dst + kLanes * kDepth * 2, &cols_map, i * kDepth, col0, full + 8 * s);
-      if constexpr (MX) {
-        tma_3d(dst + operand_bytes(BN), &row_scales, 0, 2 * i, row0 / kMxRows, full + 8 * s);
-        tma_3d(dst + operand_bytes(BN) + 2 * kMxBlock, &col_scales, 0, 2 * i, col0 / kMxRows, full + 8 * s);
-      }
+      if constexpr (KIND != kMxRaw) tma_2d(dst + rows_bytes(KIND), &cols_map, i * kDepth, col0, full + 8 * s);
+      if constexpr (KIND != kBf16) tma_3d(dst + kLanes * kDepth * 2, &row_scales, 0, 2 * i, row0 / kMxRows, full + 8 * s);
+      if constexpr (KIND == kMx) tma_3d(dst + rows_bytes(KIND) + BN * kDepth * 2, &col_scales, 0, 2 * i, col0 / kMxRows, full + 8 * s);
     }
   } else if (warp == 1) {
     for (int i = step0; i < step1; ++i) {
       const int s = (i - step0) % kStages, turn = (i - step0) / kStages;
+      if (KIND == kMxRaw && !warp_wait(landed + 8 * (i - step0), 0, abort, &g_linear_tile_wait_timeouts)) break;
       if (!warp_wait(full + 8 * s, turn & 1, abort, &g_linear_tile_wait_timeouts)) break;
       tmem_fence_after();
       const uint32_t src = smem_addr(stages) + s * kStageBytes;
-      const uint64_t da = desc_k_major(src), db = desc_k_major(src + kLanes * kDepth * 2);
+      const uint32_t cols = KIND == kMxRaw ? smem_addr(raw_at) + (i - step0) * cols_bytes(BN, KIND) : src + rows_bytes(KIND);
+      const uint64_t da = desc_k_major(src), db = desc_k_major(cols);
       if (elect_one()) {
-        if constexpr (MX) {
+        if constexpr (KIND != kBf16) {
           // (what a block of scales holds beyond K's last 64 columns is not used: it need not be there)
           const uint32_t sa = tmem + acc_cols(BN) + s * 16, sb = sa + 8;
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            if (k % 2 == 0 && 2 * i + k / 2 < a.mx_blocks) {
-              copy_scales(sa + 2 * k, src + operand_bytes(BN) + k / 2 * kMxBlock);
-              copy_scales(sb + 2 * k, src + operand_bytes(BN) + (2 + k / 2) * kMxBlock);
+          for (int k = 0; k < 2; ++k)
+            if (2 * i + k < a.mx_blocks) {
+              copy_scales(sa + 4 * k, src + kLanes * kDepth * 2 + k * kMxBlock);
+              copy_scales(sb + 4 * k, cols + BN * kDepth * 2 + k * kMxBlock);
             }
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
             if (i * 4 + k < (a.K + 15) / 16) mma_mx(tmem, da + 2 * k, db + 2 * k, mx_shape(kLanes, BN, k % 2), sa + k / 2 * 4, sb + k / 2 * 4, i > step0 || k > 0);
           }
         } else {
@@ -164,13 +236,15 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tile_kernel(const __grid_c
       __syncwarp();
     }
     if (elect_one()) mma_commit(done);
+  } else if (KIND == kMxRaw && warp >= 2) {
+    bring_raw<BN>(a, raw_at, landed, step0, step1, warps - 2, warp - 2, lane);
   }
   __syncwarp();
   // Accumulator -> shared memory, in the order of the output: [m][n], n contiguous.  (`done` also says that every copy has
   // been consumed, so the stages can be written over.)
   constexpr int kPitch = SWAP ? kLanes : BN + 4;
   float* part = reinterpret_cast<float*>(stages);
-  if (warp >= 2) {
+  if (warp >= 2 && warp < 6) {
     const bool ok = warp_wait(done, 0, abort, &g_linear_tile_wait_timeouts);
     tmem_fence_after();
     const int q = warp % 4, l = q * 32 + lane;
@@ -202,7 +276,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tile_kernel(const __grid_c
   drain_if_aborted(abort);
   if (warp == 1) {
     tmem_fence_after();
-    tmem_free(tmem, tmem_cols(BN, MX));
+    tmem_free(tmem, tmem_cols(BN, KIND));
   }
   if (S > 1) cluster_sync();
   // This CTA's share of the tile's rows, a warp to a row of up to 128 columns (or several shorter ones), a lane to four
@@ -210,18 +284,18 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tile_kernel(const __grid_c
   const int m0 = SWAP ? col0 : row0, n0 = SWAP ? row0 : col0;
   const int rows_here = min(SWAP ? BN : a.lanes, a.M - m0);
   const int m_from = rows_here * rank / S, m_to = rows_here * (rank + 1) / S;
-  constexpr int kQuads = SWAP ? 32 : BN / 4, kSide = 32 / kQuads, kAhead = 4, kWarps = kThreads / 32;
+  constexpr int kQuads = SWAP ? 32 : BN / 4, kSide = 32 / kQuads, kAhead = 4;
   const int n = (lane % kQuads) * 4, count = a.N - (n0 + n);
   if (n < (SWAP ? a.lanes : BN) && count > 0) {
     const uint32_t part_addr = smem_addr(part) + n * 4;
     const float4 b = a.bias ? read4<bf16>(a.bias + n0 + n, a.bias_vec, count) : make_float4(0.f, 0.f, 0.f, 0.f);
     const Out* R = static_cast<const Out*>(a.R) + n0 + n;
     Out* Y = static_cast<Out*>(a.Y) + n0 + n;
-    for (int m = m_from + warp * kSide + lane / kQuads; m < m_to; m += kWarps * kSide * kAhead) {
+    for (int m = m_from + warp * kSide + lane / kQuads; m < m_to; m += warps * kSide * kAhead) {
       float4 v[kAhead], r[kAhead];
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) {
-        const int mi = m + i * kWarps * kSide;
+        const int mi = m + i * warps * kSide;
         v[i] = r[i] = make_float4(0.f, 0.f, 0.f, 0.f);
         if (mi >= m_to) continue;
         if (S == 1) v[i] = *reinterpret_cast<const float4*>(part + mi * kPitch + n);
@@ -233,7 +307,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tile_kernel(const __grid_c
           const uint32_t peer = peer_smem(part_addr, s);
 #pragma unroll
           for (int i = 0; i < kAhead; ++i) {
-            const int mi = m + i * kWarps * kSide;
+            const int mi = m + i * warps * kSide;
             if (mi >= m_to) continue;
             const float4 u = peer_load(peer + mi * kPitch * 4);
             v[i].x += u.x, v[i].y += u.y, v[i].z += u.z, v[i].w += u.w;
@@ -242,7 +316,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tile_kernel(const __grid_c
       }
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) {
-        const int mi = m + i * kWarps * kSide;
+        const int mi = m + i * warps * kSide;
         if (mi >= m_to) continue;
         float4 z = make_float4(v[i].x + b.x, v[i].y + b.y, v[i].z + b.z, v[i].w + b.w);
         if (a.activation != APPROXIFER_ACT_NONE)
@@ -258,22 +332,27 @@ struct Maps {
   CUtensorMap rows, cols, row_scales, col_scales;
 };
 
-template <int BN, bool SWAP, typename Out, bool MX>
+template <int BN, bool SWAP, typename Out, Kind KIND>
 cudaError_t launch_one(const TileArgs& t, const Maps& m, int64_t tiles, int split, cudaStream_t stream) {
   const DeviceInfo* dev;
   cudaError_t e = current_device_info(&dev);
   if (e != cudaSuccess) return e;
-  auto kernel = linear_tile_kernel<BN, SWAP, Out, MX>;
+  auto kernel = linear_tile_kernel<BN, SWAP, Out, KIND>;
   struct Tag {};
-  if ((e = ensure_dynamic_smem<Tag>(kernel, dev->ordinal, smem_bytes(BN, MX))) != cudaSuccess) return e;
-  return launch_kernel(kernel, tiles * split, kThreads, smem_bytes(BN, MX), split, stream, m.rows, m.cols, m.row_scales, m.col_scales, t);
+  if ((e = ensure_dynamic_smem<Tag>(kernel, dev->ordinal, smem_bytes(BN, KIND))) != cudaSuccess) return e;
+  // (X in bfloat16: sixteen warps for more than eight rows.  Eight against sixteen, us: 1 x 4,096 x 4,096 6.5 / 7.0, 16 x 16,384 x 4,096
+  // 16.0 / 12.9)
+  const int threads = KIND == kMxRaw && t.M <= 8 ? threads_of(KIND) - 256 : threads_of(KIND);
+  return launch_kernel(kernel, tiles * split, threads, smem_bytes(BN, KIND), split, stream, m.rows, m.cols, m.row_scales, m.col_scales, t);
 }
 
 template <int BN, bool SWAP>
-cudaError_t launch_out(const approxifer_linear_args& a, const TileArgs& t, const Maps& m, bool mx, int64_t tiles, int split, cudaStream_t stream) {
-  if (a.out_type == APPROXIFER_TYPE_F32)
-    return mx ? launch_one<BN, SWAP, float, true>(t, m, tiles, split, stream) : launch_one<BN, SWAP, float, false>(t, m, tiles, split, stream);
-  return mx ? launch_one<BN, SWAP, bf16, true>(t, m, tiles, split, stream) : launch_one<BN, SWAP, bf16, false>(t, m, tiles, split, stream);
+cudaError_t launch_out(const approxifer_linear_args& a, const TileArgs& t, const Maps& m, Kind kind, int64_t tiles, int split, cudaStream_t stream) {
+  const bool f32 = a.out_type == APPROXIFER_TYPE_F32;
+  if constexpr (SWAP && BN <= kMxRawRows)
+    if (kind == kMxRaw) return f32 ? launch_one<BN, SWAP, float, kMxRaw>(t, m, tiles, split, stream) : launch_one<BN, SWAP, bf16, kMxRaw>(t, m, tiles, split, stream);
+  if (kind == kMx) return f32 ? launch_one<BN, SWAP, float, kMx>(t, m, tiles, split, stream) : launch_one<BN, SWAP, bf16, kMx>(t, m, tiles, split, stream);
+  return f32 ? launch_one<BN, SWAP, float, kBf16>(t, m, tiles, split, stream) : launch_one<BN, SWAP, bf16, kBf16>(t, m, tiles, split, stream);
 }
 
 cudaError_t operand_map(CUtensorMap* map, const uint16_t* base, int64_t rows, int64_t cols, int64_t rstride, int box_rows) {
@@ -296,70 +375,98 @@ bool linear_tile_eligible(const approxifer_linear_args& a) {
          a.w_rstride < (1LL << 38);
 }
 
+namespace {
+
+// The operand whose rows are the lanes, the tile's width and rows, the CTAs that share one.
+struct TilePlan {
+  bool swap;
+  int bn, split, per_tile;
+  int64_t lanes, across, tiles, tiles_cols;
+  int steps;
+};
+TilePlan plan_tiles(const approxifer_linear_args& a, bool mx, int sms) {
+  TilePlan p{};
+  // Up to 128 rows of X the product is bound by reading Wt, whose rows then become the 128 lanes, and the tile is only as
+  // wide as X has rows.  Beyond, X's rows are the lanes and the tile as wide as N needs, up to 128.  (From 65 rows on, where
+  // both tiles are 128 wide, the two ways measure the same within 2 %.)
+  p.swap = a.M <= 128;
+  p.across = p.swap ? a.M : a.N;
+  p.bn = p.across <= 16 ? 16 : p.across <= 32 ? 32 : p.across <= 64 ? 64 : 128;
+  p.lanes = p.swap ? a.N : a.M;
+  p.tiles_cols = (p.across + p.bn - 1) / p.bn;
+  p.steps = (int32_t)((a.K + kDepth - 1) / kDepth);
+  // CTAs to a tile (each with four stages of K or more), and rows to a tile: full tiles, or as many fewer as give every SM
+  // one of the same size.  A CTA's time is that of reading its rows over its part of K, plus some eight stages' worth for
+  // its start and its end (with the cluster's meeting, ten); what counts is how many of those follow each other on an SM.
+  p.split = 1, p.per_tile = kLanes;
+  double best = 0;
+  for (int s = 1; s <= 8 && (s == 1 || p.steps >= 4 * s); s *= 2) {
+    // (a cluster sits within one GPC: of its SMs some are left over, more the larger the cluster)
+    const int usable = s == 1 ? sms : s == 2 ? sms - 4 : s == 4 ? sms * 7 / 8 : sms * 3 / 4;
+    const int64_t places = usable / s / p.tiles_cols;  // tiles along the rows that run at once
+    const int64_t even = places > 0 ? ((p.lanes + places - 1) / places + 7) / 8 * 8 : kLanes;
+    for (const int64_t rows : {(int64_t)kLanes, even}) {
+      if (rows > kLanes || rows < (mx ? kLanes : kMinLanes)) continue;  // (blocks of scales have 128 rows)
+      const int64_t n = (p.lanes + rows - 1) / rows * p.tiles_cols, turns = (n * s + usable - 1) / usable;
+      const double time = turns * ((double)rows / kLanes * ((p.steps + s - 1) / s) + (s == 1 ? 8 : 10));
+      if (p.tiles == 0 || time < best) best = time, p.split = s, p.per_tile = (int)rows, p.tiles = n;
+    }
+  }
+  return p;
+}
+
+}  // namespace
+
+// X in bfloat16: its 4-bit form of a CTA's part of K has to fit beside the ring, and as every CTA makes it anew, it has to be little.
+// Measured, in a launch of its own against within the product, us: 1 x 4,096 x 4,096 (4 stages a CTA) 8.6 / 6.5, 32 rows 10.3 / 9.4;
+// 1 x 16,384 x 4,096 (16 stages a CTA) 12.2 / 9.8, 8 rows 12.3 / 11.6, 16 rows 12.4 / 13.0.
+bool linear_tile_takes_raw(const approxifer_linear_args& a, int sms) {
+  if (a.M > kMxRawRows) return false;
+  const TilePlan p = plan_tiles(a, true, sms);
+  const int steps = (p.steps + p.split - 1) / p.split;
+  return steps <= kRawSteps && steps * a.M <= 192;
+}
+
 cudaError_t launch_linear_tile(const approxifer_linear_args& a, const MxScales* mx, cudaStream_t stream) {
   const DeviceInfo* dev;
   cudaError_t e = current_device_info(&dev);
   if (e != cudaSuccess) return e;
-  // Up to 128 rows of X the product is bound by reading Wt, whose rows then become the 128 lanes, and the tile is only as
-  // wide as X has rows.  Beyond, X's rows are the lanes and the tile as wide as N needs, up to 128.  (From 65 rows on, where
-  // both tiles are 128 wide, the two ways measure the same within 2 %.)
-  const bool swap = a.M <= 128;
-  const int64_t across = swap ? a.M : a.N;
-  const int bn = across <= 16 ? 16 : across <= 32 ? 32 : across <= 64 ? 64 : 128;
-  const int64_t lanes = swap ? a.N : a.M;
-  const int64_t tiles_cols = (across + bn - 1) / bn;
+  const TilePlan p = plan_tiles(a, mx != nullptr, dev->sms);
   TileArgs t{};
   t.M = (int32_t)a.M, t.N = (int32_t)a.N, t.K = (int32_t)a.K;
-  t.steps = (int32_t)((a.K + kDepth - 1) / kDepth);
-  t.tiles_cols = (int32_t)tiles_cols;
+  t.steps = p.steps, t.tiles_cols = (int32_t)p.tiles_cols, t.lanes = p.per_tile;
   t.bias = reinterpret_cast<const bf16*>(a.bias), t.R = a.R, t.Y = a.Y, t.r_rstride = a.r_rstride, t.y_rstride = a.y_rstride;
   t.activation = a.activation;
   const int size = a.out_type == APPROXIFER_TYPE_F32 ? 4 : 2, quad = 4 * size;
   auto fits = [](const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) % bytes) == 0; };
   t.vec = fits(a.Y, quad) && a.y_rstride % 4 == 0 && (!a.R || (fits(a.R, quad) && a.r_rstride % 4 == 0));
   t.bias_vec = fits(a.bias, 8);
-  // CTAs to a tile (each with four stages of K or more), and rows to a tile: full tiles, or as many fewer as give every SM
-  // one of the same size.  A CTA's time is that of reading its rows over its part of K, plus some eight stages' worth for
-  // its start and its end (with the cluster's meeting, ten); what counts is how many of those follow each other on an SM.
-  int split = 1, per_tile = kLanes;
-  int64_t tiles = 0;
-  double best = 0;
-  for (int s = 1; s <= 8 && (s == 1 || t.steps >= 4 * s); s *= 2) {
-    // (a cluster sits within one GPC: of its SMs some are left over, more the larger the cluster)
-    const int usable = s == 1 ? dev->sms : s == 2 ? dev->sms - 4 : s == 4 ? dev->sms * 7 / 8 : dev->sms * 3 / 4;
-    const int64_t places = usable / s / tiles_cols;  // tiles along the rows that run at once
-    const int64_t even = places > 0 ? ((lanes + places - 1) / places + 7) / 8 * 8 : kLanes;
-    for (const int64_t rows : {(int64_t)kLanes, even}) {
-      if (rows > kLanes || rows < (mx ? kLanes : kMinLanes)) continue;  // (blocks of scales have 128 rows)
-      const int64_t n = (lanes + rows - 1) / rows * tiles_cols, turns = (n * s + usable - 1) / usable;
-      const double time = turns * ((double)rows / kLanes * ((t.steps + s - 1) / s) + (s == 1 ? 8 : 10));
-      if (tiles == 0 || time < best) best = time, split = s, per_tile = (int)rows, tiles = n;
-    }
-  }
-  t.lanes = per_tile;
-  if (tiles * split > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
+  if (p.tiles * p.split > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
+  const Kind kind = mx == nullptr ? kBf16 : mx->x == nullptr ? kMxRaw : kMx;
   Maps m{};
-  if ((e = operand_map(&m.rows, swap ? a.Wt : a.X, lanes, a.K, swap ? a.w_rstride : a.x_rstride, per_tile)) != cudaSuccess) return e;
-  if ((e = operand_map(&m.cols, swap ? a.X : a.Wt, across, a.K, swap ? a.x_rstride : a.w_rstride, bn)) != cudaSuccess) return e;
+  if ((e = operand_map(&m.rows, p.swap ? a.Wt : a.X, p.lanes, a.K, p.swap ? a.w_rstride : a.x_rstride, p.per_tile)) != cudaSuccess) return e;
+  if (kind != kMxRaw && (e = operand_map(&m.cols, p.swap ? a.X : a.Wt, p.across, a.K, p.swap ? a.x_rstride : a.w_rstride, p.bn)) != cudaSuccess) return e;
   if (mx) {
     t.mx_blocks = (int32_t)((mx->K + kMxCols - 1) / kMxCols);
     auto scales_map = [&](CUtensorMap* map, const uint8_t* base, int64_t n) { return make_scales_map(map, base, (n + kMxRows - 1) / kMxRows, t.mx_blocks, 1); };
-    if ((e = scales_map(&m.row_scales, swap ? mx->w : mx->x, lanes)) != cudaSuccess || (e = scales_map(&m.col_scales, swap ? mx->x : mx->w, across)) != cudaSuccess) return e;
+    if ((e = scales_map(&m.row_scales, p.swap ? mx->w : mx->x, p.lanes)) != cudaSuccess) return e;
+    if (kind == kMx && (e = scales_map(&m.col_scales, p.swap ? mx->x : mx->w, p.across)) != cudaSuccess) return e;
+    t.raw = reinterpret_cast<const bf16*>(a.X), t.raw_rstride = a.x_rstride, t.raw_columns = (int32_t)mx->K;
+    t.raw_whole = aligned16(a.X) && a.x_rstride % 8 == 0;
   }
-  const bool is_mx = mx != nullptr;
-  if (swap) {
-    switch (bn) {
-      case 16: return launch_out<16, true>(a, t, m, is_mx, tiles, split, stream);
-      case 32: return launch_out<32, true>(a, t, m, is_mx, tiles, split, stream);
-      case 64: return launch_out<64, true>(a, t, m, is_mx, tiles, split, stream);
-      default: return launch_out<128, true>(a, t, m, is_mx, tiles, split, stream);
+  if (p.swap) {
+    switch (p.bn) {
+      case 16: return launch_out<16, true>(a, t, m, kind, p.tiles, p.split, stream);
+      case 32: return launch_out<32, true>(a, t, m, kind, p.tiles, p.split, stream);
+      case 64: return launch_out<64, true>(a, t, m, kind, p.tiles, p.split, stream);
+      default: return launch_out<128, true>(a, t, m, kind, p.tiles, p.split, stream);
     }
   }
-  switch (bn) {
-    case 16: return launch_out<16, false>(a, t, m, is_mx, tiles, split, stream);
-    case 32: return launch_out<32, false>(a, t, m, is_mx, tiles, split, stream);
-    case 64: return launch_out<64, false>(a, t, m, is_mx, tiles, split, stream);
-    default: return launch_out<128, false>(a, t, m, is_mx, tiles, split, stream);
+  switch (p.bn) {
+    case 16: return launch_out<16, false>(a, t, m, kind, p.tiles, p.split, stream);
+    case 32: return launch_out<32, false>(a, t, m, kind, p.tiles, p.split, stream);
+    case 64: return launch_out<64, false>(a, t, m, kind, p.tiles, p.split, stream);
+    default: return launch_out<128, false>(a, t, m, kind, p.tiles, p.split, stream);
   }
 }
 

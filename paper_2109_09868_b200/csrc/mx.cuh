@@ -23,6 +23,31 @@ __device__ __forceinline__ float mx_inverse(uint32_t byte) { return __uint_as_fl
 // The value of a scale.
 __device__ __forceinline__ float mx_value(uint32_t byte) { return __uint_as_float(byte == 255 ? 0x7fffffffu : byte == 0 ? 0x00400000u : byte << 23); }
 
+// The activations of the 4-bit products.  Their epilogues have some 3 us a tile before the next one's products are over: where
+// bfloat16 is what is written (it shows 2^-8), the special-function unit's reciprocal (2^-22) takes the place of a division, and
+// of gelu's erf a polynomial times an exponential (Abramowitz and Stegun 7.1.26: within 1.5e-7).  8,192 x 16,384 x 256 with
+// gelu_tanh 253 -> 118 us, with gelu 184 -> 125 us.
+__device__ __forceinline__ float mx_reciprocal(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+template <int ACT, typename Out>
+__device__ __forceinline__ float mx_activate(float x) {
+  if constexpr (sizeof(Out) == 2 && (ACT == APPROXIFER_ACT_SILU || ACT == APPROXIFER_ACT_GELU_TANH)) {
+    // -x log2 e, or -2 sqrt(2/pi) (x + 0.044715 x^3) log2 e
+    const float u = ACT == APPROXIFER_ACT_SILU ? -1.4426950409f * x : x * fmaf(-0.1029432396f, x * x, -2.3022081981f);
+    return x * mx_reciprocal(1.f + pow2(u));
+  }
+  if constexpr (sizeof(Out) == 2 && ACT == APPROXIFER_ACT_GELU) {
+    // half of erfc(|x| / sqrt 2)
+    const float t = mx_reciprocal(fmaf(0.2316418826f, fabsf(x), 1.f));
+    const float h = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 0.5307027145f, -0.7265760135f), 0.7107068705f), -0.142248368f), 0.127414796f) * pow2(-0.7213475204f * x * x);
+    return x >= 0.f ? x - x * h : x * h;
+  }
+  return activate<ACT, Out>(x);
+}
+
 // Eight values (already divided by the scale) as codes, the first in the lowest bits: nearest, ties to even, at most 6.
 __device__ __forceinline__ uint32_t mx_codes(const float (&v)[8]) {
   uint32_t d;
@@ -48,49 +73,59 @@ __device__ __forceinline__ void mx_halves(uint32_t codes, uint32_t (&h)[4]) {
       : "r"(codes));
 }
 
-// Eight neighbours of a row of bfloat16 or fp32: their widened values, and the largest of their magnitudes' bits.
+// Eight neighbours of a row of bfloat16 or fp32 as they are loaded (so that many loads can be in flight), and widened, with the
+// largest of their magnitudes' bits.
 struct MxEight {
   float v[8];
   uint32_t top;
 };
-template <bool VEC>
-__device__ __forceinline__ MxEight mx_load(const bf16* p) {
+template <typename T>
+struct MxRow;
+template <>
+struct MxRow<bf16> {
   uint4 u;
-  if constexpr (VEC) {
-    u = __ldcs(reinterpret_cast<const uint4*>(p));
-  } else {
-    const unsigned short* s = reinterpret_cast<const unsigned short*>(p);
-    u = make_uint4(s[0] | (uint32_t)s[1] << 16, s[2] | (uint32_t)s[3] << 16, s[4] | (uint32_t)s[5] << 16, s[6] | (uint32_t)s[7] << 16);
+  __device__ __forceinline__ void none() { u = make_uint4(0, 0, 0, 0); }
+  template <bool VEC>
+  __device__ __forceinline__ void load(const bf16* p) {
+    if constexpr (VEC) {
+      u = __ldcs(reinterpret_cast<const uint4*>(p));
+    } else {
+      const unsigned short* s = reinterpret_cast<const unsigned short*>(p);
+      u = make_uint4(s[0] | (uint32_t)s[1] << 16, s[2] | (uint32_t)s[3] << 16, s[4] | (uint32_t)s[5] << 16, s[6] | (uint32_t)s[7] << 16);
+    }
   }
-  MxEight x;
-  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-  uint32_t top = 0;
+  __device__ __forceinline__ MxEight widened() const {
+    MxEight x;
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    uint32_t top = 0;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x.v[2 * i] = __uint_as_float(w[i] << 16), x.v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    top = __vmaxu2(top, w[i] & 0x7fff7fffu);
+    for (int i = 0; i < 4; ++i) {
+      x.v[2 * i] = __uint_as_float(w[i] << 16), x.v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+      top = __vmaxu2(top, w[i] & 0x7fff7fffu);
+    }
+    x.top = max(top << 16, top & 0xffff0000u);
+    return x;
   }
-  x.top = max(top << 16, top & 0xffff0000u);
-  return x;
-}
-template <bool VEC>
-__device__ __forceinline__ MxEight mx_load(const float* p) {
-  MxEight x;
-  if constexpr (VEC) {
-    const float4 a = __ldcs(reinterpret_cast<const float4*>(p)), b = __ldcs(reinterpret_cast<const float4*>(p) + 1);
-    x.v[0] = a.x, x.v[1] = a.y, x.v[2] = a.z, x.v[3] = a.w, x.v[4] = b.x, x.v[5] = b.y, x.v[6] = b.z, x.v[7] = b.w;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x.v[i] = p[i];
+};
+template <>
+struct MxRow<float> {
+  float4 lo, hi;
+  __device__ __forceinline__ void none() { lo = hi = make_float4(0.f, 0.f, 0.f, 0.f); }
+  template <bool VEC>
+  __device__ __forceinline__ void load(const float* p) {
+    if constexpr (VEC) lo = __ldcs(reinterpret_cast<const float4*>(p)), hi = __ldcs(reinterpret_cast<const float4*>(p) + 1);
+    else lo = make_float4(p[0], p[1], p[2], p[3]), hi = make_float4(p[4], p[5], p[6], p[7]);
   }
-  x.top = 0;
+  __device__ __forceinline__ MxEight widened() const {
+    MxEight x{{lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w}, 0};
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x.top = max(x.top, __float_as_uint(x.v[i]) & 0x7fffffffu);
-  return x;
-}
+    for (int i = 0; i < 8; ++i) x.top = max(x.top, __float_as_uint(x.v[i]) & 0x7fffffffu);
+    return x;
+  }
+};
 
 // The codes of eight values, four lanes side by side holding a group; the group's scale byte.  Whole warp.
-__device__ __forceinline__ uint32_t mx_quantize8(MxEight& x, uint32_t* byte) {
+__device__ __forceinline__ uint32_t mx_quantize8(MxEight x, uint32_t* byte) {
   uint32_t top = max(x.top, __shfl_xor_sync(0xffffffffu, x.top, 1));
   top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
   *byte = mx_scale(top);

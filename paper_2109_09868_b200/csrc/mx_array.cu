@@ -33,23 +33,20 @@ __global__ void __launch_bounds__(kThreads) mx_quantize_kernel(const __grid_cons
   const uint32_t x0 = blockIdx.x * kPieces + threadIdx.x / 16;
   let_next_start();
   wait_for_inputs();
-  MxEight v[kAhead];
+  MxRow<T> v[kAhead];
 #pragma unroll
   for (int i = 0; i < kAhead; ++i) {
     const uint32_t x = x0 + i * (kThreads / 16);
     const Piece p(g, x, at);
-    v[i].top = 0;
-    if (x < g.pieces && p.row < g.a.M && p.col < g.a.K) v[i] = mx_load<VEC>(static_cast<const T*>(g.a.X) + (int64_t)p.row * g.a.x_rstride + p.col);
-    else
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[i].v[e] = 0.f;
+    v[i].none();
+    if (x < g.pieces && p.row < g.a.M && p.col < g.a.K) v[i].template load<VEC>(static_cast<const T*>(g.a.X) + (int64_t)p.row * g.a.x_rstride + p.col);
   }
 #pragma unroll
   for (int i = 0; i < kAhead; ++i) {
     const uint32_t x = x0 + i * (kThreads / 16);
     const Piece p(g, x, at);
     uint32_t byte;
-    const uint32_t codes = mx_quantize8(v[i], &byte);
+    const uint32_t codes = mx_quantize8(v[i].widened(), &byte);
     // the bytes of the piece's four groups, of which lane 4 k has that of group k
     uint32_t word = byte << (8 * (at / 4));
     word |= __shfl_xor_sync(0xffffffffu, word, 4);

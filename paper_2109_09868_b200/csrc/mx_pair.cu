@@ -8,7 +8,7 @@
 // in its middle: its scales two columns further on.  A stage's scales are copied before the first of its products is issued: between
 // products such a copy waits for those before it (16 K products with copies between every two: 674 us, 1.6 PFLOP/s).
 //
-//   warp 0      one lane: tensor-map copies of this CTA's operands and scales, 256 columns (31 KB) a stage, six in flight
+//   warp 0      one lane: tensor-map copies of this CTA's operands and scales, 256 columns (31 KB) a stage, five in flight
 //   warp 1      of the pair's first CTA: copies of scales and tcgen05.mma for the pair; allocates the tensor memory
 //   warps 2, 3  idle (the accumulator's lanes belong to warps by their index modulo 4)
 //   warps 4-15  epilogue: three warps to each quarter of the lanes, 64 columns each; a thread has one row.  Bias, activation,
@@ -25,14 +25,14 @@ constexpr int kEpilogueWarps = 12;
 constexpr int kThreads = (4 + kEpilogueWarps) * 32;
 constexpr int kTileM = 256, kTileN = 192;
 constexpr int kRowBytes = 128;  // of a stage: 256 columns
-constexpr int kStages = 6, kScaleSlots = 5;
+constexpr int kStages = 5;
 constexpr int kXBytes = 128 * kRowBytes, kWBytes = kTileN / 2 * kRowBytes, kOperandBytes = kXBytes + kWBytes;
 constexpr int kStageBytes = kOperandBytes + 6 * kMxBlock;
 constexpr int kRoomBytes = 32 * 64;  // of an epilogue warp: 32 rows of 64 bytes
 constexpr int kHeader = 1024;
 constexpr int kSmemBytes = kHeader + 1024 + kStages * kStageBytes + kEpilogueWarps * kRoomBytes;
 constexpr int kTmemCols = 512, kScaleCols = 24;
-static_assert(2 * kTileN + kScaleSlots * kScaleCols <= kTmemCols, "the scales exceed the tensor memory");
+static_assert(2 * kTileN + kStages * kScaleCols <= kTmemCols, "the scales exceed the tensor memory");
 static_assert(kStageBytes % 1024 == 0 && kSmemBytes <= 227 * 1024, "shared memory");
 constexpr int kGroupM = 8;  // rows of tiles that are walked together: their X stays in L2 while Wt streams by
 
@@ -91,7 +91,7 @@ __device__ __forceinline__ void finish(const PairArgs& a, const CUtensorMap* y_m
   const int m = m0 + lane, left = a.N - n;
   if (a.bias) add_row<N, bf16>(a.bias + n, a.bias_whole, left, z);
 #pragma unroll
-  for (int i = 0; i < N; ++i) z[i] = activate<ACT, Out>(z[i]);
+  for (int i = 0; i < N; ++i) z[i] = mx_activate<ACT, Out>(z[i]);
   if (a.R && m < a.M) add_row<N, Out>(static_cast<const Out*>(a.R) + (int64_t)m * a.r_rstride + n, a.r_whole, left, z);
   if (a.y_whole) {
     if (lane == 0) stores_have_read();  // the last piece has left
@@ -148,62 +148,69 @@ __global__ void __launch_bounds__(kThreads, 1)
   let_next_start();  // not before: the tensor memory is held
   wait_for_inputs();
 
+  // (The ring's place and phase are counted, not divided out: a stage's products last some 400 cycles, and the warp that issues them
+  // has little time beside.)
   if (warp == 0 && lane == 0) {
-    int it = 0;
+    int s = 0;
+    uint32_t phase = 1;  // of `empty`: the first turn finds every place free
     bool ok = true;
     for (int tile = pair; tile < a.tiles && ok; tile += pairs) {
       int m0, n0;
       place(a, tile, &m0, &n0);
       m0 += rank * 128;
-      for (int k = 0; k < a.steps; ++k, ++it) {
-        const int s = it % kStages, turn = it / kStages;
-        if (turn > 0 && !(ok = bar_wait(empty + 8 * s, (turn - 1) & 1, abort, count))) break;
+      const int w0 = n0 + rank * (kTileN / 2), x_block = m0 / kMxRows, w_block = n0 / kMxRows;
+      for (int k = 0; k < a.steps; ++k) {
+        if (!(ok = bar_wait(empty + 8 * s, phase, abort, count))) break;
         if (rank == 0) bar_expect(full + 8 * s, 2 * kStageBytes);  // both CTAs' copies count on the first one's barrier
         const uint32_t bar = peer_smem(full + 8 * s, 0), dst = stages + s * kStageBytes;
         tma_2d_pair(dst, &x_map, k * 64, m0, bar);
-        tma_2d_pair(dst + kXBytes, &w_map, k * 64, n0 + rank * (kTileN / 2), bar);
-        tma_3d_pair(dst + kOperandBytes, &x_scales, 0, 2 * k, m0 / kMxRows, bar);
-        tma_3d_pair(dst + kOperandBytes + 2 * kMxBlock, &w_scales, 0, 2 * k, n0 / kMxRows, bar);
+        tma_2d_pair(dst + kXBytes, &w_map, k * 64, w0, bar);
+        tma_3d_pair(dst + kOperandBytes, &x_scales, 0, 2 * k, x_block, bar);
+        tma_3d_pair(dst + kOperandBytes + 2 * kMxBlock, &w_scales, 0, 2 * k, w_block, bar);
+        if (++s == kStages) s = 0, phase ^= 1;
       }
     }
   } else if (warp == 1 && rank == 0) {
-    int it = 0, n = 0;
+    int s = 0, n = 0;
+    uint32_t phase = 0;
     bool ok = true;
     for (int tile = pair; tile < a.tiles && ok; tile += pairs, ++n) {
       const int acc = n & 1;
       int m0, n0;
       place(a, tile, &m0, &n0);
-      const uint32_t skip = n0 % kMxRows / 32;
+      const uint32_t skip = n0 % kMxRows / 32, d = tmem + acc * kTileN;
       if (n >= 2 && !(ok = warp_wait(drained + 8 * acc, (n / 2 - 1) & 1, abort, count))) break;
       tmem_fence_after();
-      for (int k = 0; k < a.steps; ++k, ++it) {
-        const int s = it % kStages, turn = it / kStages;
-        // the products that used this slot of scales are over (they are those of the stage five before)
-        if (it >= kScaleSlots && !(ok = warp_wait(empty + 8 * ((it - kScaleSlots) % kStages), ((it - kScaleSlots) / kStages) & 1, abort, count))) break;
-        if (!(ok = warp_wait(full + 8 * s, turn & 1, abort, count))) break;
+      for (int k = 0; k < a.steps; ++k) {
+        if (!(ok = warp_wait(full + 8 * s, phase, abort, count))) break;
         tmem_fence_after();
-        const uint32_t src = stages + s * kStageBytes;
+        const uint32_t src = stages + s * kStageBytes, from = src + kOperandBytes, sx = tmem + 2 * kTileN + s * kScaleCols, sw = sx + 8;
         const uint64_t da = desc_k_major(src), db = desc_k_major(src + kXBytes);
+        const int left = a.products - 4 * k;
         if (elect_one()) {
-          const uint32_t sx = tmem + 2 * kTileN + it % kScaleSlots * kScaleCols, sw = sx + 8, from = src + kOperandBytes;
-          // (what lies beyond K's last 64 columns is not used: it need not be zero, nor its scales there)
-#pragma unroll
-          for (int j = 0; j < 2; ++j)
-            if (2 * k + j < a.blocks) {
-              copy_scales_pair(sx + 4 * j, from + j * kMxBlock);
-              copy_scales_pair(sw + 8 * j, from + (2 + j) * kMxBlock);
-              copy_scales_pair(sw + 8 * j + 4, from + (4 + j) * kMxBlock);
-            }
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (4 * k + j < a.products)
-              mma_mx_pair(tmem + acc * kTileN, da + 2 * j, db + 2 * j, mx_shape(kTileM, kTileN, j % 2), sx + j / 2 * 4, sw + j / 2 * 8 + skip, k > 0 || j > 0);
+          copy_scales_pair(sx, from);
+          copy_scales_pair(sw, from + 2 * kMxBlock);
+          copy_scales_pair(sw + 4, from + 4 * kMxBlock);
+          if (left > 2) {
+            copy_scales_pair(sx + 4, from + kMxBlock);
+            copy_scales_pair(sw + 8, from + 3 * kMxBlock);
+            copy_scales_pair(sw + 12, from + 5 * kMxBlock);
+          }
+          mma_mx_pair(d, da, db, mx_shape(kTileM, kTileN, 0), sx, sw + skip, k > 0);
+          if (left >= 4) {
+            mma_mx_pair(d, da + 2, db + 2, mx_shape(kTileM, kTileN, 1), sx, sw + skip, true);
+            mma_mx_pair(d, da + 4, db + 4, mx_shape(kTileM, kTileN, 0), sx + 4, sw + 8 + skip, true);
+            mma_mx_pair(d, da + 6, db + 6, mx_shape(kTileM, kTileN, 1), sx + 4, sw + 8 + skip, true);
+          } else {  // (what lies beyond K's last 64 columns is not used: it need not be zero, nor its scales there)
+            if (left > 1) mma_mx_pair(d, da + 2, db + 2, mx_shape(kTileM, kTileN, 1), sx, sw + skip, true);
+            if (left > 2) mma_mx_pair(d, da + 4, db + 4, mx_shape(kTileM, kTileN, 0), sx + 4, sw + 8 + skip, true);
+          }
           mma_commit_pair(empty + 8 * s);
+          if (k + 1 == a.steps) mma_commit_pair(ready + 8 * acc);
         }
         __syncwarp();
+        if (++s == kStages) s = 0, phase ^= 1;
       }
-      if (ok && elect_one()) mma_commit_pair(ready + 8 * acc);
-      __syncwarp();
     }
   } else if (warp >= 4) {
     const int q = warp % 4, part = (warp - 4) / 4;
