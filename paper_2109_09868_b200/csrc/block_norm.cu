@@ -79,7 +79,7 @@ __device__ __forceinline__ void store4(T* p, int step, int count, const float (&
 }
 
 __device__ __forceinline__ float gate_of(int act, float x) {
-  if (act == APPROXIFER_GATE_SIGMOID) return 1.f / (1.f + expf(-x));
+  if (act == APPROXIFER_GATE_SIGMOID) return __fdividef(1.f, 1.f + expf(-x));  // (a division of two units' error; 1 / infinity is 0)
   if (act == APPROXIFER_GATE_TANH) return tanhf(x);
   return x;
 }
@@ -106,8 +106,8 @@ __device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_
 enum GateKind { kGateNone, kGateColumns, kGateRows };  // one row for all tokens; a row, or a value, for each
 
 // Q fours of elements a thread.  Elements that are not there are zero and stay out of the sums.
-template <typename S, typename T, int Q, bool VEC, bool RING, GateKind GATE>
-__global__ void __launch_bounds__(kMaxThreads) block_norm_kernel(const __grid_constant__ approxifer_block_norm_args a, int stages) {
+template <typename S, typename T, int Q, bool VEC, bool RING, GateKind GATE, int MOST>
+__global__ void __launch_bounds__(MOST, MOST == kMaxThreads ? 1 : 10) block_norm_kernel(const __grid_constant__ approxifer_block_norm_args a, int stages) {
   extern __shared__ __align__(128) unsigned char smem[];
   constexpr bool kHold = RING;  // weights and gate stay in registers
   const int L = blockDim.x, lane = threadIdx.x;  // threads to a row
@@ -117,8 +117,9 @@ __global__ void __launch_bounds__(kMaxThreads) block_norm_kernel(const __grid_co
   int64_t t = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
   const T* G = static_cast<const T*>(a.gate);
   // this thread's fours: the first element, how many there are
+  const int mine = VEC ? 0 : (a.N - lane + L - 1) / L;
   auto first = [&](int q) { return VEC ? (q * L + lane) * 4 : q * 4 * L + lane; };
-  auto there = [&](int q) { return VEC ? a.N - first(q) : (a.N - first(q) + L - 1) / L; };
+  auto there = [&](int q) { return VEC ? a.N - first(q) : mine - 4 * q; };
   const float inv_n = 1.f / (float)a.N;
   // (ring) a stage: a row of R, of Y, of the gate
   const uint32_t r_bytes = a.N * sizeof(S), y_bytes = a.Y ? a.N * sizeof(T) : 0, g_bytes = GATE == kGateRows && a.g_cstride ? a.N * sizeof(T) : 0;
@@ -157,6 +158,24 @@ __global__ void __launch_bounds__(kMaxThreads) block_norm_kernel(const __grid_co
 #pragma unroll
         for (int i = 0; i < 4; ++i) gate[q][i] = gate_of(a.gate_activation, v.at(i));
       }
+    }
+  }
+  if constexpr (!RING) {
+    // What is needed only after the first sums is asked for now, into the cache: a row's time is that of its loads after each other.
+    auto ask = [&](const void* p, int64_t at) {
+      const T* from = static_cast<const T*>(p) + at;
+#pragma unroll
+      for (int q = 0; q < Q; ++q)
+#pragma unroll
+        for (int i = 0; i < (VEC ? 1 : 4); ++i)
+          if (there(q) > i) asm volatile("prefetch.global.L1 [%0];" ::"l"(from + first(q) + i * L));
+    };
+    if (t < a.T) {
+      if (GATE != kGateNone && a.g_cstride) ask(G, t * a.g_rstride);
+      if (a.after_weight) ask(a.after_weight, 0);
+      if (a.after_bias) ask(a.after_bias, 0);
+      if (a.before_weight) ask(a.before_weight, 0);
+      if (a.before_bias) ask(a.before_bias, 0);
     }
   }
   int turn = 0, s = 0;
@@ -274,7 +293,8 @@ __global__ void __launch_bounds__(kMaxThreads) block_norm_kernel(const __grid_co
   }
 }
 
-template <typename S, typename T, int Q, bool VEC, bool RING>
+// (Narrow rows: registers for ten CTAs of 128 threads on an SM.)
+template <typename S, typename T, int Q, bool VEC, bool RING, int MOST = kMaxThreads>
 cudaError_t launch_kind(const approxifer_block_norm_args& a, const DeviceInfo& dev, int64_t ctas, dim3 block, int smem, int stages, cudaStream_t stream) {
   auto launch = [&](auto kernel, auto tag) {
     const cudaError_t e = ensure_dynamic_smem<decltype(tag)>(kernel, dev.ordinal, smem);
@@ -283,9 +303,9 @@ cudaError_t launch_kind(const approxifer_block_norm_args& a, const DeviceInfo& d
   struct None {};
   struct Columns {};
   struct Rows {};
-  if (a.gate == nullptr) return launch(block_norm_kernel<S, T, Q, VEC, RING, kGateNone>, None{});
-  if (a.g_rstride == 0 && a.g_cstride == 1) return launch(block_norm_kernel<S, T, Q, VEC, RING, kGateColumns>, Columns{});
-  return launch(block_norm_kernel<S, T, Q, VEC, RING, kGateRows>, Rows{});
+  if (a.gate == nullptr) return launch(block_norm_kernel<S, T, Q, VEC, RING, kGateNone, MOST>, None{});
+  if (a.g_rstride == 0 && a.g_cstride == 1) return launch(block_norm_kernel<S, T, Q, VEC, RING, kGateColumns, MOST>, Columns{});
+  return launch(block_norm_kernel<S, T, Q, VEC, RING, kGateRows, MOST>, Rows{});
 }
 
 template <typename S, typename T>
@@ -309,6 +329,8 @@ cudaError_t launch_types(const approxifer_block_norm_args& a, const DeviceInfo& 
   const int rows = threads == 32 ? 4 : 1;
   const dim3 block(threads, rows);
   const int64_t ctas = (a.T + rows - 1) / rows;
+  if (fours == 2 && threads * rows <= 128)
+    return vec ? launch_kind<S, T, 2, true, false, 128>(a, dev, ctas, block, kHeader, 0, stream) : launch_kind<S, T, 2, false, false, 128>(a, dev, ctas, block, kHeader, 0, stream);
   if (fours == 2) return vec ? launch_kind<S, T, 2, true, false>(a, dev, ctas, block, kHeader, 0, stream) : launch_kind<S, T, 2, false, false>(a, dev, ctas, block, kHeader, 0, stream);
   return vec ? launch_kind<S, T, 4, true, false>(a, dev, ctas, block, kHeader, 0, stream) : launch_kind<S, T, 4, false, false>(a, dev, ctas, block, kHeader, 0, stream);
 }
