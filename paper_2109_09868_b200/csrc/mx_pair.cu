@@ -6,13 +6,19 @@
 // scales of five stages: 24 columns each, two blocks (128 x 128 elements) of the CTA's rows of X and two times two of the tile's rows
 // of Wt, of which each CTA needs all.  That is why a tile has 192 columns and not 256.  A tile then starts at a block's first row or
 // in its middle: its scales two columns further on.  A stage's scales are copied before the first of its products is issued: between
-// products such a copy waits for those before it (16 K products with copies between every two: 674 us, 1.6 PFLOP/s).
+// products such a copy waits for those before it (copies between every two: 674 us with gelu_tanh where this order took 450).
 //
 //   warp 0      one lane: tensor-map copies of this CTA's operands and scales, 256 columns (31 KB) a stage, five in flight
 //   warp 1      of the pair's first CTA: copies of scales and tcgen05.mma for the pair; allocates the tensor memory
 //   warps 2, 3  idle (the accumulator's lanes belong to warps by their index modulo 4)
 //   warps 4-15  epilogue: three warps to each quarter of the lanes, 64 columns each; a thread has one row.  Bias, activation,
 //               residual and the one rounding in registers, then through 2 KB of shared memory a warp by tensor-map stores.
+//
+// Bound by the way of the operands into the SM (with one product of a stage's four left out it takes as long; some 54 bytes a cycle
+// arrive, the tensor cores could use 83), and, repeated, by the power limit (1.6 GHz).  Measured: 8,192 x 16,384 x 4,096 236 us, 4.65
+// PFLOP/s, with gelu_tanh 246 us, with K = 256 82 us.  Tried and not faster: tiles of 256 columns whose accumulators share 64 columns
+// of tensor memory, read first by the epilogue (230 us, with gelu_tanh 256 us, with K = 1,024 114 against 99 us: a tile waits for those
+// reads).
 #include "mx.cuh"
 
 namespace approxifer {
