@@ -135,11 +135,14 @@ __device__ __forceinline__ uint32_t pages_of(uint32_t there, int c, int page_shi
 template <int TQ>
 __device__ __forceinline__ bool find_job(const TileArgs& g, int S, int rank, Job<true>* job) {  // over a common prefix
   const approxifer_attention_args& a = g.a;
-  // of every key head and query block so many parts of the prefix, of the last block, if it has one tile only, fewer
-  const int per_head = (g.blocks - 1) * g.prior.parts + g.prior.last_parts;
-  const int x = blockIdx.x / S, in_head = x % per_head, block = min(in_head / g.prior.parts, g.blocks - 1);
-  const int part = in_head - block * g.prior.parts, parts = block == g.blocks - 1 ? g.prior.last_parts : g.prior.parts;
-  job->hk = x / per_head;
+  // query blocks with their parts of the prefix, those of all key heads next to each other; the blocks from `cut` on have other parts
+  const int cut = g.prior.cut, first = cut * g.prior.parts * a.Hkv;
+  int x = blockIdx.x / S;
+  const bool late = x >= first;
+  const int parts = late ? g.prior.last_parts : g.prior.parts;
+  x -= late ? first : 0;
+  job->hk = x / parts % a.Hkv;
+  const int block = (late ? cut : 0) + x / parts / a.Hkv, part = x % parts;
   job->b = 0;
   job->piece = part;
   job->tokens = g.tokens;
@@ -525,7 +528,7 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
         if (FORM == kOverPrefix && mine && half == 0) g.prior.ml[job.piece * g.prior.rows + row_at] = make_float2(m == -CUDART_INF_F ? m : m * scale, l);
         const int64_t to = !mine ? -1 : FORM == kOverPrefix ? (job.piece * g.prior.rows + row_at) * DP
                                                              : (int64_t)(job.token0 + token) * a.o_tstride + (int64_t)(job.hk * g.group + r % g.group) * a.o_hstride;
-        const int parts = FORM == kBehindPrefix ? g.prior.parts : 0;  // (a row of fewer gives the others no weight)
+        const int parts = FORM == kBehindPrefix ? g.prior.most : 0;  // (a row of fewer gives the others no weight)
 #pragma unroll 1
         for (int x = 0; x < 32; x += kTogether * kSide) {
           float4 y[kTogether];
@@ -820,7 +823,7 @@ template <int DP, Form FORM>
 cudaError_t launch_one(const TileArgs& g, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const DeviceInfo& dev, cudaStream_t stream) {
   const approxifer_attention_args& a = g.a;
   if constexpr (FORM == kOverPrefix) {
-    const int64_t ctas = ((int64_t)(g.blocks - 1) * g.prior.parts + g.prior.last_parts) * a.Hkv;
+    const int64_t ctas = ((int64_t)g.prior.cut * g.prior.parts + (int64_t)(g.blocks - g.prior.cut) * g.prior.last_parts) * a.Hkv;
     return g.prior.split > 1 ? launch_split<DP, true, FORM>(g, q, k, v, dev, ctas, g.prior.split, stream) : launch_split<DP, false, FORM>(g, q, k, v, dev, ctas, 1, stream);
   }
   const int64_t ctas = (int64_t)g.blocks * a.batch * a.Hkv;
@@ -890,10 +893,11 @@ cudaError_t launch_attention_tile(const approxifer_attention_args& a, cudaStream
   return e != cudaSuccess ? e : launch_form<kPlain>(tile_args(a), *dev, stream);
 }
 
-// The parts that the prefix is cut into, and how many CTAs (a cluster, which joins their results) share one.  All CTAs of a turn run
-// at once; a CTA's time is that of its steps and some four more for its start and end, a cluster's meeting one more, and every part is
-// written and read once by those who join them.  Of two tiles in turn each hides the other's softmax:
-// a block of one takes nearly as long (1.75 us a step, two 1.98).
+// The parts that the prefix is cut into, and how many CTAs (a cluster, which joins their results) share one.  A CTA's time is that of
+// its steps and some four more for its start and end, a cluster's meeting four more, and every part is written and read once by those
+// who join them.  Of two tiles in turn each hides the other's softmax: a block of one takes nearly as long (1.75 us a step, two 1.98).
+//   Few blocks: all CTAs at once; the last block, if it has one tile only, in fewer parts.
+//   More blocks than places: as many as fill them in whole turns uncut, the rest cut so that their CTAs fill one more.
 PrefixParts prefix_parts(const approxifer_prefix_attention_args& p, const DeviceInfo& dev) {
   const approxifer_attention_args& a = p.own;
   const int dp = padded_head(a), tiles = tiles_of(dp), tokens = kRows / (a.Hq / a.Hkv), per_cta = tiles * tokens, per_sm = 3 - tiles;
@@ -902,21 +906,32 @@ PrefixParts prefix_parts(const approxifer_prefix_attention_args& p, const Device
   const bool half = tiles == 2 && a.T - (blocks - 1) * per_cta <= tokens;  // the last block has one tile
   PrefixParts best{};
   best.rows = a.T * a.Hq;
-  best.last_token = (blocks - 1) * per_cta;
   const double step = dp == 128 ? 2.0e-6 : 1.0e-6;  // s
   const double join = ((double)best.rows * dp * 8 / 5e12 + 0.1e-6) / step;
   double least = 0;
+  auto offer = [&](double time, int64_t cut, int64_t parts, int64_t last, int split) {
+    if (best.parts != 0 && time >= least) return;
+    least = time, best.cut = (int32_t)cut, best.parts = (int32_t)parts, best.last_parts = (int32_t)last, best.split = split;
+  };
   for (int s = 1; s <= kMaxSplit && s <= steps; s *= 2) {
     // (a cluster sits within one GPC: of its SMs some are left over, more the larger the cluster)
     const int64_t places = (int64_t)(s == 1 ? dev.sms : s == 2 ? dev.sms - 4 : s == 4 ? dev.sms * 7 / 8 : dev.sms * 3 / 4) * per_sm / s;
+    const double ends = s > 1 ? 8 : 4;
     for (int64_t n = 1; n * s <= steps && n <= 64; ++n) {
       const int64_t last = half ? (n * 4 + 4) / 5 : n;
       const int64_t turns = (((blocks - 1) * n + last) * a.Hkv + places - 1) / places;
       const double longest = (double)steps / s / (blocks > 1 ? n : last) * (blocks > 1 || !half ? 1.0 : 0.88);
-      const double time = turns * (longest + (s > 1 ? 8 : 4)) + n * join;
-      if (best.parts == 0 || time < least) least = time, best.parts = (int32_t)n, best.last_parts = (int32_t)last, best.split = s;
+      offer(turns * (longest + ends) + n * join, blocks - 1, n, last, s);
     }
   }
+  const int64_t places = (int64_t)dev.sms * per_sm, whole = blocks * a.Hkv / places, cut = whole * places / a.Hkv;  // blocks of whole turns
+  for (int64_t n = 2; whole > 0 && cut < blocks && n <= steps && n <= 64; ++n) {
+    const int64_t turns = ((blocks - cut) * n * a.Hkv + places - 1) / places;
+    const double rest = (double)(blocks - cut) / blocks;
+    offer(whole * (steps + 4.0) + turns * ((double)steps / n + 4) + (1 - rest + rest * n) * join, cut, 1, n, 1);
+  }
+  best.last_token = best.cut * (int64_t)per_cta;
+  best.most = best.cut > 0 && best.parts > best.last_parts ? best.parts : best.last_parts;
   return best;
 }
 

@@ -65,7 +65,7 @@ bool on_tensor_cores(const approxifer_prefix_attention_args& p) {
   a.table_pages = p.prefix_pages;
   return attention_tile_eligible(a);
 }
-int64_t parts_bytes(const PrefixParts& p, const approxifer_attention_args& a) { return p.parts * p.rows * ((a.D <= 64 ? 64 : 128) + 2) * (int64_t)sizeof(float); }
+int64_t parts_bytes(const PrefixParts& p, const approxifer_attention_args& a) { return p.most * p.rows * ((a.D <= 64 ? 64 : 128) + 2) * (int64_t)sizeof(float); }
 bool has_prefix(const approxifer_prefix_attention_args& p) { return p.prefix_len > 0 && p.prefix_pages > 0; }
 }  // namespace
 
@@ -87,7 +87,7 @@ cudaError_t launch_prefix_attention(const approxifer_prefix_attention_args& p, c
     PrefixParts parts = prefix_parts(p, *dev);
     approxifer_attention_args own = p.own;
     parts.o = static_cast<float*>(own.workspace);
-    parts.ml = reinterpret_cast<float2*>(parts.o + parts.parts * parts.rows * (own.D <= 64 ? 64 : 128));
+    parts.ml = reinterpret_cast<float2*>(parts.o + parts.most * parts.rows * (own.D <= 64 ? 64 : 128));
     const int64_t used = (parts_bytes(parts, own) + 15) / 16 * 16;
     own.workspace = static_cast<char*>(own.workspace) + used, own.workspace_bytes -= used;
     if ((e = launch_attention_over_prefix(p, parts, stream)) != cudaSuccess) return e;

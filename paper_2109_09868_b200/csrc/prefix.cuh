@@ -8,11 +8,13 @@ namespace approxifer {
 // The prefix is cut into `parts`; of each, for every row (token, query head), the weighted sum of the values (fp32, the head size
 // rounded up to 64 or 128) and the maximum (of the scores in powers of two) and sum of the weights.
 struct PrefixParts {
-  float* o;    // [parts][rows][64 or 128]
-  float2* ml;  // [parts][rows]
+  float* o;    // [most][rows][64 or 128]
+  float2* ml;  // [most][rows]
   int64_t rows;
-  int64_t last_token;          // from this token on (the last query block of the kernel over the prefix)
+  int64_t last_token;          // from this token on (the query blocks from `cut` on of the kernel over the prefix)
   int32_t parts, last_parts;   // so many parts instead
+  int32_t most;                // the larger of the two
+  int32_t cut;
   int32_t split;               // CTAs that share a part, as a cluster
 };
 
