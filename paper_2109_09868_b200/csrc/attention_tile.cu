@@ -165,6 +165,7 @@ __device__ __forceinline__ bool find_job(const TileArgs& g, int S, int rank, Job
   job->hk = x % a.Hkv;
   x /= a.Hkv;
   job->b = x % a.batch;
+  job->piece = g.prior.most;  // (kOwnPart)
   const int block = g.blocks - 1 - x / a.batch;
   const int start = __ldg(a.q_start + job->b), queries = __ldg(a.q_start + job->b + 1) - start, held = __ldg(a.kv_len + job->b);
   const int skip = block * TQ * g.tokens;
@@ -246,8 +247,10 @@ __device__ __forceinline__ Item item_at(const Job<FLAT>& job, int n) {
 }
 
 // kOverPrefix: all tokens over the common prefix, into partial results; kBehindPrefix: tokens over their sequences' own keys, joined
-// with those.
-enum Form { kPlain, kOverPrefix, kBehindPrefix };
+// with those; kOwnPart: the same, into one partial result more.
+enum Form { kPlain, kOverPrefix, kBehindPrefix, kOwnPart };
+constexpr bool behind(Form f) { return f == kBehindPrefix || f == kOwnPart; }
+constexpr bool into_part(Form f) { return f == kOverPrefix || f == kOwnPart; }
 
 template <int DP, bool CLUSTER, Form FORM>
 __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
@@ -294,11 +297,11 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
   }
   // (Behind a prefix: the kernel before this one lets it start only once it has waited for what came before, so the call's inputs
   // are there; what that kernel leaves is waited for where it is needed, and by each CTA.)
-  if constexpr (FORM != kBehindPrefix) wait_for_inputs();
+  if constexpr (!behind(FORM)) wait_for_inputs();
   Job<FORM == kOverPrefix> job;
   const int S = CLUSTER ? (int)cluster_size() : 1, rank = CLUSTER ? (int)cluster_rank() : 0;
   if (!find_job<TQ>(g, S, rank, &job)) {  // (all CTAs of a cluster or none)
-    if constexpr (FORM == kBehindPrefix) wait_for_inputs();
+    if constexpr (behind(FORM)) wait_for_inputs();
     return;
   }
   // (copies) the page of this lane's rows of a key tile, looked up a tile ahead
@@ -450,12 +453,12 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
     }
     constexpr bool kWide = FORM != kPlain && !CLUSTER;  // rows in fp32 for the partial results, or to be joined with them
     if constexpr (CLUSTER || kWide) softmax_warps_meet<TQ>();  // no product reads shared memory any more, of either tile
-    if constexpr (FORM == kBehindPrefix) wait_for_inputs();
+    if constexpr (behind(FORM)) wait_for_inputs();
     if (ok) {
       // One CTA: O / sum, by way of the tile's queries' place in shared memory (a warp keeps to its own rows and columns) into
       // whole rows; around a prefix in fp32, over queries and ring.  A cluster: O as it is into shared memory, with the row's maximum
       // and sum.
-      float inv = CLUSTER || FORM == kOverPrefix ? 1.f : l == 0.f ? 0.f : 1.f / l;
+      float inv = CLUSTER || into_part(FORM) ? 1.f : l == 0.f ? 0.f : 1.f / l;
       const int64_t row_at = (int64_t)(job.token0 + token) * a.Hq + job.hk * g.group + r % g.group;  // (of the partial results)
       PriorRow prior;
       if constexpr (FORM == kBehindPrefix && !CLUSTER) {
@@ -525,8 +528,8 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
         // Rows of this warp, a lane to four columns: out of shared memory into the partial results, or with those into the output.
         constexpr int kTogether = 8, kSide = 32 / kCols;  // rows at a time, side by side
         const int col = lane % kCols, d = half * kOut + col * 4;
-        if (FORM == kOverPrefix && mine && half == 0) g.prior.ml[job.piece * g.prior.rows + row_at] = make_float2(m == -CUDART_INF_F ? m : m * scale, l);
-        const int64_t to = !mine ? -1 : FORM == kOverPrefix ? (job.piece * g.prior.rows + row_at) * DP
+        if (into_part(FORM) && mine && half == 0) g.prior.ml[job.piece * g.prior.rows + row_at] = make_float2(m == -CUDART_INF_F ? m : m * scale, l);
+        const int64_t to = !mine ? -1 : into_part(FORM) ? (job.piece * g.prior.rows + row_at) * DP
                                                              : (int64_t)(job.token0 + token) * a.o_tstride + (int64_t)(job.hk * g.group + r % g.group) * a.o_hstride;
         const int parts = FORM == kBehindPrefix ? g.prior.most : 0;  // (a row of fewer gives the others no weight)
 #pragma unroll 1
@@ -559,7 +562,7 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
           for (int e = 0; e < kTogether; ++e) {
             const int64_t at = __shfl_sync(0xffffffffu, to, x + e * kSide + lane / kCols);
             if (at < 0) continue;
-            if constexpr (FORM == kOverPrefix) *reinterpret_cast<float4*>(g.prior.o + at + d) = y[e];
+            if constexpr (into_part(FORM)) *reinterpret_cast<float4*>(g.prior.o + at + d) = y[e];
             else if (d < a.D) *reinterpret_cast<uint2*>(reinterpret_cast<bf16*>(a.out) + at + d) = make_uint2(pack_bf16x2(y[e].x, y[e].y), pack_bf16x2(y[e].z, y[e].w));
           }
         }
@@ -775,7 +778,7 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
           const int x = x0 + e * kScoreWarp, t = x / kRows, r = x % kRows, token = t * job.tokens + r / g.group;
           if (x >= end || r / g.group >= job.tokens || token >= job.left) continue;
           const int64_t row_at = (int64_t)(job.token0 + token) * a.Hq + job.hk * g.group + r % g.group;
-          if constexpr (FORM == kOverPrefix) {
+          if constexpr (into_part(FORM)) {
             float* to = g.prior.o + (job.piece * g.prior.rows + row_at) * DP + c;
             if constexpr (DP == 128) *reinterpret_cast<float4*>(to) = make_float4(y[e][0], y[e][1], y[e][2], y[e][3]);
             else *reinterpret_cast<float2*>(to) = make_float2(y[e][0], y[e][1]);
@@ -954,7 +957,7 @@ cudaError_t launch_attention_tile_behind(const approxifer_attention_args& a, con
   if (e != cudaSuccess) return e;
   TileArgs g = tile_args(a);
   g.prior = parts;
-  return launch_form<kBehindPrefix>(g, *dev, stream);
+  return parts.apart ? launch_form<kOwnPart>(g, *dev, stream) : launch_form<kBehindPrefix>(g, *dev, stream);
 }
 
 }  // namespace approxifer

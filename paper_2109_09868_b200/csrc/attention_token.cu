@@ -305,8 +305,9 @@ __device__ __forceinline__ Joined join(const float2 (&ml)[N], const float2 (&v)[
   return j;
 }
 
-// BEHIND (here and below): the row's partial results over a common prefix are joined in.  The kernel before, which makes them, lets
-// this one start only once it has waited for what came before it: the call's inputs are there from the start.
+// BEHIND (here and below): the row's partial results over a common prefix are joined in, or (`apart`) its own becomes one more of
+// them.  The kernel before, which makes them, lets this one start only once it has waited for what came before it: the call's inputs
+// are there from the start.
 template <int DP, bool WHOLE, bool BEHIND>
 __global__ void __launch_bounds__(kThreads, kCtasPerSm) attention_token_cluster_kernel(const __grid_constant__ approxifer_attention_args a, int row_tiles,
                                                                                         int page_shift, const __grid_constant__ PrefixParts prior) {
@@ -394,6 +395,11 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) attention_token_cluster_
       PriorRow before;
       before.parts = 0;
       const int64_t row_at = (int64_t)seen.token * a.Hq + head0 + r;
+      if (prior.apart) {
+        *reinterpret_cast<float2*>(prior.o + (prior.most * prior.rows + row_at) * DP + 2 * d) = j.v;
+        if (d == 0) prior.ml[prior.most * prior.rows + row_at] = make_float2(j.m, j.l);
+        continue;
+      }
       if (seen.placed) {
         before.load(prior, row_at, seen.token);
         const float own = before.weigh(j.m, j.l);
@@ -726,8 +732,10 @@ int64_t attention_token_workspace(const approxifer_attention_args& a) {
   return (int64_t)dev->sms * kCtasPerSm * kWarps * partial_floats(a.D <= 64 ? 64 : 128) * 4;
 }
 
+bool attention_token_balanced(const approxifer_attention_args& a) { return attention_token_workspace(a) > 0 && (int64_t)a.batch * a.Hq < (1LL << 31); }
+
 int64_t attention_token_behind_workspace(const approxifer_attention_args& a) {
-  const int64_t bytes = attention_token_workspace(a);
+  const int64_t bytes = attention_token_balanced(a) ? attention_token_workspace(a) : 0;
   return bytes == 0 ? 0 : bytes + units_of(a) * rows_of_unit(a) * ((a.D <= 64 ? 64 : 128) + 2) * 4;
 }
 

@@ -8,12 +8,13 @@ namespace approxifer {
 // The prefix is cut into `parts`; of each, for every row (token, query head), the weighted sum of the values (fp32, the head size
 // rounded up to 64 or 128) and the maximum (of the scores in powers of two) and sum of the weights.
 struct PrefixParts {
-  float* o;    // [most][rows][64 or 128]
-  float2* ml;  // [most][rows]
+  float* o;    // [most, or one more][rows][64 or 128]
+  float2* ml;  // [most, or one more][rows]
   int64_t rows;
   int64_t last_token;          // from this token on (the query blocks from `cut` on of the kernel over the prefix)
   int32_t parts, last_parts;   // so many parts instead
   int32_t most;                // the larger of the two
+  int32_t apart;               // the own keys' result is a partial result too, the one after `most`: a kernel of its own joins them
   int32_t cut;
   int32_t split;               // CTAs that share a part, as a cluster
 };
@@ -98,6 +99,7 @@ PrefixParts prefix_parts(const approxifer_prefix_attention_args& a, const Device
 cudaError_t launch_attention_over_prefix(const approxifer_prefix_attention_args& a, const PrefixParts& parts, cudaStream_t stream);
 cudaError_t launch_attention_tile_behind(const approxifer_attention_args& a, const PrefixParts& parts, cudaStream_t stream);
 int64_t attention_token_behind_workspace(const approxifer_attention_args& a);
+bool attention_token_balanced(const approxifer_attention_args& a);  // ... joins by a kernel of its own in any case
 cudaError_t launch_attention_token_behind(const approxifer_attention_args& a, const PrefixParts& parts, cudaStream_t stream);
 
 }  // namespace approxifer
