@@ -573,8 +573,8 @@ int approxifer_mx_linear(const approxifer_mx_linear_args* args, void* cuda_strea
 int64_t approxifer_mx_linear_workspace(const approxifer_mx_linear_args* args);
 
 /*
- * Attention of a batch of sequences that begin with the same prefix: its keys and values lie in the caches once and are read once
- * for the batch.  (Where all K queries of a group begin alike, so do the coded queries: the encoder's weights of a coded query sum
+ * Attention of a batch of sequences that begin with the same prefix: its keys and values lie in the caches once and, but in calls so
+ * small that each sequence reads them for itself as fast, are read once for the batch.  (Where all K queries of a group begin alike, so do the coded queries: the encoder's weights of a coded query sum
  * to one.)  `own` is as for approxifer_attention, with kv_len, block_table and the positions counted from the prefix's end, window
  * and sinks 0: for a query at its sequence's own position p >= 0
  *     out = sum_j softmax_j(scale q.k_j) v_j   over all prefix_len positions of the prefix and the own positions j <= p.

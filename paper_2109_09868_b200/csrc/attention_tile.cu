@@ -76,11 +76,14 @@ struct TileArgs {
   int32_t blocks;         // query blocks (a CTA's tiles) per sequence
   int32_t page_shift;
   PrefixParts prior;      // kOverPrefix: to write; kBehindPrefix: to join
-  int32_t prefix_last;    // kOverPrefix: the prefix's last position
+  int32_t prefix_last;    // kOverPrefix, kThroughPrefix: the prefix's last position
+  const int32_t* prefix_table;  // kThroughPrefix
+  int64_t prefix_pages;
 };
 
-// What the CTA works on; all roles derive it alike.  FLAT: all rows stand at the same position.
-template <bool FLAT>
+// What the CTA works on; all roles derive it alike.  FLAT: all rows stand at the same position.  THROUGH: the tiles of a prefix come
+// first, of which every row sees all positions; they and the own tiles are counted apart.
+template <bool FLAT, bool THROUGH = false>
 struct Job {
   int b, hk, token0;   // first token (in the packed array)
   int left;            // tokens of the sequence from there on
@@ -92,8 +95,13 @@ struct Job {
   int skip, steps;       // this CTA's steps of the cluster's: from `skip` on
   int steps0, steps1;  // of the two query tiles
   int piece;           // (over a prefix) which part of it
+  int prefix_tiles, prefix_last;  // (through one)
 
-  __device__ __forceinline__ int tile(int j) const { return j + skip < sink_tiles ? j + skip : first_tile + (j + skip - sink_tiles); }
+  __device__ __forceinline__ bool of_prefix(int j) const { return THROUGH && j + skip < prefix_tiles; }
+  __device__ __forceinline__ int tile(int j) const {
+    if constexpr (THROUGH) return j + skip < prefix_tiles ? j + skip : j + skip - prefix_tiles;  // (no window, no sinks)
+    return j + skip < sink_tiles ? j + skip : first_tile + (j + skip - sink_tiles);
+  }
   __device__ __forceinline__ int pos_of(int token) const { return FLAT ? pos0 : pos0 + token; }
   __device__ __forceinline__ int first_pos(int t) const { return pos_of(t * tokens); }
   __device__ __forceinline__ int last_pos(int t) const { return pos_of(min((t + 1) * tokens, left) - 1); }
@@ -101,13 +109,15 @@ struct Job {
   // may start a tile or two later than tile 0's; there it finds nothing).
   __device__ __forceinline__ int steps_of(int t) const { return t == 0 ? steps0 : steps1; }
   // which of the 32 keys from position k on the row at `pos` sees, a bit per key
-  __device__ __forceinline__ uint32_t sees(int pos, int k) const {
+  __device__ __forceinline__ uint32_t sees(int pos, int k, bool prefix = false) const {
     auto below = [](int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; };  // bits 0 .. n-1
+    if (THROUGH && prefix) return below(prefix_last + 1 - k);
     const uint32_t past = below(pos + 1 - k);
     return window == 0 ? past : past & (~below(pos + 1 - window - k) | below(sinks - k));
   }
   __device__ __forceinline__ bool full(int t, int j) const {
     const int k0 = tile(j) * kKeys, k1 = k0 + kKeys - 1;
+    if (of_prefix(j)) return k1 <= prefix_last;
     return k1 <= first_pos(t) && (window == 0 || k0 > last_pos(t) - window || k1 < sinks);
   }
   // steps from `from` up to `to` are full for query tile t (tiles that hold sinks are left to the masked way)
@@ -115,6 +125,7 @@ struct Job {
     const int past = last_pos(t) - window, k0 = window && past >= 0 ? past / kKeys + 1 : 0, k1 = first_pos(t) < 0 ? 0 : (first_pos(t) + 1) / kKeys;
     *from = sink_tiles + max(0, k0 - first_tile) - skip;
     *to = sink_tiles + k1 - first_tile - skip;
+    if constexpr (THROUGH) *from += prefix_tiles, *to += prefix_tiles;
   }
   __device__ __forceinline__ bool part(int j, int tiles) const {  // some row of a tile that is worked on does not see all of it
     return (j < steps0 && !full(0, j)) || (tiles == 2 && j < steps1 && !full(1, j));
@@ -157,8 +168,8 @@ __device__ __forceinline__ bool find_job(const TileArgs& g, int S, int rank, Job
   return true;
 }
 
-template <int TQ>
-__device__ __forceinline__ bool find_job(const TileArgs& g, int S, int rank, Job<false>* job) {
+template <int TQ, bool THROUGH>
+__device__ __forceinline__ bool find_job(const TileArgs& g, int S, int rank, Job<false, THROUGH>* job) {
   const approxifer_attention_args& a = g.a;
   // blocks of late queries see most: they come first
   int x = blockIdx.x / S;
@@ -187,6 +198,11 @@ __device__ __forceinline__ bool find_job(const TileArgs& g, int S, int rank, Job
   const int last0 = job->last_pos(0);  // (of tile 0's rows)
   job->steps1 = TQ == 2 && job->tokens < job->left ? job->steps : 0;
   job->steps0 = job->steps1 == 0 ? job->steps : last0 < 0 ? 0 : min(job->steps, job->sink_tiles + max(0, last0 / kKeys - job->first_tile + 1));
+  if constexpr (THROUGH) {
+    job->prefix_last = g.prefix_last, job->prefix_tiles = g.prefix_last / kKeys + 1;
+    job->steps += job->prefix_tiles, job->steps0 += job->prefix_tiles;
+    if (TQ == 2 && job->tokens < job->left) job->steps1 = job->steps;
+  }
   // a cluster's CTAs take consecutive parts of the steps; a query tile takes part in a first part of each as it does of all
   job->skip = (int)((int64_t)job->steps * rank / S);
   job->steps = (int)((int64_t)job->steps * (rank + 1) / S) - job->skip;
@@ -238,8 +254,8 @@ struct Item {
   int t, j;
   bool first, last;
 };
-template <int TQ, bool FLAT>
-__device__ __forceinline__ Item item_at(const Job<FLAT>& job, int n) {
+template <int TQ, typename J>
+__device__ __forceinline__ Item item_at(const J& job, int n) {
   if (TQ == 1) return {0, n, true, true};
   const int both = min(job.steps0, job.steps1);
   if (n < 2 * both) return {n & 1, n >> 1, (n & 1) == 0, (n & 1) == 1};
@@ -247,8 +263,9 @@ __device__ __forceinline__ Item item_at(const Job<FLAT>& job, int n) {
 }
 
 // kOverPrefix: all tokens over the common prefix, into partial results; kBehindPrefix: tokens over their sequences' own keys, joined
-// with those; kOwnPart: the same, into one partial result more.
-enum Form { kPlain, kOverPrefix, kBehindPrefix, kOwnPart };
+// with those; kOwnPart: the same, into one partial result more; kThroughPrefix: the prefix and then their own keys, by every block
+// for itself.
+enum Form { kPlain, kOverPrefix, kBehindPrefix, kOwnPart, kThroughPrefix };
 constexpr bool behind(Form f) { return f == kBehindPrefix || f == kOwnPart; }
 constexpr bool into_part(Form f) { return f == kOverPrefix || f == kOwnPart; }
 
@@ -298,7 +315,8 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
   // (Behind a prefix: the kernel before this one lets it start only once it has waited for what came before, so the call's inputs
   // are there; what that kernel leaves is waited for where it is needed, and by each CTA.)
   if constexpr (!behind(FORM)) wait_for_inputs();
-  Job<FORM == kOverPrefix> job;
+  constexpr bool THROUGH = FORM == kThroughPrefix;
+  Job<FORM == kOverPrefix, THROUGH> job;
   const int S = CLUSTER ? (int)cluster_size() : 1, rank = CLUSTER ? (int)cluster_rank() : 0;
   if (!find_job<TQ>(g, S, rank, &job)) {  // (all CTAs of a cluster or none)
     if constexpr (behind(FORM)) wait_for_inputs();
@@ -310,6 +328,7 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
   auto page_of = [&](int j) -> int32_t {
     if (j >= job.steps || lane >= per_tile) return -1;
     const int64_t at = (int64_t)((job.tile(j) * kKeys) >> g.page_shift) + lane;
+    if (job.of_prefix(j)) return at < g.prefix_pages ? __ldg(g.prefix_table + at) : -1;
     return at < a.table_pages ? __ldg(table + at) : -1;
   };
   int32_t page_ahead = warp == kCopyWarp ? page_of(0) : -1;
@@ -353,6 +372,7 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
     int full_from, full_to;  // the steps in which every row of the tile sees every key
     job.full_steps(t, &full_from, &full_to);
     if (flip) full_to = 0;
+    const int whole_prefix = THROUGH && !flip ? (job.prefix_last + 1) / kKeys - job.skip : 0;  // the steps of it before which it is seen whole
     const int steps = job.steps_of(t);
     float m = mine ? -CUDART_INF_F : 0.f, l = 0.f;  // (rows that are not there never ask for another maximum)
     bool ok = true;
@@ -371,7 +391,7 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
         __syncwarp();
         if (lane == 0) bar_arrive(s_free);
       }
-      if (j < full_from || j >= full_to || there != all_pages) {  // what a row does not see becomes minus infinity
+      if ((j >= whole_prefix && (j < full_from || j >= full_to)) || there != all_pages) {  // what a row does not see becomes minus infinity
         if (flip) {
 #pragma unroll
           for (int i = 0; i < kMine; ++i) s[i] = -s[i];
@@ -379,7 +399,7 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
 #pragma unroll
         for (int c = 0; c < kMine; c += 32) {
           const int k = half * kMine + c;
-          const uint32_t sees = job.sees(pos, job.tile(j) * kKeys + k) & pages_of(there, k, g.page_shift);
+          const uint32_t sees = job.sees(pos, job.tile(j) * kKeys + k, job.of_prefix(j)) & pages_of(there, k, g.page_shift);
           if (__any_sync(0xffffffffu, sees != 0xffffffffu)) {
 #pragma unroll
             for (int i = 0; i < 32; ++i) s[c + i] = sees & (1u << i) ? s[c + i] : -CUDART_INF_F;
@@ -454,6 +474,7 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
     constexpr bool kWide = FORM != kPlain && !CLUSTER;  // rows in fp32 for the partial results, or to be joined with them
     if constexpr (CLUSTER || kWide) softmax_warps_meet<TQ>();  // no product reads shared memory any more, of either tile
     if constexpr (behind(FORM)) wait_for_inputs();
+    if (THROUGH && pos < 0) l = 0.f, m = -CUDART_INF_F;  // (before the sequence's own first position: it sees nothing)
     if (ok) {
       // One CTA: O / sum, by way of the tile's queries' place in shared memory (a warp keeps to its own rows and columns) into
       // whole rows; around a prefix in fp32, over queries and ring.  A cluster: O as it is into shared memory, with the row's maximum
@@ -486,17 +507,18 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
 #pragma unroll
           for (int i = 0; i < 16; ++i) y[i] = 0.f;
         }
-        if (mine && add_back) {
+        if (mine && add_back && !(THROUGH && pos < 0)) {
           // infinities and NaN that were taken out of tiles seen in part, for the rows that do see them
           const int d0 = half * kOut + c;
 #pragma unroll 1
           for (int j = 0; j < job.steps; ++j) {
             if (!job.part(j, TQ)) continue;
             const int k0 = job.tile(j) * kKeys;
+            const bool prefix = job.of_prefix(j);
 #pragma unroll 1
-            for (int k = k0; k < k0 + kKeys && k <= min(pos, job.p1); ++k) {
+            for (int k = k0; k < k0 + kKeys && k <= (prefix ? job.prefix_last : min(pos, job.p1)); ++k) {
               if (a.window && k <= pos - a.window && k >= a.sinks) continue;
-              const int32_t page = __ldg(table + (k >> g.page_shift));
+              const int32_t page = __ldg((prefix ? g.prefix_table : table) + (k >> g.page_shift));
               if (page < 0 || page >= a.num_pages) continue;
               const bf16* v = reinterpret_cast<const bf16*>(a.v_cache) + page * a.vc_pstride + job.hk * a.vc_hstride +
                               (k & ((1 << g.page_shift) - 1)) * a.vc_rstride;
@@ -709,7 +731,7 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
               w.x &= ~b0, w.y &= ~b1, w.z &= ~b2, w.w &= ~b3;
               v[x] = w;
               const int at = k0 + (x / 8) % kKeys;
-              if (at <= job.p1 && (at >= job.lo || at < job.sinks)) *poison = 1;  // (a row of this CTA may see it)
+              if (job.of_prefix(j) ? at <= job.prefix_last : at <= job.p1 && (at >= job.lo || at < job.sinks)) *poison = 1;  // (a row of this CTA may see it)
             }
           }
           async_proxy_fence();
@@ -836,6 +858,7 @@ cudaError_t launch_one(const TileArgs& g, const CUtensorMap& q, const CUtensorMa
   // 2,048, 2 heads of 128: 38 / 22; 80 blocks of 64 cut in two for two CTAs on every SM: 31 / 35, hence one CTA to an SM.
   int64_t most = a.table_pages * a.page_size;
   if (a.window && (int64_t)a.window + a.max_q + a.sinks < most) most = (int64_t)a.window + a.max_q + a.sinks;
+  if constexpr (FORM == kThroughPrefix) most += g.prefix_last + 1;
   const int held = dev.sms * 3 / 4;
   int split = 1;
   while (split < kMaxSplit && ctas * split * 2 <= held && most >= (int64_t)split * 2 * 3 * kKeys) split *= 2;
@@ -934,6 +957,7 @@ PrefixParts prefix_parts(const approxifer_prefix_attention_args& p, const Device
     offer(whole * (steps + 4.0) + turns * ((double)steps / n + 4) + (1 - rest + rest * n) * join, cut, 1, n, 1);
   }
   best.last_token = best.cut * (int64_t)per_cta;
+  best.time = least;
   best.most = best.cut > 0 && best.parts > best.last_parts ? best.parts : best.last_parts;
   return best;
 }
@@ -958,6 +982,36 @@ cudaError_t launch_attention_tile_behind(const approxifer_attention_args& a, con
   TileArgs g = tile_args(a);
   g.prior = parts;
   return parts.apart ? launch_form<kOwnPart>(g, *dev, stream) : launch_form<kBehindPrefix>(g, *dev, stream);
+}
+
+// A short prefix, or few query blocks: walked by every block for itself, in one launch.  In steps, as prefix_parts counts them: the
+// blocks' turns over prefix and own keys, shared by clusters where there are few, against those over the prefix, then over the own keys,
+// and a third launch where many parts are joined.  (The lengths are on the device: all sequences count as the longest may be.)
+// Measured, in two or three launches against through, us: 8 sequences of 178 behind 108, 4 key heads of 96, 31 / 17; 2 of 46 behind 154,
+// 4 of 128, 24 / 15; 3 of 72 behind 580, 2 of 128, 21 / 23; 3 of 8 behind 4,096, 4 of 128, 18 / 24 (with clusters).
+bool attention_tile_through_wanted(const approxifer_prefix_attention_args& p, const PrefixParts& parts, int sms) {
+  const approxifer_attention_args& a = p.own;
+  const TileArgs g = tile_args(a);
+  const int per_sm = 3 - tiles_of(padded_head(a));
+  const double own = (double)((a.table_pages * a.page_size < a.max_q ? a.max_q : a.table_pages * a.page_size) + kKeys - 1) / kKeys;
+  const double prefix = (double)((p.prefix_len < p.prefix_pages * a.page_size ? p.prefix_len : p.prefix_pages * a.page_size) + kKeys - 1) / kKeys;
+  const int64_t blocks = (int64_t)g.blocks * a.batch * a.Hkv;
+  int split = 1;
+  while (split < kMaxSplit && blocks * split * 2 <= sms * 3 / 4 && prefix + own >= split * 2 * 3) split *= 2;
+  const int64_t places = (int64_t)sms * per_sm;
+  const double turns = (double)((blocks * split + places - 1) / places);
+  const double through = turns * ((prefix + own) / split + (split > 1 ? 8 : 4));
+  return through < parts.time + turns * (own + 2) + (parts.most > 2 ? 1 : 0);
+}
+
+cudaError_t launch_attention_tile_through(const approxifer_prefix_attention_args& p, cudaStream_t stream) {
+  const DeviceInfo* dev;
+  const cudaError_t e = current_device_info(&dev);
+  if (e != cudaSuccess) return e;
+  TileArgs g = tile_args(p.own);
+  const int64_t room = p.prefix_pages * p.own.page_size;
+  g.prefix_last = (int32_t)((p.prefix_len < room ? p.prefix_len : room) - 1), g.prefix_table = p.prefix_table, g.prefix_pages = p.prefix_pages;
+  return launch_form<kThroughPrefix>(g, *dev, stream);
 }
 
 }  // namespace approxifer

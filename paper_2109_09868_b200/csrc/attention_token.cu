@@ -75,6 +75,7 @@ struct Seen {
   int32_t token;  // its index, or -1 where the sequence has no new token (max_q = 1)
   bool placed;    // (behind a prefix) it has a position of its own
   int32_t sink_chunks, skip, chunks;
+  int32_t prefix_chunks;  // (through a prefix) so many of them come first: those of the prefix, whose positions and table are its own
   __device__ __forceinline__ int32_t position(int c, int keys) const { return (c < sink_chunks ? c : c + skip) * keys; }
   // which of the keys of the chunk at `pos` are seen, a bit per key
   __device__ __forceinline__ uint32_t sees(int32_t pos, int keys) const {
@@ -98,6 +99,7 @@ __device__ __forceinline__ Seen seen_by(const approxifer_attention_args& a, int 
   s.skip = from - s.sink_chunks;
   const int in_window = s.last >= 0 ? s.last / keys - from + 1 : 0;
   s.chunks = s.last >= 0 ? s.sink_chunks + (in_window > 0 ? in_window : 0) : 0;
+  s.prefix_chunks = 0;
   s.table = a.block_table + (int64_t)b * a.table_stride;
   return s;
 }
@@ -148,19 +150,21 @@ struct Warp {
     l[0] = l[1] = 0.f;
   }
 
-  __device__ __forceinline__ Spot look_up(const approxifer_attention_args& a, int page_shift, const Seen& s, int c) const {
+  __device__ __forceinline__ Spot look_up(const approxifer_attention_args& a, int page_shift, const Seen& s, int c, const PrefixParts* through = nullptr) const {
     Spot at = nowhere<WHOLE>();
     if (c >= s.chunks) return at;
-    const int32_t pos = s.position(c, kKeys);
-    at.sees = s.sees(pos, kKeys);
+    const bool of_prefix = through && c < s.prefix_chunks;
+    const int32_t pos = of_prefix ? c * kKeys : s.position(c - s.prefix_chunks, kKeys);
+    at.sees = of_prefix ? bits_below(kKeys) & bits_below(through->last + 1 - pos) : s.sees(pos, kKeys);
+    const int32_t* table = of_prefix ? through->table : s.table;
     if constexpr (WHOLE) {
-      at.page = __ldg(s.table + (pos >> page_shift));
+      at.page = __ldg(table + (pos >> page_shift));
       at.row = pos & ((1 << page_shift) - 1);
       if (at.page < 0 || at.page >= a.num_pages) at.page = 0, at.sees = 0;
     } else {
       const uint32_t j = (uint32_t)pos + lane % kKeys, entry = j / (uint32_t)a.page_size;
       at.row = (int32_t)(j - entry * (uint32_t)a.page_size);
-      if ((at.sees >> (lane % kKeys)) & 1) at.page = __ldg(s.table + entry);
+      if ((at.sees >> (lane % kKeys)) & 1) at.page = __ldg(table + entry);
       if (at.page >= a.num_pages) at.page = -1;
     }
     return at;
@@ -308,10 +312,13 @@ __device__ __forceinline__ Joined join(const float2 (&ml)[N], const float2 (&v)[
 // BEHIND (here and below): the row's partial results over a common prefix are joined in, or (`apart`) its own becomes one more of
 // them.  The kernel before, which makes them, lets this one start only once it has waited for what came before it: the call's inputs
 // are there from the start.
-template <int DP, bool WHOLE, bool BEHIND>
+// THROUGH: a prefix is walked before the sequence's own keys, by every sequence for itself.
+enum Form { kAlone, kBehind, kThrough };
+template <int DP, bool WHOLE, Form FORM>
 __global__ void __launch_bounds__(kThreads, kCtasPerSm) attention_token_cluster_kernel(const __grid_constant__ approxifer_attention_args a, int row_tiles,
                                                                                         int page_shift, const __grid_constant__ PrefixParts prior) {
   extern __shared__ __align__(1024) unsigned char smem[];
+  constexpr bool BEHIND = FORM == kBehind;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const int S = (int)cluster_size(), rank = (int)cluster_rank();
   let_next_start();
@@ -321,7 +328,9 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) attention_token_cluster_
   unit /= row_tiles;
   const int hk = unit % a.Hkv, b = unit / a.Hkv;
   const int group = a.Hq / a.Hkv, head0 = hk * group + rt * kRows, rows = min(kRows, group - rt * kRows);
-  const Seen seen = seen_by(a, b, keys_of(DP));
+  Seen seen = seen_by(a, b, keys_of(DP));
+  if (FORM == kThrough && seen.placed) seen.prefix_chunks = prior.last / keys_of(DP) + 1, seen.chunks += seen.prefix_chunks;
+  const PrefixParts* through = FORM == kThrough ? &prior : nullptr;
   const int stride = S * kWarps, c0 = rank * kWarps + warp;
 
   Warp<DP, WHOLE> w;
@@ -329,17 +338,17 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) attention_token_cluster_
   uint32_t there[kStages];
 #pragma unroll
   for (int s = 0; s < kStages - 1; ++s) {
-    there[s] = w.fetch(a, s, w.look_up(a, page_shift, seen, c0 + s * stride), hk);
+    there[s] = w.fetch(a, s, w.look_up(a, page_shift, seen, c0 + s * stride, through), hk);
     copy_commit();
   }
-  Spot ahead = w.look_up(a, page_shift, seen, c0 + (kStages - 1) * stride);
+  Spot ahead = w.look_up(a, page_shift, seen, c0 + (kStages - 1) * stride, through);
   w.start(a, seen.token, head0, rows);
   const float scale = a.scale * 1.4426950408889634f;
   int slot = 0;
   for (int c = c0; c < seen.chunks; c += stride) {
     there[kStages - 1] = w.fetch(a, (slot + kStages - 1) % kStages, ahead, hk);
     copy_commit();
-    ahead = w.look_up(a, page_shift, seen, c + kStages * stride);
+    ahead = w.look_up(a, page_shift, seen, c + kStages * stride, through);
     copy_wait<kStages - 1>();
     __syncwarp();
     w.reduce(slot, there[0], scale);
@@ -688,10 +697,10 @@ int64_t most_seen(const approxifer_attention_args& a) {
   return a.window && (int64_t)a.window + a.sinks < held ? (int64_t)a.window + a.sinks : held;
 }
 int64_t units_of(const approxifer_attention_args& a) { return (int64_t)a.batch * a.Hkv * ((a.Hq / a.Hkv + kRows - 1) / kRows); }
-template <int DP, bool WHOLE, bool BEHIND>
+template <int DP, bool WHOLE, Form FORM>
 cudaError_t launch_cluster(const approxifer_attention_args& a, const PrefixParts& prior, const DeviceInfo& dev, int row_tiles, int page_shift, int64_t units, int split,
                            cudaStream_t stream) {
-  auto kernel = attention_token_cluster_kernel<DP, WHOLE, BEHIND>;
+  auto kernel = attention_token_cluster_kernel<DP, WHOLE, FORM>;
   struct Tag {};
   cudaError_t e = ensure_dynamic_smem<Tag>(kernel, dev.ordinal, smem_bytes(DP));
   if (e != cudaSuccess) return e;
@@ -740,7 +749,7 @@ int64_t attention_token_behind_workspace(const approxifer_attention_args& a) {
 }
 
 namespace {
-template <bool BEHIND>
+template <Form FORM>
 cudaError_t launch_form(const approxifer_attention_args& a, const PrefixParts& prior, cudaStream_t stream) {
   const DeviceInfo* dev;
   const cudaError_t e = current_device_info(&dev);
@@ -749,23 +758,34 @@ cudaError_t launch_form(const approxifer_attention_args& a, const PrefixParts& p
   const int dp = a.D <= 64 ? 64 : 128, keys = keys_of(dp);
   const int page_shift = exact_log2(a.page_size);  // pages of whole chunks and a power of two: one look-up a chunk
   const bool is_whole = page_shift >= 0 && a.page_size >= keys;
+  constexpr bool BEHIND = FORM == kBehind;
   const int64_t need = BEHIND ? attention_token_behind_workspace(a) : attention_token_workspace(a);
-  if (need > 0 && a.workspace_bytes >= need && (int64_t)a.batch * a.Hq < (1LL << 31)) {
+  if (FORM != kThrough && need > 0 && a.workspace_bytes >= need && (int64_t)a.batch * a.Hq < (1LL << 31)) {
     auto launch = is_whole ? (dp == 64 ? launch_balanced<64, true, BEHIND> : launch_balanced<128, true, BEHIND>)
                            : dp == 64 ? launch_balanced<64, false, BEHIND> : launch_balanced<128, false, BEHIND>;
     return launch(a, prior, *dev, row_tiles, page_shift, stream);
   }
   // Until there are about four CTAs for every place on the GPU, none with less than two chunks for each warp.
-  const int64_t units = units_of(a), most = most_seen(a);
+  const int64_t units = units_of(a), most = most_seen(a) + (FORM == kThrough ? prior.last + 1 : 0);
   int split = 1;
   while (split < kMaxSplit && units * split < 4LL * kCtasPerSm * dev->sms && most >= (int64_t)split * 2 * kWarps * keys * 2) split *= 2;
-  auto launch = is_whole ? (dp == 64 ? launch_cluster<64, true, BEHIND> : launch_cluster<128, true, BEHIND>)
-                         : dp == 64 ? launch_cluster<64, false, BEHIND> : launch_cluster<128, false, BEHIND>;
+  auto launch = is_whole ? (dp == 64 ? launch_cluster<64, true, FORM> : launch_cluster<128, true, FORM>)
+                         : dp == 64 ? launch_cluster<64, false, FORM> : launch_cluster<128, false, FORM>;
   return launch(a, prior, *dev, row_tiles, page_shift, units, split, stream);
 }
 }  // namespace
 
-cudaError_t launch_attention_token(const approxifer_attention_args& a, cudaStream_t stream) { return launch_form<false>(a, PrefixParts{}, stream); }
-cudaError_t launch_attention_token_behind(const approxifer_attention_args& a, const PrefixParts& prior, cudaStream_t stream) { return launch_form<true>(a, prior, stream); }
+cudaError_t launch_attention_token(const approxifer_attention_args& a, cudaStream_t stream) { return launch_form<kAlone>(a, PrefixParts{}, stream); }
+cudaError_t launch_attention_token_behind(const approxifer_attention_args& a, const PrefixParts& prior, cudaStream_t stream) { return launch_form<kBehind>(a, prior, stream); }
+
+// A short prefix, or few sequences: read by every sequence for itself, in one launch.  As far as the cluster form is the one for the
+// whole (see wants_balance).  Measured, in two steps against through, us: 5 sequences behind 1,003, 2 key heads of 64, 9.1 / 7.1; 19 behind
+// 450, 1 of 80, 12.2 / 7.7; 66 behind 479, 2 of 96, 14.0 / 11.0; 3 behind 510 with 1,239 of their own, 8 of 96, 13.1 / 11.1.
+bool attention_token_through_wanted(const approxifer_attention_args& a, int64_t prefix_len) { return units_of(a) * (most_seen(a) + prefix_len) < 64 * 1024; }
+cudaError_t launch_attention_token_through(const approxifer_attention_args& a, const int32_t* prefix_table, int32_t last, cudaStream_t stream) {
+  PrefixParts p{};
+  p.table = prefix_table, p.last = last;
+  return launch_form<kThrough>(a, p, stream);
+}
 
 }  // namespace approxifer

@@ -216,7 +216,8 @@ __global__ void __launch_bounds__(threads_of(KIND), 1) linear_tile_kernel(const 
       if (elect_one()) {
         if constexpr (KIND != kBf16) {
           // (what a block of scales holds beyond K's last 64 columns is not used: it need not be there)
-          const uint32_t sa = tmem + acc_cols(BN) + s * 16, sb = sa + 8;
+          const uint32_t sa = tmem + acc_cols(BN) + s * 16, sb = sa + 8, first = sb + col0 % kMxRows / 32;
+          // (a tile that starts within a block of scales starts in its middle, two columns on: an odd column is a misaligned address)
 #pragma unroll
           for (int k = 0; k < 2; ++k)
             if (2 * i + k < a.mx_blocks) {
@@ -225,7 +226,7 @@ __global__ void __launch_bounds__(threads_of(KIND), 1) linear_tile_kernel(const 
             }
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            if (i * 4 + k < (a.K + 15) / 16) mma_mx(tmem, da + 2 * k, db + 2 * k, mx_shape(kLanes, BN, k % 2), sa + k / 2 * 4, sb + k / 2 * 4, i > step0 || k > 0);
+            if (i * 4 + k < (a.K + 15) / 16) mma_mx(tmem, da + 2 * k, db + 2 * k, mx_shape(kLanes, BN, k % 2), sa + k / 2 * 4, first + k / 2 * 4, i > step0 || k > 0);
           }
         } else {
 #pragma unroll
@@ -384,6 +385,25 @@ struct TilePlan {
   int64_t lanes, across, tiles, tiles_cols;
   int steps;
 };
+// Of 4-bit operands (full tiles only: blocks of scales have 128 rows): also how wide a tile is, since a stage is soon through and a
+// tile's end, its columns joined, activated and stored, is what small products consist of.  A CTA's time, in stages of narrow tiles
+// (0.2 us): its stages, longer with the tile's width; some eight for its start (ten with a cluster's meeting); sixteen for the end of 128
+// columns, shared by the cluster; clusters that follow each other find their places late.
+TilePlan plan_mx_tiles(TilePlan p, int sms) {
+  double best = 0;
+  TilePlan chosen = p;
+  for (int bn = p.bn; bn == p.bn || bn >= 64; bn /= 2) {  // (tiles side by side start at a block's first row or in its middle: see the kernel)
+    const int64_t tiles_cols = (p.across + bn - 1) / bn, tiles = (p.lanes + kLanes - 1) / kLanes * tiles_cols;
+    for (int s = 1; s <= 8 && (s == 1 || p.steps >= 4 * s); s *= 2) {
+      const int usable = s == 1 ? sms : s == 2 ? sms - 4 : s == 4 ? sms * 7 / 8 : sms * 3 / 4;
+      const int64_t turns = (tiles * s + usable - 1) / usable;
+      const double time = turns * ((p.steps + s - 1) / s * (1 + bn / 160.0) + (s == 1 ? 8 : 10) + 16.0 * bn / 128 / s) + (s > 1 ? 6 * (turns - 1) : 0);
+      if (best == 0 || time < best) best = time, chosen.bn = bn, chosen.split = s, chosen.per_tile = kLanes, chosen.tiles = tiles, chosen.tiles_cols = tiles_cols;
+    }
+  }
+  return chosen;
+}
+
 TilePlan plan_tiles(const approxifer_linear_args& a, bool mx, int sms) {
   TilePlan p{};
   // Up to 128 rows of X the product is bound by reading Wt, whose rows then become the 128 lanes, and the tile is only as
@@ -395,6 +415,7 @@ TilePlan plan_tiles(const approxifer_linear_args& a, bool mx, int sms) {
   p.lanes = p.swap ? a.N : a.M;
   p.tiles_cols = (p.across + p.bn - 1) / p.bn;
   p.steps = (int32_t)((a.K + kDepth - 1) / kDepth);
+  if (mx) return plan_mx_tiles(p, sms);
   // CTAs to a tile (each with four stages of K or more), and rows to a tile: full tiles, or as many fewer as give every SM
   // one of the same size.  A CTA's time is that of reading its rows over its part of K, plus some eight stages' worth for
   // its start and its end (with the cluster's meeting, ten); what counts is how many of those follow each other on an SM.
@@ -406,7 +427,7 @@ TilePlan plan_tiles(const approxifer_linear_args& a, bool mx, int sms) {
     const int64_t places = usable / s / p.tiles_cols;  // tiles along the rows that run at once
     const int64_t even = places > 0 ? ((p.lanes + places - 1) / places + 7) / 8 * 8 : kLanes;
     for (const int64_t rows : {(int64_t)kLanes, even}) {
-      if (rows > kLanes || rows < (mx ? kLanes : kMinLanes)) continue;  // (blocks of scales have 128 rows)
+      if (rows > kLanes || rows < kMinLanes) continue;
       const int64_t n = (p.lanes + rows - 1) / rows * p.tiles_cols, turns = (n * s + usable - 1) / usable;
       const double time = turns * ((double)rows / kLanes * ((p.steps + s - 1) / s) + (s == 1 ? 8 : 10));
       if (p.tiles == 0 || time < best) best = time, p.split = s, p.per_tile = (int)rows, p.tiles = n;

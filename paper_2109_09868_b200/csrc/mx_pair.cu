@@ -50,7 +50,7 @@ struct PairArgs {
   const void* R;
   void* Y;
   int64_t r_rstride, y_rstride;
-  int32_t bias_whole, r_whole, y_whole;  // 16 bytes at a time; y: tensor-map stores
+  int32_t bias_whole, whole;      // the bias; Y and R: 16 bytes at a time, Y by tensor-map stores
 };
 
 // Tiles in bands of kGroupM rows of tiles, down a band's columns of tiles.
@@ -90,7 +90,7 @@ __device__ __forceinline__ void add_row(const T* p, bool whole, int count, float
   }
 }
 
-// 64 bytes of the thread's row m, from column n on: z is what the accumulator holds.
+// 64 bytes of the thread's row m0 + lane, from column n on: z is what the accumulator holds.
 template <typename Out, int ACT, int N>
 __device__ __forceinline__ void finish(const PairArgs& a, const CUtensorMap* y_map, int m0, int n, float (&z)[N], unsigned char* room, int lane) {
   static_assert(N * sizeof(Out) == 64, "64 bytes of a row");
@@ -98,8 +98,9 @@ __device__ __forceinline__ void finish(const PairArgs& a, const CUtensorMap* y_m
   if (a.bias) add_row<N, bf16>(a.bias + n, a.bias_whole, left, z);
 #pragma unroll
   for (int i = 0; i < N; ++i) z[i] = mx_activate<ACT, Out>(z[i]);
-  if (a.R && m < a.M) add_row<N, Out>(static_cast<const Out*>(a.R) + (int64_t)m * a.r_rstride + n, a.r_whole, left, z);
-  if (a.y_whole) {
+  auto place16 = [&](int row, int i) { return room + row * 64 + ((i ^ ((row >> 1) & 3)) << 4); };  // the i-th 16 bytes of a row (the 64-byte swizzle)
+  if (a.whole) {
+    if (a.R && m < a.M) add_row<N, Out>(static_cast<const Out*>(a.R) + (int64_t)m * a.r_rstride + n, true, left, z);
     if (lane == 0) stores_have_read();  // the last piece has left
     __syncwarp();
 #pragma unroll
@@ -109,16 +110,35 @@ __device__ __forceinline__ void finish(const PairArgs& a, const CUtensorMap* y_m
         u = make_uint4(pack_bf16x2(z[8 * i], z[8 * i + 1]), pack_bf16x2(z[8 * i + 2], z[8 * i + 3]), pack_bf16x2(z[8 * i + 4], z[8 * i + 5]), pack_bf16x2(z[8 * i + 6], z[8 * i + 7]));
       else
         u = make_uint4(__float_as_uint(z[4 * i]), __float_as_uint(z[4 * i + 1]), __float_as_uint(z[4 * i + 2]), __float_as_uint(z[4 * i + 3]));
-      *reinterpret_cast<uint4*>(room + lane * 64 + ((i ^ ((lane >> 1) & 3)) << 4)) = u;  // (the 64-byte swizzle)
+      *reinterpret_cast<uint4*>(place16(lane, i)) = u;
     }
     async_proxy_fence();
     __syncwarp();
     if (lane == 0 && m0 < a.M && left > 0) store_tile(y_map, smem_addr(room), n, m0);
-  } else if (m < a.M) {
-    Out* y = static_cast<Out*>(a.Y) + (int64_t)m * a.y_rstride + n;
+    return;
+  }
+  // Rows that are not whole 16 bytes: sixteen columns at a time through shared memory in fp32, so that neighbouring lanes write, and
+  // read of the residual, neighbours of a row.
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (i < left) y[i] = narrow<Out>(z[i]);
+  for (int c = 0; c < N; c += 16) {
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<float4*>(place16(lane, i)) = make_float4(z[c + 4 * i], z[c + 4 * i + 1], z[c + 4 * i + 2], z[c + 4 * i + 3]);
+    __syncwarp();
+    const int col = n + c + lane % 16, rows = col < a.N ? a.M - m0 - lane / 16 : 0;  // (of every second row from this lane's first on)
+    float r[16];
+    if (a.R) {
+      const Out* from = static_cast<const Out*>(a.R) + (int64_t)(m0 + lane / 16) * a.r_rstride + col;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) r[i] = 2 * i < rows ? widen(from[2 * i * a.r_rstride]) : 0.f;
+    }
+    Out* to = static_cast<Out*>(a.Y) + (int64_t)(m0 + lane / 16) * a.y_rstride + col;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      float y = reinterpret_cast<const float*>(place16(2 * i + lane / 16, lane % 16 / 4))[lane % 4];
+      if (a.R) y += r[i];
+      if (2 * i < rows) to[2 * i * a.y_rstride] = narrow<Out>(y);
+    }
   }
 }
 
@@ -143,7 +163,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int s = 0; s < 2; ++s) bar_init(ready + 8 * s, 1), bar_init(drained + 8 * s, 2 * kEpilogueWarps);
     *abort = 0;
     bar_init_done();
-    prefetch_map(&x_map), prefetch_map(&w_map), prefetch_map(&x_scales), prefetch_map(&w_scales), prefetch_map(&y_map);
+    prefetch_map(&x_map), prefetch_map(&w_map), prefetch_map(&x_scales), prefetch_map(&w_scales);
+    if (a.whole) prefetch_map(&y_map);
   }
   if (warp == 1) tmem_alloc_pair(smem_addr(tmem_slot), kTmemCols);
   tmem_fence_before();
@@ -302,8 +323,8 @@ cudaError_t launch_mx_pair(const approxifer_mx_linear_args& a, cudaStream_t stre
   if (tm * tn > 0x3fffffffLL || tn > (1 << 27)) return cudaErrorInvalidConfiguration;
   t.tiles_m = (int32_t)tm, t.tiles_n = (int32_t)tn, t.tiles = (int32_t)(tm * tn);
   t.bias = reinterpret_cast<const bf16*>(a.bias), t.R = a.R, t.Y = a.Y, t.r_rstride = a.r_rstride, t.y_rstride = a.y_rstride;
-  t.bias_whole = aligned16(a.bias), t.r_whole = aligned16(a.R) && a.r_rstride * size % 16 == 0;
-  t.y_whole = aligned16(a.Y) && a.y_rstride * size % 16 == 0 && a.y_rstride < (1LL << 37);
+  t.bias_whole = aligned16(a.bias);
+  t.whole = aligned16(a.Y) && a.y_rstride * size % 16 == 0 && a.y_rstride < (1LL << 37) && (!a.R || (aligned16(a.R) && a.r_rstride * size % 16 == 0));
   Maps m{};
   const uint64_t xe[2] = {(uint64_t)a.K / 4, (uint64_t)a.M}, xs[2] = {1, (uint64_t)a.x_rstride / 2}, we[2] = {(uint64_t)a.K / 4, (uint64_t)a.N}, ws[2] = {1, (uint64_t)a.w_rstride / 2};
   const uint32_t x_box[2] = {64, 128}, w_box[2] = {64, kTileN / 2};
@@ -311,7 +332,7 @@ cudaError_t launch_mx_pair(const approxifer_mx_linear_args& a, cudaStream_t stre
       (e = make_scales_map(&m.x_scales, a.x_scales, (a.M + kMxRows - 1) / kMxRows, t.blocks, 1)) != cudaSuccess ||
       (e = make_scales_map(&m.w_scales, a.w_scales, (a.N + kMxRows - 1) / kMxRows, t.blocks, 2)) != cudaSuccess)
     return e;
-  if (t.y_whole && (e = make_store_map(&m.y, a.Y, f32, a.M, a.N, a.y_rstride)) != cudaSuccess) return e;
+  if (t.whole && (e = make_store_map(&m.y, a.Y, f32, a.M, a.N, a.y_rstride)) != cudaSuccess) return e;
   return f32 ? launch_out<float>(a.activation, t, m, *dev, stream) : launch_out<bf16>(a.activation, t, m, *dev, stream);
 }
 

@@ -130,7 +130,14 @@ bool on_tensor_cores(const approxifer_prefix_attention_args& p) {
   a.table_pages = p.prefix_pages;
   return attention_tile_eligible(a);
 }
-bool has_prefix(const approxifer_prefix_attention_args& p) { return p.prefix_len > 0 && p.prefix_pages > 0; }
+// Positions of the prefix that its table has pages for.
+int64_t positions_of(const approxifer_prefix_attention_args& p) { return p.prefix_len < p.prefix_pages * p.own.page_size ? p.prefix_len : p.prefix_pages * p.own.page_size; }
+bool has_prefix(const approxifer_prefix_attention_args& p) { return positions_of(p) > 0; }
+// Whether the sequences, or their query blocks, walk the prefix each for itself.
+bool through(const approxifer_prefix_attention_args& p, const DeviceInfo& dev) {
+  if (attention_token_eligible(p.own)) return attention_token_through_wanted(p.own, positions_of(p));
+  return positions_of(p) + p.own.table_pages * p.own.page_size < (1LL << 30) && attention_tile_through_wanted(p, prefix_parts(p, dev), dev.sms);
+}
 
 // The parts of the prefix and the bytes that they, with one more for the own keys where that is kept apart, take.  Few partial results
 // are joined on the way by the kernels over the own keys; of many each row's would be read one batch after another by the few CTAs
@@ -152,6 +159,7 @@ int64_t prefix_attention_workspace(const approxifer_prefix_attention_args& p) {
   if (!on_tensor_cores(p) || current_device_info(&dev) != cudaSuccess) return 0;
   const bool token = attention_token_eligible(p.own);
   if (!has_prefix(p)) return token ? attention_token_workspace(p.own) : 0;
+  if (through(p, *dev)) return 0;
   int64_t bytes;
   parts_of(p, *dev, &bytes);
   return bytes + (token ? attention_token_behind_workspace(p.own) : 0);
@@ -163,6 +171,9 @@ cudaError_t launch_prefix_attention(const approxifer_prefix_attention_args& p, c
     const DeviceInfo* dev;
     cudaError_t e = current_device_info(&dev);
     if (e != cudaSuccess) return e;
+    if (through(p, *dev))
+      return attention_token_eligible(p.own) ? launch_attention_token_through(p.own, p.prefix_table, (int32_t)(positions_of(p) - 1), stream)
+                                             : launch_attention_tile_through(p, stream);
     int64_t used;
     PrefixParts parts = parts_of(p, *dev, &used);
     approxifer_attention_args own = p.own;

@@ -17,6 +17,10 @@ struct PrefixParts {
   int32_t apart;               // the own keys' result is a partial result too, the one after `most`: a kernel of its own joins them
   int32_t cut;
   int32_t split;               // CTAs that share a part, as a cluster
+  double time;                 // what the kernel over the prefix is thought to take, in steps
+  // (single tokens that walk the prefix themselves) its table, its last position
+  const int32_t* table;
+  int32_t last;
 };
 
 #ifdef __CUDACC__
@@ -97,9 +101,13 @@ struct PriorRow {
 
 PrefixParts prefix_parts(const approxifer_prefix_attention_args& a, const DeviceInfo& dev);  // (pointers left out); see attention_tile.cu
 cudaError_t launch_attention_over_prefix(const approxifer_prefix_attention_args& a, const PrefixParts& parts, cudaStream_t stream);
+bool attention_tile_through_wanted(const approxifer_prefix_attention_args& a, const PrefixParts& parts, int sms);
+cudaError_t launch_attention_tile_through(const approxifer_prefix_attention_args& a, cudaStream_t stream);
 cudaError_t launch_attention_tile_behind(const approxifer_attention_args& a, const PrefixParts& parts, cudaStream_t stream);
 int64_t attention_token_behind_workspace(const approxifer_attention_args& a);
 bool attention_token_balanced(const approxifer_attention_args& a);  // ... joins by a kernel of its own in any case
+bool attention_token_through_wanted(const approxifer_attention_args& a, int64_t prefix_len);
+cudaError_t launch_attention_token_through(const approxifer_attention_args& a, const int32_t* prefix_table, int32_t last, cudaStream_t stream);
 cudaError_t launch_attention_token_behind(const approxifer_attention_args& a, const PrefixParts& parts, cudaStream_t stream);
 
 }  // namespace approxifer
