@@ -754,9 +754,17 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
     if (warp < kScoreWarp) {
       const float scale = fmaxf(fabsf(a.scale) * 1.4426950408889634f, 1e-37f);
       const uint32_t parts = smem_addr(part_rows), sums = smem_addr(row_sums);
-      constexpr int kAt = 2;  // rows whose loads are in flight together
+      constexpr int kAt = FORM == kPlain ? 1 : 2;  // rows whose loads are in flight together (partial results: all rows are, else often few)
       const int end = TQ * kRows * (rank + 1) / S, c = lane * (DP / 32);  // this lane's columns
       for (int x0 = TQ * kRows * rank / S + warp; x0 < end; x0 += kScoreWarp * kAt) {
+        auto live = [&](int x) {
+          const int in_tile = x % kRows / g.group;
+          return x < end && in_tile < job.tokens && x / kRows * job.tokens + in_tile < job.left;
+        };
+        bool any = false;
+#pragma unroll
+        for (int e = 0; e < kAt; ++e) any |= live(x0 + e * kScoreWarp);
+        if (!any) continue;
         float2 ml[kAt][kMaxSplit];
         float best[kAt], total[kAt], y[kAt][4];
 #pragma unroll
@@ -798,7 +806,7 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
 #pragma unroll
         for (int e = 0; e < kAt; ++e) {
           const int x = x0 + e * kScoreWarp, t = x / kRows, r = x % kRows, token = t * job.tokens + r / g.group;
-          if (x >= end || r / g.group >= job.tokens || token >= job.left) continue;
+          if (!live(x)) continue;
           const int64_t row_at = (int64_t)(job.token0 + token) * a.Hq + job.hk * g.group + r % g.group;
           if constexpr (into_part(FORM)) {
             float* to = g.prior.o + (job.piece * g.prior.rows + row_at) * DP + c;
@@ -844,6 +852,16 @@ cudaError_t launch_split(const TileArgs& g, const CUtensorMap& q, const CUtensor
   return launch_kernel(kernel, ctas * split, threads_of(DP), smem_bytes(DP), split, stream, q, k, v, g);
 }
 
+// Few query blocks: as many CTAs to each, along the keys, as the GPU holds, each with three tiles of keys or more.  (The
+// lengths are on the device: what a block can see at most says how far it is worth cutting.)  Measured, one CTA a block
+// against the cluster, us: 2 queries at 4,000 keys, 1 key head of 128: 62 / 16; 10 at 4,000, 8 heads of 64: 44 / 13; 64 at
+// 2,048, 2 heads of 128: 38 / 22; 80 blocks of 64 cut in two for two CTAs on every SM: 31 / 35, hence one CTA to an SM.
+int split_of(int64_t blocks, int64_t most, int sms) {
+  int split = 1;
+  while (split < kMaxSplit && blocks * split * 2 <= sms * 3 / 4 && most >= (int64_t)split * 2 * 3 * kKeys) split *= 2;
+  return split;
+}
+
 template <int DP, Form FORM>
 cudaError_t launch_one(const TileArgs& g, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const DeviceInfo& dev, cudaStream_t stream) {
   const approxifer_attention_args& a = g.a;
@@ -852,16 +870,10 @@ cudaError_t launch_one(const TileArgs& g, const CUtensorMap& q, const CUtensorMa
     return g.prior.split > 1 ? launch_split<DP, true, FORM>(g, q, k, v, dev, ctas, g.prior.split, stream) : launch_split<DP, false, FORM>(g, q, k, v, dev, ctas, 1, stream);
   }
   const int64_t ctas = (int64_t)g.blocks * a.batch * a.Hkv;
-  // Few query blocks: as many CTAs to each, along the keys, as the GPU holds, each with three tiles of keys or more.  (The
-  // lengths are on the device: what a block can see at most says how far it is worth cutting.)  Measured, one CTA a block
-  // against the cluster, us: 2 queries at 4,000 keys, 1 key head of 128: 62 / 16; 10 at 4,000, 8 heads of 64: 44 / 13; 64 at
-  // 2,048, 2 heads of 128: 38 / 22; 80 blocks of 64 cut in two for two CTAs on every SM: 31 / 35, hence one CTA to an SM.
   int64_t most = a.table_pages * a.page_size;
   if (a.window && (int64_t)a.window + a.max_q + a.sinks < most) most = (int64_t)a.window + a.max_q + a.sinks;
   if constexpr (FORM == kThroughPrefix) most += g.prefix_last + 1;
-  const int held = dev.sms * 3 / 4;
-  int split = 1;
-  while (split < kMaxSplit && ctas * split * 2 <= held && most >= (int64_t)split * 2 * 3 * kKeys) split *= 2;
+  const int split = split_of(ctas, most, dev.sms);
   return split > 1 ? launch_split<DP, true, FORM>(g, q, k, v, dev, ctas, split, stream) : launch_split<DP, false, FORM>(g, q, k, v, dev, ctas, 1, stream);
 }
 
@@ -985,23 +997,21 @@ cudaError_t launch_attention_tile_behind(const approxifer_attention_args& a, con
 }
 
 // A short prefix, or few query blocks: walked by every block for itself, in one launch.  In steps, as prefix_parts counts them: the
-// blocks' turns over prefix and own keys, shared by clusters where there are few, against those over the prefix, then over the own keys,
-// and a third launch where many parts are joined.  (The lengths are on the device: all sequences count as the longest may be.)
+// blocks' turns over the prefix, shared by clusters where there are few, against the kernel over it, a second launch, and a third where
+// many parts are joined.  (The lengths are on the device: all sequences count as the longest may be; their own keys, and clusters for
+// them, cost either way.)
 // Measured, in two or three launches against through, us: 8 sequences of 178 behind 108, 4 key heads of 96, 31 / 17; 2 of 46 behind 154,
 // 4 of 128, 24 / 15; 3 of 72 behind 580, 2 of 128, 21 / 23; 3 of 8 behind 4,096, 4 of 128, 18 / 24 (with clusters).
 bool attention_tile_through_wanted(const approxifer_prefix_attention_args& p, const PrefixParts& parts, int sms) {
   const approxifer_attention_args& a = p.own;
   const TileArgs g = tile_args(a);
-  const int per_sm = 3 - tiles_of(padded_head(a));
-  const double own = (double)((a.table_pages * a.page_size < a.max_q ? a.max_q : a.table_pages * a.page_size) + kKeys - 1) / kKeys;
-  const double prefix = (double)((p.prefix_len < p.prefix_pages * a.page_size ? p.prefix_len : p.prefix_pages * a.page_size) + kKeys - 1) / kKeys;
-  const int64_t blocks = (int64_t)g.blocks * a.batch * a.Hkv;
-  int split = 1;
-  while (split < kMaxSplit && blocks * split * 2 <= sms * 3 / 4 && prefix + own >= split * 2 * 3) split *= 2;
-  const int64_t places = (int64_t)sms * per_sm;
-  const double turns = (double)((blocks * split + places - 1) / places);
-  const double through = turns * ((prefix + own) / split + (split > 1 ? 8 : 4));
-  return through < parts.time + turns * (own + 2) + (parts.most > 2 ? 1 : 0);
+  const int64_t room = p.prefix_pages * a.page_size, positions = p.prefix_len < room ? p.prefix_len : room;
+  const int64_t blocks = (int64_t)g.blocks * a.batch * a.Hkv, places = (int64_t)sms * (3 - tiles_of(padded_head(a)));
+  const int64_t own = a.table_pages * a.page_size;
+  const int split = split_of(blocks, positions + own, sms);
+  const bool meets = split > 1 && split_of(blocks, own, sms) == 1;  // (clusters that the own keys alone would not have)
+  const double turns = (double)((blocks * split + places - 1) / places), steps = (double)((positions + kKeys - 1) / kKeys);
+  return turns * steps / split + (meets ? 8 : 0) < parts.time + 2 + (parts.most > 2 ? 1 : 0);
 }
 
 cudaError_t launch_attention_tile_through(const approxifer_prefix_attention_args& p, cudaStream_t stream) {

@@ -19,7 +19,9 @@ __global__ void __launch_bounds__(kElementThreads) prefix_element_kernel(const _
   const int64_t t = unit / a.Hq;
   const int h = (int)(unit % a.Hq), hk = h / (a.Hq / a.Hkv);
   const int b = sequence_of(a.q_start, a.batch, t);
-  const int64_t p = (int64_t)__ldg(a.kv_len + b) - (__ldg(a.q_start + b + 1) - t);  // kv_len - q_len + (t - start)
+  const int end = __ldg(a.q_start + b + 1);
+  if (t >= end) return;  // (behind the last sequence: left as it is)
+  const int64_t p = (int64_t)__ldg(a.kv_len + b) - (end - t);  // kv_len - q_len + (t - start)
   const bf16* q = reinterpret_cast<const bf16*>(a.q) + t * a.q_tstride + h * a.q_hstride;
   float qv[8], acc[8] = {};
 #pragma unroll
