@@ -548,12 +548,14 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
       }
       if constexpr (kWide) {
         // Rows of this warp, a lane to four columns: out of shared memory into the partial results, or with those into the output.
-        constexpr int kTogether = 8, kSide = 32 / kCols;  // rows at a time, side by side
+        constexpr int kTogether = FORM == kBehindPrefix ? 4 : 8, kSide = 32 / kCols;  // rows at a time, side by side
         const int col = lane % kCols, d = half * kOut + col * 4;
         if (into_part(FORM) && mine && half == 0) g.prior.ml[job.piece * g.prior.rows + row_at] = make_float2(m == -CUDART_INF_F ? m : m * scale, l);
         const int64_t to = !mine ? -1 : into_part(FORM) ? (job.piece * g.prior.rows + row_at) * DP
                                                              : (int64_t)(job.token0 + token) * a.o_tstride + (int64_t)(job.hk * g.group + r % g.group) * a.o_hstride;
-        const int parts = FORM == kBehindPrefix ? g.prior.most : 0;  // (a row of fewer gives the others no weight)
+        float part_weight[kOnTheWay];
+#pragma unroll
+        for (int p = 0; p < kOnTheWay; ++p) part_weight[p] = FORM == kBehindPrefix && p < prior.parts ? prior.weight(prior.first[p]) : 0.f;
 #pragma unroll 1
         for (int x = 0; x < 32; x += kTogether * kSide) {
           float4 y[kTogether];
@@ -563,22 +565,21 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
             y[e] = *reinterpret_cast<const float4*>(own_rows + row * kOut * 4 + ((col ^ (row & (kCols - 1))) << 4));
           }
           if constexpr (FORM == kBehindPrefix) {
-#pragma unroll 1
-            for (int p = 0; p < parts; ++p) {
-              const float mine_w = p < prior.parts ? prior.weight(__ldcg(g.prior.ml + p * g.prior.rows + row_at).x) : 0.f;
-              float4 v[kTogether];
-              float w[kTogether];
+            float4 v[kOnTheWay][kTogether];
+#pragma unroll
+            for (int p = 0; p < kOnTheWay; ++p)
 #pragma unroll
               for (int e = 0; e < kTogether; ++e) {
-                const int row = x + e * kSide + lane / kCols;
-                const int64_t at = __shfl_sync(0xffffffffu, p < prior.parts ? row_at : -1, row);
-                w[e] = __shfl_sync(0xffffffffu, mine_w, row);
-                v[e] = at >= 0 ? __ldcg(reinterpret_cast<const float4*>(g.prior.o + (p * g.prior.rows + at) * DP + d)) : make_float4(0.f, 0.f, 0.f, 0.f);
+                const int64_t at = __shfl_sync(0xffffffffu, p < prior.parts ? row_at : -1, x + e * kSide + lane / kCols);
+                v[p][e] = at >= 0 ? __ldcg(reinterpret_cast<const float4*>(g.prior.o + (p * g.prior.rows + at) * DP + d)) : make_float4(0.f, 0.f, 0.f, 0.f);
               }
 #pragma unroll
-              for (int e = 0; e < kTogether; ++e)
-                y[e] = make_float4(fmaf(w[e], v[e].x, y[e].x), fmaf(w[e], v[e].y, y[e].y), fmaf(w[e], v[e].z, y[e].z), fmaf(w[e], v[e].w, y[e].w));
-            }
+            for (int p = 0; p < kOnTheWay; ++p)
+#pragma unroll
+              for (int e = 0; e < kTogether; ++e) {
+                const float w = __shfl_sync(0xffffffffu, part_weight[p], x + e * kSide + lane / kCols);
+                y[e] = make_float4(fmaf(w, v[p][e].x, y[e].x), fmaf(w, v[p][e].y, y[e].y), fmaf(w, v[p][e].z, y[e].z), fmaf(w, v[p][e].w, y[e].w));
+              }
           }
 #pragma unroll
           for (int e = 0; e < kTogether; ++e) {
@@ -1011,7 +1012,7 @@ bool attention_tile_through_wanted(const approxifer_prefix_attention_args& p, co
   const int split = split_of(blocks, positions + own, sms);
   const bool meets = split > 1 && split_of(blocks, own, sms) == 1;  // (clusters that the own keys alone would not have)
   const double turns = (double)((blocks * split + places - 1) / places), steps = (double)((positions + kKeys - 1) / kKeys);
-  return turns * steps / split + (meets ? 8 : 0) < parts.time + 2 + (parts.most > 2 ? 1 : 0);
+  return turns * steps / split + (meets ? 8 : 0) < parts.time + 2 + (parts.most > kOnTheWay ? 1 : 0);
 }
 
 cudaError_t launch_attention_tile_through(const approxifer_prefix_attention_args& p, cudaStream_t stream) {

@@ -148,8 +148,7 @@ bool through(const approxifer_prefix_attention_args& p, const DeviceInfo& dev) {
 PrefixParts parts_of(const approxifer_prefix_attention_args& p, const DeviceInfo& dev, int64_t* bytes) {
   PrefixParts parts = prefix_parts(p, dev);
   const bool token = attention_token_eligible(p.own);
-  parts.apart = token ? parts.most > 8 && !attention_token_balanced(p.own) : parts.most > 2;
-  if (p.own.T * p.own.Hq > 0x7fffffffLL) parts.apart = 0;
+  parts.apart = token ? parts.most > 8 && !attention_token_balanced(p.own) : parts.most > kOnTheWay;
   *bytes = ((parts.most + parts.apart) * parts.rows * ((p.own.D <= 64 ? 64 : 128) + 2) * (int64_t)sizeof(float) + 15) / 16 * 16;
   return parts;
 }

@@ -23,6 +23,8 @@ struct PrefixParts {
   int32_t last;
 };
 
+constexpr int kOnTheWay = 2;  // as many partial results the kernels over several tokens' own keys join; more are joined apart
+
 #ifdef __CUDACC__
 __device__ __forceinline__ float power_of_two(float x) {
   float y;
@@ -34,6 +36,7 @@ __device__ __forceinline__ float power_of_two(float x) {
 struct PriorRow {
   int parts;
   float top, inv;
+  float first[2];  // the maxima of the first two
 
   __device__ __forceinline__ void load(const PrefixParts& p, int64_t row, int64_t token) {
     constexpr int kAt = 8;
@@ -43,6 +46,7 @@ struct PriorRow {
       float2 v[kAt];
 #pragma unroll
       for (int e = 0; e < kAt; ++e) v[e] = i + e < parts ? __ldcg(p.ml + (i + e) * p.rows + row) : make_float2(-CUDART_INF_F, 0.f);
+      if (i == 0) first[0] = v[0].x, first[1] = v[1].x;
       float most = top;
 #pragma unroll
       for (int e = 0; e < kAt; ++e) most = fmaxf(most, v[e].x);
