@@ -12,6 +12,10 @@
 //            one is worked on, and weights and a gate that is the same for all rows are read once for all of them
 //   direct   few rows, rows that are not whole 16 bytes, or too long for two of them in shared memory: loads straight into
 //            registers, a CTA (up to 256 elements a warp) to a row
+//
+// Measured: 16,384 tokens of 4,096, stream in fp32, gate by columns, 133 us, 6.1 TB/s, from a graph, 145 us, 5.5 TB/s, call after call;
+// 1,237 tokens of 1,003 in fp32, two layer norms with biases, a gate by elements, 11 us (bound by the issue of 4-byte accesses: 53 %, and
+// four meetings a row); one token of 4,096 3.9 us, two meetings after its loads.
 #include "async.cuh"
 
 namespace approxifer {
