@@ -26,7 +26,7 @@ __device__ __forceinline__ float mx_value(uint32_t byte) { return __uint_as_floa
 // The activations of the 4-bit products.  Their epilogues have some 3 us a tile before the next one's products are over: where
 // bfloat16 is what is written (it shows 2^-8), the special-function unit's reciprocal (2^-22) takes the place of a division, and
 // of gelu's erf a polynomial times an exponential (Abramowitz and Stegun 7.1.26: within 1.5e-7).  8,192 x 16,384 x 256 with
-// gelu_tanh 253 -> 118 us, with gelu 184 -> 125 us.
+// gelu 200 -> 140 us, with gelu_tanh 126 us, with none 84 us.
 __device__ __forceinline__ float mx_reciprocal(float x) {
   float r;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -43,7 +43,7 @@ __device__ __forceinline__ float mx_activate(float x) {
     // half of erfc(|x| / sqrt 2)
     const float t = mx_reciprocal(fmaf(0.2316418826f, fabsf(x), 1.f));
     const float h = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 0.5307027145f, -0.7265760135f), 0.7107068705f), -0.142248368f), 0.127414796f) * pow2(-0.7213475204f * x * x);
-    return x >= 0.f ? x - x * h : x * h;
+    return x * (x >= 0.f ? 1.f - h : h);  // (a factor: infinity stays)
   }
   return activate<ACT, Out>(x);
 }

@@ -219,6 +219,24 @@ def test_mx_linear_nan_stays_in_its_rows_and_columns(M, N, K):
     check(got[rows][:, cols], want[rows][:, cols], bound[rows][:, cols])
 
 
+@pytest.mark.parametrize("M,N", [(1, 40), (20, 300), (300, 1003), (3000, 1400), (3000, 1003)])
+@pytest.mark.parametrize("act", ["none", "relu", "gelu", "gelu_tanh", "silu"])
+@pytest.mark.parametrize("out", [BF, F32])
+def test_mx_linear_activations_at_their_ends(M, N, act, out):
+    """Infinities, NaN, the largest and very negative numbers before the activation: what the formula makes of them in 64 bits."""
+    x, w = spread((M, 64), 1), ref.mx_quantize(normal((N, 64), 2, std=0.1))
+    ends = torch.tensor([float("inf"), float("-inf"), float("nan"), 3e38, -3e38, 1e5, -1e5, 95.0, -95.0, 0.0], dtype=BF)
+    b = ends.repeat(N // len(ends) + 1)[:N].contiguous()
+    z = ref.mx_values(*ref.mx_quantize(x)) @ ref.mx_values(*w).T + b.double()
+    f = torch.nn.functional
+    want = {"none": lambda t: t, "relu": f.relu, "gelu": f.gelu, "gelu_tanh": lambda t: f.gelu(t, approximate="tanh"), "silu": f.silu}[act](z)
+    _, bound = ref.linear(ref.mx_values(*ref.mx_quantize(x)), ref.mx_values(*w), torch.where(torch.isfinite(b), b, torch.zeros_like(b)), act, None, out)
+    got = ap.approxifer_mx_linear(x.cuda(), w[0].cuda(), w[1].cuda(), bias=b.cuda(), activation=act, out_dtype=out).double().cpu()
+    assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(got == float("inf"), want == float("inf")) and torch.equal(got == float("-inf"), want == float("-inf"))
+    finite = torch.isfinite(want)
+    assert ((got - want).abs() <= bound)[finite].all()
+
+
 @pytest.mark.parametrize("M", [1, 24, 300, 3000])
 def test_mx_linear_is_repeatable_and_runs_on_a_stream_and_in_a_graph(M):
     x, b = spread((M, 2048), 1).cuda(), normal((1024,), 3).cuda()
