@@ -27,6 +27,7 @@ namespace {
 constexpr int kMaxThreads = 1024;
 constexpr int kMaxStages = 4;
 constexpr int kHeader = 384;            // barriers, the sums' meeting place
+constexpr int kStaged = 2;              // fours a thread where weights, biases and the gate are copied ahead by the direct form
 constexpr int kRingBytes = 200 * 1024;  // of an SM's shared memory, for all its CTAs
 
 // Four elements of type T, as they are loaded.
@@ -48,18 +49,47 @@ struct Four<float> {
   __device__ __forceinline__ void pin() {}
 };
 
-// VEC: four neighbours.  Else: four elements `step` apart, of which `count` are there.
-template <bool VEC, typename T>
-__device__ __forceinline__ Four<T> load4(const T* p, int step, int count) {
+template <int BYTES>
+__device__ __forceinline__ void copy_ahead(uint32_t dst, const void* src, int there) {  // `there` bytes of it, then zeros
+  asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(BYTES), "r"(there) : "memory");
+}
+__device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
+// How a thread's fours lie in the rows.
+enum Access {
+  kWhole,     // four neighbours, a row beginning with the first of four at a whole address
+  kShifted,   // four neighbours at a whole address in the tokens' rows, which begin anywhere, all arrays' alike: at both ends there may be
+              // fewer.  (In weights, and in a gate that is the same for all rows, the four then lie anywhere.)
+  kElements,  // four elements a CTA's width apart
+};
+
+// The elements `first` (+ 0 .. 3, or + 0 .. 3 times `step`) of a row or of the weights, those that are there: in kElements `count` of them.
+template <Access A, bool OF_ROW, typename T>
+__device__ __forceinline__ Four<T> load4(const T* p, int first, int step, int count) {
   Four<T> v;
-  if constexpr (VEC) {
-    using Raw = decltype(v.u);
+  using Raw = decltype(v.u);
+  p += first;
+  if constexpr (A == kWhole) {
     v.u = Raw{};
     if (count > 0) v.u = *reinterpret_cast<const Raw*>(p);
   } else {
     T x[4];
+    if constexpr (A == kShifted) {
+      if (first >= 0 && count >= 4) {
+        if constexpr (OF_ROW) {
+          v.u = *reinterpret_cast<const Raw*>(p);
+          return v;
+        }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = i < count ? p[(int64_t)i * step] : narrow<T>(0.f);
+        for (int i = 0; i < 4; ++i) x[i] = p[i];
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = i < count && first + i >= 0 ? p[i] : narrow<T>(0.f);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = i < count ? p[(int64_t)i * step] : narrow<T>(0.f);
+    }
     if constexpr (sizeof(T) == 2) {
       const auto bits = [](bf16 b) { return (uint32_t)__bfloat16_as_ushort(b); };
       v.u = make_uint2(bits(x[0]) | bits(x[1]) << 16, bits(x[2]) | bits(x[3]) << 16);
@@ -69,16 +99,59 @@ __device__ __forceinline__ Four<T> load4(const T* p, int step, int count) {
   }
   return v;
 }
-template <bool VEC, typename T>
-__device__ __forceinline__ void store4(T* p, int step, int count, const float (&v)[4]) {
-  if constexpr (VEC) {
-    if (count <= 0) return;
+// Starts copying them to the thread's own place in shared memory, 16 bytes or, of whole fours of bfloat16, 8.  (Copies are of 4 bytes or
+// more: of bfloat16 that lies anywhere the two whole fours that hold the four, which are put together when they are read.)
+template <Access A, typename T>
+constexpr bool can_copy = sizeof(T) == 4 || A != kElements;
+template <Access A, typename T>
+constexpr int place_bytes = sizeof(T) == 2 && A == kWhole ? 8 : 16;
+template <Access A, bool OF_ROW, typename T>
+__device__ __forceinline__ void copy4(unsigned char* place, const T* p, int first, int step, int count) {
+  const uint32_t dst = smem_addr(place);
+  if (A == kWhole ? count > 0 : A == kShifted && OF_ROW && first >= 0 && count >= 4) {
+    copy_ahead<4 * sizeof(T)>(dst, p + first, 4 * sizeof(T));
+  } else if constexpr (A != kWhole && sizeof(T) == 4) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const bool there = i < count && (A == kElements || first + i >= 0);
+      copy_ahead<4>(dst + 4 * i, there ? p + first + (A == kElements ? (int64_t)i * step : i) : p, there ? 4 : 0);
+    }
+  } else if constexpr (A == kShifted && OF_ROW) {
+    *reinterpret_cast<Four<T>*>(place) = load4<A, OF_ROW, T>(p, first, step, count);
+  } else if constexpr (A == kShifted) {
+    const int from = first & ~3, n = first + count;
+    if (from >= 0 && from + 8 <= n) {
+      copy_ahead<8>(dst, p + from, 8);
+      copy_ahead<8>(dst + 8, p + from + 4, 8);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) reinterpret_cast<T*>(place)[i] = from + i >= 0 && from + i < n ? p[from + i] : narrow<T>(0.f);
+    }
+  }
+}
+template <Access A, bool OF_ROW, typename T>
+__device__ __forceinline__ Four<T> copied4(const unsigned char* place, int first) {
+  Four<T> v;
+  if constexpr (A == kShifted && !OF_ROW && sizeof(T) == 2) {
+    const uint4 u = *reinterpret_cast<const uint4*>(place);
+    const bool far = first & 2;
+    const uint32_t x = far ? u.y : u.x, y = far ? u.z : u.y, z = far ? u.w : u.z;
+    v.u = make_uint2(__funnelshift_r(x, y, (first & 1) * 16), __funnelshift_r(y, z, (first & 1) * 16));
+  } else {
+    v.u = *reinterpret_cast<const decltype(v.u)*>(place);
+  }
+  return v;
+}
+template <Access A, typename T>
+__device__ __forceinline__ void store4(T* p, int first, int step, int count, const float (&v)[4]) {
+  p += first;
+  if (A == kWhole ? count > 0 : A == kShifted && first >= 0 && count >= 4) {
     if constexpr (sizeof(T) == 2) __stcs(reinterpret_cast<uint2*>(p), make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])));
     else __stcs(reinterpret_cast<float4*>(p), make_float4(v[0], v[1], v[2], v[3]));
-  } else {
+  } else if constexpr (A != kWhole) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      if (i < count) p[(int64_t)i * step] = narrow<T>(v[i]);
+      if (i < count && (A == kElements || first + i >= 0)) p[A == kElements ? (int64_t)i * step : i] = narrow<T>(v[i]);
   }
 }
 
@@ -110,7 +183,7 @@ __device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_
 enum GateKind { kGateNone, kGateColumns, kGateRows };  // one row for all tokens; a row, or a value, for each
 
 // Q fours of elements a thread.  Elements that are not there are zero and stay out of the sums.
-template <typename S, typename T, int Q, bool VEC, bool RING, GateKind GATE, int MOST>
+template <typename S, typename T, int Q, Access A, bool RING, GateKind GATE, int MOST>
 __global__ void __launch_bounds__(MOST, MOST == kMaxThreads ? 1 : 10) block_norm_kernel(const __grid_constant__ approxifer_block_norm_args a, int stages) {
   extern __shared__ __align__(128) unsigned char smem[];
   constexpr bool kHold = RING;  // weights and gate stay in registers
@@ -121,9 +194,11 @@ __global__ void __launch_bounds__(MOST, MOST == kMaxThreads ? 1 : 10) block_norm
   int64_t t = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
   const T* G = static_cast<const T*>(a.gate);
   // this thread's fours: the first element, how many there are
-  const int mine = VEC ? 0 : (a.N - lane + L - 1) / L;
-  auto first = [&](int q) { return VEC ? (q * L + lane) * 4 : q * 4 * L + lane; };
-  auto there = [&](int q) { return VEC ? a.N - first(q) : mine - 4 * q; };
+  const int mine = A == kElements ? (a.N - lane + L - 1) / L : 0;
+  const int shift = A == kShifted ? (int)(reinterpret_cast<uintptr_t>(static_cast<const S*>(a.R) + t * a.r_rstride) / sizeof(S) % 4) : 0;
+  auto first = [&](int q) { return A == kElements ? q * 4 * L + lane : (q * L + lane) * 4 - shift; };
+  auto there = [&](int q) { return A == kElements ? mine - 4 * q : a.N - first(q); };
+  auto holds = [&](int q, int i) { return i < there(q) && (A != kShifted || first(q) + i >= 0); };
   const float inv_n = 1.f / (float)a.N;
   // (ring) a stage: a row of R, of Y, of the gate
   const uint32_t r_bytes = a.N * sizeof(S), y_bytes = a.Y ? a.N * sizeof(T) : 0, g_bytes = GATE == kGateRows && a.g_cstride ? a.N * sizeof(T) : 0;
@@ -151,7 +226,7 @@ __global__ void __launch_bounds__(MOST, MOST == kMaxThreads ? 1 : 10) block_norm
 
   Four<T> aw[Q], bw[Q];
   float gate[Q][4];
-  auto vector4 = [&](const void* p, int q) { return load4<VEC, T>(static_cast<const T*>(p) + first(q), L, there(q)); };
+  auto vector4 = [&](const void* p, int q) { return load4<A, false, T>(static_cast<const T*>(p), first(q), L, there(q)); };
   if constexpr (kHold) {
 #pragma unroll
     for (int q = 0; q < Q; ++q) {
@@ -164,24 +239,39 @@ __global__ void __launch_bounds__(MOST, MOST == kMaxThreads ? 1 : 10) block_norm
       }
     }
   }
+  // What is needed only after the first sums is copied to this thread's place in shared memory meanwhile (a row's time is that of its
+  // loads after each other), or, where it cannot be, asked for into the cache.
+  enum Array { kGateRow, kAfterWeight, kAfterBias, kBeforeWeight, kBeforeBias };
+  constexpr bool kStage = !RING && Q == kStaged, kCopy = kStage && can_copy<A, T>;
+  auto place = [&](int array, int q) {
+    return smem + kHeader + ((array * Q + q) * (blockDim.x * blockDim.y) + threadIdx.y * blockDim.x + threadIdx.x) * place_bytes<A, T>;
+  };
   if constexpr (!RING) {
-    // What is needed only after the first sums is asked for now, into the cache: a row's time is that of its loads after each other.
-    auto ask = [&](const void* p, int64_t at) {
-      const T* from = static_cast<const T*>(p) + at;
+    auto ask = [&](auto of_row, int array, const T* from) {
 #pragma unroll
-      for (int q = 0; q < Q; ++q)
+      for (int q = 0; q < Q; ++q) {
+        if constexpr (kCopy) {
+          copy4<A, decltype(of_row)::value, T>(place(array, q), from, first(q), L, there(q));
+        } else {
 #pragma unroll
-        for (int i = 0; i < (VEC ? 1 : 4); ++i)
-          if (there(q) > i) asm volatile("prefetch.global.L1 [%0];" ::"l"(from + first(q) + i * L));
+          for (int i = 0; i < (A == kElements ? 4 : 1); ++i)
+            if (holds(q, i)) asm volatile("prefetch.global.L1 [%0];" ::"l"(from + first(q) + i * L));
+        }
+      }
+    };
+    auto rest = [&](int array, const void* p) {
+      if (p) ask(std::false_type{}, array, static_cast<const T*>(p));
     };
     if (t < a.T) {
-      if (GATE != kGateNone && a.g_cstride) ask(G, t * a.g_rstride);
-      if (a.after_weight) ask(a.after_weight, 0);
-      if (a.after_bias) ask(a.after_bias, 0);
-      if (a.before_weight) ask(a.before_weight, 0);
-      if (a.before_bias) ask(a.before_bias, 0);
+      if (GATE != kGateNone && a.g_cstride) ask(std::bool_constant<GATE == kGateRows>{}, kGateRow, G + t * a.g_rstride);
+      rest(kAfterWeight, a.after_weight), rest(kAfterBias, a.after_bias), rest(kBeforeWeight, a.before_weight), rest(kBeforeBias, a.before_bias);
     }
   }
+  // Of weights and biases.
+  auto again = [&](int array, const void* p, int q) {
+    if constexpr (kCopy) return copied4<A, false, T>(place(array, q), first(q));
+    else return vector4(p, q);
+  };
   int turn = 0, s = 0;
   auto one_row = [&]() {
     float x[Q][4], res[Q][4], one = 1.f;
@@ -197,10 +287,10 @@ __global__ void __launch_bounds__(MOST, MOST == kMaxThreads ? 1 : 10) block_norm
       Four<T> yv[Q], gv[Q];
 #pragma unroll
       for (int q = 0; q < Q; ++q) {
-        rv[q] = load4<VEC, S>(R + first(q), L, there(q));
-        if (a.Y) yv[q] = load4<VEC, T>(Y + first(q), L, there(q));
+        rv[q] = load4<A, true, S>(R, first(q), L, there(q));
+        if (a.Y) yv[q] = load4<A, true, T>(Y, first(q), L, there(q));
         if constexpr (GATE == kGateRows && RING)
-          if (a.g_cstride) gv[q] = load4<VEC, T>(g + first(q), L, there(q));
+          if (a.g_cstride) gv[q] = load4<A, true, T>(g, first(q), L, there(q));
       }
       if constexpr (GATE == kGateRows) {
         if (!a.g_cstride) one = gate_of(a.gate_activation, widen(G[t * a.g_rstride]));
@@ -221,7 +311,7 @@ __global__ void __launch_bounds__(MOST, MOST == kMaxThreads ? 1 : 10) block_norm
         if (++s == stages) s = 0, ++turn;
       }
     }
-    auto norm = [&](int kind, float (&x)[Q][4], const void* w, Four<T> (&held)[Q], const void* b) {
+    auto norm = [&](int kind, float (&x)[Q][4], int weights, const void* w, Four<T> (&held)[Q], const void* b) {
       if (kind == APPROXIFER_NORM_NONE) return;
       if (kind == APPROXIFER_NORM_LAYER) {
         float sum = 0.f;
@@ -233,7 +323,7 @@ __global__ void __launch_bounds__(MOST, MOST == kMaxThreads ? 1 : 10) block_norm
 #pragma unroll
         for (int q = 0; q < Q; ++q)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) x[q][i] = i < there(q) ? x[q][i] - mean : 0.f;
+          for (int i = 0; i < 4; ++i) x[q][i] = holds(q, i) ? x[q][i] - mean : 0.f;
       }
       float sq = 0.f;
 #pragma unroll
@@ -241,31 +331,34 @@ __global__ void __launch_bounds__(MOST, MOST == kMaxThreads ? 1 : 10) block_norm
 #pragma unroll
         for (int i = 0; i < 4; ++i) sq = fmaf(x[q][i], x[q][i], sq);
       const float k = rsqrtf(row.sum(sq) * inv_n + a.eps);
+      if constexpr (kCopy) copies_done();
 #pragma unroll
       for (int q = 0; q < Q; ++q) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[q][i] *= k;
         if (w) {
-          if (!kHold) held[q] = vector4(w, q);
+          if (!kHold) held[q] = again(weights, w, q);
           held[q].pin();
 #pragma unroll
           for (int i = 0; i < 4; ++i) x[q][i] *= held[q].at(i);
         }
         if (b) {
-          const Four<T> v = vector4(b, q);
+          const Four<T> v = again(weights + 1, b, q);
 #pragma unroll
           for (int i = 0; i < 4; ++i) x[q][i] += v.at(i);
         }
       }
     };
     if (a.Y) {
-      norm(a.after, x, a.after_weight, aw, a.after_bias);
+      norm(a.after, x, kAfterWeight, a.after_weight, aw, a.after_bias);
       S* out = static_cast<S*>(a.R_out) + t * a.ro_rstride;
 #pragma unroll
       for (int q = 0; q < Q; ++q) {
         if constexpr (GATE != kGateNone && !RING) {
           if (a.g_cstride) {
-            const Four<T> v = vector4(G + t * a.g_rstride, q);
+            Four<T> v;
+            if constexpr (kCopy) copies_done(), v = copied4<A, GATE == kGateRows, T>(place(kGateRow, q), first(q));
+            else v = load4<A, GATE == kGateRows, T>(G + t * a.g_rstride, first(q), L, there(q));
 #pragma unroll
             for (int i = 0; i < 4; ++i) gate[q][i] = gate_of(a.gate_activation, v.at(i));
           } else {
@@ -276,20 +369,21 @@ __global__ void __launch_bounds__(MOST, MOST == kMaxThreads ? 1 : 10) block_norm
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float u = GATE == kGateNone ? x[q][i] : x[q][i] * gate[q][i];
-          res[q][i] = i < there(q) ? fmaf(a.block_scale, u, a.residual_scale * res[q][i]) : 0.f;
+          res[q][i] = holds(q, i) ? fmaf(a.block_scale, u, a.residual_scale * res[q][i]) : 0.f;
         }
-        store4<VEC, S>(out + first(q), L, there(q), res[q]);
+        store4<A, S>(out, first(q), L, there(q), res[q]);
       }
     }
     if (a.before != APPROXIFER_NORM_NONE) {
-      norm(a.before, res, a.before_weight, bw, a.before_bias);
+      norm(a.before, res, kBeforeWeight, a.before_weight, bw, a.before_bias);
       T* out = static_cast<T*>(a.X) + t * a.x_rstride;
 #pragma unroll
-      for (int q = 0; q < Q; ++q) store4<VEC, T>(out + first(q), L, there(q), res[q]);
+      for (int q = 0; q < Q; ++q) store4<A, T>(out, first(q), L, there(q), res[q]);
     }
   };
   if constexpr (!RING) {
     if (t < a.T) one_row();
+    if constexpr (kCopy) copies_done();  // (weights of a norm that is not asked for)
   } else {
     for (; t < a.T; t += step) one_row();
     __syncthreads();
@@ -298,7 +392,7 @@ __global__ void __launch_bounds__(MOST, MOST == kMaxThreads ? 1 : 10) block_norm
 }
 
 // (Narrow rows: registers for ten CTAs of 128 threads on an SM.)
-template <typename S, typename T, int Q, bool VEC, bool RING, int MOST = kMaxThreads>
+template <typename S, typename T, int Q, Access A, bool RING, int MOST = kMaxThreads>
 cudaError_t launch_kind(const approxifer_block_norm_args& a, const DeviceInfo& dev, int64_t ctas, dim3 block, int smem, int stages, cudaStream_t stream) {
   auto launch = [&](auto kernel, auto tag) {
     const cudaError_t e = ensure_dynamic_smem<decltype(tag)>(kernel, dev.ordinal, smem);
@@ -307,9 +401,9 @@ cudaError_t launch_kind(const approxifer_block_norm_args& a, const DeviceInfo& d
   struct None {};
   struct Columns {};
   struct Rows {};
-  if (a.gate == nullptr) return launch(block_norm_kernel<S, T, Q, VEC, RING, kGateNone, MOST>, None{});
-  if (a.g_rstride == 0 && a.g_cstride == 1) return launch(block_norm_kernel<S, T, Q, VEC, RING, kGateColumns, MOST>, Columns{});
-  return launch(block_norm_kernel<S, T, Q, VEC, RING, kGateRows, MOST>, Rows{});
+  if (a.gate == nullptr) return launch(block_norm_kernel<S, T, Q, A, RING, kGateNone, MOST>, None{});
+  if (a.g_rstride == 0 && a.g_cstride == 1) return launch(block_norm_kernel<S, T, Q, A, RING, kGateColumns, MOST>, Columns{});
+  return launch(block_norm_kernel<S, T, Q, A, RING, kGateRows, MOST>, Rows{});
 }
 
 template <typename S, typename T>
@@ -319,24 +413,38 @@ cudaError_t launch_types(const approxifer_block_norm_args& a, const DeviceInfo& 
   const bool vec = a.N % 8 == 0 && whole(a.R, a.r_rstride, sizeof(S)) && whole(a.Y, a.Y ? a.y_rstride : 0, sizeof(T)) &&
                    (!each || whole(a.gate, a.g_rstride, sizeof(T))) && aligned16(a.after_weight) && aligned16(a.after_bias) && aligned16(a.before_weight) &&
                    aligned16(a.before_bias) && whole(a.R_out, a.Y ? a.ro_rstride : 0, sizeof(S)) && whole(a.X, a.before ? a.x_rstride : 0, sizeof(T));
+  // rows of other lengths or strides: those of all arrays as far from a whole address, and a thread to each four that they touch
+  auto shift = [&](const void* p, int64_t t, int64_t stride, int size) { return (reinterpret_cast<uintptr_t>(p) / size + t * (uint64_t)stride) % 4; };
+  auto alike = [&](const void* p, int64_t stride, int size) {
+    return p == nullptr || (shift(p, 0, stride, size) == shift(a.R, 0, a.r_rstride, sizeof(S)) && (a.T == 1 || shift(p, 1, stride, size) == shift(a.R, 1, a.r_rstride, sizeof(S))));
+  };
+  // (weights, and a gate that is the same for all rows: 8 bytes of bfloat16 are copied at a time)
+  auto copies = [&](const void* p) { return sizeof(T) == 4 || aligned8(p); };
+  const bool weights = copies(a.after_weight) && copies(a.after_bias) && copies(a.before_weight) && copies(a.before_bias) && (!each || a.g_rstride != 0 || copies(a.gate));
+  const bool shifted = !vec && weights && a.N + 3 <= 16 * kMaxThreads && alike(a.Y, a.y_rstride, sizeof(T)) && alike(a.Y ? a.R_out : nullptr, a.ro_rstride, sizeof(S)) &&
+                       alike(a.before ? a.X : nullptr, a.x_rstride, sizeof(T)) && (!each || a.g_rstride == 0 || alike(a.gate, a.g_rstride, sizeof(T)));
+  const int width = shifted ? a.N + 3 : a.N;
   // eight elements a thread as long as a CTA has the threads for it
-  const int fours = a.N <= 8 * kMaxThreads ? 2 : 4;
-  const int threads = ((a.N + 4 * fours - 1) / (4 * fours) + 31) / 32 * 32;
+  const int fours = width <= 8 * kMaxThreads ? 2 : 4;
+  const int threads = ((width + 4 * fours - 1) / (4 * fours) + 31) / 32 * 32;
   if (vec && fours == 2 && threads > 32) {
     const int64_t stage = (int64_t)a.N * (sizeof(S) + (a.Y ? sizeof(T) : 0) + (each && a.g_rstride != 0 ? sizeof(T) : 0));
     const int by_threads = kMaxThreads / threads;  // (64 registers a thread)
     const int stages = (int)(kRingBytes / by_threads / stage < kMaxStages ? kRingBytes / by_threads / stage : kMaxStages);
     const int64_t fit = (int64_t)dev.sms * by_threads, turns = (a.T + fit - 1) / fit;
     if (stages >= 2 && turns >= 2)
-      return launch_kind<S, T, 2, true, true>(a, dev, (a.T + turns - 1) / turns, dim3(threads), kHeader + (int)(stages * stage), stages, stream);  // (turns of equal length)
+      return launch_kind<S, T, 2, kWhole, true>(a, dev, (a.T + turns - 1) / turns, dim3(threads), kHeader + (int)(stages * stage), stages, stream);  // (turns of equal length)
   }
   const int rows = threads == 32 ? 4 : 1;
   const dim3 block(threads, rows);
   const int64_t ctas = (a.T + rows - 1) / rows;
-  if (fours == 2 && threads * rows <= 128)
-    return vec ? launch_kind<S, T, 2, true, false, 128>(a, dev, ctas, block, kHeader, 0, stream) : launch_kind<S, T, 2, false, false, 128>(a, dev, ctas, block, kHeader, 0, stream);
-  if (fours == 2) return vec ? launch_kind<S, T, 2, true, false>(a, dev, ctas, block, kHeader, 0, stream) : launch_kind<S, T, 2, false, false>(a, dev, ctas, block, kHeader, 0, stream);
-  return vec ? launch_kind<S, T, 4, true, false>(a, dev, ctas, block, kHeader, 0, stream) : launch_kind<S, T, 4, false, false>(a, dev, ctas, block, kHeader, 0, stream);
+  auto direct = [&](auto access) {
+    constexpr Access A = decltype(access)::value;
+    const int smem = kHeader + (fours == kStaged && can_copy<A, T> ? 5 * kStaged * place_bytes<A, T> * threads * rows : 0);
+    if (fours == 2 && threads * rows <= 128) return launch_kind<S, T, 2, A, false, 128>(a, dev, ctas, block, smem, 0, stream);
+    return fours == 2 ? launch_kind<S, T, 2, A, false>(a, dev, ctas, block, smem, 0, stream) : launch_kind<S, T, 4, A, false>(a, dev, ctas, block, smem, 0, stream);
+  };
+  return vec ? direct(std::integral_constant<Access, kWhole>{}) : shifted ? direct(std::integral_constant<Access, kShifted>{}) : direct(std::integral_constant<Access, kElements>{});
 }
 
 }  // namespace

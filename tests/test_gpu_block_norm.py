@@ -200,3 +200,28 @@ def test_block_norm_refuses_what_the_library_cannot_take():
                 dict(residual_out=r.expand(4, 64)[:1].expand(4, 64))):
         with pytest.raises(ap.ApproxiferError):
             ap.approxifer_block_norm(**dict(good, **bad))
+
+
+@pytest.mark.parametrize("T,N", [(1, 5), (9, 77), (300, 515), (40, 1004), (7, 4100), (3, 8189), (3, 8192), (2, 16381), (2, 16382), (2, 16384)])
+@pytest.mark.parametrize("stream,dtype", [(F32, F32), (F32, BF), (BF, BF)])
+def test_block_norm_rows_that_begin_anywhere(T, N, stream, dtype):
+    """Rows that lie alike in all arrays, at each distance from a whole address, and rows that do not."""
+    gates = ("element", "column", "token", None)
+    for i, offsets in enumerate(((1, 1, 1, 1, 1), (2, 2, 2, 2, 2), (3, 7, 3, 3, 11), (0, 0, 0, 0, 0), (1, 2, 3, 4, 5), (0, 0, 1, 0, 0))):
+        for pads in ((5, 5, 5, 5, 5), (12, 12, 12, 12, 12), (12, 13, 14, 12, 15)):
+            v, k = case(T, N, stream, dtype, "layer" if i % 2 else "rms", "rms" if i % 2 else "layer", gates[i % 4], "sigmoid", i % 3 == 0, 1.0)
+            first, second = ref.block_norm(**v, **k, residual_scale=0.5, block_scale=1.0, eps=1e-6)
+            dev = {n: None if t is None else t.cuda() for n, t in v.items()}
+            types = (stream, dtype, dtype, stream, dtype)
+            wide = [torch.full((T + 2, N + 11 + p), 7.0, dtype=t, device="cuda") for p, t in zip(pads, types)]
+            views = [w[1: 1 + T, o: o + N] for w, o in zip(wide, offsets)]
+            for n, view in zip(("residual", "block", "gate"), views):
+                if dev[n] is not None and dev[n].shape == view.shape:
+                    view.copy_(dev[n])
+                    dev[n] = view
+            r, x = ap.approxifer_block_norm(**dev, **k, residual_scale=0.5, block_scale=1.0, eps=1e-6, residual_out=views[3], next_out=views[4])
+            check(r, first, "residual")
+            check(x, second, "next")
+            for w, view in zip(wide[3:], views[3:]):
+                view.fill_(7.0)
+                assert bool((w == 7.0).all())
