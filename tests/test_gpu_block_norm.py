@@ -202,7 +202,7 @@ def test_block_norm_refuses_what_the_library_cannot_take():
             ap.approxifer_block_norm(**dict(good, **bad))
 
 
-@pytest.mark.parametrize("T,N", [(1, 5), (9, 77), (300, 515), (40, 1004), (7, 4100), (3, 8189), (3, 8192), (2, 16381), (2, 16382), (2, 16384)])
+@pytest.mark.parametrize("T,N", [(1, 5), (9, 77), (300, 515), (40, 1004), (7, 4100), (3, 8189), (3, 8192), (2, 16381), (2, 16382), (2, 16384), (160, 2051), (150, 8189)])
 @pytest.mark.parametrize("stream,dtype", [(F32, F32), (F32, BF), (BF, BF)])
 def test_block_norm_rows_that_begin_anywhere(T, N, stream, dtype):
     """Rows that lie alike in all arrays, at each distance from a whole address, and rows that do not."""
