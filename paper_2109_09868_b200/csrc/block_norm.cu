@@ -14,8 +14,8 @@
 //            registers, a CTA (up to 256 elements a warp) to a row
 //
 // Measured: 16,384 tokens of 4,096, stream in fp32, gate by columns, 133 us, 6.1 TB/s, from a graph, 145 us, 5.5 TB/s, call after call;
-// 1,237 tokens of 1,003 in fp32, two layer norms with biases, a gate by elements, 11 us (bound by the issue of 4-byte accesses: 53 %, and
-// four meetings a row); one token of 4,096 3.9 us, two meetings after its loads.
+// 1,237 tokens of 1,003 in fp32, two layer norms with biases, a gate by elements, 9.7 us (half of it instruction issue, and four meetings a
+// row, nearly at the same time in all of them: one row by itself takes 3.5); one token of 4,096 2.9 us.
 #include "async.cuh"
 
 namespace approxifer {
@@ -53,7 +53,10 @@ template <int BYTES>
 __device__ __forceinline__ void copy_ahead(uint32_t dst, const void* src, int there) {  // `there` bytes of it, then zeros
   asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(BYTES), "r"(there) : "memory");
 }
-__device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+__device__ __forceinline__ void copies_done() {  // (of the warp)
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  __syncwarp();
+}
 
 // How a thread's fours lie in the rows.
 enum Access {
@@ -99,7 +102,7 @@ __device__ __forceinline__ Four<T> load4(const T* p, int first, int step, int co
   }
   return v;
 }
-// Starts copying them to the thread's own place in shared memory, 16 bytes or, of whole fours of bfloat16, 8.  (Copies are of 4 bytes or
+// Starts copying them (whole warps) to the thread's own place in shared memory, 16 bytes or, of whole fours of bfloat16, 8.  (Copies are of 4 bytes or
 // more: of bfloat16 that lies anywhere the two whole fours that hold the four, which are put together when they are read.)
 template <Access A, typename T>
 constexpr bool can_copy = sizeof(T) == 4 || A != kElements;
@@ -110,14 +113,19 @@ __device__ __forceinline__ void copy4(unsigned char* place, const T* p, int firs
   const uint32_t dst = smem_addr(place);
   if (A == kWhole ? count > 0 : A == kShifted && OF_ROW && first >= 0 && count >= 4) {
     copy_ahead<4 * sizeof(T)>(dst, p + first, 4 * sizeof(T));
-  } else if constexpr (A != kWhole && sizeof(T) == 4) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const bool there = i < count && (A == kElements || first + i >= 0);
-      copy_ahead<4>(dst + 4 * i, there ? p + first + (A == kElements ? (int64_t)i * step : i) : p, there ? 4 : 0);
-    }
   } else if constexpr (A == kShifted && OF_ROW) {
     *reinterpret_cast<Four<T>*>(place) = load4<A, OF_ROW, T>(p, first, step, count);
+  } else if constexpr (A == kShifted && sizeof(T) == 4) {  // (a warp's fours lie side by side, here and there: its lanes copy neighbours)
+    const int lane = threadIdx.x % 32, n = first + count;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int on = 32 * i - 3 * lane, at = first + on;
+      const bool there = at >= 0 && at < n;
+      copy_ahead<4>(dst + 4 * on, there ? p + at : p, there ? 4 : 0);
+    }
+  } else if constexpr (A == kElements && sizeof(T) == 4) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) copy_ahead<4>(dst + 4 * i, i < count ? p + first + (int64_t)i * step : p, i < count ? 4 : 0);
   } else if constexpr (A == kShifted) {
     const int from = first & ~3, n = first + count;
     if (from >= 0 && from + 8 <= n) {
@@ -434,7 +442,13 @@ cudaError_t launch_types(const approxifer_block_norm_args& a, const DeviceInfo& 
     const int by_threads = kMaxThreads / threads;  // (64 registers a thread)
     const int stages = (int)(kRingBytes / by_threads / stage < kMaxStages ? kRingBytes / by_threads / stage : kMaxStages);
     const int64_t fit = (int64_t)dev.sms * by_threads, turns = (a.T + fit - 1) / fit;
-    if (stages >= 2 && turns >= 2)
+    // The ring's start costs what two or three rows do.  Narrow rows, of which an SM holds many CTAs, hide their loads without it, all
+    // the more where a gate by elements takes its registers.  Measured, ring against direct, us: 300 rows of 4,096 (2 turns), rms norms,
+    // 5.9 / 5.3, 600 with a gate by columns (3 turns) 9.3 / 10.0, 16,384 133 / 218; 300 of 8,192 7.9 / 9.6; of 1,024, layer norms and a gate by
+    // elements, 1,300 (2 turns) 10.3 / 7.1, 30,000 119 / 104, rms norms and a gate by columns 62 / 81; 5,000 of 264 (3 turns) 8.9 / 7.3.
+    const bool narrow = threads <= 128;
+    const int64_t least = threads > 512 ? 2 : narrow ? 8 : 3;
+    if (stages >= 2 && turns >= least && !(narrow && each))
       return launch_kind<S, T, 2, kWhole, true>(a, dev, (a.T + turns - 1) / turns, dim3(threads), kHeader + (int)(stages * stage), stages, stream);  // (turns of equal length)
   }
   const int rows = threads == 32 ? 4 : 1;

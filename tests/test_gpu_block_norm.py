@@ -61,6 +61,9 @@ CASES = [  # T, N, stream, type, after, before, gate, activation, biases, mean
     (9001, 288, BF, BF, None, "rms", None, "none", False, 0.0),
     (1237, 1003, F32, F32, "layer", "layer", "element", "sigmoid", True, 0.0),
     (900, 2048, BF, BF, "rms", None, "column", "none", True, 0.0),
+    (30000, 264, BF, BF, "rms", "layer", "column", "tanh", True, 0.0),      # many narrow rows: turns over the ring
+    (12000, 1000, F32, BF, "layer", "rms", None, "none", True, 1.0),
+    (12000, 520, F32, F32, "rms", "rms", "token", "sigmoid", False, 0.0),
     (900, 2056, F32, BF, None, None, "element", "tanh", False, 0.0),
 ]
 
