@@ -158,6 +158,26 @@ __device__ __forceinline__ void bring_raw(const TileArgs& a, unsigned char* to, 
   }
 }
 
+// (4 bits) One choice of the activation for all values that a thread has in hand: with one for each, the instructions fetched lie
+// scattered over the code of all activations, and in a small product those fetches are waited for; nor has any of these activations a
+// division's long way, which the zeros beyond a tile's rows took.  Measured, 115 x 272 x 224 with gelu_tanh 8.9 -> 5.6 us, with rows of
+// 273 13.3 -> 6.1 us (without an activation 4.3 and 4.6).
+template <typename Out, int N>
+__device__ __forceinline__ void activate_all(int act, float4 (&v)[N]) {
+  auto each = [&](auto code) {
+    constexpr int ACT = decltype(code)::value;
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = make_float4(mx_activate<ACT, Out>(v[i].x), mx_activate<ACT, Out>(v[i].y), mx_activate<ACT, Out>(v[i].z), mx_activate<ACT, Out>(v[i].w));
+  };
+  switch (act) {
+    case APPROXIFER_ACT_RELU: return each(std::integral_constant<int, APPROXIFER_ACT_RELU>{});
+    case APPROXIFER_ACT_GELU: return each(std::integral_constant<int, APPROXIFER_ACT_GELU>{});
+    case APPROXIFER_ACT_GELU_TANH: return each(std::integral_constant<int, APPROXIFER_ACT_GELU_TANH>{});
+    case APPROXIFER_ACT_SILU: return each(std::integral_constant<int, APPROXIFER_ACT_SILU>{});
+    default: return;
+  }
+}
+
 template <int BN, bool SWAP, typename Out, Kind KIND>
 __global__ void __launch_bounds__(threads_of(KIND), 1) linear_tile_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_constant__ CUtensorMap cols_map,
                                                                const __grid_constant__ CUtensorMap row_scales, const __grid_constant__ CUtensorMap col_scales,
@@ -320,13 +340,21 @@ __global__ void __launch_bounds__(threads_of(KIND), 1) linear_tile_kernel(const 
           }
         }
       }
+      if constexpr (KIND != kBf16) {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) v[i] = make_float4(v[i].x + b.x, v[i].y + b.y, v[i].z + b.z, v[i].w + b.w);
+        activate_all<Out>(a.activation, v);
+      }
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) {
         const int mi = m + i * warps * kSide;
         if (mi >= m_to) continue;
-        float4 z = make_float4(v[i].x + b.x, v[i].y + b.y, v[i].z + b.z, v[i].w + b.w);
-        if (a.activation != APPROXIFER_ACT_NONE)
-          z = make_float4(activate<Out>(a.activation, z.x), activate<Out>(a.activation, z.y), activate<Out>(a.activation, z.z), activate<Out>(a.activation, z.w));
+        float4 z = v[i];
+        if constexpr (KIND == kBf16) {
+          z = make_float4(v[i].x + b.x, v[i].y + b.y, v[i].z + b.z, v[i].w + b.w);
+          if (a.activation != APPROXIFER_ACT_NONE)
+            z = make_float4(activate<Out>(a.activation, z.x), activate<Out>(a.activation, z.y), activate<Out>(a.activation, z.z), activate<Out>(a.activation, z.w));
+        }
         write4<Out>(Y + (int64_t)(m0 + mi) * a.y_rstride, make_float4(z.x + r[i].x, z.y + r[i].y, z.z + r[i].z, z.w + r[i].w), a.vec, count);
       }
     }

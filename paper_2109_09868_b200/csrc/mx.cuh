@@ -23,7 +23,7 @@ __device__ __forceinline__ float mx_inverse(uint32_t byte) { return __uint_as_fl
 // The value of a scale.
 __device__ __forceinline__ float mx_value(uint32_t byte) { return __uint_as_float(byte == 255 ? 0x7fffffffu : byte == 0 ? 0x00400000u : byte << 23); }
 
-// The activations of the 4-bit products.  Their epilogues have some 3 us a tile before the next one's products are over: where
+// The activations of the 4-bit products.  The pair kernel's epilogues have some 3 us a tile before the next one's products are over: where
 // bfloat16 is what is written (it shows 2^-8), the special-function unit's reciprocal (2^-22) takes the place of a division, and
 // of gelu's erf a polynomial times an exponential (Abramowitz and Stegun 7.1.26: within 1.5e-7).  8,192 x 16,384 x 256 with
 // gelu 200 -> 140 us, with gelu_tanh 126 us, with none 84 us.
@@ -45,6 +45,9 @@ __device__ __forceinline__ float mx_activate(float x) {
     const float h = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 0.5307027145f, -0.7265760135f), 0.7107068705f), -0.142248368f), 0.127414796f) * pow2(-0.7213475204f * x * x);
     return x * (x >= 0.f ? 1.f - h : h);  // (a factor: infinity stays)
   }
+  // (fp32: a division of two units' error.  It has no long way, which a correctly rounded one takes for zero and what overflows.)
+  if constexpr (ACT == APPROXIFER_ACT_SILU) return __fdividef(x, 1.f + expf(-x));
+  if constexpr (ACT == APPROXIFER_ACT_GELU_TANH) return __fdividef(x, 1.f + expf(-1.5957691f * (x + 0.044715f * x * x * x)));
   return activate<ACT, Out>(x);
 }
 
