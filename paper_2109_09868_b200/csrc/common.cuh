@@ -4,6 +4,7 @@
 
 #include <atomic>
 #include <cstdint>
+#include <mutex>
 
 #include "tables.h"
 
@@ -137,12 +138,16 @@ struct DeviceInfo {
 cudaError_t current_device_info(const DeviceInfo** out);
 
 // Raises a kernel's dynamic shared-memory limit to `bytes` on device `dev` unless an earlier call already
-// did (one cache per kernel: instantiate with the kernel's own tag type).
+// did (one cache per kernel: instantiate with the kernel's own tag type).  The limit is only ever raised: of two threads that ask
+// for different sizes, one after the other sets it and records what it has set.
 template <typename KernelTag, typename Kernel>
 cudaError_t ensure_dynamic_smem(Kernel kernel, int dev, int bytes) {
   static std::atomic<int> granted[kMaxDevices];
+  static std::mutex raising;
   if (dev < 0 || dev >= kMaxDevices) return cudaErrorInvalidDevice;
   if (bytes <= 48 * 1024 || bytes <= granted[dev].load(std::memory_order_acquire)) return cudaSuccess;
+  const std::lock_guard<std::mutex> hold(raising);
+  if (bytes <= granted[dev].load(std::memory_order_relaxed)) return cudaSuccess;
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
   if (e == cudaSuccess) granted[dev].store(bytes, std::memory_order_release);
   return e;
