@@ -580,8 +580,10 @@ int64_t approxifer_mx_linear_workspace(const approxifer_mx_linear_args* args);
  *     out = sum_j softmax_j(scale q.k_j) v_j   over all prefix_len positions of the prefix and the own positions j <= p.
  * Position j of the prefix lies in page prefix_table[j / page_size], row j % page_size.  A page outside 0 .. num_pages-1, or beyond
  * its table, holds nothing.  A row with p < 0 (kv_len[b] shorter than the queries) is zero, as is one that sees nothing.
- * prefix_len = 0 is allowed.  The layouts that approxifer_attention runs on the tensor cores are run so here, in two steps that
- * meet in own.workspace, which has to hold approxifer_prefix_attention_workspace bytes; others run an element-wise kernel.
+ * prefix_len = 0 is allowed.  The layouts that approxifer_attention runs on the tensor cores are run so here: in one launch, in which
+ * each sequence reads a short prefix for itself, or in two or three that meet in own.workspace, which has to hold
+ * approxifer_prefix_attention_workspace bytes.  (Single tokens, where prompts could not have their layout: each sequence reads the prefix for
+ * itself.)  Others run an element-wise kernel.  The weights are rounded to bfloat16 as there.
  */
 typedef struct approxifer_prefix_attention_args {
   approxifer_attention_args own;

@@ -135,8 +135,10 @@ __global__ void __launch_bounds__(128) prefix_join_kernel(const __grid_constant_
   }
 }
 
-// Whether the call runs on the tensor cores: what the kernel over the prefix takes, the ones over the own keys take too.
-bool on_tensor_cores(const approxifer_prefix_attention_args& p) {
+// Whether the kernel over the prefix takes the call: the ones over the own keys then take it too.  (Of single tokens attention_token.cu
+// takes more: pages of any size, queries and outputs at 4 bytes, any number of query heads to a key head.  Those walk the prefix each for
+// itself: 16 behind 4,096 in pages of 24, 32 heads on 8 of 128, 65 us, where the element-wise kernel takes 3.9 ms.)
+bool tiles_take(const approxifer_prefix_attention_args& p) {
   approxifer_attention_args a = p.own;
   if (!attention_tile_eligible(a)) return false;
   a.table_pages = p.prefix_pages;
@@ -147,7 +149,7 @@ int64_t positions_of(const approxifer_prefix_attention_args& p) { return p.prefi
 bool has_prefix(const approxifer_prefix_attention_args& p) { return positions_of(p) > 0; }
 // Whether the sequences, or their query blocks, walk the prefix each for itself.
 bool through(const approxifer_prefix_attention_args& p, const DeviceInfo& dev) {
-  if (attention_token_eligible(p.own)) return attention_token_through_wanted(p.own, positions_of(p));
+  if (attention_token_eligible(p.own)) return !tiles_take(p) || attention_token_through_wanted(p.own, positions_of(p));
   return positions_of(p) + p.own.table_pages * p.own.page_size < (1LL << 30) && attention_tile_through_wanted(p, prefix_parts(p, dev), dev.sms);
 }
 
@@ -167,8 +169,8 @@ PrefixParts parts_of(const approxifer_prefix_attention_args& p, const DeviceInfo
 
 int64_t prefix_attention_workspace(const approxifer_prefix_attention_args& p) {
   const DeviceInfo* dev;
-  if (!on_tensor_cores(p) || current_device_info(&dev) != cudaSuccess) return 0;
   const bool token = attention_token_eligible(p.own);
+  if (!(token || tiles_take(p)) || current_device_info(&dev) != cudaSuccess) return 0;
   if (!has_prefix(p)) return token ? attention_token_workspace(p.own) : 0;
   if (through(p, *dev)) return 0;
   int64_t bytes;
@@ -177,7 +179,7 @@ int64_t prefix_attention_workspace(const approxifer_prefix_attention_args& p) {
 }
 
 cudaError_t launch_prefix_attention(const approxifer_prefix_attention_args& p, cudaStream_t stream) {
-  if (on_tensor_cores(p)) {
+  if (attention_token_eligible(p.own) || tiles_take(p)) {
     if (!has_prefix(p)) return launch_attention(p.own, stream);
     const DeviceInfo* dev;
     cudaError_t e = current_device_info(&dev);
