@@ -14,7 +14,11 @@ namespace approxifer {
 // Launches a kernel of these operators: as a cluster of `cluster` CTAs (1: none), and so that its CTAs may start, set up
 // their barriers and tensor memory and wait in wait_for_inputs() while the kernel before it on the stream still drains.
 // (A kernel so launched calls wait_for_inputs() in every thread that goes on to read or write global memory, and in at
-// least one of every CTA: what follows it on the stream may count on its end alone.)
+// least one of every CTA: what follows it on the stream may count on its end alone.
+// One exception: the kernels that follow the kernel over a common prefix within a call (prefix.cu) read the call's inputs, and write
+// places of the workspace that the kernel over the prefix does not use, before they wait.  They may, because that kernel lets the next one start
+// only after its own wait, in all its CTAs: whatever came before the call has ended by then.  What it leaves, and the output, they touch
+// only after theirs, and they still wait in every CTA.)
 template <typename... Params, typename... Args>
 cudaError_t launch_kernel(void (*kernel)(Params...), dim3 grid, dim3 block, int smem, int cluster, cudaStream_t stream, Args&&... args) {
   cudaLaunchConfig_t cfg = {};

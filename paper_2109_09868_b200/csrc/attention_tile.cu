@@ -337,7 +337,9 @@ __global__ void __launch_bounds__(threads_of(DP), 3 - tiles_of(DP))
   __syncthreads();
   tmem_fence_after();
   const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
-  let_next_start();  // not before: the tensor memory is held
+  // Not before the tensor memory is held; nor, over a prefix, before the wait above: the next kernel then reads the call's inputs, and
+  // writes its part of the workspace, without a wait of its own.
+  let_next_start();
 
   // The softmax warps keep scores in registers; the four others give up theirs (two tiles: 512 x 104 + 128 x 64 = 640 x 96
   // registers at the launch; one: 256 x 96 + 128 x 48 = 384 x 80).
