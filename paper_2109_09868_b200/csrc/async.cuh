@@ -58,7 +58,8 @@ cudaError_t make_tensor_map(CUtensorMap* map, const void* base, int rank, const 
 cudaError_t make_scales_map(CUtensorMap* map, const void* base, int64_t row_blocks, int64_t col_blocks, int rows);
 
 // Tensor map of an output [rows][cols] (fp32 or bfloat16) written in pieces of 32 rows of 64 bytes, taken from shared memory with the
-// 64-byte swizzle.  Elements outside the array are not written.
+// 64-byte swizzle.  Rows outside the array are not written, nor are columns, but those by whole 16 bytes only: of the 16 bytes in which a
+// row ends all are.
 cudaError_t make_store_map(CUtensorMap* map, void* base, bool f32, int64_t rows, int64_t cols, int64_t rstride);
 
 #ifdef __CUDACC__

@@ -50,7 +50,7 @@ struct PairArgs {
   const void* R;
   void* Y;
   int64_t r_rstride, y_rstride;
-  int32_t bias_whole, whole;      // the bias; Y and R: 16 bytes at a time, Y by tensor-map stores
+  int32_t bias_whole, whole;      // the bias; Y and R: 16 bytes at a time, Y by tensor-map stores but for the end of ragged rows
 };
 
 // Tiles in bands of kGroupM rows of tiles, down a band's columns of tiles.
@@ -99,7 +99,9 @@ __device__ __forceinline__ void finish(const PairArgs& a, const CUtensorMap* y_m
 #pragma unroll
   for (int i = 0; i < N; ++i) z[i] = mx_activate<ACT, Out>(z[i]);
   auto place16 = [&](int row, int i) { return room + row * 64 + ((i ^ ((row >> 1) & 3)) << 4); };  // the i-th 16 bytes of a row (the 64-byte swizzle)
-  if (a.whole) {
+  // (A tensor-map store leaves out what lies beyond a row's end by whole 16 bytes, no less: where the row ends within 16, its last piece
+  // goes the other way.)
+  if (a.whole && (left >= N || a.N % (16 / (int)sizeof(Out)) == 0)) {
     if (a.R && m < a.M) add_row<N, Out>(static_cast<const Out*>(a.R) + (int64_t)m * a.r_rstride + n, true, left, z);
     if (lane == 0) stores_have_read();  // the last piece has left
     __syncwarp();
@@ -119,6 +121,7 @@ __device__ __forceinline__ void finish(const PairArgs& a, const CUtensorMap* y_m
   }
   // Rows that are not whole 16 bytes: sixteen columns at a time through shared memory in fp32, so that neighbouring lanes write, and
   // read of the residual, neighbours of a row.
+  if (a.whole && lane == 0) stores_have_read();  // the last piece has left
 #pragma unroll
   for (int c = 0; c < N; c += 16) {
     __syncwarp();
