@@ -486,7 +486,8 @@ int64_t approxifer_attention_workspace(const approxifer_attention_args* args);
  *   X     [T][N]; with before = NONE it is not written and may be NULL
  * R and R_out are of stream_type; Y, gate, weights, biases and X of `type`.  R_out may be R, and X may be Y (same strides); else
  * outputs overlap nothing.  T = 0 is a valid no-op; 1 <= N <= 16384.  Rows of whole 16 bytes (N a multiple of 8, strides and bases
- * of 16 bytes) are read and written 16 bytes at a time, others element by element.
+ * of 16 bytes) are read and written four elements at a time; so are rows that begin anywhere, where those of all arrays lie alike (the
+ * same number of elements from a multiple of four; weights and biases of bfloat16 at 8 bytes); others go element by element.
  */
 typedef struct approxifer_block_norm_args {
   int64_t T;

@@ -8,6 +8,10 @@
 //   P = 2^(S' - m)  two threads share a row, 64 scores each in registers; P (bfloat16) goes to tensor memory
 //   O += P V        P from tensor memory, V from shared memory as it lies in the cache (MN-major); O fp32 in tensor memory
 //
+// P is rounded to bfloat16 because the instruction takes both operands in one type and V is held in bfloat16 (in 16 bits more, as a second
+// product of what the rounding leaves over, O would be twice the work).  A weight is then off by up to 2^-8 of itself, the sum of the weights
+// is of them as they were: outputs err by 0.20 to 0.23 % (root mean square) where their own rounding alone makes 0.17 %.
+//
 // What a tile's rows wait for is the chain S -> softmax -> P -> O, not any one unit.  Up to D = 64 tensor memory holds S, P
 // and O of a tile side by side for two CTAs on an SM: S is free again as soon as it has been loaded into registers, and the
 // next one is formed while the softmax works on the last.  Beyond, P lies over S, and the two tiles of a CTA take turns: the

@@ -6,7 +6,8 @@
 // pipeline of its own: it copies chunks into its private ring (16-byte asynchronous copies, pages looked up one chunk ahead,
 // positions that are not there filled with zeros) and reduces the oldest with mma.m16n8k16 (the query heads are the 16
 // rows; a tcgen05 tile of 128 rows would be seven eighths padding, and the tensor pipes idle either way), keeping the
-// running maximum and sum of the softmax and the output in fp32 registers.  Two ways to deal the chunks:
+// running maximum and sum of the softmax and the output in fp32 registers (the weights in bfloat16, as in attention_tile.cu and
+// for its reason: the instruction's operands have one type).  Two ways to deal the chunks:
 //
 //   cluster form   a cluster of up to 8 CTAs takes one unit; its warps' results meet in the cluster's shared memory.  One
 //                  launch, no workspace: the form for small calls.

@@ -5,10 +5,11 @@
 // sum o of its values; joined, out = sum 2^(m_i - m) o_i / sum 2^(m_i - m) l_i.  The kernel over the prefix (attention_tile.cu) has the
 // tokens of all sequences side by side as the rows of its tiles, so that the prefix's keys and values are read once for them, and cuts
 // the prefix so that its CTAs fill the GPU; the kernels over the own keys (attention_token.cu for single tokens, attention_tile.cu) start
-// while its last CTAs run and need what it left only at their end.  A short prefix, or one of few sequences, each sequence walks itself.
+// while its last CTAs run and need what it left only at their end.  A short prefix, or one of few sequences, each sequence walks itself;
+// so do single tokens in layouts that the kernel over the prefix does not take.
 //
 // Measured: 96 single tokens behind 32,768, 32 heads on 8 of 128, up to 700 own keys, 112 to 119 us (under a profiler the prefix 69, own
-// keys 41, joining 13); eight prompts of 100 to 300 tokens behind 4,096 139 to 144 us (119, 51 before its last step); five single tokens
+// keys 41, joining 13); eight prompts of 100 to 300 tokens behind 4,096 139 to 145 us; five single tokens
 // behind 1,003, heads of 64, 7.1 to 8.6 us.
 #include "async.cuh"
 #include "prefix.cuh"

@@ -130,7 +130,7 @@ def approxifer_prefix_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache:
                                 block_table: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor, max_q: int, scale: Optional[float] = None,
                                 out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """As approxifer_attention, for sequences that begin with the same prefix of `prefix_len` positions, which lies in the pages
-    prefix_table [pages] int32 once and is read once for all.  block_table and kv_len say of each sequence what follows the
+    prefix_table [pages] int32 once and, but in small calls, is read once for all.  block_table and kv_len say of each sequence what follows the
     prefix; every query sees the prefix and its sequence's own positions up to itself.  workspace: CUDA memory (allocated
     where it is not given)."""
     args = (q, k_cache, v_cache, prefix_table, prefix_len, block_table, q_start, kv_len, max_q, scale, out, workspace)
